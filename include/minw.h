@@ -546,6 +546,143 @@ MINW_API minw_status minw_conv_first(const float *x, int32_t B, int32_t C, int32
                             uint32_t *planes_out, float *y_out, void *stream);
 
 /* ---------------------------------------------------------------------- */
+/* Heads: group norm, clipped updates, 4-bit weights                       */
+/* (interface additions: the paper normalises by given BN maps, steps      */
+/* without a norm and quantizes to 1-3 bits)                               */
+/* ---------------------------------------------------------------------- */
+
+/* Type of a tensor's values, and activations. */
+enum { MINW_F32 = 0, MINW_BF16 = 1 };
+enum {
+    MINW_ACT_NONE = 0,
+    MINW_ACT_HARDTANH = 1,    /* min(1, max(-1, z)); its gradient passes on |z| <= 1 (Eq. activation) */
+    MINW_ACT_RELU = 2,        /* max(0, z); its gradient passes on z > 0 */
+    MINW_ACT_SILU = 3         /* z / (1 + e^-z) */
+};
+
+/* Group norm with an activation, channels last: x [B][P][C] (P pixels, rows
+ * of ldx >= C elements per pixel, images P ldx elements apart), the C
+ * channels in G groups of C / G.  Per image and group, over its n = P C / G
+ * values:
+ *   mean = sum x / n,  rstd = 1 / sqrt(sum (x - mean)^2 / n + eps)
+ *   z = gamma[c] (x - mean) rstd + beta[c],  y = act(z)
+ * in fp32 whatever the types (bf16 outputs round once, to nearest even); the
+ * variance is summed about the mean.  y: rows of ldy >= C elements; elements
+ * past C of a row are neither read nor written.  y may be x when types and
+ * row lengths are the same, and may not overlap it otherwise.  gamma, beta
+ * (nullable: 1 and 0): fp32 [C].  mean, rstd (nullable): fp32 [B][G], what
+ * the backward needs.  A NaN or infinity makes its own group's outputs NaN,
+ * no other's.
+ * x, y are aligned to their elements; rows on 16-byte boundaries (8 for bf16
+ * rows) run wider loads.  workspace: device scratch of
+ * minw_group_norm_workspace_bytes (16-byte aligned, contents meaningless
+ * before and after; null where that is 0); calls that share one must not run
+ * concurrently.  B = 0 does nothing.  Errors: MINW_EINVAL (null x or y, B < 0,
+ * P < 1, C < 1, G < 1 or not dividing C, short rows, unknown type or act,
+ * eps negative or not finite, misaligned or short workspace),
+ * MINW_EUNSUPPORTED (P >= 2^30, or more blocks than a grid holds). */
+MINW_API size_t minw_group_norm_workspace_bytes(int32_t B, int64_t P, int32_t C, int32_t G, int32_t backward);
+MINW_API minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamma,
+                                     const float *beta, int32_t B, int64_t P, int32_t C, int32_t G, float eps,
+                                     int32_t act, void *y, int32_t y_type, int64_t ldy, float *mean, float *rstd,
+                                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its backward from x, the saved mean and rstd, and dy = dL/dy (rows of lddy
+ * elements): with xh = (x - mean) rstd, dz = dy act'(gamma xh + beta),
+ *   dbeta[c] = sum_{b,p} dz,  dgamma[c] = sum_{b,p} dz xh
+ *   dx = rstd (gamma dz - sum_g(gamma dz) / n - xh sum_g(gamma dz xh) / n)
+ * dx has x's type, rows of lddx elements, and may be x or dy (same type and
+ * row length).  dgamma, dbeta (nullable): fp32 [C].  All sums are fp32 in a
+ * fixed order (the same bits on every call).  B = 0 writes zeros to dgamma
+ * and dbeta.  workspace and errors as the forward (backward = 1). */
+MINW_API minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx, const void *dy,
+                                              int32_t dy_type, int64_t lddy, const float *gamma, const float *beta,
+                                              const float *mean, const float *rstd, int32_t B, int64_t P, int32_t C,
+                                              int32_t G, int32_t act, void *dx, int64_t lddx, float *dgamma,
+                                              float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/* One tensor of a list (host struct): n values of type at data (device,
+ * aligned to its elements; n = 0 is allowed).  limit: a weight tensor's clip
+ * (minw_sgd_clip_norm), 1 for Algorithm 1's, infinity for none. */
+typedef struct {
+    void *data;
+    int64_t n;
+    int32_t type;
+    float limit;
+} minw_tensor;
+
+/* Global gradient norm: *norm (device) = sqrt(sum over all tensors of g^2),
+ * squares summed in fp32 within a block of at most 32768 values and in fp64
+ * across blocks; a block whose squares leave fp32's range is summed again in
+ * fp64, so the norm is right wherever it is an fp32 number.  Infinite
+ * or NaN gradients give an infinite or NaN norm.  grads: host array, read
+ * during the call.  The sums' order is fixed by the lengths (the same bits
+ * on every call).  workspace: device scratch of
+ * minw_grad_workspace_bytes(count), 16-byte aligned, contents meaningless
+ * before and after.  count = 0 writes 0.
+ * Errors: MINW_EINVAL (count < 0, null grads, norm or workspace, a tensor with
+ * n < 0, null data with n > 0, unknown type, misaligned data; short
+ * workspace), MINW_EUNSUPPORTED (2^46 values or more). */
+MINW_API size_t minw_grad_workspace_bytes(int32_t count);
+MINW_API minw_status minw_grad_norm(const minw_tensor *grads, int32_t count, float *norm, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* Clipping by the global norm: out_t = k g_t with k = max_norm / norm where
+ * norm > max_norm, else 1 (and the norm as minw_grad_norm).  Where the norm
+ * is not finite, out_t = g_t: the caller reads the norm and skips the step.
+ * out: host array of tensors of grads' lengths and types; each may be its
+ * gradient (clipped in place: nothing is written where k = 1) and may overlap
+ * no other.  max_norm > 0, finite.  Errors as minw_grad_norm. */
+MINW_API minw_status minw_grad_clip(const minw_tensor *grads, const minw_tensor *out, int32_t count, float max_norm,
+                                    float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The update of Algorithm 1 (minw_sgd_clip) on all tensors of a network with
+ * gradients clipped by their global norm:
+ *   w = min(limit, max(-limit, fmaf(-lr, k g, w)))
+ * in fp32 (weights fp32 or bf16; bf16 weights round once), limit per weight
+ * tensor.  Where the norm is not finite no weight changes.  Errors as
+ * minw_grad_clip; limit >= 0, lr finite. */
+MINW_API minw_status minw_sgd_clip_norm(const minw_tensor *weights, const minw_tensor *grads, int32_t count,
+                                        float max_norm, float lr, float *norm, void *workspace,
+                                        size_t workspace_bytes, void *stream);
+
+/* "w4" layout: weights [O][K] as 4-bit codes with one bf16 scale per row and
+ * group of `group` consecutive values (32, 64, 128 or a larger multiple of
+ * 128): w = (code - 8) scale, code in 0..15.  codes (16-byte aligned): rows
+ * of 64 ceil(K / 128) bytes; each 64 bytes hold 128 values as 16
+ * little-endian 32-bit words, word 4 t + j (t, j in 0..3) the values
+ * 32 j + 8 t + i (i in 0..7), value i in nibble i / 2 + 4 (i % 2).  Values
+ * past K have code 8 (zero).  scales: bf16 [O][ceil(K / group)].
+ *
+ * minw_pack_w4 makes them from w [O][K] (MINW_F32 or MINW_BF16, dense).
+ * q NULL: scale = bf16(max |w| / 7) of the group (fp32 division, both
+ *   roundings to nearest even), code = 8 + rint(w / scale) kept in 1..15; a
+ *   group whose scale is 0 or not finite has codes 8.
+ * q given (host): the levels of the quantizer h in integer units (Eq. sign /
+ *   tnn / qnn at w channel_scale[o], or w q->scale when channel_scale is
+ *   null), as minw_pack_weight_bf16 writes them, with scales 1: the
+ *   weight-only layer of 1-3 bits for minw_w4_matvec.
+ * Errors: MINW_EINVAL (null pointers, sizes < 1, group, type, q, alignment),
+ * MINW_EUNSUPPORTED (sizes past 2^28). */
+MINW_API minw_status minw_pack_w4(const void *w, int32_t type, int32_t O, int32_t K, int32_t group,
+                                  const minw_quant *q, const float *channel_scale, uint8_t *codes, uint16_t *scales,
+                                  void *stream);
+
+/* Products of a few vectors with w4 weights: x [T][K] (rows of ldx elements),
+ *   acc[t][o] = sum over k of x[t][k] w[o][k]     (fp32 sums; fp32 x enters as three bf16 parts, exactly)
+ *   y[t][o] = act(fmaf(acc, scale[o], shift[o]))  (nullable: 1 and 0; as minw_conv2d_bf16's epilogue)
+ * y: rows of ldy elements, fp32 or bf16 (rounded once); may not overlap x.
+ * The weights are read once for up to 32 bf16 or 10 fp32 vectors and again
+ * for each further such set: made for a token or a few.  T = 0 does nothing.
+ * The same bits on every call.  Errors: MINW_EINVAL (null pointers, T < 0,
+ * O or K < 1, group, types, act, short rows, alignment: codes 16 bytes, the
+ * others their elements), MINW_EUNSUPPORTED (sizes past 2^28). */
+MINW_API minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T, const uint8_t *codes,
+                                    const uint16_t *scales, int32_t O, int32_t K, int32_t group, const float *scale,
+                                    const float *shift, int32_t act, void *y, int32_t y_type, int64_t ldy,
+                                    void *stream);
+
+/* ---------------------------------------------------------------------- */
 /* Whole-network forward (Algorithm 1, inference branch)                   */
 /* ---------------------------------------------------------------------- */
 

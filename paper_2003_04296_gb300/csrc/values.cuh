@@ -1,0 +1,91 @@
+// values.cuh -- vectors of fp32 or bf16 values as they lie in memory, and the
+// activations of the group norm and of the 4-bit products.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "common.cuh"
+
+namespace minw {
+
+// V consecutive values of type T (float, or uint16_t holding bf16 bits), one load or store of up to 16 bytes each.
+// The address is a multiple of the load's size.
+template <typename T, int V>
+struct Vec {
+    static constexpr int BYTES = V * (int)sizeof(T);
+    static constexpr int WORDS = BYTES < 4 ? 1 : BYTES / 4;
+    uint32_t w[WORDS];
+
+    __device__ __forceinline__ void load(const T *p) {
+        if constexpr (BYTES == 2) {
+            w[0] = *reinterpret_cast<const uint16_t *>(p);
+        } else if constexpr (BYTES == 4) {
+            w[0] = *reinterpret_cast<const uint32_t *>(p);
+        } else if constexpr (BYTES == 8) {
+            const uint2 v = *reinterpret_cast<const uint2 *>(p);
+            w[0] = v.x; w[1] = v.y;
+        } else {
+#pragma unroll
+            for (int k = 0; k < WORDS / 4; ++k) {
+                const uint4 v = reinterpret_cast<const uint4 *>(p)[k];
+                w[4 * k] = v.x; w[4 * k + 1] = v.y; w[4 * k + 2] = v.z; w[4 * k + 3] = v.w;
+            }
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const {
+        if constexpr (BYTES == 2) {
+            *reinterpret_cast<uint16_t *>(p) = (uint16_t)w[0];
+        } else if constexpr (BYTES == 4) {
+            *reinterpret_cast<uint32_t *>(p) = w[0];
+        } else if constexpr (BYTES == 8) {
+            *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < WORDS / 4; ++k)
+                reinterpret_cast<uint4 *>(p)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
+    }
+    // all V values at once: bf16 rounds to nearest even, two to a conversion
+    __device__ __forceinline__ void set(const float *v) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) w[i] = __float_as_uint(v[i]);
+        } else if constexpr (V == 1) {
+            w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[i], v[i + 1]);
+                w[i >> 1] = *reinterpret_cast<const uint32_t *>(&b);
+            }
+        }
+    }
+};
+
+// 1 / (1 + e^-z): tends to 0 and 1 at both ends (e^-z = infinity gives 0).
+__device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+
+// y = act(z); a NaN stays one.
+__device__ __forceinline__ float act_value(float z, int act) {
+    if (act == MINW_ACT_HARDTANH) return z > 1.0f ? 1.0f : z < -1.0f ? -1.0f : z;
+    if (act == MINW_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (act == MINW_ACT_SILU) return z * sigmoidf_(z);
+    return z;
+}
+
+// dy act'(z).  HardTanh passes the gradient on |z| <= 1 (Eq. activation's mask), ReLU on z > 0.
+__device__ __forceinline__ float act_grad(float z, float dy, int act) {
+    if (act == MINW_ACT_HARDTANH) return fabsf(z) <= 1.0f ? dy : 0.0f;
+    if (act == MINW_ACT_RELU) return z > 0.0f ? dy : 0.0f;
+    if (act == MINW_ACT_SILU) {
+        const float s = sigmoidf_(z);
+        return dy * (s * fmaf(z, 1.0f - s, 1.0f));
+    }
+    return dy;
+}
+
+}  // namespace minw

@@ -7,6 +7,7 @@ kernels; there is no fallback of any kind.  torch provides device memory and
 streams.
 """
 import ctypes
+import math
 import os
 
 import torch
@@ -20,6 +21,8 @@ VARIANT_AUTO, VARIANT_POPC, VARIANT_TC, VARIANT_TC_E4M3, VARIANT_TC_E2M1, VARIAN
 VARIANT_TC_E2M1_N128 = 6
 CODES_E4M3, CODES_E2M1 = 0, 1
 LAYER_CONV, LAYER_FC = 0, 1
+F32, BF16 = 0, 1
+ACT_NONE, ACT_HARDTANH, ACT_RELU, ACT_SILU = range(4)
 
 
 class MinwError(RuntimeError):
@@ -55,6 +58,10 @@ class PipeRates(ctypes.Structure):
                 ("bmma_b1_mac_per_s", ctypes.c_double), ("imma_s8_mac_per_s", ctypes.c_double),
                 ("tc_e4m3_flop_per_s", ctypes.c_double * 2), ("tc_e2m1_flop_per_s", ctypes.c_double * 2),
                 ("tc_bf16_flop_per_s", ctypes.c_double * 2), ("tma_box_cycles", ctypes.c_double)]
+
+
+class Tensor(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("limit", ctypes.c_float)]
 
 
 class LayerDesc(ctypes.Structure):
@@ -168,6 +175,18 @@ SIGNATURES = {
                                      ctypes.c_size_t, _P]),
     "minw_fc_codes_noalloc": (ctypes.c_int, [_P, _I32, _I32, _I32, _P, _I32, _I32, _P, _P, _QP, _P, _P, _P, _P,
                                              _P]),
+    "minw_group_norm_workspace_bytes": (ctypes.c_size_t, [_I32, _I64, _I32, _I32, _I32]),
+    "minw_group_norm": (ctypes.c_int, [_P, _I32, _I64, _P, _P, _I32, _I64, _I32, _I32, _F, _I32, _P, _I32, _I64, _P, _P,
+                                       _P, ctypes.c_size_t, _P]),
+    "minw_group_norm_backward": (ctypes.c_int, [_P, _I32, _I64, _P, _I32, _I64, _P, _P, _P, _P, _I32, _I64, _I32, _I32,
+                                                _I32, _P, _I64, _P, _P, _P, ctypes.c_size_t, _P]),
+    "minw_grad_workspace_bytes": (ctypes.c_size_t, [_I32]),
+    "minw_grad_norm": (ctypes.c_int, [_P, _I32, _P, _P, ctypes.c_size_t, _P]),
+    "minw_grad_clip": (ctypes.c_int, [_P, _P, _I32, _F, _P, _P, ctypes.c_size_t, _P]),
+    "minw_sgd_clip_norm": (ctypes.c_int, [_P, _P, _I32, _F, _F, _P, _P, ctypes.c_size_t, _P]),
+    "minw_pack_w4": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _QP, _P, _P, _P, _P]),
+    "minw_w4_matvec": (ctypes.c_int, [_P, _I32, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _I32, _P, _I32, _I64,
+                                      _P]),
     "minw_net_create": (ctypes.c_int, [ctypes.POINTER(LayerDesc), _I32, _I32, _I32, _P,
                                        ctypes.POINTER(ctypes.c_void_p)]),
     "minw_resnet18_create": (ctypes.c_int, [ctypes.POINTER(ResNet18Desc), _I32, _P,
@@ -245,6 +264,53 @@ def _host_ptr(a):
 def _stream(stream):
     s = stream if stream is not None else torch.cuda.current_stream()
     return ctypes.c_void_p(s.cuda_stream)
+
+
+_VALUE_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _value_type(t):
+    try:
+        return _VALUE_TYPES[t.dtype]
+    except KeyError:
+        raise ValueError(f"float32 or bfloat16 expected, got {t.dtype}") from None
+
+
+def _rows(t):
+    """(pointer, row length) of a channels-last tensor [..., C] whose rows lie a fixed number of elements apart (the
+    first C channels of a wider buffer, for instance)."""
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    size, stride = t.shape, t.stride()
+    if t.is_contiguous():
+        return t.data_ptr(), size[-1]
+    if size[-1] != 1 and stride[-1] != 1:
+        raise ValueError("the last dimension has to be contiguous")
+    ld, inner = None, 1                   # row length, rows inside the dimension
+    for n, st in zip(reversed(size[:-1]), reversed(stride[:-1])):
+        if n == 1:
+            continue
+        if ld is None:
+            if st < size[-1]:
+                raise ValueError("rows overlap")
+            ld = st
+        elif st != ld * inner:
+            raise ValueError("rows a fixed number of elements apart expected")
+        inner *= n
+    return t.data_ptr(), size[-1] if ld is None else ld
+
+
+def _f32(t, n, what):
+    """Pointer of a dense fp32 vector of n values (None passes)."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.numel() != n:
+        raise ValueError(f"{what}: {n} float32 values expected")
+    return _ptr(t)
+
+
+def _scratch(workspace):
+    return (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
 
 
 def quant(bits, thr=(0.0, 0.0, 0.0), scale=1.0):
@@ -791,3 +857,143 @@ def layer_descs(net_params, device):
             c, h, w = L["O"], 1, 1
         out.append(d)
     return out
+
+
+# ---------------------------------------------------------------------------
+# heads: group norm, clipped updates, 4-bit weights
+# ---------------------------------------------------------------------------
+
+def minw_group_norm_workspace_bytes(B, P, C, groups, backward=False):
+    return lib().minw_group_norm_workspace_bytes(int(B), int(P), int(C), int(groups), int(bool(backward)))
+
+
+def _image_rows(x, groups):
+    if x.dim() < 2:
+        raise ValueError("[B, ..., C] expected")
+    B, C = x.shape[0], x.shape[-1]
+    return B, math.prod(x.shape[1:-1]), C, int(groups)
+
+
+def minw_group_norm(x, gamma, beta, groups, eps, y, act=ACT_NONE, mean=None, rstd=None, workspace=None, stream=None):
+    """y = act(group norm of x) on channels-last tensors [B, ..., C] (fp32 or bf16, each; rows may be wider than C);
+    gamma, beta fp32 [C] or None; mean, rstd fp32 [B, groups] or None receive the statistics."""
+    B, P, C, G = _image_rows(x, groups)
+    if y.shape != x.shape:
+        raise ValueError("y: x's shape expected")
+    px, ldx = _rows(x)
+    py, ldy = _rows(y)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_group_norm(px, _value_type(x), ldx, _f32(gamma, C, "gamma"), _f32(beta, C, "beta"), B, P, C, G,
+                                 float(eps), int(act), py, _value_type(y), ldy, _f32(mean, B * G, "mean"),
+                                 _f32(rstd, B * G, "rstd"), ws, ws_bytes, _stream(stream)), "minw_group_norm")
+
+
+def minw_group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, dx, dgamma=None, dbeta=None, act=ACT_NONE,
+                             workspace=None, stream=None):
+    """dx (x's type), dgamma, dbeta from dy and the forward's mean and rstd."""
+    B, P, C, G = _image_rows(x, groups)
+    if dy.shape != x.shape or dx.shape != x.shape or dx.dtype != x.dtype:
+        raise ValueError("dy, dx: x's shape expected, and dx its type")
+    px, ldx = _rows(x)
+    pd, ldd = _rows(dy)
+    po, ldo = _rows(dx)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_group_norm_backward(px, _value_type(x), ldx, pd, _value_type(dy), ldd, _f32(gamma, C, "gamma"),
+                                          _f32(beta, C, "beta"), _f32(mean, B * G, "mean"), _f32(rstd, B * G, "rstd"),
+                                          B, P, C, G, int(act), po, ldo, _f32(dgamma, C, "dgamma"),
+                                          _f32(dbeta, C, "dbeta"), ws, ws_bytes, _stream(stream)),
+           "minw_group_norm_backward")
+
+
+class TensorList:
+    """Dense device tensors (fp32 or bf16, any lengths and offsets) as the host array that the calls on lists take;
+    made once for tensors that stay where they are.  limits: the clip of each weight tensor, or one for all (infinity
+    for none).  Holds its tensors."""
+
+    def __init__(self, tensors, limits=float("inf")):
+        self.tensors = list(tensors)
+        n = len(self.tensors)
+        limits = [float(limits)] * n if isinstance(limits, (int, float)) else [float(v) for v in limits]
+        if len(limits) != n:
+            raise ValueError("a limit per tensor expected")
+        self.array = (Tensor * max(1, n))()
+        for e, t, limit in zip(self.array, self.tensors, limits):
+            p = _ptr(t)
+            e.data, e.n, e.type, e.limit = p.value, t.numel(), _value_type(t), limit
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _list(tensors):
+    return tensors if isinstance(tensors, TensorList) else TensorList(tensors)
+
+
+def _pair(a, b):
+    a, b = _list(a), _list(b)
+    if len(a) != len(b):
+        raise ValueError("lists of the same length expected")
+    return a, b
+
+
+def minw_grad_workspace_bytes(count):
+    return lib().minw_grad_workspace_bytes(int(count))
+
+
+def minw_grad_norm(grads, norm, workspace, stream=None):
+    """norm (one fp32 value on the device) = the 2-norm over all tensors of grads (a TensorList, or tensors)."""
+    g = _list(grads)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_grad_norm(g.array, len(g), _f32(norm, 1, "norm"), ws, ws_bytes, _stream(stream)),
+           "minw_grad_norm")
+
+
+def minw_grad_clip(grads, out, max_norm, norm, workspace, stream=None):
+    """out = grads scaled to the norm max_norm where theirs is larger (out may be grads)."""
+    g, o = _pair(grads, out)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_grad_clip(g.array, o.array, len(g), float(max_norm), _f32(norm, 1, "norm"), ws, ws_bytes,
+                                _stream(stream)), "minw_grad_clip")
+
+
+def minw_sgd_clip_norm(weights, grads, max_norm, lr, norm, workspace, stream=None):
+    """weights -= lr times the clipped grads, each kept within its limit (a TensorList's)."""
+    w, g = _pair(weights, grads)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_sgd_clip_norm(w.array, g.array, len(g), float(max_norm), float(lr), _f32(norm, 1, "norm"), ws,
+                                    ws_bytes, _stream(stream)), "minw_sgd_clip_norm")
+
+
+def w4_shapes(O, K, group):
+    """Shapes of the w4 layout of [O][K] weights: (codes uint8, scales bfloat16)."""
+    return (O, (K + 127) // 128 * 64), (O, (K + group - 1) // group)
+
+
+def _w4(codes, scales, O, K, group):
+    if group < 1 or (tuple(codes.shape), tuple(scales.shape)) != w4_shapes(O, K, group):
+        raise ValueError("codes and scales of w4_shapes(O, K, group) expected")
+    if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
+        raise ValueError("codes uint8 and scales bfloat16 expected")
+    return _ptr(codes), _ptr(scales)
+
+
+def minw_pack_w4(w, group, codes, scales, q=None, channel_scale=None, stream=None):
+    """w [O][K] (fp32 or bf16) -> 4-bit codes and group scales; with q, the levels of that quantizer (1-3 bits) in
+    integer units, scales 1."""
+    O, K = w.shape
+    pc, ps = _w4(codes, scales, O, K, int(group))
+    _check(lib().minw_pack_w4(_ptr(w), _value_type(w), O, K, int(group), None if q is None else ctypes.byref(q),
+                              _f32(channel_scale, O, "channel_scale"), pc, ps, _stream(stream)), "minw_pack_w4")
+
+
+def minw_w4_matvec(x, codes, scales, group, y, scale=None, shift=None, act=ACT_NONE, stream=None):
+    """y [T][O] = act(scale (x [T][K] times the w4 weights) + shift); x, y fp32 or bf16, rows may be wider."""
+    (T, K), (Ty, O) = x.shape, y.shape
+    if T != Ty:
+        raise ValueError("x and y: the same number of rows expected")
+    px, ldx = _rows(x)
+    py, ldy = _rows(y)
+    pc, ps = _w4(codes, scales, O, K, int(group))
+    _check(lib().minw_w4_matvec(px, _value_type(x), ldx, T, pc, ps, O, K, int(group), _f32(scale, O, "scale"),
+                                _f32(shift, O, "shift"), int(act), py, _value_type(y), ldy, _stream(stream)),
+           "minw_w4_matvec")
