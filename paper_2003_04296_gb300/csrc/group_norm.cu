@@ -1,84 +1,9 @@
-// group_norm.cu -- group norm with an activation on channels-last rows,
-// forward and backward.
-//
-// Statistics of n values are (count, mean, M2 = sum of squared deviations from
-// that mean), and two sets merge exactly as
-//   mean = (n_a m_a + n_b m_b) / (n_a + n_b),
-//   M2 = M2_a + M2_b + n_a (m_a - mean)^2 + n_b (m_b - mean)^2,
-// so a mean far from zero costs no digits and one pass over the data is
-// enough: a thread takes the mean and M2 of the values it holds, threads,
-// blocks and clusters merge in a fixed order.
-//
-// Both directions are bound by memory: the forward has to read x and write y,
-// the backward to read x and dy and write dx.
-#include <cooperative_groups.h>
-#include <cuda_runtime.h>
-#include <math.h>
-#include <stdint.h>
-
-#include "kernels.cuh"
-#include "values.cuh"
-
-namespace cg = cooperative_groups;
+// group_norm.cu -- forward of the group norm with an activation on
+// channels-last rows (group_norm.cuh: statistics, tiles and plans).
+#include "group_norm.cuh"
 
 namespace minw {
 namespace gn {
-
-constexpr int THREADS = 256;
-
-struct Args {
-    const void *x, *dy;
-    void *y;                       // y, or dx
-    int64_t ldx, lddy, ldy;
-    const float *gamma, *beta;     // nullable
-    const float *mean_in, *rstd_in;
-    float *mean, *rstd;            // forward: saved statistics (nullable)
-    float2 *part;                  // streaming: per image, chunk and channel (mean, M2), or (sum dz, sum dz xh)
-    float2 *stat;                  // streaming: per image and group (mean, rstd), or (s1, s2)
-    float2 *chan;                  // backward: per image and channel (sum dz, sum dz xh)
-    float *dgamma, *dbeta;         // nullable
-    int B, P, C, G, Cg, act;
-    float eps;
-    int chunks, ppc;               // pixel chunks per image, pixels per chunk
-    int L, slabs;                  // lanes (V channels each) of a slab, slabs of a row
-};
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-    return v;
-}
-
-// gamma and beta of channels c .. c + V - 1.
-template <int V>
-__device__ __forceinline__ void load_affine(const Args &a, int c, float *ga, float *be) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        ga[i] = a.gamma ? a.gamma[c + i] : 1.0f;
-        be[i] = a.beta ? a.beta[c + i] : 0.0f;
-    }
-}
-
-// Where a block of the streaming kernels works: image, chunk of its pixels, slab of its channels.
-struct Place {
-    int b, chunk, slab, p0, p1, rows, row, c;
-    bool active;
-};
-template <int V>
-__device__ __forceinline__ Place place(const Args &a, int64_t block) {
-    Place w;
-    w.slab = (int)(block % a.slabs);
-    const int64_t bc = block / a.slabs;
-    w.chunk = (int)(bc % a.chunks);
-    w.b = (int)(bc / a.chunks);
-    w.p0 = w.chunk * a.ppc;
-    w.p1 = min(a.P, w.p0 + a.ppc);
-    w.rows = THREADS / a.L;
-    w.row = (int)threadIdx.x / a.L;
-    w.c = (w.slab * a.L + (int)threadIdx.x % a.L) * V;
-    w.active = w.row < w.rows && w.c < a.C;
-    return w;
-}
 
 // ---------------------------------------------------------------------------
 // Streaming forward: statistics per chunk and channel, merged per group, then
@@ -208,282 +133,176 @@ __global__ void __launch_bounds__(THREADS) apply_kernel(Args a) {
     }
     const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
     TY *y = static_cast<TY *>(a.y) + (int64_t)w.b * a.P * a.ldy + w.c;
-    for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
-        Vec<T, V> v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u * w.rows < w.p1) v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p + u * w.rows >= w.p1) break;
-            float z[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                z[i] = act_value(fmaf((v[u].get(i) - mean[i]) * rstd[i], ga[i], be[i]), a.act);
-            Vec<TY, V> o;
-            o.set(z);
-            o.store(y + (int64_t)(p + u * w.rows) * a.ldy);
-        }
-    }
-}
-
-// ---------------------------------------------------------------------------
-// Streaming backward: the channel sums per chunk, merged per image, then a
-// second pass over x and dy.
-// ---------------------------------------------------------------------------
-
-// Statistics of the V channels at c.
-template <int V>
-__device__ __forceinline__ void load_stats(const Args &a, int b, int c, float *mean, float *rstd) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int64_t g = (int64_t)b * a.G + (c + i) / a.Cg;
-        mean[i] = a.mean_in[g];
-        rstd[i] = a.rstd_in[g];
-    }
-}
-
-template <typename T, typename TD, int V>
-__global__ void __launch_bounds__(THREADS) bwd_sum_kernel(Args a) {
-    pdl_trigger();
-    pdl_wait();
-    constexpr int U = V == 1 ? 8 : 2;
-    __shared__ float2 red[THREADS * V];
-    const Place w = place<V>(a, blockIdx.x);
-    float db[V], dg[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) db[i] = dg[i] = 0.0f;
-    if (w.active) {
-        float ga[V], be[V], mean[V], rstd[V];
-        load_affine<V>(a, w.c, ga, be);
-        load_stats<V>(a, w.b, w.c, mean, rstd);
-        const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
-        const TD *dy = static_cast<const TD *>(a.dy) + (int64_t)w.b * a.P * a.lddy + w.c;
+    with_act(a.act, [&](auto act) {
         for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
             Vec<T, V> v[U];
-            Vec<TD, V> d[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                if (p + u * w.rows < w.p1) {
-                    v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-                    d[u].load(dy + (int64_t)(p + u * w.rows) * a.lddy);
-                }
+                if (p + u * w.rows < w.p1) v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 if (p + u * w.rows >= w.p1) break;
+                float z[V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xh = (v[u].get(i) - mean[i]) * rstd[i];
-                    const float dz = act_grad(fmaf(xh, ga[i], be[i]), d[u].get(i), a.act);
-                    db[i] += dz;
-                    dg[i] = fmaf(dz, xh, dg[i]);
+                for (int i = 0; i < V; ++i)
+                    z[i] = act_value<act.value>(fmaf((v[u].get(i) - mean[i]) * rstd[i], ga[i], be[i]));
+                Vec<TY, V> o;
+                o.set(z);
+                o.store(y + (int64_t)(p + u * w.rows) * a.ldy);
+            }
+        }
+    });
+}
+
+// GPT: groups among a thread's V channels (V / GPT channels of each).
+template <typename T, typename TY, int V, int GPT, int NV>
+__global__ void __launch_bounds__(THREADS) fused_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int W = V / GPT;
+    __shared__ float em[THREADS * GPT], eq[THREADS * GPT];
+    __shared__ float2 cta[MAX_SLAB_GROUPS], all[MAX_SLAB_GROUPS];
+    const Tile w = tile<V>(a);
+    const T *x = static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c;
+    Vec<T, V> v[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < w.n) v[i].load(x + (int64_t)(i * w.rows) * a.ldx);
+
+    // this thread's statistics of each of its groups: n W values
+    const float inv = w.n > 0 ? 1.0f / (float)(w.n * W) : 0.0f;
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) {
+        float s = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < w.n) {
+#pragma unroll
+                for (int k = 0; k < W; ++k) s += v[i].get(g * W + k);
+            }
+        s *= inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < w.n) {
+#pragma unroll
+                for (int k = 0; k < W; ++k) {
+                    const float d = v[i].get(g * W + k) - s;
+                    q = fmaf(d, d, q);
                 }
             }
+        if (w.row < w.rows) {
+            em[(w.row * a.L + w.lane) * GPT + g] = s;
+            eq[(w.row * a.L + w.lane) * GPT + g] = q;
         }
-    }
-    const int W = a.L * V;
-    if (w.row < w.rows) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) red[w.row * W + ((int)threadIdx.x % a.L) * V + i] = make_float2(db[i], dg[i]);
     }
     __syncthreads();
-    for (int e = threadIdx.x; e < W; e += THREADS) {
-        const int c = w.slab * W + e;
-        if (c >= a.C) break;
-        float s0 = 0.0f, s1 = 0.0f;
-        for (int r = 0; r < w.rows; ++r) {
-            s0 += red[r * W + e].x;
-            s1 += red[r * W + e].y;
-        }
-        a.part[((int64_t)w.b * a.chunks + w.chunk) * a.C + c] = make_float2(s0, s1);
-    }
-}
 
-// Block = one image's group: its channels' sums over the chunks, then s1 and s2.
-__global__ void __launch_bounds__(THREADS) bwd_merge_kernel(Args a) {
-    pdl_trigger();
-    pdl_wait();
-    __shared__ float2 red[THREADS / 32];
-    const int b = (int)(blockIdx.x / a.G), g = (int)(blockIdx.x % a.G), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int e = warp; e < a.Cg; e += THREADS / 32) {          // a warp per channel
-        const int c = g * a.Cg + e;
-        float db = 0.0f, dg = 0.0f;
-        for (int k = lane; k < a.chunks; k += 32) {
-            const float2 t = a.part[((int64_t)b * a.chunks + k) * a.C + c];
-            db += t.x;
-            dg += t.y;
+    // a warp per group: the rows x (Cg / W) entries of this block
+    const int groups = a.L * V / a.Cg, per = a.Cg / W, np = w.p1 - w.p0, lane = threadIdx.x & 31;
+    for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {
+        float s = 0.0f;
+        const int entries = min(w.rows, np) * per;
+        for (int e = lane; e < entries; e += 32) {
+            const int r = e / per;
+            s = fmaf((float)((np - r + w.rows - 1) / w.rows), em[r * a.L * GPT + g * per + e % per], s);
         }
-        db = warp_sum(db);
-        dg = warp_sum(dg);
-        if (lane == 0) a.chan[(int64_t)b * a.C + c] = make_float2(db, dg);
-        const float ga = a.gamma ? a.gamma[c] : 1.0f;
-        s1 = fmaf(ga, db, s1);
-        s2 = fmaf(ga, dg, s2);
-    }
-    if (lane == 0) red[warp] = make_float2(s1, s2);
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s1 = s2 = 0.0f;
-        for (int k = 0; k < THREADS / 32; ++k) {
-            s1 += red[k].x;
-            s2 += red[k].y;
+        const float mean = np > 0 ? warp_sum(s) / ((float)np * (float)per) : 0.0f;
+        s = 0.0f;
+        for (int e = lane; e < entries; e += 32) {
+            const int r = e / per, at = r * a.L * GPT + g * per + e % per;
+            const float d = em[at] - mean;
+            s += fmaf(d * d, (float)((np - r + w.rows - 1) / w.rows * W), eq[at]);
         }
-        const float n = (float)a.P * (float)a.Cg;
-        a.stat[blockIdx.x] = make_float2(s1 / n, s2 / n);
+        s = warp_sum(s);
+        if (lane == 0) cta[g] = make_float2(mean, s);
     }
-}
 
-template <typename T, typename TD, int V>
-__global__ void __launch_bounds__(THREADS) bwd_apply_kernel(Args a) {
-    pdl_trigger();
-    pdl_wait();
-    constexpr int U = V == 1 ? 8 : 2;
-    const Place w = place<V>(a, (int64_t)gridDim.x - 1 - blockIdx.x);
-    if (!w.active) return;
-    float ga[V], be[V], mean[V], rstd[V], s1[V], s2[V];
-    load_affine<V>(a, w.c, ga, be);
-    load_stats<V>(a, w.b, w.c, mean, rstd);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
-        s1[i] = t.x;
-        s2[i] = t.y;
-    }
-    const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
-    const TD *dy = static_cast<const TD *>(a.dy) + (int64_t)w.b * a.P * a.lddy + w.c;
-    T *dx = static_cast<T *>(a.y) + (int64_t)w.b * a.P * a.ldy + w.c;
-    for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
-        Vec<T, V> v[U];
-        Vec<TD, V> d[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p + u * w.rows < w.p1) {
-                v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-                d[u].load(dy + (int64_t)(p + u * w.rows) * a.lddy);
+    // the cluster's blocks; the same sums in every block
+    cg::cluster_group cluster = cg::this_cluster();
+    if (a.chunks > 1) cluster.sync();
+    else __syncthreads();
+    for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {
+        float2 t = make_float2(0.0f, 0.0f);
+        float n = 0.0f;
+        if (lane < a.chunks) {
+            t = *(a.chunks > 1 ? cluster.map_shared_rank(&cta[g], lane) : &cta[g]);
+            const int q0 = min(a.P, lane * a.ppc);
+            n = (float)(min(a.P, q0 + a.ppc) - q0) * (float)a.Cg;
+        }
+        const float total = (float)a.P * (float)a.Cg;
+        const float mean = warp_sum(n * t.x) / total;
+        const float d = t.x - mean;
+        const float rstd = 1.0f / sqrtf(warp_sum(n > 0.0f ? fmaf(d * d, n, t.y) : 0.0f) / total + a.eps);
+        if (lane == 0) {
+            all[g] = make_float2(mean, rstd);
+            if (w.rank == 0) {
+                const int64_t at = (int64_t)w.b * a.G + w.slab * groups + g;
+                if (a.mean) a.mean[at] = mean;
+                if (a.rstd) a.rstd[at] = rstd;
             }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (p + u * w.rows >= w.p1) break;
-            float o[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float xh = (v[u].get(i) - mean[i]) * rstd[i];
-                const float dz = act_grad(fmaf(xh, ga[i], be[i]), d[u].get(i), a.act);
-                o[i] = rstd[i] * (fmaf(ga[i], dz, -s1[i]) - xh * s2[i]);
-            }
-            Vec<T, V> r;
-            r.set(o);
-            r.store(dx + (int64_t)(p + u * w.rows) * a.ldy);
         }
     }
-}
-
-// dbeta, dgamma: the images' channel sums, a warp per channel of 32, 8 rows of images side by side.
-__global__ void __launch_bounds__(THREADS) affine_grad_kernel(Args a) {
-    pdl_trigger();
-    pdl_wait();
-    __shared__ float2 red[8][33];
-    const int c = (int)blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
-    float db = 0.0f, dg = 0.0f;
-    if (c < a.C)
-        for (int b = r; b < a.B; b += 8) {
-            const float2 t = a.chan[(int64_t)b * a.C + c];
-            db += t.x;
-            dg += t.y;
-        }
-    red[r][threadIdx.x & 31] = make_float2(db, dg);
+    if (a.chunks > 1) cluster.barrier_arrive();
     __syncthreads();
-    if (r == 0 && c < a.C) {
-        db = dg = 0.0f;
+    if (w.n > 0) {
+        float ga[V], be[V], mean[GPT], rstd[GPT];
+        load_affine<V>(a, w.c, ga, be);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            db += red[k][threadIdx.x].x;
-            dg += red[k][threadIdx.x].y;
+        for (int g = 0; g < GPT; ++g) {
+            const float2 t = all[(w.lane * V + g * W) / a.Cg];
+            mean[g] = t.x;
+            rstd[g] = t.y;
         }
-        if (a.dbeta) a.dbeta[c] = db;
-        if (a.dgamma) a.dgamma[c] = dg;
+        TY *y = static_cast<TY *>(a.y) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldy + w.c;
+        with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) {
+                    float z[V];
+#pragma unroll
+                    for (int k = 0; k < V; ++k)
+                        z[k] = act_value<act.value>(fmaf((v[i].get(k) - mean[k / W]) * rstd[k / W], ga[k], be[k]));
+                    Vec<TY, V> o;
+                    o.set(z);
+                    o.store(y + (int64_t)(i * w.rows) * a.ldy);
+                }
+        });
     }
+    if (a.chunks > 1) cluster.barrier_wait();              // no block leaves while its sums are read
 }
 
-// ---------------------------------------------------------------------------
-// Host side
-// ---------------------------------------------------------------------------
-
-using namespace minw_host;
-
-static size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
-
-// Pixel chunks per image of the streaming kernels: about eight blocks per SM over all images, at least 64 pixels each.
-static int chunks_of(int B, int64_t P) {
-    int64_t k = (8 * 152 + B - 1) / B;
-    if (k > (P + 63) / 64) k = (P + 63) / 64;
-    return (int)(k < 1 ? 1 : k);
+template <typename T, typename TY, int V, int GPT>
+static auto fused_of(int NV) {
+    if constexpr (V == 1) return fused_kernel<T, TY, 1, 1, 32>;
+    else return NV == 8 ? fused_kernel<T, TY, V, GPT, 8> : fused_kernel<T, TY, V, GPT, 16>;
 }
-
-struct Layout {
-    size_t part, stat, chan, total;
-};
-static Layout layout(int B, int64_t P, int C, int G, bool backward) {
-    Layout l;
-    size_t off = 0;
-    auto take = [&](size_t n) { const size_t r = off; off += al256(n * sizeof(float2)); return r; };
-    l.part = take((size_t)B * chunks_of(B, P) * C);
-    l.stat = take((size_t)B * G);
-    l.chan = backward ? take((size_t)B * C) : off;
-    l.total = off;
-    return l;
-}
-
-static bool valid_type(int t) { return t == MINW_F32 || t == MINW_BF16; }
-static int bytes_of(int t) { return t == MINW_BF16 ? 2 : 4; }
-
-// Whether a tensor's rows start on multiples of V values (at most 16 bytes of them).
-static bool fits(const void *p, int64_t ld, int type, int V) {
-    const int bytes = bytes_of(type) * V > 16 ? 16 : bytes_of(type) * V;
-    return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * bytes_of(type) % bytes == 0;
-}
-
-// An output at an input's address replaces it value by value.
-static bool in_place_ok(const void *in, int in_type, int64_t in_ld, const void *out, int out_type, int64_t out_ld) {
-    return in == nullptr || in != out || (in_type == out_type && in_ld == out_ld);
-}
-
-static cudaError_t launch(void (*kern)(Args), int64_t blocks, cudaStream_t s, const Args &a) {
-    return launch_pdl_stream(false, kern, dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
-}
-
-// Lanes and slabs of the streaming kernels for V channels a lane.
-static void lanes(Args &a, int V) {
-    const int lanes = a.C / V;
-    a.slabs = (lanes + THREADS - 1) / THREADS;
-    a.L = (lanes + a.slabs - 1) / a.slabs;
-}
-
 template <typename T, typename TY>
 static minw_status forward(Args a, int V, cudaStream_t s) {
+    Plan pl;
+    if (Args f = a; one_pass(f, pl, (int)sizeof(T), V, false)) {
+        const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
+        if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
+        void (*kern)(Args) = pl.V == 1 ? fused_of<T, TY, 1, 1>(pl.NV)
+                           : pl.V == 4 ? (pl.GPT == 1 ? fused_of<T, TY, 4, 1>(pl.NV) : fused_of<T, TY, 4, 4>(pl.NV))
+                                       : nullptr;
+        if constexpr (sizeof(T) == 2)
+            if (pl.V == 8) kern = pl.GPT == 1 ? fused_of<T, TY, 8, 1>(pl.NV) : fused_of<T, TY, 8, 2>(pl.NV);
+        if (launch_cluster(kern, blocks, s, f) != cudaSuccess) return MINW_ECUDA;
+        return launch_status();
+    }
     lanes(a, V);
     const int64_t blocks = (int64_t)a.B * a.chunks * a.slabs;
     if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
-    auto stat = V == 8 ? stat_kernel<T, 8> : V == 4 ? stat_kernel<T, 4> : stat_kernel<T, 1>;
-    auto apply = V == 8 ? apply_kernel<T, TY, 8> : V == 4 ? apply_kernel<T, TY, 4> : apply_kernel<T, TY, 1>;
+    void (*stat)(Args) = V == 4 ? stat_kernel<T, 4> : stat_kernel<T, 1>;
+    void (*apply)(Args) = V == 4 ? apply_kernel<T, TY, 4> : apply_kernel<T, TY, 1>;
+    if constexpr (sizeof(T) == 2)
+        if (V == 8) {
+            stat = stat_kernel<T, 8>;
+            apply = apply_kernel<T, TY, 8>;
+        }
     if (launch(stat, blocks, s, a) != cudaSuccess || launch(stat_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess ||
         launch(apply, blocks, s, a) != cudaSuccess)
         return MINW_ECUDA;
-    return launch_status();
-}
-
-template <typename T, typename TD>
-static minw_status backward(Args a, int V, cudaStream_t s) {
-    lanes(a, V);
-    const int64_t blocks = (int64_t)a.B * a.chunks * a.slabs;
-    if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
-    auto sum = V == 8 ? bwd_sum_kernel<T, TD, 8> : V == 4 ? bwd_sum_kernel<T, TD, 4> : bwd_sum_kernel<T, TD, 1>;
-    auto apply = V == 8 ? bwd_apply_kernel<T, TD, 8> : V == 4 ? bwd_apply_kernel<T, TD, 4> : bwd_apply_kernel<T, TD, 1>;
-    if (launch(sum, blocks, s, a) != cudaSuccess || launch(bwd_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess ||
-        launch(apply, blocks, s, a) != cudaSuccess)
-        return MINW_ECUDA;
-    if ((a.dgamma || a.dbeta) && launch(affine_grad_kernel, (a.C + 31) / 32, s, a) != cudaSuccess) return MINW_ECUDA;
     return launch_status();
 }
 
@@ -529,48 +348,6 @@ minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const fl
     if (x_type == MINW_BF16)
         return y_type == MINW_BF16 ? gn::forward<uint16_t, uint16_t>(a, V, s) : gn::forward<uint16_t, float>(a, V, s);
     return y_type == MINW_BF16 ? gn::forward<float, uint16_t>(a, V, s) : gn::forward<float, float>(a, V, s);
-}
-
-minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx, const void *dy, int32_t dy_type,
-                                     int64_t lddy, const float *gamma, const float *beta, const float *mean,
-                                     const float *rstd, int32_t B, int64_t P, int32_t C, int32_t G, int32_t act,
-                                     void *dx, int64_t lddx, float *dgamma, float *dbeta, void *workspace,
-                                     size_t workspace_bytes, void *stream) {
-    if ((B != 0 && (!x || !dy || !dx || !mean || !rstd)) || B < 0 || P < 1 || C < 1 || G < 1 || C % G != 0) return MINW_EINVAL;
-    if (ldx < C || lddy < C || lddx < C) return MINW_EINVAL;
-    if (!gn::valid_type(x_type) || !gn::valid_type(dy_type) || act < MINW_ACT_NONE || act > MINW_ACT_SILU)
-        return MINW_EINVAL;
-    if (!gn::fits(x, 1, x_type, 1) || !gn::fits(dy, 1, dy_type, 1) || !gn::fits(dx, 1, x_type, 1)) return MINW_EINVAL;
-    if (!gn::in_place_ok(x, x_type, ldx, dx, x_type, lddx) || !gn::in_place_ok(dy, dy_type, lddy, dx, x_type, lddx))
-        return MINW_EINVAL;
-    if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;
-    cudaStream_t s = (cudaStream_t)stream;
-    if (B == 0) {
-        if (dgamma && cudaMemsetAsync(dgamma, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
-        if (dbeta && cudaMemsetAsync(dbeta, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
-        return MINW_OK;
-    }
-    const gn::Layout l = gn::layout(B, P, C, G, true);
-    if (!workspace || !aligned16(workspace) || workspace_bytes < l.total) return MINW_EINVAL;
-    uint8_t *ws = static_cast<uint8_t *>(workspace);
-    gn::Args a{};
-    a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.y = dx; a.ldy = lddx; a.gamma = gamma; a.beta = beta;
-    a.mean_in = mean; a.rstd_in = rstd; a.dgamma = dgamma; a.dbeta = dbeta;
-    a.B = B; a.P = (int)P; a.C = C; a.G = G; a.Cg = C / G; a.act = act;
-    a.chunks = gn::chunks_of(B, P);
-    a.ppc = (int)((P + a.chunks - 1) / a.chunks);
-    a.chunks = (int)((P + a.ppc - 1) / a.ppc);
-    a.part = reinterpret_cast<float2 *>(ws + l.part);
-    a.stat = reinterpret_cast<float2 *>(ws + l.stat);
-    a.chan = reinterpret_cast<float2 *>(ws + l.chan);
-    int V = x_type == MINW_BF16 ? 8 : 4;
-    while (V > 1 && (C % V != 0 || !gn::fits(x, ldx, x_type, V) || !gn::fits(dy, lddy, dy_type, V) ||
-                     !gn::fits(dx, lddx, x_type, V)))
-        V = V == 8 ? 4 : 1;
-    if (x_type == MINW_BF16)
-        return dy_type == MINW_BF16 ? gn::backward<uint16_t, uint16_t>(a, V, s)
-                                    : gn::backward<uint16_t, float>(a, V, s);
-    return dy_type == MINW_BF16 ? gn::backward<float, uint16_t>(a, V, s) : gn::backward<float, float>(a, V, s);
 }
 
 }  // extern "C"

@@ -1,0 +1,417 @@
+// group_norm_bwd.cu -- backward of the group norm with an activation on
+// channels-last rows (group_norm.cuh: tiles and plans).  The two sums over a
+// group follow from the channel sums that dgamma and dbeta need anyway.
+#include "group_norm.cuh"
+
+namespace minw {
+namespace gn {
+
+// ---------------------------------------------------------------------------
+// Streaming backward: the channel sums per chunk, merged per image, then a
+// second pass over x and dy.
+// ---------------------------------------------------------------------------
+
+// Statistics of the V channels at c.
+template <int V>
+__device__ __forceinline__ void load_stats(const Args &a, int b, int c, float *mean, float *rstd) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const int64_t g = (int64_t)b * a.G + (c + i) / a.Cg;
+        mean[i] = a.mean_in[g];
+        rstd[i] = a.rstd_in[g];
+    }
+}
+
+template <typename T, typename TD, int V>
+__global__ void __launch_bounds__(THREADS) bwd_sum_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int U = V == 1 ? 8 : 2;
+    __shared__ float2 red[THREADS * V];
+    const Place w = place<V>(a, blockIdx.x);
+    float db[V], dg[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) db[i] = dg[i] = 0.0f;
+    if (w.active) {
+        float ga[V], be[V], mean[V], rstd[V];
+        load_affine<V>(a, w.c, ga, be);
+        load_stats<V>(a, w.b, w.c, mean, rstd);
+        const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
+        const TD *dy = static_cast<const TD *>(a.dy) + (int64_t)w.b * a.P * a.lddy + w.c;
+        with_act(a.act, [&](auto act) {
+            for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
+                Vec<T, V> v[U];
+                Vec<TD, V> d[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (p + u * w.rows < w.p1) {
+                        v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
+                        d[u].load(dy + (int64_t)(p + u * w.rows) * a.lddy);
+                    }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (p + u * w.rows >= w.p1) break;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        const float xh = (v[u].get(i) - mean[i]) * rstd[i];
+                        const float dz = act_grad<act.value>(fmaf(xh, ga[i], be[i]), d[u].get(i));
+                        db[i] += dz;
+                        dg[i] = fmaf(dz, xh, dg[i]);
+                    }
+                }
+            }
+        });
+    }
+    const int W = a.L * V;
+    if (w.row < w.rows) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[w.row * W + ((int)threadIdx.x % a.L) * V + i] = make_float2(db[i], dg[i]);
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < W; e += THREADS) {
+        const int c = w.slab * W + e;
+        if (c >= a.C) break;
+        float s0 = 0.0f, s1 = 0.0f;
+        for (int r = 0; r < w.rows; ++r) {
+            s0 += red[r * W + e].x;
+            s1 += red[r * W + e].y;
+        }
+        a.part[((int64_t)w.b * a.chunks + w.chunk) * a.C + c] = make_float2(s0, s1);
+    }
+}
+
+// Block = one image's group: its channels' sums over the chunks, then s1 and s2.
+__global__ void __launch_bounds__(THREADS) bwd_merge_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    __shared__ float2 red[THREADS / 32];
+    const int b = (int)(blockIdx.x / a.G), g = (int)(blockIdx.x % a.G), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float s1 = 0.0f, s2 = 0.0f;
+    for (int e = warp; e < a.Cg; e += THREADS / 32) {          // a warp per channel
+        const int c = g * a.Cg + e;
+        float db = 0.0f, dg = 0.0f;
+        for (int k = lane; k < a.chunks; k += 32) {
+            const float2 t = a.part[((int64_t)b * a.chunks + k) * a.C + c];
+            db += t.x;
+            dg += t.y;
+        }
+        db = warp_sum(db);
+        dg = warp_sum(dg);
+        if (lane == 0) a.chan[(int64_t)b * a.C + c] = make_float2(db, dg);
+        const float ga = a.gamma ? a.gamma[c] : 1.0f;
+        s1 = fmaf(ga, db, s1);
+        s2 = fmaf(ga, dg, s2);
+    }
+    if (lane == 0) red[warp] = make_float2(s1, s2);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s1 = s2 = 0.0f;
+        for (int k = 0; k < THREADS / 32; ++k) {
+            s1 += red[k].x;
+            s2 += red[k].y;
+        }
+        const float n = (float)a.P * (float)a.Cg;
+        a.stat[blockIdx.x] = make_float2(s1 / n, s2 / n);
+    }
+}
+
+template <typename T, typename TD, int V>
+__global__ void __launch_bounds__(THREADS) bwd_apply_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int U = V == 1 ? 8 : 2;
+    const Place w = place<V>(a, (int64_t)gridDim.x - 1 - blockIdx.x);
+    if (!w.active) return;
+    float ga[V], be[V], mean[V], rstd[V], s1[V], s2[V];
+    load_affine<V>(a, w.c, ga, be);
+    load_stats<V>(a, w.b, w.c, mean, rstd);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
+        s1[i] = t.x;
+        s2[i] = t.y;
+    }
+    const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
+    const TD *dy = static_cast<const TD *>(a.dy) + (int64_t)w.b * a.P * a.lddy + w.c;
+    T *dx = static_cast<T *>(a.y) + (int64_t)w.b * a.P * a.ldy + w.c;
+    with_act(a.act, [&](auto act) {
+        for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
+            Vec<T, V> v[U];
+            Vec<TD, V> d[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p + u * w.rows < w.p1) {
+                    v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
+                    d[u].load(dy + (int64_t)(p + u * w.rows) * a.lddy);
+                }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (p + u * w.rows >= w.p1) break;
+                float o[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float xh = (v[u].get(i) - mean[i]) * rstd[i];
+                    const float dz = act_grad<act.value>(fmaf(xh, ga[i], be[i]), d[u].get(i));
+                    o[i] = rstd[i] * (fmaf(ga[i], dz, -s1[i]) - xh * s2[i]);
+                }
+                Vec<T, V> r;
+                r.set(o);
+                r.store(dx + (int64_t)(p + u * w.rows) * a.ldy);
+            }
+        }
+    });
+}
+
+// ---------------------------------------------------------------------------
+// One pass over x and dy.
+// ---------------------------------------------------------------------------
+
+template <typename T, typename TD, int V, int GPT, int NV>
+__global__ void __launch_bounds__(THREADS) fused_bwd_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int W = V / GPT;
+    __shared__ float2 red[THREADS * V];                    // rows x channels, then segments x channels
+    __shared__ float2 group[MAX_SLAB_GROUPS];
+    const Tile w = tile<V>(a);
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+    const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
+    Vec<T, V> v[NV];
+    Vec<TD, V> d[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < w.n) {
+            v[i].load(x + (int64_t)(i * w.rows) * a.ldx);
+            d[i].load(dy + (int64_t)(i * w.rows) * a.lddy);
+        }
+    const int CW = a.L * V, g0 = w.slab * (CW / a.Cg);     // channels of the slab, its first group
+    float ga[V], be[V], mean[GPT], rstd[GPT];
+    load_affine<V>(a, w.c, ga, be);
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) {
+        const int64_t at = (int64_t)w.b * a.G + g0 + (w.lane * V + g * W) / a.Cg;
+        mean[g] = a.mean_in[at];
+        rstd[g] = a.rstd_in[at];
+    }
+    {
+        float db[V], dg[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) db[k] = dg[k] = 0.0f;
+        with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) {
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        const float xh = (v[i].get(k) - mean[k / W]) * rstd[k / W];
+                        const float dz = act_grad<act.value>(fmaf(xh, ga[k], be[k]), d[i].get(k));
+                        db[k] += dz;
+                        dg[k] = fmaf(dz, xh, dg[k]);
+                    }
+                }
+        });
+        if (w.row < w.rows) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) red[w.row * CW + w.lane * V + k] = make_float2(db[k], dg[k]);
+        }
+    }
+    __syncthreads();
+    // channel sums of this block: THREADS / CW threads a channel, each every so many rows (into row of its number)
+    const int seg = CW >= THREADS ? 1 : min(THREADS / CW, w.rows);
+    for (int e = threadIdx.x; e < seg * CW; e += THREADS) {
+        const int c = e % CW, s = e / CW;
+        float2 t = red[s * CW + c];
+        for (int r = s + seg; r < w.rows; r += seg) {
+            t.x += red[r * CW + c].x;
+            t.y += red[r * CW + c].y;
+        }
+        red[s * CW + c] = t;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < CW; c += THREADS) {
+        float2 t = red[c];
+        for (int s = 1; s < seg; ++s) {
+            t.x += red[s * CW + c].x;
+            t.y += red[s * CW + c].y;
+        }
+        red[c] = t;
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    float2 *tot = red;
+    if (a.chunks > 1) {
+        // the cluster's blocks: their sums stay in place while the totals go behind them
+        cluster.sync();
+        tot = w.rows > 1 ? red + CW : nullptr;
+        for (int c = threadIdx.x; c < CW; c += THREADS) {
+            float2 t = make_float2(0.0f, 0.0f);
+            for (int k = 0; k < a.chunks; ++k) {
+                const float2 u = *cluster.map_shared_rank(&red[c], k);
+                t.x += u.x;
+                t.y += u.y;
+            }
+            tot[c] = t;
+        }
+        cluster.barrier_arrive();
+    }
+    __syncthreads();
+    if (w.rank == 0)
+        for (int c = threadIdx.x; c < CW; c += THREADS) a.chan[(int64_t)w.b * a.C + w.slab * CW + c] = tot[c];
+    const float n = (float)a.P * (float)a.Cg;
+    for (int g = threadIdx.x >> 5; g < CW / a.Cg; g += THREADS / 32) {
+        float s1 = 0.0f, s2 = 0.0f;
+        for (int k = threadIdx.x & 31; k < a.Cg; k += 32) {
+            const float2 t = tot[g * a.Cg + k];
+            const float gk = a.gamma ? a.gamma[w.slab * CW + g * a.Cg + k] : 1.0f;
+            s1 = fmaf(gk, t.x, s1);
+            s2 = fmaf(gk, t.y, s2);
+        }
+        s1 = warp_sum(s1);
+        s2 = warp_sum(s2);
+        if ((threadIdx.x & 31) == 0) group[g] = make_float2(s1 / n, s2 / n);
+    }
+    __syncthreads();
+    if (w.n > 0) {
+        float s1[GPT], s2[GPT];
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            const float2 t = group[(w.lane * V + g * W) / a.Cg];
+            s1[g] = t.x;
+            s2[g] = t.y;
+        }
+        T *dx = static_cast<T *>(a.y) + p * a.ldy + w.c;
+        with_act(a.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) {
+                    float o[V];
+#pragma unroll
+                    for (int k = 0; k < V; ++k) {
+                        const float xh = (v[i].get(k) - mean[k / W]) * rstd[k / W];
+                        const float dz = act_grad<act.value>(fmaf(xh, ga[k], be[k]), d[i].get(k));
+                        o[k] = rstd[k / W] * (fmaf(ga[k], dz, -s1[k / W]) - xh * s2[k / W]);
+                    }
+                    Vec<T, V> r;
+                    r.set(o);
+                    r.store(dx + (int64_t)(i * w.rows) * a.ldy);
+                }
+        });
+    }
+    if (a.chunks > 1) cluster.barrier_wait();              // no block leaves while its sums are read
+}
+
+// dbeta, dgamma: the images' channel sums, a warp per channel of 32, 8 rows of images side by side.
+__global__ void __launch_bounds__(THREADS) affine_grad_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    __shared__ float2 red[8][33];
+    const int c = (int)blockIdx.x * 32 + (threadIdx.x & 31), r = threadIdx.x >> 5;
+    float db = 0.0f, dg = 0.0f;
+    if (c < a.C)
+        for (int b = r; b < a.B; b += 8) {
+            const float2 t = a.chan[(int64_t)b * a.C + c];
+            db += t.x;
+            dg += t.y;
+        }
+    red[r][threadIdx.x & 31] = make_float2(db, dg);
+    __syncthreads();
+    if (r == 0 && c < a.C) {
+        db = dg = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            db += red[k][threadIdx.x].x;
+            dg += red[k][threadIdx.x].y;
+        }
+        if (a.dbeta) a.dbeta[c] = db;
+        if (a.dgamma) a.dgamma[c] = dg;
+    }
+}
+
+template <typename T, typename TD, int V, int GPT>
+static auto fused_bwd_of() {
+    if constexpr (V == 1) return fused_bwd_kernel<T, TD, 1, 1, 32>;
+    else return fused_bwd_kernel<T, TD, V, GPT, 8>;
+}
+
+template <typename T, typename TD>
+static minw_status backward(Args a, int V, cudaStream_t s) {
+    Plan pl;
+    if (Args f = a; one_pass(f, pl, (int)sizeof(T), V, true)) {
+        const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
+        if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
+        void (*kern)(Args) = pl.V == 1 ? fused_bwd_of<T, TD, 1, 1>()
+                           : pl.V == 4 ? (pl.GPT == 1 ? fused_bwd_of<T, TD, 4, 1>() : fused_bwd_of<T, TD, 4, 4>())
+                                       : nullptr;
+        if constexpr (sizeof(T) == 2)
+            if (pl.V == 8) kern = pl.GPT == 1 ? fused_bwd_of<T, TD, 8, 1>() : fused_bwd_of<T, TD, 8, 2>();
+        if (launch_cluster(kern, blocks, s, f) != cudaSuccess) return MINW_ECUDA;
+    } else {
+        lanes(a, V);
+        const int64_t blocks = (int64_t)a.B * a.chunks * a.slabs;
+        if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
+        void (*sum)(Args) = V == 4 ? bwd_sum_kernel<T, TD, 4> : bwd_sum_kernel<T, TD, 1>;
+        void (*apply)(Args) = V == 4 ? bwd_apply_kernel<T, TD, 4> : bwd_apply_kernel<T, TD, 1>;
+        if constexpr (sizeof(T) == 2)
+            if (V == 8) {
+                sum = bwd_sum_kernel<T, TD, 8>;
+                apply = bwd_apply_kernel<T, TD, 8>;
+            }
+        if (launch(sum, blocks, s, a) != cudaSuccess ||
+            launch(bwd_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess || launch(apply, blocks, s, a) != cudaSuccess)
+            return MINW_ECUDA;
+    }
+    if ((a.dgamma || a.dbeta) && launch(affine_grad_kernel, (a.C + 31) / 32, s, a) != cudaSuccess) return MINW_ECUDA;
+    return launch_status();
+}
+
+}  // namespace gn
+}  // namespace minw
+
+using namespace minw;
+using namespace minw_host;
+
+extern "C" {
+
+minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx, const void *dy, int32_t dy_type,
+                                     int64_t lddy, const float *gamma, const float *beta, const float *mean,
+                                     const float *rstd, int32_t B, int64_t P, int32_t C, int32_t G, int32_t act,
+                                     void *dx, int64_t lddx, float *dgamma, float *dbeta, void *workspace,
+                                     size_t workspace_bytes, void *stream) {
+    if ((B != 0 && (!x || !dy || !dx || !mean || !rstd)) || B < 0 || P < 1 || C < 1 || G < 1 || C % G != 0) return MINW_EINVAL;
+    if (ldx < C || lddy < C || lddx < C) return MINW_EINVAL;
+    if (!gn::valid_type(x_type) || !gn::valid_type(dy_type) || act < MINW_ACT_NONE || act > MINW_ACT_SILU)
+        return MINW_EINVAL;
+    if (!gn::fits(x, 1, x_type, 1) || !gn::fits(dy, 1, dy_type, 1) || !gn::fits(dx, 1, x_type, 1)) return MINW_EINVAL;
+    if (!gn::in_place_ok(x, x_type, ldx, dx, x_type, lddx) || !gn::in_place_ok(dy, dy_type, lddy, dx, x_type, lddx))
+        return MINW_EINVAL;
+    if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (B == 0) {
+        if (dgamma && cudaMemsetAsync(dgamma, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
+        if (dbeta && cudaMemsetAsync(dbeta, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
+        return MINW_OK;
+    }
+    const gn::Layout l = gn::layout(B, P, C, G, true);
+    if (!workspace || !aligned16(workspace) || workspace_bytes < l.total) return MINW_EINVAL;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    gn::Args a{};
+    a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.y = dx; a.ldy = lddx; a.gamma = gamma; a.beta = beta;
+    a.mean_in = mean; a.rstd_in = rstd; a.dgamma = dgamma; a.dbeta = dbeta;
+    a.B = B; a.P = (int)P; a.C = C; a.G = G; a.Cg = C / G; a.act = act;
+    a.chunks = gn::chunks_of(B, P);
+    a.ppc = (int)((P + a.chunks - 1) / a.chunks);
+    a.chunks = (int)((P + a.ppc - 1) / a.ppc);
+    a.part = reinterpret_cast<float2 *>(ws + l.part);
+    a.stat = reinterpret_cast<float2 *>(ws + l.stat);
+    a.chan = reinterpret_cast<float2 *>(ws + l.chan);
+    int V = x_type == MINW_BF16 ? 8 : 4;
+    while (V > 1 && (C % V != 0 || !gn::fits(x, ldx, x_type, V) || !gn::fits(dy, lddy, dy_type, V) ||
+                     !gn::fits(dx, lddx, x_type, V)))
+        V = V == 8 ? 4 : 1;
+    if (x_type == MINW_BF16)
+        return dy_type == MINW_BF16 ? gn::backward<uint16_t, uint16_t>(a, V, s)
+                                    : gn::backward<uint16_t, float>(a, V, s);
+    return dy_type == MINW_BF16 ? gn::backward<float, uint16_t>(a, V, s) : gn::backward<float, float>(a, V, s);
+}
+
+}  // extern "C"

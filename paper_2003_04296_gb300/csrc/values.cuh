@@ -4,6 +4,8 @@
 
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace minw {
@@ -70,22 +72,33 @@ struct Vec {
 __device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 // y = act(z); a NaN stays one.
-__device__ __forceinline__ float act_value(float z, int act) {
-    if (act == MINW_ACT_HARDTANH) return z > 1.0f ? 1.0f : z < -1.0f ? -1.0f : z;
-    if (act == MINW_ACT_RELU) return z < 0.0f ? 0.0f : z;
-    if (act == MINW_ACT_SILU) return z * sigmoidf_(z);
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == MINW_ACT_HARDTANH) return z > 1.0f ? 1.0f : z < -1.0f ? -1.0f : z;
+    if constexpr (ACT == MINW_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == MINW_ACT_SILU) return z * sigmoidf_(z);
     return z;
 }
 
 // dy act'(z).  HardTanh passes the gradient on |z| <= 1 (Eq. activation's mask), ReLU on z > 0.
-__device__ __forceinline__ float act_grad(float z, float dy, int act) {
-    if (act == MINW_ACT_HARDTANH) return fabsf(z) <= 1.0f ? dy : 0.0f;
-    if (act == MINW_ACT_RELU) return z > 0.0f ? dy : 0.0f;
-    if (act == MINW_ACT_SILU) {
+template <int ACT>
+__device__ __forceinline__ float act_grad(float z, float dy) {
+    if constexpr (ACT == MINW_ACT_HARDTANH) return fabsf(z) <= 1.0f ? dy : 0.0f;
+    if constexpr (ACT == MINW_ACT_RELU) return z > 0.0f ? dy : 0.0f;
+    if constexpr (ACT == MINW_ACT_SILU) {
         const float s = sigmoidf_(z);
         return dy * (s * fmaf(z, 1.0f - s, 1.0f));
     }
     return dy;
+}
+
+// f(std::integral_constant<int, act>): the choice once around a loop, not at each value.
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    if (act == MINW_ACT_HARDTANH) f(std::integral_constant<int, MINW_ACT_HARDTANH>{});
+    else if (act == MINW_ACT_RELU) f(std::integral_constant<int, MINW_ACT_RELU>{});
+    else if (act == MINW_ACT_SILU) f(std::integral_constant<int, MINW_ACT_SILU>{});
+    else f(std::integral_constant<int, MINW_ACT_NONE>{});
 }
 
 }  // namespace minw

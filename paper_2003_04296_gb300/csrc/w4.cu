@@ -262,7 +262,8 @@ __global__ void __launch_bounds__(THREADS) matvec_kernel(Args a) {
                 for (int k = 0; k < nk; ++k)
                     sum += src[((k * a.wr + r / 16) * 16 + r % 16) * CW + tk * a.parts + i];
             }
-        const float z = act_value(fmaf(sum, a.scale ? a.scale[o] : 1.0f, a.shift ? a.shift[o] : 0.0f), a.act);
+        float z = fmaf(sum, a.scale ? a.scale[o] : 1.0f, a.shift ? a.shift[o] : 0.0f);
+        with_act(a.act, [&](auto act) { z = act_value<act.value>(z); });
         const int64_t at = (int64_t)(t0 + tk) * a.ldy + o;
         if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(z));
         else static_cast<float *>(a.y)[at] = z;
