@@ -154,13 +154,64 @@ __global__ void __launch_bounds__(THREADS) apply_kernel(Args a) {
     });
 }
 
-// GPT: groups among a thread's V channels (V / GPT channels of each).
+// Sums over a block of each thread's GPT values, one per group of its channels; afterwards every thread has the
+// sums of its own groups.  `per` entries (a thread's value is one) make a group, L GPT a row.
+template <int GPT>
+struct GroupSum {
+    float part[THREADS * GPT], total[MAX_SLAB_GROUPS];
+};
+template <int GPT>
+__device__ __forceinline__ void group_sum(float *s, GroupSum<GPT> &sm, const Args &a, const Tile &w, int per) {
+    const int groups = a.L * GPT / per, lane = threadIdx.x & 31;
+    if (a.butterfly) {
+        // lanes 32 apart in a row or in a group of one are powers of two apart: exchanges within a warp, then the
+        // eight warps' sums
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1)
+            if (d < per || d >= a.L) {
+#pragma unroll
+                for (int g = 0; g < GPT; ++g) s[g] += __shfl_xor_sync(0xffffffffu, s[g], d);
+            }
+        const int at = w.lane * GPT / per;
+        if (lane < a.L && lane % per == 0) {
+#pragma unroll
+            for (int g = 0; g < GPT; ++g) sm.part[(threadIdx.x >> 5) * groups + at + g] = s[g];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            s[g] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < THREADS / 32; ++k) s[g] += sm.part[k * groups + at + g];
+        }
+    } else {
+        const int row = a.L * GPT;
+        if (w.row < w.rows) {
+#pragma unroll
+            for (int g = 0; g < GPT; ++g) sm.part[w.row * row + w.lane * GPT + g] = s[g];
+        }
+        __syncthreads();
+        for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {      // a warp per group
+            float t = 0.0f;
+            for (int e = lane; e < w.rows * per; e += 32) t += sm.part[e / per * row + g * per + e % per];
+            t = warp_sum(t);
+            if (lane == 0) sm.total[g] = t;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) s[g] = sm.total[(w.lane * GPT + g) / per];
+    }
+}
+
+// GPT: groups among a thread's V channels (W = V / GPT channels of each).  A thread sums its values and their
+// squared deviations from its own mean; the block's mean turns the latter into deviations from that (n W (m - mean)^2
+// more), and the cluster's mean likewise.
 template <typename T, typename TY, int V, int GPT, int NV>
-__global__ void __launch_bounds__(THREADS) fused_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int W = V / GPT;
-    __shared__ float em[THREADS * GPT], eq[THREADS * GPT];
+    constexpr int W = V / GPT, NP = V / 2 > 0 ? V / 2 : 1;
+    __shared__ GroupSum<GPT> sums[2];
     __shared__ float2 cta[MAX_SLAB_GROUPS], all[MAX_SLAB_GROUPS];
     const Tile w = tile<V>(a);
     const T *x = static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c;
@@ -169,99 +220,153 @@ __global__ void __launch_bounds__(THREADS) fused_kernel(Args a) {
     for (int i = 0; i < NV; ++i)
         if (i < w.n) v[i].load(x + (int64_t)(i * w.rows) * a.ldx);
 
-    // this thread's statistics of each of its groups: n W values
-    const float inv = w.n > 0 ? 1.0f / (float)(w.n * W) : 0.0f;
+    const int per = a.Cg / W, groups = a.L * GPT / per;
+    float mean[GPT], m2[GPT];
+    {
+        const float inv = w.n > 0 ? 1.0f / (float)(w.n * W) : 0.0f;
+        float own[GPT];
+        if constexpr (V == 1) {
+            float s = 0.0f, q = 0.0f;
 #pragma unroll
-    for (int g = 0; g < GPT; ++g) {
-        float s = 0.0f, q = 0.0f;
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) s += v[i].get(0);
+            own[0] = s * inv;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < w.n) {
-#pragma unroll
-                for (int k = 0; k < W; ++k) s += v[i].get(g * W + k);
-            }
-        s *= inv;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (i < w.n) {
-#pragma unroll
-                for (int k = 0; k < W; ++k) {
-                    const float d = v[i].get(g * W + k) - s;
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) {
+                    const float d = v[i].get(0) - own[0];
                     q = fmaf(d, d, q);
                 }
-            }
-        if (w.row < w.rows) {
-            em[(w.row * a.L + w.lane) * GPT + g] = s;
-            eq[(w.row * a.L + w.lane) * GPT + g] = q;
+            mean[0] = s;
+            m2[0] = q;
+        } else {
+            // pairs of channels: of one group, or (W = 1) of two
+            Pair s[NP], q[NP];
+#pragma unroll
+            for (int k = 0; k < NP; ++k) s[k] = q[k] = pair(0.0f, 0.0f);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) {
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) s[k] = add2(s[k], v[i].get2(k));
+                }
+            auto fold = [&](const Pair *p, float *f) {
+                if constexpr (W == 1) {
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        const float2 h = halves(p[k]);
+                        f[2 * k] = h.x;
+                        f[2 * k + 1] = h.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int g = 0; g < GPT; ++g) {
+                        Pair t = p[g * W / 2];
+#pragma unroll
+                        for (int k = 1; k < W / 2; ++k) t = add2(t, p[g * W / 2 + k]);
+                        const float2 h = halves(t);
+                        f[g] = h.x + h.y;
+                    }
+                }
+            };
+            fold(s, mean);
+#pragma unroll
+            for (int g = 0; g < GPT; ++g) own[g] = mean[g] * inv;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+                if (i < w.n) {
+#pragma unroll
+                    for (int k = 0; k < NP; ++k) {
+                        const Pair d = add2(v[i].get2(k), pair(-own[2 * k / W], -own[(2 * k + 1) / W]));
+                        q[k] = fma2(d, d, q[k]);
+                    }
+                }
+            fold(q, m2);
         }
-    }
-    __syncthreads();
-
-    // a warp per group: the rows x (Cg / W) entries of this block
-    const int groups = a.L * V / a.Cg, per = a.Cg / W, np = w.p1 - w.p0, lane = threadIdx.x & 31;
-    for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {
-        float s = 0.0f;
-        const int entries = min(w.rows, np) * per;
-        for (int e = lane; e < entries; e += 32) {
-            const int r = e / per;
-            s = fmaf((float)((np - r + w.rows - 1) / w.rows), em[r * a.L * GPT + g * per + e % per], s);
-        }
-        const float mean = np > 0 ? warp_sum(s) / ((float)np * (float)per) : 0.0f;
-        s = 0.0f;
-        for (int e = lane; e < entries; e += 32) {
-            const int r = e / per, at = r * a.L * GPT + g * per + e % per;
-            const float d = em[at] - mean;
-            s += fmaf(d * d, (float)((np - r + w.rows - 1) / w.rows * W), eq[at]);
-        }
-        s = warp_sum(s);
-        if (lane == 0) cta[g] = make_float2(mean, s);
-    }
-
-    // the cluster's blocks; the same sums in every block
-    cg::cluster_group cluster = cg::this_cluster();
-    if (a.chunks > 1) cluster.sync();
-    else __syncthreads();
-    for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {
-        float2 t = make_float2(0.0f, 0.0f);
-        float n = 0.0f;
-        if (lane < a.chunks) {
-            t = *(a.chunks > 1 ? cluster.map_shared_rank(&cta[g], lane) : &cta[g]);
-            const int q0 = min(a.P, lane * a.ppc);
-            n = (float)(min(a.P, q0 + a.ppc) - q0) * (float)a.Cg;
-        }
-        const float total = (float)a.P * (float)a.Cg;
-        const float mean = warp_sum(n * t.x) / total;
-        const float d = t.x - mean;
-        const float rstd = 1.0f / sqrtf(warp_sum(n > 0.0f ? fmaf(d * d, n, t.y) : 0.0f) / total + a.eps);
-        if (lane == 0) {
-            all[g] = make_float2(mean, rstd);
-            if (w.rank == 0) {
-                const int64_t at = (int64_t)w.b * a.G + w.slab * groups + g;
-                if (a.mean) a.mean[at] = mean;
-                if (a.rstd) a.rstd[at] = rstd;
-            }
-        }
-    }
-    if (a.chunks > 1) cluster.barrier_arrive();
-    __syncthreads();
-    if (w.n > 0) {
-        float ga[V], be[V], mean[GPT], rstd[GPT];
-        load_affine<V>(a, w.c, ga, be);
+        group_sum<GPT>(mean, sums[0], a, w, per);
+        const float np = (float)(w.p1 - w.p0) * (float)a.Cg;
 #pragma unroll
         for (int g = 0; g < GPT; ++g) {
-            const float2 t = all[(w.lane * V + g * W) / a.Cg];
-            mean[g] = t.x;
-            rstd[g] = t.y;
+            mean[g] = w.p1 > w.p0 ? mean[g] / np : 0.0f;
+            const float d = own[g] - mean[g];
+            if (w.n > 0) m2[g] = fmaf(d * d, (float)(w.n * W), m2[g]);
         }
+        group_sum<GPT>(m2, sums[1], a, w, per);
+    }
+
+    cg::cluster_group cluster = cg::this_cluster();
+    const float total = (float)a.P * (float)a.Cg;
+    float rstd[GPT];
+    if (a.chunks > 1) {
+        // the cluster's blocks: sixteen threads a group, one for each; the same sums in every block
+        if (w.row == 0) {
+#pragma unroll
+            for (int g = 0; g < GPT; ++g)
+                if ((w.lane * GPT + g) % per == 0) cta[(w.lane * GPT + g) / per] = make_float2(mean[g], m2[g]);
+        }
+        cluster.sync();
+        for (int g = threadIdx.x >> 4; g < (groups + 1) / 2 * 2; g += THREADS / 16) {    // both halves of a warp alike
+            const int k = threadIdx.x & 15;
+            float2 t = make_float2(0.0f, 0.0f);
+            float n = 0.0f;
+            if (k < a.chunks && g < groups) {
+                t = *cluster.map_shared_rank(&cta[g], k);
+                const int q0 = min(a.P, k * a.ppc);
+                n = (float)(min(a.P, q0 + a.ppc) - q0) * (float)a.Cg;
+            }
+            float s = n * t.x;
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+            s /= total;
+            const float d0 = t.x - s;
+            float q = n > 0.0f ? fmaf(d0 * d0, n, t.y) : 0.0f;
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
+            if (k == 0 && g < groups) all[g] = make_float2(s, q);
+        }
+        cluster.barrier_arrive();
+        __syncthreads();
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            const float2 t = all[(w.lane * GPT + g) / per];
+            mean[g] = t.x;
+            m2[g] = t.y;
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) rstd[g] = 1.0f / sqrtf(m2[g] / total + a.eps);
+    if (w.rank == 0 && w.row == 0) {
+#pragma unroll
+        for (int g = 0; g < GPT; ++g)
+            if ((w.lane * GPT + g) % per == 0) {
+                const int64_t at = (int64_t)w.b * a.G + w.slab * groups + (w.lane * GPT + g) / per;
+                if (a.mean) a.mean[at] = mean[g];
+                if (a.rstd) a.rstd[at] = rstd[g];
+            }
+    }
+    if (w.n > 0) {
+        float ga[V], be[V];
+        load_affine<V>(a, w.c, ga, be);
         TY *y = static_cast<TY *>(a.y) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldy + w.c;
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < w.n) {
                     float z[V];
+                    if constexpr (V == 1) {
+                        z[0] = fmaf((v[i].get(0) - mean[0]) * rstd[0], ga[0], be[0]);
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < V; ++k)
-                        z[k] = act_value<act.value>(fmaf((v[i].get(k) - mean[k / W]) * rstd[k / W], ga[k], be[k]));
+                        for (int k = 0; k < NP; ++k) {
+                            const int g0 = 2 * k / W, g1 = (2 * k + 1) / W;
+                            const Pair xh = mul2(add2(v[i].get2(k), pair(-mean[g0], -mean[g1])), pair(rstd[g0], rstd[g1]));
+                            const float2 h = halves(fma2(xh, pair(ga[2 * k], ga[2 * k + 1]), pair(be[2 * k], be[2 * k + 1])));
+                            z[2 * k] = h.x;
+                            z[2 * k + 1] = h.y;
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < V; ++k) z[k] = act_value<act.value>(z[k]);
                     Vec<TY, V> o;
                     o.set(z);
                     o.store(y + (int64_t)(i * w.rows) * a.ldy);
@@ -283,7 +388,8 @@ static minw_status forward(Args a, int V, cudaStream_t s) {
         const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
         if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
         void (*kern)(Args) = pl.V == 1 ? fused_of<T, TY, 1, 1>(pl.NV)
-                           : pl.V == 4 ? (pl.GPT == 1 ? fused_of<T, TY, 4, 1>(pl.NV) : fused_of<T, TY, 4, 4>(pl.NV))
+                           : pl.V == 4 ? (pl.GPT == 1 ? fused_of<T, TY, 4, 1>(pl.NV) : pl.GPT == 2 ? fused_of<T, TY, 4, 2>(pl.NV)
+                                                                                       : fused_of<T, TY, 4, 4>(pl.NV))
                                        : nullptr;
         if constexpr (sizeof(T) == 2)
             if (pl.V == 8) kern = pl.GPT == 1 ? fused_of<T, TY, 8, 1>(pl.NV) : fused_of<T, TY, 8, 2>(pl.NV);

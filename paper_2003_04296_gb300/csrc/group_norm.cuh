@@ -43,6 +43,7 @@ struct Args {
     float eps;
     int chunks, ppc;               // pixel chunks per image, pixels per chunk
     int L, slabs;                  // lanes (V channels each) of a slab, slabs of a row
+    int butterfly;                 // one pass: lanes and the lanes of a group are powers of two within a warp
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -172,7 +173,7 @@ struct Plan {
 };
 inline bool one_pass(Args &a, Plan &pl, int bytes, int V0, bool backward) {
     pl.V = V0 == 8 && a.Cg % 4 != 0 ? 4 : V0;
-    pl.GPT = a.Cg % pl.V == 0 ? 1 : pl.V == 8 ? 2 : pl.V;
+    pl.GPT = a.Cg % pl.V == 0 ? 1 : pl.V == 8 || a.Cg % 2 == 0 ? 2 : pl.V;
     for (int width = 128; width >= 32; width /= 2)
         for (int k = 1; k <= a.G && k <= MAX_SLAB_GROUPS; ++k) {
             const int channels = k * a.Cg;
@@ -184,6 +185,9 @@ inline bool one_pass(Args &a, Plan &pl, int bytes, int V0, bool backward) {
             pl.NV = pl.V == 1 ? 32 : backward || a.P <= 64 * rows ? 8 : 16;
             const int64_t cap = (int64_t)rows * pl.NV, cluster = (a.P + cap - 1) / cap;
             if (cluster > 16 || (backward && cluster > 1 && rows < 2)) break;     // a cluster's totals go behind the block's sums
+            const int W = pl.V / pl.GPT, lanes_of_group = a.Cg / W;
+            a.butterfly = L <= 32 && (L & (L - 1)) == 0 &&
+                          (lanes_of_group == 1 || (pl.GPT == 1 && (lanes_of_group & (lanes_of_group - 1)) == 0));
             a.L = L;
             a.slabs = a.G / k;
             a.chunks = (int)cluster;

@@ -340,7 +340,8 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
         const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
         if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
         void (*kern)(Args) = pl.V == 1 ? fused_bwd_of<T, TD, 1, 1>()
-                           : pl.V == 4 ? (pl.GPT == 1 ? fused_bwd_of<T, TD, 4, 1>() : fused_bwd_of<T, TD, 4, 4>())
+                           : pl.V == 4 ? (pl.GPT == 1 ? fused_bwd_of<T, TD, 4, 1>() : pl.GPT == 2 ? fused_bwd_of<T, TD, 4, 2>()
+                                                                                     : fused_bwd_of<T, TD, 4, 4>())
                                        : nullptr;
         if constexpr (sizeof(T) == 2)
             if (pl.V == 8) kern = pl.GPT == 1 ? fused_bwd_of<T, TD, 8, 1>() : fused_bwd_of<T, TD, 8, 2>();

@@ -10,6 +10,36 @@
 
 namespace minw {
 
+// Two fp32 values in a register pair: one instruction for both.
+struct Pair {
+    uint64_t v;
+};
+__device__ __forceinline__ Pair pair(float lo, float hi) {
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p.v) : "f"(lo), "f"(hi));
+    return p;
+}
+__device__ __forceinline__ float2 halves(Pair p) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(p.v));
+    return f;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
 // V consecutive values of type T (float, or uint16_t holding bf16 bits), one load or store of up to 16 bytes each.
 // The address is a multiple of the load's size.
 template <typename T, int V>
@@ -51,6 +81,8 @@ struct Vec {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
         else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
     }
+    // values 2 k and 2 k + 1
+    __device__ __forceinline__ Pair get2(int k) const { return pair(get(2 * k), get(2 * k + 1)); }
     // all V values at once: bf16 rounds to nearest even, two to a conversion
     __device__ __forceinline__ void set(const float *v) {
         if constexpr (sizeof(T) == 4) {
@@ -68,14 +100,26 @@ struct Vec {
     }
 };
 
+// The larger and the smaller of two values; a NaN among them stays one (fmaxf and fminf drop it).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // 1 / (1 + e^-z): tends to 0 and 1 at both ends (e^-z = infinity gives 0).
 __device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
 
 // y = act(z); a NaN stays one.
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
-    if constexpr (ACT == MINW_ACT_HARDTANH) return z > 1.0f ? 1.0f : z < -1.0f ? -1.0f : z;
-    if constexpr (ACT == MINW_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if constexpr (ACT == MINW_ACT_HARDTANH) return min_nan(max_nan(z, -1.0f), 1.0f);
+    if constexpr (ACT == MINW_ACT_RELU) return max_nan(z, 0.0f);
     if constexpr (ACT == MINW_ACT_SILU) return z * sigmoidf_(z);
     return z;
 }

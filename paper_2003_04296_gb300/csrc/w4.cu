@@ -136,39 +136,81 @@ __device__ __forceinline__ void split3(float v, uint16_t *p) {
     p[2] = __bfloat16_as_ushort(__float2bfloat16_rn(r - __uint_as_float(m & 0xffff0000u)));
 }
 
+__device__ __forceinline__ void copy16(uint16_t *dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
+                 "r"(bytes)
+                 : "memory");
+}
+
 // Blocks [b0, b0 + n) of the pass's vectors into shared memory, columns of n 128 + 32 values (the 64 bytes
 // over put the eight columns of a tile into different banks), zero past K.
 __device__ __forceinline__ void stage(const Args &a, uint16_t *xs, int t0, int tokens, int b0, int n) {
-    const int pitch = n * 128 + 32, k0 = b0 * 128;
+    const int pitch = n * 128 + 32, k0 = b0 * 128, valid = min(a.K - k0, n * 128);
     if (a.x_bf16) {
-        const uint16_t *x = static_cast<const uint16_t *>(a.x);
+        const uint16_t *x = static_cast<const uint16_t *>(a.x) + (int64_t)t0 * a.ldx + k0;
         const bool wide = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && a.ldx % 8 == 0;
-        for (int e = threadIdx.x; e < tokens * n * 16; e += THREADS) {
-            const int t = e / (n * 16), k = 8 * (e % (n * 16));
-            const uint16_t *src = x + (int64_t)(t0 + t) * a.ldx + k0 + k;
-            uint16_t *dst = xs + t * pitch + k;
-            if (wide && k0 + k + 8 <= a.K) {
-                *reinterpret_cast<uint4 *>(dst) = *reinterpret_cast<const uint4 *>(src);
-            } else {
+        for (int t = 0; t < tokens; ++t, x += a.ldx) {
+            uint16_t *dst = xs + t * pitch;
+            for (int k = 8 * threadIdx.x; k < n * 128; k += 8 * THREADS) {
+                const int left = valid - k;
+                if (wide) {
+                    copy16(dst + k, left > 0 ? x + k : x, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
+                } else {
+                    uint16_t v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dst[i] = k0 + k + i < a.K ? src[i] : (uint16_t)0;
+                    for (int i = 0; i < 8; ++i) v[i] = i < left ? x[k + i] : (uint16_t)0;
+                    *reinterpret_cast<uint4 *>(dst + k) =
+                        make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
+                                   v[6] | (uint32_t)v[7] << 16);
+                }
             }
         }
+        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
     } else {
-        const float *x = static_cast<const float *>(a.x);
-        for (int e = threadIdx.x; e < tokens * n * 128; e += THREADS) {
-            const int t = e / (n * 128), k = e % (n * 128);
-            uint16_t p[3] = {0, 0, 0};
-            if (k0 + k < a.K) split3(x[(int64_t)(t0 + t) * a.ldx + k0 + k], p);
+        constexpr int U = 4;                                         // loads in flight
+        const float *x = static_cast<const float *>(a.x) + (int64_t)t0 * a.ldx + k0;
+        const bool wide = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && a.ldx % 4 == 0;
+        const int per = n * 32, all = tokens * per;                  // fours of a column, of all
+        for (int e0 = threadIdx.x; e0 < all; e0 += U * THREADS) {
+            float4 v[U];
 #pragma unroll
-            for (int i = 0; i < 3; ++i) xs[(3 * t + i) * pitch + k] = p[i];
+            for (int u = 0; u < U; ++u) {
+                const int e = e0 + u * THREADS, t = e / per, k = 4 * (e - t * per), left = valid - k;
+                v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                if (e >= all) continue;
+                const float *src = x + (int64_t)t * a.ldx + k;
+                if (wide && left >= 4) {
+                    v[u] = *reinterpret_cast<const float4 *>(src);
+                } else {
+                    if (left > 0) v[u].x = src[0];
+                    if (left > 1) v[u].y = src[1];
+                    if (left > 2) v[u].z = src[2];
+                    if (left > 3) v[u].w = src[3];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = e0 + u * THREADS, t = e / per, k = 4 * (e - t * per);
+                if (e >= all) break;
+                uint16_t p[4][3];
+                split3(v[u].x, p[0]);
+                split3(v[u].y, p[1]);
+                split3(v[u].z, p[2]);
+                split3(v[u].w, p[3]);
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    *reinterpret_cast<uint2 *>(xs + (3 * t + i) * pitch + k) =
+                        make_uint2(p[0][i] | (uint32_t)p[1][i] << 16, p[2][i] | (uint32_t)p[3][i] << 16);
+            }
         }
     }
 }
 
+constexpr int DEPTH = 4;              // blocks of 128 values that a warp has in flight
+
 // NT: tiles of 8 columns; FL: words of a lane's four that share a scale (1, 2, 4 for groups of 32, 64, 128 and more).
 template <int NT, int FL>
-__global__ void __launch_bounds__(THREADS) matvec_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, 2) matvec_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
     extern __shared__ __align__(16) uint8_t smem[];
@@ -189,48 +231,69 @@ __global__ void __launch_bounds__(THREADS) matvec_kernel(Args a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) tot[n][i] = 0.0f;
 
+    // codes and scales of the warp's next DEPTH blocks
+    uint4 u0[DEPTH], u1[DEPTH];
+    uint32_t f0[DEPTH], f1[DEPTH];                                     // lane t: the scale of word t
+    auto fetch = [&](int d, int kb) {
+        if (kb >= last) return;
+        u0[d] = __ldcs(w0 + kb * 4);
+        u1[d] = __ldcs(w1 + kb * 4);
+        const int sg = FL == 4 ? (a.gb == 1 ? kb : kb / a.gb) : kb * (4 / FL) + t / FL;
+        f0[d] = sg < a.groups ? s0[sg] : 0u;                           // a group past the last holds padding only
+        f1[d] = sg < a.groups ? s1[sg] : 0u;
+    };
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d) fetch(d, first + wk + d * nk);
+
     for (int c0 = first; c0 < last; c0 += a.xblocks) {
         const int nb = min(a.xblocks, last - c0), pitch = nb * 128 + 32;
         __syncthreads();
         stage(a, xs, t0, tokens, c0, nb);
         __syncthreads();
-        for (int kb = c0 + wk; kb < c0 + nb; kb += nk) {
-            const uint4 u0 = w0[kb * 4], u1 = w1[kb * 4];
-            const uint32_t q0[4] = {u0.x, u0.y, u0.z, u0.w}, q1[4] = {u1.x, u1.y, u1.z, u1.w};
-            float acc[NT][4];
+        for (int k0 = c0 + wk; k0 < c0 + nb; k0 += DEPTH * nk) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if (j % FL == 0) {
+            for (int d = 0; d < DEPTH; ++d) {
+                const int kb = k0 + d * nk;
+                if (kb >= c0 + nb) break;
+                const uint32_t q0[4] = {u0[d].x, u0[d].y, u0[d].z, u0[d].w}, q1[4] = {u1[d].x, u1[d].y, u1[d].z, u1[d].w};
+                float h0[4 / FL], h1[4 / FL];
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+                for (int s = 0; s < 4 / FL; ++s) {
+                    h0[s] = __uint_as_float((FL == 4 ? f0[d] : __shfl_sync(0xffffffffu, f0[d], s * FL, 4)) << 16);
+                    h1[s] = __uint_as_float((FL == 4 ? f1[d] : __shfl_sync(0xffffffffu, f1[d], s * FL, 4)) << 16);
                 }
-                uint32_t a0[4], a1[4];
+                fetch(d, kb + DEPTH * nk);
+                float acc[NT][4];
 #pragma unroll
-                for (int p = 0; p < 4; ++p) {
-                    a0[p] = levels(q0[j], p);
-                    a1[p] = levels(q1[j], p);
-                }
+                for (int j = 0; j < 4; ++j) {
+                    if (j % FL == 0) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    uint4 b = make_uint4(0, 0, 0, 0);
-                    if (n * 8 + g < cols)
-                        b = *reinterpret_cast<const uint4 *>(xs + (n * 8 + g) * pitch + (kb - c0) * 128 + 32 * j + 8 * t);
-                    mma(acc[n], a0[0], a1[0], a0[1], a1[1], b.x, b.y);
-                    mma(acc[n], a0[2], a1[2], a0[3], a1[3], b.z, b.w);
-                }
-                if (j % FL == FL - 1) {
-                    const int sg = FL == 4 ? (a.gb == 1 ? kb : kb / a.gb) : kb * (4 / FL) + j / FL;
-                    // a group past the last holds padding only
-                    const float f0 = sg < a.groups ? __uint_as_float((uint32_t)s0[sg] << 16) : 0.0f;
-                    const float f1 = sg < a.groups ? __uint_as_float((uint32_t)s1[sg] << 16) : 0.0f;
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+                    }
+                    uint32_t a0[4], a1[4];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        a0[p] = levels(q0[j], p);
+                        a1[p] = levels(q1[j], p);
+                    }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        tot[n][0] = fmaf(f0, acc[n][0], tot[n][0]);
-                        tot[n][1] = fmaf(f0, acc[n][1], tot[n][1]);
-                        tot[n][2] = fmaf(f1, acc[n][2], tot[n][2]);
-                        tot[n][3] = fmaf(f1, acc[n][3], tot[n][3]);
+                        uint4 b = make_uint4(0, 0, 0, 0);
+                        if (n * 8 + g < cols)
+                            b = *reinterpret_cast<const uint4 *>(xs + (n * 8 + g) * pitch + (kb - c0) * 128 + 32 * j + 8 * t);
+                        mma(acc[n], a0[0], a1[0], a0[1], a1[1], b.x, b.y);
+                        mma(acc[n], a0[2], a1[2], a0[3], a1[3], b.z, b.w);
+                    }
+                    if (j % FL == FL - 1) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            tot[n][0] = fmaf(h0[j / FL], acc[n][0], tot[n][0]);
+                            tot[n][1] = fmaf(h0[j / FL], acc[n][1], tot[n][1]);
+                            tot[n][2] = fmaf(h1[j / FL], acc[n][2], tot[n][2]);
+                            tot[n][3] = fmaf(h1[j / FL], acc[n][3], tot[n][3]);
+                        }
                     }
                 }
             }
@@ -290,7 +353,7 @@ static cudaError_t pack(const void *w, int O, int K, int Kp, int group, const mi
 template <int NT, int FL>
 static cudaError_t launch(const Args &a, dim3 grid, size_t smem, cudaStream_t s) {
     auto kern = matvec_kernel<NT, FL>;
-    if (!allow_shared(reinterpret_cast<const void *>(kern), 160 * 1024)) return cudaErrorInvalidValue;
+    if (!allow_shared(reinterpret_cast<const void *>(kern), 112 * 1024)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(THREADS);
@@ -360,16 +423,30 @@ minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T
     const int passes = (T + a.tokens - 1) / a.tokens, cols = a.tokens * a.parts, NT = (cols + 7) / 8;
     if (passes > 65535) return MINW_EUNSUPPORTED;
     const int nb = a.Kp / 128, sms = num_sms() > 0 ? num_sms() : 152;
-    // rows of a CTA: 16 per warp along them; K is split over the other warps, then over a cluster's CTAs, until
-    // there are two CTAs for each SM
-    a.wr = 1;
-    while (a.wr < 8 && (int64_t)((O + 32 * a.wr - 1) / (32 * a.wr)) >= 2 * sms) a.wr *= 2;
-    const int tiles = (O + 16 * a.wr - 1) / (16 * a.wr), nk = w4::WARPS / a.wr;
-    a.split = 1;
-    while (a.split < 8 && (int64_t)tiles * a.split < 2 * sms && nb >= 2 * a.split * nk) a.split *= 2;
-    a.bpc = (nb + a.split - 1) / a.split;
-    int xb = (96 * 1024 / 2 / cols - 32) / 128;                      // at most 96 KB of x
-    xb = xb < 1 ? 1 : xb / nk * nk > 0 ? xb / nk * nk : xb;
+    // Rows of a CTA (16 for each of wr warps side by side; the other warps split K) and CTAs of a cluster (which split K
+    // too): the pair with the least estimated time, waves of two CTAs per SM times a CTA's clocks -- its share of the
+    // memory rate for the codes, of L2's for x (fp32 values are split into parts as well), and a fixed part.
+    double best = 1e30;
+    for (int wr = 1; wr <= w4::WARPS; wr *= 2)
+        for (int split = 1; split <= 8; split *= 2) {
+            const int64_t tiles = (O + 16 * wr - 1) / (16 * wr);
+            const int bpc = (nb + split - 1) / split;
+            if (split > 1 && bpc * split - nb >= bpc) continue;                   // a CTA without a block
+            const int round = w4::WARPS / wr * w4::DEPTH;                         // x in shared memory: a round at least
+            if ((bpc < round ? bpc : round) * cols > 400) continue;               // (100 KB)
+            const int steps = (bpc * wr + w4::WARPS - 1) / w4::WARPS * w4::WARPS / wr;     // blocks, the warps' last ones whole
+            const double clocks = steps * (wr * 1024 / 11.0) + bpc * a.tokens * 128 * (a.x_bf16 ? 0.06 : 0.28) + 2500;
+            const double t = (double)((tiles * split * passes + 2 * sms - 1) / (2 * sms)) * clocks;
+            if (t < best) {
+                best = t;
+                a.wr = wr;
+                a.split = split;
+                a.bpc = bpc;
+            }
+        }
+    const int tiles = (O + 16 * a.wr - 1) / (16 * a.wr), unit = w4::WARPS / a.wr * w4::DEPTH;
+    int xb = 400 / cols;                                             // at most 100 KB of x at a time, whole rounds of the warps
+    xb = xb / unit * unit > 0 ? xb / unit * unit : unit;
     a.xblocks = a.bpc < xb ? a.bpc : xb;
     size_t smem = (size_t)cols * (a.xblocks * 128 + 32) * 2;
     const size_t red = (size_t)w4::WARPS * 16 * 8 * NT * sizeof(float);

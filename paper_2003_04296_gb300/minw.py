@@ -262,8 +262,10 @@ def _host_ptr(a):
 
 
 def _stream(stream):
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return ctypes.c_void_p(s.cuda_stream)
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    # the current stream's handle without a Stream object around it (3 us of a call's host time)
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 _VALUE_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
@@ -276,14 +278,25 @@ def _value_type(t):
         raise ValueError(f"float32 or bfloat16 expected, got {t.dtype}") from None
 
 
+def _addr(t):
+    """_ptr as a plain number (the calls on small tensors are bound by the host)."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise ValueError("device tensor expected")
+    if not t.is_contiguous():
+        raise ValueError("contiguous tensor expected")
+    return t.data_ptr()
+
+
 def _rows(t):
-    """(pointer, row length) of a channels-last tensor [..., C] whose rows lie a fixed number of elements apart (the
+    """(address, row length) of a channels-last tensor [..., C] whose rows lie a fixed number of elements apart (the
     first C channels of a wider buffer, for instance)."""
     if not t.is_cuda:
         raise ValueError("device tensor expected")
-    size, stride = t.shape, t.stride()
     if t.is_contiguous():
-        return t.data_ptr(), size[-1]
+        return t.data_ptr(), t.size(-1)
+    size, stride = t.shape, t.stride()
     if size[-1] != 1 and stride[-1] != 1:
         raise ValueError("the last dimension has to be contiguous")
     ld, inner = None, 1                   # row length, rows inside the dimension
@@ -301,16 +314,16 @@ def _rows(t):
 
 
 def _f32(t, n, what):
-    """Pointer of a dense fp32 vector of n values (None passes)."""
+    """Address of a dense fp32 vector of n values (None passes)."""
     if t is None:
         return None
     if t.dtype != torch.float32 or t.numel() != n:
         raise ValueError(f"{what}: {n} float32 values expected")
-    return _ptr(t)
+    return _addr(t)
 
 
 def _scratch(workspace):
-    return (None, 0) if workspace is None else (_ptr(workspace), workspace.numel() * workspace.element_size())
+    return (None, 0) if workspace is None else (_addr(workspace), workspace.numel() * workspace.element_size())
 
 
 def quant(bits, thr=(0.0, 0.0, 0.0), scale=1.0):
@@ -870,8 +883,8 @@ def minw_group_norm_workspace_bytes(B, P, C, groups, backward=False):
 def _image_rows(x, groups):
     if x.dim() < 2:
         raise ValueError("[B, ..., C] expected")
-    B, C = x.shape[0], x.shape[-1]
-    return B, math.prod(x.shape[1:-1]), C, int(groups)
+    shape = x.shape
+    return shape[0], math.prod(shape[1:-1]), shape[-1], int(groups)
 
 
 def minw_group_norm(x, gamma, beta, groups, eps, y, act=ACT_NONE, mean=None, rstd=None, workspace=None, stream=None):
@@ -974,7 +987,7 @@ def _w4(codes, scales, O, K, group):
         raise ValueError("codes and scales of w4_shapes(O, K, group) expected")
     if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
         raise ValueError("codes uint8 and scales bfloat16 expected")
-    return _ptr(codes), _ptr(scales)
+    return _addr(codes), _addr(scales)
 
 
 def minw_pack_w4(w, group, codes, scales, q=None, channel_scale=None, stream=None):
