@@ -612,9 +612,9 @@ typedef struct {
 } minw_tensor;
 
 /* Global gradient norm: *norm (device) = sqrt(sum over all tensors of g^2),
- * squares summed in fp32 within a block of at most 32768 values and in fp64
- * across blocks; a block whose squares leave fp32's range is summed again in
- * fp64, so the norm is right wherever it is an fp32 number.  Infinite
+ * squares summed in fp32 up to 32 at a time, those sums with compensation and
+ * in fp64 across blocks; a block whose squares leave fp32's range is summed
+ * again in fp64, so the norm is right wherever it is an fp32 number.  Infinite
  * or NaN gradients give an infinite or NaN norm.  grads: host array, read
  * during the call.  The sums' order is fixed by the lengths (the same bits
  * on every call).  workspace: device scratch of
@@ -622,7 +622,7 @@ typedef struct {
  * before and after.  count = 0 writes 0.
  * Errors: MINW_EINVAL (count < 0, null grads, norm or workspace, a tensor with
  * n < 0, null data with n > 0, unknown type, misaligned data; short
- * workspace), MINW_EUNSUPPORTED (2^46 values or more). */
+ * workspace), MINW_EUNSUPPORTED (2^42 values or more). */
 MINW_API size_t minw_grad_workspace_bytes(int32_t count);
 MINW_API minw_status minw_grad_norm(const minw_tensor *grads, int32_t count, float *norm, void *workspace,
                                     size_t workspace_bytes, void *stream);

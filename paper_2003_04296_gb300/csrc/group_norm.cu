@@ -161,28 +161,26 @@ struct GroupSum {
     float part[THREADS * GPT], total[MAX_SLAB_GROUPS];
 };
 template <int GPT>
-__device__ __forceinline__ void group_sum(float *s, GroupSum<GPT> &sm, const Args &a, const Tile &w, int per) {
-    const int groups = a.L * GPT / per, lane = threadIdx.x & 31;
+__device__ __forceinline__ void group_sum(float *s, GroupSum<GPT> &sm, const Args &a, const Tile &w) {
+    const int lane = threadIdx.x & 31, at = a.by_per.div(w.lane * GPT);
     if (a.butterfly) {
-        // lanes 32 apart in a row or in a group of one are powers of two apart: exchanges within a warp, then the
-        // eight warps' sums
+        // lanes of a warp with the same channels, then those of a group, by exchanges; then the eight warps' sums
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1)
-            if (d < per || d >= a.L) {
+            if (d < a.per || d >= a.L) {
 #pragma unroll
                 for (int g = 0; g < GPT; ++g) s[g] += __shfl_xor_sync(0xffffffffu, s[g], d);
             }
-        const int at = w.lane * GPT / per;
-        if (lane < a.L && lane % per == 0) {
+        if (lane < a.L && (lane & (a.per - 1)) == 0) {
 #pragma unroll
-            for (int g = 0; g < GPT; ++g) sm.part[(threadIdx.x >> 5) * groups + at + g] = s[g];
+            for (int g = 0; g < GPT; ++g) sm.part[(threadIdx.x >> 5) * a.groups + at + g] = s[g];
         }
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < GPT; ++g) {
             s[g] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < THREADS / 32; ++k) s[g] += sm.part[k * groups + at + g];
+            for (int k = 0; k < THREADS / 32; ++k) s[g] += sm.part[k * a.groups + at + g];
         }
     } else {
         const int row = a.L * GPT;
@@ -191,15 +189,18 @@ __device__ __forceinline__ void group_sum(float *s, GroupSum<GPT> &sm, const Arg
             for (int g = 0; g < GPT; ++g) sm.part[w.row * row + w.lane * GPT + g] = s[g];
         }
         __syncthreads();
-        for (int g = threadIdx.x >> 5; g < groups; g += THREADS / 32) {      // a warp per group
+        for (int g = threadIdx.x >> 5; g < a.groups; g += THREADS / 32) {      // a warp per group
             float t = 0.0f;
-            for (int e = lane; e < w.rows * per; e += 32) t += sm.part[e / per * row + g * per + e % per];
+            for (int e = lane; e < w.rows * a.per; e += 32) {
+                const int r = a.by_per.div(e);
+                t += sm.part[r * row + g * a.per + e - r * a.per];
+            }
             t = warp_sum(t);
             if (lane == 0) sm.total[g] = t;
         }
         __syncthreads();
 #pragma unroll
-        for (int g = 0; g < GPT; ++g) s[g] = sm.total[(w.lane * GPT + g) / per];
+        for (int g = 0; g < GPT; ++g) s[g] = sm.total[a.by_per.div(w.lane * GPT + g)];
     }
 }
 
@@ -210,106 +211,88 @@ template <typename T, typename TY, int V, int GPT, int NV>
 __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int W = V / GPT, NP = V / 2 > 0 ? V / 2 : 1;
+    constexpr int W = V / GPT, NP = (V + 1) / 2;
     __shared__ GroupSum<GPT> sums[2];
     __shared__ float2 cta[MAX_SLAB_GROUPS], all[MAX_SLAB_GROUPS];
     const Tile w = tile<V>(a);
     const T *x = static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c;
+    const int64_t step = (int64_t)w.rows * a.ldx;
     Vec<T, V> v[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
-        if (i < w.n) v[i].load(x + (int64_t)(i * w.rows) * a.ldx);
+        if (i < w.n) v[i].load(x + i * step);
 
-    const int per = a.Cg / W, groups = a.L * GPT / per;
     float mean[GPT], m2[GPT];
     {
-        const float inv = w.n > 0 ? 1.0f / (float)(w.n * W) : 0.0f;
+        // pairs of channels: of one group, or (W = 1) of two
+        Pair s[NP], q[NP];
+#pragma unroll
+        for (int k = 0; k < NP; ++k) s[k] = q[k] = pair(0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < w.n) {
+#pragma unroll
+                for (int k = 0; k < NP; ++k) s[k] = add2(s[k], v[i].get2(k));
+            }
+        auto fold = [&](const Pair *p, float *f) {
+            if constexpr (W == 1) {
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const float2 h = halves(p[k]);
+                    f[2 * k] = h.x;
+                    if (V > 1) f[2 * k + 1] = h.y;
+                }
+            } else {
+#pragma unroll
+                for (int g = 0; g < GPT; ++g) {
+                    Pair t = p[g * W / 2];
+#pragma unroll
+                    for (int k = 1; k < W / 2; ++k) t = add2(t, p[g * W / 2 + k]);
+                    const float2 h = halves(t);
+                    f[g] = h.x + h.y;
+                }
+            }
+        };
+        fold(s, mean);
+        const float values = (float)(w.n * W), inv = w.n > 0 ? __fdividef(1.0f, values) : 0.0f;
         float own[GPT];
-        if constexpr (V == 1) {
-            float s = 0.0f, q = 0.0f;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < w.n) s += v[i].get(0);
-            own[0] = s * inv;
+        for (int g = 0; g < GPT; ++g) own[g] = mean[g] * inv;
 #pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < w.n) {
-                    const float d = v[i].get(0) - own[0];
-                    q = fmaf(d, d, q);
+        for (int i = 0; i < NV; ++i)
+            if (i < w.n) {
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const Pair d = add2(v[i].get2(k), pick_group<V, W>(own, k, -1.0f));
+                    q[k] = fma2(d, d, q[k]);
                 }
-            mean[0] = s;
-            m2[0] = q;
-        } else {
-            // pairs of channels: of one group, or (W = 1) of two
-            Pair s[NP], q[NP];
-#pragma unroll
-            for (int k = 0; k < NP; ++k) s[k] = q[k] = pair(0.0f, 0.0f);
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < w.n) {
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) s[k] = add2(s[k], v[i].get2(k));
-                }
-            auto fold = [&](const Pair *p, float *f) {
-                if constexpr (W == 1) {
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const float2 h = halves(p[k]);
-                        f[2 * k] = h.x;
-                        f[2 * k + 1] = h.y;
-                    }
-                } else {
-#pragma unroll
-                    for (int g = 0; g < GPT; ++g) {
-                        Pair t = p[g * W / 2];
-#pragma unroll
-                        for (int k = 1; k < W / 2; ++k) t = add2(t, p[g * W / 2 + k]);
-                        const float2 h = halves(t);
-                        f[g] = h.x + h.y;
-                    }
-                }
-            };
-            fold(s, mean);
-#pragma unroll
-            for (int g = 0; g < GPT; ++g) own[g] = mean[g] * inv;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < w.n) {
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const Pair d = add2(v[i].get2(k), pair(-own[2 * k / W], -own[(2 * k + 1) / W]));
-                        q[k] = fma2(d, d, q[k]);
-                    }
-                }
-            fold(q, m2);
-        }
-        group_sum<GPT>(mean, sums[0], a, w, per);
-        const float np = (float)(w.p1 - w.p0) * (float)a.Cg;
+            }
+        fold(q, m2);
+        group_sum<GPT>(mean, sums[0], a, w);
+        const float block = w.p1 > w.p0 ? __fdividef(1.0f, (float)(w.p1 - w.p0) * (float)a.Cg) : 0.0f;
 #pragma unroll
         for (int g = 0; g < GPT; ++g) {
-            mean[g] = w.p1 > w.p0 ? mean[g] / np : 0.0f;
+            mean[g] *= block;
             const float d = own[g] - mean[g];
-            if (w.n > 0) m2[g] = fmaf(d * d, (float)(w.n * W), m2[g]);
+            if (w.n > 0) m2[g] = fmaf(d * d, values, m2[g]);
         }
-        group_sum<GPT>(m2, sums[1], a, w, per);
+        group_sum<GPT>(m2, sums[1], a, w);
     }
 
-    cg::cluster_group cluster = cg::this_cluster();
-    const float total = (float)a.P * (float)a.Cg;
     float rstd[GPT];
     if (a.chunks > 1) {
         // the cluster's blocks: sixteen threads a group, one for each; the same sums in every block
         if (w.row == 0) {
 #pragma unroll
-            for (int g = 0; g < GPT; ++g)
-                if ((w.lane * GPT + g) % per == 0) cta[(w.lane * GPT + g) / per] = make_float2(mean[g], m2[g]);
+            for (int g = 0; g < GPT; ++g) cta[a.by_per.div(w.lane * GPT + g)] = make_float2(mean[g], m2[g]);
         }
+        cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
-        for (int g = threadIdx.x >> 4; g < (groups + 1) / 2 * 2; g += THREADS / 16) {    // both halves of a warp alike
+        for (int g = threadIdx.x >> 4; g < (a.groups + 1) / 2 * 2; g += THREADS / 16) {    // both halves of a warp alike
             const int k = threadIdx.x & 15;
             float2 t = make_float2(0.0f, 0.0f);
             float n = 0.0f;
-            if (k < a.chunks && g < groups) {
+            if (k < a.chunks && g < a.groups) {
                 t = *cluster.map_shared_rank(&cta[g], k);
                 const int q0 = min(a.P, k * a.ppc);
                 n = (float)(min(a.P, q0 + a.ppc) - q0) * (float)a.Cg;
@@ -317,63 +300,56 @@ __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused
             float s = n * t.x;
 #pragma unroll
             for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-            s /= total;
+            s *= a.inv_total;
             const float d0 = t.x - s;
             float q = n > 0.0f ? fmaf(d0 * d0, n, t.y) : 0.0f;
 #pragma unroll
             for (int d = 8; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-            if (k == 0 && g < groups) all[g] = make_float2(s, q);
+            if (k == 0 && g < a.groups) all[g] = make_float2(s, q);
         }
-        cluster.barrier_arrive();
+        cluster_done_reading();
         __syncthreads();
 #pragma unroll
         for (int g = 0; g < GPT; ++g) {
-            const float2 t = all[(w.lane * GPT + g) / per];
+            const float2 t = all[a.by_per.div(w.lane * GPT + g)];
             mean[g] = t.x;
             m2[g] = t.y;
         }
     }
 #pragma unroll
-    for (int g = 0; g < GPT; ++g) rstd[g] = 1.0f / sqrtf(m2[g] / total + a.eps);
+    for (int g = 0; g < GPT; ++g) rstd[g] = rsqrtf(fmaf(m2[g], a.inv_total, a.eps));
     if (w.rank == 0 && w.row == 0) {
 #pragma unroll
-        for (int g = 0; g < GPT; ++g)
-            if ((w.lane * GPT + g) % per == 0) {
-                const int64_t at = (int64_t)w.b * a.G + w.slab * groups + (w.lane * GPT + g) / per;
-                if (a.mean) a.mean[at] = mean[g];
-                if (a.rstd) a.rstd[at] = rstd[g];
-            }
+        for (int g = 0; g < GPT; ++g) {
+            const int64_t at = (int64_t)w.b * a.G + w.slab * a.groups + a.by_per.div(w.lane * GPT + g);
+            if (a.mean) a.mean[at] = mean[g];
+            if (a.rstd) a.rstd[at] = rstd[g];
+        }
     }
     if (w.n > 0) {
         float ga[V], be[V];
         load_affine<V>(a, w.c, ga, be);
         TY *y = static_cast<TY *>(a.y) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldy + w.c;
+        const int64_t ystep = (int64_t)w.rows * a.ldy;
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < w.n) {
-                    float z[V];
-                    if constexpr (V == 1) {
-                        z[0] = fmaf((v[i].get(0) - mean[0]) * rstd[0], ga[0], be[0]);
-                    } else {
+                    float z[2 * NP];
 #pragma unroll
-                        for (int k = 0; k < NP; ++k) {
-                            const int g0 = 2 * k / W, g1 = (2 * k + 1) / W;
-                            const Pair xh = mul2(add2(v[i].get2(k), pair(-mean[g0], -mean[g1])), pair(rstd[g0], rstd[g1]));
-                            const float2 h = halves(fma2(xh, pair(ga[2 * k], ga[2 * k + 1]), pair(be[2 * k], be[2 * k + 1])));
-                            z[2 * k] = h.x;
-                            z[2 * k + 1] = h.y;
-                        }
+                    for (int k = 0; k < NP; ++k) {
+                        const Pair xh = mul2(add2(v[i].get2(k), pick_group<V, W>(mean, k, -1.0f)), pick_group<V, W>(rstd, k));
+                        const float2 h = halves(fma2(xh, pick<V>(ga, k), pick<V>(be, k)));
+                        z[2 * k] = act_value<act.value>(h.x);
+                        z[2 * k + 1] = act_value<act.value>(h.y);
                     }
-#pragma unroll
-                    for (int k = 0; k < V; ++k) z[k] = act_value<act.value>(z[k]);
                     Vec<TY, V> o;
                     o.set(z);
-                    o.store(y + (int64_t)(i * w.rows) * a.ldy);
+                    o.store(y + i * ystep);
                 }
         });
     }
-    if (a.chunks > 1) cluster.barrier_wait();              // no block leaves while its sums are read
+    if (a.chunks > 1) cluster_leave();
 }
 
 template <typename T, typename TY, int V, int GPT>
@@ -391,8 +367,11 @@ static minw_status forward(Args a, int V, cudaStream_t s) {
                            : pl.V == 4 ? (pl.GPT == 1 ? fused_of<T, TY, 4, 1>(pl.NV) : pl.GPT == 2 ? fused_of<T, TY, 4, 2>(pl.NV)
                                                                                        : fused_of<T, TY, 4, 4>(pl.NV))
                                        : nullptr;
-        if constexpr (sizeof(T) == 2)
-            if (pl.V == 8) kern = pl.GPT == 1 ? fused_of<T, TY, 8, 1>(pl.NV) : fused_of<T, TY, 8, 2>(pl.NV);
+        if constexpr (sizeof(T) == 2 && sizeof(TY) == 2)
+            if (pl.V == 8)
+                kern = pl.GPT == 1   ? fused_of<T, TY, 8, 1>(pl.NV)
+                       : pl.GPT == 2 ? fused_of<T, TY, 8, 2>(pl.NV)
+                                     : fused_of<T, TY, 8, 4>(pl.NV);
         if (launch_cluster(kern, blocks, s, f) != cudaSuccess) return MINW_ECUDA;
         return launch_status();
     }
@@ -401,7 +380,7 @@ static minw_status forward(Args a, int V, cudaStream_t s) {
     if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
     void (*stat)(Args) = V == 4 ? stat_kernel<T, 4> : stat_kernel<T, 1>;
     void (*apply)(Args) = V == 4 ? apply_kernel<T, TY, 4> : apply_kernel<T, TY, 1>;
-    if constexpr (sizeof(T) == 2)
+    if constexpr (sizeof(T) == 2 && sizeof(TY) == 2)
         if (V == 8) {
             stat = stat_kernel<T, 8>;
             apply = apply_kernel<T, TY, 8>;
@@ -448,7 +427,7 @@ minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const fl
     a.chunks = (int)((P + a.ppc - 1) / a.ppc);                // no chunk without a pixel
     a.part = reinterpret_cast<float2 *>(ws + l.part);
     a.stat = reinterpret_cast<float2 *>(ws + l.stat);
-    int V = x_type == MINW_BF16 ? 8 : 4;
+    int V = x_type == MINW_BF16 && y_type == MINW_BF16 ? 8 : 4;       // 16 bytes of the wider type
     while (V > 1 && (C % V != 0 || !gn::fits(x, ldx, x_type, V) || !gn::fits(y, ldy, y_type, V))) V = V == 8 ? 4 : 1;
     cudaStream_t s = (cudaStream_t)stream;
     if (x_type == MINW_BF16)

@@ -43,7 +43,12 @@ struct Args {
     float eps;
     int chunks, ppc;               // pixel chunks per image, pixels per chunk
     int L, slabs;                  // lanes (V channels each) of a slab, slabs of a row
-    int butterfly;                 // one pass: lanes and the lanes of a group are powers of two within a warp
+    // one pass
+    int butterfly;                 // lanes and the lanes of a group are powers of two within a warp
+    int rows, groups, per;         // pixel rows of a block, groups of a slab, entries (a thread's share of a group) of a group
+    float inv_total;               // 1 / (P Cg)
+    int seg;                       // backward: threads that sum a channel's rows
+    Div by_L, by_rows, by_per, by_chunks, by_slabs, by_channels;
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -97,18 +102,29 @@ struct Tile {
 template <int V>
 __device__ __forceinline__ Tile tile(const Args &a) {
     Tile w;
-    w.rank = (int)(blockIdx.x % a.chunks);
-    const unsigned bs = blockIdx.x / a.chunks;
-    w.slab = (int)(bs % a.slabs);
-    w.b = (int)(bs / a.slabs);
+    const int bs = a.by_chunks.div((int)blockIdx.x);
+    w.rank = (int)blockIdx.x - bs * a.chunks;
+    w.b = a.by_slabs.div(bs);
+    w.slab = bs - w.b * a.slabs;
     w.p0 = min(a.P, w.rank * a.ppc);
     w.p1 = min(a.P, w.p0 + a.ppc);
-    w.lane = (int)threadIdx.x % a.L;
-    w.row = (int)threadIdx.x / a.L;
-    w.rows = THREADS / a.L;
+    w.row = a.by_L.div((int)threadIdx.x);
+    w.lane = (int)threadIdx.x - w.row * a.L;
+    w.rows = a.rows;
     w.c = (w.slab * a.L + w.lane) * V;
-    w.n = w.row < w.rows && w.p0 + w.row < w.p1 ? (w.p1 - w.p0 - w.row - 1) / w.rows + 1 : 0;
+    w.n = w.row < w.rows && w.p0 + w.row < w.p1 ? a.by_rows.div(w.p1 - w.p0 - w.row - 1) + 1 : 0;
     return w;
+}
+
+// Halves 2 k and 2 k + 1 of V values (the second 0 for a single one).
+template <int V>
+__device__ __forceinline__ Pair pick(const float *f, int k) {
+    return pair(f[2 * k], V > 1 ? f[2 * k + 1] : 0.0f);
+}
+// The same from one value per group of W channels, negated or not.
+template <int V, int W>
+__device__ __forceinline__ Pair pick_group(const float *f, int k, float sign = 1.0f) {
+    return pair(sign * f[2 * k / W], V > 1 ? sign * f[(2 * k + 1) / W] : 0.0f);
 }
 
 // ---------------------------------------------------------------------------
@@ -172,8 +188,8 @@ struct Plan {
     int V, GPT, NV;
 };
 inline bool one_pass(Args &a, Plan &pl, int bytes, int V0, bool backward) {
-    pl.V = V0 == 8 && a.Cg % 4 != 0 ? 4 : V0;
-    pl.GPT = a.Cg % pl.V == 0 ? 1 : pl.V == 8 || a.Cg % 2 == 0 ? 2 : pl.V;
+    pl.V = V0 == 8 && a.Cg % 2 != 0 ? 4 : V0;
+    pl.GPT = a.Cg % pl.V == 0 ? 1 : pl.V == 8 ? (a.Cg % 4 == 0 ? 2 : 4) : a.Cg % 2 == 0 ? 2 : pl.V;
     for (int width = 128; width >= 32; width /= 2)
         for (int k = 1; k <= a.G && k <= MAX_SLAB_GROUPS; ++k) {
             const int channels = k * a.Cg;
@@ -185,11 +201,20 @@ inline bool one_pass(Args &a, Plan &pl, int bytes, int V0, bool backward) {
             pl.NV = pl.V == 1 ? 32 : backward || a.P <= 64 * rows ? 8 : 16;
             const int64_t cap = (int64_t)rows * pl.NV, cluster = (a.P + cap - 1) / cap;
             if (cluster > 16 || (backward && cluster > 1 && rows < 2)) break;     // a cluster's totals go behind the block's sums
-            const int W = pl.V / pl.GPT, lanes_of_group = a.Cg / W;
-            a.butterfly = L <= 32 && (L & (L - 1)) == 0 &&
-                          (lanes_of_group == 1 || (pl.GPT == 1 && (lanes_of_group & (lanes_of_group - 1)) == 0));
+            a.per = a.Cg / (pl.V / pl.GPT);
+            a.butterfly = L <= 32 && (L & (L - 1)) == 0 && (a.per == 1 || (pl.GPT == 1 && (a.per & (a.per - 1)) == 0));
+            a.rows = rows;
+            a.groups = k;
             a.L = L;
             a.slabs = a.G / k;
+            a.inv_total = (float)(1.0 / ((double)a.P * a.Cg));
+            a.seg = channels >= THREADS ? 1 : THREADS / channels < rows ? THREADS / channels : rows;
+            a.by_channels = Div((uint32_t)channels);
+            a.by_L = Div(L);
+            a.by_rows = Div(rows);
+            a.by_per = Div(a.per);
+            a.by_chunks = Div((uint32_t)cluster);
+            a.by_slabs = Div((uint32_t)a.slabs);
             a.chunks = (int)cluster;
             a.ppc = (int)((a.P + cluster - 1) / cluster);
             return true;

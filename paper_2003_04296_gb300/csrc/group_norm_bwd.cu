@@ -167,14 +167,14 @@ __global__ void __launch_bounds__(THREADS) bwd_apply_kernel(Args a) {
 // ---------------------------------------------------------------------------
 
 template <typename T, typename TD, int V, int GPT, int NV>
-__global__ void __launch_bounds__(THREADS) fused_bwd_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, 2) fused_bwd_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int W = V / GPT;
+    constexpr int W = V / GPT, NP = (V + 1) / 2;
     __shared__ float2 red[THREADS * V];                    // rows x channels, then segments x channels
     __shared__ float2 group[MAX_SLAB_GROUPS];
     const Tile w = tile<V>(a);
-    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, xstep = (int64_t)w.rows * a.ldx, dstep = (int64_t)w.rows * a.lddy;
     const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
     const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
     Vec<T, V> v[NV];
@@ -182,67 +182,71 @@ __global__ void __launch_bounds__(THREADS) fused_bwd_kernel(Args a) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
         if (i < w.n) {
-            v[i].load(x + (int64_t)(i * w.rows) * a.ldx);
-            d[i].load(dy + (int64_t)(i * w.rows) * a.lddy);
+            v[i].load(x + i * xstep);
+            d[i].load(dy + i * dstep);
         }
-    const int CW = a.L * V, g0 = w.slab * (CW / a.Cg);     // channels of the slab, its first group
+    const int CW = a.L * V;                                // channels of the slab
     float ga[V], be[V], mean[GPT], rstd[GPT];
     load_affine<V>(a, w.c, ga, be);
 #pragma unroll
     for (int g = 0; g < GPT; ++g) {
-        const int64_t at = (int64_t)w.b * a.G + g0 + (w.lane * V + g * W) / a.Cg;
+        const int64_t at = (int64_t)w.b * a.G + w.slab * a.groups + a.by_per.div(w.lane * GPT + g);
         mean[g] = a.mean_in[at];
         rstd[g] = a.rstd_in[at];
     }
     {
-        float db[V], dg[V];
+        Pair db[NP], dg[NP];
 #pragma unroll
-        for (int k = 0; k < V; ++k) db[k] = dg[k] = 0.0f;
+        for (int k = 0; k < NP; ++k) db[k] = dg[k] = pair(0.0f, 0.0f);
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < w.n) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const float xh = (v[i].get(k) - mean[k / W]) * rstd[k / W];
-                        const float dz = act_grad<act.value>(fmaf(xh, ga[k], be[k]), d[i].get(k));
-                        db[k] += dz;
-                        dg[k] = fmaf(dz, xh, dg[k]);
+                    for (int k = 0; k < NP; ++k) {
+                        const Pair xh = mul2(add2(v[i].get2(k), pick_group<V, W>(mean, k, -1.0f)), pick_group<V, W>(rstd, k));
+                        const Pair dz = act_grad2<act.value>(fma2(xh, pick<V>(ga, k), pick<V>(be, k)), d[i].get2(k));
+                        db[k] = add2(db[k], dz);
+                        dg[k] = fma2(dz, xh, dg[k]);
                     }
                 }
         });
         if (w.row < w.rows) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) red[w.row * CW + w.lane * V + k] = make_float2(db[k], dg[k]);
+            for (int k = 0; k < NP; ++k) {
+                const float2 b = halves(db[k]), g = halves(dg[k]);
+                red[w.row * CW + w.lane * V + 2 * k] = make_float2(b.x, g.x);
+                if (V > 1) red[w.row * CW + w.lane * V + 2 * k + 1] = make_float2(b.y, g.y);
+            }
         }
     }
     __syncthreads();
-    // channel sums of this block: THREADS / CW threads a channel, each every so many rows (into row of its number)
-    const int seg = CW >= THREADS ? 1 : min(THREADS / CW, w.rows);
-    for (int e = threadIdx.x; e < seg * CW; e += THREADS) {
-        const int c = e % CW, s = e / CW;
+    // channel sums of this block: `seg` threads a channel, each every so many rows (into the row of its number)
+    for (int s = a.by_channels.div((int)threadIdx.x), c = (int)threadIdx.x - s * CW; s < a.seg;) {
         float2 t = red[s * CW + c];
-        for (int r = s + seg; r < w.rows; r += seg) {
+        for (int r = s + a.seg; r < w.rows; r += a.seg) {
             t.x += red[r * CW + c].x;
             t.y += red[r * CW + c].y;
         }
         red[s * CW + c] = t;
+        c += THREADS;                                      // more channels than threads: one segment
+        if (a.seg > 1 || c >= CW) break;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < CW; c += THREADS) {
         float2 t = red[c];
-        for (int s = 1; s < seg; ++s) {
+        for (int s = 1; s < a.seg; ++s) {
             t.x += red[s * CW + c].x;
             t.y += red[s * CW + c].y;
         }
         red[c] = t;
     }
-    cg::cluster_group cluster = cg::this_cluster();
     float2 *tot = red;
     if (a.chunks > 1) {
         // the cluster's blocks: their sums stay in place while the totals go behind them
+        cg::cluster_group cluster = cg::this_cluster();
         cluster.sync();
-        tot = w.rows > 1 ? red + CW : nullptr;
+        tot = red + CW;
         for (int c = threadIdx.x; c < CW; c += THREADS) {
             float2 t = make_float2(0.0f, 0.0f);
             for (int k = 0; k < a.chunks; ++k) {
@@ -252,13 +256,12 @@ __global__ void __launch_bounds__(THREADS) fused_bwd_kernel(Args a) {
             }
             tot[c] = t;
         }
-        cluster.barrier_arrive();
+        cluster_done_reading();
     }
     __syncthreads();
     if (w.rank == 0)
         for (int c = threadIdx.x; c < CW; c += THREADS) a.chan[(int64_t)w.b * a.C + w.slab * CW + c] = tot[c];
-    const float n = (float)a.P * (float)a.Cg;
-    for (int g = threadIdx.x >> 5; g < CW / a.Cg; g += THREADS / 32) {
+    for (int g = threadIdx.x >> 5; g < a.groups; g += THREADS / 32) {
         float s1 = 0.0f, s2 = 0.0f;
         for (int k = threadIdx.x & 31; k < a.Cg; k += 32) {
             const float2 t = tot[g * a.Cg + k];
@@ -268,36 +271,41 @@ __global__ void __launch_bounds__(THREADS) fused_bwd_kernel(Args a) {
         }
         s1 = warp_sum(s1);
         s2 = warp_sum(s2);
-        if ((threadIdx.x & 31) == 0) group[g] = make_float2(s1 / n, s2 / n);
+        if ((threadIdx.x & 31) == 0) group[g] = make_float2(s1 * a.inv_total, s2 * a.inv_total);
     }
     __syncthreads();
     if (w.n > 0) {
         float s1[GPT], s2[GPT];
 #pragma unroll
         for (int g = 0; g < GPT; ++g) {
-            const float2 t = group[(w.lane * V + g * W) / a.Cg];
+            const float2 t = group[a.by_per.div(w.lane * GPT + g)];
             s1[g] = t.x;
             s2[g] = t.y;
         }
         T *dx = static_cast<T *>(a.y) + p * a.ldy + w.c;
+        const int64_t ostep = (int64_t)w.rows * a.ldy;
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
                 if (i < w.n) {
-                    float o[V];
+                    float o[2 * NP];
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        const float xh = (v[i].get(k) - mean[k / W]) * rstd[k / W];
-                        const float dz = act_grad<act.value>(fmaf(xh, ga[k], be[k]), d[i].get(k));
-                        o[k] = rstd[k / W] * (fmaf(ga[k], dz, -s1[k / W]) - xh * s2[k / W]);
+                    for (int k = 0; k < NP; ++k) {
+                        const Pair r2 = pick_group<V, W>(rstd, k), gk = pick<V>(ga, k);
+                        const Pair xh = mul2(add2(v[i].get2(k), pick_group<V, W>(mean, k, -1.0f)), r2);
+                        const Pair dz = act_grad2<act.value>(fma2(xh, gk, pick<V>(be, k)), d[i].get2(k));
+                        const Pair t = fma2(gk, dz, pick_group<V, W>(s1, k, -1.0f));
+                        const float2 h = halves(mul2(r2, fma2(xh, pick_group<V, W>(s2, k, -1.0f), t)));
+                        o[2 * k] = h.x;
+                        o[2 * k + 1] = h.y;
                     }
                     Vec<T, V> r;
                     r.set(o);
-                    r.store(dx + (int64_t)(i * w.rows) * a.ldy);
+                    r.store(dx + i * ostep);
                 }
         });
     }
-    if (a.chunks > 1) cluster.barrier_wait();              // no block leaves while its sums are read
+    if (a.chunks > 1) cluster_leave();
 }
 
 // dbeta, dgamma: the images' channel sums, a warp per channel of 32, 8 rows of images side by side.
@@ -343,8 +351,11 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
                            : pl.V == 4 ? (pl.GPT == 1 ? fused_bwd_of<T, TD, 4, 1>() : pl.GPT == 2 ? fused_bwd_of<T, TD, 4, 2>()
                                                                                      : fused_bwd_of<T, TD, 4, 4>())
                                        : nullptr;
-        if constexpr (sizeof(T) == 2)
-            if (pl.V == 8) kern = pl.GPT == 1 ? fused_bwd_of<T, TD, 8, 1>() : fused_bwd_of<T, TD, 8, 2>();
+        if constexpr (sizeof(T) == 2 && sizeof(TD) == 2)
+            if (pl.V == 8)
+                kern = pl.GPT == 1   ? fused_bwd_of<T, TD, 8, 1>()
+                       : pl.GPT == 2 ? fused_bwd_of<T, TD, 8, 2>()
+                                     : fused_bwd_of<T, TD, 8, 4>();
         if (launch_cluster(kern, blocks, s, f) != cudaSuccess) return MINW_ECUDA;
     } else {
         lanes(a, V);
@@ -352,7 +363,7 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
         if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
         void (*sum)(Args) = V == 4 ? bwd_sum_kernel<T, TD, 4> : bwd_sum_kernel<T, TD, 1>;
         void (*apply)(Args) = V == 4 ? bwd_apply_kernel<T, TD, 4> : bwd_apply_kernel<T, TD, 1>;
-        if constexpr (sizeof(T) == 2)
+        if constexpr (sizeof(T) == 2 && sizeof(TD) == 2)
             if (V == 8) {
                 sum = bwd_sum_kernel<T, TD, 8>;
                 apply = bwd_apply_kernel<T, TD, 8>;
@@ -405,7 +416,7 @@ minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx,
     a.part = reinterpret_cast<float2 *>(ws + l.part);
     a.stat = reinterpret_cast<float2 *>(ws + l.stat);
     a.chan = reinterpret_cast<float2 *>(ws + l.chan);
-    int V = x_type == MINW_BF16 ? 8 : 4;
+    int V = x_type == MINW_BF16 && dy_type == MINW_BF16 ? 8 : 4;      // 16 bytes of the wider type
     while (V > 1 && (C % V != 0 || !gn::fits(x, ldx, x_type, V) || !gn::fits(dy, lddy, dy_type, V) ||
                      !gn::fits(dx, lddx, x_type, V)))
         V = V == 8 ? 4 : 1;

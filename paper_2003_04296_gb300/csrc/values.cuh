@@ -1,5 +1,6 @@
-// values.cuh -- vectors of fp32 or bf16 values as they lie in memory, and the
-// activations of the group norm and of the 4-bit products.
+// values.cuh -- what the kernels of a head share: vectors of fp32 or bf16 values
+// as they lie in memory, fp32 pairs, activations, the end of a cluster, division
+// by numbers the host knows.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -81,8 +82,8 @@ struct Vec {
         if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
         else return __uint_as_float((i & 1) ? (w[i >> 1] & 0xffff0000u) : (w[i >> 1] << 16));
     }
-    // values 2 k and 2 k + 1
-    __device__ __forceinline__ Pair get2(int k) const { return pair(get(2 * k), get(2 * k + 1)); }
+    // values 2 k and 2 k + 1 (0 past a single one)
+    __device__ __forceinline__ Pair get2(int k) const { return pair(get(2 * k), V > 1 ? get(2 * k + 1) : 0.0f); }
     // all V values at once: bf16 rounds to nearest even, two to a conversion
     __device__ __forceinline__ void set(const float *v) {
         if constexpr (sizeof(T) == 4) {
@@ -112,8 +113,14 @@ __device__ __forceinline__ float min_nan(float a, float b) {
     return r;
 }
 
-// 1 / (1 + e^-z): tends to 0 and 1 at both ends (e^-z = infinity gives 0).
-__device__ __forceinline__ float sigmoidf_(float z) { return __fdividef(1.0f, 1.0f + __expf(-z)); }
+// 1 / (1 + e^-z): tends to 0 and 1 at both ends (e^-z = infinity gives 0).  Two approximate instructions, each within
+// 2 ulp; the argument's rounding adds |z| 2^-24.
+__device__ __forceinline__ float sigmoidf_(float z) {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + e));
+    return r;
+}
 
 // y = act(z); a NaN stays one.
 template <int ACT>
@@ -135,6 +142,33 @@ __device__ __forceinline__ float act_grad(float z, float dy) {
     }
     return dy;
 }
+
+template <int ACT>
+__device__ __forceinline__ Pair act_grad2(Pair z, Pair dy) {
+    if constexpr (ACT == MINW_ACT_NONE) return dy;
+    const float2 zf = halves(z), df = halves(dy);
+    if constexpr (ACT == MINW_ACT_SILU) {
+        const Pair s = pair(sigmoidf_(zf.x), sigmoidf_(zf.y)), one = pair(1.0f, 1.0f);
+        return mul2(dy, mul2(s, fma2(z, fma2(s, pair(-1.0f, -1.0f), one), one)));
+    }
+    return pair(act_grad<ACT>(zf.x, df.x), act_grad<ACT>(zf.y, df.y));
+}
+
+// The end of a cluster: no block leaves while others read its shared memory.  Arriving needs no memory ordering, the
+// values read have been used by then.
+__device__ __forceinline__ void cluster_done_reading() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_leave() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
+
+// n / d for 0 <= n < 2^31 with the divisor known on the host: a product's upper half and a shift.
+struct Div {
+    uint32_t d = 1, m = 1, s = 0;
+    Div() = default;
+    explicit Div(uint32_t by) : d(by) {
+        while ((1ull << s) < by) ++s;
+        m = (uint32_t)(((1ull << 32) * ((1ull << s) - by)) / by + 1);
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)((__umulhi(m, (uint32_t)n) + (uint32_t)n) >> s); }
+};
 
 // f(std::integral_constant<int, act>): the choice once around a loop, not at each value.
 template <typename F>

@@ -32,7 +32,7 @@ namespace cg = cooperative_groups;
 namespace minw {
 namespace w4 {
 
-constexpr int THREADS = 256, WARPS = THREADS / 32;
+constexpr int THREADS = 256;          // of a packing block
 
 // ---------------------------------------------------------------------------
 // Packing
@@ -99,18 +99,20 @@ struct Args {
     const uint16_t *scales;
     const float *scale, *shift;
     void *y;
-    int T, O, K, Kp, groups, gb;       // gb: blocks of 128 values per group (groups of 128 and more)
+    int T, O, K, nb, groups, group;    // nb: blocks of 128 values of a row
     int x_bf16, y_bf16, act;
     int parts, tokens;                 // columns of a vector (1, or 3 for fp32), vectors of a pass
-    int wr;                            // warps side by side along the rows; the others split K
-    int split, bpc;                    // CTAs of a cluster (they split K), blocks of 128 values of each
-    int xblocks;                       // blocks of x in shared memory at a time
+    int wr, wk;                        // warps side by side along the rows, and along K
+    int split, upc;                    // CTAs of a cluster (they split K), units of two blocks of each
+    int xunits;                        // units whose x and scales are in shared memory at a time
+    int scale_pitch, scale_at, ring_at;   // values between rows of scales there; where scales and codes lie (bytes)
+    Div by_blocks;                     // blocks of 128 values per group (groups of 128 and more)
 };
 
 __device__ __forceinline__ uint32_t levels(uint32_t word, int p) {
-    uint32_t v = ((word >> (4 * p)) & 0x000f000fu) | 0x43004300u;         // 128 + code, twice
-    const uint32_t off = 0x43084308u;                                       // 136
-    asm("sub.rn.bf16x2 %0, %0, %1;" : "+r"(v) : "r"(off));
+    uint32_t v = word >> (4 * p);
+    asm("lop3.b32 %0, %0, %1, %2, 0xea;" : "+r"(v) : "r"(0x000f000fu), "r"(0x43004300u));     // (v & ..) | ..: 128 + code
+    asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(v) : "r"(0x3f803f80u), "r"(0xc308c308u));      // 1 v - 136
     return v;
 }
 
@@ -136,22 +138,23 @@ __device__ __forceinline__ void split3(float v, uint16_t *p) {
     p[2] = __bfloat16_as_ushort(__float2bfloat16_rn(r - __uint_as_float(m & 0xffff0000u)));
 }
 
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void copy16(uint16_t *dst, const void *src, int bytes) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src),
-                 "r"(bytes)
-                 : "memory");
+    copy16((uint32_t)__cvta_generic_to_shared(dst), src, bytes);
 }
 
 // Blocks [b0, b0 + n) of the pass's vectors into shared memory, columns of n 128 + 32 values (the 64 bytes
 // over put the eight columns of a tile into different banks), zero past K.
-__device__ __forceinline__ void stage(const Args &a, uint16_t *xs, int t0, int tokens, int b0, int n) {
-    const int pitch = n * 128 + 32, k0 = b0 * 128, valid = min(a.K - k0, n * 128);
+__device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int tokens, int b0, int n) {
+    const int pitch = n * 128 + 32, k0 = b0 * 128, valid = min(a.K - k0, n * 128), threads = blockDim.x;
     if (a.x_bf16) {
         const uint16_t *x = static_cast<const uint16_t *>(a.x) + (int64_t)t0 * a.ldx + k0;
         const bool wide = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && a.ldx % 8 == 0;
         for (int t = 0; t < tokens; ++t, x += a.ldx) {
             uint16_t *dst = xs + t * pitch;
-            for (int k = 8 * threadIdx.x; k < n * 128; k += 8 * THREADS) {
+            for (int k = 8 * threadIdx.x; k < n * 128; k += 8 * threads) {
                 const int left = valid - k;
                 if (wide) {
                     copy16(dst + k, left > 0 ? x + k : x, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
@@ -165,17 +168,16 @@ __device__ __forceinline__ void stage(const Args &a, uint16_t *xs, int t0, int t
                 }
             }
         }
-        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
     } else {
         constexpr int U = 4;                                         // loads in flight
         const float *x = static_cast<const float *>(a.x) + (int64_t)t0 * a.ldx + k0;
         const bool wide = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && a.ldx % 4 == 0;
         const int per = n * 32, all = tokens * per;                  // fours of a column, of all
-        for (int e0 = threadIdx.x; e0 < all; e0 += U * THREADS) {
+        for (int e0 = threadIdx.x; e0 < all; e0 += U * threads) {
             float4 v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int e = e0 + u * THREADS, t = e / per, k = 4 * (e - t * per), left = valid - k;
+                const int e = e0 + u * threads, t = e / per, k = 4 * (e - t * per), left = valid - k;
                 v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                 if (e >= all) continue;
                 const float *src = x + (int64_t)t * a.ldx + k;
@@ -190,7 +192,7 @@ __device__ __forceinline__ void stage(const Args &a, uint16_t *xs, int t0, int t
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int e = e0 + u * THREADS, t = e / per, k = 4 * (e - t * per);
+                const int e = e0 + u * threads, t = e / per, k = 4 * (e - t * per);
                 if (e >= all) break;
                 uint16_t p[4][3];
                 split3(v[u].x, p[0]);
@@ -206,72 +208,124 @@ __device__ __forceinline__ void stage(const Args &a, uint16_t *xs, int t0, int t
     }
 }
 
-constexpr int DEPTH = 4;              // blocks of 128 values that a warp has in flight
+// The scales of the CTA's rows for the same blocks, from the group of the first on; zero for groups past the last (they
+// hold padding only).
+__device__ __forceinline__ void stage_scales(const Args &a, uint16_t *ss, int row0, int b0, int n) {
+    const int g0 = b0 * 128 / a.group, g1 = min(a.groups, ((b0 + n) * 128 - 1) / a.group + 1), threads = blockDim.x;
+    const int eights = a.scale_pitch / 8, all = a.wr * 16 * eights;
+    const bool wide = (reinterpret_cast<uintptr_t>(a.scales + g0) & 15) == 0 && a.groups % 8 == 0;
+    for (int e = threadIdx.x; e < all; e += threads) {
+        const int r = e / eights, k = 8 * (e - r * eights), left = g1 - g0 - k;
+        const uint16_t *src = a.scales + (int64_t)min(row0 + r, a.O - 1) * a.groups + g0 + k;
+        uint16_t *dst = ss + r * a.scale_pitch + k;
+        if (wide) {
+            copy16(dst, left > 0 ? src : a.scales, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
+        } else {
+            uint16_t v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? src[i] : (uint16_t)0;
+            *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16,
+                                                         v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
+        }
+    }
+}
+
+constexpr int WARPS = 8;              // of a CTA, at most
+constexpr int RING = 4;               // units that a warp has in flight: asynchronous copies to its own part of shared memory
+constexpr int UNIT_BYTES = 2048;      // 16 rows x two blocks (128 bytes of a row side by side)
 
 // NT: tiles of 8 columns; FL: words of a lane's four that share a scale (1, 2, 4 for groups of 32, 64, 128 and more).
 template <int NT, int FL>
-__global__ void __launch_bounds__(THREADS, 2) matvec_kernel(Args a) {
+__global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
     extern __shared__ __align__(16) uint8_t smem[];
-    uint16_t *xs = reinterpret_cast<uint16_t *>(smem);
+    uint16_t *xs = reinterpret_cast<uint16_t *>(smem), *ss = reinterpret_cast<uint16_t *>(smem + a.scale_at);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int wr = warp % a.wr, wk = warp / a.wr, nk = WARPS / a.wr;
+    const int wr = warp % a.wr, wk = warp / a.wr;
     const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
     const int t0 = blockIdx.y * a.tokens, tokens = min(a.tokens, a.T - t0), cols = tokens * a.parts;
-    const int row = (tile * a.wr + wr) * 16 + g;
-    const int r0 = min(row, a.O - 1), r1 = min(row + 8, a.O - 1);       // rows past the last repeat it and are not stored
-    const uint4 *w0 = reinterpret_cast<const uint4 *>(a.codes + (int64_t)r0 * (a.Kp / 2)) + t;
-    const uint4 *w1 = reinterpret_cast<const uint4 *>(a.codes + (int64_t)r1 * (a.Kp / 2)) + t;
-    const uint16_t *s0 = a.scales + (int64_t)r0 * a.groups, *s1 = a.scales + (int64_t)r1 * a.groups;
-    const int first = rank * a.bpc, last = min(a.Kp / 128, first + a.bpc);
+    const int row0 = tile * a.wr * 16, row = row0 + wr * 16 + g;
+    const int64_t pitch = (int64_t)a.nb * 64;
+    // rows past the last repeat it and are not stored
+    const uint8_t *w0 = a.codes + min(row, a.O - 1) * pitch + 16 * t, *w1 = a.codes + min(row + 8, a.O - 1) * pitch + 16 * t;
+    const int first = rank * a.upc, last = min((a.nb + 1) / 2, first + a.upc);
+    uint8_t *ring = smem + a.ring_at + warp * (RING * UNIT_BYTES) + lane * 16;
+    const uint32_t ring_copy = (uint32_t)__cvta_generic_to_shared(ring);
+    const int step = a.wk * 128;
+    int next = first + wk, fetched = 0, used = 0;                        // slots as offsets in bytes
+    w0 += next * 128;
+    w1 += next * 128;
+    auto fetch = [&]() {                                                 // a lane reads back what it has copied itself
+        if (next < last) {
+            // a block past the last: zeros (against zeros of x)
+            const int bytes = 2 * next + 1 < a.nb ? 16 : 0, more = bytes * 4;
+            const uint32_t d = ring_copy + fetched;
+            copy16(d, w0, 16);
+            copy16(d + 512, w1, 16);
+            copy16(d + 1024, w0 + more, bytes);
+            copy16(d + 1536, w1 + more, bytes);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        next += a.wk;
+        w0 += step;
+        w1 += step;
+        fetched = (fetched + UNIT_BYTES) & (RING * UNIT_BYTES - 1);
+    };
+
     float tot[NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) tot[n][i] = 0.0f;
+#pragma unroll
+    for (int d = 0; d < RING - 1; ++d) fetch();
 
-    // codes and scales of the warp's next DEPTH blocks
-    uint4 u0[DEPTH], u1[DEPTH];
-    uint32_t f0[DEPTH], f1[DEPTH];                                     // lane t: the scale of word t
-    auto fetch = [&](int d, int kb) {
-        if (kb >= last) return;
-        u0[d] = __ldcs(w0 + kb * 4);
-        u1[d] = __ldcs(w1 + kb * 4);
-        const int sg = FL == 4 ? (a.gb == 1 ? kb : kb / a.gb) : kb * (4 / FL) + t / FL;
-        f0[d] = sg < a.groups ? s0[sg] : 0u;                           // a group past the last holds padding only
-        f1[d] = sg < a.groups ? s1[sg] : 0u;
-    };
-#pragma unroll
-    for (int d = 0; d < DEPTH; ++d) fetch(d, first + wk + d * nk);
-
-    for (int c0 = first; c0 < last; c0 += a.xblocks) {
-        const int nb = min(a.xblocks, last - c0), pitch = nb * 128 + 32;
+    for (int c0 = first; c0 < last; c0 += a.xunits) {
+        const int b0 = 2 * c0, nb = 2 * min(a.xunits, last - c0), xpitch = nb * 128 + 32;
+        const int g0 = FL == 4 ? a.by_blocks.div(b0) : b0 * (4 / FL);
         __syncthreads();
-        stage(a, xs, t0, tokens, c0, nb);
+        stage_x(a, xs, t0, tokens, b0, nb);
+        stage_scales(a, ss, row0, b0, nb);
+        if (threadIdx.x < 32) *reinterpret_cast<uint4 *>(xs + cols * xpitch + 8 * threadIdx.x) = make_uint4(0, 0, 0, 0);
+        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
         __syncthreads();
-        for (int k0 = c0 + wk; k0 < c0 + nb; k0 += DEPTH * nk) {
+        // this lane's column of each tile, at its values of the unit; a column past the last is 256 zeros
+        const uint16_t *xr[NT];
+        int xstep[NT];
 #pragma unroll
-            for (int d = 0; d < DEPTH; ++d) {
-                const int kb = k0 + d * nk;
-                if (kb >= c0 + nb) break;
-                const uint32_t q0[4] = {u0[d].x, u0[d].y, u0[d].z, u0[d].w}, q1[4] = {u1[d].x, u1[d].y, u1[d].z, u1[d].w};
-                float h0[4 / FL], h1[4 / FL];
+        for (int n = 0; n < NT; ++n) {
+            const bool live = n * 8 + g < cols;
+            xr[n] = xs + (live ? (n * 8 + g) * xpitch + wk * 256 : cols * xpitch) + 8 * t;
+            xstep[n] = live ? a.wk * 256 : 0;
+        }
+        const uint16_t *sr = ss + (wr * 16 + g) * a.scale_pitch - g0;
+        const int end = min(c0 + a.xunits, last);
+        for (int u = c0 + wk; u < end; u += a.wk) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(RING - 2) : "memory");
+            fetch();
+            const uint8_t *d = ring + used;
+            used = (used + UNIT_BYTES) & (RING * UNIT_BYTES - 1);
 #pragma unroll
-                for (int s = 0; s < 4 / FL; ++s) {
-                    h0[s] = __uint_as_float((FL == 4 ? f0[d] : __shfl_sync(0xffffffffu, f0[d], s * FL, 4)) << 16);
-                    h1[s] = __uint_as_float((FL == 4 ? f1[d] : __shfl_sync(0xffffffffu, f1[d], s * FL, 4)) << 16);
-                }
-                fetch(d, kb + DEPTH * nk);
-                float acc[NT][4];
+            for (int b = 0; b < 2; ++b) {
+                const uint4 u0 = *reinterpret_cast<const uint4 *>(d + b * 1024);
+                const uint4 u1 = *reinterpret_cast<const uint4 *>(d + b * 1024 + 512);
+                const uint32_t q0[4] = {u0.x, u0.y, u0.z, u0.w}, q1[4] = {u1.x, u1.y, u1.z, u1.w};
+                const uint16_t *sb = sr + (FL == 4 ? a.by_blocks.div(2 * u + b) : (2 * u + b) * (4 / FL));
+                // a scale's words in one sum, the four words of a long group in two (shorter chains of dependent products)
+                constexpr int SUMS = FL == 4 ? 2 : 1;
+                float acc[SUMS][NT][4];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     if (j % FL == 0) {
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                        for (int h = 0; h < SUMS; ++h)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[n][i] = 0.0f;
+                            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) acc[h][n][i] = 0.0f;
                     }
+                    const int h = j % SUMS;
                     uint32_t a0[4], a1[4];
 #pragma unroll
                     for (int p = 0; p < 4; ++p) {
@@ -280,58 +334,79 @@ __global__ void __launch_bounds__(THREADS, 2) matvec_kernel(Args a) {
                     }
 #pragma unroll
                     for (int n = 0; n < NT; ++n) {
-                        uint4 b = make_uint4(0, 0, 0, 0);
-                        if (n * 8 + g < cols)
-                            b = *reinterpret_cast<const uint4 *>(xs + (n * 8 + g) * pitch + (kb - c0) * 128 + 32 * j + 8 * t);
-                        mma(acc[n], a0[0], a1[0], a0[1], a1[1], b.x, b.y);
-                        mma(acc[n], a0[2], a1[2], a0[3], a1[3], b.z, b.w);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(xr[n] + 128 * b + 32 * j);
+                        mma(acc[h][n], a0[0], a1[0], a0[1], a1[1], v.x, v.y);
+                        mma(acc[h][n], a0[2], a1[2], a0[3], a1[3], v.z, v.w);
                     }
                     if (j % FL == FL - 1) {
+                        const float f0 = __uint_as_float((uint32_t)sb[j / FL] << 16);
+                        const float f1 = __uint_as_float((uint32_t)sb[8 * a.scale_pitch + j / FL] << 16);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            tot[n][0] = fmaf(h0[j / FL], acc[n][0], tot[n][0]);
-                            tot[n][1] = fmaf(h0[j / FL], acc[n][1], tot[n][1]);
-                            tot[n][2] = fmaf(h1[j / FL], acc[n][2], tot[n][2]);
-                            tot[n][3] = fmaf(h1[j / FL], acc[n][3], tot[n][3]);
-                        }
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float sum = SUMS == 1 ? acc[0][n][i] : acc[0][n][i] + acc[SUMS - 1][n][i];
+                                tot[n][i] = fmaf(i < 2 ? f0 : f1, sum, tot[n][i]);
+                            }
                     }
                 }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) xr[n] += xstep[n];
         }
     }
 
-    // the warps' sums [warp][16 rows][8 NT columns], then the cluster's, in a fixed order
+    // the warps' sums [warp][16 rows][8 NT columns], added up over the warps along K into the first wr, then over the
+    // cluster; all in a fixed order
     constexpr int CW = 8 * NT;
     float *red = reinterpret_cast<float *>(smem);
     __syncthreads();
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         float *d = red + (warp * 16 + g) * CW + n * 8 + 2 * t;
-        d[0] = tot[n][0];
-        d[1] = tot[n][1];
-        d[8 * CW] = tot[n][2];
-        d[8 * CW + 1] = tot[n][3];
+        *reinterpret_cast<float2 *>(d) = make_float2(tot[n][0], tot[n][1]);
+        *reinterpret_cast<float2 *>(d + 8 * CW) = make_float2(tot[n][2], tot[n][3]);
+    }
+    __syncthreads();
+    const int rows = a.wr * 16, size = rows * CW;
+    if (a.wk > 1) {
+        for (int e = threadIdx.x; e < size; e += blockDim.x) {
+            float v[WARPS];
+#pragma unroll
+            for (int k = 0; k < WARPS; ++k) v[k] = k < a.wk ? red[k * size + e] : 0.0f;
+#pragma unroll
+            for (int k = 1; k < WARPS; ++k) v[0] += v[k];
+            red[e] = v[0];
+        }
     }
     cg::cluster_group cluster = cg::this_cluster();
-    cluster.sync();
-    const int rows = a.wr * 16, each = (rows + a.split - 1) / a.split, rr0 = rank * each, rr1 = min(rows, rr0 + each);
-    for (int e = threadIdx.x; e < (rr1 - rr0) * tokens; e += THREADS) {
-        const int r = rr0 + e / tokens, tk = e % tokens, o = tile * rows + r;
+    if (a.split > 1) cluster.sync();
+    else __syncthreads();
+    const int each = (rows + a.split - 1) / a.split, rr0 = rank * each, rr1 = min(rows, rr0 + each);
+    for (int e = threadIdx.x; e < (rr1 - rr0) * tokens; e += blockDim.x) {
+        const int q = e / tokens, tk = e - q * tokens, r = rr0 + q, o = row0 + r;
         if (o >= a.O) continue;
         float sum = 0.0f;
-        for (int i = a.parts - 1; i >= 0; --i)                        // the smallest part first
-            for (int c = 0; c < a.split; ++c) {
-                const float *src = cluster.map_shared_rank(red, c);
-                for (int k = 0; k < nk; ++k)
-                    sum += src[((k * a.wr + r / 16) * 16 + r % 16) * CW + tk * a.parts + i];
-            }
+        for (int i = a.parts - 1; i >= 0; --i) {                      // the smallest part first
+            float *at = red + r * CW + tk * a.parts + i;
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                v[c] = a.split == 1 ? (c == 0 ? *at : 0.0f) : c < a.split ? *cluster.map_shared_rank(at, c) : 0.0f;
+#pragma unroll
+            for (int c = 1; c < 8; ++c) v[0] += v[c];
+            sum += v[0];
+        }
         float z = fmaf(sum, a.scale ? a.scale[o] : 1.0f, a.shift ? a.shift[o] : 0.0f);
         with_act(a.act, [&](auto act) { z = act_value<act.value>(z); });
         const int64_t at = (int64_t)(t0 + tk) * a.ldy + o;
         if (a.y_bf16) static_cast<uint16_t *>(a.y)[at] = __bfloat16_as_ushort(__float2bfloat16_rn(z));
         else static_cast<float *>(a.y)[at] = z;
     }
-    cluster.sync();                                                    // no CTA leaves while its sums are read
+    if (a.split > 1) {
+        cluster_done_reading();
+        cluster_leave();
+    }
 }
 
 using namespace minw_host;
@@ -356,7 +431,7 @@ static cudaError_t launch(const Args &a, dim3 grid, size_t smem, cudaStream_t s)
     if (!allow_shared(reinterpret_cast<const void *>(kern), 112 * 1024)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(32u * a.wr * a.wk);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -414,42 +489,57 @@ minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T
     if (T == 0) return MINW_OK;
     w4::Args a{};
     a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy; a.codes = codes; a.scales = scales; a.scale = scale; a.shift = shift;
-    a.T = T; a.O = O; a.K = K; a.Kp = (K + 127) / 128 * 128; a.groups = (K + group - 1) / group;
-    a.gb = group >= 128 ? group / 128 : 1;
+    a.T = T; a.O = O; a.K = K; a.nb = (K + 127) / 128; a.groups = (K + group - 1) / group; a.group = group;
+    a.by_blocks = Div(group >= 128 ? group / 128 : 1);
     a.x_bf16 = x_type == MINW_BF16; a.y_bf16 = y_type == MINW_BF16; a.act = act;
     a.parts = a.x_bf16 ? 1 : 3;
     const int most = 32 / a.parts;                                   // vectors of a pass: 32 columns
     a.tokens = T < most ? T : most;
     const int passes = (T + a.tokens - 1) / a.tokens, cols = a.tokens * a.parts, NT = (cols + 7) / 8;
     if (passes > 65535) return MINW_EUNSUPPORTED;
-    const int nb = a.Kp / 128, sms = num_sms() > 0 ? num_sms() : 152;
-    // Rows of a CTA (16 for each of wr warps side by side; the other warps split K) and CTAs of a cluster (which split K
-    // too): the pair with the least estimated time, waves of two CTAs per SM times a CTA's clocks -- its share of the
-    // memory rate for the codes, of L2's for x (fp32 values are split into parts as well), and a fixed part.
-    double best = 1e30;
-    for (int wr = 1; wr <= w4::WARPS; wr *= 2)
-        for (int split = 1; split <= 8; split *= 2) {
-            const int64_t tiles = (O + 16 * wr - 1) / (16 * wr);
-            const int bpc = (nb + split - 1) / split;
-            if (split > 1 && bpc * split - nb >= bpc) continue;                   // a CTA without a block
-            const int round = w4::WARPS / wr * w4::DEPTH;                         // x in shared memory: a round at least
-            if ((bpc < round ? bpc : round) * cols > 400) continue;               // (100 KB)
-            const int steps = (bpc * wr + w4::WARPS - 1) / w4::WARPS * w4::WARPS / wr;     // blocks, the warps' last ones whole
-            const double clocks = steps * (wr * 1024 / 11.0) + bpc * a.tokens * 128 * (a.x_bf16 ? 0.06 : 0.28) + 2500;
-            const double t = (double)((tiles * split * passes + 2 * sms - 1) / (2 * sms)) * clocks;
+    const int units = (a.nb + 1) / 2, sms = num_sms() > 0 ? num_sms() : 152;
+    // wr warps along the rows (16 each) and wk along K make a CTA, `split` CTAs a cluster, which splits K too: the
+    // choice with the least estimated clocks.  An SM holds two CTAs of up to 100 KB of shared memory: the rings, and x
+    // and scales of as many units (whole rounds of the warps) as fit.  Measured on one to 48 columns (T = 1: 1024 x
+    // 1024 to 16384 x 16384): twelve warps of an SM take 18 / (1 + 0.07 columns) bytes of codes a clock, fewer
+    // warps their share of that; a wave of CTAs has a fixed part, so have a cluster and each further filling of x.
+    float best = 1e30f;
+    // with the share of the SMs' places that clusters of this size can take (cudaOccupancyMaxActiveClusters)
+    static const struct { int n; float places; } splits[] = {{1, 1.0f}, {2, 1.0f}, {3, 0.957f}, {4, 0.973f}, {6, 0.907f}, {8, 0.947f}};
+    const float x_rate = a.tokens * 256 * (a.x_bf16 ? 0.03f : 0.14f), cap = 18.0f / (1.0f + 0.07f * cols);
+    int tiles = 0;
+    for (int wr = 1; wr <= w4::WARPS; ++wr) {
+        const int wk = w4::WARPS / wr, warps = wr * wk, rows = (O + 16 * wr - 1) / (16 * wr);
+        const int room = 100 * 1024 - warps * w4::RING * w4::UNIT_BYTES - cols * 64 - 512 - wr * 16 * 32;
+        const int fit = room / (cols * 512 + wr * 32 * (group >= 256 ? 1 : 256 / group));
+        const float one = cap * (warps >= 12 ? 1.0f : warps / 12.0f), two = cap * (warps >= 6 ? 1.0f : warps / 6.0f);
+        for (const auto &sp : splits) {
+            const int split = sp.n, upc = (units + split - 1) / split, slots = (int)(2 * sms * sp.places);
+            if (upc * (split - 1) >= units) break;                                // a CTA without a unit
+            const int xunits = upc <= fit ? upc : fit / wk * wk;
+            if (xunits == 0) continue;
+            const float bytes = (float)((upc + wk - 1) / wk * wk * wr * w4::UNIT_BYTES);    // the warps' last units are whole
+            const float fixed = 1500.0f * ((upc + xunits - 1) / xunits) + (split > 1 ? 1000.0f : 0.0f);
+            const float t1 = bytes / one + upc * x_rate + fixed, t2 = 2 * (bytes / two + upc * x_rate) + fixed;
+            const int64_t ctas = (int64_t)rows * split * passes, rest = ctas % slots;
+            const float t = (float)(ctas / slots) * t2 + (rest > sms ? t2 : rest > 0 ? t1 : 0.0f);
             if (t < best) {
                 best = t;
                 a.wr = wr;
+                a.wk = wk;
                 a.split = split;
-                a.bpc = bpc;
+                a.upc = upc;
+                a.xunits = xunits;
+                tiles = rows;
             }
         }
-    const int tiles = (O + 16 * a.wr - 1) / (16 * a.wr), unit = w4::WARPS / a.wr * w4::DEPTH;
-    int xb = 400 / cols;                                             // at most 100 KB of x at a time, whole rounds of the warps
-    xb = xb / unit * unit > 0 ? xb / unit * unit : unit;
-    a.xblocks = a.bpc < xb ? a.bpc : xb;
-    size_t smem = (size_t)cols * (a.xblocks * 128 + 32) * 2;
-    const size_t red = (size_t)w4::WARPS * 16 * 8 * NT * sizeof(float);
+    }
+    const int ring = a.wr * a.wk * w4::RING * w4::UNIT_BYTES;
+    a.scale_pitch = ((group >= 256 ? a.xunits * 256 / group + 2 : a.xunits * (256 / group)) + 7) / 8 * 8;
+    a.scale_at = (cols * (a.xunits * 256 + 32) + 256) * 2;
+    a.ring_at = a.scale_at + a.wr * 16 * a.scale_pitch * 2;
+    size_t smem = (size_t)a.ring_at + ring;
+    const size_t red = (size_t)a.wr * a.wk * 16 * 8 * NT * sizeof(float);
     if (smem < red) smem = red;
     const dim3 grid((unsigned)(tiles * a.split), (unsigned)passes);
     cudaStream_t s = (cudaStream_t)stream;
