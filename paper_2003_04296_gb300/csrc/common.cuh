@@ -391,8 +391,6 @@ void max_shared_carveout(const void *kern);
 // Allows kern bytes of dynamic shared memory (set once per kernel and device: the attribute call costs the
 // host about as much as a launch).
 bool allow_shared(const void *kern, int bytes);
-// Allows kern clusters of more than eight blocks (likewise).
-bool allow_large_clusters(const void *kern);
 
 // cuTensorMapEncodeTiled from the driver (nullptr when it is unavailable).
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,

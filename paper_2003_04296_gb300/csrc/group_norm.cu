@@ -6,71 +6,44 @@ namespace minw {
 namespace gn {
 
 // ---------------------------------------------------------------------------
-// Streaming forward: statistics per chunk and channel, merged per group, then
-// a second pass over x.
+// Groups wider than a block's lanes: statistics per chunk and channel, merged
+// per group, then a second pass over x.
 // ---------------------------------------------------------------------------
 
 template <typename T, int V>
-__global__ void __launch_bounds__(THREADS) stat_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, 4) stat_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int U = V == 1 ? 8 : 4;                        // pixels in flight per thread
+    constexpr int NP = (V + 1) / 2;
     __shared__ float2 red[THREADS * V];
     const Place w = place<V>(a, blockIdx.x);
-    float m[V], q[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) m[i] = q[i] = 0.0f;
-    int n = 0;
-    if (w.active) {
-        const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
-        for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
-            Vec<T, V> v[U];
-            int k = 0;
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (p + u * w.rows < w.p1) {
-                    v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-                    k = u + 1;
-                }
-            const float inv = 1.0f / (float)k, share = (float)k / (float)(n + k);
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float s = 0.0f, d2 = 0.0f;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u < k) s += v[u].get(i);
-                s *= inv;
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (u < k) {
-                        const float d = v[u].get(i) - s;
-                        d2 = fmaf(d, d, d2);
-                    }
-                const float d = s - m[i];
-                m[i] = fmaf(d, share, m[i]);
-                q[i] += fmaf(d * d, (float)n * share, d2);
-            }
-            n += k;
-        }
-    }
-    // rows of the block: row r holds (pixels - r + rows - 1) / rows of them
-    const int W = a.L * V, np = w.p1 - w.p0;
+    Pair m[NP], q[NP];
+    channel_stats<T, V, V == 1 ? 16 : 4>(
+        static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c, w.rows * a.ldx, w.n, m, q);
+    // rows of the block: the first `more` hold `most` pixels each, the others one fewer
+    const int W = a.L * V, np = w.p1 - w.p0, whole = (np - 1) / w.rows;
+    const int more = np - whole * w.rows;
+    const float most = (float)(whole + 1);
     if (w.row < w.rows) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) red[w.row * W + ((int)threadIdx.x % a.L) * V + i] = make_float2(m[i], q[i]);
+        for (int k = 0; k < NP; ++k) {
+            const float2 mk = halves(m[k]), qk = halves(q[k]);
+            red[w.row * W + w.lane * V + 2 * k] = make_float2(mk.x, qk.x);
+            if (V > 1) red[w.row * W + w.lane * V + 2 * k + 1] = make_float2(mk.y, qk.y);
+        }
     }
     __syncthreads();
     for (int e = threadIdx.x; e < W; e += THREADS) {
         const int c = w.slab * W + e;
         if (c >= a.C) break;
         float s = 0.0f;
-        for (int r = 0; r < w.rows; ++r) s = fmaf((float)((np - r + w.rows - 1) / w.rows), red[r * W + e].x, s);
+        for (int r = 0; r < w.rows; ++r) s = fmaf(r < more ? most : most - 1.0f, red[r * W + e].x, s);
         const float mean = s / (float)np;
         float M2 = 0.0f;
         for (int r = 0; r < w.rows; ++r) {
             const float2 t = red[r * W + e];
             const float d = t.x - mean;
-            M2 += fmaf(d * d, (float)((np - r + w.rows - 1) / w.rows), t.y);
+            M2 += fmaf(d * d, r < more ? most : most - 1.0f, t.y);
         }
         a.part[((int64_t)w.b * a.chunks + w.chunk) * a.C + c] = make_float2(mean, M2);
     }
@@ -96,19 +69,21 @@ __global__ void __launch_bounds__(THREADS) stat_merge_kernel(Args a) {
     };
     const float n = (float)a.P * (float)a.Cg;
     float s = 0.0f;
+#pragma unroll 4
     for (int e = threadIdx.x; e < entries; e += THREADS) {
         const int k = e / a.Cg;
         s = fmaf((float)(min(a.P, (k + 1) * a.ppc) - k * a.ppc), part[(int64_t)k * a.C + e % a.Cg].x, s);
     }
     const float mean = block_sum(s) / n;
     s = 0.0f;
+#pragma unroll 4
     for (int e = threadIdx.x; e < entries; e += THREADS) {
         const int k = e / a.Cg;
         const float2 t = part[(int64_t)k * a.C + e % a.Cg];
         const float d = t.x - mean;
         s += fmaf(d * d, (float)(min(a.P, (k + 1) * a.ppc) - k * a.ppc), t.y);
     }
-    const float rstd = 1.0f / sqrtf(block_sum(s) / n + a.eps);
+    const float rstd = rsqrtf(block_sum(s) / n + a.eps);
     if (threadIdx.x == 0) {
         a.stat[blockIdx.x] = make_float2(mean, rstd);
         if (a.mean) a.mean[blockIdx.x] = mean;
@@ -117,42 +92,40 @@ __global__ void __launch_bounds__(THREADS) stat_merge_kernel(Args a) {
 }
 
 template <typename T, typename TY, int V>
-__global__ void __launch_bounds__(THREADS) apply_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, 4) apply_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int U = V == 1 ? 8 : 4;
+    constexpr int NP = (V + 1) / 2;
     const Place w = place<V>(a, (int64_t)gridDim.x - 1 - blockIdx.x);     // the last chunks read are still in L2
-    if (!w.active) return;
-    float ga[V], be[V], mean[V], rstd[V];
-    load_affine<V>(a, w.c, ga, be);
+    if (w.n == 0) return;
+    Pair nm[NP], sc[NP], sh[NP];
+    {
+        float ga[V], be[V], mean[V];
+        load_affine<V>(a, w.c, ga, be);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
-        mean[i] = t.x;
-        rstd[i] = t.y;
-    }
-    const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
-    TY *y = static_cast<TY *>(a.y) + (int64_t)w.b * a.P * a.ldy + w.c;
-    with_act(a.act, [&](auto act) {
-        for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
-            Vec<T, V> v[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (p + u * w.rows < w.p1) v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (p + u * w.rows >= w.p1) break;
-                float z[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    z[i] = act_value<act.value>(fmaf((v[u].get(i) - mean[i]) * rstd[i], ga[i], be[i]));
-                Vec<TY, V> o;
-                o.set(z);
-                o.store(y + (int64_t)(p + u * w.rows) * a.ldy);
-            }
+        for (int i = 0; i < V; ++i) {
+            const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
+            mean[i] = -t.x;
+            ga[i] *= t.y;
         }
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            nm[k] = pick<V>(mean, k);
+            sc[k] = pick<V>(ga, k);
+            sh[k] = pick<V>(be, k);
+        }
+    }
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    with_act(a.act, [&](auto act) {
+        apply_pixels<T, TY, V, V == 1 ? 8 : 4, act.value>(static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
+                                                          static_cast<TY *>(a.y) + p * a.ldy + w.c, w.rows * a.ldy, w.n,
+                                                          nm, sc, sh);
     });
 }
+
+// ---------------------------------------------------------------------------
+// One kernel
+// ---------------------------------------------------------------------------
 
 // Sums over a block of each thread's GPT values, one per group of its channels; afterwards every thread has the
 // sums of its own groups.  `per` entries (a thread's value is one) make a group, L GPT a row.
@@ -204,16 +177,135 @@ __device__ __forceinline__ void group_sum(float *s, GroupSum<GPT> &sm, const Arg
     }
 }
 
-// GPT: groups among a thread's V channels (W = V / GPT channels of each).  A thread sums its values and their
-// squared deviations from its own mean; the block's mean turns the latter into deviations from that (n W (m - mean)^2
-// more), and the cluster's mean likewise.
+template <int GPT>
+struct Shared {
+    GroupSum<GPT> sums[2];
+    float2 cta[MAX_SLAB_GROUPS], all[MAX_SLAB_GROUPS];
+};
+
+// The block's mean and M2 of each of a thread's GPT groups from its own `values` values' mean and M2 of them: the block's
+// mean turns M2 into deviations from that (values (own - mean)^2 more).
+template <int GPT>
+__device__ __forceinline__ void merge_block(const Args &a, const Tile &w, Shared<GPT> &sm, const float *own, float values,
+                                            float *mean, float *m2) {
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) mean[g] = own[g] * values;
+    group_sum<GPT>(mean, sm.sums[0], a, w);
+    const float block = w.p1 > w.p0 ? __fdividef(1.0f, (float)(w.p1 - w.p0) * (float)a.Cg) : 0.0f;
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) {
+        mean[g] *= block;
+        const float d = own[g] - mean[g];
+        if (values > 0.0f) m2[g] = fmaf(d * d, values, m2[g]);
+    }
+    group_sum<GPT>(m2, sm.sums[1], a, w);
+}
+
+// The cluster's in sm.all from its blocks' (chunks first .. first + size - 1 of the image); the same sums in every block.
+// Afterwards the cluster has arrived at its end (cluster_leave).
+template <int GPT>
+__device__ __forceinline__ void merge_cluster(const Args &a, const Tile &w, Shared<GPT> &sm, int first, int size,
+                                              const float *mean, const float *m2) {
+    if (w.row == 0) {
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) sm.cta[a.by_per.div(w.lane * GPT + g)] = make_float2(mean[g], m2[g]);
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    const int all = min(a.P, (first + size) * a.ppc) - min(a.P, first * a.ppc);
+    const float inv = __fdividef(1.0f, (float)max(all, 1) * (float)a.Cg);
+    // eight threads a group, one for each block
+    for (int g = threadIdx.x >> 3; g < (a.groups + 3) / 4 * 4; g += THREADS / 8) {     // all of a warp alike
+        const int k = threadIdx.x & 7;
+        float2 t = make_float2(0.0f, 0.0f);
+        float n = 0.0f;
+        if (k < size && g < a.groups) {
+            t = *cluster.map_shared_rank(&sm.cta[g], k);
+            n = (float)(min(a.P, (first + k + 1) * a.ppc) - min(a.P, (first + k) * a.ppc)) * (float)a.Cg;
+        }
+        float s = n * t.x;
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        s *= inv;
+        const float d0 = t.x - s;
+        float q = n > 0.0f ? fmaf(d0 * d0, n, t.y) : 0.0f;
+#pragma unroll
+        for (int d = 4; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
+        if (k == 0 && g < a.groups) sm.all[g] = make_float2(s, q);
+    }
+    cluster_done_reading();
+    __syncthreads();
+}
+
+// Mean and rstd of each of a thread's groups, saved by the image's first block.
+template <int GPT>
+__device__ __forceinline__ void merge(const Args &a, const Tile &w, Shared<GPT> &sm, const float *own, float *m2,
+                                      float values, float *mean, float *rstd) {
+    merge_block<GPT>(a, w, sm, own, values, mean, m2);
+    if (a.chunks > 1) {
+        merge_cluster<GPT>(a, w, sm, 0, a.chunks, mean, m2);
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            const float2 t = sm.all[a.by_per.div(w.lane * GPT + g)];
+            mean[g] = t.x;
+            m2[g] = t.y;
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) rstd[g] = rsqrtf(fmaf(m2[g], a.inv_total, a.eps));
+    if (w.rank == 0 && w.row == 0) {
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            const int64_t at = (int64_t)w.b * a.G + w.slab * a.groups + a.by_per.div(w.lane * GPT + g);
+            if (a.mean) a.mean[at] = mean[g];
+            if (a.rstd) a.rstd[at] = rstd[g];
+        }
+    }
+}
+
+// Mean and M2 of a thread's groups from its channels' of n values each.
+template <int V, int GPT>
+__device__ __forceinline__ void fold_channels(const Pair *m, const Pair *q, int n, float *own, float *m2) {
+    constexpr int W = V / GPT;
+#pragma unroll
+    for (int g = 0; g < GPT; ++g) {
+        float f[W], s = 0.0f, d2 = 0.0f, r = 0.0f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const float2 h = halves(m[(g * W + k) / 2]), h2 = halves(q[(g * W + k) / 2]);
+            f[k] = (g * W + k) % 2 ? h.y : h.x;
+            s += f[k];
+            r += (g * W + k) % 2 ? h2.y : h2.x;
+        }
+        own[g] = s * (1.0f / W);
+#pragma unroll
+        for (int k = 0; k < W; ++k) d2 = fmaf(f[k] - own[g], f[k] - own[g], d2);
+        m2[g] = fmaf(d2, (float)n, r);
+    }
+}
+
+// Minus the means, rstd gamma and beta of a thread's channels, in pairs.
+template <int V, int GPT>
+__device__ __forceinline__ void coefficients(const Args &a, int c, const float *mean, const float *rstd, Pair *nm, Pair *sc,
+                                             Pair *sh) {
+    constexpr int W = V / GPT, NP = (V + 1) / 2;
+    float ga[V], be[V];
+    load_affine<V>(a, c, ga, be);
+#pragma unroll
+    for (int k = 0; k < NP; ++k) {
+        nm[k] = pick_group<V, W>(mean, k, -1.0f);
+        sc[k] = mul2(pick_group<V, W>(rstd, k), pick<V>(ga, k));
+        sh[k] = pick<V>(be, k);
+    }
+}
+
+// In registers.  GPT: groups among a thread's V channels (W = V / GPT channels of each); NV: pixels of a thread at most.
 template <typename T, typename TY, int V, int GPT, int NV>
-__global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
     constexpr int W = V / GPT, NP = (V + 1) / 2;
-    __shared__ GroupSum<GPT> sums[2];
-    __shared__ float2 cta[MAX_SLAB_GROUPS], all[MAX_SLAB_GROUPS];
+    __shared__ Shared<GPT> sm;
     const Tile w = tile<V>(a);
     const T *x = static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c;
     const int64_t step = (int64_t)w.rows * a.ldx;
@@ -222,7 +314,7 @@ __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused
     for (int i = 0; i < NV; ++i)
         if (i < w.n) v[i].load(x + i * step);
 
-    float mean[GPT], m2[GPT];
+    float mean[GPT], rstd[GPT];
     {
         // pairs of channels: of one group, or (W = 1) of two
         Pair s[NP], q[NP];
@@ -253,11 +345,11 @@ __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused
                 }
             }
         };
-        fold(s, mean);
+        float own[GPT], m2[GPT];
+        fold(s, own);
         const float values = (float)(w.n * W), inv = w.n > 0 ? __fdividef(1.0f, values) : 0.0f;
-        float own[GPT];
 #pragma unroll
-        for (int g = 0; g < GPT; ++g) own[g] = mean[g] * inv;
+        for (int g = 0; g < GPT; ++g) own[g] *= inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if (i < w.n) {
@@ -268,67 +360,11 @@ __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused
                 }
             }
         fold(q, m2);
-        group_sum<GPT>(mean, sums[0], a, w);
-        const float block = w.p1 > w.p0 ? __fdividef(1.0f, (float)(w.p1 - w.p0) * (float)a.Cg) : 0.0f;
-#pragma unroll
-        for (int g = 0; g < GPT; ++g) {
-            mean[g] *= block;
-            const float d = own[g] - mean[g];
-            if (w.n > 0) m2[g] = fmaf(d * d, values, m2[g]);
-        }
-        group_sum<GPT>(m2, sums[1], a, w);
-    }
-
-    float rstd[GPT];
-    if (a.chunks > 1) {
-        // the cluster's blocks: sixteen threads a group, one for each; the same sums in every block
-        if (w.row == 0) {
-#pragma unroll
-            for (int g = 0; g < GPT; ++g) cta[a.by_per.div(w.lane * GPT + g)] = make_float2(mean[g], m2[g]);
-        }
-        cg::cluster_group cluster = cg::this_cluster();
-        cluster.sync();
-        for (int g = threadIdx.x >> 4; g < (a.groups + 1) / 2 * 2; g += THREADS / 16) {    // both halves of a warp alike
-            const int k = threadIdx.x & 15;
-            float2 t = make_float2(0.0f, 0.0f);
-            float n = 0.0f;
-            if (k < a.chunks && g < a.groups) {
-                t = *cluster.map_shared_rank(&cta[g], k);
-                const int q0 = min(a.P, k * a.ppc);
-                n = (float)(min(a.P, q0 + a.ppc) - q0) * (float)a.Cg;
-            }
-            float s = n * t.x;
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-            s *= a.inv_total;
-            const float d0 = t.x - s;
-            float q = n > 0.0f ? fmaf(d0 * d0, n, t.y) : 0.0f;
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) q += __shfl_xor_sync(0xffffffffu, q, d);
-            if (k == 0 && g < a.groups) all[g] = make_float2(s, q);
-        }
-        cluster_done_reading();
-        __syncthreads();
-#pragma unroll
-        for (int g = 0; g < GPT; ++g) {
-            const float2 t = all[a.by_per.div(w.lane * GPT + g)];
-            mean[g] = t.x;
-            m2[g] = t.y;
-        }
-    }
-#pragma unroll
-    for (int g = 0; g < GPT; ++g) rstd[g] = rsqrtf(fmaf(m2[g], a.inv_total, a.eps));
-    if (w.rank == 0 && w.row == 0) {
-#pragma unroll
-        for (int g = 0; g < GPT; ++g) {
-            const int64_t at = (int64_t)w.b * a.G + w.slab * a.groups + a.by_per.div(w.lane * GPT + g);
-            if (a.mean) a.mean[at] = mean[g];
-            if (a.rstd) a.rstd[at] = rstd[g];
-        }
+        merge<GPT>(a, w, sm, own, m2, values, mean, rstd);
     }
     if (w.n > 0) {
-        float ga[V], be[V];
-        load_affine<V>(a, w.c, ga, be);
+        Pair nm[NP], sc[NP], sh[NP];
+        coefficients<V, GPT>(a, w.c, mean, rstd, nm, sc, sh);
         TY *y = static_cast<TY *>(a.y) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldy + w.c;
         const int64_t ystep = (int64_t)w.rows * a.ldy;
         with_act(a.act, [&](auto act) {
@@ -338,8 +374,7 @@ __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused
                     float z[2 * NP];
 #pragma unroll
                     for (int k = 0; k < NP; ++k) {
-                        const Pair xh = mul2(add2(v[i].get2(k), pick_group<V, W>(mean, k, -1.0f)), pick_group<V, W>(rstd, k));
-                        const float2 h = halves(fma2(xh, pick<V>(ga, k), pick<V>(be, k)));
+                        const float2 h = halves(fma2(add2(v[i].get2(k), nm[k]), sc[k], sh[k]));
                         z[2 * k] = act_value<act.value>(h.x);
                         z[2 * k + 1] = act_value<act.value>(h.y);
                     }
@@ -352,32 +387,157 @@ __global__ void __launch_bounds__(THREADS, NV == 8 ? 4 : NV == 16 ? 2 : 3) fused
     if (a.chunks > 1) cluster_leave();
 }
 
+// In two readings.
 template <typename T, typename TY, int V, int GPT>
-static auto fused_of(int NV) {
-    if constexpr (V == 1) return fused_kernel<T, TY, 1, 1, 32>;
-    else return NV == 8 ? fused_kernel<T, TY, V, GPT, 8> : fused_kernel<T, TY, V, GPT, 16>;
+__global__ void __launch_bounds__(THREADS, 4) reread_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int W = V / GPT, NP = (V + 1) / 2;
+    __shared__ Shared<GPT> sm;
+    const Tile w = tile<V>(a);
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, step = (int64_t)w.rows * a.ldx;
+    const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+    float mean[GPT], rstd[GPT];
+    {
+        Pair m[NP], q[NP];
+        channel_stats<T, V, V == 1 ? 16 : 4>(x, step, w.n, m, q);
+        float own[GPT], m2[GPT];
+        fold_channels<V, GPT>(m, q, w.n, own, m2);
+        merge<GPT>(a, w, sm, own, m2, (float)w.n * (float)W, mean, rstd);
+    }
+    if (w.n > 0) {
+        Pair nm[NP], sc[NP], sh[NP];
+        coefficients<V, GPT>(a, w.c, mean, rstd, nm, sc, sh);
+        with_act(a.act, [&](auto act) {
+            apply_pixels<T, TY, V, V == 1 ? 8 : 4, act.value>(x, step, static_cast<TY *>(a.y) + p * a.ldy + w.c,
+                                                              (int64_t)w.rows * a.ldy, w.n, nm, sc, sh);
+        });
+    }
+    if (a.chunks > 1) cluster_leave();
 }
+
+// ---------------------------------------------------------------------------
+// Two kernels, for images that no cluster could take alone: the statistics of
+// every STREAM_CLUSTER chunks of an image, merged by a cluster; then each block
+// merges its image's and applies them to its chunk.
+// ---------------------------------------------------------------------------
+
+template <typename T, int V, int GPT>
+__global__ void __launch_bounds__(THREADS, 4) chunk_stats_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int W = V / GPT, NP = (V + 1) / 2;
+    __shared__ Shared<GPT> sm;
+    const Tile w = tile<V>(a);
+    float own[GPT], m2[GPT], mean[GPT];
+    {
+        Pair m[NP], q[NP];
+        channel_stats<T, V, V == 1 ? 16 : 4>(
+            static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c, (int64_t)w.rows * a.ldx, w.n, m,
+            q);
+        fold_channels<V, GPT>(m, q, w.n, own, m2);
+    }
+    merge_block<GPT>(a, w, sm, own, (float)w.n * (float)W, mean, m2);
+    const int first = w.rank / STREAM_CLUSTER * STREAM_CLUSTER;
+    merge_cluster<GPT>(a, w, sm, first, STREAM_CLUSTER, mean, m2);
+    if (w.rank == first) {
+        float2 *part = a.part + ((int64_t)w.b * (a.chunks / STREAM_CLUSTER) + w.rank / STREAM_CLUSTER) * a.G;
+        for (int g = threadIdx.x; g < a.groups; g += THREADS) part[w.slab * a.groups + g] = sm.all[g];
+    }
+    cluster_leave();
+}
+
+template <typename T, typename TY, int V, int GPT>
+__global__ void __launch_bounds__(THREADS, 4) chunk_apply_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int NP = (V + 1) / 2, EACH = (STREAM_BLOCKS / STREAM_CLUSTER + 31) / 32;
+    __shared__ float2 all[MAX_SLAB_GROUPS];
+    const Tile w = tile<V>(a);
+    const int parts = a.chunks / STREAM_CLUSTER, lane = threadIdx.x & 31;
+    const float2 *part = a.part + (int64_t)w.b * parts * a.G + w.slab * a.groups;
+    for (int g = threadIdx.x >> 5; g < a.groups; g += THREADS / 32) {           // a warp per group
+        float2 t[EACH];
+        float n[EACH], s = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int k = lane + 32 * e;
+            t[e] = k < parts ? part[(int64_t)k * a.G + g] : make_float2(0.0f, 0.0f);
+            n[e] = k < parts ? (float)(min(a.P, (k + 1) * STREAM_CLUSTER * a.ppc) - min(a.P, k * STREAM_CLUSTER * a.ppc)) * (float)a.Cg
+                             : 0.0f;
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) s = fmaf(n[e], t[e].x, s);
+        const float mean = warp_sum(s) * a.inv_total;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const float d = t[e].x - mean;
+            if (n[e] > 0.0f) q += fmaf(d * d, n[e], t[e].y);
+        }
+        const float rstd = rsqrtf(fmaf(warp_sum(q), a.inv_total, a.eps));
+        if (lane == 0) {
+            all[g] = make_float2(mean, rstd);
+            const int64_t at = (int64_t)w.b * a.G + w.slab * a.groups + g;
+            if (w.rank == 0 && a.mean) a.mean[at] = mean;
+            if (w.rank == 0 && a.rstd) a.rstd[at] = rstd;
+        }
+    }
+    __syncthreads();
+    if (w.n == 0) return;
+    Pair nm[NP], sc[NP], sh[NP];
+    {
+        float mean[GPT], rstd[GPT];
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            const float2 t = all[a.by_per.div(w.lane * GPT + g)];
+            mean[g] = t.x;
+            rstd[g] = t.y;
+        }
+        coefficients<V, GPT>(a, w.c, mean, rstd, nm, sc, sh);
+    }
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    with_act(a.act, [&](auto act) {
+        apply_pixels<T, TY, V, V == 1 ? 8 : 4, act.value>(static_cast<const T *>(a.x) + p * a.ldx + w.c,
+                                                          (int64_t)w.rows * a.ldx, static_cast<TY *>(a.y) + p * a.ldy + w.c,
+                                                          (int64_t)w.rows * a.ldy, w.n, nm, sc, sh);
+    });
+}
+
+// The kernels of a plan: one, or the two of images in chunks.
+struct Kernels {
+    void (*one)(Args), (*stats)(Args), (*apply)(Args);
+};
+template <typename T, typename TY, int V, int GPT>
+static Kernels kernels_of(bool held) {
+    return {held ? held_kernel<T, TY, V, GPT, V == 1 ? 32 : 8> : reread_kernel<T, TY, V, GPT>, chunk_stats_kernel<T, V, GPT>,
+            chunk_apply_kernel<T, TY, V, GPT>};
+}
+
 template <typename T, typename TY>
 static minw_status forward(Args a, int V, cudaStream_t s) {
     Plan pl;
-    if (Args f = a; one_pass(f, pl, (int)sizeof(T), V, false)) {
-        const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
-        if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
-        void (*kern)(Args) = pl.V == 1 ? fused_of<T, TY, 1, 1>(pl.NV)
-                           : pl.V == 4 ? (pl.GPT == 1 ? fused_of<T, TY, 4, 1>(pl.NV) : pl.GPT == 2 ? fused_of<T, TY, 4, 2>(pl.NV)
-                                                                                       : fused_of<T, TY, 4, 4>(pl.NV))
-                                       : nullptr;
+    if (plan(a, pl, (int)sizeof(T), V, false)) {
+        Kernels k = pl.V == 1    ? kernels_of<T, TY, 1, 1>(pl.held)
+                    : pl.GPT == 1 ? kernels_of<T, TY, 4, 1>(pl.held)
+                    : pl.GPT == 2 ? kernels_of<T, TY, 4, 2>(pl.held)
+                                  : kernels_of<T, TY, 4, 4>(pl.held);
         if constexpr (sizeof(T) == 2 && sizeof(TY) == 2)
             if (pl.V == 8)
-                kern = pl.GPT == 1   ? fused_of<T, TY, 8, 1>(pl.NV)
-                       : pl.GPT == 2 ? fused_of<T, TY, 8, 2>(pl.NV)
-                                     : fused_of<T, TY, 8, 4>(pl.NV);
-        if (launch_cluster(kern, blocks, s, f) != cudaSuccess) return MINW_ECUDA;
+                k = pl.GPT == 1   ? kernels_of<T, TY, 8, 1>(pl.held)
+                    : pl.GPT == 2 ? kernels_of<T, TY, 8, 2>(pl.held)
+                                  : kernels_of<T, TY, 8, 4>(pl.held);
+        if (pl.one) {
+            const int64_t blocks = (int64_t)a.B * a.slabs * a.chunks;
+            if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
+            return launch_cluster(k.one, blocks, a.chunks, s, a) == cudaSuccess ? launch_status() : MINW_ECUDA;
+        }
+        int64_t blocks;
+        if (!in_chunks(a, true, blocks)) return MINW_EUNSUPPORTED;
+        if (launch_cluster(k.stats, blocks, STREAM_CLUSTER, s, a) != cudaSuccess || launch(k.apply, blocks, s, a) != cudaSuccess)
+            return MINW_ECUDA;
         return launch_status();
     }
     lanes(a, V);
-    const int64_t blocks = (int64_t)a.B * a.chunks * a.slabs;
-    if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
     void (*stat)(Args) = V == 4 ? stat_kernel<T, 4> : stat_kernel<T, 1>;
     void (*apply)(Args) = V == 4 ? apply_kernel<T, TY, 4> : apply_kernel<T, TY, 1>;
     if constexpr (sizeof(T) == 2 && sizeof(TY) == 2)
@@ -385,6 +545,8 @@ static minw_status forward(Args a, int V, cudaStream_t s) {
             stat = stat_kernel<T, 8>;
             apply = apply_kernel<T, TY, 8>;
         }
+    int64_t blocks;
+    if (!in_chunks(a, false, blocks)) return MINW_EUNSUPPORTED;
     if (launch(stat, blocks, s, a) != cudaSuccess || launch(stat_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess ||
         launch(apply, blocks, s, a) != cudaSuccess)
         return MINW_ECUDA;
@@ -401,7 +563,7 @@ extern "C" {
 
 size_t minw_group_norm_workspace_bytes(int32_t B, int64_t P, int32_t C, int32_t G, int32_t backward) {
     if (B <= 0 || P <= 0 || C <= 0 || G <= 0 || C % G != 0 || P >= (1ll << 30)) return 0;
-    return gn::layout(B, P, C, G, backward != 0).total;
+    return gn::layout(B, C, G, backward != 0).total;
 }
 
 minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamma, const float *beta,
@@ -416,15 +578,12 @@ minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const fl
         return MINW_EINVAL;
     if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;
     if (B == 0) return MINW_OK;
-    const gn::Layout l = gn::layout(B, P, C, G, false);
+    const gn::Layout l = gn::layout(B, C, G, false);
     if (!workspace || !aligned16(workspace) || workspace_bytes < l.total) return MINW_EINVAL;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     gn::Args a{};
     a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
     a.B = B; a.P = (int)P; a.C = C; a.G = G; a.Cg = C / G; a.act = act; a.eps = eps;
-    a.chunks = gn::chunks_of(B, P);
-    a.ppc = (int)((P + a.chunks - 1) / a.chunks);
-    a.chunks = (int)((P + a.ppc - 1) / a.ppc);                // no chunk without a pixel
     a.part = reinterpret_cast<float2 *>(ws + l.part);
     a.stat = reinterpret_cast<float2 *>(ws + l.stat);
     int V = x_type == MINW_BF16 && y_type == MINW_BF16 ? 8 : 4;       // 16 bytes of the wider type

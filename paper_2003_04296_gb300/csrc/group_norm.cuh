@@ -35,7 +35,8 @@ struct Args {
     const float *gamma, *beta;     // nullable
     const float *mean_in, *rstd_in;
     float *mean, *rstd;            // forward: saved statistics (nullable)
-    float2 *part;                  // streaming: per image, chunk and channel (mean, M2), or (sum dz, sum dz xh)
+    float2 *part;                  // per image, cluster of chunks and group, or chunk and channel: (mean, M2); the backward's
+                                   // per image, chunk and channel (sum dz, sum dz xh)
     float2 *stat;                  // streaming: per image and group (mean, rstd), or (s1, s2)
     float2 *chan;                  // backward: per image and channel (sum dz, sum dz xh)
     float *dgamma, *dbeta;         // nullable
@@ -43,12 +44,12 @@ struct Args {
     float eps;
     int chunks, ppc;               // pixel chunks per image, pixels per chunk
     int L, slabs;                  // lanes (V channels each) of a slab, slabs of a row
-    // one pass
+    // slabs of whole groups
     int butterfly;                 // lanes and the lanes of a group are powers of two within a warp
     int rows, groups, per;         // pixel rows of a block, groups of a slab, entries (a thread's share of a group) of a group
     float inv_total;               // 1 / (P Cg)
     int seg;                       // backward: threads that sum a channel's rows
-    Div by_L, by_rows, by_per, by_chunks, by_slabs, by_channels;
+    Div by_L, by_rows, by_per, by_Cg, by_chunks, by_slabs, by_channels;
 };
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -67,10 +68,106 @@ __device__ __forceinline__ void load_affine(const Args &a, int c, float *ga, flo
     }
 }
 
+// Statistics of a thread's n pixels, `step` values apart, of V channels: means and M2 of each channel, in pairs.  U pixels
+// at a time: their mean and M2 by themselves, merged into the channel's.
+template <typename T, int V, int U>
+__device__ __forceinline__ void channel_stats(const T *x, int64_t step, int n, Pair *m, Pair *q) {
+    constexpr int NP = (V + 1) / 2;
+#pragma unroll
+    for (int k = 0; k < NP; ++k) m[k] = q[k] = pair(0.0f, 0.0f);
+    int i = 0;
+    for (; i + U <= n; i += U, x += U * step) {
+        Vec<T, V> v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u].load(x + u * step);
+        const float share = __fdividef((float)U, (float)(i + U)), cross = (float)i * share;
+        const Pair inv = pair(1.0f / U, 1.0f / U), sh = pair(share, share), cr = pair(cross, cross), minus = pair(-1.0f, -1.0f);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            Pair s = v[0].get2(k);
+#pragma unroll
+            for (int u = 1; u < U; ++u) s = add2(s, v[u].get2(k));
+            s = mul2(s, inv);
+            const Pair ns = mul2(s, minus);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const Pair d = add2(v[u].get2(k), ns);
+                q[k] = fma2(d, d, q[k]);
+            }
+            const Pair d = fma2(m[k], minus, s);
+            m[k] = fma2(d, sh, m[k]);
+            q[k] = fma2(mul2(d, d), cr, q[k]);
+        }
+    }
+    if (i == n) return;
+    // the last few: their loads together, then one by one
+    Vec<T, V> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (i + u < n) v[u].load(x + u * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        if (i + u >= n) break;
+        const float share = __fdividef(1.0f, (float)(i + u + 1)), cross = (float)(i + u) * share;
+        const Pair sh = pair(share, share), cr = pair(cross, cross), minus = pair(-1.0f, -1.0f);
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            const Pair d = fma2(m[k], minus, v[u].get2(k));
+            m[k] = fma2(d, sh, m[k]);
+            q[k] = fma2(mul2(d, d), cr, q[k]);
+        }
+    }
+}
+
+// f(u, i) for a thread's n pixels, U at a time, after load(u, i) for all of those.
+template <int U, typename L, typename F>
+__device__ __forceinline__ void batches(int n, L load, F f) {
+    int i = 0;
+    for (; i + U <= n; i += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) load(u, i + u);
+#pragma unroll
+        for (int u = 0; u < U; ++u) f(u, i + u);
+    }
+    if (i == n) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (i + u < n) load(u, i + u);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (i + u < n) f(u, i + u);
+}
+
+// y = act((x - mean) a + b) on a thread's n pixels: minus the means, a = rstd gamma and b = beta in pairs.
+template <typename T, typename TY, int V, int U, int ACT>
+__device__ __forceinline__ void apply_pixels(const T *x, int64_t xstep, TY *y, int64_t ystep, int n, const Pair *nm,
+                                             const Pair *a, const Pair *b) {
+    constexpr int NP = (V + 1) / 2;
+    Vec<T, V> v[U];
+    batches<U>(
+        n,
+        [&](int u, int) {
+            v[u].load(x);
+            x += xstep;
+        },
+        [&](int u, int) {
+            float z[2 * NP];
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                const float2 h = halves(fma2(add2(v[u].get2(k), nm[k]), a[k], b[k]));
+                z[2 * k] = act_value<ACT>(h.x);
+                z[2 * k + 1] = act_value<ACT>(h.y);
+            }
+            Vec<TY, V> o;
+            o.set(z);
+            o.store(y);
+            y += ystep;
+        });
+}
+
 // Where a block of the streaming kernels works: image, chunk of its pixels, slab of its channels.
 struct Place {
-    int b, chunk, slab, p0, p1, rows, row, c;
-    bool active;
+    int b, chunk, slab, p0, p1, rows, row, lane, c, n;
 };
 template <int V>
 __device__ __forceinline__ Place place(const Args &a, int64_t block) {
@@ -83,18 +180,21 @@ __device__ __forceinline__ Place place(const Args &a, int64_t block) {
     w.p1 = min(a.P, w.p0 + a.ppc);
     w.rows = THREADS / a.L;
     w.row = (int)threadIdx.x / a.L;
-    w.c = (w.slab * a.L + (int)threadIdx.x % a.L) * V;
-    w.active = w.row < w.rows && w.c < a.C;
+    w.lane = (int)threadIdx.x % a.L;
+    w.c = (w.slab * a.L + w.lane) * V;
+    const bool some = w.row < w.rows && w.c < a.C && w.p0 + w.row < w.p1;
+    w.n = some ? (w.p1 - w.p0 - w.row - 1) / w.rows + 1 : 0;
     return w;
 }
 
 // ---------------------------------------------------------------------------
-// One pass: an image's slab of whole groups (L lanes of V channels) stays in
-// the registers of a block, or of a cluster of blocks that split its pixels;
-// x (and dy) are read once.
+// One kernel: a block, or a cluster of blocks that split the pixels, takes an
+// image's slab of whole groups (L lanes of V channels).  Small slabs stay in
+// its registers; larger ones are read again, from L2, once their sums are known.
 // ---------------------------------------------------------------------------
 
 constexpr int MAX_SLAB_GROUPS = 256;
+constexpr int HELD_CLUSTER = 2, HELD_CLUSTER_BWD = 4;        // blocks of a cluster that holds its slab in registers, at most
 
 struct Tile {
     int b, slab, rank, p0, p1, lane, row, rows, c, n;      // n: pixels of this thread
@@ -135,9 +235,12 @@ using namespace minw_host;
 
 inline size_t al256(size_t v) { return (v + 255) & ~(size_t)255; }
 
-// Pixel chunks per image of the streaming kernels: about eight blocks per SM over all images, at least 64 pixels each.
-inline int chunks_of(int B, int64_t P) {
-    int64_t k = (8 * 152 + B - 1) / B;
+// Resident blocks of the streaming kernels (half of them in the backward), and the chunks that a cluster merges.
+constexpr int STREAM_BLOCKS = 4 * 152, STREAM_CLUSTER = 4;
+
+// Pixel chunks per image for B images of so many slabs, at least 64 pixels each.
+inline int chunks_of(int blocks, int B, int slabs, int64_t P) {
+    int64_t k = blocks / ((int64_t)B * slabs);
     if (k > (P + 63) / 64) k = (P + 63) / 64;
     return (int)(k < 1 ? 1 : k);
 }
@@ -145,11 +248,11 @@ inline int chunks_of(int B, int64_t P) {
 struct Layout {
     size_t part, stat, chan, total;
 };
-inline Layout layout(int B, int64_t P, int C, int G, bool backward) {
+inline Layout layout(int B, int C, int G, bool backward) {
     Layout l;
     size_t off = 0;
     auto take = [&](size_t n) { const size_t r = off; off += al256(n * sizeof(float2)); return r; };
-    l.part = take((size_t)B * chunks_of(B, P) * C);
+    l.part = take((size_t)(B > STREAM_BLOCKS ? B : STREAM_BLOCKS) * C);      // B chunks_of(B) at most, for fewer images too
     l.stat = take((size_t)B * G);
     l.chan = backward ? take((size_t)B * C) : off;
     l.total = off;
@@ -174,63 +277,95 @@ inline cudaError_t launch(void (*kern)(Args), int64_t blocks, cudaStream_t s, co
     return launch_pdl_stream(false, kern, dim3((unsigned)blocks), dim3(THREADS), 0, s, a);
 }
 
-// Lanes and slabs of the streaming kernels for V channels a lane.
+// Lanes and slabs, V channels a lane, without regard to groups.
 inline void lanes(Args &a, int V) {
-    const int lanes = a.C / V;
-    a.slabs = (lanes + THREADS - 1) / THREADS;
-    a.L = (lanes + a.slabs - 1) / a.slabs;
+    const int all = a.C / V;
+    a.slabs = (all + THREADS - 1) / THREADS;
+    a.L = (all + a.slabs - 1) / a.slabs;
 }
 
-// The one-pass plan: slabs of whole groups, at least 128 bytes of a row wide where one fits (64, then 32 where not), the
-// narrowest such, so that the blocks are many and their clusters small; clusters of at most 16 blocks of
-// THREADS / L rows of NV pixels.
+// The plan for slabs of whole groups: at least 128 bytes of a row wide where one fits (64 where not: the
+// memory's lines are 128 bytes, or where the wide ones are too few to fill the SMs), the narrowest such, so that the
+// blocks are many.
 struct Plan {
-    int V, GPT, NV;
+    int V, GPT;
+    bool one, held;               // one kernel, with x in registers; false: images in chunks
 };
-inline bool one_pass(Args &a, Plan &pl, int bytes, int V0, bool backward) {
-    pl.V = V0 == 8 && a.Cg % 2 != 0 ? 4 : V0;
+inline bool plan(Args &a, Plan &pl, int bytes, int V0, bool backward) {
+    const int sms = num_sms() > 0 ? num_sms() : 152, places = (backward ? 2 : 4) * sms;      // resident blocks
+    pl.V = V0 == 8 && a.Cg % 2 != 0 && !backward ? 4 : V0;
     pl.GPT = a.Cg % pl.V == 0 ? 1 : pl.V == 8 ? (a.Cg % 4 == 0 ? 2 : 4) : a.Cg % 2 == 0 ? 2 : pl.V;
-    for (int width = 128; width >= 32; width /= 2)
-        for (int k = 1; k <= a.G && k <= MAX_SLAB_GROUPS; ++k) {
-            const int channels = k * a.Cg;
-            if (a.G % k != 0 || channels % pl.V != 0 || (channels * bytes < width && k < a.G)) continue;
-            const int L = channels / pl.V;
-            if (L > THREADS) break;
-            const int rows = THREADS / L;
-            // the backward holds two tensors, so never more than 8 vectors of each
-            pl.NV = pl.V == 1 ? 32 : backward || a.P <= 64 * rows ? 8 : 16;
-            const int64_t cap = (int64_t)rows * pl.NV, cluster = (a.P + cap - 1) / cap;
-            if (cluster > 16 || (backward && cluster > 1 && rows < 2)) break;     // a cluster's totals go behind the block's sums
-            a.per = a.Cg / (pl.V / pl.GPT);
-            a.butterfly = L <= 32 && (L & (L - 1)) == 0 && (a.per == 1 || (pl.GPT == 1 && (a.per & (a.per - 1)) == 0));
-            a.rows = rows;
-            a.groups = k;
-            a.L = L;
-            a.slabs = a.G / k;
-            a.inv_total = (float)(1.0 / ((double)a.P * a.Cg));
-            a.seg = channels >= THREADS ? 1 : THREADS / channels < rows ? THREADS / channels : rows;
-            a.by_channels = Div((uint32_t)channels);
-            a.by_L = Div(L);
-            a.by_rows = Div(rows);
-            a.by_per = Div(a.per);
-            a.by_chunks = Div((uint32_t)cluster);
-            a.by_slabs = Div((uint32_t)a.slabs);
-            a.chunks = (int)cluster;
-            a.ppc = (int)((a.P + cluster - 1) / cluster);
-            return true;
+    int k = 0, channels = 0, L = 0, rows = 0, cluster = 0;
+    // t groups make a slab: whole lines of rows that begin on one, whole rows, or at least `width` bytes
+    auto slab = [&](int width, bool lines) {
+        for (int t = 1; t <= a.G && t <= MAX_SLAB_GROUPS && t * a.Cg / pl.V <= THREADS; ++t) {
+            if (a.G % t != 0 || t * a.Cg % pl.V != 0 || t * a.Cg * bytes < (t == a.G ? 0 : width)) continue;
+            if (lines && t != a.G && (t * a.Cg * bytes % 128 != 0 || a.ldx * bytes % 128 != 0)) continue;
+            if (lines && t * a.Cg * bytes > 512) break;
+            k = t;
+            return;
         }
-    return false;
+    };
+    slab(128, true);
+    if (k == 0) slab(128, false);
+    const int wide = k;
+    if (k == 0 || (int64_t)a.B * (a.G / k) * 8 < places) slab(64, false);
+    if (wide != 0 && (int64_t)a.B * (a.G / k) * 8 < sms) k = wide;      // images in chunks: the chunks fill the SMs
+    if (k == 0) slab(32, false);
+    if (k == 0) return false;
+    channels = k * a.Cg;
+    L = channels / pl.V;
+    rows = THREADS / L;
+    const int64_t slabs = (int64_t)a.B * (a.G / k);
+    const int cap = rows * (pl.V == 1 ? 32 : 8);
+    cluster = (a.P + cap - 1) / cap;
+    pl.held = cluster <= (backward ? HELD_CLUSTER_BWD : HELD_CLUSTER);
+    if (!pl.held) {
+        // as many blocks as fit at a time; in the backward twice as many where a thread still has 16 pixels
+        for (cluster = 1; cluster < 8 && slabs * cluster * 2 <= places; cluster *= 2) {}
+        if (backward && cluster < 8 && slabs * cluster <= places && a.P >= 32 * cluster * rows) cluster *= 2;
+    }
+    pl.one = pl.held || slabs * cluster >= sms;                         // fewer blocks than SMs: in chunks
+    if (backward && (!pl.one || (cluster > 1 && rows < 2))) return false;              // a cluster's totals go behind the block's sums
+    a.per = a.Cg / (pl.V / pl.GPT);
+    a.butterfly = L <= 32 && (L & (L - 1)) == 0 && (a.per == 1 || (pl.GPT == 1 && (a.per & (a.per - 1)) == 0));
+    a.rows = rows;
+    a.groups = k;
+    a.L = L;
+    a.slabs = a.G / k;
+    a.chunks = cluster;
+    a.ppc = (a.P + cluster - 1) / cluster;
+    a.inv_total = (float)(1.0 / ((double)a.P * a.Cg));
+    a.seg = channels >= THREADS ? 1 : THREADS / channels < rows ? THREADS / channels : rows;
+    a.by_channels = Div((uint32_t)channels);
+    a.by_L = Div(L);
+    a.by_rows = Div(rows);
+    a.by_per = Div(a.per);
+    a.by_Cg = Div(a.Cg);
+    a.by_chunks = Div((uint32_t)cluster);
+    a.by_slabs = Div((uint32_t)a.slabs);
+    return true;
 }
 
-inline cudaError_t launch_cluster(void (*kern)(Args), int64_t blocks, cudaStream_t s, const Args &a) {
-    if (a.chunks > 8 && !allow_large_clusters(reinterpret_cast<const void *>(kern))) return cudaErrorInvalidValue;
+// Chunks of images: for the kernels that merge clusters of them (the last chunks may then be empty), or not.
+inline bool in_chunks(Args &a, bool clusters, int64_t &blocks) {
+    a.chunks = chunks_of(a.dy ? STREAM_BLOCKS / 2 : STREAM_BLOCKS, a.B, a.slabs, a.P);
+    a.ppc = (a.P + a.chunks - 1) / a.chunks;
+    a.chunks = (a.P + a.ppc - 1) / a.ppc;                           // no chunk without a pixel
+    if (clusters) a.chunks = (a.chunks + STREAM_CLUSTER - 1) / STREAM_CLUSTER * STREAM_CLUSTER;
+    a.by_chunks = Div((uint32_t)a.chunks);
+    blocks = (int64_t)a.B * a.chunks * a.slabs;
+    return blocks < (1ll << 31) && (int64_t)a.B * a.G < (1ll << 31);
+}
+
+inline cudaError_t launch_cluster(void (*kern)(Args), int64_t blocks, int cluster, cudaStream_t s, const Args &a) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(THREADS);
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = (unsigned)a.chunks;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;

@@ -11,61 +11,135 @@ namespace gn {
 // second pass over x and dy.
 // ---------------------------------------------------------------------------
 
-// Statistics of the V channels at c.
+// What a thread's V channels need, in pairs: minus the means, rstd, gamma, beta.
 template <int V>
-__device__ __forceinline__ void load_stats(const Args &a, int b, int c, float *mean, float *rstd) {
+struct Coef {
+    static constexpr int NP = (V + 1) / 2;
+    Pair nm[NP], r[NP], ga[NP], be[NP];
+
+    __device__ __forceinline__ void load(const Args &a, int b, int c) {
+        float g[V], h[V], mean[V], rstd[V];
+        load_affine<V>(a, c, g, h);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int64_t g = (int64_t)b * a.G + (c + i) / a.Cg;
-        mean[i] = a.mean_in[g];
-        rstd[i] = a.rstd_in[g];
+        for (int i = 0; i < V; ++i) {
+            const int64_t at = (int64_t)b * a.G + (c + i) / a.Cg;
+            mean[i] = -a.mean_in[at];
+            rstd[i] = a.rstd_in[at];
+        }
+#pragma unroll
+        for (int k = 0; k < NP; ++k) {
+            nm[k] = pick<V>(mean, k);
+            r[k] = pick<V>(rstd, k);
+            ga[k] = pick<V>(g, k);
+            be[k] = pick<V>(h, k);
+        }
+    }
+};
+
+// Sums of dz and dz xh of one pixel's channels.
+template <int ACT, int V, typename X, typename D>
+__device__ __forceinline__ void add_pixel(const X &x, const D &dy, const Coef<V> &co, Pair *db, Pair *dg) {
+#pragma unroll
+    for (int k = 0; k < Coef<V>::NP; ++k) {
+        const Pair xh = mul2(add2(x.get2(k), co.nm[k]), co.r[k]);
+        const Pair dz = act_grad2<ACT>(fma2(xh, co.ga[k], co.be[k]), dy.get2(k));
+        db[k] = add2(db[k], dz);
+        dg[k] = fma2(dz, xh, dg[k]);
+    }
+}
+
+// dx of one pixel: minus s1 and s2 of its channels' groups in pairs.
+template <int ACT, int V, typename X, typename D>
+__device__ __forceinline__ X pixel_gradient(const X &x, const D &dy, const Coef<V> &co, const Pair *ns1, const Pair *ns2) {
+    float o[2 * Coef<V>::NP];
+#pragma unroll
+    for (int k = 0; k < Coef<V>::NP; ++k) {
+        const Pair xh = mul2(add2(x.get2(k), co.nm[k]), co.r[k]);
+        const Pair dz = act_grad2<ACT>(fma2(xh, co.ga[k], co.be[k]), dy.get2(k));
+        const float2 h = halves(mul2(co.r[k], fma2(xh, ns2[k], fma2(co.ga[k], dz, ns1[k]))));
+        o[2 * k] = h.x;
+        o[2 * k + 1] = h.y;
+    }
+    X r;
+    r.set(o);
+    return r;
+}
+
+// Sums over a thread's n pixels, `step` values apart.
+template <typename T, typename TD, int V, int U>
+__device__ __forceinline__ void channel_sums(int act, const T *x, int64_t xstep, const TD *dy, int64_t dstep, int n,
+                                             const Coef<V> &co, Pair *db, Pair *dg) {
+#pragma unroll
+    for (int k = 0; k < Coef<V>::NP; ++k) db[k] = dg[k] = pair(0.0f, 0.0f);
+    with_act(act, [&](auto act_) {
+        const T *px = x;
+        const TD *pd = dy;
+        Vec<T, V> v[U];
+        Vec<TD, V> d[U];
+        batches<U>(
+            n,
+            [&](int u, int) {
+                v[u].load(px);
+                d[u].load(pd);
+                px += xstep;
+                pd += dstep;
+            },
+            [&](int u, int) { add_pixel<act_.value, V>(v[u], d[u], co, db, dg); });
+    });
+}
+
+template <typename T, typename TD, int V, int U>
+__device__ __forceinline__ void gradient_pixels(int act, const T *x, int64_t xstep, const TD *dy, int64_t dstep, T *dx,
+                                                int64_t ostep, int n, const Coef<V> &co, const Pair *ns1,
+                                                const Pair *ns2) {
+    with_act(act, [&](auto act_) {
+        const T *px = x;
+        const TD *pd = dy;
+        T *po = dx;
+        Vec<T, V> v[U];
+        Vec<TD, V> d[U];
+        batches<U>(
+            n,
+            [&](int u, int) {
+                v[u].load(px);
+                d[u].load(pd);
+                px += xstep;
+                pd += dstep;
+            },
+            [&](int u, int) {
+                pixel_gradient<act_.value, V>(v[u], d[u], co, ns1, ns2).store(po);
+                po += ostep;
+            });
+    });
+}
+
+// A thread's channel sums into its row of the block's.
+template <int V>
+__device__ __forceinline__ void put_sums(float2 *at, const Pair *db, const Pair *dg) {
+#pragma unroll
+    for (int k = 0; k < (V + 1) / 2; ++k) {
+        const float2 b = halves(db[k]), g = halves(dg[k]);
+        at[2 * k] = make_float2(b.x, g.x);
+        if (V > 1) at[2 * k + 1] = make_float2(b.y, g.y);
     }
 }
 
 template <typename T, typename TD, int V>
-__global__ void __launch_bounds__(THREADS) bwd_sum_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, 2) bwd_sum_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int U = V == 1 ? 8 : 2;
     __shared__ float2 red[THREADS * V];
     const Place w = place<V>(a, blockIdx.x);
-    float db[V], dg[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) db[i] = dg[i] = 0.0f;
-    if (w.active) {
-        float ga[V], be[V], mean[V], rstd[V];
-        load_affine<V>(a, w.c, ga, be);
-        load_stats<V>(a, w.b, w.c, mean, rstd);
-        const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
-        const TD *dy = static_cast<const TD *>(a.dy) + (int64_t)w.b * a.P * a.lddy + w.c;
-        with_act(a.act, [&](auto act) {
-            for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
-                Vec<T, V> v[U];
-                Vec<TD, V> d[U];
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (p + u * w.rows < w.p1) {
-                        v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-                        d[u].load(dy + (int64_t)(p + u * w.rows) * a.lddy);
-                    }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    if (p + u * w.rows >= w.p1) break;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const float xh = (v[u].get(i) - mean[i]) * rstd[i];
-                        const float dz = act_grad<act.value>(fmaf(xh, ga[i], be[i]), d[u].get(i));
-                        db[i] += dz;
-                        dg[i] = fmaf(dz, xh, dg[i]);
-                    }
-                }
-            }
-        });
-    }
     const int W = a.L * V;
     if (w.row < w.rows) {
-#pragma unroll
-        for (int i = 0; i < V; ++i) red[w.row * W + ((int)threadIdx.x % a.L) * V + i] = make_float2(db[i], dg[i]);
+        Pair db[Coef<V>::NP], dg[Coef<V>::NP];
+        Coef<V> co;
+        if (w.n > 0) co.load(a, w.b, w.c);
+        const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+        channel_sums<T, TD, V, V == 1 ? 8 : 4>(a.act, static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
+                                               static_cast<const TD *>(a.dy) + p * a.lddy + w.c, w.rows * a.lddy, w.n, co,
+                                               db, dg);
+        put_sums<V>(red + w.row * W + w.lane * V, db, dg);
     }
     __syncthreads();
     for (int e = threadIdx.x; e < W; e += THREADS) {
@@ -116,112 +190,54 @@ __global__ void __launch_bounds__(THREADS) bwd_merge_kernel(Args a) {
 }
 
 template <typename T, typename TD, int V>
-__global__ void __launch_bounds__(THREADS) bwd_apply_kernel(Args a) {
+__global__ void __launch_bounds__(THREADS, 2) bwd_apply_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int U = V == 1 ? 8 : 2;
     const Place w = place<V>(a, (int64_t)gridDim.x - 1 - blockIdx.x);
-    if (!w.active) return;
-    float ga[V], be[V], mean[V], rstd[V], s1[V], s2[V];
-    load_affine<V>(a, w.c, ga, be);
-    load_stats<V>(a, w.b, w.c, mean, rstd);
+    if (w.n == 0) return;
+    Coef<V> co;
+    co.load(a, w.b, w.c);
+    Pair ns1[Coef<V>::NP], ns2[Coef<V>::NP];
+    {
+        float s1[V], s2[V];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
-        s1[i] = t.x;
-        s2[i] = t.y;
-    }
-    const T *x = static_cast<const T *>(a.x) + (int64_t)w.b * a.P * a.ldx + w.c;
-    const TD *dy = static_cast<const TD *>(a.dy) + (int64_t)w.b * a.P * a.lddy + w.c;
-    T *dx = static_cast<T *>(a.y) + (int64_t)w.b * a.P * a.ldy + w.c;
-    with_act(a.act, [&](auto act) {
-        for (int p = w.p0 + w.row; p < w.p1; p += U * w.rows) {
-            Vec<T, V> v[U];
-            Vec<TD, V> d[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (p + u * w.rows < w.p1) {
-                    v[u].load(x + (int64_t)(p + u * w.rows) * a.ldx);
-                    d[u].load(dy + (int64_t)(p + u * w.rows) * a.lddy);
-                }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (p + u * w.rows >= w.p1) break;
-                float o[V];
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float xh = (v[u].get(i) - mean[i]) * rstd[i];
-                    const float dz = act_grad<act.value>(fmaf(xh, ga[i], be[i]), d[u].get(i));
-                    o[i] = rstd[i] * (fmaf(ga[i], dz, -s1[i]) - xh * s2[i]);
-                }
-                Vec<T, V> r;
-                r.set(o);
-                r.store(dx + (int64_t)(p + u * w.rows) * a.ldy);
-            }
+        for (int i = 0; i < V; ++i) {
+            const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
+            s1[i] = -t.x;
+            s2[i] = -t.y;
         }
-    });
+#pragma unroll
+        for (int k = 0; k < Coef<V>::NP; ++k) {
+            ns1[k] = pick<V>(s1, k);
+            ns2[k] = pick<V>(s2, k);
+        }
+    }
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    gradient_pixels<T, TD, V, V == 1 ? 8 : 4>(a.act, static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
+                                              static_cast<const TD *>(a.dy) + p * a.lddy + w.c, w.rows * a.lddy,
+                                              static_cast<T *>(a.y) + p * a.ldy + w.c, w.rows * a.ldy, w.n, co, ns1, ns2);
 }
 
 // ---------------------------------------------------------------------------
-// One pass over x and dy.
+// One kernel.
 // ---------------------------------------------------------------------------
 
-template <typename T, typename TD, int V, int GPT, int NV>
-__global__ void __launch_bounds__(THREADS, 2) fused_bwd_kernel(Args a) {
-    pdl_trigger();
-    pdl_wait();
-    constexpr int W = V / GPT, NP = (V + 1) / 2;
-    __shared__ float2 red[THREADS * V];                    // rows x channels, then segments x channels
-    __shared__ float2 group[MAX_SLAB_GROUPS];
-    const Tile w = tile<V>(a);
-    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, xstep = (int64_t)w.rows * a.ldx, dstep = (int64_t)w.rows * a.lddy;
-    const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
-    const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
-    Vec<T, V> v[NV];
-    Vec<TD, V> d[NV];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-        if (i < w.n) {
-            v[i].load(x + i * xstep);
-            d[i].load(dy + i * dstep);
-        }
+template <int V>
+struct Shared {
+    float2 red[THREADS * V];               // rows x channels, then segments x channels
+    float2 group[MAX_SLAB_GROUPS];
+};
+
+// Minus s1 and s2 of a thread's channels from its sums: the block's rows, the cluster's blocks, the groups' channels, all
+// in a fixed order; and the image's channel sums for dgamma and dbeta.  Afterwards a cluster has arrived at its end.
+template <int V>
+__device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &sm, const Pair *db, const Pair *dg, Pair *ns1,
+                                       Pair *ns2) {
     const int CW = a.L * V;                                // channels of the slab
-    float ga[V], be[V], mean[GPT], rstd[GPT];
-    load_affine<V>(a, w.c, ga, be);
-#pragma unroll
-    for (int g = 0; g < GPT; ++g) {
-        const int64_t at = (int64_t)w.b * a.G + w.slab * a.groups + a.by_per.div(w.lane * GPT + g);
-        mean[g] = a.mean_in[at];
-        rstd[g] = a.rstd_in[at];
-    }
-    {
-        Pair db[NP], dg[NP];
-#pragma unroll
-        for (int k = 0; k < NP; ++k) db[k] = dg[k] = pair(0.0f, 0.0f);
-        with_act(a.act, [&](auto act) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (i < w.n) {
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const Pair xh = mul2(add2(v[i].get2(k), pick_group<V, W>(mean, k, -1.0f)), pick_group<V, W>(rstd, k));
-                        const Pair dz = act_grad2<act.value>(fma2(xh, pick<V>(ga, k), pick<V>(be, k)), d[i].get2(k));
-                        db[k] = add2(db[k], dz);
-                        dg[k] = fma2(dz, xh, dg[k]);
-                    }
-                }
-        });
-        if (w.row < w.rows) {
-#pragma unroll
-            for (int k = 0; k < NP; ++k) {
-                const float2 b = halves(db[k]), g = halves(dg[k]);
-                red[w.row * CW + w.lane * V + 2 * k] = make_float2(b.x, g.x);
-                if (V > 1) red[w.row * CW + w.lane * V + 2 * k + 1] = make_float2(b.y, g.y);
-            }
-        }
-    }
+    float2 *red = sm.red;
+    if (w.row < w.rows) put_sums<V>(red + w.row * CW + w.lane * V, db, dg);
     __syncthreads();
-    // channel sums of this block: `seg` threads a channel, each every so many rows (into the row of its number)
+    // `seg` threads a channel, each every so many rows (into the row of its number)
     for (int s = a.by_channels.div((int)threadIdx.x), c = (int)threadIdx.x - s * CW; s < a.seg;) {
         float2 t = red[s * CW + c];
         for (int r = s + a.seg; r < w.rows; r += a.seg) {
@@ -248,13 +264,16 @@ __global__ void __launch_bounds__(THREADS, 2) fused_bwd_kernel(Args a) {
         cluster.sync();
         tot = red + CW;
         for (int c = threadIdx.x; c < CW; c += THREADS) {
-            float2 t = make_float2(0.0f, 0.0f);
-            for (int k = 0; k < a.chunks; ++k) {
-                const float2 u = *cluster.map_shared_rank(&red[c], k);
-                t.x += u.x;
-                t.y += u.y;
+            float2 u[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                u[k] = k < a.chunks ? *cluster.map_shared_rank(&red[c], k) : make_float2(0.0f, 0.0f);
+#pragma unroll
+            for (int k = 1; k < 8; ++k) {
+                u[0].x += u[k].x;
+                u[0].y += u[k].y;
             }
-            tot[c] = t;
+            tot[c] = u[0];
         }
         cluster_done_reading();
     }
@@ -271,40 +290,87 @@ __global__ void __launch_bounds__(THREADS, 2) fused_bwd_kernel(Args a) {
         }
         s1 = warp_sum(s1);
         s2 = warp_sum(s2);
-        if ((threadIdx.x & 31) == 0) group[g] = make_float2(s1 * a.inv_total, s2 * a.inv_total);
+        if ((threadIdx.x & 31) == 0) sm.group[g] = make_float2(-s1 * a.inv_total, -s2 * a.inv_total);
     }
     __syncthreads();
-    if (w.n > 0) {
-        float s1[GPT], s2[GPT];
+    float f1[V], f2[V];
 #pragma unroll
-        for (int g = 0; g < GPT; ++g) {
-            const float2 t = group[a.by_per.div(w.lane * GPT + g)];
-            s1[g] = t.x;
-            s2[g] = t.y;
+    for (int i = 0; i < V; ++i) {
+        const float2 t = sm.group[a.by_Cg.div(w.lane * V + i)];
+        f1[i] = t.x;
+        f2[i] = t.y;
+    }
+#pragma unroll
+    for (int k = 0; k < (V + 1) / 2; ++k) {
+        ns1[k] = pick<V>(f1, k);
+        ns2[k] = pick<V>(f2, k);
+    }
+}
+
+// In registers: at most NV pixels of each thread.
+template <typename T, typename TD, int V, int NV>
+__global__ void __launch_bounds__(THREADS, 2) held_bwd_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int NP = Coef<V>::NP;
+    __shared__ Shared<V> sm;
+    const Tile w = tile<V>(a);
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, xstep = (int64_t)w.rows * a.ldx, dstep = (int64_t)w.rows * a.lddy;
+    const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+    const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
+    Vec<T, V> v[NV];
+    Vec<TD, V> d[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+        if (i < w.n) {
+            v[i].load(x + i * xstep);
+            d[i].load(dy + i * dstep);
         }
-        T *dx = static_cast<T *>(a.y) + p * a.ldy + w.c;
-        const int64_t ostep = (int64_t)w.rows * a.ldy;
+    Coef<V> co;
+    co.load(a, w.b, w.c);
+    Pair ns1[NP], ns2[NP];
+    {
+        Pair db[NP], dg[NP];
+#pragma unroll
+        for (int k = 0; k < NP; ++k) db[k] = dg[k] = pair(0.0f, 0.0f);
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (i < w.n) {
-                    float o[2 * NP];
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const Pair r2 = pick_group<V, W>(rstd, k), gk = pick<V>(ga, k);
-                        const Pair xh = mul2(add2(v[i].get2(k), pick_group<V, W>(mean, k, -1.0f)), r2);
-                        const Pair dz = act_grad2<act.value>(fma2(xh, gk, pick<V>(be, k)), d[i].get2(k));
-                        const Pair t = fma2(gk, dz, pick_group<V, W>(s1, k, -1.0f));
-                        const float2 h = halves(mul2(r2, fma2(xh, pick_group<V, W>(s2, k, -1.0f), t)));
-                        o[2 * k] = h.x;
-                        o[2 * k + 1] = h.y;
-                    }
-                    Vec<T, V> r;
-                    r.set(o);
-                    r.store(dx + i * ostep);
-                }
+                if (i < w.n) add_pixel<act.value, V>(v[i], d[i], co, db, dg);
         });
+        totals<V>(a, w, sm, db, dg, ns1, ns2);
     }
+    T *dx = static_cast<T *>(a.y) + p * a.ldy + w.c;
+    const int64_t ostep = (int64_t)w.rows * a.ldy;
+    with_act(a.act, [&](auto act) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (i < w.n) pixel_gradient<act.value, V>(v[i], d[i], co, ns1, ns2).store(dx + i * ostep);
+    });
+    if (a.chunks > 1) cluster_leave();
+}
+
+// In two readings.
+template <typename T, typename TD, int V>
+__global__ void __launch_bounds__(THREADS, 2) reread_bwd_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int NP = Coef<V>::NP, U = V == 1 ? 8 : 4;
+    __shared__ Shared<V> sm;
+    const Tile w = tile<V>(a);
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, xstep = (int64_t)w.rows * a.ldx, dstep = (int64_t)w.rows * a.lddy;
+    const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+    const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
+    Coef<V> co;
+    co.load(a, w.b, w.c);
+    Pair ns1[NP], ns2[NP];
+    {
+        Pair db[NP], dg[NP];
+        channel_sums<T, TD, V, U>(a.act, x, xstep, dy, dstep, w.n, co, db, dg);
+        totals<V>(a, w, sm, db, dg, ns1, ns2);
+    }
+    gradient_pixels<T, TD, V, U>(a.act, x, xstep, dy, dstep, static_cast<T *>(a.y) + p * a.ldy + w.c,
+                                 (int64_t)w.rows * a.ldy, w.n, co, ns1, ns2);
     if (a.chunks > 1) cluster_leave();
 }
 
@@ -335,32 +401,23 @@ __global__ void __launch_bounds__(THREADS) affine_grad_kernel(Args a) {
     }
 }
 
-template <typename T, typename TD, int V, int GPT>
-static auto fused_bwd_of() {
-    if constexpr (V == 1) return fused_bwd_kernel<T, TD, 1, 1, 32>;
-    else return fused_bwd_kernel<T, TD, V, GPT, 8>;
+template <typename T, typename TD, int V>
+static void (*kernel_of(bool held))(Args) {
+    return held ? held_bwd_kernel<T, TD, V, V == 1 ? 32 : 8> : reread_bwd_kernel<T, TD, V>;
 }
 
 template <typename T, typename TD>
 static minw_status backward(Args a, int V, cudaStream_t s) {
     Plan pl;
-    if (Args f = a; one_pass(f, pl, (int)sizeof(T), V, true)) {
+    if (Args f = a; plan(f, pl, (int)sizeof(T), V, true)) {
         const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
         if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
-        void (*kern)(Args) = pl.V == 1 ? fused_bwd_of<T, TD, 1, 1>()
-                           : pl.V == 4 ? (pl.GPT == 1 ? fused_bwd_of<T, TD, 4, 1>() : pl.GPT == 2 ? fused_bwd_of<T, TD, 4, 2>()
-                                                                                     : fused_bwd_of<T, TD, 4, 4>())
-                                       : nullptr;
+        void (*kern)(Args) = pl.V == 1 ? kernel_of<T, TD, 1>(pl.held) : kernel_of<T, TD, 4>(pl.held);
         if constexpr (sizeof(T) == 2 && sizeof(TD) == 2)
-            if (pl.V == 8)
-                kern = pl.GPT == 1   ? fused_bwd_of<T, TD, 8, 1>()
-                       : pl.GPT == 2 ? fused_bwd_of<T, TD, 8, 2>()
-                                     : fused_bwd_of<T, TD, 8, 4>();
-        if (launch_cluster(kern, blocks, s, f) != cudaSuccess) return MINW_ECUDA;
+            if (pl.V == 8) kern = kernel_of<T, TD, 8>(pl.held);
+        if (launch_cluster(kern, blocks, f.chunks, s, f) != cudaSuccess) return MINW_ECUDA;
     } else {
         lanes(a, V);
-        const int64_t blocks = (int64_t)a.B * a.chunks * a.slabs;
-        if (blocks >= (1ll << 31) || (int64_t)a.B * a.G >= (1ll << 31)) return MINW_EUNSUPPORTED;
         void (*sum)(Args) = V == 4 ? bwd_sum_kernel<T, TD, 4> : bwd_sum_kernel<T, TD, 1>;
         void (*apply)(Args) = V == 4 ? bwd_apply_kernel<T, TD, 4> : bwd_apply_kernel<T, TD, 1>;
         if constexpr (sizeof(T) == 2 && sizeof(TD) == 2)
@@ -368,6 +425,8 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
                 sum = bwd_sum_kernel<T, TD, 8>;
                 apply = bwd_apply_kernel<T, TD, 8>;
             }
+        int64_t blocks;
+        if (!in_chunks(a, false, blocks)) return MINW_EUNSUPPORTED;
         if (launch(sum, blocks, s, a) != cudaSuccess ||
             launch(bwd_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess || launch(apply, blocks, s, a) != cudaSuccess)
             return MINW_ECUDA;
@@ -403,16 +462,13 @@ minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx,
         if (dbeta && cudaMemsetAsync(dbeta, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
         return MINW_OK;
     }
-    const gn::Layout l = gn::layout(B, P, C, G, true);
+    const gn::Layout l = gn::layout(B, C, G, true);
     if (!workspace || !aligned16(workspace) || workspace_bytes < l.total) return MINW_EINVAL;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     gn::Args a{};
     a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.y = dx; a.ldy = lddx; a.gamma = gamma; a.beta = beta;
     a.mean_in = mean; a.rstd_in = rstd; a.dgamma = dgamma; a.dbeta = dbeta;
     a.B = B; a.P = (int)P; a.C = C; a.G = G; a.Cg = C / G; a.act = act;
-    a.chunks = gn::chunks_of(B, P);
-    a.ppc = (int)((P + a.chunks - 1) / a.chunks);
-    a.chunks = (int)((P + a.ppc - 1) / a.ppc);
     a.part = reinterpret_cast<float2 *>(ws + l.part);
     a.stat = reinterpret_cast<float2 *>(ws + l.stat);
     a.chan = reinterpret_cast<float2 *>(ws + l.chan);

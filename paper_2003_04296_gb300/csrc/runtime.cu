@@ -73,19 +73,6 @@ bool allow_shared(const void *kern, int bytes) {
     return true;
 }
 
-bool allow_large_clusters(const void *kern) {
-    static std::mutex mu;
-    static std::set<std::pair<int, const void *>> done;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return false;
-    std::lock_guard<std::mutex> lock(mu);
-    const std::pair<int, const void *> key(dev, kern);
-    if (done.count(key)) return true;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
-    done.insert(key);
-    return true;
-}
-
 void max_shared_carveout(const void *kern) {
     static std::mutex mu;
     static std::unordered_set<const void *> done;
