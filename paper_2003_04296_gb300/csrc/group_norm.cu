@@ -563,7 +563,7 @@ extern "C" {
 
 size_t minw_group_norm_workspace_bytes(int32_t B, int64_t P, int32_t C, int32_t G, int32_t backward) {
     if (B <= 0 || P <= 0 || C <= 0 || G <= 0 || C % G != 0 || P >= (1ll << 30)) return 0;
-    return gn::layout(B, C, G, backward != 0).total;
+    return gn::layout(B, P, C, G, backward != 0).total;
 }
 
 minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamma, const float *beta,
@@ -578,7 +578,7 @@ minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const fl
         return MINW_EINVAL;
     if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;
     if (B == 0) return MINW_OK;
-    const gn::Layout l = gn::layout(B, C, G, false);
+    const gn::Layout l = gn::layout(B, P, C, G, false);
     if (!workspace || !aligned16(workspace) || workspace_bytes < l.total) return MINW_EINVAL;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     gn::Args a{};

@@ -248,11 +248,12 @@ inline int chunks_of(int blocks, int B, int slabs, int64_t P) {
 struct Layout {
     size_t part, stat, chan, total;
 };
-inline Layout layout(int B, int C, int G, bool backward) {
+inline Layout layout(int B, int64_t P, int C, int G, bool backward) {
     Layout l;
     size_t off = 0;
     auto take = [&](size_t n) { const size_t r = off; off += al256(n * sizeof(float2)); return r; };
-    l.part = take((size_t)(B > STREAM_BLOCKS ? B : STREAM_BLOCKS) * C);      // B chunks_of(B) at most, for fewer images too
+    const int64_t chunks = B * ((P + 63) / 64), most = B > STREAM_BLOCKS ? B : STREAM_BLOCKS;       // of all images
+    l.part = take((size_t)(chunks < most ? chunks : most) * C);
     l.stat = take((size_t)B * G);
     l.chan = backward ? take((size_t)B * C) : off;
     l.total = off;

@@ -462,7 +462,7 @@ minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx,
         if (dbeta && cudaMemsetAsync(dbeta, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
         return MINW_OK;
     }
-    const gn::Layout l = gn::layout(B, C, G, true);
+    const gn::Layout l = gn::layout(B, P, C, G, true);
     if (!workspace || !aligned16(workspace) || workspace_bytes < l.total) return MINW_EINVAL;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     gn::Args a{};

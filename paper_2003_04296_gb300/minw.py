@@ -265,7 +265,8 @@ def _stream(stream):
     if stream is not None:
         return ctypes.c_void_p(stream.cuda_stream)
     # the current stream's handle without a Stream object around it (3 us of a call's host time)
-    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if torch.cuda.is_initialized() else \
+        ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 _VALUE_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
@@ -313,17 +314,20 @@ def _rows(t):
     return t.data_ptr(), size[-1] if ld is None else ld
 
 
+_FLOAT = torch.float32
+
+
 def _f32(t, n, what):
     """Address of a dense fp32 vector of n values (None passes)."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.numel() != n:
+    if t.dtype is not _FLOAT or t.numel() != n:
         raise ValueError(f"{what}: {n} float32 values expected")
     return _addr(t)
 
 
 def _scratch(workspace):
-    return (None, 0) if workspace is None else (_addr(workspace), workspace.numel() * workspace.element_size())
+    return (None, 0) if workspace is None else (_addr(workspace), workspace.nbytes)
 
 
 def quant(bits, thr=(0.0, 0.0, 0.0), scale=1.0):
@@ -881,10 +885,14 @@ def minw_group_norm_workspace_bytes(B, P, C, groups, backward=False):
 
 
 def _image_rows(x, groups):
-    if x.dim() < 2:
-        raise ValueError("[B, ..., C] expected")
     shape = x.shape
-    return shape[0], math.prod(shape[1:-1]), shape[-1], int(groups)
+    if len(shape) == 3:
+        B, P, C = shape
+    elif len(shape) >= 2:
+        B, P, C = shape[0], math.prod(shape[1:-1]), shape[-1]
+    else:
+        raise ValueError("[B, ..., C] expected")
+    return B, P, C, groups
 
 
 def minw_group_norm(x, gamma, beta, groups, eps, y, act=ACT_NONE, mean=None, rstd=None, workspace=None, stream=None):

@@ -63,6 +63,7 @@ CASES = [
     ([30_000_000, 3], 0, "b", "f"),                          # chunks of the largest size, several a block
     ([11] * 100, 1, "f", "f"), ([11 + 7 * (i % 50) for i in range(801)], 0, "f", "f"),   # three capacities, two launches
     ([5] * 1700, 0, "b", "b"),
+    ([3000] * 864 + [0] * 200, 0, "f", "f"), ([0] * 900 + [70_000] * 2, 1, "f", "b"), ([9] * 864 + [0, 0, 5, 0], 2, "b", "f"),
 ]
 
 
