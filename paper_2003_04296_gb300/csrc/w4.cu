@@ -105,7 +105,9 @@ struct Args {
     int wr, wk;                        // warps side by side along the rows, and along K
     int split, upc;                    // CTAs of a cluster (they split K), units of two blocks of each
     int xunits;                        // units whose x and scales are in shared memory at a time
-    int scale_pitch, scale_at, ring_at;   // values between rows of scales there; where scales and codes lie (bytes)
+    int xpitch, scale_pitch;           // values between columns of x, and between rows of scales, there
+    int scale_at, ring_at;             // where scales and codes lie (bytes)
+    Div by_row, by_eights;             // loads of 16 bytes of a column's x, of a row's scales
     Div by_blocks;                     // blocks of 128 values per group (groups of 128 and more)
 };
 
@@ -145,42 +147,41 @@ __device__ __forceinline__ void copy16(uint16_t *dst, const void *src, int bytes
     copy16((uint32_t)__cvta_generic_to_shared(dst), src, bytes);
 }
 
-// Blocks [b0, b0 + n) of the pass's vectors into shared memory, columns of n 128 + 32 values (the 64 bytes
-// over put the eight columns of a tile into different banks), zero past K.
-__device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int tokens, int b0, int n) {
-    const int pitch = n * 128 + 32, k0 = b0 * 128, valid = min(a.K - k0, n * 128), threads = blockDim.x;
+// The pass's vectors from value k0 on into shared memory, xunits units of them: columns of xpitch values (the 64
+// bytes over put the eight columns of a tile into different banks), zero past K.
+__device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int tokens, int k0) {
+    const int threads = blockDim.x, per_row = a.by_row.d, all = tokens * per_row;
     if (a.x_bf16) {
         const uint16_t *x = static_cast<const uint16_t *>(a.x) + (int64_t)t0 * a.ldx + k0;
         const bool wide = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && a.ldx % 8 == 0;
-        for (int t = 0; t < tokens; ++t, x += a.ldx) {
-            uint16_t *dst = xs + t * pitch;
-            for (int k = 8 * threadIdx.x; k < n * 128; k += 8 * threads) {
-                const int left = valid - k;
-                if (wide) {
-                    copy16(dst + k, left > 0 ? x + k : x, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
-                } else {
-                    uint16_t v[8];
+        for (int e = threadIdx.x; e < all; e += threads) {           // eights
+            const int t = a.by_row.div(e), k = 8 * (e - t * per_row), left = a.K - k0 - k;
+            const uint16_t *src = x + t * a.ldx + k;
+            uint16_t *dst = xs + t * a.xpitch + k;
+            if (wide) {
+                copy16(dst, left > 0 ? src : x, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
+            } else {
+                uint16_t v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = i < left ? x[k + i] : (uint16_t)0;
-                    *reinterpret_cast<uint4 *>(dst + k) =
-                        make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16, v[4] | (uint32_t)v[5] << 16,
-                                   v[6] | (uint32_t)v[7] << 16);
-                }
+                for (int i = 0; i < 8; ++i) v[i] = i < left ? src[i] : (uint16_t)0;
+                *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16,
+                                                             v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
             }
         }
     } else {
         constexpr int U = 4;                                         // loads in flight
         const float *x = static_cast<const float *>(a.x) + (int64_t)t0 * a.ldx + k0;
         const bool wide = (reinterpret_cast<uintptr_t>(x) & 15) == 0 && a.ldx % 4 == 0;
-        const int per = n * 32, all = tokens * per;                  // fours of a column, of all
-        for (int e0 = threadIdx.x; e0 < all; e0 += U * threads) {
+        for (int e0 = threadIdx.x; e0 < all; e0 += U * threads) {    // fours
             float4 v[U];
+            int at[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int e = e0 + u * threads, t = e / per, k = 4 * (e - t * per), left = valid - k;
+                const int e = e0 + u * threads, t = a.by_row.div(e), k = 4 * (e - t * per_row), left = a.K - k0 - k;
                 v[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                at[u] = 3 * t * a.xpitch + k;
                 if (e >= all) continue;
-                const float *src = x + (int64_t)t * a.ldx + k;
+                const float *src = x + t * a.ldx + k;
                 if (wide && left >= 4) {
                     v[u] = *reinterpret_cast<const float4 *>(src);
                 } else {
@@ -192,8 +193,7 @@ __device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int e = e0 + u * threads, t = e / per, k = 4 * (e - t * per);
-                if (e >= all) break;
+                if (e0 + u * threads >= all) break;
                 uint16_t p[4][3];
                 split3(v[u].x, p[0]);
                 split3(v[u].y, p[1]);
@@ -201,23 +201,22 @@ __device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int
                 split3(v[u].w, p[3]);
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
-                    *reinterpret_cast<uint2 *>(xs + (3 * t + i) * pitch + k) =
+                    *reinterpret_cast<uint2 *>(xs + at[u] + i * a.xpitch) =
                         make_uint2(p[0][i] | (uint32_t)p[1][i] << 16, p[2][i] | (uint32_t)p[3][i] << 16);
             }
         }
     }
 }
 
-// The scales of the CTA's rows for the same blocks, from the group of the first on; zero for groups past the last (they
-// hold padding only).
-__device__ __forceinline__ void stage_scales(const Args &a, uint16_t *ss, int row0, int b0, int n) {
-    const int g0 = b0 * 128 / a.group, g1 = min(a.groups, ((b0 + n) * 128 - 1) / a.group + 1), threads = blockDim.x;
-    const int eights = a.scale_pitch / 8, all = a.wr * 16 * eights;
+// The scales of the CTA's rows from group g0 on, scale_pitch of each; zero for groups past the last (they hold padding
+// only).
+__device__ __forceinline__ void stage_scales(const Args &a, uint16_t *ss, int row0, int g0) {
+    const int threads = blockDim.x, eights = a.by_eights.d, all = a.wr * 16 * eights;
     const bool wide = (reinterpret_cast<uintptr_t>(a.scales + g0) & 15) == 0 && a.groups % 8 == 0;
     for (int e = threadIdx.x; e < all; e += threads) {
-        const int r = e / eights, k = 8 * (e - r * eights), left = g1 - g0 - k;
+        const int r = a.by_eights.div(e), k = 8 * (e - r * eights), left = a.groups - g0 - k;
         const uint16_t *src = a.scales + (int64_t)min(row0 + r, a.O - 1) * a.groups + g0 + k;
-        uint16_t *dst = ss + r * a.scale_pitch + k;
+        uint16_t *dst = ss + 8 * e;
         if (wide) {
             copy16(dst, left > 0 ? src : a.scales, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
         } else {
@@ -231,7 +230,9 @@ __device__ __forceinline__ void stage_scales(const Args &a, uint16_t *ss, int ro
 }
 
 constexpr int WARPS = 8;              // of a CTA, at most
-constexpr int RING = 4;               // units that a warp has in flight: asynchronous copies to its own part of shared memory
+// Units of a warp's ring in shared memory, one of them in use, the others on their way (asynchronous copies): for one
+// tile of columns, and for several, which leave more time for each.
+__host__ __device__ constexpr int ring_of(int NT) { return NT == 1 ? 4 : 2; }
 constexpr int UNIT_BYTES = 2048;      // 16 rows x two blocks (128 bytes of a row side by side)
 
 // NT: tiles of 8 columns; FL: words of a lane's four that share a scale (1, 2, 4 for groups of 32, 64, 128 and more).
@@ -239,6 +240,7 @@ template <int NT, int FL>
 __global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
+    constexpr int RING = ring_of(NT);
     extern __shared__ __align__(16) uint8_t smem[];
     uint16_t *xs = reinterpret_cast<uint16_t *>(smem), *ss = reinterpret_cast<uint16_t *>(smem + a.scale_at);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -282,11 +284,11 @@ __global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
     for (int d = 0; d < RING - 1; ++d) fetch();
 
     for (int c0 = first; c0 < last; c0 += a.xunits) {
-        const int b0 = 2 * c0, nb = 2 * min(a.xunits, last - c0), xpitch = nb * 128 + 32;
+        const int b0 = 2 * c0, xpitch = a.xpitch;
         const int g0 = FL == 4 ? a.by_blocks.div(b0) : b0 * (4 / FL);
         __syncthreads();
-        stage_x(a, xs, t0, tokens, b0, nb);
-        stage_scales(a, ss, row0, b0, nb);
+        stage_x(a, xs, t0, tokens, b0 * 128);
+        stage_scales(a, ss, row0, g0);
         if (threadIdx.x < 32) *reinterpret_cast<uint4 *>(xs + cols * xpitch + 8 * threadIdx.x) = make_uint4(0, 0, 0, 0);
         asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
         __syncthreads();
@@ -501,18 +503,18 @@ minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T
     // wr warps along the rows (16 each) and wk along K make a CTA, `split` CTAs a cluster, which splits K too: the
     // choice with the least estimated clocks.  An SM holds two CTAs of up to 100 KB of shared memory: the rings, and x
     // and scales of as many units (whole rounds of the warps) as fit.  Measured on one to 48 columns (T = 1: 1024 x
-    // 1024 to 16384 x 16384): twelve warps of an SM take 18 / (1 + 0.07 columns) bytes of codes a clock, fewer
+    // 1024 to 16384 x 16384): fourteen warps of an SM take 18 / (1 + 0.07 columns) bytes of codes a clock, fewer
     // warps their share of that; a wave of CTAs has a fixed part, so have a cluster and each further filling of x.
     float best = 1e30f;
     // with the share of the SMs' places that clusters of this size can take (cudaOccupancyMaxActiveClusters)
-    static const struct { int n; float places; } splits[] = {{1, 1.0f}, {2, 1.0f}, {3, 0.957f}, {4, 0.973f}, {6, 0.907f}, {8, 0.947f}};
+    static const struct { int n; float places; } splits[] = {{1, 1.0f}, {2, 1.0f}, {3, 0.957f}, {4, 0.974f}, {6, 0.908f}, {8, 0.948f}};
     const float x_rate = a.tokens * 256 * (a.x_bf16 ? 0.03f : 0.14f), cap = 18.0f / (1.0f + 0.07f * cols);
     int tiles = 0;
     for (int wr = 1; wr <= w4::WARPS; ++wr) {
         const int wk = w4::WARPS / wr, warps = wr * wk, rows = (O + 16 * wr - 1) / (16 * wr);
-        const int room = 100 * 1024 - warps * w4::RING * w4::UNIT_BYTES - cols * 64 - 512 - wr * 16 * 32;
+        const int room = 100 * 1024 - warps * w4::ring_of(NT) * w4::UNIT_BYTES - cols * 64 - 512 - wr * 16 * 32;
         const int fit = room / (cols * 512 + wr * 32 * (group >= 256 ? 1 : 256 / group));
-        const float one = cap * (warps >= 12 ? 1.0f : warps / 12.0f), two = cap * (warps >= 6 ? 1.0f : warps / 6.0f);
+        const float one = cap * (warps / 14.0f), two = cap * (warps >= 7 ? 1.0f : warps / 7.0f);
         for (const auto &sp : splits) {
             const int split = sp.n, upc = (units + split - 1) / split, slots = (int)(2 * sms * sp.places);
             if (upc * (split - 1) >= units) break;                                // a CTA without a unit
@@ -534,9 +536,12 @@ minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T
             }
         }
     }
-    const int ring = a.wr * a.wk * w4::RING * w4::UNIT_BYTES;
+    const int ring = a.wr * a.wk * w4::ring_of(NT) * w4::UNIT_BYTES;
+    a.xpitch = a.xunits * 256 + 32;
+    a.by_row = Div((uint32_t)a.xunits * (a.x_bf16 ? 32 : 64));
     a.scale_pitch = ((group >= 256 ? a.xunits * 256 / group + 2 : a.xunits * (256 / group)) + 7) / 8 * 8;
-    a.scale_at = (cols * (a.xunits * 256 + 32) + 256) * 2;
+    a.by_eights = Div((uint32_t)a.scale_pitch / 8);
+    a.scale_at = (cols * a.xpitch + 256) * 2;
     a.ring_at = a.scale_at + a.wr * 16 * a.scale_pitch * 2;
     size_t smem = (size_t)a.ring_at + ring;
     const size_t red = (size_t)a.wr * a.wk * 16 * 8 * NT * sizeof(float);
