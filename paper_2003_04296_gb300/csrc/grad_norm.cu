@@ -435,18 +435,18 @@ static minw_status run(const Call &c) {
                 return launch_small(c.op == CLIP ? small_kernel<CLIP, CAP> : small_kernel<UPDATE, CAP>, l.shares, c.s, l,
                                     c.max_norm, c.lr, c.norm) == cudaSuccess
                            ? launch_status()
-                           : MINW_ECUDA;
+                           : launch_failed();
         const int blocks = blocks_of(l.shares, SQUARES_PER_SM);
         if (launch_pdl_stream(false, squares_kernel<CAP>, dim3((unsigned)blocks), dim3(THREADS), 0, c.s, l,
                               c.part + parts) != cudaSuccess)
-            return MINW_ECUDA;
+            return launch_failed();
         parts += blocks;
         ++launches;
     }
     if (c.op < 0 || parts == 0) {
         if (launch_pdl_stream(false, norm_kernel, dim3(1), dim3(THREADS), 0, c.s, (const double *)c.part, parts,
                               c.norm) != cudaSuccess)
-            return MINW_ECUDA;
+            return launch_failed();
         return launch_status();
     }
     float *norm = c.norm;
@@ -457,7 +457,7 @@ static minw_status run(const Call &c) {
         if (launch_pdl_stream(false, c.op == CLIP ? step_kernel<CLIP, CAP> : step_kernel<UPDATE, CAP>,
                               dim3((unsigned)blocks_of(l.shares, STEP_PER_SM)), dim3(THREADS), 0, c.s, l,
                               (const double *)c.part, parts, c.max_norm, c.lr, norm) != cudaSuccess)
-            return MINW_ECUDA;
+            return launch_failed();
         norm = nullptr;
     }
     return launch_status();

@@ -529,12 +529,12 @@ static minw_status forward(Args a, int V, cudaStream_t s) {
         if (pl.one) {
             const int64_t blocks = (int64_t)a.B * a.slabs * a.chunks;
             if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
-            return launch_cluster(k.one, blocks, a.chunks, s, a) == cudaSuccess ? launch_status() : MINW_ECUDA;
+            return launch_cluster(k.one, blocks, a.chunks, s, a) == cudaSuccess ? launch_status() : launch_failed();
         }
         int64_t blocks;
         if (!in_chunks(a, true, blocks)) return MINW_EUNSUPPORTED;
         if (launch_cluster(k.stats, blocks, STREAM_CLUSTER, s, a) != cudaSuccess || launch(k.apply, blocks, s, a) != cudaSuccess)
-            return MINW_ECUDA;
+            return launch_failed();
         return launch_status();
     }
     lanes(a, V);
@@ -549,7 +549,7 @@ static minw_status forward(Args a, int V, cudaStream_t s) {
     if (!in_chunks(a, false, blocks)) return MINW_EUNSUPPORTED;
     if (launch(stat, blocks, s, a) != cudaSuccess || launch(stat_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess ||
         launch(apply, blocks, s, a) != cudaSuccess)
-        return MINW_ECUDA;
+        return launch_failed();
     return launch_status();
 }
 

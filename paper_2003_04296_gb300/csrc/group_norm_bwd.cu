@@ -415,7 +415,7 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
         void (*kern)(Args) = pl.V == 1 ? kernel_of<T, TD, 1>(pl.held) : kernel_of<T, TD, 4>(pl.held);
         if constexpr (sizeof(T) == 2 && sizeof(TD) == 2)
             if (pl.V == 8) kern = kernel_of<T, TD, 8>(pl.held);
-        if (launch_cluster(kern, blocks, f.chunks, s, f) != cudaSuccess) return MINW_ECUDA;
+        if (launch_cluster(kern, blocks, f.chunks, s, f) != cudaSuccess) return launch_failed();
     } else {
         lanes(a, V);
         void (*sum)(Args) = V == 4 ? bwd_sum_kernel<T, TD, 4> : bwd_sum_kernel<T, TD, 1>;
@@ -429,9 +429,9 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
         if (!in_chunks(a, false, blocks)) return MINW_EUNSUPPORTED;
         if (launch(sum, blocks, s, a) != cudaSuccess ||
             launch(bwd_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess || launch(apply, blocks, s, a) != cudaSuccess)
-            return MINW_ECUDA;
+            return launch_failed();
     }
-    if ((a.dgamma || a.dbeta) && launch(affine_grad_kernel, (a.C + 31) / 32, s, a) != cudaSuccess) return MINW_ECUDA;
+    if ((a.dgamma || a.dbeta) && launch(affine_grad_kernel, (a.C + 31) / 32, s, a) != cudaSuccess) return launch_failed();
     return launch_status();
 }
 
@@ -458,8 +458,8 @@ minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx,
     if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;
     cudaStream_t s = (cudaStream_t)stream;
     if (B == 0) {
-        if (dgamma && cudaMemsetAsync(dgamma, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
-        if (dbeta && cudaMemsetAsync(dbeta, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return MINW_ECUDA;
+        if (dgamma && cudaMemsetAsync(dgamma, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return launch_failed();
+        if (dbeta && cudaMemsetAsync(dbeta, 0, sizeof(float) * (size_t)C, s) != cudaSuccess) return launch_failed();
         return MINW_OK;
     }
     const gn::Layout l = gn::layout(B, P, C, G, true);

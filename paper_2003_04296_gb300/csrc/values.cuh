@@ -180,3 +180,13 @@ __device__ __forceinline__ void with_act(int act, F f) {
 }
 
 }  // namespace minw
+
+namespace minw_host {
+
+// The status of a launch that the runtime refused, whose error would else be the next call's.
+inline minw_status launch_failed() {
+    cudaGetLastError();
+    return MINW_ECUDA;
+}
+
+}  // namespace minw_host

@@ -474,7 +474,7 @@ minw_status minw_pack_w4(const void *w, int32_t type, int32_t O, int32_t K, int3
     cudaStream_t s = (cudaStream_t)stream;
     const cudaError_t e = type == MINW_BF16 ? w4::pack<uint16_t>(w, O, K, Kp, group, q, channel_scale, codes, scales, s)
                                             : w4::pack<float>(w, O, K, Kp, group, q, channel_scale, codes, scales, s);
-    return e == cudaSuccess ? launch_status() : MINW_ECUDA;
+    return e == cudaSuccess ? launch_status() : launch_failed();
 }
 
 minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T, const uint8_t *codes,
@@ -552,7 +552,7 @@ minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T
                         : NT == 2 ? w4::launch_group<2>(a, group, grid, smem, s)
                         : NT == 3 ? w4::launch_group<3>(a, group, grid, smem, s)
                                   : w4::launch_group<4>(a, group, grid, smem, s);
-    return e == cudaSuccess ? launch_status() : MINW_ECUDA;
+    return e == cudaSuccess ? launch_status() : launch_failed();
 }
 
 }  // extern "C"
