@@ -182,6 +182,7 @@ struct Shared {
     GroupSum<GPT> sums[2];
     float2 cta[MAX_SLAB_GROUPS], all[MAX_SLAB_GROUPS];
 };
+static_assert(sizeof(Shared<4>) == 8 * (THREADS * 4 + MAX_SLAB_GROUPS) + 16 * MAX_SLAB_GROUPS, "plan() counts on it");
 
 // The block's mean and M2 of each of a thread's GPT groups from its own `values` values' mean and M2 of them: the block's
 // mean turns M2 into deviations from that (values (own - mean)^2 more).
@@ -299,6 +300,29 @@ __device__ __forceinline__ void coefficients(const Args &a, int c, const float *
     }
 }
 
+// Each group's sum of a thread's sums of channel pairs: of one group, or (W = 1) of two.
+template <int V, int GPT>
+__device__ __forceinline__ void fold_pairs(const Pair *p, float *f) {
+    constexpr int W = V / GPT;
+    if constexpr (W == 1) {
+#pragma unroll
+        for (int k = 0; k < (V + 1) / 2; ++k) {
+            const float2 h = halves(p[k]);
+            f[2 * k] = h.x;
+            if (V > 1) f[2 * k + 1] = h.y;
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            Pair t = p[g * W / 2];
+#pragma unroll
+            for (int k = 1; k < W / 2; ++k) t = add2(t, p[g * W / 2 + k]);
+            const float2 h = halves(t);
+            f[g] = h.x + h.y;
+        }
+    }
+}
+
 // In registers.  GPT: groups among a thread's V channels (W = V / GPT channels of each); NV: pixels of a thread at most.
 template <typename T, typename TY, int V, int GPT, int NV>
 __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
@@ -326,27 +350,8 @@ __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
 #pragma unroll
                 for (int k = 0; k < NP; ++k) s[k] = add2(s[k], v[i].get2(k));
             }
-        auto fold = [&](const Pair *p, float *f) {
-            if constexpr (W == 1) {
-#pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const float2 h = halves(p[k]);
-                    f[2 * k] = h.x;
-                    if (V > 1) f[2 * k + 1] = h.y;
-                }
-            } else {
-#pragma unroll
-                for (int g = 0; g < GPT; ++g) {
-                    Pair t = p[g * W / 2];
-#pragma unroll
-                    for (int k = 1; k < W / 2; ++k) t = add2(t, p[g * W / 2 + k]);
-                    const float2 h = halves(t);
-                    f[g] = h.x + h.y;
-                }
-            }
-        };
         float own[GPT], m2[GPT];
-        fold(s, own);
+        fold_pairs<V, GPT>(s, own);
         const float values = (float)(w.n * W), inv = w.n > 0 ? __fdividef(1.0f, values) : 0.0f;
 #pragma unroll
         for (int g = 0; g < GPT; ++g) own[g] *= inv;
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
                     q[k] = fma2(d, d, q[k]);
                 }
             }
-        fold(q, m2);
+        fold_pairs<V, GPT>(q, m2);
         merge<GPT>(a, w, sm, own, m2, values, mean, rstd);
     }
     if (w.n > 0) {
@@ -382,6 +387,82 @@ __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
                     o.set(z);
                     o.store(y + i * ystep);
                 }
+        });
+    }
+    if (a.chunks > 1) cluster_leave();
+}
+
+// In shared memory.  Each thread copies the vectors that it reads, so that only the sums need barriers.
+template <typename T, typename TY, int V, int GPT>
+__global__ void __launch_bounds__(THREADS, 3) shared_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int W = V / GPT, NP = V / 2, U = 4, BYTES = Vec<T, V>::BYTES;
+    extern __shared__ __align__(16) uint8_t data[];
+    __shared__ Shared<GPT> sm;
+    const Tile w = tile<V>(a);
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    uint8_t *own_data = data + threadIdx.x * BYTES;
+    {
+        const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+        const int64_t step = (int64_t)w.rows * a.ldx;
+#pragma unroll U
+        for (int i = 0; i < w.n; ++i, x += step) copy_async<BYTES>(own_data + i * (THREADS * BYTES), x);
+        asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+    }
+    auto value = [&](int i) {
+        Vec<T, V> v;
+        v.load(reinterpret_cast<const T *>(own_data + i * (THREADS * BYTES)));
+        return v;
+    };
+    float mean[GPT], rstd[GPT];
+    {
+        Pair s[NP], q[NP];
+#pragma unroll
+        for (int k = 0; k < NP; ++k) s[k] = q[k] = pair(0.0f, 0.0f);
+#pragma unroll U
+        for (int i = 0; i < w.n; ++i) {
+            const Vec<T, V> v = value(i);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) s[k] = add2(s[k], v.get2(k));
+        }
+        float own[GPT], m2[GPT];
+        fold_pairs<V, GPT>(s, own);
+        const float values = (float)(w.n * W), inv = w.n > 0 ? __fdividef(1.0f, values) : 0.0f;
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) own[g] *= inv;
+#pragma unroll U
+        for (int i = 0; i < w.n; ++i) {
+            const Vec<T, V> v = value(i);
+#pragma unroll
+            for (int k = 0; k < NP; ++k) {
+                const Pair d = add2(v.get2(k), pick_group<V, W>(own, k, -1.0f));
+                q[k] = fma2(d, d, q[k]);
+            }
+        }
+        fold_pairs<V, GPT>(q, m2);
+        merge<GPT>(a, w, sm, own, m2, values, mean, rstd);
+    }
+    if (w.n > 0) {
+        Pair nm[NP], sc[NP], sh[NP];
+        coefficients<V, GPT>(a, w.c, mean, rstd, nm, sc, sh);
+        const int64_t ystep = (int64_t)w.rows * a.ldy;
+        with_act(a.act, [&](auto act) {
+            TY *y = static_cast<TY *>(a.y) + p * a.ldy + w.c;
+#pragma unroll U
+            for (int i = 0; i < w.n; ++i, y += ystep) {
+                const Vec<T, V> v = value(i);
+                float z[V];
+#pragma unroll
+                for (int k = 0; k < NP; ++k) {
+                    const float2 h = halves(fma2(add2(v.get2(k), nm[k]), sc[k], sh[k]));
+                    z[2 * k] = act_value<act.value>(h.x);
+                    z[2 * k + 1] = act_value<act.value>(h.y);
+                }
+                Vec<TY, V> o;
+                o.set(z);
+                o.store(y);
+            }
         });
     }
     if (a.chunks > 1) cluster_leave();
@@ -508,32 +589,35 @@ struct Kernels {
     void (*one)(Args), (*stats)(Args), (*apply)(Args);
 };
 template <typename T, typename TY, int V, int GPT>
-static Kernels kernels_of(bool held) {
-    return {held ? held_kernel<T, TY, V, GPT, V == 1 ? 32 : 8> : reread_kernel<T, TY, V, GPT>, chunk_stats_kernel<T, V, GPT>,
-            chunk_apply_kernel<T, TY, V, GPT>};
+static Kernels kernels_of(Way way) {
+    Kernels k = {way == HELD ? held_kernel<T, TY, V, GPT, V == 1 ? 32 : 8> : reread_kernel<T, TY, V, GPT>,
+                 chunk_stats_kernel<T, V, GPT>, chunk_apply_kernel<T, TY, V, GPT>};
+    if constexpr (V > 1)
+        if (way == SHARED) k.one = shared_kernel<T, TY, V, GPT>;
+    return k;
 }
 
 template <typename T, typename TY>
 static minw_status forward(Args a, int V, cudaStream_t s) {
     Plan pl;
-    if (plan(a, pl, (int)sizeof(T), V, false)) {
-        Kernels k = pl.V == 1    ? kernels_of<T, TY, 1, 1>(pl.held)
-                    : pl.GPT == 1 ? kernels_of<T, TY, 4, 1>(pl.held)
-                    : pl.GPT == 2 ? kernels_of<T, TY, 4, 2>(pl.held)
-                                  : kernels_of<T, TY, 4, 4>(pl.held);
+    if (plan(a, pl, (int)sizeof(T), 0, V)) {
+        Kernels k = pl.V == 1    ? kernels_of<T, TY, 1, 1>(pl.way)
+                    : pl.GPT == 1 ? kernels_of<T, TY, 4, 1>(pl.way)
+                    : pl.GPT == 2 ? kernels_of<T, TY, 4, 2>(pl.way)
+                                  : kernels_of<T, TY, 4, 4>(pl.way);
         if constexpr (sizeof(T) == 2 && sizeof(TY) == 2)
             if (pl.V == 8)
-                k = pl.GPT == 1   ? kernels_of<T, TY, 8, 1>(pl.held)
-                    : pl.GPT == 2 ? kernels_of<T, TY, 8, 2>(pl.held)
-                                  : kernels_of<T, TY, 8, 4>(pl.held);
-        if (pl.one) {
+                k = pl.GPT == 1   ? kernels_of<T, TY, 8, 1>(pl.way)
+                    : pl.GPT == 2 ? kernels_of<T, TY, 8, 2>(pl.way)
+                                  : kernels_of<T, TY, 8, 4>(pl.way);
+        if (pl.way != CHUNKS) {
             const int64_t blocks = (int64_t)a.B * a.slabs * a.chunks;
             if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
-            return launch_cluster(k.one, blocks, a.chunks, s, a) == cudaSuccess ? launch_status() : launch_failed();
+            return launch_cluster(k.one, blocks, a.chunks, pl.smem, s, a) == cudaSuccess ? launch_status() : launch_failed();
         }
         int64_t blocks;
         if (!in_chunks(a, true, blocks)) return MINW_EUNSUPPORTED;
-        if (launch_cluster(k.stats, blocks, STREAM_CLUSTER, s, a) != cudaSuccess || launch(k.apply, blocks, s, a) != cudaSuccess)
+        if (launch_cluster(k.stats, blocks, STREAM_CLUSTER, 0, s, a) != cudaSuccess || launch(k.apply, blocks, s, a) != cudaSuccess)
             return launch_failed();
         return launch_status();
     }

@@ -189,12 +189,14 @@ __device__ __forceinline__ Place place(const Args &a, int64_t block) {
 
 // ---------------------------------------------------------------------------
 // One kernel: a block, or a cluster of blocks that split the pixels, takes an
-// image's slab of whole groups (L lanes of V channels).  Small slabs stay in
-// its registers; larger ones are read again, from L2, once their sums are known.
+// image's slab of whole groups (L lanes of V channels).  A slab stays in shared
+// memory where there are no more slabs than the SMs can hold at a time, small
+// ones in registers where there are; larger ones are read again, from L2, once
+// their sums are known.
 // ---------------------------------------------------------------------------
 
 constexpr int MAX_SLAB_GROUPS = 256;
-constexpr int HELD_CLUSTER = 2, HELD_CLUSTER_BWD = 4;        // blocks of a cluster that holds its slab in registers, at most
+constexpr int HELD_CLUSTER = 4;        // blocks of a cluster that holds its slab in registers, at most
 
 struct Tile {
     int b, slab, rank, p0, p1, lane, row, rows, c, n;      // n: pixels of this thread
@@ -288,11 +290,15 @@ inline void lanes(Args &a, int V) {
 // The plan for slabs of whole groups: at least 128 bytes of a row wide where one fits (64 where not: the
 // memory's lines are 128 bytes, or where the wide ones are too few to fill the SMs), the narrowest such, so that the
 // blocks are many.
+enum Way { SHARED, HELD, REREAD, CHUNKS };      // in shared memory, in registers, read twice; images in chunks
 struct Plan {
     int V, GPT;
-    bool one, held;               // one kernel, with x in registers; false: images in chunks
+    Way way;
+    int smem;                                   // of a block: its vectors
 };
-inline bool plan(Args &a, Plan &pl, int bytes, int V0, bool backward) {
+constexpr int SHARED_MOST = 100 * 1024;         // (two blocks per SM)
+inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
+    const bool backward = dy_bytes != 0;
     const int sms = num_sms() > 0 ? num_sms() : 152, places = (backward ? 2 : 4) * sms;      // resident blocks
     pl.V = V0 == 8 && a.Cg % 2 != 0 && !backward ? 4 : V0;
     pl.GPT = a.Cg % pl.V == 0 ? 1 : pl.V == 8 ? (a.Cg % 4 == 0 ? 2 : 4) : a.Cg % 2 == 0 ? 2 : pl.V;
@@ -320,14 +326,36 @@ inline bool plan(Args &a, Plan &pl, int bytes, int V0, bool backward) {
     const int64_t slabs = (int64_t)a.B * (a.G / k);
     const int cap = rows * (pl.V == 1 ? 32 : 8);
     cluster = (a.P + cap - 1) / cap;
-    pl.held = cluster <= (backward ? HELD_CLUSTER_BWD : HELD_CLUSTER);
-    if (!pl.held) {
+    pl.way = cluster <= HELD_CLUSTER ? HELD : REREAD;
+    pl.smem = 0;
+    if (pl.V > 1) {
+        auto share = [&](int n) { return (int64_t)((a.P + n - 1) / n + rows - 1) / rows * THREADS * pl.V * (bytes + dy_bytes); };
+        // the kernels' own shared memory: sums and statistics, or the channels' sums of the rows
+        const int static_bytes = backward ? 8 * THREADS * pl.V + 8 * MAX_SLAB_GROUPS
+                                          : 8 * (THREADS * pl.GPT + MAX_SLAB_GROUPS) + 16 * MAX_SLAB_GROUPS;
+        // clusters of more than two blocks leave up to a tenth of the places empty
+        auto resident = [&](int n) {
+            const int64_t each = 227 * 1024 / (share(n) + static_bytes + 1024), most = backward ? 2 : 3;
+            return share(n) <= SHARED_MOST && slabs * n <= (each < most ? each : most) * sms * (n > 2 ? 9 : 10) / 10;
+        };
+        int n = 1;
+        while (n <= 8 && !resident(n)) ++n;
+        if (n <= 8) {
+            // two blocks per SM where a thread keeps four pixels
+            while (n <= 4 && slabs * n * 2 <= 2 * sms && a.P >= 8 * n * rows && resident(2 * n)) n *= 2;
+            cluster = n;
+            pl.way = SHARED;
+            pl.smem = (int)share(n);
+        }
+    }
+    if (pl.way == REREAD) {
         // as many blocks as fit at a time; in the backward twice as many where a thread still has 16 pixels
         for (cluster = 1; cluster < 8 && slabs * cluster * 2 <= places; cluster *= 2) {}
         if (backward && cluster < 8 && slabs * cluster <= places && a.P >= 32 * cluster * rows) cluster *= 2;
+        if (slabs * cluster < sms) pl.way = CHUNKS;                     // fewer blocks than SMs
     }
-    pl.one = pl.held || slabs * cluster >= sms;                         // fewer blocks than SMs: in chunks
-    if (backward && (!pl.one || (cluster > 1 && rows < 2))) return false;              // a cluster's totals go behind the block's sums
+    // a cluster's totals go behind the block's sums
+    if (backward && (pl.way == CHUNKS || (cluster > 1 && rows < 2))) return false;
     a.per = a.Cg / (pl.V / pl.GPT);
     a.butterfly = L <= 32 && (L & (L - 1)) == 0 && (a.per == 1 || (pl.GPT == 1 && (a.per & (a.per - 1)) == 0));
     a.rows = rows;
@@ -359,10 +387,12 @@ inline bool in_chunks(Args &a, bool clusters, int64_t &blocks) {
     return blocks < (1ll << 31) && (int64_t)a.B * a.G < (1ll << 31);
 }
 
-inline cudaError_t launch_cluster(void (*kern)(Args), int64_t blocks, int cluster, cudaStream_t s, const Args &a) {
+inline cudaError_t launch_cluster(void (*kern)(Args), int64_t blocks, int cluster, int smem, cudaStream_t s, const Args &a) {
+    if (smem > 32 * 1024 && !allow_shared(reinterpret_cast<const void *>(kern), SHARED_MOST)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;

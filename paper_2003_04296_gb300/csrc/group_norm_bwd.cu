@@ -227,6 +227,7 @@ struct Shared {
     float2 red[THREADS * V];               // rows x channels, then segments x channels
     float2 group[MAX_SLAB_GROUPS];
 };
+static_assert(sizeof(Shared<8>) == 8 * THREADS * 8 + 8 * MAX_SLAB_GROUPS, "plan() counts on it");
 
 // Minus s1 and s2 of a thread's channels from its sums: the block's rows, the cluster's blocks, the groups' channels, all
 // in a fixed order; and the image's channel sums for dgamma and dbeta.  Afterwards a cluster has arrived at its end.
@@ -350,6 +351,65 @@ __global__ void __launch_bounds__(THREADS, 2) held_bwd_kernel(Args a) {
     if (a.chunks > 1) cluster_leave();
 }
 
+// In shared memory.  Each thread copies the vectors that it reads, so that only the sums need barriers.
+template <typename T, typename TD, int V>
+__global__ void __launch_bounds__(THREADS, 2) shared_bwd_kernel(Args a) {
+    pdl_trigger();
+    pdl_wait();
+    constexpr int NP = V / 2, U = 2, BYTES = Vec<T, V>::BYTES + Vec<TD, V>::BYTES, XB = Vec<T, V>::BYTES;
+    extern __shared__ __align__(16) uint8_t data[];
+    __shared__ Shared<V> sm;
+    const Tile w = tile<V>(a);
+    const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
+    // a pixel's vectors of all threads: x, then dy
+    uint8_t *own_x = data + threadIdx.x * XB, *own_d = data + THREADS * XB + threadIdx.x * (BYTES - XB);
+    {
+        const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+        const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
+        const int64_t xstep = (int64_t)w.rows * a.ldx, dstep = (int64_t)w.rows * a.lddy;
+#pragma unroll 4
+        for (int i = 0; i < w.n; ++i, x += xstep, dy += dstep) {
+            copy_async<XB>(own_x + i * (THREADS * BYTES), x);
+            copy_async<BYTES - XB>(own_d + i * (THREADS * BYTES), dy);
+        }
+    }
+    Coef<V> co;
+    co.load(a, w.b, w.c);
+    asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
+    auto pixel = [&](int i, Vec<T, V> &v, Vec<TD, V> &d) {
+        v.load(reinterpret_cast<const T *>(own_x + i * (THREADS * BYTES)));
+        d.load(reinterpret_cast<const TD *>(own_d + i * (THREADS * BYTES)));
+    };
+    Pair ns1[NP], ns2[NP];
+    {
+        Pair db[NP], dg[NP];
+#pragma unroll
+        for (int k = 0; k < NP; ++k) db[k] = dg[k] = pair(0.0f, 0.0f);
+        with_act(a.act, [&](auto act) {
+#pragma unroll U
+            for (int i = 0; i < w.n; ++i) {
+                Vec<T, V> v;
+                Vec<TD, V> d;
+                pixel(i, v, d);
+                add_pixel<act.value, V>(v, d, co, db, dg);
+            }
+        });
+        totals<V>(a, w, sm, db, dg, ns1, ns2);
+    }
+    const int64_t ostep = (int64_t)w.rows * a.ldy;
+    with_act(a.act, [&](auto act) {
+        T *dx = static_cast<T *>(a.y) + p * a.ldy + w.c;
+#pragma unroll U
+        for (int i = 0; i < w.n; ++i, dx += ostep) {
+            Vec<T, V> v;
+            Vec<TD, V> d;
+            pixel(i, v, d);
+            pixel_gradient<act.value, V>(v, d, co, ns1, ns2).store(dx);
+        }
+    });
+    if (a.chunks > 1) cluster_leave();
+}
+
 // In two readings.
 template <typename T, typename TD, int V>
 __global__ void __launch_bounds__(THREADS, 2) reread_bwd_kernel(Args a) {
@@ -402,20 +462,22 @@ __global__ void __launch_bounds__(THREADS) affine_grad_kernel(Args a) {
 }
 
 template <typename T, typename TD, int V>
-static void (*kernel_of(bool held))(Args) {
-    return held ? held_bwd_kernel<T, TD, V, V == 1 ? 32 : 8> : reread_bwd_kernel<T, TD, V>;
+static void (*kernel_of(Way way))(Args) {
+    if constexpr (V > 1)
+        if (way == SHARED) return shared_bwd_kernel<T, TD, V>;
+    return way == HELD ? held_bwd_kernel<T, TD, V, V == 1 ? 32 : 8> : reread_bwd_kernel<T, TD, V>;
 }
 
 template <typename T, typename TD>
 static minw_status backward(Args a, int V, cudaStream_t s) {
     Plan pl;
-    if (Args f = a; plan(f, pl, (int)sizeof(T), V, true)) {
+    if (Args f = a; plan(f, pl, (int)sizeof(T), (int)sizeof(TD), V)) {
         const int64_t blocks = (int64_t)f.B * f.slabs * f.chunks;
         if (blocks >= (1ll << 31)) return MINW_EUNSUPPORTED;
-        void (*kern)(Args) = pl.V == 1 ? kernel_of<T, TD, 1>(pl.held) : kernel_of<T, TD, 4>(pl.held);
+        void (*kern)(Args) = pl.V == 1 ? kernel_of<T, TD, 1>(pl.way) : kernel_of<T, TD, 4>(pl.way);
         if constexpr (sizeof(T) == 2 && sizeof(TD) == 2)
-            if (pl.V == 8) kern = kernel_of<T, TD, 8>(pl.held);
-        if (launch_cluster(kern, blocks, f.chunks, s, f) != cudaSuccess) return launch_failed();
+            if (pl.V == 8) kern = kernel_of<T, TD, 8>(pl.way);
+        if (launch_cluster(kern, blocks, f.chunks, pl.smem, s, f) != cudaSuccess) return launch_failed();
     } else {
         lanes(a, V);
         void (*sum)(Args) = V == 4 ? bwd_sum_kernel<T, TD, 4> : bwd_sum_kernel<T, TD, 1>;

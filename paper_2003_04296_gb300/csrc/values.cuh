@@ -101,6 +101,14 @@ struct Vec {
     }
 };
 
+// BYTES (8 or 16) from global to shared memory, asynchronously.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void *dst, const void *src) {
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(d), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(d), "l"(src) : "memory");
+}
+
 // The larger and the smaller of two values; a NaN among them stays one (fmaxf and fminf drop it).
 __device__ __forceinline__ float max_nan(float a, float b) {
     float r;
