@@ -667,6 +667,7 @@ minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const fl
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     gn::Args a{};
     a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy; a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd;
+    a.wide_affine = gamma && beta && aligned16(gamma) && aligned16(beta);
     a.B = B; a.P = (int)P; a.C = C; a.G = G; a.Cg = C / G; a.act = act; a.eps = eps;
     a.part = reinterpret_cast<float2 *>(ws + l.part);
     a.stat = reinterpret_cast<float2 *>(ws + l.stat);

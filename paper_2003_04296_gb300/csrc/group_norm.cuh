@@ -33,6 +33,7 @@ struct Args {
     void *y;                       // y, or dx
     int64_t ldx, lddy, ldy;
     const float *gamma, *beta;     // nullable
+    int wide_affine;               // both given, on 16-byte boundaries
     const float *mean_in, *rstd_in;
     float *mean, *rstd;            // forward: saved statistics (nullable)
     float2 *part;                  // per image, cluster of chunks and group, or chunk and channel: (mean, M2); the backward's
@@ -61,6 +62,15 @@ __device__ __forceinline__ float warp_sum(float v) {
 // gamma and beta of channels c .. c + V - 1.
 template <int V>
 __device__ __forceinline__ void load_affine(const Args &a, int c, float *ga, float *be) {
+    if (V >= 4 && a.wide_affine) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            const float4 g = *reinterpret_cast<const float4 *>(a.gamma + c + i), b = *reinterpret_cast<const float4 *>(a.beta + c + i);
+            ga[i] = g.x; ga[i + 1] = g.y; ga[i + 2] = g.z; ga[i + 3] = g.w;
+            be[i] = b.x; be[i + 1] = b.y; be[i + 2] = b.z; be[i + 3] = b.w;
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         ga[i] = a.gamma ? a.gamma[c + i] : 1.0f;
@@ -331,7 +341,7 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
     if (pl.V > 1) {
         auto share = [&](int n) { return (int64_t)((a.P + n - 1) / n + rows - 1) / rows * THREADS * pl.V * (bytes + dy_bytes); };
         // the kernels' own shared memory: sums and statistics, or the channels' sums of the rows
-        const int static_bytes = backward ? 8 * THREADS * pl.V + 8 * MAX_SLAB_GROUPS
+        const int static_bytes = backward ? 8 * THREADS * pl.V + 12 * MAX_SLAB_GROUPS
                                           : 8 * (THREADS * pl.GPT + MAX_SLAB_GROUPS) + 16 * MAX_SLAB_GROUPS;
         // clusters of more than two blocks leave up to a tenth of the places empty
         auto resident = [&](int n) {

@@ -11,52 +11,52 @@ namespace gn {
 // second pass over x and dy.
 // ---------------------------------------------------------------------------
 
-// What a thread's V channels need, in pairs: minus the means, rstd, gamma, beta.
+// What a thread's V channels need, in pairs: minus the means, scale = rstd gamma, beta.  With t = x - mean, z = scale t +
+// beta; the sums are those of dz and dz t (times rstd at their end, dgamma), and dx = scale dz - rstd s1 - t rstd^2 s2.
 template <int V>
 struct Coef {
     static constexpr int NP = (V + 1) / 2;
-    Pair nm[NP], r[NP], ga[NP], be[NP];
+    Pair nm[NP], sc[NP], be[NP];
 
     __device__ __forceinline__ void load(const Args &a, int b, int c) {
-        float g[V], h[V], mean[V], rstd[V];
+        float g[V], h[V], mean[V];
         load_affine<V>(a, c, g, h);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const int64_t at = (int64_t)b * a.G + (c + i) / a.Cg;
             mean[i] = -a.mean_in[at];
-            rstd[i] = a.rstd_in[at];
+            g[i] *= a.rstd_in[at];
         }
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
             nm[k] = pick<V>(mean, k);
-            r[k] = pick<V>(rstd, k);
-            ga[k] = pick<V>(g, k);
+            sc[k] = pick<V>(g, k);
             be[k] = pick<V>(h, k);
         }
     }
 };
 
-// Sums of dz and dz xh of one pixel's channels.
+// Sums of dz and dz t of one pixel's channels.
 template <int ACT, int V, typename X, typename D>
 __device__ __forceinline__ void add_pixel(const X &x, const D &dy, const Coef<V> &co, Pair *db, Pair *dg) {
 #pragma unroll
     for (int k = 0; k < Coef<V>::NP; ++k) {
-        const Pair xh = mul2(add2(x.get2(k), co.nm[k]), co.r[k]);
-        const Pair dz = act_grad2<ACT>(fma2(xh, co.ga[k], co.be[k]), dy.get2(k));
+        const Pair t = add2(x.get2(k), co.nm[k]);
+        const Pair dz = act_grad2<ACT>(fma2(t, co.sc[k], co.be[k]), dy.get2(k));
         db[k] = add2(db[k], dz);
-        dg[k] = fma2(dz, xh, dg[k]);
+        dg[k] = fma2(dz, t, dg[k]);
     }
 }
 
-// dx of one pixel: minus s1 and s2 of its channels' groups in pairs.
+// dx of one pixel: n1 = - rstd s1 and n2 = - rstd^2 s2 of its channels' groups in pairs.
 template <int ACT, int V, typename X, typename D>
-__device__ __forceinline__ X pixel_gradient(const X &x, const D &dy, const Coef<V> &co, const Pair *ns1, const Pair *ns2) {
+__device__ __forceinline__ X pixel_gradient(const X &x, const D &dy, const Coef<V> &co, const Pair *n1, const Pair *n2) {
     float o[2 * Coef<V>::NP];
 #pragma unroll
     for (int k = 0; k < Coef<V>::NP; ++k) {
-        const Pair xh = mul2(add2(x.get2(k), co.nm[k]), co.r[k]);
-        const Pair dz = act_grad2<ACT>(fma2(xh, co.ga[k], co.be[k]), dy.get2(k));
-        const float2 h = halves(mul2(co.r[k], fma2(xh, ns2[k], fma2(co.ga[k], dz, ns1[k]))));
+        const Pair t = add2(x.get2(k), co.nm[k]);
+        const Pair dz = act_grad2<ACT>(fma2(t, co.sc[k], co.be[k]), dy.get2(k));
+        const float2 h = halves(fma2(co.sc[k], dz, fma2(t, n2[k], n1[k])));
         o[2 * k] = h.x;
         o[2 * k + 1] = h.y;
     }
@@ -90,8 +90,8 @@ __device__ __forceinline__ void channel_sums(int act, const T *x, int64_t xstep,
 
 template <typename T, typename TD, int V, int U>
 __device__ __forceinline__ void gradient_pixels(int act, const T *x, int64_t xstep, const TD *dy, int64_t dstep, T *dx,
-                                                int64_t ostep, int n, const Coef<V> &co, const Pair *ns1,
-                                                const Pair *ns2) {
+                                                int64_t ostep, int n, const Coef<V> &co, const Pair *n1,
+                                                const Pair *n2) {
     with_act(act, [&](auto act_) {
         const T *px = x;
         const TD *pd = dy;
@@ -107,7 +107,7 @@ __device__ __forceinline__ void gradient_pixels(int act, const T *x, int64_t xst
                 pd += dstep;
             },
             [&](int u, int) {
-                pixel_gradient<act_.value, V>(v[u], d[u], co, ns1, ns2).store(po);
+                pixel_gradient<act_.value, V>(v[u], d[u], co, n1, n2).store(po);
                 po += ostep;
             });
     });
@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(THREADS, 2) bwd_sum_kernel(Args a) {
             s0 += red[r * W + e].x;
             s1 += red[r * W + e].y;
         }
-        a.part[((int64_t)w.b * a.chunks + w.chunk) * a.C + c] = make_float2(s0, s1);
+        a.part[((int64_t)w.b * a.chunks + w.chunk) * a.C + c] =
+            make_float2(s0, s1 * a.rstd_in[(int64_t)w.b * a.G + c / a.Cg]);
     }
 }
 
@@ -197,25 +198,27 @@ __global__ void __launch_bounds__(THREADS, 2) bwd_apply_kernel(Args a) {
     if (w.n == 0) return;
     Coef<V> co;
     co.load(a, w.b, w.c);
-    Pair ns1[Coef<V>::NP], ns2[Coef<V>::NP];
+    Pair n1[Coef<V>::NP], n2[Coef<V>::NP];
     {
         float s1[V], s2[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const float2 t = a.stat[(int64_t)w.b * a.G + (w.c + i) / a.Cg];
-            s1[i] = -t.x;
-            s2[i] = -t.y;
+            const int64_t at = (int64_t)w.b * a.G + (w.c + i) / a.Cg;
+            const float2 t = a.stat[at];
+            const float r = a.rstd_in[at];
+            s1[i] = -t.x * r;
+            s2[i] = -t.y * r * r;
         }
 #pragma unroll
         for (int k = 0; k < Coef<V>::NP; ++k) {
-            ns1[k] = pick<V>(s1, k);
-            ns2[k] = pick<V>(s2, k);
+            n1[k] = pick<V>(s1, k);
+            n2[k] = pick<V>(s2, k);
         }
     }
     const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
     gradient_pixels<T, TD, V, V == 1 ? 8 : 4>(a.act, static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
                                               static_cast<const TD *>(a.dy) + p * a.lddy + w.c, w.rows * a.lddy,
-                                              static_cast<T *>(a.y) + p * a.ldy + w.c, w.rows * a.ldy, w.n, co, ns1, ns2);
+                                              static_cast<T *>(a.y) + p * a.ldy + w.c, w.rows * a.ldy, w.n, co, n1, n2);
 }
 
 // ---------------------------------------------------------------------------
@@ -226,14 +229,19 @@ template <int V>
 struct Shared {
     float2 red[THREADS * V];               // rows x channels, then segments x channels
     float2 group[MAX_SLAB_GROUPS];
-};
-static_assert(sizeof(Shared<8>) == 8 * THREADS * 8 + 8 * MAX_SLAB_GROUPS, "plan() counts on it");
+    float rstd[MAX_SLAB_GROUPS];           // of the slab's groups
 
-// Minus s1 and s2 of a thread's channels from its sums: the block's rows, the cluster's blocks, the groups' channels, all
+    __device__ __forceinline__ void load_rstd(const Args &a, const Tile &w) {
+        for (int g = threadIdx.x; g < a.groups; g += THREADS) rstd[g] = a.rstd_in[(int64_t)w.b * a.G + w.slab * a.groups + g];
+    }
+};
+static_assert(sizeof(Shared<8>) == 8 * THREADS * 8 + 12 * MAX_SLAB_GROUPS, "plan() counts on it");
+
+// n1 and n2 of a thread's channels from its sums: the block's rows, the cluster's blocks, the groups' channels, all
 // in a fixed order; and the image's channel sums for dgamma and dbeta.  Afterwards a cluster has arrived at its end.
 template <int V>
-__device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &sm, const Pair *db, const Pair *dg, Pair *ns1,
-                                       Pair *ns2) {
+__device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &sm, const Pair *db, const Pair *dg, Pair *n1,
+                                       Pair *n2) {
     const int CW = a.L * V;                                // channels of the slab
     float2 *red = sm.red;
     if (w.row < w.rows) put_sums<V>(red + w.row * CW + w.lane * V, db, dg);
@@ -256,7 +264,7 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
             t.x += red[s * CW + c].x;
             t.y += red[s * CW + c].y;
         }
-        red[c] = t;
+        red[c] = make_float2(t.x, t.y * sm.rstd[a.by_Cg.div(c)]);
     }
     float2 *tot = red;
     if (a.chunks > 1) {
@@ -291,7 +299,10 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
         }
         s1 = warp_sum(s1);
         s2 = warp_sum(s2);
-        if ((threadIdx.x & 31) == 0) sm.group[g] = make_float2(-s1 * a.inv_total, -s2 * a.inv_total);
+        if ((threadIdx.x & 31) == 0) {
+            const float r = -sm.rstd[g] * a.inv_total;
+            sm.group[g] = make_float2(s1 * r, s2 * r * sm.rstd[g]);
+        }
     }
     __syncthreads();
     float f1[V], f2[V];
@@ -303,8 +314,8 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
     }
 #pragma unroll
     for (int k = 0; k < (V + 1) / 2; ++k) {
-        ns1[k] = pick<V>(f1, k);
-        ns2[k] = pick<V>(f2, k);
+        n1[k] = pick<V>(f1, k);
+        n2[k] = pick<V>(f2, k);
     }
 }
 
@@ -329,7 +340,8 @@ __global__ void __launch_bounds__(THREADS, 2) held_bwd_kernel(Args a) {
         }
     Coef<V> co;
     co.load(a, w.b, w.c);
-    Pair ns1[NP], ns2[NP];
+    sm.load_rstd(a, w);
+    Pair n1[NP], n2[NP];
     {
         Pair db[NP], dg[NP];
 #pragma unroll
@@ -339,14 +351,14 @@ __global__ void __launch_bounds__(THREADS, 2) held_bwd_kernel(Args a) {
             for (int i = 0; i < NV; ++i)
                 if (i < w.n) add_pixel<act.value, V>(v[i], d[i], co, db, dg);
         });
-        totals<V>(a, w, sm, db, dg, ns1, ns2);
+        totals<V>(a, w, sm, db, dg, n1, n2);
     }
     T *dx = static_cast<T *>(a.y) + p * a.ldy + w.c;
     const int64_t ostep = (int64_t)w.rows * a.ldy;
     with_act(a.act, [&](auto act) {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (i < w.n) pixel_gradient<act.value, V>(v[i], d[i], co, ns1, ns2).store(dx + i * ostep);
+            if (i < w.n) pixel_gradient<act.value, V>(v[i], d[i], co, n1, n2).store(dx + i * ostep);
     });
     if (a.chunks > 1) cluster_leave();
 }
@@ -375,12 +387,13 @@ __global__ void __launch_bounds__(THREADS, 2) shared_bwd_kernel(Args a) {
     }
     Coef<V> co;
     co.load(a, w.b, w.c);
+    sm.load_rstd(a, w);
     asm volatile("cp.async.commit_group;\ncp.async.wait_group 0;" ::: "memory");
     auto pixel = [&](int i, Vec<T, V> &v, Vec<TD, V> &d) {
         v.load(reinterpret_cast<const T *>(own_x + i * (THREADS * BYTES)));
         d.load(reinterpret_cast<const TD *>(own_d + i * (THREADS * BYTES)));
     };
-    Pair ns1[NP], ns2[NP];
+    Pair n1[NP], n2[NP];
     {
         Pair db[NP], dg[NP];
 #pragma unroll
@@ -394,7 +407,7 @@ __global__ void __launch_bounds__(THREADS, 2) shared_bwd_kernel(Args a) {
                 add_pixel<act.value, V>(v, d, co, db, dg);
             }
         });
-        totals<V>(a, w, sm, db, dg, ns1, ns2);
+        totals<V>(a, w, sm, db, dg, n1, n2);
     }
     const int64_t ostep = (int64_t)w.rows * a.ldy;
     with_act(a.act, [&](auto act) {
@@ -404,7 +417,7 @@ __global__ void __launch_bounds__(THREADS, 2) shared_bwd_kernel(Args a) {
             Vec<T, V> v;
             Vec<TD, V> d;
             pixel(i, v, d);
-            pixel_gradient<act.value, V>(v, d, co, ns1, ns2).store(dx);
+            pixel_gradient<act.value, V>(v, d, co, n1, n2).store(dx);
         }
     });
     if (a.chunks > 1) cluster_leave();
@@ -423,14 +436,15 @@ __global__ void __launch_bounds__(THREADS, 2) reread_bwd_kernel(Args a) {
     const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
     Coef<V> co;
     co.load(a, w.b, w.c);
-    Pair ns1[NP], ns2[NP];
+    sm.load_rstd(a, w);
+    Pair n1[NP], n2[NP];
     {
         Pair db[NP], dg[NP];
         channel_sums<T, TD, V, U>(a.act, x, xstep, dy, dstep, w.n, co, db, dg);
-        totals<V>(a, w, sm, db, dg, ns1, ns2);
+        totals<V>(a, w, sm, db, dg, n1, n2);
     }
     gradient_pixels<T, TD, V, U>(a.act, x, xstep, dy, dstep, static_cast<T *>(a.y) + p * a.ldy + w.c,
-                                 (int64_t)w.rows * a.ldy, w.n, co, ns1, ns2);
+                                 (int64_t)w.rows * a.ldy, w.n, co, n1, n2);
     if (a.chunks > 1) cluster_leave();
 }
 
@@ -530,6 +544,7 @@ minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx,
     gn::Args a{};
     a.x = x; a.ldx = ldx; a.dy = dy; a.lddy = lddy; a.y = dx; a.ldy = lddx; a.gamma = gamma; a.beta = beta;
     a.mean_in = mean; a.rstd_in = rstd; a.dgamma = dgamma; a.dbeta = dbeta;
+    a.wide_affine = gamma && beta && aligned16(gamma) && aligned16(beta);
     a.B = B; a.P = (int)P; a.C = C; a.G = G; a.Cg = C / G; a.act = act;
     a.part = reinterpret_cast<float2 *>(ws + l.part);
     a.stat = reinterpret_cast<float2 *>(ws + l.stat);
