@@ -129,23 +129,24 @@ __device__ __forceinline__ void channel_stats(const T *x, int64_t step, int n, P
     }
 }
 
-// f(u, i) for a thread's n pixels, U at a time, after load(u, i) for all of those.
-template <int U, typename L, typename F>
-__device__ __forceinline__ void batches(int n, L load, F f) {
+// f(u) for a thread's n pixels, U at a time, after load(u) for all of those; once() when the first are on their way.
+template <int U, typename L, typename O, typename F>
+__device__ __forceinline__ void batches(int n, L load, O once, F f) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (u < n) load(u);
+    once();
     int i = 0;
     for (; i + U <= n; i += U) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load(u, i + u);
+        for (int u = 0; u < U; ++u) f(u);
 #pragma unroll
-        for (int u = 0; u < U; ++u) f(u, i + u);
+        for (int u = 0; u < U; ++u)
+            if (i + U + u < n) load(u);
     }
-    if (i == n) return;
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if (i + u < n) load(u, i + u);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (i + u < n) f(u, i + u);
+        if (i + u < n) f(u);
 }
 
 // y = act((x - mean) a + b) on a thread's n pixels: minus the means, a = rstd gamma and b = beta in pairs.
@@ -156,11 +157,12 @@ __device__ __forceinline__ void apply_pixels(const T *x, int64_t xstep, TY *y, i
     Vec<T, V> v[U];
     batches<U>(
         n,
-        [&](int u, int) {
+        [&](int u) {
             v[u].load(x);
             x += xstep;
         },
-        [&](int u, int) {
+        [] {},
+        [&](int u) {
             float z[2 * NP];
 #pragma unroll
             for (int k = 0; k < NP; ++k) {
@@ -295,6 +297,7 @@ inline void lanes(Args &a, int V) {
     const int all = a.C / V;
     a.slabs = (all + THREADS - 1) / THREADS;
     a.L = (all + a.slabs - 1) / a.slabs;
+    a.by_Cg = Div(a.Cg);
 }
 
 // The plan for slabs of whole groups: at least 128 bytes of a row wide where one fits (64 where not: the
@@ -341,7 +344,7 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
     if (pl.V > 1) {
         auto share = [&](int n) { return (int64_t)((a.P + n - 1) / n + rows - 1) / rows * THREADS * pl.V * (bytes + dy_bytes); };
         // the kernels' own shared memory: sums and statistics, or the channels' sums of the rows
-        const int static_bytes = backward ? 8 * THREADS * pl.V + 12 * MAX_SLAB_GROUPS
+        const int static_bytes = backward ? 8 * THREADS * (pl.V + 1) + 12 * MAX_SLAB_GROUPS
                                           : 8 * (THREADS * pl.GPT + MAX_SLAB_GROUPS) + 16 * MAX_SLAB_GROUPS;
         // clusters of more than two blocks leave up to a tenth of the places empty
         auto resident = [&](int n) {

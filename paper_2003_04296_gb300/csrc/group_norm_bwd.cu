@@ -18,14 +18,22 @@ struct Coef {
     static constexpr int NP = (V + 1) / 2;
     Pair nm[NP], sc[NP], be[NP];
 
-    __device__ __forceinline__ void load(const Args &a, int b, int c) {
-        float g[V], h[V], mean[V];
+    // in two steps, so that the pixels' loads can be on their way between
+    float g[V], h[V], mean[V], rstd[V];
+    __device__ __forceinline__ void fetch(const Args &a, int b, int c) {
         load_affine<V>(a, c, g, h);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int64_t at = (int64_t)b * a.G + (c + i) / a.Cg;
-            mean[i] = -a.mean_in[at];
-            g[i] *= a.rstd_in[at];
+            const int64_t at = (int64_t)b * a.G + a.by_Cg.div(c + i);
+            mean[i] = a.mean_in[at];
+            rstd[i] = a.rstd_in[at];
+        }
+    }
+    __device__ __forceinline__ void finish() {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            mean[i] = -mean[i];
+            g[i] *= rstd[i];
         }
 #pragma unroll
         for (int k = 0; k < NP; ++k) {
@@ -33,6 +41,10 @@ struct Coef {
             sc[k] = pick<V>(g, k);
             be[k] = pick<V>(h, k);
         }
+    }
+    __device__ __forceinline__ void load(const Args &a, int b, int c) {
+        fetch(a, b, c);
+        finish();
     }
 };
 
@@ -65,10 +77,10 @@ __device__ __forceinline__ X pixel_gradient(const X &x, const D &dy, const Coef<
     return r;
 }
 
-// Sums over a thread's n pixels, `step` values apart.
+// Sums over a thread's n pixels, `step` values apart; co has been fetched.
 template <typename T, typename TD, int V, int U>
 __device__ __forceinline__ void channel_sums(int act, const T *x, int64_t xstep, const TD *dy, int64_t dstep, int n,
-                                             const Coef<V> &co, Pair *db, Pair *dg) {
+                                             Coef<V> &co, Pair *db, Pair *dg) {
 #pragma unroll
     for (int k = 0; k < Coef<V>::NP; ++k) db[k] = dg[k] = pair(0.0f, 0.0f);
     with_act(act, [&](auto act_) {
@@ -78,13 +90,13 @@ __device__ __forceinline__ void channel_sums(int act, const T *x, int64_t xstep,
         Vec<TD, V> d[U];
         batches<U>(
             n,
-            [&](int u, int) {
+            [&](int u) {
                 v[u].load(px);
                 d[u].load(pd);
                 px += xstep;
                 pd += dstep;
             },
-            [&](int u, int) { add_pixel<act_.value, V>(v[u], d[u], co, db, dg); });
+            [&] { co.finish(); }, [&](int u) { add_pixel<act_.value, V>(v[u], d[u], co, db, dg); });
     });
 }
 
@@ -100,13 +112,14 @@ __device__ __forceinline__ void gradient_pixels(int act, const T *x, int64_t xst
         Vec<TD, V> d[U];
         batches<U>(
             n,
-            [&](int u, int) {
+            [&](int u) {
                 v[u].load(px);
                 d[u].load(pd);
                 px += xstep;
                 pd += dstep;
             },
-            [&](int u, int) {
+            [] {},
+            [&](int u) {
                 pixel_gradient<act_.value, V>(v[u], d[u], co, n1, n2).store(po);
                 po += ostep;
             });
@@ -134,7 +147,7 @@ __global__ void __launch_bounds__(THREADS, 2) bwd_sum_kernel(Args a) {
     if (w.row < w.rows) {
         Pair db[Coef<V>::NP], dg[Coef<V>::NP];
         Coef<V> co;
-        if (w.n > 0) co.load(a, w.b, w.c);
+        if (w.n > 0) co.fetch(a, w.b, w.c);
         const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
         channel_sums<T, TD, V, V == 1 ? 8 : 4>(a.act, static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
                                                static_cast<const TD *>(a.dy) + p * a.lddy + w.c, w.rows * a.lddy, w.n, co,
@@ -229,13 +242,14 @@ template <int V>
 struct Shared {
     float2 red[THREADS * V];               // rows x channels, then segments x channels
     float2 group[MAX_SLAB_GROUPS];
+    float2 scaled[THREADS];                // totals times gamma, where a thread has no more than one channel
     float rstd[MAX_SLAB_GROUPS];           // of the slab's groups
 
     __device__ __forceinline__ void load_rstd(const Args &a, const Tile &w) {
         for (int g = threadIdx.x; g < a.groups; g += THREADS) rstd[g] = a.rstd_in[(int64_t)w.b * a.G + w.slab * a.groups + g];
     }
 };
-static_assert(sizeof(Shared<8>) == 8 * THREADS * 8 + 12 * MAX_SLAB_GROUPS, "plan() counts on it");
+static_assert(sizeof(Shared<8>) == 8 * THREADS * 9 + 12 * MAX_SLAB_GROUPS, "plan() counts on it");
 
 // n1 and n2 of a thread's channels from its sums: the block's rows, the cluster's blocks, the groups' channels, all
 // in a fixed order; and the image's channel sums for dgamma and dbeta.  Afterwards a cluster has arrived at its end.
@@ -244,6 +258,8 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
                                        Pair *n2) {
     const int CW = a.L * V;                                // channels of the slab
     float2 *red = sm.red;
+    const bool few = CW <= THREADS;
+    const float gamma = few && a.gamma && (int)threadIdx.x < CW ? a.gamma[w.slab * CW + threadIdx.x] : 1.0f;      // early
     if (w.row < w.rows) put_sums<V>(red + w.row * CW + w.lane * V, db, dg);
     __syncthreads();
     // `seg` threads a channel, each every so many rows (into the row of its number)
@@ -264,7 +280,9 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
             t.x += red[s * CW + c].x;
             t.y += red[s * CW + c].y;
         }
-        red[c] = make_float2(t.x, t.y * sm.rstd[a.by_Cg.div(c)]);
+        t.y *= sm.rstd[a.by_Cg.div(c)];
+        red[c] = t;
+        if (few) sm.scaled[c] = make_float2(gamma * t.x, gamma * t.y);
     }
     float2 *tot = red;
     if (a.chunks > 1) {
@@ -283,6 +301,7 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
                 u[0].y += u[k].y;
             }
             tot[c] = u[0];
+            if (few) sm.scaled[c] = make_float2(gamma * u[0].x, gamma * u[0].y);
         }
         cluster_done_reading();
     }
@@ -292,10 +311,13 @@ __device__ __forceinline__ void totals(const Args &a, const Tile &w, Shared<V> &
     for (int g = threadIdx.x >> 5; g < a.groups; g += THREADS / 32) {
         float s1 = 0.0f, s2 = 0.0f;
         for (int k = threadIdx.x & 31; k < a.Cg; k += 32) {
-            const float2 t = tot[g * a.Cg + k];
-            const float gk = a.gamma ? a.gamma[w.slab * CW + g * a.Cg + k] : 1.0f;
-            s1 = fmaf(gk, t.x, s1);
-            s2 = fmaf(gk, t.y, s2);
+            float2 t = sm.scaled[few ? g * a.Cg + k : 0];
+            if (!few) {
+                const float gk = a.gamma ? a.gamma[w.slab * CW + g * a.Cg + k] : 1.0f;
+                t = make_float2(gk * tot[g * a.Cg + k].x, gk * tot[g * a.Cg + k].y);
+            }
+            s1 += t.x;
+            s2 += t.y;
         }
         s1 = warp_sum(s1);
         s2 = warp_sum(s2);
@@ -428,19 +450,19 @@ template <typename T, typename TD, int V>
 __global__ void __launch_bounds__(THREADS, 2) reread_bwd_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
-    constexpr int NP = Coef<V>::NP, U = V == 1 ? 8 : 4;
+    constexpr int NP = Coef<V>::NP, U = V == 8 ? 4 : 8;
     __shared__ Shared<V> sm;
     const Tile w = tile<V>(a);
     const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, xstep = (int64_t)w.rows * a.ldx, dstep = (int64_t)w.rows * a.lddy;
     const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
     const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
     Coef<V> co;
-    co.load(a, w.b, w.c);
-    sm.load_rstd(a, w);
+    co.fetch(a, w.b, w.c);
     Pair n1[NP], n2[NP];
     {
         Pair db[NP], dg[NP];
         channel_sums<T, TD, V, U>(a.act, x, xstep, dy, dstep, w.n, co, db, dg);
+        sm.load_rstd(a, w);
         totals<V>(a, w, sm, db, dg, n1, n2);
     }
     gradient_pixels<T, TD, V, U>(a.act, x, xstep, dy, dstep, static_cast<T *>(a.y) + p * a.ldy + w.c,
