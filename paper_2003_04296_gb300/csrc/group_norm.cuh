@@ -401,7 +401,8 @@ inline bool in_chunks(Args &a, bool clusters, int64_t &blocks) {
 }
 
 inline cudaError_t launch_cluster(void (*kern)(Args), int64_t blocks, int cluster, int smem, cudaStream_t s, const Args &a) {
-    if (smem > 32 * 1024 && !allow_shared(reinterpret_cast<const void *>(kern), SHARED_MOST)) return cudaErrorInvalidValue;
+    // (48 KB without it, the kernel's own included)
+    if (smem > 0 && !allow_shared(reinterpret_cast<const void *>(kern), SHARED_MOST)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(THREADS);

@@ -289,6 +289,13 @@ def test_backward(M, case):
     assert (obuf[:, :, rest] == 777).all()
 
 
+@pytest.mark.parametrize("P", [64, 96, 100, 128, 160, 200, 256, 400, 512])
+@pytest.mark.parametrize("types", ["bb", "bf", "ff"])
+def test_backward_of_small_slabs(M, P, types):
+    """From a few KB of shared memory per block to more than 48, where a launch has to ask for it."""
+    test_backward(M, (2, P, 64, 8, 64, 0, types[0], types[1], 1))
+
+
 @pytest.mark.parametrize("case", [(2, 40, 24, 4, 24, 0, "f", "f", 0), (2, 40, 24, 4, 24, 0, "f", "f", 3),
                                   (1, 1500, 32, 8, 32, 0, "f", "f", 3)])
 def test_backward_against_differences(M, case):
