@@ -375,18 +375,7 @@ __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
         with_act(a.act, [&](auto act) {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
-                if (i < w.n) {
-                    float z[2 * NP];
-#pragma unroll
-                    for (int k = 0; k < NP; ++k) {
-                        const float2 h = halves(fma2(add2(v[i].get2(k), nm[k]), sc[k], sh[k]));
-                        z[2 * k] = act_value<act.value>(h.x);
-                        z[2 * k + 1] = act_value<act.value>(h.y);
-                    }
-                    Vec<TY, V> o;
-                    o.set(z);
-                    o.store(y + i * ystep);
-                }
+                if (i < w.n) apply_pixel<T, TY, V, act.value>(v[i], y + i * ystep, nm, sc, sh);
         });
     }
     if (a.chunks > 1) cluster_leave();
@@ -450,19 +439,7 @@ __global__ void __launch_bounds__(THREADS, 3) shared_kernel(Args a) {
         with_act(a.act, [&](auto act) {
             TY *y = static_cast<TY *>(a.y) + p * a.ldy + w.c;
 #pragma unroll U
-            for (int i = 0; i < w.n; ++i, y += ystep) {
-                const Vec<T, V> v = value(i);
-                float z[V];
-#pragma unroll
-                for (int k = 0; k < NP; ++k) {
-                    const float2 h = halves(fma2(add2(v.get2(k), nm[k]), sc[k], sh[k]));
-                    z[2 * k] = act_value<act.value>(h.x);
-                    z[2 * k + 1] = act_value<act.value>(h.y);
-                }
-                Vec<TY, V> o;
-                o.set(z);
-                o.store(y);
-            }
+            for (int i = 0; i < w.n; ++i, y += ystep) apply_pixel<T, TY, V, act.value>(value(i), y, nm, sc, sh);
         });
     }
     if (a.chunks > 1) cluster_leave();
@@ -508,14 +485,15 @@ __global__ void __launch_bounds__(THREADS, 4) chunk_stats_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
     constexpr int W = V / GPT, NP = (V + 1) / 2;
+    __shared__ __align__(16) uint8_t data[V == 1 ? 16 : RING_BYTES<T, V, 4>];
     __shared__ Shared<GPT> sm;
     const Tile w = tile<V>(a);
     float own[GPT], m2[GPT], mean[GPT];
     {
         Pair m[NP], q[NP];
-        channel_stats<T, V, V == 1 ? 16 : 4>(
-            static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c, (int64_t)w.rows * a.ldx, w.n, m,
-            q);
+        const T *x = static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c;
+        if constexpr (V == 1) channel_stats<T, V, 16>(x, (int64_t)w.rows * a.ldx, w.n, m, q);
+        else channel_stats_ring<T, V, 4>(data, x, (int64_t)w.rows * a.ldx, w.n, m, q);
         fold_channels<V, GPT>(m, q, w.n, own, m2);
     }
     merge_block<GPT>(a, w, sm, own, (float)w.n * (float)W, mean, m2);

@@ -296,6 +296,14 @@ def test_backward_of_small_slabs(M, P, types):
     test_backward(M, (2, P, 64, 8, 64, 0, types[0], types[1], 1))
 
 
+@pytest.mark.parametrize("case", [(150, 1029, 64, 8, 64, 0, "b", "b", 3), (150, 1311, 64, 4, 64, 0, "b", "b", 1),
+                                  (80, 1090, 64, 16, 64, 0, "f", "f", 0), (110, 2050, 32, 8, 32, 0, "f", "b", 3),
+                                  (130, 1200, 60, 5, 68, 4, "b", "f", 2)])
+def test_backward_of_slabs_that_fit_nowhere(M, case):
+    """More than the SMs hold at a time: the sums' last pixels are still at hand, the others read again."""
+    test_backward(M, case)
+
+
 @pytest.mark.parametrize("case", [(2, 40, 24, 4, 24, 0, "f", "f", 0), (2, 40, 24, 4, 24, 0, "f", "f", 3),
                                   (1, 1500, 32, 8, 32, 0, "f", "f", 3)])
 def test_backward_against_differences(M, case):
