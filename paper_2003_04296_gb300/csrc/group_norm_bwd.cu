@@ -201,6 +201,7 @@ template <typename T, typename TD, int V>
 __global__ void __launch_bounds__(THREADS, 2) bwd_sum_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
+    extern __shared__ __align__(16) uint8_t data[];
     __shared__ float2 red[THREADS * V];
     const Place w = place<V>(a, blockIdx.x);
     const int W = a.L * V;
@@ -209,9 +210,10 @@ __global__ void __launch_bounds__(THREADS, 2) bwd_sum_kernel(Args a) {
         Coef<V> co;
         if (w.n > 0) co.fetch(a, w.b, w.c);
         const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
-        channel_sums<T, TD, V, V == 1 ? 8 : 4>(a.act, static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
-                                               static_cast<const TD *>(a.dy) + p * a.lddy + w.c, w.rows * a.lddy, w.n, co,
-                                               db, dg);
+        const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+        const TD *dy = static_cast<const TD *>(a.dy) + p * a.lddy + w.c;
+        if constexpr (V == 1) channel_sums<T, TD, V, 8>(a.act, x, w.rows * a.ldx, dy, w.rows * a.lddy, w.n, co, db, dg);
+        else Ring<T, TD, V>(data).sums(a.act, x, w.rows * a.ldx, dy, w.rows * a.lddy, w.n, co, db, dg);
         put_sums<V>(red + w.row * W + w.lane * V, db, dg);
     }
     __syncthreads();
@@ -592,7 +594,8 @@ static minw_status backward(Args a, int V, cudaStream_t s) {
             }
         int64_t blocks;
         if (!in_chunks(a, false, blocks)) return MINW_EUNSUPPORTED;
-        if (launch(sum, blocks, s, a) != cudaSuccess ||
+        const int ring = V > 1 ? RING_PIXELS * THREADS * V * (int)(sizeof(T) + sizeof(TD)) : 0;
+        if (launch_cluster(sum, blocks, 1, ring, s, a) != cudaSuccess ||
             launch(bwd_merge_kernel, (int64_t)a.B * a.G, s, a) != cudaSuccess || launch(apply, blocks, s, a) != cudaSuccess)
             return launch_failed();
     }
