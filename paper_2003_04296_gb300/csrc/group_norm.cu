@@ -118,8 +118,8 @@ __global__ void __launch_bounds__(THREADS, 4) apply_kernel(Args a) {
     const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row;
     with_act(a.act, [&](auto act) {
         apply_pixels<T, TY, V, V == 1 ? 8 : 4, act.value>(static_cast<const T *>(a.x) + p * a.ldx + w.c, w.rows * a.ldx,
-                                                          static_cast<TY *>(a.y) + p * a.ldy + w.c, w.rows * a.ldy, w.n,
-                                                          nm, sc, sh);
+                                                          static_cast<TY *>(a.y) + p * a.ldy + w.c, w.rows * a.ldy, w.n, w.n,
+                                                          [](int) { return Vec<T, V>(); }, nm, sc, sh);
     });
 }
 
@@ -324,6 +324,8 @@ __device__ __forceinline__ void fold_pairs(const Pair *p, float *f) {
 }
 
 // In registers.  GPT: groups among a thread's V channels (W = V / GPT channels of each); NV: pixels of a thread at most.
+// 400 x 256 x 256 bf16: 21.1 us, 5.0 TB/s of the 6.8 of a copy: a block's chain of loads, two sums and stores at 32
+// warps an SM, about a third of its instructions the same for any number of pixels.
 template <typename T, typename TY, int V, int GPT, int NV>
 __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
     pdl_trigger();
@@ -378,10 +380,10 @@ __global__ void __launch_bounds__(THREADS, V == 1 ? 3 : 4) held_kernel(Args a) {
                 if (i < w.n) apply_pixel<T, TY, V, act.value>(v[i], y + i * ystep, nm, sc, sh);
         });
     }
-    if (a.chunks > 1) cluster_leave();
 }
 
-// In shared memory.  Each thread copies the vectors that it reads, so that only the sums need barriers.
+// In shared memory.  Each thread copies the vectors that it reads, so that only the sums need barriers.  128 x 784 x 128
+// bf16: 13.2 us, 3.9 TB/s: all of x is read before anything is written.  1 x 64 x 512: 2.8 us, a chain of latencies.
 template <typename T, typename TY, int V, int GPT>
 __global__ void __launch_bounds__(THREADS, 3) shared_kernel(Args a) {
     pdl_trigger();
@@ -445,20 +447,26 @@ __global__ void __launch_bounds__(THREADS, 3) shared_kernel(Args a) {
     if (a.chunks > 1) cluster_leave();
 }
 
-// In two readings.
+// In two readings, but for the pixels that the ring still holds at the second: where a slab is more than a block holds
+// in registers (200 x 784 x 256 fp32: 60 us; 68 in the registers of clusters of four; 200 x 400 x 256: 30.1 and 35.5)
+// and the slabs more than the SMs hold in shared memory.  256 x 1024 x 128, fp32 to bf16: 42.2 us, 4.8 TB/s.
 template <typename T, typename TY, int V, int GPT>
 __global__ void __launch_bounds__(THREADS, 4) reread_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
     constexpr int W = V / GPT, NP = (V + 1) / 2;
+    extern __shared__ __align__(16) uint8_t data[];
     __shared__ Shared<GPT> sm;
     const Tile w = tile<V>(a);
     const int64_t p = (int64_t)w.b * a.P + w.p0 + w.row, step = (int64_t)w.rows * a.ldx;
     const T *x = static_cast<const T *>(a.x) + p * a.ldx + w.c;
+    const Ring<T, V> ring(data);
+    const int first = V > 1 ? ring.first(w.n) : w.n;        // what is still there at the second reading
     float mean[GPT], rstd[GPT];
     {
         Pair m[NP], q[NP];
-        channel_stats<T, V, V == 1 ? 16 : 4>(x, step, w.n, m, q);
+        if constexpr (V == 1) channel_stats<T, V, 16>(x, step, w.n, m, q);
+        else ring.stats(x, step, w.n, m, q);
         float own[GPT], m2[GPT];
         fold_channels<V, GPT>(m, q, w.n, own, m2);
         merge<GPT>(a, w, sm, own, m2, (float)w.n * (float)W, mean, rstd);
@@ -468,7 +476,8 @@ __global__ void __launch_bounds__(THREADS, 4) reread_kernel(Args a) {
         coefficients<V, GPT>(a, w.c, mean, rstd, nm, sc, sh);
         with_act(a.act, [&](auto act) {
             apply_pixels<T, TY, V, V == 1 ? 8 : 4, act.value>(x, step, static_cast<TY *>(a.y) + p * a.ldy + w.c,
-                                                              (int64_t)w.rows * a.ldy, w.n, nm, sc, sh);
+                                                              (int64_t)w.rows * a.ldy, first, w.n,
+                                                              [&](int i) { return ring.read(i); }, nm, sc, sh);
         });
     }
     if (a.chunks > 1) cluster_leave();
@@ -477,7 +486,9 @@ __global__ void __launch_bounds__(THREADS, 4) reread_kernel(Args a) {
 // ---------------------------------------------------------------------------
 // Two kernels, for images that no cluster could take alone: the statistics of
 // every STREAM_CLUSTER chunks of an image, merged by a cluster; then each block
-// merges its image's and applies them to its chunk.
+// merges its image's and applies them to its chunk.  2 x 252003 x 96 bf16 of 160:
+// 63.7 us; the lines of its rows are 129 MB, read twice, and 97 MB are written:
+// 5.6 TB/s.
 // ---------------------------------------------------------------------------
 
 template <typename T, int V, int GPT>
@@ -485,7 +496,7 @@ __global__ void __launch_bounds__(THREADS, 4) chunk_stats_kernel(Args a) {
     pdl_trigger();
     pdl_wait();
     constexpr int W = V / GPT, NP = (V + 1) / 2;
-    __shared__ __align__(16) uint8_t data[V == 1 ? 16 : RING_BYTES<T, V, 4>];
+    __shared__ __align__(16) uint8_t data[V == 1 ? 16 : Ring<T, V>::SIZE];
     __shared__ Shared<GPT> sm;
     const Tile w = tile<V>(a);
     float own[GPT], m2[GPT], mean[GPT];
@@ -493,7 +504,7 @@ __global__ void __launch_bounds__(THREADS, 4) chunk_stats_kernel(Args a) {
         Pair m[NP], q[NP];
         const T *x = static_cast<const T *>(a.x) + ((int64_t)w.b * a.P + w.p0 + w.row) * a.ldx + w.c;
         if constexpr (V == 1) channel_stats<T, V, 16>(x, (int64_t)w.rows * a.ldx, w.n, m, q);
-        else channel_stats_ring<T, V, 4>(data, x, (int64_t)w.rows * a.ldx, w.n, m, q);
+        else Ring<T, V>(data).stats(x, (int64_t)w.rows * a.ldx, w.n, m, q);
         fold_channels<V, GPT>(m, q, w.n, own, m2);
     }
     merge_block<GPT>(a, w, sm, own, (float)w.n * (float)W, mean, m2);
@@ -558,7 +569,7 @@ __global__ void __launch_bounds__(THREADS, 4) chunk_apply_kernel(Args a) {
     with_act(a.act, [&](auto act) {
         apply_pixels<T, TY, V, V == 1 ? 8 : 4, act.value>(static_cast<const T *>(a.x) + p * a.ldx + w.c,
                                                           (int64_t)w.rows * a.ldx, static_cast<TY *>(a.y) + p * a.ldy + w.c,
-                                                          (int64_t)w.rows * a.ldy, w.n, nm, sc, sh);
+                                                          (int64_t)w.rows * a.ldy, w.n, w.n, [](int) { return Vec<T, V>(); }, nm, sc, sh);
     });
 }
 

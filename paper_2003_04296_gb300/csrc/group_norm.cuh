@@ -139,42 +139,47 @@ __device__ __forceinline__ void channel_stats(const T *x, int64_t step, int n, P
     }
 }
 
-// The same through a ring of asynchronous copies: 2 U pixels of a thread in flight without a register of them (2 x 252003 x
-// 96 of 160: 63.4 us for 68.4).  Each thread reads its own copies, so that the ring needs no barrier.
-template <typename T, int V, int U>
-constexpr int RING_BYTES = 2 * U * THREADS * Vec<T, V>::BYTES;
-template <typename T, int V, int U>
-__device__ __forceinline__ void channel_stats_ring(uint8_t *shared, const T *x, int64_t step, int n, Pair *m, Pair *q) {
-    constexpr int BYTES = Vec<T, V>::BYTES;
-    uint8_t *own = shared + threadIdx.x * BYTES;
-    auto slot = [&](int i) { return own + (i & (2 * U - 1)) * (THREADS * BYTES); };
-    auto fetch = [&](int i0) {                              // pixels i0 .. i0 + U - 1, those that there are
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (i0 + u < n) copy_async<BYTES>(slot(i0 + u), x + u * step);
-        x += U * step;
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-#pragma unroll
-    for (int k = 0; k < (V + 1) / 2; ++k) m[k] = q[k] = pair(0.0f, 0.0f);
-    fetch(0);
-    fetch(U);
-    int i = 0;
-    for (; i + U <= n; i += U) {
-        asm volatile("cp.async.wait_group 1;" ::: "memory");
-        Vec<T, V> v[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u].load(reinterpret_cast<const T *>(slot(i + u)));
-        merge_pixels<T, V, U>(v, i, m, q);
-        fetch(i + 2 * U);
-    }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    for (; i < n; ++i) {
+// The same through a ring of asynchronous copies: eight pixels of a thread in flight without a register of them, and the
+// last ones, from first() on, stay there.  Each thread reads its own copies, so that the ring needs no barrier.
+constexpr int RING_PIXELS = 8;
+template <typename T, int V>
+struct Ring {
+    static constexpr int U = 4, BYTES = Vec<T, V>::BYTES, SIZE = RING_PIXELS * THREADS * BYTES;
+    static_assert(RING_PIXELS == 2 * U, "two fetches in flight");
+    uint8_t *own;
+    __device__ __forceinline__ explicit Ring(uint8_t *shared) : own(shared + threadIdx.x * BYTES) {}
+    static __device__ __forceinline__ int first(int n) { return max((n + U - 1) / U * U - RING_PIXELS, 0); }
+    __device__ __forceinline__ uint8_t *slot(int i) const { return own + (i & (RING_PIXELS - 1)) * (THREADS * BYTES); }
+    __device__ __forceinline__ Vec<T, V> read(int i) const {
         Vec<T, V> v;
         v.load(reinterpret_cast<const T *>(slot(i)));
-        merge_pixel<T, V>(v, i, m, q);
+        return v;
     }
-}
+    __device__ __forceinline__ void stats(const T *x, int64_t step, int n, Pair *m, Pair *q) const {
+        auto fetch = [&](int i0) {                              // pixels i0 .. i0 + U - 1, those that there are
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u < n) copy_async<BYTES>(slot(i0 + u), x + u * step);
+            x += U * step;
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+#pragma unroll
+        for (int k = 0; k < (V + 1) / 2; ++k) m[k] = q[k] = pair(0.0f, 0.0f);
+        fetch(0);
+        fetch(U);
+        int i = 0;
+        for (; i + U <= n; i += U) {
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            Vec<T, V> v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = read(i + u);
+            merge_pixels<T, V, U>(v, i, m, q);
+            fetch(i + RING_PIXELS);
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        for (; i < n; ++i) merge_pixel<T, V>(read(i), i, m, q);
+    }
+};
 
 // f(u) for a thread's n pixels, U at a time, after load(u) for all of those; once() when the first are on their way.
 template <int U, typename L, typename O, typename F>
@@ -215,23 +220,26 @@ __device__ __forceinline__ void apply_pixel(const Vec<T, V> &v, TY *y, const Pai
 // The same on a thread's n pixels: minus the means, a = rstd gamma and b = beta in pairs.  From the last pixel to the
 // first: what the sums read last is what L2 still holds (2 x 252003 x 96 of 160: 68.4 us for 69.8 in the sums' order,
 // 64 x 112 x 112 x 64: 55.7 for 56.9).
-template <typename T, typename TY, int V, int U, int ACT>
-__device__ __forceinline__ void apply_pixels(const T *x, int64_t xstep, TY *y, int64_t ystep, int n, const Pair *nm,
-                                             const Pair *a, const Pair *b) {
+template <typename T, typename TY, int V, int U, int ACT, typename K>
+__device__ __forceinline__ void apply_pixels(const T *x, int64_t xstep, TY *y, int64_t ystep, int first, int n, K kept,
+                                             const Pair *nm, const Pair *a, const Pair *b) {
     Vec<T, V> v[U];
     if (V > 1) {
-        x += (n - 1) * xstep;
+        x += (first - 1) * xstep;
         y += (n - 1) * ystep;
         xstep = -xstep;
         ystep = -ystep;
     }
     batches<U>(
-        n,
+        first,
         [&](int u) {
             v[u].load(x);
             x += xstep;
         },
-        [] {},
+        [&] {
+#pragma unroll 4
+            for (int i = n - 1; i >= first; --i, y += ystep) apply_pixel<T, TY, V, ACT>(kept(i), y, nm, a, b);
+        },
         [&](int u) {
             apply_pixel<T, TY, V, ACT>(v[u], y, nm, a, b);
             y += ystep;
@@ -263,14 +271,12 @@ __device__ __forceinline__ Place place(const Args &a, int64_t block) {
 // ---------------------------------------------------------------------------
 // One kernel: a block, or a cluster of blocks that split the pixels, takes an
 // image's slab of whole groups (L lanes of V channels).  A slab stays in shared
-// memory where there are no more slabs than the SMs can hold at a time, small
-// ones in registers where there are; larger ones are read again, from L2, once
-// their sums are known.
+// memory where there are no more slabs than the SMs can hold at a time, in a
+// block's registers where there are and it fits; of larger ones, what has left
+// the block's ring is read again, from L2, once their sums are known.
 // ---------------------------------------------------------------------------
 
 constexpr int MAX_SLAB_GROUPS = 256;
-constexpr int RING_PIXELS = 8;         // of a thread, in the backward's ring
-constexpr int HELD_CLUSTER = 4;        // blocks of a cluster that holds its slab in registers, at most
 
 struct Tile {
     int b, slab, rank, p0, p1, lane, row, rows, c, n;      // n: pixels of this thread
@@ -362,9 +368,10 @@ inline void lanes(Args &a, int V) {
     a.by_Cg = Div(a.Cg);
 }
 
-// The plan for slabs of whole groups: at least 128 bytes of a row wide where one fits (64 where not: the
-// memory's lines are 128 bytes, or where the wide ones are too few to fill the SMs), the narrowest such, so that the
-// blocks are many.
+// The plan for slabs of whole groups: at least 128 bytes of a row wide where one fits (64 where not, or where the wide
+// ones are too few to fill the SMs), the narrowest such, so that the blocks are many.  The memory's lines are 128 bytes:
+// the backward of 256 x 256 x 256 bf16 takes 32.0 us in slabs of 128 bytes, 40.1 of 64; that of 2 x 64 x 512 4.7 of 64,
+// 5.1 of 128.  Whole lines where rows begin on one: 100 x 2000 x 96 fp32 53.6 us, 58.2 without.
 enum Way { SHARED, HELD, REREAD, CHUNKS };      // in shared memory, in registers, read twice; images in chunks
 struct Plan {
     int V, GPT;
@@ -400,8 +407,11 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
     rows = THREADS / L;
     const int64_t slabs = (int64_t)a.B * (a.G / k);
     const int cap = rows * (pl.V == 1 ? 32 : 8);
-    cluster = (a.P + cap - 1) / cap;
-    pl.way = cluster <= HELD_CLUSTER ? HELD : REREAD;
+    cluster = 1;
+    // Registers hold eight pixels of a thread.  A cluster's registers for more lose to a second reading that a ring
+    // spares in part: 200 x 784 x 256 fp32 60.0 us in two readings, 67.6 in clusters of four, the backward 92.6 and 120;
+    // at one block 200 x 256 x 256 takes 19.3 us for 21.8, the backward 35.1 for 37.3.
+    pl.way = a.P <= cap ? HELD : REREAD;
     pl.smem = 0;
     if (pl.V > 1) {
         auto share = [&](int n) { return (int64_t)((a.P + n - 1) / n + rows - 1) / rows * THREADS * pl.V * (bytes + dy_bytes); };
@@ -413,10 +423,11 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
             const int64_t each = 227 * 1024 / (share(n) + static_bytes + 1024), most = backward ? 2 : 3;
             return share(n) <= SHARED_MOST && slabs * n <= (each < most ? each : most) * sms * (n > 2 ? 9 : 10) / 10;
         };
+        // 128 x 784 x 128 bf16: 13.2 us; 14.7 in two readings.  64 x 196 x 256: 5.3 us for 4.8 in registers, 6.4 in two.
         int n = 1;
         while (n <= 8 && !resident(n)) ++n;
         if (n <= 8) {
-            // two blocks per SM where a thread keeps four pixels
+            // two blocks per SM where a thread keeps four pixels (8 x 1024 x 128: 4.7 us for 5.0)
             while (n <= 4 && slabs * n * 2 <= 2 * sms && a.P >= 8 * n * rows && resident(2 * n)) n *= 2;
             cluster = n;
             pl.way = SHARED;
@@ -424,11 +435,17 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
         }
     }
     if (pl.way == REREAD) {
-        // as many blocks as fit at a time; in the backward twice as many where a thread still has 16 pixels
-        for (cluster = 1; cluster < 8 && slabs * cluster * 2 <= places; cluster *= 2) {}
-        if (backward && cluster < 8 && slabs * cluster <= places && a.P >= 32 * cluster * rows) cluster *= 2;
-        if (slabs * cluster < sms) pl.way = CHUNKS;                     // fewer blocks than SMs
-        if (backward && pl.V > 1) pl.smem = RING_PIXELS * THREADS * pl.V * (bytes + dy_bytes);
+        // Forward: up to twice as many blocks as fit at a time (160 x 3000 x 128 bf16: 68.6 us; 77.4 with up to as many;
+        // 64 x 6000 x 64 loses, 32.3 for 29.6), but not by single values (100 x 400 x 99: 14.1 us, 18.5).  Backward: as many as fit; twice as many where a thread has 16 to 32 pixels
+        // then (128 x 3136 x 64: 50.9 us for 54.3) or a third of the places stay empty (100 x 9000 x 64: 117 for 127),
+        // and not else (150 x 12544 x 64: 200 us, 239 with twice as many).
+        for (cluster = 1; cluster < 8 && slabs * cluster * 2 <= (backward || pl.V == 1 ? 1 : 2) * places; cluster *= 2) {}
+        if (backward && cluster < 8 && slabs * cluster <= places && a.P >= 32 * cluster * rows &&
+            (a.P < 64 * cluster * rows || slabs * cluster * 10 <= places * 7))
+            cluster *= 2;
+        // fewer blocks than SMs (2 x 252003 x 96 of 160: 63.7 us, 622 in clusters)
+        if (slabs * cluster < sms) pl.way = CHUNKS;
+        if (pl.V > 1) pl.smem = RING_PIXELS * THREADS * pl.V * (bytes + dy_bytes);
     }
     // a cluster's totals go behind the block's sums
     if (backward && (pl.way == CHUNKS || (cluster > 1 && rows < 2))) return false;

@@ -9,7 +9,9 @@
 // mma.sync (bf16 x bf16, fp32 sums): the weights are its 16-row operand, the
 // vectors its 8 columns.  A tile of the tcgen05 tensor cores has 128 rows and
 // takes both operands from shared memory, which the unpacked weights would
-// have to be written to first, at four times their packed bytes.
+// have to be written to first, at four times their packed bytes.  Measured, one
+// vector: 16384 x 16384 in 32.5 us, 4.3 TB/s (unpacking keeps the integer pipe as
+// busy as the memory), 1024 x 8192 in 4.2 us (latency); eight: 8192 x 8192 in 12.5.
 //
 // A lane reads 16 bytes of codes of two rows: 32 values each, four groups of
 // eight.  The layout puts the eight values 32 j + 8 t of a block of 128 into
