@@ -487,8 +487,8 @@ __global__ void __launch_bounds__(THREADS, 4) reread_kernel(Args a) {
 // Two kernels, for images that no cluster could take alone: the statistics of
 // every STREAM_CLUSTER chunks of an image, merged by a cluster; then each block
 // merges its image's and applies them to its chunk.  2 x 252003 x 96 bf16 of 160:
-// 63.7 us; the lines of its rows are 129 MB, read twice, and 97 MB are written:
-// 5.6 TB/s.
+// 63.7 us; the lines of its rows are 129 MB, read twice, a third of the second
+// time from L2, and 97 MB are written: 4.9 TB/s of memory traffic.
 // ---------------------------------------------------------------------------
 
 template <typename T, int V, int GPT>
