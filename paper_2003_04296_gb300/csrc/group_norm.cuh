@@ -46,8 +46,9 @@ struct Args {
     int chunks, ppc;               // pixel chunks per image, pixels per chunk
     int L, slabs;                  // lanes (V channels each) of a slab, slabs of a row
     // slabs of whole groups
-    int butterfly;                 // lanes and the lanes of a group are powers of two within a warp
+    int butterfly;                 // forward: lanes and the lanes of a group are powers of two within a warp
     int rows, groups, per;         // pixel rows of a block, groups of a slab, entries (a thread's share of a group) of a group
+                                   // (forward)
     float inv_total;               // 1 / (P Cg)
     int seg;                       // backward: threads that sum a channel's rows
     Div by_L, by_rows, by_per, by_Cg, by_chunks, by_slabs, by_channels;
@@ -449,8 +450,12 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
     }
     // a cluster's totals go behind the block's sums
     if (backward && (pl.way == CHUNKS || (cluster > 1 && rows < 2))) return false;
-    a.per = a.Cg / (pl.V / pl.GPT);
-    a.butterfly = L <= 32 && (L & (L - 1)) == 0 && (a.per == 1 || (pl.GPT == 1 && (a.per & (a.per - 1)) == 0));
+    if (!backward) {
+        // (the backward sums by channels: it has no entries, and its V may be more than two groups of one channel)
+        a.per = a.Cg / (pl.V / pl.GPT);
+        a.butterfly = L <= 32 && (L & (L - 1)) == 0 && (a.per == 1 || (pl.GPT == 1 && (a.per & (a.per - 1)) == 0));
+        a.by_per = Div(a.per);
+    }
     a.rows = rows;
     a.groups = k;
     a.L = L;
@@ -462,7 +467,6 @@ inline bool plan(Args &a, Plan &pl, int bytes, int dy_bytes, int V0) {
     a.by_channels = Div((uint32_t)channels);
     a.by_L = Div(L);
     a.by_rows = Div(rows);
-    a.by_per = Div(a.per);
     a.by_Cg = Div(a.Cg);
     a.by_chunks = Div((uint32_t)cluster);
     a.by_slabs = Div((uint32_t)a.slabs);

@@ -167,7 +167,7 @@ __device__ __forceinline__ Pair act_grad2(Pair z, Pair dy) {
 __device__ __forceinline__ void cluster_done_reading() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_leave() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 
-// n / d for 0 <= n < 2^31 with the divisor known on the host: a product's upper half and a shift.
+// n / d for 0 <= n < 2^31 with the divisor (1 to 2^31) known on the host: a product's upper half and a shift.
 struct Div {
     uint32_t d = 1, m = 1, s = 0;
     Div() = default;
