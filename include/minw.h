@@ -573,13 +573,14 @@ enum {
  * (nullable: 1 and 0): fp32 [C].  mean, rstd (nullable): fp32 [B][G], what
  * the backward needs.  A NaN or infinity makes its own group's outputs NaN,
  * no other's.
- * x, y are aligned to their elements; rows on 16-byte boundaries (8 for bf16
- * rows) run wider loads.  workspace: device scratch of
+ * All of them are aligned to their elements; rows on 16-byte boundaries (8
+ * for bf16 rows) run wider loads.  workspace: device scratch of
  * minw_group_norm_workspace_bytes (16-byte aligned, contents meaningless
  * before and after; null where that is 0); calls that share one must not run
  * concurrently.  B = 0 does nothing.  Errors: MINW_EINVAL (null x or y, B < 0,
  * P < 1, C < 1, G < 1 or not dividing C, short rows, unknown type or act,
- * eps negative or not finite, misaligned or short workspace),
+ * eps negative or not finite, a misaligned tensor or vector, misaligned or
+ * short workspace),
  * MINW_EUNSUPPORTED (P >= 2^30, or more blocks than a grid holds). */
 MINW_API size_t minw_group_norm_workspace_bytes(int32_t B, int64_t P, int32_t C, int32_t G, int32_t backward);
 MINW_API minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamma,

@@ -649,6 +649,7 @@ minw_status minw_group_norm(const void *x, int32_t x_type, int64_t ldx, const fl
     if (!(eps >= 0.0f && isfinite(eps))) return MINW_EINVAL;
     if (!gn::fits(x, 1, x_type, 1) || !gn::fits(y, 1, y_type, 1) || !gn::in_place_ok(x, x_type, ldx, y, y_type, ldy))
         return MINW_EINVAL;
+    if (!on_floats(gamma, beta, mean, rstd)) return MINW_EINVAL;
     if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;
     if (B == 0) return MINW_OK;
     const gn::Layout l = gn::layout(B, P, C, G, false);

@@ -636,6 +636,7 @@ minw_status minw_group_norm_backward(const void *x, int32_t x_type, int64_t ldx,
     if (!gn::valid_type(x_type) || !gn::valid_type(dy_type) || act < MINW_ACT_NONE || act > MINW_ACT_SILU)
         return MINW_EINVAL;
     if (!gn::fits(x, 1, x_type, 1) || !gn::fits(dy, 1, dy_type, 1) || !gn::fits(dx, 1, x_type, 1)) return MINW_EINVAL;
+    if (!on_floats(gamma, beta, mean, rstd, dgamma, dbeta)) return MINW_EINVAL;
     if (!gn::in_place_ok(x, x_type, ldx, dx, x_type, lddx) || !gn::in_place_ok(dy, dy_type, lddy, dx, x_type, lddx))
         return MINW_EINVAL;
     if (P >= (1ll << 30)) return MINW_EUNSUPPORTED;

@@ -191,6 +191,12 @@ __device__ __forceinline__ void with_act(int act, F f) {
 
 namespace minw_host {
 
+// Whether every fp32 vector (null: not given) lies on its elements' boundary.
+template <typename... T>
+inline bool on_floats(const T *...p) {
+    return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0;
+}
+
 // The status of a launch that the runtime refused, whose error would else be the next call's.
 inline minw_status launch_failed() {
     cudaGetLastError();

@@ -467,7 +467,7 @@ minw_status minw_pack_w4(const void *w, int32_t type, int32_t O, int32_t K, int3
                          const float *channel_scale, uint8_t *codes, uint16_t *scales, void *stream) {
     if (!w || !codes || !scales || O < 1 || K < 1 || !w4::valid_group(group)) return MINW_EINVAL;
     if ((type != MINW_F32 && type != MINW_BF16) || (q && !valid_quant(q))) return MINW_EINVAL;
-    if (!aligned16(codes) || reinterpret_cast<uintptr_t>(scales) % 2 != 0 ||
+    if (!aligned16(codes) || reinterpret_cast<uintptr_t>(scales) % 2 != 0 || !on_floats(channel_scale) ||
         reinterpret_cast<uintptr_t>(w) % (type == MINW_BF16 ? 2 : 4) != 0)
         return MINW_EINVAL;
     if (K > (1 << 28) || group > (1 << 28)) return MINW_EUNSUPPORTED;
@@ -485,7 +485,7 @@ minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T
     if (!codes || !scales || (T != 0 && (!x || !y)) || T < 0 || O < 1 || K < 1 || ldx < K || ldy < O) return MINW_EINVAL;
     if (!w4::valid_group(group) || act < MINW_ACT_NONE || act > MINW_ACT_SILU) return MINW_EINVAL;
     if ((x_type != MINW_F32 && x_type != MINW_BF16) || (y_type != MINW_F32 && y_type != MINW_BF16)) return MINW_EINVAL;
-    if (!aligned16(codes) || reinterpret_cast<uintptr_t>(scales) % 2 != 0 ||
+    if (!aligned16(codes) || reinterpret_cast<uintptr_t>(scales) % 2 != 0 || !on_floats(scale, shift) ||
         reinterpret_cast<uintptr_t>(x) % (x_type == MINW_BF16 ? 2 : 4) != 0 ||
         reinterpret_cast<uintptr_t>(y) % (y_type == MINW_BF16 ? 2 : 4) != 0)
         return MINW_EINVAL;
