@@ -39,7 +39,7 @@ class Head:
         self.norm = torch.empty(1, device="cuda")
         self.grad_ws = self._bytes(minw.minw_grad_workspace_bytes(len(self.grads)))
         self.buffers = {}
-        self.codes = self.scales = None
+        self.codes = self.scales = self.packed = None
 
     @staticmethod
     def _bytes(n):
@@ -99,20 +99,25 @@ class Head:
         return loss
 
     def pack(self):
-        """The weights as 4-bit codes with a scale per group."""
+        """The weights as 4-bit codes with a scale per group, and what goes with them as it is now: steps taken later
+        change no answer until the next pack()."""
         cs, ss = minw.w4_shapes(self.O, self.K, self.w4_group)
         self.codes = torch.empty(cs, dtype=torch.uint8, device="cuda")
         self.scales = torch.empty(ss, dtype=torch.bfloat16, device="cuda")
         minw.minw_pack_w4(self.w, self.w4_group, self.codes, self.scales)
+        self.packed = [t.clone() for t in (self.gamma, self.beta, self.bias)]
 
     def answer(self, x):
-        """Logits [T][classes] of one input or a few, from the packed weights."""
+        """Logits [T][classes] of one input or a few, from the head as it was packed."""
+        if self.packed is None:
+            raise RuntimeError("pack() comes before the first answer")
+        gamma, beta, bias = self.packed
         T = x.shape[0]
         a = torch.empty((T, self.P, self.C), dtype=torch.bfloat16, device="cuda")
         y = torch.empty((T, self.O), device="cuda")
-        minw.minw_group_norm(x.view(T, self.P, self.C), self.gamma, self.beta, self.G, EPS, a, act=minw.ACT_HARDTANH,
+        minw.minw_group_norm(x.view(T, self.P, self.C), gamma, beta, self.G, EPS, a, act=minw.ACT_HARDTANH,
                              workspace=self._bytes(minw.minw_group_norm_workspace_bytes(T, self.P, self.C, self.G)))
-        minw.minw_w4_matvec(a.view(T, self.K), self.codes, self.scales, self.w4_group, y, shift=self.bias)
+        minw.minw_w4_matvec(a.view(T, self.K), self.codes, self.scales, self.w4_group, y, shift=bias)
         return y
 
 
