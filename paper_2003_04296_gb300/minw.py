@@ -934,7 +934,8 @@ class TensorList:
     def __init__(self, tensors, limits=float("inf")):
         self.tensors = list(tensors)
         n = len(self.tensors)
-        limits = [float(limits)] * n if isinstance(limits, (int, float)) else [float(v) for v in limits]
+        one = isinstance(limits, (int, float)) or getattr(limits, "ndim", None) == 0          # numpy's and torch's too
+        limits = [float(limits)] * n if one else [float(v) for v in limits]
         if len(limits) != n:
             raise ValueError("a limit per tensor expected")
         self.array = (Tensor * max(1, n))()
