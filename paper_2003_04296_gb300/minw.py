@@ -264,9 +264,14 @@ def _host_ptr(a):
 def _stream(stream):
     if stream is not None:
         return ctypes.c_void_p(stream.cuda_stream)
-    # the current stream's handle without a Stream object around it (3 us of a call's host time)
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if torch.cuda.is_initialized() else \
-        ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the current stream's handle without a Stream object around it (3 us of a call's host time), where torch has these
+    # functions: they are no part of its interface
+    if torch.cuda.is_initialized():
+        try:
+            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        except AttributeError:
+            pass
+    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
 _VALUE_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
