@@ -116,7 +116,7 @@ struct Args {
 __device__ __forceinline__ uint32_t levels(uint32_t word, int p) {
     uint32_t v = word >> (4 * p);
     asm("lop3.b32 %0, %0, %1, %2, 0xea;" : "+r"(v) : "r"(0x000f000fu), "r"(0x43004300u));     // (v & ..) | ..: 128 + code
-    asm("fma.rn.bf16x2 %0, %0, %1, %2;" : "+r"(v) : "r"(0x3f803f80u), "r"(0xc308c308u));      // 1 v - 136
+    asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(v) : "r"(0xc308c308u));                            // - 136
     return v;
 }
 
