@@ -617,8 +617,11 @@ typedef struct {
  * in fp64 across blocks; a block whose squares leave fp32's range is summed
  * again in fp64, so the norm is right wherever it is an fp32 number.  Infinite
  * or NaN gradients give an infinite or NaN norm.  grads: host array, read
- * during the call.  The sums' order is fixed by the lengths (the same bits
- * on every call).  workspace: device scratch of
+ * during the call.  The sums' order follows from the entry point, the lengths
+ * and types, the addresses modulo 16 and the device: the same bits on every
+ * call where these are the same, possibly other last bits where one differs
+ * (tensors at other offsets; the norm alone, or with a clip or an update).
+ * workspace: device scratch of
  * minw_grad_workspace_bytes(count), 16-byte aligned, contents meaningless
  * before and after.  count = 0 writes 0.
  * Errors: MINW_EINVAL (count < 0, null grads, norm or workspace, a tensor with
@@ -641,8 +644,9 @@ MINW_API minw_status minw_grad_clip(const minw_tensor *grads, const minw_tensor 
  * gradients clipped by their global norm:
  *   w = min(limit, max(-limit, fmaf(-lr, k g, w)))
  * in fp32 (weights fp32 or bf16; bf16 weights round once), limit per weight
- * tensor.  Where the norm is not finite no weight changes.  Errors as
- * minw_grad_clip; limit >= 0, lr finite. */
+ * tensor.  Weights may overlap neither each other nor a gradient.  Where the
+ * norm is not finite no weight changes.  Errors as minw_grad_clip; limit >= 0,
+ * lr finite. */
 MINW_API minw_status minw_sgd_clip_norm(const minw_tensor *weights, const minw_tensor *grads, int32_t count,
                                         float max_norm, float lr, float *norm, void *workspace,
                                         size_t workspace_bytes, void *stream);
@@ -677,7 +681,8 @@ MINW_API minw_status minw_pack_w4(const void *w, int32_t type, int32_t O, int32_
  * for each further such set: made for a token or a few.  T = 0 does nothing.
  * The same bits on every call.  Errors: MINW_EINVAL (null pointers, T < 0,
  * O or K < 1, group, types, act, short rows, alignment: codes 16 bytes, the
- * others their elements), MINW_EUNSUPPORTED (sizes past 2^28). */
+ * others their elements), MINW_EUNSUPPORTED (O, K or group past 2^28, vectors
+ * of more than 65535 such sets). */
 MINW_API minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T, const uint8_t *codes,
                                     const uint16_t *scales, int32_t O, int32_t K, int32_t group, const float *scale,
                                     const float *shift, int32_t act, void *y, int32_t y_type, int64_t ldy,

@@ -244,6 +244,8 @@ __device__ __forceinline__ float step(float g, float w, float k, float lr, float
     return v > limit ? limit : v < -limit ? -limit : v;
 }
 
+// Vectors where both tensors' begin together, else value by value (14 M fp32 in 33 tensors, gradients in one buffer and
+// weights of their own allocation: the update 81 us for 40).
 template <int OP, typename TG, typename TO>
 __device__ __forceinline__ void steps(const Entry &e, int64_t i0, int64_t i1, float k, float lr) {
     constexpr int V = sizeof(TG) == 2 && sizeof(TO) == 2 ? 8 : 4, U = OP == UPDATE ? 2 : 4;

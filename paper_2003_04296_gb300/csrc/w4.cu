@@ -10,8 +10,13 @@
 // vectors its 8 columns.  A tile of the tcgen05 tensor cores has 128 rows and
 // takes both operands from shared memory, which the unpacked weights would
 // have to be written to first, at four times their packed bytes.  Measured, one
-// vector: 16384 x 16384 in 32.5 us, 4.3 TB/s (unpacking keeps the integer pipe as
-// busy as the memory), 1024 x 8192 in 4.2 us (latency); eight: 8192 x 8192 in 12.5.
+// vector: 16384 x 16384 in 32.7 us, 4.2 TB/s, 1024 x 8192 in 4.2 us (latency);
+// eight: 8192 x 8192 in 12.6.  No unit is full in the first (counters, shares of
+// the whole launch): instructions issue in 48 % of the clocks, the integer pipe
+// is busy 43 %, the shared memory's reads 54 %, DRAM 50 %.  14 warps an SM, three
+// to a scheduler, hide too little of each other's waits: for the integer pipe's
+// turn 17 % of a warp's time, for fixed latencies 13 %, at the barriers around
+// the vectors' staging 11 %, for data 6 %.
 //
 // A lane reads 16 bytes of codes of two rows: 32 values each, four groups of
 // eight.  The layout puts the eight values 32 j + 8 t of a block of 128 into
@@ -40,7 +45,8 @@ constexpr int THREADS = 256;          // of a packing block
 // Packing
 // ---------------------------------------------------------------------------
 
-// S lanes per row and group: the group's largest magnitude, its scale, its codes.
+// S lanes per row and group: the group's largest magnitude, its scale, its codes.  Single loads, w read twice: once per
+// set of weights (16384 x 16384 fp32 469 us).
 template <typename T, int S>
 __global__ void __launch_bounds__(THREADS) pack_kernel(const T *__restrict__ w, int O, int K, int Kp, int group,
                                                        int quantize, QParams q, const float *channel_scale,

@@ -933,8 +933,9 @@ def minw_group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, dx, dgamma=
 
 class TensorList:
     """Dense device tensors (fp32 or bf16, any lengths and offsets) as the host array that the calls on lists take;
-    made once for tensors that stay where they are.  limits: the clip of each weight tensor, or one for all (infinity
-    for none).  Holds its tensors."""
+    made once for tensors that stay where they are: it holds the tensors and the addresses they had when it was made.
+    Making one takes the host 0.7 us a tensor (232 us for 331; a call with two such lists 10 us), as does a call that is
+    given plain lists of tensors.  limits: the clip of each weight tensor, or one for all (infinity for none)."""
 
     def __init__(self, tensors, limits=float("inf")):
         self.tensors = list(tensors)
