@@ -651,6 +651,59 @@ MINW_API minw_status minw_sgd_clip_norm(const minw_tensor *weights, const minw_t
                                         float max_norm, float lr, float *norm, void *workspace,
                                         size_t workspace_bytes, void *stream);
 
+/* One matrix of a list (host struct): rows x cols values of type at data
+ * (device, aligned to its elements), row-major with ld >= cols elements
+ * between rows; elements past cols of a row are neither read nor written.
+ * rows or cols may be 0.  limit: a weight matrix's clip (minw_sgd_orthogonal),
+ * 1 for Algorithm 1's, infinity for none. */
+typedef struct {
+    void *data;
+    int64_t ld;
+    int32_t rows, cols;
+    int32_t type;
+    float limit;
+} minw_matrix;
+
+/* Orthogonalised matrices: out_t = NS(g_t), the result of `steps` (1 to 10, 5
+ * as a rule) Newton-Schulz steps on each matrix of the list by itself:
+ *   X = g / |g|_F,   then   X <- a X + b (X X^T) X + c (X X^T)^2 X
+ * with (a, b, c) = (3.4445, -4.7750, 2.0315) (tall matrices as their
+ * transposes): the singular vectors stay, after five steps singular values
+ * from about 1e-3 |g|_F up lie between 0.68 and 1.21.
+ * Products run on two-part fp16 operands (22 bits) with fp32 sums.  Against
+ * the formula in 64 bits, relative to the result's Frobenius norm: within
+ * 1e-4 for each three steps begun (five: 1.4e-5 at most as measured), and one
+ * rounding to nearest even for bf16 outputs.  The norm
+ * is right wherever its square is an fp64 number.  A matrix of zeros gives
+ * zeros; one with an infinity or a NaN gives NaN everywhere and changes no
+ * other's result.  The same bits on every call.
+ * grads, out: host arrays of count, read during the call; out has the
+ * gradients' rows and cols, any type and ld, and may be its gradient (same
+ * type and ld), but may overlap no other tensor.  workspace: device scratch of
+ * minw_orthogonal_workspace_bytes(grads, count) (rows and cols count; about 28
+ * bytes a value of a square matrix, 8 to 16 of a long one, its sides
+ * rounded up to 128), 16-byte aligned, contents meaningless before and after;
+ * calls that share one must not run concurrently.  count = 0 does nothing.
+ * Errors: MINW_EINVAL (count < 0, null lists, steps, negative sizes, null data
+ * with values, ld < cols, unknown type, lists of other sizes, misaligned data,
+ * missing, misaligned or short workspace), MINW_EUNSUPPORTED (a side past
+ * 2^22, the shorter one past 2^15, 2^26 tiles of 128 x 128 or more). */
+MINW_API size_t minw_orthogonal_workspace_bytes(const minw_matrix *grads, int32_t count);
+MINW_API minw_status minw_orthogonalize(const minw_matrix *grads, const minw_matrix *out, int32_t count, int32_t steps,
+                                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* The orthogonalised update of a list of weight matrices:
+ *   m = fmaf(momentum, m, g),   u = nesterov ? fmaf(momentum, m, g) : m
+ *   w = min(limit, max(-limit, fmaf(-lr s, NS(u), w))),  s = sqrt(max(1, rows / cols))
+ * in fp32 (weights fp32 or bf16, bf16 rounded once; momenta fp32), limit per
+ * weight matrix.  momenta NULL: u = g.  Where u has an infinity or a NaN,
+ * that matrix's weights and momenta stay as they are.  Weights, momenta and
+ * gradients may not overlap.  Errors as minw_orthogonalize; limit >= 0,
+ * momentum and lr finite. */
+MINW_API minw_status minw_sgd_orthogonal(const minw_matrix *weights, const minw_matrix *momenta, const minw_matrix *grads,
+                                         int32_t count, int32_t steps, float momentum, int32_t nesterov, float lr,
+                                         void *workspace, size_t workspace_bytes, void *stream);
+
 /* "w4" layout: weights [O][K] as 4-bit codes with one bf16 scale per row and
  * group of `group` consecutive values (32, 64, 128 or a larger multiple of
  * 128): w = (code - 8) scale, code in 0..15.  codes (16-byte aligned): rows

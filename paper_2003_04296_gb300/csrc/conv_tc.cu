@@ -2726,7 +2726,7 @@ extern "C" minw_status minw_get_last_device_error(void *stream) {
     // the other kernels' flags: all are read, so that each report clears all of them
     int any = flag;
     for (int (*take)() : {minw::take_first_error, minw::take_first_tc_error, minw::take_planes_tc_error,
-                          minw::take_wres_error, minw::take_wdense_error, minw::take_wgrad_error}) {
+                          minw::take_wres_error, minw::take_wdense_error, minw::take_wgrad_error, minw::take_orth_error}) {
         const int f = take();
         if (f < 0) return MINW_ECUDA;
         any |= f;

@@ -132,6 +132,7 @@ struct WgradArgs {
 size_t conv_wgrad_workspace_bytes(const WgradArgs &a);      // the partial sums
 minw_status launch_conv_wgrad(const WgradArgs &a, float *part, float lr, float two_alpha, float *W, cudaStream_t s);
 int take_wgrad_error();                                     // timeout flag (as take_first_error)
+int take_orth_error();                                      // orthogonal.cu's
 bool conv_tc_supported(const ConvArgs &a);
 // Workspace the tensor-core path needs to split K for this shape (0: it does not split).
 size_t conv_tc_workspace_bytes(const ConvArgs &a);

@@ -1,0 +1,987 @@
+// orthogonal.cu -- orthogonalised updates of lists of matrices: each matrix divided
+// by its norm and taken through Newton-Schulz products, which bring its singular
+// values to about 1.
+//
+// One step is X <- (a I + b A + c A^2) X with A = X X^T of the smaller side, m x m.
+// Every step is a polynomial in the first A times X, and polynomials in A commute
+// and are symmetric, so several steps (a stage) run on m x m matrices alone:
+//   Z = a I + b A + c A^2,   Q <- Z Q,   A <- (Z A) Z
+// and Q X comes once at the stage's end: for n >= m a third of the direct form's
+// operations, half of them on symmetric results whose other half is a mirror image.
+// What that costs is precision: an error e of A counts 11.9^steps e where the
+// singular values are small.  So every matrix is held as the sum of two fp16 numbers
+// (22 bits), a product takes three fp16 products, hi hi + hi lo + lo hi, and a stage has
+// three steps at most.  The tensor cores truncate their fp32 sums, so they add up hi hi over
+// 128 of K alone and fp32 registers the rest, to nearest.  Against the formula in 64 bits,
+// 1024 x 8192, a gradient of few strong directions (Frobenius): 1.3e-5, as near as plain fp32
+// products (1.5e-5); chunks of 256, 512 and all of K 2.4e-5, 3.2e-5 and 3.0e-5, of 64 7.5e-6
+// at 1.05 times the time; five steps in one stage 3e-3 to 9e-3.
+//
+// The scales are powers of two that the mathematics gives: a matrix of Frobenius norm
+// f in [1/2, 1) 2^e enters as X 2^(15 - e), so that nothing overflows and the smallest
+// part lost is 2^-40 of the norm; singular values stay below 1.2025 from then on,
+// A below 1.447, Z below 3.4446.
+//
+// Operands lie in the workspace as the tensor cores read them: blocks of 128 rows x 64
+// columns, 16 KB, swizzled in rows of 128 bytes.  Such a block is a K-major operand of
+// 128 rows or, column group by column group, an MN-major one, so X serves X X^T, X^T X, Q X and
+// X Q without a transposed copy, blocks travel as plain bulk copies, and no
+// matrix of a list needs a tensor map.
+//
+// A list goes through the kernels together: level k of all its matrices is one
+// launch.  Clusters split the sums of a tile where there are fewer tiles than SMs.
+#include <cooperative_groups.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "kernels.cuh"
+#include "values.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace minw {
+
+static __device__ int g_orth_error = 0;
+
+namespace orth {
+
+constexpr int T = 128;                       // rows and columns of a tile
+constexpr uint32_t BLOCK = 16384;            // bytes of 128 rows x 64 columns of fp16
+constexpr int THREADS = 256;
+constexpr int LOADER = 8, ISSUER = 9;        // a product's warps beside the eight that take its sums
+constexpr int CHUNK = 2;                     // blocks of 64 of K that the tensor cores sum by themselves
+constexpr int STAGES = 3;
+constexpr uint32_t STAGE = 4 * BLOCK;        // hi and lo of both operands, 64 of K
+constexpr int PITCH = 132;                   // floats between rows of a tile in shared memory
+constexpr int CAP = 224;                     // matrices of a launch
+constexpr int FEW = 16;                      // ... of a launch with short arguments
+constexpr float CA = 3.4445f, CB = -4.7750f, CC = 2.0315f;
+constexpr int SLOTS = 6;                     // m x m matrices: two for A, Z, Z A, two for Q
+
+struct Stat {
+    float scale1, scale2;                    // X = these two times the matrix
+    float gram;                              // 1 / mu^2, with mu the norm of X 2^-15
+    float apply;                             // 1 / mu
+    int finite;
+};
+
+struct Mat {
+    const void *g;
+    float *mom;
+    void *out;
+    uint8_t *x0, *x1, *small;                // hi blocks, then lo blocks; `small`: SLOTS of them
+    int64_t ldg, ldm, ldo;
+    int rows, cols;
+    int tri0, full0;                         // tiles of the matrices before: lower triangles of m x m, of X
+    float limit, rate;
+    uint8_t g_bf16, o_bf16, tall, gvec, mvec, ovec;
+
+    __host__ __device__ int rb() const { return (rows + T - 1) / T; }
+    __host__ __device__ int cb() const { return (cols + T - 1) / T; }                   // of 128 columns
+    __host__ __device__ int mb() const { return tall ? cb() : rb(); }
+    __host__ __device__ int side() const { return tall ? cols : rows; }
+};
+
+struct Sizes {
+    int count, tri, full;                    // matrices; tiles of their lower triangles, of X
+    const Mat *table;                        // in the workspace
+    Stat *stat;
+    double *part;                            // a sum of squares for each tile of X
+};
+
+template <int N>
+struct Table {
+    Mat m[N];
+};
+
+// The matrix of tile t: the last one that begins at or before it.
+template <bool TRI>
+__device__ __forceinline__ int find(const Mat *m, int count, int t) {
+    int lo = 0, hi = count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((TRI ? m[mid].tri0 : m[mid].full0) <= t) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Byte of (row, column) in a block.
+__device__ __forceinline__ uint32_t at(int r, int c) {
+    return (uint32_t)(r * 128 + ((((c >> 3) ^ r) & 7) << 4) + (c & 7) * 2);
+}
+
+// v as the sum of two fp16 numbers, eight values: one 16-byte store each.
+__device__ __forceinline__ void split8(const float *v, uint4 &hi, uint4 &lo) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const __half2 a = __floats2half2_rn(v[2 * k], v[2 * k + 1]);
+        const float2 f = __half22float2(a);
+        const __half2 b = __floats2half2_rn(v[2 * k] - f.x, v[2 * k + 1] - f.y);
+        h[k] = *reinterpret_cast<const uint32_t *>(&a);
+        l[k] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+__device__ __forceinline__ void join8(const uint4 &hi, const uint4 &lo, float *v) {
+    const uint32_t h[4] = {hi.x, hi.y, hi.z, hi.w}, l[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&h[k]));
+        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&l[k]));
+        v[2 * k] = a.x + b.x;
+        v[2 * k + 1] = a.y + b.y;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The matrix in: its norm, then its scaled blocks and the momentum's step
+// ---------------------------------------------------------------------------
+
+struct Step {
+    float mu;
+    int use, nesterov;                       // use: a momentum is given
+};
+
+template <typename V>
+__device__ __forceinline__ void load8(const V *p, int64_t at_, int left, bool vec, float *v) {
+    if (vec && left >= 8) {
+        Vec<V, 8> w;
+        w.load(p + at_);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = w.get(i);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            v[i] = 0.0f;
+            if (i < left) {
+                Vec<V, 1> w;
+                w.load(p + at_ + i);
+                v[i] = w.get(0);
+            }
+        }
+    }
+}
+
+// Eight values of row r from column c on: the momentum's step m = mu m + g and what is orthogonalised, u.  Zeros outside.
+__device__ __forceinline__ void value8(const Mat &m, const Step &s, int r, int c, float *u, float *mom) {
+    const int left = r < m.rows ? m.cols - c : 0;
+    if (m.g_bf16) load8(static_cast<const uint16_t *>(m.g), r * m.ldg + c, left, m.gvec, u);
+    else load8(static_cast<const float *>(m.g), r * m.ldg + c, left, m.gvec, u);
+    if (s.use) {
+        load8(m.mom, r * m.ldm + c, left, m.mvec, mom);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            mom[i] = fmaf(s.mu, mom[i], u[i]);
+            u[i] = s.nesterov ? fmaf(s.mu, mom[i], u[i]) : mom[i];
+        }
+    }
+}
+
+__device__ __forceinline__ double sum64(double v) {
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    return v;
+}
+
+// A block's tile: 128 rows x 128 columns, eight values a thread at a time.
+template <int N>
+__global__ void __launch_bounds__(THREADS) squares_kernel(const __grid_constant__ Table<N> table, Sizes l, Step s) {
+    pdl_trigger();
+    pdl_wait();
+    __shared__ double red[THREADS / 32];
+    // the list's matrices into the workspace, where the kernels after this one find them (a launch with 23 KB of
+    // arguments takes the host three times as long)
+    if (blockIdx.x == 0) {
+        static_assert(sizeof(Mat) % 8 == 0, "whole words");
+        const uint64_t *from = reinterpret_cast<const uint64_t *>(&table);
+        uint64_t *to = reinterpret_cast<uint64_t *>(const_cast<Mat *>(l.table));
+        for (int k = threadIdx.x; k < l.count * (int)(sizeof(Mat) / 8); k += THREADS) to[k] = from[k];
+    }
+    const Mat &m = table.m[find<false>(table.m, l.count, blockIdx.x)];
+    const int t = blockIdx.x - m.full0, r0 = t / m.cb() * T + (threadIdx.x >> 4), c = t % m.cb() * T + (threadIdx.x & 15) * 8;
+    float sum = 0.0f;
+    double d = 0.0;
+#pragma unroll 2
+    for (int k = 0; k < T; k += 16) {
+        float u[8], mom[8], q = 0.0f;
+        bool some = false;
+        value8(m, s, r0 + k, c, u, mom);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q = fmaf(u[i], u[i], q);
+            some = some || u[i] != 0.0f;
+        }
+        // squares that leave fp32's range (or may have lost bits to it) are added in fp64
+        if (q >= 1e-30f && q <= 1e35f) sum += q;
+        else if (some)
+#pragma unroll 1
+            for (int i = 0; i < 8; ++i) d = fma((double)u[i], (double)u[i], d);
+    }
+    d = sum64(d + (double)sum);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = d;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < THREADS / 32; ++k) d += red[k];
+        l.part[blockIdx.x] = d;
+    }
+}
+
+__global__ void __launch_bounds__(THREADS) enter_kernel(Sizes l, Step s, int lo_part) {
+    pdl_trigger();
+    pdl_wait();
+    __shared__ double red[THREADS / 32];
+    __shared__ Stat st;
+    const int which = find<false>(l.table, l.count, blockIdx.x);
+    const Mat m = l.table[which];
+    const int t = blockIdx.x - m.full0, tiles = m.rb() * m.cb();
+    double d = 0.0;
+    for (int k = threadIdx.x; k < tiles; k += THREADS) d += l.part[m.full0 + k];
+    d = sum64(d);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = d;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < THREADS / 32; ++k) d += red[k];
+        int e = 0;
+        const bool finite = d <= 1.7e308;
+        const double mu = finite && d > 0.0 ? frexp(sqrt(d), &e) : 1.0;        // the norm is mu 2^e
+        st.finite = finite;
+        // 2^(15 - e) in two factors, each an fp32 number for every e from -149 to 150
+        const int h = (15 - e) / 2;
+        st.scale1 = finite ? ldexpf(1.0f, h) : 0.0f;
+        st.scale2 = finite ? ldexpf(1.0f, 15 - e - h) : 0.0f;
+        st.apply = (float)(1.0 / mu);
+        st.gram = (float)(1.0 / (mu * mu));
+        if (t == 0) l.stat[which] = st;
+    }
+    __syncthreads();
+    const int rt = t / m.cb(), ct = t % m.cb(), c8 = (threadIdx.x & 15) * 8, c = ct * T + c8;
+    const int64_t blocks = (int64_t)m.rb() * m.cb() * 2;
+    uint8_t *b = m.x0 + ((int64_t)rt * m.cb() * 2 + ct * 2 + (c8 >> 6)) * BLOCK;
+#pragma unroll 2
+    for (int k = threadIdx.x >> 4; k < T; k += 16) {
+        float u[8], mom[8];
+        const int r = rt * T + k;
+        value8(m, s, r, c, u, mom);
+        if (s.use && st.finite && r < m.rows) {
+            float *p = m.mom + r * m.ldm + c;
+            if (m.mvec && m.cols - c >= 8) {
+                reinterpret_cast<float4 *>(p)[0] = make_float4(mom[0], mom[1], mom[2], mom[3]);
+                reinterpret_cast<float4 *>(p)[1] = make_float4(mom[4], mom[5], mom[6], mom[7]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c + i < m.cols) p[i] = mom[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = st.finite ? u[i] * st.scale1 * st.scale2 : 0.0f;
+        uint4 hi, lo;
+        split8(u, hi, lo);
+        *reinterpret_cast<uint4 *>(b + at(k, c8 & 63)) = hi;
+        if (lo_part) *reinterpret_cast<uint4 *>(b + blocks * BLOCK + at(k, c8 & 63)) = lo;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Products
+// ---------------------------------------------------------------------------
+
+enum Mode { GRAM, POLY, MUL, APPLY, LEAVE };
+
+struct Product {
+    int p, q, out;                           // slots of the factors and the result (LEAVE, APPLY: p = Q)
+    float factor;                            // of the sum, on its way to the result's scale
+};
+
+struct Level {
+    int mode, products, split;
+    Product pr[2];
+    int x1;                                  // GRAM, APPLY, LEAVE: X is the one of a later stage
+    int x_lo;                                // ... and has a lo part
+    float a, b;                              // POLY: a I + b (slot p) + factor sum, in the result's scale
+    int update;                              // LEAVE: weights are updated
+    float lr;
+    long long wait_cycles;
+};
+
+__device__ __forceinline__ uint32_t su32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(uint64_t *b, uint32_t n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;\n" ::"r"(su32(b)), "r"(n));
+}
+__device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 100000;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(su32(b)), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool bar_wait(uint64_t *b, uint32_t parity, long long limit) {
+    if (bar_try(b, parity)) return true;
+    const long long t0 = clock64();
+    while (!bar_try(b, parity)) {
+        if (clock64() - t0 > limit) {
+            atomicExch(&g_orth_error, 1);
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;\n" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory"); }
+
+// Blocks in shared memory.  K-major: rows of 64 K values, eight rows 1024 bytes on.  MN-major: pieces of 64 columns, 64
+// rows of K each (8 KB), eight rows of K 1024 bytes on.
+__device__ __forceinline__ uint64_t desc(uint32_t addr, bool mn) {
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(mn ? 8192u >> 4 : 1u) << 16) | ((uint64_t)(1024 >> 4) << 32) |
+           ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p, e;\n .reg .b32 r;\n setp.ne.b32 p, %4, 0;\n elect.sync r|e, 0xffffffff;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+                 "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+}
+__device__ __forceinline__ void mma_commit(uint64_t *bar) {
+    asm volatile("{\n .reg .pred e;\n .reg .b32 r;\n elect.sync r|e, 0xffffffff;\n"
+                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(su32(bar))
+                 : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const uint8_t *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(su32(bar))
+                 : "memory");
+}
+
+// An operand of a tile: hi blocks at `p`, lo blocks `lo` bytes on (0: none), `wide` blocks to a row of blocks.
+struct Side {
+    const uint8_t *p;
+    int64_t lo;
+    int wide, tile;
+    bool mn;
+
+    __device__ __forceinline__ void load(uint32_t dst, int kb, uint64_t *bar) const {
+        if (!mn) {
+            const uint8_t *s = p + ((int64_t)tile * wide + kb) * BLOCK;
+            bulk_load(dst, s, BLOCK, bar);
+            if (lo) bulk_load(dst + BLOCK, s + lo, BLOCK, bar);
+        } else {
+            const uint8_t *s = p + ((int64_t)(kb >> 1) * wide + 2 * tile) * BLOCK + (kb & 1) * (BLOCK / 2);
+            bulk_load(dst, s, BLOCK / 2, bar);
+            bulk_load(dst + BLOCK / 2, s + BLOCK, BLOCK / 2, bar);
+            if (lo) {
+                bulk_load(dst + BLOCK, s + lo, BLOCK / 2, bar);
+                bulk_load(dst + BLOCK + BLOCK / 2, s + lo + BLOCK, BLOCK / 2, bar);
+            }
+        }
+    }
+    __device__ __forceinline__ uint32_t bytes() const { return lo ? 2 * BLOCK : BLOCK; }
+};
+
+struct Smem {
+    uint64_t full[STAGES], empty[STAGES], sums[2], taken[2];
+    uint32_t tmem;
+};
+
+__device__ __forceinline__ void load32(uint32_t addr, float *v) {
+    uint32_t w[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "
+        "%13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, "
+        "[%32];\n"
+        : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]),
+          "=r"(w[8]), "=r"(w[9]), "=r"(w[10]), "=r"(w[11]), "=r"(w[12]), "=r"(w[13]), "=r"(w[14]),
+          "=r"(w[15]), "=r"(w[16]), "=r"(w[17]), "=r"(w[18]), "=r"(w[19]), "=r"(w[20]), "=r"(w[21]),
+          "=r"(w[22]), "=r"(w[23]), "=r"(w[24]), "=r"(w[25]), "=r"(w[26]), "=r"(w[27]), "=r"(w[28]),
+          "=r"(w[29]), "=r"(w[30]), "=r"(w[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(w[k]);
+}
+
+__global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const __grid_constant__ Level v) {
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *ring = smem_raw + ((1024u - (su32(smem_raw) & 1023u)) & 1023u);
+    float *acc = reinterpret_cast<float *>(ring);               // the tile, once the ring is done with
+    __shared__ Smem sm;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            bar_init(&sm.full[s], 1);
+            bar_init(&sm.empty[s], 1);
+        }
+        for (int k = 0; k < 2; ++k) {
+            bar_init(&sm.sums[k], 1);
+            bar_init(&sm.taken[k], THREADS / 32);
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    }
+    if (warp == ISSUER) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(su32(&sm.tmem)));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n");
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sm.tmem;
+    pdl_trigger();
+
+    // what this block computes: matrix, product, tile (i, j), share of K
+    const int split = v.split, rank = blockIdx.x % split, tri = v.mode <= MUL;
+    int t = blockIdx.x / split, which = 0;
+    if (tri) {
+        which = t / l.tri;
+        t -= which * l.tri;
+    }
+    pdl_wait();
+    const int index = tri ? find<true>(l.table, l.count, t) : find<false>(l.table, l.count, t);
+    const Mat m = l.table[index];
+    const Product pr = v.pr[which];
+    const int mb = m.mb();
+    const int64_t small_blocks = (int64_t)mb * mb * 2 * BLOCK, slot = 2 * small_blocks;
+    const int64_t x_blocks = (int64_t)m.rb() * m.cb() * 2 * BLOCK;
+    uint8_t *x = v.x1 ? m.x1 : m.x0;
+    int i, j;
+    if (tri) {
+        t -= m.tri0;
+        i = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+        while ((i + 1) * (i + 2) / 2 <= t) ++i;
+        while (i * (i + 1) / 2 > t) --i;
+        j = t - i * (i + 1) / 2;
+    } else {
+        t -= m.full0;
+        i = t / m.cb();
+        j = t % m.cb();
+    }
+    const Side sx{x, v.x_lo ? x_blocks : 0, 2 * m.cb(), 0, false};
+    Side a, b;
+    int kbs;                                                    // blocks of 64 along K
+    if (v.mode == GRAM) {
+        a = b = sx;
+        a.tile = i;
+        b.tile = j;
+        a.mn = b.mn = m.tall;
+        kbs = 2 * (m.tall ? m.rb() : m.cb());
+    } else {
+        const Side sp{m.small + pr.p * slot, small_blocks, 2 * mb, i, false};
+        const Side sq{m.small + pr.q * slot, small_blocks, 2 * mb, j, false};
+        kbs = 2 * mb;
+        a = sp;
+        b = sq;
+        if (!tri) {
+            if (m.tall) {                                       // X Q
+                a = sx;
+                a.tile = i;
+                b = sp;
+                b.tile = j;
+            } else {                                            // Q X
+                b = sx;
+                b.tile = j;
+                b.mn = true;
+            }
+        }
+    }
+    const int kb0 = rank * kbs / split, kb1 = (rank + 1) * kbs / split;
+    const bool same = a.p == b.p && a.tile == b.tile && a.mn == b.mn;
+    const uint32_t bytes = a.bytes() + (same ? 0 : b.bytes());
+    bool ok = true;
+    if (warp == LOADER) {
+        if (lane == 0) {
+            int s = 0, lap = 0, g = 0;
+            for (int kb = kb0; kb < kb1; ++kb, ++g) {
+                if (lap > 0 && !bar_wait(&sm.empty[s], (lap - 1) & 1, v.wait_cycles)) break;
+                const uint32_t dst = su32(ring) + s * STAGE;
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(su32(&sm.full[s])),
+                             "r"(bytes)
+                             : "memory");
+                a.load(dst, kb, &sm.full[s]);
+                if (!same) b.load(dst + 2 * BLOCK, kb, &sm.full[s]);
+                if (++s == STAGES) { s = 0; ++lap; }
+            }
+            // every load has landed before the ring is used again
+            for (int k = g > STAGES ? g - STAGES : 0; k < g; ++k)
+                if (!bar_wait(&sm.full[k % STAGES], (k / STAGES) & 1, v.wait_cycles)) break;
+        }
+        __syncwarp();
+    } else if (warp == ISSUER) {
+        // D fp32, A and B fp16; bits 15 and 16: MN-major
+        const uint32_t idesc = (1u << 4) | ((a.mn ? 1u : 0u) << 15) | ((b.mn ? 1u : 0u) << 16) | ((uint32_t)(T >> 3) << 17) | (8u << 24);
+        const uint32_t ka = a.mn ? 2048 >> 4 : 32 >> 4, kbk = b.mn ? 2048 >> 4 : 32 >> 4;      // 16 of K
+        int s = 0, chunk = 0;
+        uint32_t phase = 0u, rest = 0u;
+        for (int at_ = kb0; at_ < kb1 && ok; at_ += CHUNK, ++chunk) {
+            const int end = min(at_ + CHUNK, kb1);
+            if (chunk >= 2 && !__all_sync(0xffffffffu, bar_wait(&sm.taken[chunk & 1], (chunk / 2 - 1) & 1, v.wait_cycles)))
+                ok = false;
+            fence_after();
+            const uint32_t d = tmem + T * (chunk & 1), small = tmem + 2 * T;
+            uint32_t on = 0u;
+            for (int kb = at_; kb < end && ok; ++kb) {
+                if (!__all_sync(0xffffffffu, bar_wait(&sm.full[s], phase, v.wait_cycles))) { ok = false; break; }
+                fence_after();
+                const uint32_t base = su32(ring) + s * STAGE;
+                const uint64_t ad = desc(base, a.mn), bd = desc(same ? base : base + 2 * BLOCK, b.mn);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_f16(d, ad + k * ka, bd + k * kbk, idesc, k > 0 ? 1u : on);
+                on = 1u;
+                if (b.lo) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_f16(small, ad + k * ka, bd + (BLOCK >> 4) + k * kbk, idesc, k > 0 ? 1u : rest);
+                    rest = 1u;
+                }
+                if (a.lo) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_f16(small, ad + (BLOCK >> 4) + k * ka, bd + k * kbk, idesc, k > 0 ? 1u : rest);
+                    rest = 1u;
+                }
+                mma_commit(&sm.empty[s]);
+                if (++s == STAGES) { s = 0; phase ^= 1u; }
+            }
+            if (ok) mma_commit(&sm.sums[chunk & 1]);
+        }
+    }
+    __syncwarp();
+    // The sums from tensor memory into registers, a chunk at a time; zero where this share of K is empty.
+    float sum[64];
+    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 64);
+    if (warp < THREADS / 32) {
+#pragma unroll
+        for (int k = 0; k < 64; ++k) sum[k] = 0.0f;
+        int chunk = 0;
+        for (int at_ = kb0; at_ < kb1 && ok; at_ += CHUNK, ++chunk) {
+            ok = __all_sync(0xffffffffu, bar_wait(&sm.sums[chunk & 1], (chunk >> 1) & 1, v.wait_cycles));
+            fence_after();
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                float w[32];
+                load32(mine + T * (chunk & 1) + c, w);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) sum[c + k] += w[k];
+            }
+            fence_before();
+            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(su32(&sm.taken[chunk & 1])) : "memory");
+        }
+        if (kb1 > kb0 && (a.lo || b.lo)) {
+#pragma unroll
+            for (int c = 0; c < 64; c += 32) {
+                float w[32];
+                load32(mine + 2 * T + c, w);
+#pragma unroll
+                for (int k = 0; k < 32; ++k) sum[c + k] += w[k];
+            }
+        }
+    }
+    ok = __syncthreads_and(ok);                                 // and the last loads have landed
+    if (warp < THREADS / 32) {
+        float *d = acc + ((warp & 3) * 32 + lane) * PITCH + (warp >> 2) * 64;
+#pragma unroll
+        for (int k = 0; k < 64; k += 4) *reinterpret_cast<float4 *>(d + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    if (split > 1) cluster.sync();
+    else __syncthreads();
+
+    // this block's rows of the tile, eight columns a thread at a time
+    const int rows = T / split, r0 = rank * rows;
+    const Stat st = v.mode == GRAM || v.mode == LEAVE || v.mode == APPLY ? l.stat[index] : Stat{};
+    float factor = pr.factor;
+    if (v.mode == GRAM && !v.x1) factor *= st.gram;
+    if (v.mode >= APPLY && !v.x1) factor *= st.apply;
+    uint8_t *out = v.mode == APPLY ? m.x1 : m.small + pr.out * slot;
+    const int wide = v.mode == APPLY ? 2 * m.cb() : 2 * mb;
+    const int64_t lo = v.mode == APPLY ? x_blocks : small_blocks;
+    const int c = (threadIdx.x & 15) * 8;
+    for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32; r += 16) {
+        float z[8];
+        float *mine = acc + r * PITCH + c;
+#pragma unroll
+        for (int k = 0; k < 8; k += 4) {
+            float4 f = *reinterpret_cast<const float4 *>(mine + k);
+            if (split > 1) {
+                float4 o[8];                                    // all on their way at once
+#pragma unroll
+                for (int p = 0; p < 8; ++p)
+                    if (p < split) o[p] = *reinterpret_cast<const float4 *>(cluster.map_shared_rank(mine + k, p));
+                f = o[0];
+#pragma unroll
+                for (int p = 1; p < 8; ++p)
+                    if (p < split) { f.x += o[p].x; f.y += o[p].y; f.z += o[p].z; f.w += o[p].w; }
+            }
+            z[k] = f.x; z[k + 1] = f.y; z[k + 2] = f.z; z[k + 3] = f.w;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) z[k] *= factor;
+        const uint32_t in_block = at(r, c & 63);
+        if (v.mode == POLY) {
+            const uint8_t *s = m.small + pr.p * slot + ((int64_t)i * wide + 2 * j + (c >> 6)) * BLOCK + in_block;
+            float f[8];
+            join8(*reinterpret_cast<const uint4 *>(s), *reinterpret_cast<const uint4 *>(s + small_blocks), f);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                z[k] = fmaf(v.b, f[k], z[k]);
+                if (i * T + r == j * T + c + k) z[k] += v.a;
+            }
+        }
+        if (v.mode != LEAVE) {
+            if (ok) {
+                uint4 h, w;
+                split8(z, h, w);
+                uint8_t *d = out + ((int64_t)i * wide + 2 * j + (c >> 6)) * BLOCK + in_block;
+                *reinterpret_cast<uint4 *>(d) = h;
+                *reinterpret_cast<uint4 *>(d + lo) = w;
+            }
+            if (tri && i != j) {
+                *reinterpret_cast<float4 *>(mine) = make_float4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<float4 *>(mine + 4) = make_float4(z[4], z[5], z[6], z[7]);
+            }
+        } else if (ok && i * T + r < m.rows) {
+            const int64_t e = (int64_t)(i * T + r) * m.ldo + j * T + c;
+            const int left = m.cols - j * T - c;
+            const bool vec = m.ovec && left >= 8;
+            if (v.update) {
+                if (!st.finite) continue;
+                float w[8];
+                if (m.o_bf16) load8(static_cast<const uint16_t *>(m.out), e, left, m.ovec, w);
+                else load8(static_cast<const float *>(m.out), e, left, m.ovec, w);
+                const float rate = -v.lr * m.rate;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float n = fmaf(rate, z[k], w[k]);
+                    z[k] = n > m.limit ? m.limit : n < -m.limit ? -m.limit : n;
+                }
+            } else if (!st.finite) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) z[k] = __int_as_float(0x7fc00000);
+            }
+            if (m.o_bf16) {
+                uint16_t *o = static_cast<uint16_t *>(m.out) + e;
+                if (vec) {
+                    Vec<uint16_t, 8> w;
+                    w.set(z);
+                    w.store(o);
+                } else {
+                    for (int k = 0; k < 8; ++k)
+                        if (k < left) o[k] = __bfloat16_as_ushort(__float2bfloat16_rn(z[k]));
+                }
+            } else {
+                float *o = static_cast<float *>(m.out) + e;
+                if (vec) {
+                    Vec<float, 8> w;
+                    w.set(z);
+                    w.store(o);
+                } else {
+                    for (int k = 0; k < 8; ++k)
+                        if (k < left) o[k] = z[k];
+                }
+            }
+        }
+    }
+    // the mirror image: eight rows of a column are eight columns of a row
+    if (tri && i != j) {
+        __syncthreads();
+        const int eights = rows / 8;
+        for (int e = threadIdx.x; e < eights * T && ok; e += THREADS + 64) {
+            const int col = e % T, r = r0 + e / T * 8;
+            float z[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] = acc[(r + k) * PITCH + col];
+            uint4 h, w;
+            split8(z, h, w);
+            uint8_t *d = out + ((int64_t)j * wide + 2 * i + (r >> 6)) * BLOCK + at(col, r & 63);
+            *reinterpret_cast<uint4 *>(d) = h;
+            *reinterpret_cast<uint4 *>(d + lo) = w;
+        }
+    }
+    fence_before();
+    if (split > 1) cluster.sync();                              // others read this block's sums
+    else __syncthreads();
+    if (warp == ISSUER) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+using namespace minw_host;
+
+constexpr int MAX_STEPS = 10;
+
+static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Workspace bytes of one matrix: X twice, the m x m matrices.
+static int64_t matrix_bytes(int rows, int cols) {
+    const int64_t rb = (rows + T - 1) / T, cb = (cols + T - 1) / T, mb = rows > cols ? cb : rb;
+    return (2 * rb * cb + SLOTS * mb * mb) * 4 * (int64_t)BLOCK;
+}
+
+static int64_t tiles_of(int rows, int cols) { return (int64_t)((rows + T - 1) / T) * ((cols + T - 1) / T); }
+
+// Fills a launch's list from matrix k on; returns the next launch's first, and the workspace that it takes.  base null: the
+// sizes alone.
+static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int k, int count,
+                uint8_t *base, int64_t *need) {
+    l.count = l.tri = l.full = 0;
+    l.table = reinterpret_cast<const Mat *>(base);
+    int64_t used = up(CAP * sizeof(Mat), 256);
+    l.stat = reinterpret_cast<Stat *>(base + used);
+    used = up(used + CAP * sizeof(Stat), 256);
+    int64_t tiles = 0;
+    for (int e = k, n = 0; e < count && n < CAP; ++e) {         // the sums of squares lie before the matrices
+        if (g[e].rows == 0 || g[e].cols == 0) continue;
+        ++n;
+        tiles += tiles_of(g[e].rows, g[e].cols);
+    }
+    l.part = reinterpret_cast<double *>(base + used);
+    used = up(used + tiles * (int64_t)sizeof(double), 1024);
+    for (; k < count && l.count < CAP; ++k) {
+        if (g[k].rows == 0 || g[k].cols == 0) continue;
+        Mat &m = table[l.count++];
+        m = Mat{};
+        m.rows = g[k].rows;
+        m.cols = g[k].cols;
+        m.tall = m.rows > m.cols;
+        m.g = g[k].data;
+        m.ldg = g[k].ld;
+        m.g_bf16 = g[k].type == MINW_BF16;
+        m.gvec = reinterpret_cast<uintptr_t>(m.g) % 16 == 0 && m.ldg % (m.g_bf16 ? 8 : 4) == 0;
+        if (mom) {
+            m.mom = static_cast<float *>(mom[k].data);
+            m.ldm = mom[k].ld;
+            m.mvec = reinterpret_cast<uintptr_t>(m.mom) % 16 == 0 && m.ldm % 4 == 0;
+        }
+        if (out) {
+            m.out = out[k].data;
+            m.ldo = out[k].ld;
+            m.o_bf16 = out[k].type == MINW_BF16;
+            m.ovec = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 && m.ldo % (m.o_bf16 ? 8 : 4) == 0;
+            m.limit = out[k].limit;
+            m.rate = m.tall ? sqrtf((float)m.rows / (float)m.cols) : 1.0f;
+        }
+        m.tri0 = l.tri;
+        m.full0 = l.full;
+        const int mb = m.mb();
+        l.tri += mb * (mb + 1) / 2;
+        l.full += m.rb() * m.cb();
+        const int64_t x = (int64_t)m.rb() * m.cb() * 4 * BLOCK;
+        m.x0 = base + used;
+        m.x1 = m.x0 + x;
+        m.small = m.x1 + x;
+        used += matrix_bytes(m.rows, m.cols);
+    }
+    *need = used;
+    return k;
+}
+
+static minw_status check(const minw_matrix *g, const minw_matrix *o, int count, bool floats) {
+    for (int k = 0; k < count; ++k) {
+        const minw_matrix &m = o ? o[k] : g[k];
+        if (m.type != MINW_F32 && (m.type != MINW_BF16 || floats)) return MINW_EINVAL;
+        if (m.rows < 0 || m.cols < 0 || m.rows != g[k].rows || m.cols != g[k].cols || m.ld < m.cols) return MINW_EINVAL;
+        if (m.rows > 0 && m.cols > 0 && !m.data) return MINW_EINVAL;
+        if (reinterpret_cast<uintptr_t>(m.data) % (m.type == MINW_BF16 ? 2 : 4) != 0) return MINW_EINVAL;
+    }
+    return MINW_OK;
+}
+
+// Tiles of a launch stay within 32 bits, a side within what an index of a tile's row of blocks takes.
+static bool sizes_fit(const minw_matrix *g, int count) {
+    int64_t tiles = 0;
+    for (int k = 0; k < count; ++k) {
+        if (g[k].rows > (1 << 22) || g[k].cols > (1 << 22) || std::min(g[k].rows, g[k].cols) > (1 << 15)) return false;
+        tiles += tiles_of(g[k].rows, g[k].cols);
+    }
+    return tiles < (1 << 26);
+}
+
+static cudaError_t launch(const Sizes &l, Level v, int64_t tiles, cudaStream_t s) {
+    const int sms = num_sms() > 0 ? num_sms() : 152;
+    // clusters split K where the tiles leave SMs idle
+    v.split = tiles * 8 <= sms ? 8 : tiles * 4 <= sms ? 4 : tiles * 2 <= sms ? 2 : 1;
+    v.wait_cycles = (long long)plan_options().wait_cycles;
+    const int smem = STAGES * (int)STAGE + 1024;
+    if (!allow_shared(reinterpret_cast<const void *>(product_kernel), smem)) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * v.split));
+    cfg.blockDim = dim3(THREADS + 64);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)v.split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    max_shared_carveout(reinterpret_cast<const void *>(product_kernel));
+    return cudaLaunchKernelEx(&cfg, product_kernel, l, v);
+}
+
+// All steps of one list.
+static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &step, int steps, bool x_lo, bool update, float lr,
+                         cudaStream_t s) {
+    const dim3 tiles((unsigned)l.full);
+    cudaError_t e0;
+    if (l.count <= FEW) {
+        Table<FEW> few;
+        std::copy(table.m, table.m + l.count, few.m);
+        e0 = launch_pdl_stream(false, squares_kernel<FEW>, tiles, dim3(THREADS), 0, s, few, l, step);
+    } else {
+        e0 = launch_pdl_stream(false, squares_kernel<CAP>, tiles, dim3(THREADS), 0, s, table, l, step);
+    }
+    if (e0 != cudaSuccess) return launch_failed();
+    if (launch_pdl_stream(false, enter_kernel, tiles, dim3(THREADS), 0, s, l, step, x_lo ? 1 : 0) !=
+        cudaSuccess)
+        return launch_failed();
+    // powers of two at which the m x m matrices are held: A, Z A below 1.447, Z below 3.4446, Q after k steps below 3.4446^k
+    const int SA = 15, SZ = 14;
+    static const int SQ[4] = {0, 14, 12, 10};
+    auto two = [](int e) { return ldexpf(1.0f, e); };
+    const int stages = (steps + 2) / 3;
+    for (int st = 0, left = steps; st < stages; ++st) {
+        const int n = (left + stages - st - 1) / (stages - st);                       // 3 + 2 of five
+        left -= n;
+        const bool last = st + 1 == stages;
+        int A = 0, Q = -1;
+        Level v{};
+        v.x1 = st > 0;
+        v.x_lo = st > 0 || x_lo;
+        v.mode = GRAM;
+        v.products = 1;
+        v.pr[0] = {0, 0, A, two(SA - 30)};
+        if (launch(l, v, l.tri, s) != cudaSuccess) return launch_failed();
+        for (int k = 1; k <= n; ++k) {
+            const int Z = k == 1 ? 4 : 2;                                             // the first Z is Q
+            Level p{};
+            p.mode = POLY;
+            p.products = 1;
+            p.pr[0] = {A, A, Z, CC * two(SZ - 2 * SA)};
+            p.a = CA * two(SZ);
+            p.b = CB * two(SZ - SA);
+            if (launch(l, p, l.tri, s) != cudaSuccess) return launch_failed();
+            Level w{};
+            w.mode = MUL;
+            if (k < n) w.pr[w.products++] = {Z, A, 3, two(-SZ)};                      // Z A
+            if (k > 1) w.pr[w.products++] = {Z, Q, Q ^ 1, two(SQ[k] - SZ - SQ[k - 1])};
+            Q = k == 1 ? 4 : Q ^ 1;
+            if (w.products > 0 && launch(l, w, (int64_t)l.tri * w.products, s) != cudaSuccess) return launch_failed();
+            if (k < n) {
+                w.products = 1;
+                w.pr[0] = {3, Z, A ^ 1, two(-SZ)};
+                if (launch(l, w, l.tri, s) != cudaSuccess) return launch_failed();
+                A ^= 1;
+            }
+        }
+        Level e{};
+        e.mode = last ? LEAVE : APPLY;
+        e.products = 1;
+        e.x1 = st > 0;
+        e.x_lo = st > 0 || x_lo;
+        e.update = update;
+        e.lr = lr;
+        e.pr[0] = {Q, Q, 0, two((last ? 0 : 15) - SQ[n] - 15)};
+        if (launch(l, e, l.full, s) != cudaSuccess) return launch_failed();
+    }
+    return launch_status();
+}
+
+static minw_status run(const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int count, int steps,
+                       const Step &step, bool update, float lr, uint8_t *ws, cudaStream_t s) {
+    bool x_lo = step.use != 0;                                  // bf16 gradients are fp16 numbers but for the smallest
+    for (int k = 0; k < count; ++k) x_lo = x_lo || g[k].type == MINW_F32;
+    Table<CAP> table;
+    Sizes l;
+    for (int k = 0; k < count;) {
+        int64_t need;
+        k = fill(table.m, l, g, mom, out, k, count, ws, &need);
+        if (l.count == 0) break;
+        const minw_status st = chain(table, l, step, steps, x_lo, update, lr, s);
+        if (st != MINW_OK) return st;
+    }
+    return MINW_OK;
+}
+
+}  // namespace orth
+
+int take_orth_error() {
+    int flag = 0;
+    if (cudaMemcpyFromSymbol(&flag, g_orth_error, sizeof(int)) != cudaSuccess) return -1;
+    if (flag) {
+        const int zero = 0;
+        if (cudaMemcpyToSymbol(g_orth_error, &zero, sizeof(int)) != cudaSuccess) return -1;
+    }
+    return flag ? 1 : 0;
+}
+
+}  // namespace minw
+
+using namespace minw;
+using namespace minw_host;
+
+extern "C" {
+
+size_t minw_orthogonal_workspace_bytes(const minw_matrix *grads, int32_t count) {
+    if (count < 0 || (count > 0 && !grads) || orth::check(grads, nullptr, count, false) != MINW_OK ||
+        !orth::sizes_fit(grads, count))
+        return 0;
+    orth::Table<orth::CAP> table;
+    orth::Sizes l;
+    int64_t most = 16;
+    for (int k = 0; k < count;) {
+        int64_t need;
+        k = orth::fill(table.m, l, grads, nullptr, nullptr, k, count, nullptr, &need);
+        most = std::max(most, need);
+    }
+    return (size_t)most;
+}
+
+static minw_status orthogonal(const minw_matrix *grads, const minw_matrix *mom, const minw_matrix *out, int32_t count,
+                              int32_t steps, const orth::Step &step, bool update, float lr, void *ws, size_t bytes,
+                              void *stream) {
+    if (count < 0 || (count > 0 && (!grads || !out)) || steps < 1 || steps > orth::MAX_STEPS) return MINW_EINVAL;
+    if (orth::check(grads, nullptr, count, false) != MINW_OK || orth::check(grads, out, count, false) != MINW_OK ||
+        (mom && orth::check(grads, mom, count, true) != MINW_OK))
+        return MINW_EINVAL;
+    for (int k = 0; k < count; ++k) {
+        if (update && !(out[k].limit >= 0.0f)) return MINW_EINVAL;
+        if (grads[k].rows == 0 || grads[k].cols == 0) continue;
+        // only an orthogonalised matrix may be its gradient
+        const bool same = out[k].data == grads[k].data;
+        if (same && (update || out[k].type != grads[k].type || out[k].ld != grads[k].ld)) return MINW_EINVAL;
+        if (mom && (mom[k].data == grads[k].data || mom[k].data == out[k].data)) return MINW_EINVAL;
+    }
+    if (!orth::sizes_fit(grads, count)) return MINW_EUNSUPPORTED;
+    bool some = false;
+    for (int k = 0; k < count; ++k) some = some || (grads[k].rows > 0 && grads[k].cols > 0);
+    if (!some) return MINW_OK;
+    if (!ws || !aligned16(ws) || bytes < minw_orthogonal_workspace_bytes(grads, count)) return MINW_EINVAL;
+    return orth::run(grads, mom, out, count, steps, step, update, lr, static_cast<uint8_t *>(ws), (cudaStream_t)stream);
+}
+
+minw_status minw_orthogonalize(const minw_matrix *grads, const minw_matrix *out, int32_t count, int32_t steps,
+                               void *workspace, size_t workspace_bytes, void *stream) {
+    return orthogonal(grads, nullptr, out, count, steps, orth::Step{0.0f, 0, 0}, false, 0.0f, workspace, workspace_bytes,
+                      stream);
+}
+
+minw_status minw_sgd_orthogonal(const minw_matrix *weights, const minw_matrix *momenta, const minw_matrix *grads,
+                                int32_t count, int32_t steps, float momentum, int32_t nesterov, float lr, void *workspace,
+                                size_t workspace_bytes, void *stream) {
+    if (!isfinite(lr) || !isfinite(momentum) || (count > 0 && !weights)) return MINW_EINVAL;
+    return orthogonal(grads, momenta, weights, count, steps, orth::Step{momentum, momenta ? 1 : 0, nesterov ? 1 : 0}, true,
+                      lr, workspace, workspace_bytes, stream);
+}
+
+}  // extern "C"

@@ -64,6 +64,11 @@ class Tensor(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("type", ctypes.c_int32), ("limit", ctypes.c_float)]
 
 
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("limit", ctypes.c_float)]
+
+
 class LayerDesc(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("C", ctypes.c_int32), ("H", ctypes.c_int32),
                 ("W", ctypes.c_int32), ("O", ctypes.c_int32), ("kh", ctypes.c_int32),
@@ -184,6 +189,9 @@ SIGNATURES = {
     "minw_grad_norm": (ctypes.c_int, [_P, _I32, _P, _P, ctypes.c_size_t, _P]),
     "minw_grad_clip": (ctypes.c_int, [_P, _P, _I32, _F, _P, _P, ctypes.c_size_t, _P]),
     "minw_sgd_clip_norm": (ctypes.c_int, [_P, _P, _I32, _F, _F, _P, _P, ctypes.c_size_t, _P]),
+    "minw_orthogonal_workspace_bytes": (ctypes.c_size_t, [_P, _I32]),
+    "minw_orthogonalize": (ctypes.c_int, [_P, _P, _I32, _I32, _P, ctypes.c_size_t, _P]),
+    "minw_sgd_orthogonal": (ctypes.c_int, [_P, _P, _P, _I32, _I32, _F, _I32, _F, _P, ctypes.c_size_t, _P]),
     "minw_pack_w4": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _QP, _P, _P, _P, _P]),
     "minw_w4_matvec": (ctypes.c_int, [_P, _I32, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _I32, _P, _I32, _I64,
                                       _P]),
@@ -931,6 +939,14 @@ def minw_group_norm_backward(x, dy, gamma, beta, mean, rstd, groups, dx, dgamma=
            "minw_group_norm_backward")
 
 
+def _limits(limits, n):
+    one = isinstance(limits, (int, float)) or getattr(limits, "ndim", None) == 0          # numpy's and torch's too
+    limits = [float(limits)] * n if one else [float(v) for v in limits]
+    if len(limits) != n:
+        raise ValueError("a limit per tensor expected")
+    return limits
+
+
 class TensorList:
     """Dense device tensors (fp32 or bf16, any lengths and offsets) as the host array that the calls on lists take;
     made once for tensors that stay where they are: it holds the tensors and the addresses they had when it was made.
@@ -939,12 +955,8 @@ class TensorList:
 
     def __init__(self, tensors, limits=float("inf")):
         self.tensors = list(tensors)
-        n = len(self.tensors)
-        one = isinstance(limits, (int, float)) or getattr(limits, "ndim", None) == 0          # numpy's and torch's too
-        limits = [float(limits)] * n if one else [float(v) for v in limits]
-        if len(limits) != n:
-            raise ValueError("a limit per tensor expected")
-        self.array = (Tensor * max(1, n))()
+        limits = _limits(limits, len(self.tensors))
+        self.array = (Tensor * max(1, len(self.tensors)))()
         for e, t, limit in zip(self.array, self.tensors, limits):
             p = _ptr(t)
             e.data, e.n, e.type, e.limit = p.value, t.numel(), _value_type(t), limit
@@ -990,6 +1002,63 @@ def minw_sgd_clip_norm(weights, grads, max_norm, lr, norm, workspace, stream=Non
     ws, ws_bytes = _scratch(workspace)
     _check(lib().minw_sgd_clip_norm(w.array, g.array, len(g), float(max_norm), float(lr), _f32(norm, 1, "norm"), ws,
                                     ws_bytes, _stream(stream)), "minw_sgd_clip_norm")
+
+
+class MatrixList:
+    """Device matrices [rows][cols] (fp32 or bf16; rows may be wider apart) as the host array that the calls on
+    matrices take; a tensor of more dimensions counts as [shape[0]][the rest] and has to be dense.  Made once for tensors that
+    stay where they are, as a TensorList.  limits: the clip of each weight matrix, or one for all (infinity for none)."""
+
+    def __init__(self, tensors, limits=float("inf")):
+        self.tensors = list(tensors)
+        limits = _limits(limits, len(self.tensors))
+        self.array = (Matrix * max(1, len(self.tensors)))()
+        for e, t, limit in zip(self.array, self.tensors, limits):
+            if t.ndim < 2:
+                raise ValueError("matrices expected")
+            if t.ndim > 2 or t.numel() == 0:
+                p, (e.rows, e.cols) = _ptr(t), (t.shape[0], math.prod(t.shape[1:]))
+                e.data, e.ld = p.value, e.cols
+            else:
+                e.rows, e.cols = t.shape
+                e.data, e.ld = _rows(t)
+            e.type, e.limit = _value_type(t), limit
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _matrices(tensors):
+    return tensors if isinstance(tensors, MatrixList) else MatrixList(tensors)
+
+
+def minw_orthogonal_workspace_bytes(grads):
+    """Workspace bytes of the calls on matrices of these sizes (a MatrixList, or tensors)."""
+    g = _matrices(grads)
+    return lib().minw_orthogonal_workspace_bytes(g.array, len(g))
+
+
+def minw_orthogonalize(grads, out, workspace, steps=5, stream=None):
+    """out = each matrix of grads orthogonalised by `steps` Newton-Schulz steps (out may be grads)."""
+    g, o = _matrices(grads), _matrices(out)
+    if len(g) != len(o):
+        raise ValueError("lists of the same length expected")
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_orthogonalize(g.array, o.array, len(g), int(steps), ws, ws_bytes, _stream(stream)),
+           "minw_orthogonalize")
+
+
+def minw_sgd_orthogonal(weights, momenta, grads, lr, workspace, momentum=0.95, nesterov=True, steps=5, stream=None):
+    """momenta = momentum momenta + grads (None: none), weights -= lr sqrt(max(1, rows / cols)) times the orthogonalised
+    result, each kept within its limit (a MatrixList's)."""
+    w, g = _matrices(weights), _matrices(grads)
+    m = None if momenta is None else _matrices(momenta)
+    if len(w) != len(g) or (m is not None and len(m) != len(g)):
+        raise ValueError("lists of the same length expected")
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_sgd_orthogonal(w.array, None if m is None else m.array, g.array, len(g), int(steps), float(momentum),
+                                     int(bool(nesterov)), float(lr), ws, ws_bytes, _stream(stream)),
+           "minw_sgd_orthogonal")
 
 
 def w4_shapes(O, K, group):
