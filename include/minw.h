@@ -741,6 +741,68 @@ MINW_API minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, 
                                     const float *shift, int32_t act, void *y, int32_t y_type, int64_t ldy,
                                     void *stream);
 
+/* Low-rank adapters of many requests beside a shared projection: row t of x
+ * [T][K] (rows of ldx elements) goes through the adapter of user u = ids[t]
+ * (device, int32 [T]), down [n][r][K] and up [n][r][O] (dense, both of
+ * p_type):
+ *   h[t] = down[u] x[t]                              (fp32 sums; r values)
+ *   y[t] = act(scale (base[t] + alpha[u] up[u]^T h[t]) + shift)
+ * A row whose u is negative or n and more has no adapter: h[t] = 0, y[t] =
+ * act(scale base[t] + shift).  base [T][O] (rows of ldbase; nullable: 0),
+ * alpha fp32 [n], scale and shift fp32 [O] (nullable: 1, 1 and 0), h fp32
+ * [T][r] (nullable).  Types are fp32 or bf16, each by itself; fp32 values
+ * enter the products as three bf16 parts (those past 3.39e38 as infinite), of
+ * whose products those below 2^-25 are left out (2^-16 where y is bf16 and h
+ * not given); y rounds
+ * once, to nearest even.  y may be base (same type and row length) and may
+ * not overlap x.  An infinity or a NaN in a row, or in its adapter, makes that row's
+ * outputs infinite or NaN, no other user's.  Elements past K and O of a row are
+ * neither read nor written.  The same bits on every call.
+ * workspace: device scratch of minw_adapters_workspace_bytes (16-byte
+ * aligned, contents meaningless before and after); calls that share one must
+ * not run concurrently.  T = 0 does nothing.  Errors: MINW_EINVAL (null
+ * pointers, T < 0, K, O, n or r < 1, unknown types or act, short rows, a
+ * tensor off its elements' boundary, y = x, y = base with another type or row
+ * length, missing, misaligned or short workspace), MINW_EUNSUPPORTED (r >
+ * 256, n >= 2^24, T >= 2^27, K or O past 2^28, more blocks than a grid holds).
+ * Rows on 16-byte boundaries run wider loads. */
+MINW_API size_t minw_adapters_workspace_bytes(int64_t T, int32_t K, int32_t O, int32_t n, int32_t r, int32_t backward);
+MINW_API minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K, const int32_t *ids,
+                                   const void *down, const void *up, int32_t p_type, int32_t n, int32_t r,
+                                   const float *alpha, const void *base, int32_t base_type, int64_t ldbase, int32_t O,
+                                   const float *scale, const float *shift, int32_t act, void *y, int32_t y_type,
+                                   int64_t ldy, float *h, void *workspace, size_t workspace_bytes, void *stream);
+
+/* minw_w4_matvec with adapters: the base is the product with the w4 weights,
+ *   y[t] = act(fmaf(acc[t] + alpha[u] up[u]^T (down[u] x[t]), scale, shift))
+ * The weights are read once for up to 32 bf16 or 10 fp32 vectors.  Workspace
+ * (backward = 0), ids and adapters as minw_adapters, the rest as
+ * minw_w4_matvec. */
+MINW_API minw_status minw_w4_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, const uint8_t *codes,
+                                      const uint16_t *scales, int32_t O, int32_t K, int32_t group, const int32_t *ids,
+                                      const void *down, const void *up, int32_t p_type, int32_t n, int32_t r,
+                                      const float *alpha, const float *scale, const float *shift, int32_t act, void *y,
+                                      int32_t y_type, int64_t ldy, void *workspace, size_t workspace_bytes,
+                                      void *stream);
+
+/* The backward of s[t] = alpha[u] up[u]^T (down[u] x[t]) from ds = dy [T][O]
+ * (rows of lddy) and the h of the forward; with v[t] = alpha[u] up[u] dy[t],
+ *   dx[t] = down[u]^T v[t]   (accumulate: added to what dx holds)
+ *   ddown[u] = sum over u's rows of v[t] x[t]^T    (fp32 [n][r][K])
+ *   dup[u] = alpha[u] sum of h[t] dy[t]^T          (fp32 [n][r][O])
+ * dx [T][K] has x's type and rows of lddx.  dx, ddown and dup are nullable
+ * (x is read for ddown alone, h for dup alone).  Users without rows get zeros,
+ * rows without an adapter dx = 0 (accumulate: unchanged).  All sums are fp32
+ * in a fixed order (the same bits on every call).  dx may overlap neither x
+ * nor dy.  workspace with backward = 1; T = 0 writes zeros to ddown and dup.
+ * Errors as minw_adapters. */
+MINW_API minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K,
+                                            const int32_t *ids, const void *down, const void *up, int32_t p_type,
+                                            int32_t n, int32_t r, const float *alpha, const float *h, const void *dy,
+                                            int32_t dy_type, int64_t lddy, int32_t O, void *dx, int64_t lddx,
+                                            int32_t accumulate, float *ddown, float *dup, void *workspace,
+                                            size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------------- */
 /* Whole-network forward (Algorithm 1, inference branch)                   */
 /* ---------------------------------------------------------------------- */

@@ -1,0 +1,889 @@
+// adapters.cu -- low-rank adapters of many requests beside a shared projection:
+// row t of user u = ids[t] goes through that user's down [r][K] and up [r][O],
+//   h_t = down_u x_t,   y_t = act(scale (base_t + alpha_u up_u^T h_t) + shift)
+// and the backward of the term that is added.
+//
+// Rows of one user share its matrices, so rows are taken in tiles of one user: where a
+// tile holds all rows, every tile finds its own (tile t belongs to the first row of its
+// user, the others leave); else a plan sorts the rows by user first.  A cluster takes a
+// tile.  Its blocks share the columns of x (K), add up their parts of h through each
+// other's shared memory, and share the columns of y (O): one launch, x, base and y
+// move once, h not at all.  The backward's v_t = alpha_u up_u dy_t, dx_t = down_u^T v_t is the
+// same kernel with the matrices exchanged; the matrices' gradients are sums over a user's rows,
+//   ddown_u = sum v_t x_t^T,   dup_u = alpha_u sum h_t dy_t^T,   a kernel of their own.
+//
+// All of it is bound by memory (r <= 64 as a rule: 2 r operations a value), so the products run
+// on mma.sync (bf16, fp32 sums) from registers, without a trip through shared memory:
+// - along K, the order of the values is free, as long as both operands have the same: a lane
+//   takes eight consecutive values of a row for two products of 16;
+// - along O (and along K in the gradients), lane g of a group of eight takes eight consecutive columns of
+//   rows 2t and 2t + 1 and pairs them up.  Its eight registers are column g of eight products, whose
+//   results are 16 consecutive columns a lane.
+// fp32 values enter as three bf16 parts (8 + 8 + 8 bits); products of parts below 2^-25 of the
+// whole are left out, and where only a bf16 result leaves, those below 2^-16.
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "kernels.cuh"
+#include "values.cuh"
+#include "w4.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace minw {
+namespace adapters {
+
+constexpr int WARPS = 8, THREADS = 32 * WARPS;
+constexpr int MAX_RANK = 256;
+
+// ---------------------------------------------------------------------------
+// The plan: rows sorted by user, in their order; tiles of at most `most` rows
+// ---------------------------------------------------------------------------
+
+struct Tile {
+    int id, start, count, pad;               // user (-1: none), place of its first row in the sorted order
+};
+
+struct Plan {
+    int *order;                              // [T] the rows, sorted
+    int *first;                              // [n + 2] place of each user's first row; n: rows of no user
+    int *tiles_n;
+    Tile *tiles;
+    int *counts;                             // [n + 1][COUNTS] where they exceed shared memory
+};
+
+constexpr int PLAN_THREADS = 1024, PLAN_WARPS = 32;
+constexpr int COUNTS = PLAN_WARPS + 1;       // of a user; odd, so that a warp's users lie in different banks
+
+__device__ __forceinline__ int user_of(int id, int n) { return id >= 0 && id < n ? id : n; }
+
+// A warp counts a run of rows, then places them; between the two, the counts [user][warp] become places.  One block:
+// 4096 rows are 4 rounds of a warp.
+__global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const int *__restrict__ ids, int T, int n, int most, Plan p,
+                                                            int in_shared) {
+    pdl_trigger();
+    pdl_wait();
+    extern __shared__ int counts_smem[];
+    int *counts = in_shared ? counts_smem : p.counts;
+    __shared__ int warp_rows[PLAN_WARPS], warp_tiles[PLAN_WARPS], base_rows, base_tiles;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int seg = ((T + PLAN_WARPS - 1) / PLAN_WARPS + 31) / 32 * 32;
+    const int t0 = min(T, warp * seg), t1 = min(T, t0 + seg);
+    for (int k = threadIdx.x; k < (n + 1) * COUNTS; k += PLAN_THREADS) counts[k] = 0;
+    if (threadIdx.x == 0) base_rows = base_tiles = 0;
+    __syncthreads();
+    for (int t = t0 + lane; t - lane < t1; t += 32) {
+        const int u = t < t1 ? user_of(ids[t], n) : -1;
+        const uint32_t m = __match_any_sync(0xffffffffu, u);
+        if (u >= 0 && lane == __ffs(m) - 1) counts[u * COUNTS + warp] += __popc(m);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int u0 = 0; u0 <= n; u0 += PLAN_THREADS) {
+        const int u = u0 + threadIdx.x;
+        int rows = 0;
+        if (u <= n)
+            for (int w = 0; w < PLAN_WARPS; ++w) {
+                const int c = counts[u * COUNTS + w];
+                counts[u * COUNTS + w] = rows;
+                rows += c;
+            }
+        const int tiles = (rows + most - 1) / most;
+        int ir = rows, it = tiles;                             // inclusive sums over the block
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int a = __shfl_up_sync(0xffffffffu, ir, d), b = __shfl_up_sync(0xffffffffu, it, d);
+            if (lane >= d) { ir += a; it += b; }
+        }
+        if (lane == 31) { warp_rows[warp] = ir; warp_tiles[warp] = it; }
+        __syncthreads();
+        int start = base_rows + ir - rows, tile = base_tiles + it - tiles;
+        for (int w = 0; w < warp; ++w) { start += warp_rows[w]; tile += warp_tiles[w]; }
+        if (u <= n) {
+            p.first[u] = start;
+            for (int w = 0; w < PLAN_WARPS; ++w) counts[u * COUNTS + w] += start;
+            for (int k = 0; k < tiles; ++k)
+                p.tiles[tile + k] = Tile{u < n ? u : -1, start + k * most, min(most, rows - k * most), 0};
+        }
+        __syncthreads();
+        if (threadIdx.x == PLAN_THREADS - 1) { base_rows = start + rows; base_tiles = tile + tiles; }
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) {
+        p.first[n + 1] = T;
+        *p.tiles_n = base_tiles;
+    }
+    for (int t = t0 + lane; t - lane < t1; t += 32) {
+        const int u = t < t1 ? user_of(ids[t], n) : -1;
+        const uint32_t m = __match_any_sync(0xffffffffu, u);
+        int at = 0;
+        if (u >= 0) at = counts[u * COUNTS + warp] + __popc(m & ((1u << lane) - 1));
+        __syncwarp();
+        if (u >= 0) {
+            p.order[at] = t;
+            if (lane == __ffs(m) - 1) counts[u * COUNTS + warp] += __popc(m);
+        }
+        __syncwarp();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Values into bf16 parts
+// ---------------------------------------------------------------------------
+
+template <typename V>
+constexpr int parts_of() { return sizeof(V) == 2 ? 1 : 3; }
+
+// Eight consecutive values as they lie in memory; zeros from `left` on.
+template <typename V>
+struct Eight {
+    uint32_t w[2 * sizeof(V)];
+
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < 2 * (int)sizeof(V); ++k) w[k] = 0u;
+    }
+    __device__ __forceinline__ void load(const V *p, int left, bool vec) {
+        if (vec && left >= 8) {
+            Vec<V, 8> v;
+            v.load(p);
+#pragma unroll
+            for (int k = 0; k < 2 * (int)sizeof(V); ++k) w[k] = v.w[k];
+        } else {
+            zero();
+            if constexpr (sizeof(V) == 4) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < left) w[k] = __float_as_uint(p[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < left) w[k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {          // a in the lower half
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// Two fp32 values as pairs of bf16 parts whose sums they are, each part rounded to nearest: what is left after one is 2^-9 of
+// the value at most, after two 2^-18 (parts cut off instead leave up to 2^-7 and 2^-15, and products without the smallest
+// are 2^-21 off).  An infinity, a NaN or a value past 3.39e38 makes the second part a NaN.
+__device__ __forceinline__ void split2(uint32_t a, uint32_t b, uint32_t *p) {
+    float x = __uint_as_float(a), y = __uint_as_float(b);
+    p[0] = bf16_pair(x, y);
+    x -= __uint_as_float(p[0] << 16);
+    y -= __uint_as_float(p[0] & 0xffff0000u);
+    p[1] = bf16_pair(x, y);
+    p[2] = bf16_pair(x - __uint_as_float(p[1] << 16), y - __uint_as_float(p[1] & 0xffff0000u));
+}
+
+// Pairs of neighbours of one row: pair k = values 2k, 2k + 1, in parts.
+template <typename V>
+__device__ __forceinline__ void along(const Eight<V> &e, uint32_t (*p)[4]) {
+    if constexpr (sizeof(V) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[0][k] = e.w[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t s[3];
+            split2(e.w[2 * k], e.w[2 * k + 1], s);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) p[i][k] = s[i];
+        }
+    }
+}
+
+// Pairs across two rows: value i of the first and of the second, in parts.
+template <typename V>
+__device__ __forceinline__ void across(const Eight<V> &a, const Eight<V> &b, int i, uint32_t *p) {
+    if constexpr (sizeof(V) == 2) p[0] = __byte_perm(a.w[i >> 1], b.w[i >> 1], (i & 1) ? 0x7632 : 0x5410);
+    else split2(a.w[i], b.w[i], p);
+}
+
+__device__ __forceinline__ void mma(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// ---------------------------------------------------------------------------
+// Through an adapter
+// ---------------------------------------------------------------------------
+
+struct Args {
+    const void *in;                          // [T][D], rows ld_in apart
+    const int *ids;
+    const void *p1, *p2;                     // [n][r][D], [n][r][E]
+    const float *alpha;                      // [n], or null: 1
+    const void *base;                        // [T][E], or null: 0
+    const float *scale, *shift;              // [E], or null: 1 and 0
+    void *out;                               // [T][E]
+    float *h;                                // [T][r] by row, or null: in p1^T
+    const float *h_in;                       // backward: [T][r] by row ...
+    float *ht, *vt;                          // ... and [r][T] by sorted row, alpha times h_in and the values here
+    int64_t ld_in, ld_base, ld_out;
+    int T, D, E, n, r, rp;                   // rp: r rounded up to 16
+    int act, base_bf16, out_bf16;
+    int in_vec, p1_vec, p2_vec, base_vec, out_vec;        // whole rows on 16-byte boundaries
+    int fine;                                // products of parts down to 2^-24
+    int split;                               // blocks of a cluster
+    Plan plan;                               // order null: every tile finds its rows
+};
+
+template <typename V>
+__device__ __forceinline__ void load16(const void *p, int64_t at, int left, bool vec, float *v) {
+    const V *q = static_cast<const V *>(p) + at;
+    if (vec && left >= 16) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            Vec<V, 8> w;
+            w.load(q + 8 * k);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[8 * k + i] = w.get(i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            v[i] = 0.0f;
+            if (i < left) {
+                Vec<V, 1> w;
+                w.load(q + i);
+                v[i] = w.get(0);
+            }
+        }
+    }
+}
+
+template <typename V>
+__device__ __forceinline__ void store16(void *p, int64_t at, int left, bool vec, const float *v) {
+    V *q = static_cast<V *>(p) + at;
+    if (vec && left >= 16) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            Vec<V, 8> w;
+            w.set(v + 8 * k);
+            w.store(q + 8 * k);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (i < left) {
+                Vec<V, 1> w;
+                w.set(v + i);
+                w.store(q + i);
+            }
+    }
+}
+
+// MT: tiles of 16 rows, NT: tiles of 8 of r in one go.  Shared memory: the warps' sums, the block's, h in parts.
+template <typename TI, typename TP, int MT, int NT>
+__global__ void __launch_bounds__(THREADS, 1) adapter_kernel(const __grid_constant__ Args a) {
+    constexpr int M = 16 * MT, R = 8 * NT, PI = parts_of<TI>(), PP = parts_of<TP>();
+    extern __shared__ __align__(16) uint8_t smem[];
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R]
+    float *part = red + WARPS * M * R;                                   // [M][rp]
+    uint16_t *hs = reinterpret_cast<uint16_t *>(part + M * a.rp);        // [3][M][rp + 8]
+    __shared__ int rows[M];
+    __shared__ int tile_id, tile_rows, tile_start;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
+    pdl_wait();
+    pdl_trigger();                            // dependents may rely on what came before this kernel
+    if (a.plan.order) {
+        if (tile >= *a.plan.tiles_n) return;
+        const Tile x = a.plan.tiles[tile];
+        if (threadIdx.x == 0) { tile_id = x.id; tile_rows = x.count; tile_start = x.start; }
+        if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
+    } else if (warp == 0) {                   // at most 64 rows
+        const int mine = user_of(a.ids[tile], a.n);
+        const int lo = lane < a.T ? user_of(a.ids[lane], a.n) : -1, hi = lane + 32 < a.T ? user_of(a.ids[lane + 32], a.n) : -1;
+        const uint32_t ml = __ballot_sync(0xffffffffu, lo == mine), mh = __ballot_sync(0xffffffffu, hi == mine);
+        const uint32_t below = (1u << lane) - 1;
+        if ((ml >> lane) & 1) rows[__popc(ml & below)] = lane;
+        if ((mh >> lane) & 1) rows[__popc(ml) + __popc(mh & below)] = lane + 32;
+        if (lane == 0) {
+            tile_id = mine < a.n ? mine : -1;
+            tile_rows = tile == (ml ? __ffs(ml) - 1 : 31 + __ffs(mh)) ? __popc(ml) + __popc(mh) : 0;
+            tile_start = 0;
+        }
+    }
+    __syncthreads();
+    const int count = tile_rows, id = tile_id;
+    if (count == 0) return;                   // an earlier row's tile; the whole cluster leaves
+    cg::cluster_group cluster = cg::this_cluster();
+
+    if (id >= 0) {
+        const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
+        for (int j0 = 0; j0 < a.r; j0 += R) {
+            float acc[MT][NT][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+            const TP *p1 = static_cast<const TP *>(a.p1) + ((int64_t)id * a.r + j0) * a.D;
+            const TI *in = static_cast<const TI *>(a.in);
+            for (int b = b0 + warp; b < b1; b += WARPS) {
+                const int k = 32 * b + 8 * t, left = a.D - k;
+                Eight<TI> x[MT][2];
+                Eight<TP> p[NT];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int e = 16 * m + 8 * i + g;
+                        if (e < count) x[m][i].load(in + rows[e] * a.ld_in + k, left, a.in_vec);
+                        else x[m][i].zero();
+                    }
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    if (j0 + 8 * j + g < a.r) p[j].load(p1 + (int64_t)(8 * j + g) * a.D + k, left, a.p1_vec);
+                    else p[j].zero();
+                }
+                uint32_t xp[MT][2][PI][4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) along(x[m][i], xp[m][i]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    uint32_t pp[PP][4];
+                    along(p[j], pp);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int l = 2; l >= 0; --l)                     // the smallest products first
+#pragma unroll
+                            for (int q = 0; q <= l; ++q) {
+                                const int v = l - q;
+                                if (q >= PI || v >= PP || (l == 2 && !a.fine)) continue;
+#pragma unroll
+                                for (int m = 0; m < MT; ++m) {
+                                    const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
+                                                           xp[m][1][q][2 * s + 1]};
+                                    mma(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
+                                }
+                            }
+                }
+            }
+            __syncthreads();                  // an earlier round's sums have been read
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    float *d = red + (warp * M + 16 * m + g) * R + 8 * j + 2 * t;
+                    *reinterpret_cast<float2 *>(d) = make_float2(acc[m][j][0], acc[m][j][1]);
+                    *reinterpret_cast<float2 *>(d + 8 * R) = make_float2(acc[m][j][2], acc[m][j][3]);
+                }
+            __syncthreads();
+            for (int e = threadIdx.x; e < M * R; e += THREADS) {
+                float v[WARPS];
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) v[w] = red[w * M * R + e];
+#pragma unroll
+                for (int w = 1; w < WARPS; ++w) v[0] += v[w];
+                const int j = j0 + e % R;
+                if (j < a.rp) part[e / R * a.rp + j] = v[0];
+            }
+        }
+        if (a.split > 1) cluster.sync();
+        else __syncthreads();
+        // h from all blocks' parts, in their order
+        const float alpha = a.alpha ? a.alpha[id] : 1.0f;
+        for (int e = threadIdx.x; e < M * a.rp; e += THREADS) {
+            float v[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                v[c] = a.split == 1 ? (c == 0 ? part[e] : 0.0f) : c < a.split ? *cluster.map_shared_rank(part + e, c) : 0.0f;
+#pragma unroll
+            for (int c = 1; c < 8; ++c) v[0] += v[c];
+            const int m = e / a.rp, j = e - m * a.rp;
+            if (rank == 0 && m < count && j < a.r) {
+                if (a.h) a.h[(int64_t)rows[m] * a.r + j] = v[0];
+                if (a.vt) a.vt[(int64_t)j * a.T + tile_start + m] = alpha * v[0];
+                if (a.ht) a.ht[(int64_t)j * a.T + tile_start + m] = alpha * a.h_in[(int64_t)rows[m] * a.r + j];
+            }
+            uint32_t s[3];
+            split2(__float_as_uint(alpha * v[0]), 0u, s);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) hs[(q * M + m) * (a.rp + 8) + j] = (uint16_t)s[q];
+        }
+        if (a.split > 1) cluster_done_reading();
+        __syncthreads();
+    } else if (rank == 0 && a.h) {
+        for (int e = threadIdx.x; e < count * a.r; e += THREADS) a.h[(int64_t)rows[e / a.r] * a.r + e % a.r] = 0.0f;
+    }
+
+    constexpr int ME = MT < 2 ? MT : 2;       // tiles of 16 rows at a time
+    const int eblocks = (a.E + 63) / 64;
+    for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS) {
+        for (int m0 = 0; m0 < MT && 16 * m0 < count; m0 += ME) {
+            float acc[ME][8][4];
+#pragma unroll
+            for (int m = 0; m < ME; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+            if (id >= 0) {
+                const int c = 64 * b + 8 * g, left = a.E - c;
+                const TP *p2 = static_cast<const TP *>(a.p2) + (int64_t)id * a.r * a.E + c;
+                for (int k = 0; k < a.rp; k += 16) {
+                    Eight<TP> p[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int j = k + 2 * t + (i & 1) + 8 * (i >> 1);
+                        if (j < a.r && left > 0) p[i].load(p2 + (int64_t)j * a.E, left, a.p2_vec);
+                        else p[i].zero();
+                    }
+                    uint32_t f[ME][3][4];
+#pragma unroll
+                    for (int m = 0; m < ME; ++m)
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) {
+                            const uint16_t *h = hs + (q * M + 16 * (m0 + m) + g) * (a.rp + 8) + k + 2 * t;
+                            f[m][q][0] = *reinterpret_cast<const uint32_t *>(h);
+                            f[m][q][1] = *reinterpret_cast<const uint32_t *>(h + 8 * (a.rp + 8));
+                            f[m][q][2] = *reinterpret_cast<const uint32_t *>(h + 8);
+                            f[m][q][3] = *reinterpret_cast<const uint32_t *>(h + 8 * (a.rp + 8) + 8);
+                        }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t q0[PP], q1[PP];
+                        across(p[0], p[1], i, q0);
+                        across(p[2], p[3], i, q1);
+#pragma unroll
+                        for (int l = 2; l >= 0; --l)
+#pragma unroll
+                            for (int q = 0; q <= l; ++q) {
+                                const int v = l - q;
+                                if (v >= PP || (l == 2 && !a.fine)) continue;
+#pragma unroll
+                                for (int m = 0; m < ME; ++m) mma(acc[m][i], f[m][q], q0[v], q1[v]);
+                            }
+                    }
+                }
+            }
+            const int c = 64 * b + 16 * t, left = a.E - c;
+            if (left <= 0) continue;
+#pragma unroll
+            for (int m = 0; m < ME; ++m)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int e = 16 * (m0 + m) + 8 * i + g;
+                    if (e >= count) continue;
+                    const int64_t row = rows[e];
+                    float z[16], f[16];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        z[k] = acc[m][k][2 * i];
+                        z[8 + k] = acc[m][k][2 * i + 1];
+                    }
+                    if (a.base) {
+                        if (a.base_bf16) load16<uint16_t>(a.base, row * a.ld_base + c, left, a.base_vec, f);
+                        else load16<float>(a.base, row * a.ld_base + c, left, a.base_vec, f);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[k] += f[k];
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (k < left) z[k] = fmaf(z[k], a.scale ? a.scale[c + k] : 1.0f, a.shift ? a.shift[c + k] : 0.0f);
+                    with_act(a.act, [&](auto act) {
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z[k] = act_value<act.value>(z[k]);
+                    });
+                    if (a.out_bf16) store16<uint16_t>(a.out, row * a.ld_out + c, left, a.out_vec, z);
+                    else store16<float>(a.out, row * a.ld_out + c, left, a.out_vec, z);
+                }
+        }
+    }
+    __syncwarp();
+    if (a.split > 1 && id >= 0) cluster_leave();
+}
+
+// ---------------------------------------------------------------------------
+// Gradients of the matrices: out_u [r][C] = sum over rows of u of a[j][place] z[row][c]
+// ---------------------------------------------------------------------------
+
+struct Job {
+    const float *a;                          // [r][T] by sorted row
+    const void *z;                           // [T][C], rows ld apart
+    float *out;                              // [n][r][C]
+    int64_t ld;
+    int C, blocks;                           // blocks: of this job for a user
+    int vec, out_vec;
+};
+
+struct GradArgs {
+    Job job[2];
+    int jobs, T, n, r, along;                // along: warps that share a user's rows (the others: columns)
+    Plan plan;
+};
+
+// RT: tiles of 16 of r in one go.  A warp takes 64 columns.
+template <typename TZ, int RT>
+__global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant__ GradArgs a) {
+    constexpr int PZ = parts_of<TZ>();
+    extern __shared__ __align__(16) uint8_t smem[];
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][64] where warps share rows
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    pdl_trigger();
+    pdl_wait();
+    const int all = a.job[0].blocks + (a.jobs > 1 ? a.job[1].blocks : 0);
+    const int u = blockIdx.x / all;
+    int b = blockIdx.x - u * all;
+    const Job &job = a.job[b >= a.job[0].blocks ? 1 : 0];
+    if (b >= a.job[0].blocks) b -= a.job[0].blocks;
+    const int wa = warp % a.along, wc = warp / a.along;
+    const int c0 = 64 * (b * (WARPS / a.along) + wc), c = c0 + 8 * g, left = job.C - c;
+    const int first = a.plan.first[u], count = a.plan.first[u + 1] - first;
+    const TZ *z = static_cast<const TZ *>(job.z) + c;
+    for (int j0 = 0; j0 < a.r; j0 += 16 * RT) {
+        float acc[RT][8][4];
+#pragma unroll
+        for (int m = 0; m < RT; ++m)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[m][i][k] = 0.0f;
+        for (int s = 16 * wa; s < count; s += 16 * a.along) {
+            Eight<TZ> v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = s + 2 * t + (i & 1) + 8 * (i >> 1);
+                if (e < count && left > 0) v[i].load(z + a.plan.order[first + e] * job.ld, left, job.vec);
+                else v[i].zero();
+            }
+            uint32_t f[RT][3][4];
+#pragma unroll
+            for (int m = 0; m < RT; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + 16 * m + g + 8 * (i & 1), e = s + 2 * t + 8 * (i >> 1);
+                    const float *p = job.a + (int64_t)j * a.T + first + e;
+                    const float x = j < a.r && e < count ? p[0] : 0.0f, y = j < a.r && e + 1 < count ? p[1] : 0.0f;
+                    uint32_t w[3];
+                    split2(__float_as_uint(x), __float_as_uint(y), w);
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) f[m][q][i] = w[q];
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t q0[PZ], q1[PZ];
+                across(v[0], v[1], i, q0);
+                across(v[2], v[3], i, q1);
+#pragma unroll
+                for (int l = 2; l >= 0; --l)
+#pragma unroll
+                    for (int q = 0; q <= l; ++q) {
+                        const int k = l - q;
+                        if (k >= PZ) continue;
+#pragma unroll
+                        for (int m = 0; m < RT; ++m) mma(acc[m][i], f[m][q], q0[k], q1[k]);
+                    }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < RT; ++m) {
+            if (a.along > 1) {                // the warps of a column block in their order, into the first
+                __syncthreads();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) red[(warp * 32 + 4 * i + k) * 32 + lane] = acc[m][i][k];
+                __syncthreads();
+                if (wa == 0)
+                    for (int w = 1; w < a.along; ++w)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) acc[m][i][k] += red[((warp + w) * 32 + 4 * i + k) * 32 + lane];
+            }
+            if (wa != 0) continue;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int j = j0 + 16 * m + 8 * i + g, cc = c0 + 16 * t;
+                if (j >= a.r || cc >= job.C) continue;
+                float y[16];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    y[k] = acc[m][k][2 * i];
+                    y[8 + k] = acc[m][k][2 * i + 1];
+                }
+                store16<float>(job.out, ((int64_t)u * a.r + j) * job.C + cc, job.C - cc, job.out_vec, y);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+
+using namespace minw_host;
+
+static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+
+// Rows of a tile: 64, where h in registers leaves room for them (r <= 32), else 32.
+static int rows_of(int r) { return r <= 32 ? 64 : 32; }
+
+constexpr int W4_ROWS = 32;                  // rows of w4 products at a time
+
+static int64_t tiles_of(int64_t T, int n, int r) { return std::min<int64_t>(T, T / rows_of(r) + std::min<int64_t>(T, (int64_t)n + 1)); }
+
+static bool counts_in_shared(int n) { return (int64_t)(n + 1) * COUNTS * 4 <= 128 * 1024; }
+
+static Plan plan_at(uint8_t *base, int64_t T, int n, int r, int64_t *used) {
+    Plan p;
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        uint8_t *q = base + at;
+        at += up(bytes, 16);
+        return q;
+    };
+    p.tiles = reinterpret_cast<Tile *>(take(tiles_of(T, n, r) * sizeof(Tile)));
+    p.order = reinterpret_cast<int *>(take(T * 4));
+    p.first = reinterpret_cast<int *>(take(((int64_t)n + 2) * 4));
+    p.tiles_n = reinterpret_cast<int *>(take(4));
+    p.counts = reinterpret_cast<int *>(take(counts_in_shared(n) ? 0 : ((int64_t)n + 1) * COUNTS * 4));
+    *used = at;
+    return p;
+}
+
+static minw_status make_plan(const Plan &p, const int *ids, int T, int n, int r, cudaStream_t s) {
+    const bool in_shared = counts_in_shared(n);
+    if (in_shared && !allow_shared(reinterpret_cast<const void *>(plan_kernel), 128 * 1024)) return MINW_ECUDA;
+    const size_t smem = in_shared ? (size_t)(n + 1) * COUNTS * 4 : 0;
+    return launch_pdl(plan_kernel, dim3(1), dim3(PLAN_THREADS), smem, s, ids, T, n, rows_of(r), p, in_shared ? 1 : 0) == cudaSuccess
+               ? MINW_OK : launch_failed();
+}
+
+template <typename TI, typename TP, int MT, int NT>
+static cudaError_t launch(const Args &a, int64_t tiles, cudaStream_t s) {
+    constexpr int M = 16 * MT;
+    const int smem = WARPS * M * 8 * NT * 4 + M * a.rp * 4 + 3 * M * (a.rp + 8) * 2;
+    auto kern = adapter_kernel<TI, TP, MT, NT>;
+    constexpr int ranks = NT == 8 ? MAX_RANK : 8 * NT;
+    const int most = WARPS * M * 8 * NT * 4 + M * ranks * 4 + 3 * M * (ranks + 8) * 2;
+    if (!allow_shared(reinterpret_cast<const void *>(kern), most)) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * a.split));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)a.split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+template <typename TI, typename TP>
+static cudaError_t launch_types(const Args &a, int64_t tiles, int most, cudaStream_t s) {
+    if (most <= 16)
+        return a.r <= 16 ? launch<TI, TP, 1, 2>(a, tiles, s) : a.r <= 32 ? launch<TI, TP, 1, 4>(a, tiles, s)
+                                                                         : launch<TI, TP, 1, 8>(a, tiles, s);
+    return a.r <= 16 ? launch<TI, TP, 4, 2>(a, tiles, s) : a.r <= 32 ? launch<TI, TP, 4, 4>(a, tiles, s)
+                                                                     : launch<TI, TP, 2, 8>(a, tiles, s);
+}
+
+static bool vec_rows(const void *p, int64_t ld, int bf16) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
+}
+
+// One pass through the adapters; types as in the public calls.  plan null: T <= rows_of(r).
+static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cudaStream_t s) {
+    a.rp = (a.r + 15) / 16 * 16;
+    a.in_vec = vec_rows(a.in, a.ld_in, in_bf16);
+    a.p1_vec = vec_rows(a.p1, a.D, p_bf16);
+    a.p2_vec = vec_rows(a.p2, a.E, p_bf16);
+    a.base_vec = vec_rows(a.base, a.ld_base, a.base_bf16);
+    a.out_vec = vec_rows(a.out, a.ld_out, a.out_bf16);
+    a.fine = !a.out_bf16 || a.h || a.vt;
+    if (plan) a.plan = *plan;
+    else a.plan = Plan{};
+    const int64_t tiles = plan ? tiles_of(a.T, a.n, a.r) : a.T;
+    a.split = tiles <= 64 ? 8 : 4;
+    const int most = plan ? rows_of(a.r) : a.T;
+    const cudaError_t e = in_bf16 ? (p_bf16 ? launch_types<uint16_t, uint16_t>(a, tiles, most, s)
+                                            : launch_types<uint16_t, float>(a, tiles, most, s))
+                                  : (p_bf16 ? launch_types<float, uint16_t>(a, tiles, most, s)
+                                            : launch_types<float, float>(a, tiles, most, s));
+    return e == cudaSuccess ? launch_status() : launch_failed();
+}
+
+template <typename TZ>
+static cudaError_t launch_grads(const GradArgs &a, int64_t grid, cudaStream_t s) {
+    const size_t smem = a.along > 1 ? WARPS * 16 * 64 * 4 : 0;
+    auto kern = a.r <= 16 ? grads_kernel<TZ, 1> : a.r <= 32 ? grads_kernel<TZ, 2> : grads_kernel<TZ, 4>;
+    return launch_pdl(kern, dim3((unsigned)grid), dim3(THREADS), smem, s, a);
+}
+
+struct Shape {
+    int64_t T;
+    int K, O, n, r;
+};
+
+static bool sizes_fit(const Shape &z) {
+    if (z.T >= (1 << 27) || z.K > (1 << 28) || z.O > (1 << 28) || z.r > MAX_RANK || z.n >= (1 << 24)) return false;
+    return (int64_t)z.n * ((z.K + 63) / 64 + (z.O + 63) / 64 + 2) < (1ll << 31) && tiles_of(z.T, z.n, z.r) * 8 < (1ll << 31);
+}
+
+static bool aligned(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % (type == MINW_BF16 ? 2 : 4) == 0; }
+static bool known(int type) { return type == MINW_F32 || type == MINW_BF16; }
+
+}  // namespace adapters
+}  // namespace minw
+
+using namespace minw;
+using namespace minw_host;
+
+extern "C" {
+
+size_t minw_adapters_workspace_bytes(int64_t T, int32_t K, int32_t O, int32_t n, int32_t r, int32_t backward) {
+    using namespace adapters;
+    const Shape z{T, K, O, n, r};
+    if (T < 0 || K < 1 || O < 1 || n < 1 || r < 1 || !sizes_fit(z)) return 0;
+    int64_t used;
+    plan_at(nullptr, T, n, r, &used);
+    if (backward) return (size_t)(used + 2 * up(T * r * 4, 16));
+    return (size_t)std::max<int64_t>(used, std::min<int64_t>(T, W4_ROWS) * O * 4);
+}
+
+minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K, const int32_t *ids,
+                          const void *down, const void *up_, int32_t p_type, int32_t n, int32_t r, const float *alpha,
+                          const void *base, int32_t base_type, int64_t ldbase, int32_t O, const float *scale,
+                          const float *shift, int32_t act, void *y, int32_t y_type, int64_t ldy, float *h, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    using namespace adapters;
+    if (T < 0 || K < 1 || O < 1 || n < 1 || r < 1 || ldx < K || ldy < O || (base && ldbase < O)) return MINW_EINVAL;
+    if (!down || !up_ || (T > 0 && (!x || !ids || !y)) || act < MINW_ACT_NONE || act > MINW_ACT_SILU) return MINW_EINVAL;
+    if (!known(x_type) || !known(p_type) || !known(y_type) || (base && !known(base_type))) return MINW_EINVAL;
+    if (!aligned(x, x_type) || !aligned(down, p_type) || !aligned(up_, p_type) || !aligned(y, y_type) ||
+        (base && !aligned(base, base_type)) || !on_floats(alpha, scale, shift, h) || !aligned(ids, MINW_F32))
+        return MINW_EINVAL;
+    if (base && base == y && (base_type != y_type || ldbase != ldy)) return MINW_EINVAL;
+    if (x && x == y) return MINW_EINVAL;
+    if (!sizes_fit(Shape{T, K, O, n, r})) return MINW_EUNSUPPORTED;
+    if (T == 0) return MINW_OK;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < minw_adapters_workspace_bytes(T, K, O, n, r, 0)) return MINW_EINVAL;
+    Args a{};
+    a.in = x; a.ld_in = ldx; a.D = K; a.E = O; a.T = (int)T; a.ids = ids; a.p1 = down; a.p2 = up_; a.n = n; a.r = r;
+    a.alpha = alpha; a.base = base; a.base_bf16 = base_type == MINW_BF16; a.ld_base = ldbase; a.scale = scale; a.shift = shift;
+    a.act = act; a.out = y; a.out_bf16 = y_type == MINW_BF16; a.ld_out = ldy; a.h = h;
+    cudaStream_t s = (cudaStream_t)stream;
+    if (T <= rows_of(r)) return through(a, x_type == MINW_BF16, p_type == MINW_BF16, nullptr, s);
+    int64_t used;
+    const Plan p = plan_at(static_cast<uint8_t *>(workspace), T, n, r, &used);
+    const minw_status st = make_plan(p, ids, (int)T, n, r, s);
+    return st != MINW_OK ? st : through(a, x_type == MINW_BF16, p_type == MINW_BF16, &p, s);
+}
+
+minw_status minw_w4_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, const uint8_t *codes,
+                             const uint16_t *scales, int32_t O, int32_t K, int32_t group, const int32_t *ids, const void *down,
+                             const void *up_, int32_t p_type, int32_t n, int32_t r, const float *alpha, const float *scale,
+                             const float *shift, int32_t act, void *y, int32_t y_type, int64_t ldy, void *workspace,
+                             size_t workspace_bytes, void *stream) {
+    using namespace adapters;
+    if (T < 0 || K < 1 || O < 1 || n < 1 || r < 1 || !down || !up_ || (T > 0 && !ids) || !known(p_type)) return MINW_EINVAL;
+    if (!aligned(down, p_type) || !aligned(up_, p_type) || !aligned(ids, MINW_F32) || !on_floats(alpha) || (x && x == y))
+        return MINW_EINVAL;
+    const minw_status ok = w4::check(x, x_type, ldx, T, codes, scales, O, K, group, scale, shift, act, y, y_type, ldy);
+    if (ok != MINW_OK) return ok;
+    if (!sizes_fit(Shape{T, K, O, n, r})) return MINW_EUNSUPPORTED;
+    if (T == 0) return MINW_OK;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < minw_adapters_workspace_bytes(T, K, O, n, r, 0)) return MINW_EINVAL;
+    const int xs = x_type == MINW_BF16 ? 2 : 4, ys = y_type == MINW_BF16 ? 2 : 4;
+    // the products of so many rows read the weights once (bf16 x); their adapters' terms go through the workspace
+    for (int64_t t0 = 0; t0 < T; t0 += W4_ROWS) {
+        const int rows = (int)std::min<int64_t>(W4_ROWS, T - t0);
+        Args a{};
+        a.in = static_cast<const uint8_t *>(x) + t0 * ldx * xs; a.ld_in = ldx; a.D = K; a.E = O; a.T = rows; a.ids = ids + t0;
+        a.p1 = down; a.p2 = up_; a.n = n; a.r = r; a.alpha = alpha; a.out = workspace; a.ld_out = O;
+        const minw_status st = through(a, x_type == MINW_BF16, p_type == MINW_BF16, nullptr, (cudaStream_t)stream);
+        if (st != MINW_OK) return st;
+        const minw_status sw = w4::matvec(a.in, x_type, ldx, rows, codes, scales, O, K, group, scale, shift, act,
+                                          static_cast<uint8_t *>(y) + t0 * ldy * ys, y_type, ldy,
+                                          static_cast<const float *>(workspace), (cudaStream_t)stream);
+        if (sw != MINW_OK) return sw;
+    }
+    return MINW_OK;
+}
+
+minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K, const int32_t *ids,
+                                   const void *down, const void *up_, int32_t p_type, int32_t n, int32_t r, const float *alpha,
+                                   const float *h, const void *dy, int32_t dy_type, int64_t lddy, int32_t O, void *dx,
+                                   int64_t lddx, int32_t accumulate, float *ddown, float *dup, void *workspace,
+                                   size_t workspace_bytes, void *stream) {
+    using namespace adapters;
+    if (T < 0 || K < 1 || O < 1 || n < 1 || r < 1 || ldx < K || lddy < O || (dx && lddx < K)) return MINW_EINVAL;
+    if (!down || !up_ || (T > 0 && (!ids || !dy || (ddown && !x) || (dup && !h)))) return MINW_EINVAL;
+    if (!known(x_type) || !known(p_type) || !known(dy_type)) return MINW_EINVAL;
+    if (!aligned(x, x_type) || !aligned(down, p_type) || !aligned(up_, p_type) || !aligned(dy, dy_type) || !aligned(dx, x_type) ||
+        !aligned(ids, MINW_F32) || !on_floats(alpha, h, ddown, dup))
+        return MINW_EINVAL;
+    if (dx && (dx == x || dx == dy)) return MINW_EINVAL;
+    if (!sizes_fit(Shape{T, K, O, n, r})) return MINW_EUNSUPPORTED;
+    if (!dx && !ddown && !dup) return MINW_OK;
+    if (T == 0 && !ddown && !dup) return MINW_OK;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < minw_adapters_workspace_bytes(T, K, O, n, r, 1)) return MINW_EINVAL;
+    cudaStream_t s = (cudaStream_t)stream;
+    int64_t used;
+    const Plan p = plan_at(static_cast<uint8_t *>(workspace), T, n, r, &used);
+    float *vt = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + used);
+    float *ht = vt + up(T * r * 4, 16) / 4;
+    minw_status st = make_plan(p, ids, (int)T, n, r, s);
+    if (st != MINW_OK) return st;
+    if (T > 0) {
+        Args a{};
+        a.in = dy; a.ld_in = lddy; a.D = O; a.E = dx ? K : 0; a.T = (int)T; a.ids = ids; a.p1 = up_; a.p2 = down; a.n = n; a.r = r;
+        a.alpha = alpha; a.out = dx; a.out_bf16 = x_type == MINW_BF16; a.ld_out = lddx;
+        if (accumulate) { a.base = dx; a.base_bf16 = a.out_bf16; a.ld_base = lddx; }
+        a.vt = ddown ? vt : nullptr;
+        a.ht = dup ? ht : nullptr;
+        a.h_in = h;
+        st = through(a, dy_type == MINW_BF16, p_type == MINW_BF16, &p, s);
+        if (st != MINW_OK) return st;
+    }
+    // jobs of one type in one launch
+    GradArgs ga{};
+    ga.T = (int)T; ga.n = n; ga.r = r; ga.plan = p;
+    const int64_t each = T / n;
+    ga.along = each >= 128 ? 8 : each >= 64 ? 4 : each >= 32 ? 2 : 1;
+    const int wide = 64 * (WARPS / ga.along);
+    const Job jobs[2] = {{vt, x, ddown, ldx, K, (K + wide - 1) / wide, vec_rows(x, ldx, x_type == MINW_BF16), vec_rows(ddown, K, 0)},
+                         {ht, dy, dup, lddy, O, (O + wide - 1) / wide, vec_rows(dy, lddy, dy_type == MINW_BF16), vec_rows(dup, O, 0)}};
+    const int types[2] = {x_type, dy_type};
+    for (int k = 0; k < 2; ++k) {
+        if (!jobs[k].out) continue;
+        ga.job[0] = jobs[k];
+        ga.jobs = 1;
+        int64_t grid = (int64_t)n * jobs[k].blocks;
+        if (k == 0 && jobs[1].out && types[0] == types[1]) {
+            ga.job[1] = jobs[1];
+            ga.jobs = 2;
+            grid += (int64_t)n * jobs[1].blocks;
+            ++k;
+        }
+        const cudaError_t e = types[k] == MINW_BF16 ? launch_grads<uint16_t>(ga, grid, s) : launch_grads<float>(ga, grid, s);
+        if (e != cudaSuccess) return launch_failed();
+    }
+    return launch_status();
+}
+
+}  // extern "C"

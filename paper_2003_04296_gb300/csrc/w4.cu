@@ -33,6 +33,7 @@
 
 #include "kernels.cuh"
 #include "values.cuh"
+#include "w4.cuh"
 
 namespace cg = cooperative_groups;
 
@@ -106,6 +107,7 @@ struct Args {
     const uint8_t *codes;
     const uint16_t *scales;
     const float *scale, *shift;
+    const float *add;                  // [T][O], or null
     void *y;
     int T, O, K, nb, groups, group;    // nb: blocks of 128 values of a row
     int x_bf16, y_bf16, act;
@@ -247,7 +249,7 @@ constexpr int UNIT_BYTES = 2048;      // 16 rows x two blocks (128 bytes of a ro
 template <int NT, int FL>
 __global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
     pdl_trigger();
-    pdl_wait();
+    if (!a.add) pdl_wait();            // what the kernel before this one wrote is needed at the end alone
     constexpr int RING = ring_of(NT);
     extern __shared__ __align__(16) uint8_t smem[];
     uint16_t *xs = reinterpret_cast<uint16_t *>(smem), *ss = reinterpret_cast<uint16_t *>(smem + a.scale_at);
@@ -392,6 +394,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
     cg::cluster_group cluster = cg::this_cluster();
     if (a.split > 1) cluster.sync();
     else __syncthreads();
+    if (a.add) pdl_wait();
     const int each = (rows + a.split - 1) / a.split, rr0 = rank * each, rr1 = min(rows, rr0 + each);
     for (int e = threadIdx.x; e < (rr1 - rr0) * tokens; e += blockDim.x) {
         const int q = e / tokens, tk = e - q * tokens, r = rr0 + q, o = row0 + r;
@@ -407,6 +410,7 @@ __global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
             for (int c = 1; c < 8; ++c) v[0] += v[c];
             sum += v[0];
         }
+        if (a.add) sum += a.add[(int64_t)(t0 + tk) * a.O + o];
         float z = fmaf(sum, a.scale ? a.scale[o] : 1.0f, a.shift ? a.shift[o] : 0.0f);
         with_act(a.act, [&](auto act) { z = act_value<act.value>(z); });
         const int64_t at = (int64_t)(t0 + tk) * a.ldy + o;
@@ -461,6 +465,87 @@ static cudaError_t launch_group(const Args &a, int group, dim3 grid, size_t smem
                                                                        : launch<NT, 4>(a, grid, smem, s);
 }
 
+minw_status check(const void *x, int x_type, int64_t ldx, int64_t T, const uint8_t *codes, const uint16_t *scales, int O, int K,
+                  int group, const float *scale, const float *shift, int act, const void *y, int y_type, int64_t ldy) {
+    if (!codes || !scales || (T != 0 && (!x || !y)) || T < 0 || O < 1 || K < 1 || ldx < K || ldy < O) return MINW_EINVAL;
+    if (!valid_group(group) || act < MINW_ACT_NONE || act > MINW_ACT_SILU) return MINW_EINVAL;
+    if ((x_type != MINW_F32 && x_type != MINW_BF16) || (y_type != MINW_F32 && y_type != MINW_BF16)) return MINW_EINVAL;
+    if (!aligned16(codes) || reinterpret_cast<uintptr_t>(scales) % 2 != 0 || !on_floats(scale, shift) ||
+        reinterpret_cast<uintptr_t>(x) % (x_type == MINW_BF16 ? 2 : 4) != 0 ||
+        reinterpret_cast<uintptr_t>(y) % (y_type == MINW_BF16 ? 2 : 4) != 0)
+        return MINW_EINVAL;
+    if (K > (1 << 28) || group > (1 << 28) || O > (1 << 28)) return MINW_EUNSUPPORTED;
+    return MINW_OK;
+}
+
+minw_status matvec(const void *x, int x_type, int64_t ldx, int T, const uint8_t *codes, const uint16_t *scales, int O, int K,
+                   int group, const float *scale, const float *shift, int act, void *y, int y_type, int64_t ldy,
+                   const float *add, cudaStream_t s) {
+    Args a{};
+    a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy; a.codes = codes; a.scales = scales; a.scale = scale; a.shift = shift;
+    a.add = add; a.T = T; a.O = O; a.K = K; a.nb = (K + 127) / 128; a.groups = (K + group - 1) / group; a.group = group;
+    a.by_blocks = Div(group >= 128 ? group / 128 : 1);
+    a.x_bf16 = x_type == MINW_BF16; a.y_bf16 = y_type == MINW_BF16; a.act = act;
+    a.parts = a.x_bf16 ? 1 : 3;
+    const int most = 32 / a.parts;                                   // vectors of a pass: 32 columns
+    a.tokens = T < most ? T : most;
+    const int passes = (T + a.tokens - 1) / a.tokens, cols = a.tokens * a.parts, NT = (cols + 7) / 8;
+    if (passes > 65535) return MINW_EUNSUPPORTED;
+    const int units = (a.nb + 1) / 2, sms = num_sms() > 0 ? num_sms() : 152;
+    // wr warps along the rows (16 each) and wk along K make a CTA, `split` CTAs a cluster, which splits K too: the
+    // choice with the least estimated clocks.  An SM holds two CTAs of up to 100 KB of shared memory: the rings, and x
+    // and scales of as many units (whole rounds of the warps) as fit.  Measured on one to 48 columns (T = 1: 1024 x
+    // 1024 to 16384 x 16384): fourteen warps of an SM take 18 / (1 + 0.07 columns) bytes of codes a clock, fewer
+    // warps their share of that; a wave of CTAs has a fixed part, so have a cluster and each further filling of x.
+    float best = 1e30f;
+    // with the share of the SMs' places that clusters of this size can take (cudaOccupancyMaxActiveClusters)
+    static const struct { int n; float places; } splits[] = {{1, 1.0f}, {2, 1.0f}, {3, 0.957f}, {4, 0.974f}, {6, 0.908f}, {8, 0.948f}};
+    const float x_rate = a.tokens * 256 * (a.x_bf16 ? 0.03f : 0.14f), cap = 18.0f / (1.0f + 0.07f * cols);
+    int tiles = 0;
+    for (int wr = 1; wr <= WARPS; ++wr) {
+        const int wk = WARPS / wr, warps = wr * wk, rows = (O + 16 * wr - 1) / (16 * wr);
+        const int room = 100 * 1024 - warps * ring_of(NT) * UNIT_BYTES - cols * 64 - 512 - wr * 16 * 32;
+        const int fit = room / (cols * 512 + wr * 32 * (group >= 256 ? 1 : 256 / group));
+        const float one = cap * (warps / 14.0f), two = cap * (warps >= 7 ? 1.0f : warps / 7.0f);
+        for (const auto &sp : splits) {
+            const int split = sp.n, upc = (units + split - 1) / split, slots = (int)(2 * sms * sp.places);
+            if (upc * (split - 1) >= units) break;                                // a CTA without a unit
+            const int xunits = upc <= fit ? upc : fit / wk * wk;
+            if (xunits == 0) continue;
+            const float bytes = (float)((upc + wk - 1) / wk * wk * wr * UNIT_BYTES);    // the warps' last units are whole
+            const float fixed = 1500.0f * ((upc + xunits - 1) / xunits) + (split > 1 ? 1000.0f : 0.0f);
+            const float t1 = bytes / one + upc * x_rate + fixed, t2 = 2 * (bytes / two + upc * x_rate) + fixed;
+            const int64_t ctas = (int64_t)rows * split * passes, rest = ctas % slots;
+            const float t = (float)(ctas / slots) * t2 + (rest > sms ? t2 : rest > 0 ? t1 : 0.0f);
+            if (t < best) {
+                best = t;
+                a.wr = wr;
+                a.wk = wk;
+                a.split = split;
+                a.upc = upc;
+                a.xunits = xunits;
+                tiles = rows;
+            }
+        }
+    }
+    const int ring = a.wr * a.wk * ring_of(NT) * UNIT_BYTES;
+    a.xpitch = a.xunits * 256 + 32;
+    a.by_row = Div((uint32_t)a.xunits * (a.x_bf16 ? 32 : 64));
+    a.scale_pitch = ((group >= 256 ? a.xunits * 256 / group + 2 : a.xunits * (256 / group)) + 7) / 8 * 8;
+    a.by_eights = Div((uint32_t)a.scale_pitch / 8);
+    a.scale_at = (cols * a.xpitch + 256) * 2;
+    a.ring_at = a.scale_at + a.wr * 16 * a.scale_pitch * 2;
+    size_t smem = (size_t)a.ring_at + ring;
+    const size_t red = (size_t)a.wr * a.wk * 16 * 8 * NT * sizeof(float);
+    if (smem < red) smem = red;
+    const dim3 grid((unsigned)(tiles * a.split), (unsigned)passes);
+    const cudaError_t e = NT == 1 ? launch_group<1>(a, group, grid, smem, s)
+                        : NT == 2 ? launch_group<2>(a, group, grid, smem, s)
+                        : NT == 3 ? launch_group<3>(a, group, grid, smem, s)
+                                  : launch_group<4>(a, group, grid, smem, s);
+    return e == cudaSuccess ? launch_status() : launch_failed();
+}
+
 }  // namespace w4
 }  // namespace minw
 
@@ -488,79 +573,10 @@ minw_status minw_pack_w4(const void *w, int32_t type, int32_t O, int32_t K, int3
 minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, int32_t T, const uint8_t *codes,
                            const uint16_t *scales, int32_t O, int32_t K, int32_t group, const float *scale,
                            const float *shift, int32_t act, void *y, int32_t y_type, int64_t ldy, void *stream) {
-    if (!codes || !scales || (T != 0 && (!x || !y)) || T < 0 || O < 1 || K < 1 || ldx < K || ldy < O) return MINW_EINVAL;
-    if (!w4::valid_group(group) || act < MINW_ACT_NONE || act > MINW_ACT_SILU) return MINW_EINVAL;
-    if ((x_type != MINW_F32 && x_type != MINW_BF16) || (y_type != MINW_F32 && y_type != MINW_BF16)) return MINW_EINVAL;
-    if (!aligned16(codes) || reinterpret_cast<uintptr_t>(scales) % 2 != 0 || !on_floats(scale, shift) ||
-        reinterpret_cast<uintptr_t>(x) % (x_type == MINW_BF16 ? 2 : 4) != 0 ||
-        reinterpret_cast<uintptr_t>(y) % (y_type == MINW_BF16 ? 2 : 4) != 0)
-        return MINW_EINVAL;
-    if (K > (1 << 28) || group > (1 << 28) || O > (1 << 28)) return MINW_EUNSUPPORTED;
-    if (T == 0) return MINW_OK;
-    w4::Args a{};
-    a.x = x; a.ldx = ldx; a.y = y; a.ldy = ldy; a.codes = codes; a.scales = scales; a.scale = scale; a.shift = shift;
-    a.T = T; a.O = O; a.K = K; a.nb = (K + 127) / 128; a.groups = (K + group - 1) / group; a.group = group;
-    a.by_blocks = Div(group >= 128 ? group / 128 : 1);
-    a.x_bf16 = x_type == MINW_BF16; a.y_bf16 = y_type == MINW_BF16; a.act = act;
-    a.parts = a.x_bf16 ? 1 : 3;
-    const int most = 32 / a.parts;                                   // vectors of a pass: 32 columns
-    a.tokens = T < most ? T : most;
-    const int passes = (T + a.tokens - 1) / a.tokens, cols = a.tokens * a.parts, NT = (cols + 7) / 8;
-    if (passes > 65535) return MINW_EUNSUPPORTED;
-    const int units = (a.nb + 1) / 2, sms = num_sms() > 0 ? num_sms() : 152;
-    // wr warps along the rows (16 each) and wk along K make a CTA, `split` CTAs a cluster, which splits K too: the
-    // choice with the least estimated clocks.  An SM holds two CTAs of up to 100 KB of shared memory: the rings, and x
-    // and scales of as many units (whole rounds of the warps) as fit.  Measured on one to 48 columns (T = 1: 1024 x
-    // 1024 to 16384 x 16384): fourteen warps of an SM take 18 / (1 + 0.07 columns) bytes of codes a clock, fewer
-    // warps their share of that; a wave of CTAs has a fixed part, so have a cluster and each further filling of x.
-    float best = 1e30f;
-    // with the share of the SMs' places that clusters of this size can take (cudaOccupancyMaxActiveClusters)
-    static const struct { int n; float places; } splits[] = {{1, 1.0f}, {2, 1.0f}, {3, 0.957f}, {4, 0.974f}, {6, 0.908f}, {8, 0.948f}};
-    const float x_rate = a.tokens * 256 * (a.x_bf16 ? 0.03f : 0.14f), cap = 18.0f / (1.0f + 0.07f * cols);
-    int tiles = 0;
-    for (int wr = 1; wr <= w4::WARPS; ++wr) {
-        const int wk = w4::WARPS / wr, warps = wr * wk, rows = (O + 16 * wr - 1) / (16 * wr);
-        const int room = 100 * 1024 - warps * w4::ring_of(NT) * w4::UNIT_BYTES - cols * 64 - 512 - wr * 16 * 32;
-        const int fit = room / (cols * 512 + wr * 32 * (group >= 256 ? 1 : 256 / group));
-        const float one = cap * (warps / 14.0f), two = cap * (warps >= 7 ? 1.0f : warps / 7.0f);
-        for (const auto &sp : splits) {
-            const int split = sp.n, upc = (units + split - 1) / split, slots = (int)(2 * sms * sp.places);
-            if (upc * (split - 1) >= units) break;                                // a CTA without a unit
-            const int xunits = upc <= fit ? upc : fit / wk * wk;
-            if (xunits == 0) continue;
-            const float bytes = (float)((upc + wk - 1) / wk * wk * wr * w4::UNIT_BYTES);    // the warps' last units are whole
-            const float fixed = 1500.0f * ((upc + xunits - 1) / xunits) + (split > 1 ? 1000.0f : 0.0f);
-            const float t1 = bytes / one + upc * x_rate + fixed, t2 = 2 * (bytes / two + upc * x_rate) + fixed;
-            const int64_t ctas = (int64_t)rows * split * passes, rest = ctas % slots;
-            const float t = (float)(ctas / slots) * t2 + (rest > sms ? t2 : rest > 0 ? t1 : 0.0f);
-            if (t < best) {
-                best = t;
-                a.wr = wr;
-                a.wk = wk;
-                a.split = split;
-                a.upc = upc;
-                a.xunits = xunits;
-                tiles = rows;
-            }
-        }
-    }
-    const int ring = a.wr * a.wk * w4::ring_of(NT) * w4::UNIT_BYTES;
-    a.xpitch = a.xunits * 256 + 32;
-    a.by_row = Div((uint32_t)a.xunits * (a.x_bf16 ? 32 : 64));
-    a.scale_pitch = ((group >= 256 ? a.xunits * 256 / group + 2 : a.xunits * (256 / group)) + 7) / 8 * 8;
-    a.by_eights = Div((uint32_t)a.scale_pitch / 8);
-    a.scale_at = (cols * a.xpitch + 256) * 2;
-    a.ring_at = a.scale_at + a.wr * 16 * a.scale_pitch * 2;
-    size_t smem = (size_t)a.ring_at + ring;
-    const size_t red = (size_t)a.wr * a.wk * 16 * 8 * NT * sizeof(float);
-    if (smem < red) smem = red;
-    const dim3 grid((unsigned)(tiles * a.split), (unsigned)passes);
-    cudaStream_t s = (cudaStream_t)stream;
-    const cudaError_t e = NT == 1 ? w4::launch_group<1>(a, group, grid, smem, s)
-                        : NT == 2 ? w4::launch_group<2>(a, group, grid, smem, s)
-                        : NT == 3 ? w4::launch_group<3>(a, group, grid, smem, s)
-                                  : w4::launch_group<4>(a, group, grid, smem, s);
-    return e == cudaSuccess ? launch_status() : launch_failed();
+    const minw_status st = w4::check(x, x_type, ldx, T, codes, scales, O, K, group, scale, shift, act, y, y_type, ldy);
+    if (st != MINW_OK || T == 0) return st;
+    return w4::matvec(x, x_type, ldx, T, codes, scales, O, K, group, scale, shift, act, y, y_type, ldy, nullptr,
+                      (cudaStream_t)stream);
 }
 
 }  // extern "C"

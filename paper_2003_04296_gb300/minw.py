@@ -192,6 +192,13 @@ SIGNATURES = {
     "minw_orthogonal_workspace_bytes": (ctypes.c_size_t, [_P, _I32]),
     "minw_orthogonalize": (ctypes.c_int, [_P, _P, _I32, _I32, _P, ctypes.c_size_t, _P]),
     "minw_sgd_orthogonal": (ctypes.c_int, [_P, _P, _P, _I32, _I32, _F, _I32, _F, _P, ctypes.c_size_t, _P]),
+    "minw_adapters_workspace_bytes": (ctypes.c_size_t, [_I64, _I32, _I32, _I32, _I32, _I32]),
+    "minw_adapters": (ctypes.c_int, [_P, _I32, _I64, _I64, _I32, _P, _P, _P, _I32, _I32, _I32, _P, _P, _I32, _I64, _I32,
+                                     _P, _P, _I32, _P, _I32, _I64, _P, _P, ctypes.c_size_t, _P]),
+    "minw_w4_adapters": (ctypes.c_int, [_P, _I32, _I64, _I64, _P, _P, _I32, _I32, _I32, _P, _P, _P, _I32, _I32, _I32, _P,
+                                        _P, _P, _I32, _P, _I32, _I64, _P, ctypes.c_size_t, _P]),
+    "minw_adapters_backward": (ctypes.c_int, [_P, _I32, _I64, _I64, _I32, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P, _I32,
+                                              _I64, _I32, _P, _I64, _I32, _P, _P, _P, ctypes.c_size_t, _P]),
     "minw_pack_w4": (ctypes.c_int, [_P, _I32, _I32, _I32, _I32, _QP, _P, _P, _P, _P]),
     "minw_w4_matvec": (ctypes.c_int, [_P, _I32, _I64, _I32, _P, _P, _I32, _I32, _I32, _P, _P, _I32, _P, _I32, _I64,
                                       _P]),
@@ -1094,3 +1101,74 @@ def minw_w4_matvec(x, codes, scales, group, y, scale=None, shift=None, act=ACT_N
     _check(lib().minw_w4_matvec(px, _value_type(x), ldx, T, pc, ps, O, K, int(group), _f32(scale, O, "scale"),
                                 _f32(shift, O, "shift"), int(act), py, _value_type(y), ldy, _stream(stream)),
            "minw_w4_matvec")
+
+
+def minw_adapters_workspace_bytes(T, K, O, n, r, backward=False):
+    """Workspace bytes for T rows through n adapters of rank r, [K] -> [O]."""
+    return lib().minw_adapters_workspace_bytes(int(T), int(K), int(O), int(n), int(r), int(bool(backward)))
+
+
+def _pools(down, up, K, O):
+    """(down, up, type, n, r) of adapters down [n][r][K], up [n][r][O]."""
+    n, r = down.shape[0], down.shape[1]
+    if tuple(down.shape) != (n, r, K) or tuple(up.shape) != (n, r, O) or down.dtype != up.dtype:
+        raise ValueError("down [n][r][K] and up [n][r][O] of one type expected")
+    return _addr(down), _addr(up), _value_type(down), n, r
+
+
+def _ids(ids, T):
+    if ids.dtype != torch.int32 or ids.numel() != T:
+        raise ValueError(f"ids: {T} int32 values expected")
+    return _addr(ids)
+
+
+def minw_adapters(x, ids, down, up, y, alpha=None, base=None, scale=None, shift=None, act=ACT_NONE, h=None, workspace=None,
+                  stream=None):
+    """y [T][O] = act(scale (base + alpha[u] (x [T][K] down[u]^T) up[u]) + shift) with u = ids[t] of each row (no adapter
+    where it is no index of the pools); h fp32 [T][r] or None receives x down[u]^T.  x, y, base: rows may be wider."""
+    (T, K), (Ty, O) = x.shape, y.shape
+    if T != Ty or (base is not None and base.shape != y.shape):
+        raise ValueError("x, y and base: the same number of rows expected, y and base: the same columns")
+    px, ldx = _rows(x)
+    py, ldy = _rows(y)
+    pb, ldb = (None, 0) if base is None else _rows(base)
+    pd, pu, pt, n, r = _pools(down, up, K, O)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_adapters(px, _value_type(x), ldx, T, K, _ids(ids, T), pd, pu, pt, n, r, _f32(alpha, n, "alpha"), pb,
+                               0 if base is None else _value_type(base), ldb, O, _f32(scale, O, "scale"),
+                               _f32(shift, O, "shift"), int(act), py, _value_type(y), ldy, _f32(h, T * r, "h"), ws, ws_bytes,
+                               _stream(stream)), "minw_adapters")
+
+
+def minw_w4_adapters(x, codes, scales, group, ids, down, up, y, alpha=None, scale=None, shift=None, act=ACT_NONE,
+                     workspace=None, stream=None):
+    """minw_w4_matvec with each row's adapter: y = act(scale (x times the w4 weights + its adapter's term) + shift)."""
+    (T, K), (Ty, O) = x.shape, y.shape
+    if T != Ty:
+        raise ValueError("x and y: the same number of rows expected")
+    px, ldx = _rows(x)
+    py, ldy = _rows(y)
+    pc, ps = _w4(codes, scales, O, K, int(group))
+    pd, pu, pt, n, r = _pools(down, up, K, O)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_w4_adapters(px, _value_type(x), ldx, T, pc, ps, O, K, int(group), _ids(ids, T), pd, pu, pt, n, r,
+                                  _f32(alpha, n, "alpha"), _f32(scale, O, "scale"), _f32(shift, O, "shift"), int(act), py,
+                                  _value_type(y), ldy, ws, ws_bytes, _stream(stream)), "minw_w4_adapters")
+
+
+def minw_adapters_backward(x, ids, down, up, h, dy, ddown=None, dup=None, dx=None, alpha=None, accumulate=False,
+                           workspace=None, stream=None):
+    """Gradients of minw_adapters' term from dy [T][O] (that of base + the term) and the forward's h: dx (x's type; added
+    to where accumulate is set), ddown and dup (fp32, of the pools' shapes); each may be None."""
+    (T, K), (Ty, O) = x.shape, dy.shape
+    if T != Ty or (dx is not None and (dx.shape != x.shape or dx.dtype != x.dtype)):
+        raise ValueError("x and dy: the same number of rows expected, dx: x's shape and type")
+    px, ldx = _rows(x)
+    pg, ldg = _rows(dy)
+    po, ldo = (None, 0) if dx is None else _rows(dx)
+    pd, pu, pt, n, r = _pools(down, up, K, O)
+    ws, ws_bytes = _scratch(workspace)
+    _check(lib().minw_adapters_backward(px, _value_type(x), ldx, T, K, _ids(ids, T), pd, pu, pt, n, r,
+                                        _f32(alpha, n, "alpha"), _f32(h, T * r, "h"), pg, _value_type(dy), ldg, O, po, ldo,
+                                        int(bool(accumulate)), _f32(ddown, n * r * K, "ddown"), _f32(dup, n * r * O, "dup"),
+                                        ws, ws_bytes, _stream(stream)), "minw_adapters_backward")
