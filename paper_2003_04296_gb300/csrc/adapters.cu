@@ -5,10 +5,9 @@
 //
 // Rows of one user share its matrices, so rows are taken in tiles of one user: where a
 // tile holds all rows, every tile finds its own (tile t belongs to the first row of its
-// user, the others leave); else a plan sorts the rows by user first.  A cluster takes a
-// tile.  Its blocks share the columns of x (K), add up their parts of h through each
-// other's shared memory, and share the columns of y (O): one launch, x, base and y
-// move once, h not at all.  The backward's v_t = alpha_u up_u dy_t, dx_t = down_u^T v_t is the
+// user, the others leave) and a cluster takes it: its blocks share the columns of x (K), add
+// up their parts of h through each other's shared memory, and share the columns of y (O), one
+// launch.  Else a plan sorts the rows by user, and the two products are a launch each.  The backward's v_t = alpha_u up_u dy_t, dx_t = down_u^T v_t is the
 // same kernel with the matrices exchanged; the matrices' gradients are sums over a user's rows,
 //   ddown_u = sum v_t x_t^T,   dup_u = alpha_u sum h_t dy_t^T,   a kernel of their own.
 //
@@ -231,13 +230,14 @@ struct Args {
     float *h;                                // [T][r] by row, or null: in p1^T
     const float *h_in;                       // backward: [T][r] by row ...
     float *ht, *vt;                          // ... and [r][T] by sorted row, alpha times h_in and the values here
+    uint16_t *hp;                            // [3][T][rp] by sorted row: alpha times the values here, in parts
     int64_t ld_in, ld_base, ld_out;
     int T, D, E, n, r, rp;                   // rp: r rounded up to 16
     int act, base_bf16, out_bf16;
     int in_vec, p1_vec, p2_vec, base_vec, out_vec;        // whole rows on 16-byte boundaries
     int fine;                                // products of parts down to 2^-24
     int split;                               // blocks of a cluster
-    Plan plan;                               // order null: every tile finds its rows
+    Plan plan;
 };
 
 template <typename V>
@@ -285,26 +285,229 @@ __device__ __forceinline__ void store16(void *p, int64_t at, int left, bool vec,
     }
 }
 
-// MT: tiles of 16 rows, NT: tiles of 8 of r in one go.  Shared memory: the warps' sums, the block's, h in parts.
-template <typename TI, typename TP, int MT, int NT>
-__global__ void __launch_bounds__(THREADS, 1) adapter_kernel(const __grid_constant__ Args a) {
-    constexpr int M = 16 * MT, R = 8 * NT, PI = parts_of<TI>(), PP = parts_of<TP>();
-    extern __shared__ __align__(16) uint8_t smem[];
-    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R]
-    float *part = red + WARPS * M * R;                                   // [M][rp]
-    uint16_t *hs = reinterpret_cast<uint16_t *>(part + M * a.rp);        // [3][M][rp + 8]
-    __shared__ int rows[M];
-    __shared__ int tile_id, tile_rows, tile_start;
+// acc[m][j] += in[rows][k] p1[j][k] over this warp's share of the blocks b0 .. b1 of 32 values: lane t's eight values of a row are
+// the operands of two products.  DEPTH blocks are on their way at a time.
+template <typename TI, typename TP, int MT, int NT, int DEPTH>
+__device__ __forceinline__ void narrow(const Args &a, const int *rows, int count, const TP *p1, int ranks, int b0, int b1,
+                                       float (*acc)[NT][4]) {
+    constexpr int PI = parts_of<TI>(), PP = parts_of<TP>();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const TI *in = static_cast<const TI *>(a.in);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+    const TI *row[MT][2];
+    bool live[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = 16 * m + 8 * i + g;
+            live[m][i] = e < count;
+            row[m][i] = in + (live[m][i] ? rows[e] : 0) * a.ld_in + 8 * t;
+        }
+    for (int b = b0 + warp * DEPTH; b < b1; b += WARPS * DEPTH) {
+        Eight<TI> x[DEPTH][MT][2];
+        Eight<TP> p[DEPTH][NT];
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            const int k = 32 * (b + d), left = b + d < b1 ? a.D - k - 8 * t : 0;
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (live[m][i] && left > 0) x[d][m][i].load(row[m][i] + k, left, a.in_vec);
+                    else x[d][m][i].zero();
+                }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if (8 * j + g < ranks && left > 0) p[d][j].load(p1 + (int64_t)(8 * j + g) * a.D + k + 8 * t, left, a.p1_vec);
+                else p[d][j].zero();
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            uint32_t xp[MT][2][PI][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) along(x[d][m][i], xp[m][i]);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                uint32_t pp[PP][4];
+                along(p[d][j], pp);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int l = 2; l >= 0; --l)                                 // the smallest products first
+#pragma unroll
+                        for (int q = 0; q <= l; ++q) {
+                            const int v = l - q;
+                            if (q >= PI || v >= PP || (l == 2 && !a.fine)) continue;
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) {
+                                const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
+                                                       xp[m][1][q][2 * s + 1]};
+                                mma(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
+                            }
+                        }
+            }
+        }
+    }
+}
+
+// The warps' sums, in their order: part[m][j], rows `pitch` apart.
+template <int MT, int NT>
+__device__ __forceinline__ void add_warps(float (*acc)[NT][4], float *red, float *part, int pitch, int ranks) {
+    constexpr int M = 16 * MT, R = 8 * NT;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    __syncthreads();                          // an earlier round's sums have been read
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            float *d = red + (warp * M + 16 * m + g) * R + 8 * j + 2 * t;
+            *reinterpret_cast<float2 *>(d) = make_float2(acc[m][j][0], acc[m][j][1]);
+            *reinterpret_cast<float2 *>(d + 8 * R) = make_float2(acc[m][j][2], acc[m][j][3]);
+        }
+    __syncthreads();
+    for (int e = threadIdx.x; e < M * R; e += THREADS) {
+        float v[WARPS];
+#pragma unroll
+        for (int w = 0; w < WARPS; ++w) v[w] = red[w * M * R + e];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) v[0] += v[w];
+        if (e % R < ranks) part[e / R * pitch + e % R] = v[0];
+    }
+}
+
+// The blocks' parts at p, in their order.
+__device__ __forceinline__ float add_blocks(const cg::cluster_group &cluster, float *p, int split) {
+    float v[8];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) v[c] = split == 1 ? (c == 0 ? *p : 0.0f) : c < split ? *cluster.map_shared_rank(p, c) : 0.0f;
+#pragma unroll
+    for (int c = 1; c < 8; ++c) v[0] += v[c];
+    return v[0];
+}
+
+// Columns 64 b .. + 63 of ME tiles of 16 rows from row m0 of the tile on: h (parts in shared memory, [3][hrows][hpitch]) times the
+// user's p2, and the epilogue.  KS steps of 16 of r are loaded at a time.
+template <typename TP, int ME, int KS>
+__device__ __forceinline__ void widen(const Args &a, const int *rows, int count, int m0, int id, int b, const uint16_t *hs,
+                                      int hrows, int hpitch) {
+    constexpr int PP = parts_of<TP>();
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    float acc[ME][8][4];
+#pragma unroll
+    for (int m = 0; m < ME; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+    if (id >= 0) {
+        const int c = 64 * b + 8 * g, left = a.E - c;
+        const TP *p2 = static_cast<const TP *>(a.p2) + (int64_t)id * a.r * a.E + c;
+        for (int k0 = 0; k0 < a.rp; k0 += 16 * KS) {
+            Eight<TP> p[KS][4];
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = k0 + 16 * s + 2 * t + (i & 1) + 8 * (i >> 1);
+                    if (j < a.r && left > 0) p[s][i].load(p2 + (int64_t)j * a.E, left, a.p2_vec);
+                    else p[s][i].zero();
+                }
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                const int k = k0 + 16 * s;
+                if (k >= a.rp) break;
+                uint32_t f[ME][3][4];
+#pragma unroll
+                for (int m = 0; m < ME; ++m)
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) {
+                        const uint16_t *h = hs + (q * hrows + m0 + 16 * m + g) * hpitch + k + 2 * t;
+                        f[m][q][0] = *reinterpret_cast<const uint32_t *>(h);
+                        f[m][q][1] = *reinterpret_cast<const uint32_t *>(h + 8 * hpitch);
+                        f[m][q][2] = *reinterpret_cast<const uint32_t *>(h + 8);
+                        f[m][q][3] = *reinterpret_cast<const uint32_t *>(h + 8 * hpitch + 8);
+                    }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t q0[PP], q1[PP];
+                    across(p[s][0], p[s][1], i, q0);
+                    across(p[s][2], p[s][3], i, q1);
+#pragma unroll
+                    for (int l = 2; l >= 0; --l)
+#pragma unroll
+                        for (int q = 0; q <= l; ++q) {
+                            const int v = l - q;
+                            if (v >= PP || (l == 2 && !a.fine)) continue;
+#pragma unroll
+                            for (int m = 0; m < ME; ++m) mma(acc[m][i], f[m][q], q0[v], q1[v]);
+                        }
+                }
+            }
+        }
+    }
+    const int c = 64 * b + 16 * t, left = a.E - c;
+    if (left > 0) {
+#pragma unroll
+        for (int m = 0; m < ME; ++m)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int e = m0 + 16 * m + 8 * i + g;
+                if (e >= count) continue;
+                const int64_t row = rows[e];
+                float z[16], f[16];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    z[k] = acc[m][k][2 * i];
+                    z[8 + k] = acc[m][k][2 * i + 1];
+                }
+                if (a.base) {
+                    if (a.base_bf16) load16<uint16_t>(a.base, row * a.ld_base + c, left, a.base_vec, f);
+                    else load16<float>(a.base, row * a.ld_base + c, left, a.base_vec, f);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) z[k] += f[k];
+                }
+                if (a.scale || a.shift) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        if (k < left) z[k] = fmaf(z[k], a.scale ? a.scale[c + k] : 1.0f, a.shift ? a.shift[c + k] : 0.0f);
+                }
+                with_act(a.act, [&](auto act) {
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) z[k] = act_value<act.value>(z[k]);
+                });
+                if (a.out_bf16) store16<uint16_t>(a.out, row * a.ld_out + c, left, a.out_vec, z);
+                else store16<float>(a.out, row * a.ld_out + c, left, a.out_vec, z);
+            }
+    }
+    __syncwarp();
+}
+
+constexpr int SMALL = 64;                     // rows that need no plan
+
+// All of a few rows, one launch: cluster `tile` takes the rows of row `tile`'s user, if it is the first of them, 16 at a time.
+template <typename TI, typename TP, int NT>
+__global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__ Args a) {
+    constexpr int R = 8 * NT, BYTES = sizeof(TI) + sizeof(TP), DEPTH = NT == 2 ? 16 / BYTES : NT == 4 ? 8 / BYTES : 1;
+    extern __shared__ __align__(16) uint8_t smem[];
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][R]
+    float *part = red + WARPS * 16 * R;                                  // [SMALL][rp]
+    uint16_t *hs = reinterpret_cast<uint16_t *>(part + SMALL * a.rp);    // [3][SMALL][rp + 8]
+    __shared__ int rows[SMALL];
+    __shared__ int tile_id, tile_rows;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
     pdl_wait();
-    pdl_trigger();                            // dependents may rely on what came before this kernel
-    if (a.plan.order) {
-        if (tile >= *a.plan.tiles_n) return;
-        const Tile x = a.plan.tiles[tile];
-        if (threadIdx.x == 0) { tile_id = x.id; tile_rows = x.count; tile_start = x.start; }
-        if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
-    } else if (warp == 0) {                   // at most 64 rows
+    pdl_trigger();                            // a dependent may rely on what came before this kernel
+    if (warp == 0) {
         const int mine = user_of(a.ids[tile], a.n);
         const int lo = lane < a.T ? user_of(a.ids[lane], a.n) : -1, hi = lane + 32 < a.T ? user_of(a.ids[lane + 32], a.n) : -1;
         const uint32_t ml = __ballot_sync(0xffffffffu, lo == mine), mh = __ballot_sync(0xffffffffu, hi == mine);
@@ -314,202 +517,124 @@ __global__ void __launch_bounds__(THREADS, 1) adapter_kernel(const __grid_consta
         if (lane == 0) {
             tile_id = mine < a.n ? mine : -1;
             tile_rows = tile == (ml ? __ffs(ml) - 1 : 31 + __ffs(mh)) ? __popc(ml) + __popc(mh) : 0;
-            tile_start = 0;
         }
     }
     __syncthreads();
     const int count = tile_rows, id = tile_id;
-    if (count == 0) return;                   // an earlier row's tile; the whole cluster leaves
+    if (count == 0) return;                   // the whole cluster leaves
     cg::cluster_group cluster = cg::this_cluster();
-
     if (id >= 0) {
         const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
-        for (int j0 = 0; j0 < a.r; j0 += R) {
-            float acc[MT][NT][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-            const TP *p1 = static_cast<const TP *>(a.p1) + ((int64_t)id * a.r + j0) * a.D;
-            const TI *in = static_cast<const TI *>(a.in);
-            for (int b = b0 + warp; b < b1; b += WARPS) {
-                const int k = 32 * b + 8 * t, left = a.D - k;
-                Eight<TI> x[MT][2];
-                Eight<TP> p[NT];
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int e = 16 * m + 8 * i + g;
-                        if (e < count) x[m][i].load(in + rows[e] * a.ld_in + k, left, a.in_vec);
-                        else x[m][i].zero();
-                    }
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    if (j0 + 8 * j + g < a.r) p[j].load(p1 + (int64_t)(8 * j + g) * a.D + k, left, a.p1_vec);
-                    else p[j].zero();
-                }
-                uint32_t xp[MT][2][PI][4];
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) along(x[m][i], xp[m][i]);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    uint32_t pp[PP][4];
-                    along(p[j], pp);
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int l = 2; l >= 0; --l)                     // the smallest products first
-#pragma unroll
-                            for (int q = 0; q <= l; ++q) {
-                                const int v = l - q;
-                                if (q >= PI || v >= PP || (l == 2 && !a.fine)) continue;
-#pragma unroll
-                                for (int m = 0; m < MT; ++m) {
-                                    const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
-                                                           xp[m][1][q][2 * s + 1]};
-                                    mma(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
-                                }
-                            }
-                }
+        for (int m0 = 0; m0 < count; m0 += 16)
+            for (int j0 = 0; j0 < a.r; j0 += R) {
+                float acc[1][NT][4];
+                narrow<TI, TP, 1, NT, DEPTH>(a, rows + m0, count - m0, static_cast<const TP *>(a.p1) + ((int64_t)id * a.r + j0) * a.D,
+                                             a.r - j0, b0, b1, acc);
+                add_warps<1, NT>(acc, red, part + m0 * a.rp + j0, a.rp, a.rp - j0);
             }
-            __syncthreads();                  // an earlier round's sums have been read
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    float *d = red + (warp * M + 16 * m + g) * R + 8 * j + 2 * t;
-                    *reinterpret_cast<float2 *>(d) = make_float2(acc[m][j][0], acc[m][j][1]);
-                    *reinterpret_cast<float2 *>(d + 8 * R) = make_float2(acc[m][j][2], acc[m][j][3]);
-                }
-            __syncthreads();
-            for (int e = threadIdx.x; e < M * R; e += THREADS) {
-                float v[WARPS];
-#pragma unroll
-                for (int w = 0; w < WARPS; ++w) v[w] = red[w * M * R + e];
-#pragma unroll
-                for (int w = 1; w < WARPS; ++w) v[0] += v[w];
-                const int j = j0 + e % R;
-                if (j < a.rp) part[e / R * a.rp + j] = v[0];
-            }
-        }
         if (a.split > 1) cluster.sync();
         else __syncthreads();
-        // h from all blocks' parts, in their order
         const float alpha = a.alpha ? a.alpha[id] : 1.0f;
-        for (int e = threadIdx.x; e < M * a.rp; e += THREADS) {
-            float v[8];
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                v[c] = a.split == 1 ? (c == 0 ? part[e] : 0.0f) : c < a.split ? *cluster.map_shared_rank(part + e, c) : 0.0f;
-#pragma unroll
-            for (int c = 1; c < 8; ++c) v[0] += v[c];
+        for (int e = threadIdx.x; e < (count + 15) / 16 * 16 * a.rp; e += THREADS) {
+            const float v = add_blocks(cluster, part + e, a.split);
             const int m = e / a.rp, j = e - m * a.rp;
-            if (rank == 0 && m < count && j < a.r) {
-                if (a.h) a.h[(int64_t)rows[m] * a.r + j] = v[0];
-                if (a.vt) a.vt[(int64_t)j * a.T + tile_start + m] = alpha * v[0];
-                if (a.ht) a.ht[(int64_t)j * a.T + tile_start + m] = alpha * a.h_in[(int64_t)rows[m] * a.r + j];
-            }
+            if (a.h && rank == 0 && m < count && j < a.r) a.h[(int64_t)rows[m] * a.r + j] = v;
             uint32_t s[3];
-            split2(__float_as_uint(alpha * v[0]), 0u, s);
+            split2(__float_as_uint(alpha * v), 0u, s);
 #pragma unroll
-            for (int q = 0; q < 3; ++q) hs[(q * M + m) * (a.rp + 8) + j] = (uint16_t)s[q];
+            for (int q = 0; q < 3; ++q) hs[(q * SMALL + m) * (a.rp + 8) + j] = (uint16_t)s[q];
         }
         if (a.split > 1) cluster_done_reading();
         __syncthreads();
     } else if (rank == 0 && a.h) {
         for (int e = threadIdx.x; e < count * a.r; e += THREADS) a.h[(int64_t)rows[e / a.r] * a.r + e % a.r] = 0.0f;
     }
-
-    constexpr int ME = MT < 2 ? MT : 2;       // tiles of 16 rows at a time
     const int eblocks = (a.E + 63) / 64;
-    for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS) {
-        for (int m0 = 0; m0 < MT && 16 * m0 < count; m0 += ME) {
-            float acc[ME][8][4];
-#pragma unroll
-            for (int m = 0; m < ME; ++m)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-            if (id >= 0) {
-                const int c = 64 * b + 8 * g, left = a.E - c;
-                const TP *p2 = static_cast<const TP *>(a.p2) + (int64_t)id * a.r * a.E + c;
-                for (int k = 0; k < a.rp; k += 16) {
-                    Eight<TP> p[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int j = k + 2 * t + (i & 1) + 8 * (i >> 1);
-                        if (j < a.r && left > 0) p[i].load(p2 + (int64_t)j * a.E, left, a.p2_vec);
-                        else p[i].zero();
-                    }
-                    uint32_t f[ME][3][4];
-#pragma unroll
-                    for (int m = 0; m < ME; ++m)
-#pragma unroll
-                        for (int q = 0; q < 3; ++q) {
-                            const uint16_t *h = hs + (q * M + 16 * (m0 + m) + g) * (a.rp + 8) + k + 2 * t;
-                            f[m][q][0] = *reinterpret_cast<const uint32_t *>(h);
-                            f[m][q][1] = *reinterpret_cast<const uint32_t *>(h + 8 * (a.rp + 8));
-                            f[m][q][2] = *reinterpret_cast<const uint32_t *>(h + 8);
-                            f[m][q][3] = *reinterpret_cast<const uint32_t *>(h + 8 * (a.rp + 8) + 8);
-                        }
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        uint32_t q0[PP], q1[PP];
-                        across(p[0], p[1], i, q0);
-                        across(p[2], p[3], i, q1);
-#pragma unroll
-                        for (int l = 2; l >= 0; --l)
-#pragma unroll
-                            for (int q = 0; q <= l; ++q) {
-                                const int v = l - q;
-                                if (v >= PP || (l == 2 && !a.fine)) continue;
-#pragma unroll
-                                for (int m = 0; m < ME; ++m) mma(acc[m][i], f[m][q], q0[v], q1[v]);
-                            }
-                    }
-                }
-            }
-            const int c = 64 * b + 16 * t, left = a.E - c;
-            if (left <= 0) continue;
-#pragma unroll
-            for (int m = 0; m < ME; ++m)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int e = 16 * (m0 + m) + 8 * i + g;
-                    if (e >= count) continue;
-                    const int64_t row = rows[e];
-                    float z[16], f[16];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        z[k] = acc[m][k][2 * i];
-                        z[8 + k] = acc[m][k][2 * i + 1];
-                    }
-                    if (a.base) {
-                        if (a.base_bf16) load16<uint16_t>(a.base, row * a.ld_base + c, left, a.base_vec, f);
-                        else load16<float>(a.base, row * a.ld_base + c, left, a.base_vec, f);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) z[k] += f[k];
-                    }
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (k < left) z[k] = fmaf(z[k], a.scale ? a.scale[c + k] : 1.0f, a.shift ? a.shift[c + k] : 0.0f);
-                    with_act(a.act, [&](auto act) {
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) z[k] = act_value<act.value>(z[k]);
-                    });
-                    if (a.out_bf16) store16<uint16_t>(a.out, row * a.ld_out + c, left, a.out_vec, z);
-                    else store16<float>(a.out, row * a.ld_out + c, left, a.out_vec, z);
-                }
-        }
-    }
+    for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS)
+        for (int m0 = 0; m0 < count; m0 += 16) widen<TP, 1, 1>(a, rows, count, m0, id, b, hs, SMALL, a.rp + 8);
     __syncwarp();
     if (a.split > 1 && id >= 0) cluster_leave();
+}
+
+// The plan's tiles, first half: h, alpha h in parts for the second half, and what the gradients need.
+template <typename TI, typename TP, int MT, int NT>
+__global__ void __launch_bounds__(THREADS, sizeof(TI) + sizeof(TP) == 4 ? 2 : 1) narrow_kernel(const __grid_constant__ Args a) {
+    constexpr int M = 16 * MT, R = 8 * NT;
+    extern __shared__ __align__(16) uint8_t smem[];
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R]
+    float *part = red + WARPS * M * R;                                   // [M][R]
+    __shared__ int rows[M];
+    const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
+    pdl_wait();
+    pdl_trigger();
+    if (tile >= *a.plan.tiles_n) return;
+    const Tile x = a.plan.tiles[tile];
+    if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
+    __syncthreads();
+    if (x.id < 0) {
+        if (rank == 0 && a.h)
+            for (int e = threadIdx.x; e < x.count * a.r; e += THREADS) a.h[(int64_t)rows[e / a.r] * a.r + e % a.r] = 0.0f;
+        return;
+    }
+    cg::cluster_group cluster = cg::this_cluster();
+    const float alpha = a.alpha ? a.alpha[x.id] : 1.0f;
+    const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
+    for (int j0 = 0; j0 < a.r; j0 += R) {
+        float acc[MT][NT][4];
+        narrow<TI, TP, MT, NT, 1>(a, rows, x.count, static_cast<const TP *>(a.p1) + ((int64_t)x.id * a.r + j0) * a.D, a.r - j0, b0, b1,
+                                  acc);
+        if (j0 > 0 && a.split > 1) cluster.sync();                       // others have read the last round's part
+        add_warps<MT, NT>(acc, red, part, R, R);
+        if (a.split > 1) cluster.sync();
+        else __syncthreads();
+        // a block finishes its share of the rows
+        const int each = (M + a.split - 1) / a.split, e1 = min(x.count, (rank + 1) * each) * R;
+        for (int e = rank * each * R + threadIdx.x; e < e1; e += THREADS) {
+            const int m = e / R, j = j0 + e % R;
+            if (j >= a.rp) continue;
+            const float v = add_blocks(cluster, part + e, a.split);
+            uint32_t s[3];
+            split2(__float_as_uint(alpha * v), 0u, s);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) a.hp[((int64_t)q * a.T + x.start + m) * a.rp + j] = (uint16_t)s[q];
+            if (j >= a.r) continue;
+            if (a.h) a.h[(int64_t)rows[m] * a.r + j] = v;
+            if (a.vt) a.vt[(int64_t)j * a.T + x.start + m] = alpha * v;
+            if (a.ht) a.ht[(int64_t)j * a.T + x.start + m] = alpha * a.h_in[(int64_t)rows[m] * a.r + j];
+        }
+    }
+    if (a.split > 1) {
+        __syncwarp();
+        cluster_done_reading();
+        cluster_leave();
+    }
+}
+
+constexpr int WIDE_WARPS = 4;
+
+// ... second half: a block takes 64 columns a warp of a tile.
+template <typename TP, int KS>
+__global__ void __launch_bounds__(32 * WIDE_WARPS) widen_kernel(const __grid_constant__ Args a, int chunks, int most) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    uint16_t *hs = reinterpret_cast<uint16_t *>(smem);                   // [3][most][rp + 8]
+    __shared__ int rows[64];
+    const int warp = threadIdx.x >> 5, tile = blockIdx.x / chunks, b = (blockIdx.x - tile * chunks) * WIDE_WARPS + warp;
+    pdl_trigger();
+    pdl_wait();
+    if (tile >= *a.plan.tiles_n) return;
+    const Tile x = a.plan.tiles[tile];
+    if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
+    const int hpitch = a.rp + 8, eights = a.rp / 8, parts = a.fine ? 3 : 2;
+    if (x.id >= 0)
+        for (int e = threadIdx.x; e < parts * most * eights; e += 32 * WIDE_WARPS) {
+            const int q = e / (most * eights), m = e / eights - q * most, j = 8 * (e % eights);
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (m < x.count) v = *reinterpret_cast<const uint4 *>(a.hp + ((int64_t)q * a.T + x.start + m) * a.rp + j);
+            *reinterpret_cast<uint4 *>(hs + (q * most + m) * hpitch + j) = v;
+        }
+    __syncthreads();
+    if (64 * b >= a.E) return;
+    for (int m0 = 0; m0 < x.count; m0 += 32) widen<TP, 2, KS>(a, rows, x.count, m0, x.id, b, hs, most, hpitch);
 }
 
 // ---------------------------------------------------------------------------
@@ -637,6 +762,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Rows of a tile: 64, where h in registers leaves room for them (r <= 32), else 32.
 static int rows_of(int r) { return r <= 32 ? 64 : 32; }
+static int rank_pitch(int r) { return (r + 15) / 16 * 16; }
 
 constexpr int W4_ROWS = 32;                  // rows of w4 products at a time
 
@@ -669,13 +795,7 @@ static minw_status make_plan(const Plan &p, const int *ids, int T, int n, int r,
                ? MINW_OK : launch_failed();
 }
 
-template <typename TI, typename TP, int MT, int NT>
-static cudaError_t launch(const Args &a, int64_t tiles, cudaStream_t s) {
-    constexpr int M = 16 * MT;
-    const int smem = WARPS * M * 8 * NT * 4 + M * a.rp * 4 + 3 * M * (a.rp + 8) * 2;
-    auto kern = adapter_kernel<TI, TP, MT, NT>;
-    constexpr int ranks = NT == 8 ? MAX_RANK : 8 * NT;
-    const int most = WARPS * M * 8 * NT * 4 + M * ranks * 4 + 3 * M * (ranks + 8) * 2;
+static cudaError_t launch_clusters(void (*kern)(Args), const Args &a, int64_t tiles, int smem, int most, cudaStream_t s) {
     if (!allow_shared(reinterpret_cast<const void *>(kern), most)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * a.split));
@@ -693,22 +813,42 @@ static cudaError_t launch(const Args &a, int64_t tiles, cudaStream_t s) {
     return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
+template <typename TI, typename TP, int NT>
+static cudaError_t launch_few(const Args &a, cudaStream_t s) {
+    constexpr int ranks = NT == 8 ? MAX_RANK : 8 * NT;
+    auto bytes = [](int rp) { return WARPS * 16 * 8 * NT * 4 + SMALL * rp * 4 + 3 * SMALL * (rp + 8) * 2; };
+    return launch_clusters(few_kernel<TI, TP, NT>, a, a.T, bytes(a.rp), bytes(ranks), s);
+}
+
+template <typename TI, typename TP, int MT, int NT>
+static cudaError_t launch_narrow(const Args &a, int64_t tiles, cudaStream_t s) {
+    constexpr int bytes = (WARPS + 1) * 16 * MT * 8 * NT * 4;
+    return launch_clusters(narrow_kernel<TI, TP, MT, NT>, a, tiles, bytes, bytes, s);
+}
+
 template <typename TI, typename TP>
-static cudaError_t launch_types(const Args &a, int64_t tiles, int most, cudaStream_t s) {
-    if (most <= 16)
-        return a.r <= 16 ? launch<TI, TP, 1, 2>(a, tiles, s) : a.r <= 32 ? launch<TI, TP, 1, 4>(a, tiles, s)
-                                                                         : launch<TI, TP, 1, 8>(a, tiles, s);
-    return a.r <= 16 ? launch<TI, TP, 4, 2>(a, tiles, s) : a.r <= 32 ? launch<TI, TP, 4, 4>(a, tiles, s)
-                                                                     : launch<TI, TP, 2, 8>(a, tiles, s);
+static cudaError_t launch_types(const Args &a, bool few, int64_t tiles, cudaStream_t s) {
+    if (few)
+        return a.r <= 16 ? launch_few<TI, TP, 2>(a, s) : a.r <= 32 ? launch_few<TI, TP, 4>(a, s) : launch_few<TI, TP, 8>(a, s);
+    return a.r <= 16 ? launch_narrow<TI, TP, 4, 2>(a, tiles, s) : a.r <= 32 ? launch_narrow<TI, TP, 4, 4>(a, tiles, s)
+                                                                            : launch_narrow<TI, TP, 2, 8>(a, tiles, s);
+}
+
+template <typename TP, int KS>
+static cudaError_t launch_widen(const Args &a, int64_t tiles, cudaStream_t s) {
+    const int chunks = (a.E + 64 * WIDE_WARPS - 1) / (64 * WIDE_WARPS), most = rows_of(a.r);
+    auto kern = widen_kernel<TP, KS>;
+    if (!allow_shared(reinterpret_cast<const void *>(kern), 3 * 64 * (MAX_RANK + 8) * 2)) return cudaErrorInvalidValue;
+    return launch_pdl(kern, dim3((unsigned)(tiles * chunks)), dim3(32 * WIDE_WARPS), (size_t)3 * most * (a.rp + 8) * 2, s, a, chunks, most);
 }
 
 static bool vec_rows(const void *p, int64_t ld, int bf16) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
 }
 
-// One pass through the adapters; types as in the public calls.  plan null: T <= rows_of(r).
+// One pass through the adapters; types as in the public calls.  plan null: T <= SMALL.
 static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cudaStream_t s) {
-    a.rp = (a.r + 15) / 16 * 16;
+    a.rp = rank_pitch(a.r);
     a.in_vec = vec_rows(a.in, a.ld_in, in_bf16);
     a.p1_vec = vec_rows(a.p1, a.D, p_bf16);
     a.p2_vec = vec_rows(a.p2, a.E, p_bf16);
@@ -716,14 +856,16 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     a.out_vec = vec_rows(a.out, a.ld_out, a.out_bf16);
     a.fine = !a.out_bf16 || a.h || a.vt;
     if (plan) a.plan = *plan;
-    else a.plan = Plan{};
     const int64_t tiles = plan ? tiles_of(a.T, a.n, a.r) : a.T;
-    a.split = tiles <= 64 ? 8 : 4;
-    const int most = plan ? rows_of(a.r) : a.T;
-    const cudaError_t e = in_bf16 ? (p_bf16 ? launch_types<uint16_t, uint16_t>(a, tiles, most, s)
-                                            : launch_types<uint16_t, float>(a, tiles, most, s))
-                                  : (p_bf16 ? launch_types<float, uint16_t>(a, tiles, most, s)
-                                            : launch_types<float, float>(a, tiles, most, s));
+    a.split = !plan ? 8 : tiles <= 38 ? 8 : tiles <= 76 ? 4 : 2;
+    cudaError_t e = in_bf16 ? (p_bf16 ? launch_types<uint16_t, uint16_t>(a, !plan, tiles, s)
+                                      : launch_types<uint16_t, float>(a, !plan, tiles, s))
+                            : (p_bf16 ? launch_types<float, uint16_t>(a, !plan, tiles, s)
+                                      : launch_types<float, float>(a, !plan, tiles, s));
+    if (e == cudaSuccess && plan && a.E > 0)
+        e = p_bf16 ? (a.rp <= 16 ? launch_widen<uint16_t, 1>(a, tiles, s) : a.rp <= 32 ? launch_widen<uint16_t, 2>(a, tiles, s)
+                                                                                       : launch_widen<uint16_t, 4>(a, tiles, s))
+                   : launch_widen<float, 1>(a, tiles, s);
     return e == cudaSuccess ? launch_status() : launch_failed();
 }
 
@@ -741,7 +883,8 @@ struct Shape {
 
 static bool sizes_fit(const Shape &z) {
     if (z.T >= (1 << 27) || z.K > (1 << 28) || z.O > (1 << 28) || z.r > MAX_RANK || z.n >= (1 << 24)) return false;
-    return (int64_t)z.n * ((z.K + 63) / 64 + (z.O + 63) / 64 + 2) < (1ll << 31) && tiles_of(z.T, z.n, z.r) * 8 < (1ll << 31);
+    const int64_t tiles = tiles_of(z.T, z.n, z.r), blocks = (z.K + 63) / 64 + (z.O + 63) / 64 + 2;
+    return z.n * blocks < (1ll << 31) && tiles * std::max<int64_t>(8, blocks) < (1ll << 31);
 }
 
 static bool aligned(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % (type == MINW_BF16 ? 2 : 4) == 0; }
@@ -761,6 +904,7 @@ size_t minw_adapters_workspace_bytes(int64_t T, int32_t K, int32_t O, int32_t n,
     if (T < 0 || K < 1 || O < 1 || n < 1 || r < 1 || !sizes_fit(z)) return 0;
     int64_t used;
     plan_at(nullptr, T, n, r, &used);
+    used += 3 * T * rank_pitch(r) * 2;
     if (backward) return (size_t)(used + 2 * up(T * r * 4, 16));
     return (size_t)std::max<int64_t>(used, std::min<int64_t>(T, W4_ROWS) * O * 4);
 }
@@ -787,9 +931,10 @@ minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T,
     a.alpha = alpha; a.base = base; a.base_bf16 = base_type == MINW_BF16; a.ld_base = ldbase; a.scale = scale; a.shift = shift;
     a.act = act; a.out = y; a.out_bf16 = y_type == MINW_BF16; a.ld_out = ldy; a.h = h;
     cudaStream_t s = (cudaStream_t)stream;
-    if (T <= rows_of(r)) return through(a, x_type == MINW_BF16, p_type == MINW_BF16, nullptr, s);
+    if (T <= SMALL) return through(a, x_type == MINW_BF16, p_type == MINW_BF16, nullptr, s);
     int64_t used;
     const Plan p = plan_at(static_cast<uint8_t *>(workspace), T, n, r, &used);
+    a.hp = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workspace) + used);
     const minw_status st = make_plan(p, ids, (int)T, n, r, s);
     return st != MINW_OK ? st : through(a, x_type == MINW_BF16, p_type == MINW_BF16, &p, s);
 }
@@ -845,7 +990,8 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
     cudaStream_t s = (cudaStream_t)stream;
     int64_t used;
     const Plan p = plan_at(static_cast<uint8_t *>(workspace), T, n, r, &used);
-    float *vt = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + used);
+    uint16_t *hp = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workspace) + used);
+    float *vt = reinterpret_cast<float *>(hp + 3 * T * rank_pitch(r));
     float *ht = vt + up(T * r * 4, 16) / 4;
     minw_status st = make_plan(p, ids, (int)T, n, r, s);
     if (st != MINW_OK) return st;
@@ -854,6 +1000,7 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
         a.in = dy; a.ld_in = lddy; a.D = O; a.E = dx ? K : 0; a.T = (int)T; a.ids = ids; a.p1 = up_; a.p2 = down; a.n = n; a.r = r;
         a.alpha = alpha; a.out = dx; a.out_bf16 = x_type == MINW_BF16; a.ld_out = lddx;
         if (accumulate) { a.base = dx; a.base_bf16 = a.out_bf16; a.ld_base = lddx; }
+        a.hp = hp;
         a.vt = ddown ? vt : nullptr;
         a.ht = dup ? ht : nullptr;
         a.h_in = h;
