@@ -39,6 +39,7 @@
 #include <algorithm>
 
 #include "kernels.cuh"
+#include "split.cuh"
 #include "values.cuh"
 
 namespace cg = cooperative_groups;
@@ -170,6 +171,23 @@ __device__ __forceinline__ void load8(const V *p, int64_t at_, int left, bool ve
     }
 }
 
+template <typename V>
+__device__ __forceinline__ void store8(V *p, int64_t at_, int left, bool vec, const float *v) {
+    if (vec && left >= 8) {
+        Vec<V, 8> w;
+        w.set(v);
+        w.store(p + at_);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) {
+                Vec<V, 1> w;
+                w.set(v + i);
+                w.store(p + at_ + i);
+            }
+    }
+}
+
 // Eight values of row r from column c on: the momentum's step m = mu m + g and what is orthogonalised, u.  Zeros outside.
 __device__ __forceinline__ void value8(const Mat &m, const Step &s, int r, int c, float *u, float *mom) {
     const int left = r < m.rows ? m.cols - c : 0;
@@ -270,17 +288,7 @@ __global__ void __launch_bounds__(THREADS) enter_kernel(Sizes l, Step s, int lo_
         float u[8], mom[8];
         const int r = rt * T + k;
         value8(m, s, r, c, u, mom);
-        if (s.use && st.finite && r < m.rows) {
-            float *p = m.mom + r * m.ldm + c;
-            if (m.mvec && m.cols - c >= 8) {
-                reinterpret_cast<float4 *>(p)[0] = make_float4(mom[0], mom[1], mom[2], mom[3]);
-                reinterpret_cast<float4 *>(p)[1] = make_float4(mom[4], mom[5], mom[6], mom[7]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (c + i < m.cols) p[i] = mom[i];
-            }
-        }
+        if (s.use && st.finite && r < m.rows) store8(m.mom, r * m.ldm + c, m.cols - c, m.mvec, mom);
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = st.finite ? u[i] * st.scale1 * st.scale2 : 0.0f;
         uint4 hi, lo;
@@ -646,7 +654,6 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         } else if (ok && i * T + r < m.rows) {
             const int64_t e = (int64_t)(i * T + r) * m.ldo + j * T + c;
             const int left = m.cols - j * T - c;
-            const bool vec = m.ovec && left >= 8;
             if (v.update) {
                 if (!st.finite) continue;
                 float w[8];
@@ -662,27 +669,8 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
 #pragma unroll
                 for (int k = 0; k < 8; ++k) z[k] = __int_as_float(0x7fc00000);
             }
-            if (m.o_bf16) {
-                uint16_t *o = static_cast<uint16_t *>(m.out) + e;
-                if (vec) {
-                    Vec<uint16_t, 8> w;
-                    w.set(z);
-                    w.store(o);
-                } else {
-                    for (int k = 0; k < 8; ++k)
-                        if (k < left) o[k] = __bfloat16_as_ushort(__float2bfloat16_rn(z[k]));
-                }
-            } else {
-                float *o = static_cast<float *>(m.out) + e;
-                if (vec) {
-                    Vec<float, 8> w;
-                    w.set(z);
-                    w.store(o);
-                } else {
-                    for (int k = 0; k < 8; ++k)
-                        if (k < left) o[k] = z[k];
-                }
-            }
+            if (m.o_bf16) store8(static_cast<uint16_t *>(m.out), e, left, m.ovec, z);
+            else store8(static_cast<float *>(m.out), e, left, m.ovec, z);
         }
     }
     // the mirror image: eight rows of a column are eight columns of a row
@@ -711,12 +699,383 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
 }
 
 // ---------------------------------------------------------------------------
+// Matrices whose smaller side is 64 at most: one launch
+// ---------------------------------------------------------------------------
+//
+// A cluster takes a matrix and holds it in its blocks' shared memory, each a share of the longer side.  Its products run on
+// mma.sync with fp32 values in three bf16 parts (products of parts below 2^-25 left out); every block takes the m x m
+// steps by itself, the Gram matrices are added up through each other's shared memory.
+
+constexpr int CLUSTER = 8, WARPS = THREADS / 32;
+constexpr int SIDE = 64;
+
+struct Small {
+    int mt;                                  // tiles of 16 of the smaller side
+    int share;                               // columns of the longer side of a block (a multiple of 64)
+    int pitch, mpitch;                       // floats between rows of X and of an m x m matrix
+    int mats_at, red_at;                     // floats
+
+    __host__ __device__ static Small of(int rows, int cols) {
+        const int side = rows < cols ? rows : cols, longer = rows < cols ? cols : rows;
+        Small s;
+        s.mt = side <= 16 ? 1 : side <= 32 ? 2 : 4;
+        s.share = (longer + CLUSTER * 64 - 1) / (CLUSTER * 64) * 64;
+        s.pitch = s.share + 4;               // rows begin in other banks
+        s.mpitch = 16 * s.mt + 4;
+        s.mats_at = 16 * s.mt * s.pitch;
+        s.red_at = s.mats_at + 16 * s.mt * s.mpitch;      // the partial sums lie where all m x m matrices but the first do
+        return s;
+    }
+    // bytes: X, five m x m matrices, or one and the warps' sums
+    __host__ int64_t bytes() const {
+        const int64_t m = 16 * mt, sums = (mt == 4 ? 4 : 8) * m * m, mats = 4 * m * mpitch;
+        return 4 * ((int64_t)m * pitch + m * mpitch + (sums > mats ? sums : mats));
+    }
+};
+
+// The parts of one fp32 row pair at k (values k, k + 1).
+__device__ __forceinline__ void parts_at(const float *p, uint32_t *s) {
+    const float2 v = *reinterpret_cast<const float2 *>(p);
+    split2(__float_as_uint(v.x), __float_as_uint(v.y), s);
+}
+
+// Six products of parts, the smallest first.
+__device__ __forceinline__ void mma_parts(float *c, const uint32_t (*a)[4], const uint32_t *b0, const uint32_t *b1) {
+#pragma unroll
+    for (int l = 2; l >= 0; --l)
+#pragma unroll
+        for (int q = 0; q <= l; ++q) mma16816(c, a[q], b0[l - q], b1[l - q]);
+}
+
+// out = factor P Q + b P + a I for m x m matrices in shared memory, Q symmetric.
+template <int MT>
+__device__ __forceinline__ void small_product(const float *P, const float *Q, float *out, int pitch, float factor, float b, float a) {
+    constexpr int TILES = MT * 2 * MT, EACH = (TILES + WARPS - 1) / WARPS;          // of 16 x 8; a warp's lie in one row of tiles
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    __syncthreads();
+    if (warp * EACH < TILES) {
+        const int i = 16 * (warp * EACH / (2 * MT)), j0 = 8 * (warp * EACH % (2 * MT));
+        float c[EACH][4];
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c[e][k] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 16 * MT; k += 16) {
+            uint32_t f[3][4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                uint32_t s[3];
+                parts_at(P + (i + g + 8 * (r & 1)) * pitch + k + 2 * t + 8 * (r >> 1), s);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) f[q][r] = s[q];
+            }
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                uint32_t b0[3], b1[3];
+                parts_at(Q + (j0 + 8 * e + g) * pitch + k + 2 * t, b0);
+                parts_at(Q + (j0 + 8 * e + g) * pitch + k + 2 * t + 8, b1);
+                mma_parts(c[e], f, b0, b1);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int r = i + g + 8 * (k >> 1), col = j0 + 8 * e + 2 * t + (k & 1);
+                out[r * pitch + col] = fmaf(factor, c[e][k], fmaf(b, P[r * pitch + col], r == col ? a : 0.0f));
+            }
+    }
+}
+
+// The Gram matrix of all blocks' shares of X, times `factor`, into `out` of every block.
+template <int MT>
+__device__ __forceinline__ void small_gram(const cg::cluster_group &cluster, const float *X, const Small &z, float *red, float *mine,
+                                           float *out, float scale) {
+    constexpr int M = 16 * MT, NB = MT == 4 ? 4 : 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    float c[MT][2 * MT][4];                                     // tiles of the lower triangle
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < 2 * MT; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) c[i][j][k] = 0.0f;
+    for (int b = warp; b < z.share / 32; b += WARPS) {
+        uint32_t p[2 * MT][3][4];
+#pragma unroll
+        for (int i = 0; i < 2 * MT; ++i) {
+            const float *x = X + (8 * i + g) * z.pitch + 32 * b + 8 * t;
+            const float4 u = reinterpret_cast<const float4 *>(x)[0], v = reinterpret_cast<const float4 *>(x)[1];
+            const float w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+            Eight<float> e;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e.w[k] = __float_as_uint(w[k] * scale);
+            along(e, p[i]);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                uint32_t f[3][4];
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    f[q][0] = p[2 * i][q][2 * s];
+                    f[q][1] = p[2 * i + 1][q][2 * s];
+                    f[q][2] = p[2 * i][q][2 * s + 1];
+                    f[q][3] = p[2 * i + 1][q][2 * s + 1];
+                }
+#pragma unroll
+                for (int j = 0; j < 2 * MT; ++j) {
+                    if (j > 2 * i + 1) continue;
+                    uint32_t b0[3], b1[3];
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) { b0[q] = p[j][q][2 * s]; b1[q] = p[j][q][2 * s + 1]; }
+                    mma_parts(c[i][j], f, b0, b1);
+                }
+            }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int turn = 0; turn < WARPS / NB; ++turn) {
+        if (warp / NB == turn) {
+            float *d = red + (warp % NB) * M * M;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < 2 * MT; ++j) {
+                    if (j > 2 * i + 1) continue;
+#pragma unroll
+                    for (int k = 0; k < 4; k += 2) {
+                        float2 *at_ = reinterpret_cast<float2 *>(d + (16 * i + g + 4 * k) * M + 8 * j + 2 * t);
+                        float2 v = make_float2(c[i][j][k], c[i][j][k + 1]);
+                        if (turn > 0) { const float2 o = *at_; v.x += o.x; v.y += o.y; }
+                        *at_ = v;
+                    }
+                }
+        }
+        __syncthreads();
+    }
+    for (int e = threadIdx.x; e < M * M; e += THREADS) {
+        const int r = e / M, col = e % M;
+        if (col > r) continue;
+        float v[NB];
+#pragma unroll
+        for (int w = 0; w < NB; ++w) v[w] = red[w * M * M + e];
+#pragma unroll
+        for (int w = 1; w < NB; ++w) v[0] += v[w];
+        mine[r * z.mpitch + col] = v[0];
+    }
+    cluster.sync();
+    for (int e = threadIdx.x; e < M * M; e += THREADS) {
+        const int r = e / M, col = e % M;
+        if (col > r) continue;
+        float *p = mine + r * z.mpitch + col;
+        float v[CLUSTER];
+#pragma unroll
+        for (int k = 0; k < CLUSTER; ++k) v[k] = *cluster.map_shared_rank(p, k);
+#pragma unroll
+        for (int k = 1; k < CLUSTER; ++k) v[0] += v[k];
+        out[r * z.mpitch + col] = v[0];
+        out[col * z.mpitch + r] = v[0];
+    }
+    cluster.sync();                                             // `mine` may be written again
+}
+
+// X = Q X, a warp's 64 columns at a time.
+template <int MT>
+__device__ __forceinline__ void small_apply(float *X, const Small &z, const float *Q, float scale) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    __syncthreads();
+    for (int b = warp; b < z.share / 64; b += WARPS) {
+        float c[MT][8][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) c[i][j][k] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 16 * MT; k += 16) {
+            uint32_t f[MT][3][4];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    uint32_t s[3];
+                    parts_at(Q + (16 * i + g + 8 * (r & 1)) * z.mpitch + k + 2 * t + 8 * (r >> 1), s);
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) f[i][q][r] = s[q];
+                }
+            const float *x = X + (k + 2 * t) * z.pitch + 64 * b + 8 * g;
+#pragma unroll
+            for (int j0 = 0; j0 < 8; j0 += 4) {
+                float4 v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = *reinterpret_cast<const float4 *>(x + ((r & 1) + 8 * (r >> 1)) * z.pitch + j0);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    auto at_ = [&](int r) { return __float_as_uint((j == 0 ? v[r].x : j == 1 ? v[r].y : j == 2 ? v[r].z : v[r].w) * scale); };
+                    uint32_t b0[3], b1[3];
+                    split2(at_(0), at_(1), b0);
+                    split2(at_(2), at_(3), b1);
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) mma_parts(c[i][j0 + j], f[i], b0, b1);
+                }
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float4 *d = reinterpret_cast<float4 *>(X + (16 * i + g + 8 * h) * z.pitch + 64 * b + 16 * t);
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {                   // columns 8 e + j of the lane's 16
+                    d[2 * e] = make_float4(c[i][0][2 * h + e], c[i][1][2 * h + e], c[i][2][2 * h + e], c[i][3][2 * h + e]);
+                    d[2 * e + 1] = make_float4(c[i][4][2 * h + e], c[i][5][2 * h + e], c[i][6][2 * h + e], c[i][7][2 * h + e]);
+                }
+            }
+    }
+    __syncthreads();
+}
+
+template <int MT>
+__device__ __forceinline__ void small_steps(const cg::cluster_group &cluster, float *smem, const Small &z, int steps, float scale) {
+    constexpr int M = 16 * MT;
+    float *X = smem, *mats = smem + z.mats_at, *red = smem + z.red_at;
+    const int size = M * z.mpitch, stages = (steps + 2) / 3;
+    float *m1 = mats + size, *m2 = m1 + size, *m3 = m2 + size, *m4 = m3 + size;
+    for (int st = 0, left = steps; st < stages; ++st) {
+        const int n = (left + stages - st - 1) / (stages - st);
+        left -= n;
+        float *A = m1, *Z = m2, *Q = m3, *W = m4;
+        small_gram<MT>(cluster, X, z, red, mats, A, st == 0 ? scale : 1.0f);
+        float factor = 1.0f;
+        if (st == 0) {                                          // the norm from the trace
+            const int lane = threadIdx.x & 31;
+            float d = lane < M ? A[lane * (z.mpitch + 1)] : 0.0f;
+            if (MT == 4) d += A[(lane + 32) * (z.mpitch + 1)];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+            factor = d > 0.0f ? __fdiv_rn(1.0f, __fsqrt_rn(d)) : 1.0f;
+            const float inv = d > 0.0f ? __fdiv_rn(1.0f, d) : 1.0f;
+            __syncthreads();
+            for (int e = threadIdx.x; e < size; e += THREADS) A[e] *= inv;
+        }
+        for (int k = 1; k <= n; ++k) {
+            float *out = k == 1 ? Q : Z;
+            small_product<MT>(A, A, out, z.mpitch, CC, CB, CA);
+            if (k > 1) {
+                small_product<MT>(Z, Q, W, z.mpitch, 1.0f, 0.0f, 0.0f);
+                float *s = Q; Q = W; W = s;
+            }
+            if (k < n) {
+                // A <- (Z A) Z through W
+                small_product<MT>(out, A, W, z.mpitch, 1.0f, 0.0f, 0.0f);
+                small_product<MT>(W, out, A, z.mpitch, 1.0f, 0.0f, 0.0f);
+            }
+        }
+        if (st == 0) {
+            __syncthreads();
+            for (int e = threadIdx.x; e < size; e += THREADS) Q[e] *= factor;
+        }
+        small_apply<MT>(X, z, Q, st == 0 ? scale : 1.0f);
+    }
+}
+
+template <int N>
+__global__ void __launch_bounds__(THREADS, 1) small_kernel(const __grid_constant__ Table<N> table, Step s, int steps, int update, float lr) {
+    pdl_trigger();
+    pdl_wait();
+    extern __shared__ __align__(16) float X[];
+    __shared__ uint32_t most;                                   // the largest magnitude's bits, of this block
+    const Mat &m = table.m[blockIdx.x / CLUSTER];
+    const int rank = blockIdx.x % CLUSTER;
+    const Small z = Small::of(m.rows, m.cols);
+    const int M = 16 * z.mt, l0 = rank * z.share;
+    cg::cluster_group cluster = cg::this_cluster();
+    if (threadIdx.x == 0) most = 0u;
+    __syncthreads();
+    // this block's share [M][share], from rows of the matrix or from its columns; zeros around it
+    uint32_t mx = 0u;
+    const int n = M * z.share;
+    for (int e0 = threadIdx.x * 8; e0 < n; e0 += THREADS * 8) {
+        float u[8], mom[8];
+        int i, l;
+        if (!m.tall) {
+            i = e0 / z.share;
+            l = e0 - i * z.share;
+            value8(m, s, l0 + l < m.cols ? i : m.rows, l0 + l, u, mom);
+        } else {
+            l = e0 / M;
+            i = e0 - l * M;
+            value8(m, s, i < m.cols ? l0 + l : m.rows, i, u, mom);
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            mx = max(mx, __float_as_uint(u[k]) & 0x7fffffffu);
+            X[m.tall ? (i + k) * z.pitch + l : i * z.pitch + l + k] = u[k];
+        }
+    }
+    mx = __reduce_max_sync(0xffffffffu, mx);
+    if ((threadIdx.x & 31) == 0) atomicMax(&most, mx);
+    cluster.sync();
+    for (int k = 0; k < CLUSTER; ++k) mx = max(mx, *cluster.map_shared_rank(&most, k));
+    const bool finite = mx < 0x7f800000u;
+    // largest magnitude to [1, 2), or as near as a factor that is an fp32 number comes (the Gram matrix of 2^-22 and more is one)
+    const int ex = mx == 0u ? 0 : max(ilogbf(__uint_as_float(mx)), -126);
+    const float scale = ldexpf(1.0f, min(-ex, 127));
+    if (finite) {
+        if (z.mt == 1) small_steps<1>(cluster, X, z, steps, scale);
+        else if (z.mt == 2) small_steps<2>(cluster, X, z, steps, scale);
+        else small_steps<4>(cluster, X, z, steps, scale);
+    }
+    const float rate = -lr * m.rate;
+    for (int e0 = threadIdx.x * 8; e0 < n; e0 += THREADS * 8) {
+        int i, l;
+        if (!m.tall) {
+            i = e0 / z.share;
+            l = e0 - i * z.share;
+        } else {
+            l = e0 / M;
+            i = e0 - l * M;
+        }
+        const int r = m.tall ? l0 + l : i, c = m.tall ? i : l0 + l, left = m.cols - c;
+        if (r >= m.rows || left <= 0 || (update && !finite)) continue;
+        if (update && s.use) {
+            float u[8], mom[8];
+            value8(m, s, r, c, u, mom);
+            store8(m.mom, r * m.ldm + c, left, m.mvec, mom);
+        }
+        float v[8], w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v[k] = finite ? X[m.tall ? (i + k) * z.pitch + l : i * z.pitch + l + k] : __int_as_float(0x7fc00000);
+        const int64_t at_ = r * m.ldo + c;
+        if (update) {
+            if (m.o_bf16) load8(static_cast<const uint16_t *>(m.out), at_, left, m.ovec, w);
+            else load8(static_cast<const float *>(m.out), at_, left, m.ovec, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float x = fmaf(rate, v[k], w[k]);
+                v[k] = x > m.limit ? m.limit : x < -m.limit ? -m.limit : x;
+            }
+        }
+        if (m.o_bf16) store8(static_cast<uint16_t *>(m.out), at_, left, m.ovec, v);
+        else store8(static_cast<float *>(m.out), at_, left, m.ovec, v);
+    }
+    cluster.sync();                                             // others read this block's magnitude
+}
+
+// ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
 
 using namespace minw_host;
 
 constexpr int MAX_STEPS = 10;
+constexpr int SMALL_BYTES = 220 * 1024;
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
@@ -727,6 +1086,38 @@ static int64_t matrix_bytes(int rows, int cols) {
 }
 
 static int64_t tiles_of(int rows, int cols) { return (int64_t)((rows + T - 1) / T) * ((cols + T - 1) / T); }
+
+static Mat describe(const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int k) {
+    Mat m{};
+    m.rows = g[k].rows;
+    m.cols = g[k].cols;
+    m.tall = m.rows > m.cols;
+    m.g = g[k].data;
+    m.ldg = g[k].ld;
+    m.g_bf16 = g[k].type == MINW_BF16;
+    m.gvec = reinterpret_cast<uintptr_t>(m.g) % 16 == 0 && m.ldg % (m.g_bf16 ? 8 : 4) == 0;
+    if (mom) {
+        m.mom = static_cast<float *>(mom[k].data);
+        m.ldm = mom[k].ld;
+        m.mvec = reinterpret_cast<uintptr_t>(m.mom) % 16 == 0 && m.ldm % 4 == 0;
+    }
+    if (out) {
+        m.out = out[k].data;
+        m.ldo = out[k].ld;
+        m.o_bf16 = out[k].type == MINW_BF16;
+        m.ovec = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 && m.ldo % (m.o_bf16 ? 8 : 4) == 0;
+        m.limit = out[k].limit;
+        m.rate = m.tall ? sqrtf((float)m.rows / (float)m.cols) : 1.0f;
+    }
+    return m;
+}
+
+// Whether a matrix goes through the launch for small sides: it fits a cluster's shared memory.
+static bool is_small(const minw_matrix &g) {
+    return std::min(g.rows, g.cols) <= SIDE && (int64_t)g.rows * g.cols <= (1 << 24) &&
+           Small::of(g.rows, g.cols).bytes() <= SMALL_BYTES;
+}
+static bool is_large(const minw_matrix &g) { return g.rows > 0 && g.cols > 0 && !is_small(g); }
 
 // Fills a launch's list from matrix k on; returns the next launch's first, and the workspace that it takes.  base null: the
 // sizes alone.
@@ -739,36 +1130,16 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
     used = up(used + CAP * sizeof(Stat), 256);
     int64_t tiles = 0;
     for (int e = k, n = 0; e < count && n < CAP; ++e) {         // the sums of squares lie before the matrices
-        if (g[e].rows == 0 || g[e].cols == 0) continue;
+        if (!is_large(g[e])) continue;
         ++n;
         tiles += tiles_of(g[e].rows, g[e].cols);
     }
     l.part = reinterpret_cast<double *>(base + used);
     used = up(used + tiles * (int64_t)sizeof(double), 1024);
     for (; k < count && l.count < CAP; ++k) {
-        if (g[k].rows == 0 || g[k].cols == 0) continue;
+        if (!is_large(g[k])) continue;
         Mat &m = table[l.count++];
-        m = Mat{};
-        m.rows = g[k].rows;
-        m.cols = g[k].cols;
-        m.tall = m.rows > m.cols;
-        m.g = g[k].data;
-        m.ldg = g[k].ld;
-        m.g_bf16 = g[k].type == MINW_BF16;
-        m.gvec = reinterpret_cast<uintptr_t>(m.g) % 16 == 0 && m.ldg % (m.g_bf16 ? 8 : 4) == 0;
-        if (mom) {
-            m.mom = static_cast<float *>(mom[k].data);
-            m.ldm = mom[k].ld;
-            m.mvec = reinterpret_cast<uintptr_t>(m.mom) % 16 == 0 && m.ldm % 4 == 0;
-        }
-        if (out) {
-            m.out = out[k].data;
-            m.ldo = out[k].ld;
-            m.o_bf16 = out[k].type == MINW_BF16;
-            m.ovec = reinterpret_cast<uintptr_t>(m.out) % 16 == 0 && m.ldo % (m.o_bf16 ? 8 : 4) == 0;
-            m.limit = out[k].limit;
-            m.rate = m.tall ? sqrtf((float)m.rows / (float)m.cols) : 1.0f;
-        }
+        m = describe(g, mom, out, k);
         m.tri0 = l.tri;
         m.full0 = l.full;
         const int mb = m.mb();
@@ -897,11 +1268,51 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
     return launch_status();
 }
 
+template <int N>
+static cudaError_t launch_small(const Table<N> &table, int count, int bytes, const Step &step, int steps, bool update, float lr,
+                                cudaStream_t s) {
+    auto kern = small_kernel<N>;
+    if (!allow_shared(reinterpret_cast<const void *>(kern), SMALL_BYTES)) return cudaErrorInvalidValue;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(count * CLUSTER));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = CLUSTER;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, table, step, steps, update ? 1 : 0, lr);
+}
+
 static minw_status run(const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int count, int steps,
                        const Step &step, bool update, float lr, uint8_t *ws, cudaStream_t s) {
     bool x_lo = step.use != 0;                                  // bf16 gradients are fp16 numbers but for the smallest
     for (int k = 0; k < count; ++k) x_lo = x_lo || g[k].type == MINW_F32;
     Table<CAP> table;
+    for (int k = 0; k < count;) {
+        int n = 0;
+        int64_t bytes = 0;
+        for (; k < count && n < CAP; ++k) {
+            if (g[k].rows == 0 || g[k].cols == 0 || !is_small(g[k])) continue;
+            table.m[n++] = describe(g, mom, out, k);
+            bytes = std::max(bytes, Small::of(g[k].rows, g[k].cols).bytes());
+        }
+        if (n == 0) break;
+        cudaError_t e;
+        if (n <= FEW) {
+            Table<FEW> few;
+            std::copy(table.m, table.m + n, few.m);
+            e = launch_small(few, n, (int)bytes, step, steps, update, lr, s);
+        } else {
+            e = launch_small(table, n, (int)bytes, step, steps, update, lr, s);
+        }
+        if (e != cudaSuccess) return launch_failed();
+    }
     Sizes l;
     for (int k = 0; k < count;) {
         int64_t need;
@@ -910,7 +1321,7 @@ static minw_status run(const minw_matrix *g, const minw_matrix *mom, const minw_
         const minw_status st = chain(table, l, step, steps, x_lo, update, lr, s);
         if (st != MINW_OK) return st;
     }
-    return MINW_OK;
+    return launch_status();
 }
 
 }  // namespace orth

@@ -1,0 +1,92 @@
+// split.cuh -- fp32 values as sums of three bf16 parts for the tensor cores'
+// warp-wide products: eight values of a row at a time, paired up along the
+// row or across two rows.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "values.cuh"
+
+namespace minw {
+
+template <typename V>
+constexpr int parts_of() { return sizeof(V) == 2 ? 1 : 3; }
+
+// Eight consecutive values as they lie in memory; zeros from `left` on.
+template <typename V>
+struct Eight {
+    uint32_t w[2 * sizeof(V)];
+
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int k = 0; k < 2 * (int)sizeof(V); ++k) w[k] = 0u;
+    }
+    __device__ __forceinline__ void load(const V *p, int left, bool vec) {
+        if (vec && left >= 8) {
+            Vec<V, 8> v;
+            v.load(p);
+#pragma unroll
+            for (int k = 0; k < 2 * (int)sizeof(V); ++k) w[k] = v.w[k];
+        } else {
+            zero();
+            if constexpr (sizeof(V) == 4) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < left) w[k] = __float_as_uint(p[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < left) w[k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {          // a in the lower half
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// Two fp32 values as pairs of bf16 parts whose sums they are, each part rounded to nearest: what is left after one is 2^-9 of
+// the value at most, after two 2^-18 (parts cut off instead leave up to 2^-7 and 2^-15, and products without the smallest
+// are 2^-21 off).  An infinity, a NaN or a value past 3.39e38 makes the second part a NaN.
+__device__ __forceinline__ void split2(uint32_t a, uint32_t b, uint32_t *p) {
+    float x = __uint_as_float(a), y = __uint_as_float(b);
+    p[0] = bf16_pair(x, y);
+    x -= __uint_as_float(p[0] << 16);
+    y -= __uint_as_float(p[0] & 0xffff0000u);
+    p[1] = bf16_pair(x, y);
+    p[2] = bf16_pair(x - __uint_as_float(p[1] << 16), y - __uint_as_float(p[1] & 0xffff0000u));
+}
+
+// Pairs of neighbours of one row: pair k = values 2k, 2k + 1, in parts.
+template <typename V>
+__device__ __forceinline__ void along(const Eight<V> &e, uint32_t (*p)[4]) {
+    if constexpr (sizeof(V) == 2) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p[0][k] = e.w[k];
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t s[3];
+            split2(e.w[2 * k], e.w[2 * k + 1], s);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) p[i][k] = s[i];
+        }
+    }
+}
+
+// Pairs across two rows: value i of the first and of the second, in parts.
+template <typename V>
+__device__ __forceinline__ void across(const Eight<V> &a, const Eight<V> &b, int i, uint32_t *p) {
+    if constexpr (sizeof(V) == 2) p[0] = __byte_perm(a.w[i >> 1], b.w[i >> 1], (i & 1) ? 0x7632 : 0x5410);
+    else split2(a.w[i], b.w[i], p);
+}
+
+__device__ __forceinline__ void mma16816(float *c, const uint32_t *a, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+}  // namespace minw

@@ -100,6 +100,7 @@ def _close(got, want, t, steps=5):
 SHAPES = [
     [(1, 1)], [(1, 200)], [(200, 1)], [(10, 1024)], [(1024, 10)], [(128, 128)], [(129, 127)], [(127, 129), (64, 64)],
     [(256, 1152)], [(1152, 256)], [(333, 1001)], [(700, 700)], [(16, 8192)] * 3 + [(16, 1024)] * 3,
+    [(17, 500)], [(500, 33)], [(64, 4096)], [(64, 4097)], [(3, 26000)], [(26000, 16)], [(32, 40), (33, 40), (64, 65), (65, 64), (1, 2)],
     [(128, 27), (128, 1152), (256, 1152), (5, 3), (0, 7), (130, 2304), (2304, 130), (7, 0)], [(1024, 4097)],
 ]
 
