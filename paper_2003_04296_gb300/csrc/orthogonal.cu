@@ -25,8 +25,8 @@
 // Operands lie in the workspace as the tensor cores read them: blocks of 128 rows x 64
 // columns, 16 KB, swizzled in rows of 128 bytes.  Such a block is a K-major operand of
 // 128 rows or, column group by column group, an MN-major one, so X serves X X^T, X^T X, Q X and
-// X Q without a transposed copy, blocks travel as plain bulk copies, and no
-// matrix of a list needs a tensor map.
+// X Q without a transposed copy, a symmetric matrix is its lower triangle alone, blocks travel
+// as plain bulk copies, and no matrix of a list needs a tensor map.
 //
 // A list goes through the kernels together: level k of all its matrices is one
 // launch.  Clusters split the sums of a tile where there are fewer tiles than SMs.
@@ -89,6 +89,7 @@ struct Mat {
 
 struct Sizes {
     int count, tri, full;                    // matrices; tiles of their lower triangles, of X
+    int small_k, long_k;                     // the largest smaller and longer side, in blocks of 64
     const Mat *table;                        // in the workspace
     Stat *stat;
     double *part;                            // a sum of squares for each tile of X
@@ -212,8 +213,8 @@ __device__ __forceinline__ double sum64(double v) {
 // A block's tile: 128 rows x 128 columns, eight values a thread at a time.
 template <int N>
 __global__ void __launch_bounds__(THREADS) squares_kernel(const __grid_constant__ Table<N> table, Sizes l, Step s) {
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();
     __shared__ double red[THREADS / 32];
     // the list's matrices into the workspace, where the kernels after this one find them (a launch with 23 KB of
     // arguments takes the host three times as long)
@@ -253,8 +254,8 @@ __global__ void __launch_bounds__(THREADS) squares_kernel(const __grid_constant_
 }
 
 __global__ void __launch_bounds__(THREADS) enter_kernel(Sizes l, Step s, int lo_part) {
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();
     __shared__ double red[THREADS / 32];
     __shared__ Stat st;
     const int which = find<false>(l.table, l.count, blockIdx.x);
@@ -369,15 +370,17 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const uint8_t *src, uint
                  : "memory");
 }
 
-// An operand of a tile: hi blocks at `p`, lo blocks `lo` bytes on (0: none), `wide` blocks to a row of blocks.
+// An operand of a tile: hi blocks at `p`, lo blocks `lo` bytes on (0: none), `wide` blocks to a row of blocks.  A symmetric
+// matrix is held as its lower triangle of tiles: a block of the upper one is the mirror image's, read the other way.
 struct Side {
     const uint8_t *p;
     int64_t lo;
     int wide, tile;
-    bool mn;
+    bool mn, sym;
 
+    __device__ __forceinline__ bool turned(int kb) const { return sym ? (kb >> 1) > tile : mn; }
     __device__ __forceinline__ void load(uint32_t dst, int kb, uint64_t *bar) const {
-        if (!mn) {
+        if (!turned(kb)) {
             const uint8_t *s = p + ((int64_t)tile * wide + kb) * BLOCK;
             bulk_load(dst, s, BLOCK, bar);
             if (lo) bulk_load(dst + BLOCK, s + lo, BLOCK, bar);
@@ -441,7 +444,6 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
     __syncthreads();
     fence_after();
     const uint32_t tmem = sm.tmem;
-    pdl_trigger();
 
     // what this block computes: matrix, product, tile (i, j), share of K
     const int split = v.split, rank = blockIdx.x % split, tri = v.mode <= MUL;
@@ -450,7 +452,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         which = t / l.tri;
         t -= which * l.tri;
     }
-    pdl_wait();
+    // the table is the first kernel's work, and that one was done before this one's predecessor let it start
     const int index = tri ? find<true>(l.table, l.count, t) : find<false>(l.table, l.count, t);
     const Mat m = l.table[index];
     const Product pr = v.pr[which];
@@ -470,7 +472,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         i = t / m.cb();
         j = t % m.cb();
     }
-    const Side sx{x, v.x_lo ? x_blocks : 0, 2 * m.cb(), 0, false};
+    const Side sx{x, v.x_lo ? x_blocks : 0, 2 * m.cb(), 0, false, false};
     Side a, b;
     int kbs;                                                    // blocks of 64 along K
     if (v.mode == GRAM) {
@@ -480,8 +482,8 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         a.mn = b.mn = m.tall;
         kbs = 2 * (m.tall ? m.rb() : m.cb());
     } else {
-        const Side sp{m.small + pr.p * slot, small_blocks, 2 * mb, i, false};
-        const Side sq{m.small + pr.q * slot, small_blocks, 2 * mb, j, false};
+        const Side sp{m.small + pr.p * slot, small_blocks, 2 * mb, i, false, true};
+        const Side sq{m.small + pr.q * slot, small_blocks, 2 * mb, j, false, true};
         kbs = 2 * mb;
         a = sp;
         b = sq;
@@ -499,8 +501,10 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         }
     }
     const int kb0 = rank * kbs / split, kb1 = (rank + 1) * kbs / split;
-    const bool same = a.p == b.p && a.tile == b.tile && a.mn == b.mn;
+    const bool same = a.p == b.p && a.tile == b.tile && a.mn == b.mn && a.sym == b.sym;
     const uint32_t bytes = a.bytes() + (same ? 0 : b.bytes());
+    pdl_wait();
+    pdl_trigger();
     bool ok = true;
     if (warp == LOADER) {
         if (lane == 0) {
@@ -522,8 +526,6 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         __syncwarp();
     } else if (warp == ISSUER) {
         // D fp32, A and B fp16; bits 15 and 16: MN-major
-        const uint32_t idesc = (1u << 4) | ((a.mn ? 1u : 0u) << 15) | ((b.mn ? 1u : 0u) << 16) | ((uint32_t)(T >> 3) << 17) | (8u << 24);
-        const uint32_t ka = a.mn ? 2048 >> 4 : 32 >> 4, kbk = b.mn ? 2048 >> 4 : 32 >> 4;      // 16 of K
         int s = 0, chunk = 0;
         uint32_t phase = 0u, rest = 0u;
         for (int at_ = kb0; at_ < kb1 && ok; at_ += CHUNK, ++chunk) {
@@ -537,7 +539,10 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
                 if (!__all_sync(0xffffffffu, bar_wait(&sm.full[s], phase, v.wait_cycles))) { ok = false; break; }
                 fence_after();
                 const uint32_t base = su32(ring) + s * STAGE;
-                const uint64_t ad = desc(base, a.mn), bd = desc(same ? base : base + 2 * BLOCK, b.mn);
+                const bool at = a.turned(kb), bt = b.turned(kb);
+                const uint32_t idesc = (1u << 4) | ((at ? 1u : 0u) << 15) | ((bt ? 1u : 0u) << 16) | ((uint32_t)(T >> 3) << 17) | (8u << 24);
+                const uint32_t ka = at ? 2048 >> 4 : 32 >> 4, kbk = bt ? 2048 >> 4 : 32 >> 4;  // 16 of K
+                const uint64_t ad = desc(base, at), bd = desc(same ? base : base + 2 * BLOCK, bt);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mma_f16(d, ad + k * ka, bd + k * kbk, idesc, k > 0 ? 1u : on);
                 on = 1u;
@@ -589,17 +594,22 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
         }
     }
     ok = __syncthreads_and(ok);                                 // and the last loads have landed
+    // Rows of the tile that this block finishes.  The other blocks' sums for them arrive in its shared memory, a share after the
+    // other, once all are done with their rings (reading them from here instead takes 2 us more: their way is there twice).
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rows = T / split, r0 = rank * rows;
+    if (split > 1) cluster.sync();
     if (warp < THREADS / 32) {
-        float *d = acc + ((warp & 3) * 32 + lane) * PITCH + (warp >> 2) * 64;
+        const int r = (warp & 3) * 32 + lane, owner = r / rows;
+        float *d = acc + (rank * rows + r - owner * rows) * PITCH + (warp >> 2) * 64;
+        if (split > 1) d = cluster.map_shared_rank(d, owner);
 #pragma unroll
         for (int k = 0; k < 64; k += 4) *reinterpret_cast<float4 *>(d + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
     }
-    cg::cluster_group cluster = cg::this_cluster();
     if (split > 1) cluster.sync();
     else __syncthreads();
 
-    // this block's rows of the tile, eight columns a thread at a time
-    const int rows = T / split, r0 = rank * rows;
+    // eight columns a thread at a time
     const Stat st = v.mode == GRAM || v.mode == LEAVE || v.mode == APPLY ? l.stat[index] : Stat{};
     float factor = pr.factor;
     if (v.mode == GRAM && !v.x1) factor *= st.gram;
@@ -610,19 +620,13 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
     const int c = (threadIdx.x & 15) * 8;
     for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32; r += 16) {
         float z[8];
-        float *mine = acc + r * PITCH + c;
 #pragma unroll
         for (int k = 0; k < 8; k += 4) {
-            float4 f = *reinterpret_cast<const float4 *>(mine + k);
-            if (split > 1) {
-                float4 o[8];                                    // all on their way at once
-#pragma unroll
-                for (int p = 0; p < 8; ++p)
-                    if (p < split) o[p] = *reinterpret_cast<const float4 *>(cluster.map_shared_rank(mine + k, p));
-                f = o[0];
-#pragma unroll
-                for (int p = 1; p < 8; ++p)
-                    if (p < split) { f.x += o[p].x; f.y += o[p].y; f.z += o[p].z; f.w += o[p].w; }
+            const float *share = acc + (r - r0) * PITCH + c + k;
+            float4 f = *reinterpret_cast<const float4 *>(share);
+            for (int p = 1; p < split; ++p) {
+                const float4 o = *reinterpret_cast<const float4 *>(share + p * rows * PITCH);
+                f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
             }
             z[k] = f.x; z[k + 1] = f.y; z[k + 2] = f.z; z[k + 3] = f.w;
         }
@@ -647,10 +651,6 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
                 *reinterpret_cast<uint4 *>(d) = h;
                 *reinterpret_cast<uint4 *>(d + lo) = w;
             }
-            if (tri && i != j) {
-                *reinterpret_cast<float4 *>(mine) = make_float4(z[0], z[1], z[2], z[3]);
-                *reinterpret_cast<float4 *>(mine + 4) = make_float4(z[4], z[5], z[6], z[7]);
-            }
         } else if (ok && i * T + r < m.rows) {
             const int64_t e = (int64_t)(i * T + r) * m.ldo + j * T + c;
             const int left = m.cols - j * T - c;
@@ -673,25 +673,8 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
             else store8(static_cast<float *>(m.out), e, left, m.ovec, z);
         }
     }
-    // the mirror image: eight rows of a column are eight columns of a row
-    if (tri && i != j) {
-        __syncthreads();
-        const int eights = rows / 8;
-        for (int e = threadIdx.x; e < eights * T && ok; e += THREADS + 64) {
-            const int col = e % T, r = r0 + e / T * 8;
-            float z[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) z[k] = acc[(r + k) * PITCH + col];
-            uint4 h, w;
-            split8(z, h, w);
-            uint8_t *d = out + ((int64_t)j * wide + 2 * i + (r >> 6)) * BLOCK + at(col, r & 63);
-            *reinterpret_cast<uint4 *>(d) = h;
-            *reinterpret_cast<uint4 *>(d + lo) = w;
-        }
-    }
     fence_before();
-    if (split > 1) cluster.sync();                              // others read this block's sums
-    else __syncthreads();
+    __syncthreads();
     if (warp == ISSUER) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));
@@ -1123,7 +1106,7 @@ static bool is_large(const minw_matrix &g) { return g.rows > 0 && g.cols > 0 && 
 // sizes alone.
 static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int k, int count,
                 uint8_t *base, int64_t *need) {
-    l.count = l.tri = l.full = 0;
+    l.count = l.tri = l.full = l.small_k = l.long_k = 0;
     l.table = reinterpret_cast<const Mat *>(base);
     int64_t used = up(CAP * sizeof(Mat), 256);
     l.stat = reinterpret_cast<Stat *>(base + used);
@@ -1143,6 +1126,8 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
         m.tri0 = l.tri;
         m.full0 = l.full;
         const int mb = m.mb();
+        l.small_k = std::max(l.small_k, 2 * mb);
+        l.long_k = std::max(l.long_k, 2 * std::max(m.rb(), m.cb()));
         l.tri += mb * (mb + 1) / 2;
         l.full += m.rb() * m.cb();
         const int64_t x = (int64_t)m.rb() * m.cb() * 4 * BLOCK;
@@ -1178,8 +1163,10 @@ static bool sizes_fit(const minw_matrix *g, int count) {
 
 static cudaError_t launch(const Sizes &l, Level v, int64_t tiles, cudaStream_t s) {
     const int sms = num_sms() > 0 ? num_sms() : 152;
-    // clusters split K where the tiles leave SMs idle
-    v.split = tiles * 8 <= sms ? 8 : tiles * 4 <= sms ? 4 : tiles * 2 <= sms ? 2 : 1;
+    // clusters split K where the tiles leave SMs idle, into shares of 256 at least
+    const int k = v.mode == GRAM ? l.long_k : l.small_k;
+    v.split = 8;
+    while (v.split > 1 && (tiles * v.split > sms || k < 4 * v.split)) v.split /= 2;
     v.wait_cycles = (long long)plan_options().wait_cycles;
     const int smem = STAGES * (int)STAGE + 1024;
     if (!allow_shared(reinterpret_cast<const void *>(product_kernel), smem)) return cudaErrorInvalidValue;
