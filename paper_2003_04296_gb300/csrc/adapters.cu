@@ -136,6 +136,71 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const int *__restric
 // Through an adapter
 // ---------------------------------------------------------------------------
 
+// How rows may be copied: by 16 bytes, by 4, or value by value.
+enum Copy { BY_VALUE, BY_WORD, BY_SIXTEEN };
+
+// `bytes` (16, 8 or 4) to shared memory, asynchronously, the first `n` of them from src and zeros behind.
+template <int BYTES>
+__device__ __forceinline__ void copy_fill(uint32_t dst, const void *src, int n) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(n), "n"(BYTES) : "memory");
+}
+
+// Eight values to where this lane alone will read them back: 16 bytes at dst, the next 16 (fp32) 512 on.  Zeros from `left` on.
+template <typename V>
+__device__ __forceinline__ void fetch8_wide(uint32_t dst, const V *p, int left) {
+    constexpr int N = 16 / (int)sizeof(V);                               // values in 16 bytes
+#pragma unroll
+    for (int h = 0; h < 8 / N; ++h) {
+        const int n = min(max(left - h * N, 0), N);
+        copy_fill<16>(dst + 512 * h, n > 0 ? p + h * N : p, n * (int)sizeof(V));
+    }
+}
+
+// The same however the row lies.  For loops that are not unrolled: all ways inlined at a dozen places, the instructions do not
+// stay in their caches (half of the time lost).
+template <typename V>
+__device__ __forceinline__ void fetch8(uint32_t dst, const V *p, int left, int how) {
+    constexpr int N = 16 / (int)sizeof(V), W = 4 / (int)sizeof(V);      // ... in a word
+    if (how == BY_SIXTEEN) {
+        fetch8_wide(dst, p, left);
+    } else if (how == BY_WORD) {
+#pragma unroll
+        for (int k = 0; k < 8 / W; ++k) {
+            const int n = min(max(left - k * W, 0), W);
+            copy_fill<4>(dst + (k * W / N) * 512 + (k * 4) % 16, n > 0 ? p + k * W : p, n * (int)sizeof(V));
+        }
+    } else {
+        Eight<V> e;
+        e.load(p, left, false);
+#pragma unroll
+        for (int h = 0; h < 8 / N; ++h)
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 512 * h), "r"(e.w[4 * h]), "r"(e.w[4 * h + 1]),
+                         "r"(e.w[4 * h + 2]), "r"(e.w[4 * h + 3])
+                         : "memory");
+    }
+}
+
+template <typename V>
+__device__ __forceinline__ void fetched8(uint32_t src, Eight<V> &e) {
+#pragma unroll
+    for (int h = 0; h < (int)sizeof(V) / 2; ++h)
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(e.w[4 * h]), "=r"(e.w[4 * h + 1]), "=r"(e.w[4 * h + 2]), "=r"(e.w[4 * h + 3])
+                     : "r"(src + 512 * h)
+                     : "memory");
+}
+
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// Where value j (of 16) of a row of h lies in its parts: the four that lane t of a product takes, 2t, 2t + 1, 2t + 8, 2t + 9,
+// side by side.
+__device__ __forceinline__ int place(int j) { return ((j & 7) >> 1) * 4 + (j >> 3) * 2 + (j & 1); }
+__device__ __forceinline__ int value_at(int p) { return 2 * (p >> 2) + (p & 1) + 8 * ((p >> 1) & 1); }
+
 struct Args {
     const void *in;                          // [T][D], rows ld_in apart
     const int *ids;
@@ -146,13 +211,15 @@ struct Args {
     void *out;                               // [T][E]
     float *h;                                // [T][r] by row, or null: in p1^T
     const float *h_in;                       // backward: [T][r] by row ...
-    float *ht, *vt;                          // ... and [r][T] by sorted row, alpha times h_in and the values here
-    uint16_t *hp;                            // [3][T][rp] by sorted row: alpha times the values here, in parts
+    uint16_t *hp, *hh;                       // [3][T][rp] by sorted row, in parts: alpha times the values here, alpha times h_in
     int64_t ld_in, ld_base, ld_out;
     int T, D, E, n, r, rp;                   // rp: r rounded up to 16
     int act, base_bf16, out_bf16;
     int in_vec, p1_vec, p2_vec, base_vec, out_vec;        // whole rows on 16-byte boundaries
-    int fine;                                // products of parts down to 2^-24
+    int in_copy, p1_copy, p2_copy;           // Copy
+    int most;                                // rows of a plan's tile
+    int scale_vec;                           // scale and shift on 16-byte boundaries
+    int fine;                                // products of parts down to 2^-25
     int split;                               // blocks of a cluster
     Plan plan;
 };
@@ -263,7 +330,7 @@ __device__ __forceinline__ void narrow(const Args &a, const int *rows, int count
 #pragma unroll
                         for (int q = 0; q <= l; ++q) {
                             const int v = l - q;
-                            if (q >= PI || v >= PP || (l == 2 && !a.fine)) continue;
+                            if (q >= PI || v >= PP) continue;
 #pragma unroll
                             for (int m = 0; m < MT; ++m) {
                                 const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
@@ -363,7 +430,7 @@ __device__ __forceinline__ void widen(const Args &a, const int *rows, int count,
 #pragma unroll
                         for (int q = 0; q <= l; ++q) {
                             const int v = l - q;
-                            if (v >= PP || (l == 2 && !a.fine)) continue;
+                            if (v >= PP) continue;
 #pragma unroll
                             for (int m = 0; m < ME; ++m) mma16816(acc[m][i], f[m][q], q0[v], q1[v]);
                         }
@@ -473,19 +540,35 @@ __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__
     if (a.split > 1 && id >= 0) cluster_leave();
 }
 
-// The plan's tiles, first half: h, alpha h in parts for the second half, and what the gradients need.
+// What the kernels below have on its way: a warp copies units of what it will work on next into a ring of its own in shared
+// memory, and a lane reads back what it has copied itself, without a barrier.  (The same loads into registers, two
+// blocks of 8 warps an SM: 35 and 67 us for the two halves of 4096 rows, 4096 -> 4096 at rank 64.)
+
 template <typename TI, typename TP, int MT, int NT>
-__global__ void __launch_bounds__(THREADS, sizeof(TI) + sizeof(TP) == 4 ? 2 : 1) narrow_kernel(const __grid_constant__ Args a) {
-    constexpr int M = 16 * MT, R = 8 * NT;
+struct NarrowRing {
+    static constexpr int UNIT = (MT * 2 * (int)sizeof(TI) + NT * (int)sizeof(TP)) / 2 * 512;       // 32 values along D
+    static constexpr int DEPTH = 200 * 1024 / (WARPS * UNIT) < 4 ? 200 * 1024 / (WARPS * UNIT) : 4;
+    static constexpr int BYTES = WARPS * DEPTH * UNIT;
+    static_assert(DEPTH >= 2 && BYTES >= (WARPS + 1) * 16 * MT * 8 * NT * 4, "the sums lie where the ring was");
+};
+
+// The plan's tiles, first half: h, and alpha h in parts for the second half and the gradients.
+template <typename TI, typename TP, int MT, int NT>
+__global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constant__ Args a) {
+    constexpr int M = 16 * MT, R = 8 * NT, PI = parts_of<TI>(), PP = parts_of<TP>(), CI = sizeof(TI) / 2, CP = sizeof(TP) / 2;
+    using Ring = NarrowRing<TI, TP, MT, NT>;
     extern __shared__ __align__(16) uint8_t smem[];
-    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R]
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R], when the ring is done with
     float *part = red + WARPS * M * R;                                   // [M][R]
     __shared__ int rows[M];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
+    const uint32_t ring = shared_at(smem) + warp * Ring::DEPTH * Ring::UNIT + lane * 16;
     pdl_wait();
     pdl_trigger();
-    if (tile >= *a.plan.tiles_n) return;
-    const Tile x = a.plan.tiles[tile];
+    const int tiles = *a.plan.tiles_n;
+    const Tile x = a.plan.tiles[tile];                                   // there is room for as many as blocks
+    if (tile >= tiles) return;
     if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
     __syncthreads();
     if (x.id < 0) {
@@ -496,11 +579,99 @@ __global__ void __launch_bounds__(THREADS, sizeof(TI) + sizeof(TP) == 4 ? 2 : 1)
     cg::cluster_group cluster = cg::this_cluster();
     const float alpha = a.alpha ? a.alpha[x.id] : 1.0f;
     const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
+    const TI *row[MT][2];
+    bool live[MT][2];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = 16 * m + 8 * i + g;
+            live[m][i] = e < x.count;
+            row[m][i] = static_cast<const TI *>(a.in) + (live[m][i] ? rows[e] : rows[0]) * a.ld_in + 8 * t;
+        }
     for (int j0 = 0; j0 < a.r; j0 += R) {
+        const TP *p1 = static_cast<const TP *>(a.p1) + ((int64_t)x.id * a.r + j0) * a.D + 8 * t;
+        int next = b0 + warp, put = 0, get = 0;
+        auto fetch = [&]() {
+            if (next < b1) {
+                const uint32_t d = ring + put * Ring::UNIT;
+                const int k = 32 * next, left = a.D - k - 8 * t;
+                if (a.in_copy == BY_SIXTEEN && a.p1_copy == BY_SIXTEEN) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            fetch8_wide(d + (2 * m + i) * CI * 512, left > 0 ? row[m][i] + k : row[m][i], live[m][i] ? left : 0);
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        const bool some = j0 + 8 * j + g < a.r && left > 0;
+                        fetch8_wide(d + (2 * MT * CI + j * CP) * 512, some ? p1 + (int64_t)(8 * j + g) * a.D + k : p1, some ? left : 0);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int e = 0; e < 2 * MT; ++e) {
+                        const bool some = 8 * e + g < x.count && left > 0;
+                        const TI *in = static_cast<const TI *>(a.in);
+                        fetch8(d + e * CI * 512, some ? in + rows[8 * e + g] * a.ld_in + k + 8 * t : in, some ? left : 0, a.in_copy);
+                    }
+#pragma unroll 1
+                    for (int j = 0; j < NT; ++j) {
+                        const bool some = j0 + 8 * j + g < a.r && left > 0;
+                        fetch8(d + (2 * MT * CI + j * CP) * 512, some ? p1 + (int64_t)(8 * j + g) * a.D + k : p1, some ? left : 0, a.p1_copy);
+                    }
+                }
+            }
+            commit();
+            next += WARPS;
+            if (++put == Ring::DEPTH) put = 0;
+        };
+#pragma unroll
+        for (int d = 0; d < Ring::DEPTH - 1; ++d) fetch();
         float acc[MT][NT][4];
-        narrow<TI, TP, MT, NT, 1>(a, rows, x.count, static_cast<const TP *>(a.p1) + ((int64_t)x.id * a.r + j0) * a.D, a.r - j0, b0, b1,
-                                  acc);
-        if (j0 > 0 && a.split > 1) cluster.sync();                       // others have read the last round's part
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+        for (int b = b0 + warp; b < b1; b += WARPS) {
+            arrived<Ring::DEPTH - 2>();
+            fetch();
+            const uint32_t d = ring + get * Ring::UNIT;
+            if (++get == Ring::DEPTH) get = 0;
+            uint32_t xp[MT][2][PI][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    Eight<TI> e;
+                    fetched8(d + (2 * m + i) * CI * 512, e);
+                    along(e, xp[m][i]);
+                }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                Eight<TP> e;
+                uint32_t pp[PP][4];
+                fetched8(d + (2 * MT * CI + j * CP) * 512, e);
+                along(e, pp);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int l = 2; l >= 0; --l)                                 // the smallest products first
+#pragma unroll
+                        for (int q = 0; q <= l; ++q) {
+                            const int v = l - q;
+                            if (q >= PI || v >= PP) continue;
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) {
+                                const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
+                                                       xp[m][1][q][2 * s + 1]};
+                                mma16816(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
+                            }
+                        }
+            }
+        }
+        arrived<0>();
         add_warps<MT, NT>(acc, red, part, R, R);
         if (a.split > 1) cluster.sync();
         else __syncthreads();
@@ -510,14 +681,22 @@ __global__ void __launch_bounds__(THREADS, sizeof(TI) + sizeof(TP) == 4 ? 2 : 1)
             const int m = e / R, j = j0 + e % R;
             if (j >= a.rp) continue;
             const float v = add_blocks(cluster, part + e, a.split);
+            const int64_t at = (int64_t)(x.start + m) * a.rp + j / 16 * 16 + place(j & 15);
             uint32_t s[3];
             split2(__float_as_uint(alpha * v), 0u, s);
 #pragma unroll
-            for (int q = 0; q < 3; ++q) a.hp[((int64_t)q * a.T + x.start + m) * a.rp + j] = (uint16_t)s[q];
-            if (j >= a.r) continue;
-            if (a.h) a.h[(int64_t)rows[m] * a.r + j] = v;
-            if (a.vt) a.vt[(int64_t)j * a.T + x.start + m] = alpha * v;
-            if (a.ht) a.ht[(int64_t)j * a.T + x.start + m] = alpha * a.h_in[(int64_t)rows[m] * a.r + j];
+            for (int q = 0; q < 3; ++q) a.hp[(int64_t)q * a.T * a.rp + at] = (uint16_t)s[q];
+            if (a.h && j < a.r) a.h[(int64_t)rows[m] * a.r + j] = v;
+            if (a.hh) {
+                split2(__float_as_uint(j < a.r ? alpha * a.h_in[(int64_t)rows[m] * a.r + j] : 0.0f), 0u, s);
+#pragma unroll
+                for (int q = 0; q < 3; ++q) a.hh[(int64_t)q * a.T * a.rp + at] = (uint16_t)s[q];
+            }
+        }
+        // before the next round's ring lies where the parts are
+        if (j0 + R < a.r) {
+            if (a.split > 1) cluster.sync();
+            else __syncthreads();
         }
     }
     if (a.split > 1) {
@@ -527,31 +706,245 @@ __global__ void __launch_bounds__(THREADS, sizeof(TI) + sizeof(TP) == 4 ? 2 : 1)
     }
 }
 
-constexpr int WIDE_WARPS = 4;
-
-// ... second half: a block takes 64 columns a warp of a tile.
+// Bytes of a warp of the second half: its ring (blocks of 64 columns, 16 KS of r), h in parts.
 template <typename TP, int KS>
-__global__ void __launch_bounds__(32 * WIDE_WARPS) widen_kernel(const __grid_constant__ Args a, int chunks, int most) {
+struct WidenRing {
+    static constexpr int BLOCK = KS * 4 * (int)sizeof(TP) / 2 * 512;
+    static constexpr int BYTES = 2 * BLOCK > 16384 ? 2 * BLOCK : 16384;
+    static constexpr int DEPTH = BYTES / BLOCK;
+};
+// Halves (of 32 rows) x tiles of 16 x steps x parts.
+__host__ __device__ inline int h_bytes(int most, int rp, int fine) { return rp > 64 ? 0 : most / 16 * (rp / 16) * (fine ? 3 : 2) * 512; }
+
+// A lane's four rows of 16 columns.
+template <typename V>
+__device__ __forceinline__ void put16(const Args &a, const int (*rows)[2], int c, int left, const float (*acc)[8][4]) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            float v[16];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) v[k] = acc[m][k & 7][2 * i + (k >> 3)];
+            if (rows[m][i] >= 0) store16<V>(a.out, (int64_t)rows[m][i] * a.ld_out + c, left, a.out_vec, v);
+        }
+}
+
+// ... second half: a warp takes `per` blocks of 64 columns of a tile, and works by itself.
+template <typename TP, int KS, bool FINE>
+__global__ void __launch_bounds__(THREADS, 1) widen_kernel(const __grid_constant__ Args a, int tiles_most, int groups, int per) {
+    constexpr int PP = parts_of<TP>(), CP = sizeof(TP) / 2;
+    using Ring = WidenRing<TP, KS>;
     extern __shared__ __align__(16) uint8_t smem[];
-    uint16_t *hs = reinterpret_cast<uint16_t *>(smem);                   // [3][most][rp + 8]
-    __shared__ int rows[64];
-    const int warp = threadIdx.x >> 5, tile = blockIdx.x / chunks, b = (blockIdx.x - tile * chunks) * WIDE_WARPS + warp;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    constexpr int PARTS = FINE ? 3 : 2;
+    const int steps = a.rp / 16;
+    const uint32_t ring = shared_at(smem) + warp * (Ring::BYTES + h_bytes(a.most, a.rp, FINE)) + lane * 16;
+    const uint32_t hs = ring - lane * 8 + Ring::BYTES;
+    const int64_t task = (int64_t)blockIdx.x * (blockDim.x >> 5) + warp;
+    const int tile = (int)(task / groups), first = (int)(task - (int64_t)tile * groups) * per, last = min((a.E + 63) / 64, first + per);
     pdl_trigger();
     pdl_wait();
-    if (tile >= *a.plan.tiles_n) return;
+    if (tile >= tiles_most || first >= last) return;
+    const int tiles = *a.plan.tiles_n;
     const Tile x = a.plan.tiles[tile];
-    if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
-    const int hpitch = a.rp + 8, eights = a.rp / 8, parts = a.fine ? 3 : 2;
-    if (x.id >= 0)
-        for (int e = threadIdx.x; e < parts * most * eights; e += 32 * WIDE_WARPS) {
-            const int q = e / (most * eights), m = e / eights - q * most, j = 8 * (e % eights);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (m < x.count) v = *reinterpret_cast<const uint4 *>(a.hp + ((int64_t)q * a.T + x.start + m) * a.rp + j);
-            *reinterpret_cast<uint4 *>(hs + (q * most + m) * hpitch + j) = v;
+    if (tile >= tiles) return;
+    const bool big = a.rp > 64;                                          // h stays in global memory, r in chunks of 64
+    const int chunks = big ? (a.rp + 63) / 64 : 1, units = x.id >= 0 ? (last - first) * chunks : 0;
+    const int halves = x.count > 32 ? 2 : 1;
+    int rows[2][2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int e = 32 * h + 16 * m + 8 * i + g;
+                rows[h][m][i] = e < x.count ? a.plan.order[x.start + e] : -1;
+            }
+    const TP *p2 = static_cast<const TP *>(a.p2) + (int64_t)max(x.id, 0) * a.r * a.E;
+    int put = 0, next = 0;
+    auto fetch = [&]() {
+        if (next < units) {
+            const int b = next / chunks, c = 64 * (first + b) + 8 * g, k0 = (next - b * chunks) * 64, left = a.E - c;
+            const uint32_t d = ring + put * Ring::BLOCK;
+            if (a.p2_copy == BY_SIXTEEN) {
+#pragma unroll
+                for (int e = 0; e < 4 * KS; ++e) {
+                    const int j = k0 + 16 * (e >> 2) + 2 * t + (e & 1) + 8 * ((e >> 1) & 1);
+                    const bool some = j < a.r && left > 0;
+                    fetch8_wide(d + e * CP * 512, some ? p2 + (int64_t)j * a.E + c : p2, some ? left : 0);
+                }
+            } else {
+#pragma unroll 1
+                for (int e = 0; e < 4 * KS; ++e) {
+                    const int j = k0 + 16 * (e >> 2) + 2 * t + (e & 1) + 8 * ((e >> 1) & 1);
+                    const bool some = j < a.r && left > 0;
+                    fetch8(d + e * CP * 512, some ? p2 + (int64_t)j * a.E + c : p2, some ? left : 0, a.p2_copy);
+                }
+            }
         }
-    __syncthreads();
-    if (64 * b >= a.E) return;
-    for (int m0 = 0; m0 < x.count; m0 += 32) widen<TP, 2, KS>(a, rows, x.count, m0, x.id, b, hs, most, hpitch);
+        commit();
+        ++next;
+        if (++put == Ring::DEPTH) put = 0;
+    };
+    // Lane's parts of h of row e (of 16 + 8 i + g) at step s: 8 bytes.
+    auto h_at = [&](int q, int e, int s) { return a.hp + ((int64_t)q * a.T + x.start + min(e, x.count - 1)) * a.rp + 16 * s + 4 * t; };
+    if (x.id >= 0 && !big)
+        for (int m = 0; m < 2 * halves; ++m)
+            for (int s = 0; s < steps; ++s)
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int e = 16 * m + 8 * i + g;
+                        copy_fill<8>(hs + ((m * steps + s) * PARTS + q) * 512 + i * 256, h_at(q, e, s), e < x.count ? 8 : 0);
+                    }
+    if (x.id >= 0)
+#pragma unroll
+        for (int d = 0; d < Ring::DEPTH - 1; ++d) fetch();
+    int get = 0;
+    for (int b = first; b < last; ++b) {
+        const int c = 64 * b + 16 * t, left = a.E - c;
+        const bool whole = 64 * b + 64 <= a.E, early = a.base && a.base_bf16 && a.base_vec && whole;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (h >= halves) break;
+            uint4 base[2][2][2];                                         // on its way during the products
+            if (early) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint16_t *p = static_cast<const uint16_t *>(a.base) + (int64_t)max(rows[h][m][i], 0) * a.ld_base + c;
+                        base[m][i][0] = reinterpret_cast<const uint4 *>(p)[0];
+                        base[m][i][1] = reinterpret_cast<const uint4 *>(p)[1];
+                    }
+            } else if (a.base && left > 0) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int64_t at = (int64_t)max(rows[h][m][i], 0) * a.ld_base + c;
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(a.base) + at * (a.base_bf16 ? 2 : 4)));
+                    }
+            }
+            float acc[2][8][4];
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+            if (x.id >= 0)
+                for (int ch = 0; ch < chunks; ++ch) {
+                    if (h == 0) {
+                        fetch();                                         // where the last one read was
+                        arrived<Ring::DEPTH - 1>();
+                    }
+                    const uint32_t d = ring + get * Ring::BLOCK;
+                    if (h + 1 == halves && ++get == Ring::DEPTH) get = 0;
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) {
+                        const int step = 4 * ch + s;
+                        if (step >= steps) break;
+                        Eight<TP> p[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) fetched8(d + (4 * s + i) * CP * 512, p[i]);
+                        uint32_t f[2][3][4];
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+#pragma unroll
+                            for (int q = 0; q < PARTS; ++q) {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    uint32_t lo, hi;
+                                    if (big) {
+                                        const uint2 w = *reinterpret_cast<const uint2 *>(h_at(q, 16 * m + 8 * i + g, step));
+                                        lo = w.x;
+                                        hi = w.y;
+                                    } else {
+                                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
+                                                     : "=r"(lo), "=r"(hi)
+                                                     : "r"(hs + (((2 * h + m) * steps + step) * PARTS + q) * 512 + i * 256)
+                                                     : "memory");
+                                    }
+                                    f[m][q][i] = lo;
+                                    f[m][q][2 + i] = hi;
+                                }
+                            }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t q0[PP], q1[PP];
+                            across(p[0], p[1], i, q0);
+                            across(p[2], p[3], i, q1);
+#pragma unroll
+                            for (int l = 2; l >= 0; --l)
+#pragma unroll
+                                for (int q = 0; q <= l; ++q) {
+                                    const int v = l - q;
+                                    if (v >= PP || (l == 2 && !FINE)) continue;
+#pragma unroll
+                                    for (int m = 0; m < 2; ++m) mma16816(acc[m][i], f[m][q], q0[v], q1[v]);
+                                }
+                        }
+                    }
+                }
+            // value k of the lane's 16 of row (m, i)
+            auto z = [&](int m, int i, int k) -> float & { return acc[m][k & 7][2 * i + (k >> 3)]; };
+            if (early) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) {
+                            const uint4 q = base[m][i][k >> 3];
+                            const int e = (k & 7) >> 1;
+                            const uint32_t w = e == 0 ? q.x : e == 1 ? q.y : e == 2 ? q.z : q.w;
+                            z(m, i, k) += __uint_as_float((k & 1) ? w & 0xffff0000u : w << 16);
+                        }
+            } else if (a.base) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float f[16];
+                        const int64_t at = (int64_t)max(rows[h][m][i], 0) * a.ld_base + c;
+                        const int n = rows[h][m][i] >= 0 ? left : 0;
+                        if (a.base_bf16) load16<uint16_t>(a.base, at, n, a.base_vec, f);
+                        else load16<float>(a.base, at, n, a.base_vec, f);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z(m, i, k) += f[k];
+                    }
+            }
+            if (a.scale || a.shift) {
+                float sc[16], sh[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) { sc[k] = 1.0f; sh[k] = 0.0f; }
+                if (a.scale) load16<float>(a.scale, c, left, a.scale_vec, sc);
+                if (a.shift) load16<float>(a.shift, c, left, a.scale_vec, sh);
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z(m, i, k) = fmaf(z(m, i, k), sc[k], sh[k]);
+            }
+            if (a.act != MINW_ACT_NONE)
+                with_act(a.act, [&](auto act) {
+#pragma unroll
+                    for (int m = 0; m < 2; ++m)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) z(m, i, k) = act_value<act.value>(z(m, i, k));
+                });
+            if (a.out_bf16) put16<uint16_t>(a, rows[h], c, whole ? 64 : left, acc);
+            else put16<float>(a, rows[h], c, whole ? 64 : left, acc);
+            __syncwarp();
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -559,29 +952,41 @@ __global__ void __launch_bounds__(32 * WIDE_WARPS) widen_kernel(const __grid_con
 // ---------------------------------------------------------------------------
 
 struct Job {
-    const float *a;                          // [r][T] by sorted row
+    const uint16_t *a;                       // [3][T][rp] by sorted row, in parts
     const void *z;                           // [T][C], rows ld apart
     float *out;                              // [n][r][C]
     int64_t ld;
     int C, blocks;                           // blocks: of this job for a user
-    int vec, out_vec;
+    int copy, out_vec;
 };
 
 struct GradArgs {
     Job job[2];
-    int jobs, T, n, r, along;                // along: warps that share a user's rows (the others: columns)
+    int jobs, T, n, r, rp, along;            // along: warps that share a user's rows (the others: columns)
     Plan plan;
 };
 
-// RT: tiles of 16 of r in one go.  A warp takes 64 columns.
+constexpr int CHUNK = 64;                    // rows whose parts are in shared memory at a time
+constexpr int ORDER = 1024;                  // rows whose places are
+
+template <typename TZ, int RT>
+struct GradRing {
+    static constexpr int UNIT = 4 * (int)sizeof(TZ) / 2 * 512, DEPTH = 16384 / UNIT, BYTES = WARPS * DEPTH * UNIT;
+    static constexpr int PITCH = 16 * RT + 8, PARTS = 3 * CHUNK * PITCH * 2;       // bytes of a chunk's parts, twice
+    static constexpr int ALL = BYTES + 2 * PARTS;
+};
+
+// RT: tiles of 16 of r in one go.  A warp takes 64 columns: its rows' values come by a ring of its own (as above), the parts of the
+// rows, which all warps need, by chunks for the block.
 template <typename TZ, int RT>
 __global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant__ GradArgs a) {
-    constexpr int PZ = parts_of<TZ>();
+    constexpr int PZ = parts_of<TZ>(), CZ = sizeof(TZ) / 2;
+    using Ring = GradRing<TZ, RT>;
     extern __shared__ __align__(16) uint8_t smem[];
     float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][64] where warps share rows
+    uint8_t *parts = smem + Ring::BYTES;                                 // [2][3][CHUNK][PITCH]
+    __shared__ int order[ORDER];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    pdl_trigger();
-    pdl_wait();
     const int all = a.job[0].blocks + (a.jobs > 1 ? a.job[1].blocks : 0);
     const int u = blockIdx.x / all;
     int b = blockIdx.x - u * all;
@@ -589,8 +994,11 @@ __global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant
     if (b >= a.job[0].blocks) b -= a.job[0].blocks;
     const int wa = warp % a.along, wc = warp / a.along;
     const int c0 = 64 * (b * (WARPS / a.along) + wc), c = c0 + 8 * g, left = job.C - c;
+    const uint32_t ring = shared_at(smem) + warp * Ring::DEPTH * Ring::UNIT + lane * 16;
+    const TZ *z = static_cast<const TZ *>(job.z);
+    pdl_trigger();
+    pdl_wait();
     const int first = a.plan.first[u], count = a.plan.first[u + 1] - first;
-    const TZ *z = static_cast<const TZ *>(job.z) + c;
     for (int j0 = 0; j0 < a.r; j0 += 16 * RT) {
         float acc[RT][8][4];
 #pragma unroll
@@ -599,42 +1007,104 @@ __global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant
             for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) acc[m][i][k] = 0.0f;
-        for (int s = 16 * wa; s < count; s += 16 * a.along) {
-            Eight<TZ> v[4];
+        const int ranks = min(16 * RT, a.rp - j0);
+        for (int s0 = 0; s0 < count; s0 += ORDER) {
+            const int seg = min(ORDER, count - s0);
+            __syncthreads();
+            for (int e = threadIdx.x; e < seg; e += THREADS) order[e] = a.plan.order[first + s0 + e];
+            __syncthreads();
+            // the warp's steps of 16 rows: wa, wa + along, ...
+            int next = wa, put = 0, get = 0;
+            auto fetch = [&]() {
+                if (16 * next < seg) {
+                    const uint32_t d = ring + put * Ring::UNIT;
+                    if (job.copy == BY_SIXTEEN) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = s + 2 * t + (i & 1) + 8 * (i >> 1);
-                if (e < count && left > 0) v[i].load(z + a.plan.order[first + e] * job.ld, left, job.vec);
-                else v[i].zero();
-            }
-            uint32_t f[RT][3][4];
-#pragma unroll
-            for (int m = 0; m < RT; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = j0 + 16 * m + g + 8 * (i & 1), e = s + 2 * t + 8 * (i >> 1);
-                    const float *p = job.a + (int64_t)j * a.T + first + e;
-                    const float x = j < a.r && e < count ? p[0] : 0.0f, y = j < a.r && e + 1 < count ? p[1] : 0.0f;
-                    uint32_t w[3];
-                    split2(__float_as_uint(x), __float_as_uint(y), w);
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) f[m][q][i] = w[q];
-                }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint32_t q0[PZ], q1[PZ];
-                across(v[0], v[1], i, q0);
-                across(v[2], v[3], i, q1);
-#pragma unroll
-                for (int l = 2; l >= 0; --l)
-#pragma unroll
-                    for (int q = 0; q <= l; ++q) {
-                        const int k = l - q;
-                        if (k >= PZ) continue;
-#pragma unroll
-                        for (int m = 0; m < RT; ++m) mma16816(acc[m][i], f[m][q], q0[k], q1[k]);
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = 16 * next + 2 * t + (i & 1) + 8 * (i >> 1);
+                            const bool some = e < seg && left > 0;
+                            fetch8_wide(d + i * CZ * 512, some ? z + order[e] * job.ld + c : z, some ? left : 0);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int i = 0; i < 4; ++i) {
+                            const int e = 16 * next + 2 * t + (i & 1) + 8 * (i >> 1);
+                            const bool some = e < seg && left > 0;
+                            fetch8(d + i * CZ * 512, some ? z + order[e] * job.ld + c : z, some ? left : 0, job.copy);
+                        }
                     }
+                }
+                next += a.along;
+                if (++put == Ring::DEPTH) put = 0;
+            };
+            auto fetch_parts = [&](int chunk) {                          // rows past the last: zeros
+                const int rows0 = chunk * CHUNK, eights = ranks / 8;
+                if (rows0 < seg)
+                    for (int e = threadIdx.x; e < 3 * CHUNK * eights; e += THREADS) {
+                        const int q = e / (CHUNK * eights), m = e / eights - q * CHUNK, j = 8 * (e % eights);
+                        const bool some = rows0 + m < seg;
+                        copy_fill<16>(shared_at(parts + (chunk & 1) * Ring::PARTS + ((q * CHUNK + m) * Ring::PITCH + j) * 2),
+                                      job.a + ((int64_t)q * a.T + first + s0 + (some ? rows0 + m : 0)) * a.rp + j0 + j, some ? 16 : 0);
+                    }
+            };
+            fetch_parts(0);
+            commit();
+#pragma unroll
+            for (int d = 0; d < Ring::DEPTH - 1; ++d) {
+                fetch();
+                commit();
             }
+            for (int chunk = 0; chunk * CHUNK < seg; ++chunk) {
+                // the chunk's parts went out before the units of the chunk before (the first one's: of the whole ring)
+                if (a.along == 1) arrived<(Ring::DEPTH > 4 ? 4 : 3)>();
+                else if (a.along == 2) arrived<2>();
+                else arrived<1>();
+                __syncthreads();
+                fetch_parts(chunk + 1);
+                commit();
+                for (int s = 0; s < CHUNK / 16; ++s) {
+                    const int step = chunk * (CHUNK / 16) + s;
+                    if (step % a.along != wa || 16 * step >= seg) continue;
+                    fetch();
+                    commit();
+                    arrived<Ring::DEPTH - 1>();
+                    const uint32_t d = ring + get * Ring::UNIT;
+                    if (++get == Ring::DEPTH) get = 0;
+                    Eight<TZ> v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) fetched8(d + i * CZ * 512, v[i]);
+                    uint32_t f[RT][3][4];
+#pragma unroll
+                    for (int m = 0; m < RT; ++m)
+#pragma unroll
+                        for (int q = 0; q < 3; ++q) {
+                            // four transposed 8 x 8 pieces: rows 0-7 and 8-15 of both halves of j
+                            const uint32_t at = shared_at(parts + (chunk & 1) * Ring::PARTS) +
+                                                ((q * CHUNK + 16 * s + (lane & 7) + 8 * (lane >> 4)) * Ring::PITCH + 16 * m + 8 * ((lane >> 3) & 1)) * 2;
+                            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(f[m][q][0]), "=r"(f[m][q][1]), "=r"(f[m][q][2]), "=r"(f[m][q][3])
+                                         : "r"(at)
+                                         : "memory");
+                        }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t q0[PZ], q1[PZ];
+                        across(v[0], v[1], i, q0);
+                        across(v[2], v[3], i, q1);
+#pragma unroll
+                        for (int l = 2; l >= 0; --l)
+#pragma unroll
+                            for (int q = 0; q <= l; ++q) {
+                                const int k = l - q;
+                                if (k >= PZ) continue;
+#pragma unroll
+                                for (int m = 0; m < RT; ++m) mma16816(acc[m][i], f[m][q], q0[k], q1[k]);
+                            }
+                    }
+                }
+                __syncthreads();                                         // the parts have been read
+            }
+            arrived<0>();
         }
 #pragma unroll
         for (int m = 0; m < RT; ++m) {
@@ -655,7 +1125,7 @@ __global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant
             if (wa != 0) continue;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int j = j0 + 16 * m + 8 * i + g, cc = c0 + 16 * t;
+                const int j = j0 + 16 * m + value_at(8 * i + g), cc = c0 + 16 * t;
                 if (j >= a.r || cc >= job.C) continue;
                 float y[16];
 #pragma unroll
@@ -666,6 +1136,7 @@ __global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant
                 store16<float>(job.out, ((int64_t)u * a.r + j) * job.C + cc, job.C - cc, job.out_vec, y);
             }
         }
+        __syncthreads();
     }
 }
 
@@ -677,13 +1148,13 @@ using namespace minw_host;
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
-// Rows of a tile: 64, where h in registers leaves room for them (r <= 32), else 32.
-static int rows_of(int r) { return r <= 32 ? 64 : 32; }
+// Rows of a tile: 64, where h in registers (and a ring in shared memory) leaves room for them, else 32.
+static int rows_of(int r, bool bf16) { return r <= 32 || (r <= 64 && bf16) ? 64 : 32; }
 static int rank_pitch(int r) { return (r + 15) / 16 * 16; }
 
 constexpr int W4_ROWS = 32;                  // rows of w4 products at a time
 
-static int64_t tiles_of(int64_t T, int n, int r) { return std::min<int64_t>(T, T / rows_of(r) + std::min<int64_t>(T, (int64_t)n + 1)); }
+static int64_t tiles_of(int64_t T, int n, int most) { return std::min<int64_t>(T, T / most + std::min<int64_t>(T, (int64_t)n + 1)); }
 
 static bool counts_in_shared(int n) { return (int64_t)(n + 1) * COUNTS * 4 <= 128 * 1024; }
 
@@ -695,7 +1166,7 @@ static Plan plan_at(uint8_t *base, int64_t T, int n, int r, int64_t *used) {
         at += up(bytes, 16);
         return q;
     };
-    p.tiles = reinterpret_cast<Tile *>(take(tiles_of(T, n, r) * sizeof(Tile)));
+    p.tiles = reinterpret_cast<Tile *>(take(tiles_of(T, n, rows_of(r, false)) * sizeof(Tile)));
     p.order = reinterpret_cast<int *>(take(T * 4));
     p.first = reinterpret_cast<int *>(take(((int64_t)n + 2) * 4));
     p.tiles_n = reinterpret_cast<int *>(take(4));
@@ -704,11 +1175,11 @@ static Plan plan_at(uint8_t *base, int64_t T, int n, int r, int64_t *used) {
     return p;
 }
 
-static minw_status make_plan(const Plan &p, const int *ids, int T, int n, int r, cudaStream_t s) {
+static minw_status make_plan(const Plan &p, const int *ids, int T, int n, int most, cudaStream_t s) {
     const bool in_shared = counts_in_shared(n);
     if (in_shared && !allow_shared(reinterpret_cast<const void *>(plan_kernel), 128 * 1024)) return MINW_ECUDA;
     const size_t smem = in_shared ? (size_t)(n + 1) * COUNTS * 4 : 0;
-    return launch_pdl(plan_kernel, dim3(1), dim3(PLAN_THREADS), smem, s, ids, T, n, rows_of(r), p, in_shared ? 1 : 0) == cudaSuccess
+    return launch_pdl(plan_kernel, dim3(1), dim3(PLAN_THREADS), smem, s, ids, T, n, most, p, in_shared ? 1 : 0) == cudaSuccess
                ? MINW_OK : launch_failed();
 }
 
@@ -739,7 +1210,7 @@ static cudaError_t launch_few(const Args &a, cudaStream_t s) {
 
 template <typename TI, typename TP, int MT, int NT>
 static cudaError_t launch_narrow(const Args &a, int64_t tiles, cudaStream_t s) {
-    constexpr int bytes = (WARPS + 1) * 16 * MT * 8 * NT * 4;
+    constexpr int bytes = NarrowRing<TI, TP, MT, NT>::BYTES;
     return launch_clusters(narrow_kernel<TI, TP, MT, NT>, a, tiles, bytes, bytes, s);
 }
 
@@ -748,19 +1219,29 @@ static cudaError_t launch_types(const Args &a, bool few, int64_t tiles, cudaStre
     if (few)
         return a.r <= 16 ? launch_few<TI, TP, 2>(a, s) : a.r <= 32 ? launch_few<TI, TP, 4>(a, s) : launch_few<TI, TP, 8>(a, s);
     return a.r <= 16 ? launch_narrow<TI, TP, 4, 2>(a, tiles, s) : a.r <= 32 ? launch_narrow<TI, TP, 4, 4>(a, tiles, s)
-                                                                            : launch_narrow<TI, TP, 2, 8>(a, tiles, s);
+                     : a.most == 32 ? launch_narrow<TI, TP, 2, 8>(a, tiles, s) : launch_narrow<uint16_t, uint16_t, 4, 8>(a, tiles, s);
 }
 
 template <typename TP, int KS>
 static cudaError_t launch_widen(const Args &a, int64_t tiles, cudaStream_t s) {
-    const int chunks = (a.E + 64 * WIDE_WARPS - 1) / (64 * WIDE_WARPS), most = rows_of(a.r);
-    auto kern = widen_kernel<TP, KS>;
-    if (!allow_shared(reinterpret_cast<const void *>(kern), 3 * 64 * (MAX_RANK + 8) * 2)) return cudaErrorInvalidValue;
-    return launch_pdl(kern, dim3((unsigned)(tiles * chunks)), dim3(32 * WIDE_WARPS), (size_t)3 * most * (a.rp + 8) * 2, s, a, chunks, most);
+    constexpr int LIMIT = 225 * 1024;
+    auto kern = a.fine ? widen_kernel<TP, KS, true> : widen_kernel<TP, KS, false>;
+    if (!allow_shared(reinterpret_cast<const void *>(kern), LIMIT)) return cudaErrorInvalidValue;
+    const int bytes = WidenRing<TP, KS>::BYTES + h_bytes(a.most, a.rp, a.fine), warps = std::min(WARPS, LIMIT / bytes);
+    // blocks of columns of a warp: all warps of the SMs busy once, if the tiles are few
+    const int blocks = (a.E + 63) / 64, sms = num_sms() > 0 ? num_sms() : 152;
+    const int groups = (int)std::min<int64_t>(blocks, std::max<int64_t>(1, (int64_t)sms * warps / tiles));
+    const int per = (blocks + groups - 1) / groups, g = (blocks + per - 1) / per;
+    return launch_pdl(kern, dim3((unsigned)((tiles * g + warps - 1) / warps)), dim3(32 * warps), (size_t)warps * bytes, s, a, (int)tiles, g, per);
 }
 
 static bool vec_rows(const void *p, int64_t ld, int bf16) {
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
+}
+
+static int copy_rows(const void *p, int64_t ld, int bf16) {
+    const int size = bf16 ? 2 : 4;
+    return vec_rows(p, ld, bf16) ? BY_SIXTEEN : reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld * size % 4 == 0 ? BY_WORD : BY_VALUE;
 }
 
 // One pass through the adapters; types as in the public calls.  plan null: T <= SMALL.
@@ -771,10 +1252,16 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     a.p2_vec = vec_rows(a.p2, a.E, p_bf16);
     a.base_vec = vec_rows(a.base, a.ld_base, a.base_bf16);
     a.out_vec = vec_rows(a.out, a.ld_out, a.out_bf16);
-    a.fine = !a.out_bf16 || a.h || a.vt;
+    a.in_copy = copy_rows(a.in, a.ld_in, in_bf16);
+    a.p1_copy = copy_rows(a.p1, a.D, p_bf16);
+    a.p2_copy = copy_rows(a.p2, a.E, p_bf16);
+    a.scale_vec = vec_rows(a.scale, 4, 0) && vec_rows(a.shift, 4, 0);
     if (plan) a.plan = *plan;
-    const int64_t tiles = plan ? tiles_of(a.T, a.n, a.r) : a.T;
-    a.split = !plan ? 8 : tiles <= 38 ? 8 : tiles <= 76 ? 4 : 2;
+    const int64_t tiles = plan ? tiles_of(a.T, a.n, a.most) : a.T;
+    // a block an SM: as many blocks to a tile as there are SMs for
+    const int sms = num_sms() > 0 ? num_sms() : 152;
+    a.split = 8;
+    while (plan && a.split > 1 && tiles * a.split > sms + sms / 8) a.split /= 2;         // (tiles: a bound, mostly above)
     cudaError_t e = in_bf16 ? (p_bf16 ? launch_types<uint16_t, uint16_t>(a, !plan, tiles, s)
                                       : launch_types<uint16_t, float>(a, !plan, tiles, s))
                             : (p_bf16 ? launch_types<float, uint16_t>(a, !plan, tiles, s)
@@ -782,15 +1269,21 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     if (e == cudaSuccess && plan && a.E > 0)
         e = p_bf16 ? (a.rp <= 16 ? launch_widen<uint16_t, 1>(a, tiles, s) : a.rp <= 32 ? launch_widen<uint16_t, 2>(a, tiles, s)
                                                                                        : launch_widen<uint16_t, 4>(a, tiles, s))
-                   : launch_widen<float, 1>(a, tiles, s);
+                   : (a.rp <= 16 ? launch_widen<float, 1>(a, tiles, s) : a.rp <= 32 ? launch_widen<float, 2>(a, tiles, s)
+                                                                                    : launch_widen<float, 4>(a, tiles, s));
     return e == cudaSuccess ? launch_status() : launch_failed();
+}
+
+template <typename TZ, int RT>
+static cudaError_t launch_grads_of(const GradArgs &a, int64_t grid, cudaStream_t s) {
+    constexpr int bytes = GradRing<TZ, RT>::ALL;
+    if (!allow_shared(reinterpret_cast<const void *>(grads_kernel<TZ, RT>), bytes)) return cudaErrorInvalidValue;
+    return launch_pdl(grads_kernel<TZ, RT>, dim3((unsigned)grid), dim3(THREADS), bytes, s, a);
 }
 
 template <typename TZ>
 static cudaError_t launch_grads(const GradArgs &a, int64_t grid, cudaStream_t s) {
-    const size_t smem = a.along > 1 ? WARPS * 16 * 64 * 4 : 0;
-    auto kern = a.r <= 16 ? grads_kernel<TZ, 1> : a.r <= 32 ? grads_kernel<TZ, 2> : grads_kernel<TZ, 4>;
-    return launch_pdl(kern, dim3((unsigned)grid), dim3(THREADS), smem, s, a);
+    return a.r <= 16 ? launch_grads_of<TZ, 1>(a, grid, s) : a.r <= 32 ? launch_grads_of<TZ, 2>(a, grid, s) : launch_grads_of<TZ, 4>(a, grid, s);
 }
 
 struct Shape {
@@ -800,7 +1293,7 @@ struct Shape {
 
 static bool sizes_fit(const Shape &z) {
     if (z.T >= (1 << 27) || z.K > (1 << 28) || z.O > (1 << 28) || z.r > MAX_RANK || z.n >= (1 << 24)) return false;
-    const int64_t tiles = tiles_of(z.T, z.n, z.r), blocks = (z.K + 63) / 64 + (z.O + 63) / 64 + 2;
+    const int64_t tiles = tiles_of(z.T, z.n, rows_of(z.r, false)), blocks = (z.K + 63) / 64 + (z.O + 63) / 64 + 2;
     return z.n * blocks < (1ll << 31) && tiles * std::max<int64_t>(8, blocks) < (1ll << 31);
 }
 
@@ -822,7 +1315,7 @@ size_t minw_adapters_workspace_bytes(int64_t T, int32_t K, int32_t O, int32_t n,
     int64_t used;
     plan_at(nullptr, T, n, r, &used);
     used += 3 * T * rank_pitch(r) * 2;
-    if (backward) return (size_t)(used + 2 * up(T * r * 4, 16));
+    if (backward) return (size_t)(used + 3 * T * rank_pitch(r) * 2);
     return (size_t)std::max<int64_t>(used, std::min<int64_t>(T, W4_ROWS) * O * 4);
 }
 
@@ -847,12 +1340,14 @@ minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T,
     a.in = x; a.ld_in = ldx; a.D = K; a.E = O; a.T = (int)T; a.ids = ids; a.p1 = down; a.p2 = up_; a.n = n; a.r = r;
     a.alpha = alpha; a.base = base; a.base_bf16 = base_type == MINW_BF16; a.ld_base = ldbase; a.scale = scale; a.shift = shift;
     a.act = act; a.out = y; a.out_bf16 = y_type == MINW_BF16; a.ld_out = ldy; a.h = h;
+    a.fine = !a.out_bf16 || h;
+    a.most = rows_of(r, x_type == MINW_BF16 && p_type == MINW_BF16);
     cudaStream_t s = (cudaStream_t)stream;
     if (T <= SMALL) return through(a, x_type == MINW_BF16, p_type == MINW_BF16, nullptr, s);
     int64_t used;
     const Plan p = plan_at(static_cast<uint8_t *>(workspace), T, n, r, &used);
     a.hp = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workspace) + used);
-    const minw_status st = make_plan(p, ids, (int)T, n, r, s);
+    const minw_status st = make_plan(p, ids, (int)T, n, a.most, s);
     return st != MINW_OK ? st : through(a, x_type == MINW_BF16, p_type == MINW_BF16, &p, s);
 }
 
@@ -876,7 +1371,7 @@ minw_status minw_w4_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t
         const int rows = (int)std::min<int64_t>(W4_ROWS, T - t0);
         Args a{};
         a.in = static_cast<const uint8_t *>(x) + t0 * ldx * xs; a.ld_in = ldx; a.D = K; a.E = O; a.T = rows; a.ids = ids + t0;
-        a.p1 = down; a.p2 = up_; a.n = n; a.r = r; a.alpha = alpha; a.out = workspace; a.ld_out = O;
+        a.p1 = down; a.p2 = up_; a.n = n; a.r = r; a.alpha = alpha; a.out = workspace; a.ld_out = O; a.fine = 1;
         const minw_status st = through(a, x_type == MINW_BF16, p_type == MINW_BF16, nullptr, (cudaStream_t)stream);
         if (st != MINW_OK) return st;
         const minw_status sw = w4::matvec(a.in, x_type, ldx, rows, codes, scales, O, K, group, scale, shift, act,
@@ -908,9 +1403,9 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
     int64_t used;
     const Plan p = plan_at(static_cast<uint8_t *>(workspace), T, n, r, &used);
     uint16_t *hp = reinterpret_cast<uint16_t *>(static_cast<uint8_t *>(workspace) + used);
-    float *vt = reinterpret_cast<float *>(hp + 3 * T * rank_pitch(r));
-    float *ht = vt + up(T * r * 4, 16) / 4;
-    minw_status st = make_plan(p, ids, (int)T, n, r, s);
+    uint16_t *hh = hp + 3 * T * rank_pitch(r);
+    const int most = rows_of(r, dy_type == MINW_BF16 && p_type == MINW_BF16);
+    minw_status st = make_plan(p, ids, (int)T, n, most, s);
     if (st != MINW_OK) return st;
     if (T > 0) {
         Args a{};
@@ -918,20 +1413,24 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
         a.alpha = alpha; a.out = dx; a.out_bf16 = x_type == MINW_BF16; a.ld_out = lddx;
         if (accumulate) { a.base = dx; a.base_bf16 = a.out_bf16; a.ld_base = lddx; }
         a.hp = hp;
-        a.vt = ddown ? vt : nullptr;
-        a.ht = dup ? ht : nullptr;
+        a.hh = dup ? hh : nullptr;
         a.h_in = h;
+        a.fine = !a.out_bf16 || ddown;
+        a.most = most;
         st = through(a, dy_type == MINW_BF16, p_type == MINW_BF16, &p, s);
         if (st != MINW_OK) return st;
     }
     // jobs of one type in one launch
     GradArgs ga{};
-    ga.T = (int)T; ga.n = n; ga.r = r; ga.plan = p;
-    const int64_t each = T / n;
-    ga.along = each >= 128 ? 8 : each >= 64 ? 4 : each >= 32 ? 2 : 1;
+    ga.T = (int)T; ga.n = n; ga.r = r; ga.rp = rank_pitch(r); ga.plan = p;
+    // warps share a user's rows where its columns leave SMs without a block, if there are steps of 16 rows for them
+    const int sms = num_sms() > 0 ? num_sms() : 152;
+    const int64_t columns = ((ddown ? (K + 63) / 64 : 0) + (dup ? (O + 63) / 64 : 0)) * (int64_t)n;
+    ga.along = 1;
+    while (ga.along < WARPS / 2 && columns * ga.along / WARPS < 2 * sms && T / n >= 16 * ga.along) ga.along *= 2;
     const int wide = 64 * (WARPS / ga.along);
-    const Job jobs[2] = {{vt, x, ddown, ldx, K, (K + wide - 1) / wide, vec_rows(x, ldx, x_type == MINW_BF16), vec_rows(ddown, K, 0)},
-                         {ht, dy, dup, lddy, O, (O + wide - 1) / wide, vec_rows(dy, lddy, dy_type == MINW_BF16), vec_rows(dup, O, 0)}};
+    const Job jobs[2] = {{hp, x, ddown, ldx, K, (K + wide - 1) / wide, copy_rows(x, ldx, x_type == MINW_BF16), vec_rows(ddown, K, 0)},
+                         {hh, dy, dup, lddy, O, (O + wide - 1) / wide, copy_rows(dy, lddy, dy_type == MINW_BF16), vec_rows(dup, O, 0)}};
     const int types[2] = {x_type, dy_type};
     for (int k = 0; k < 2; ++k) {
         if (!jobs[k].out) continue;
