@@ -218,7 +218,6 @@ struct Args {
     int in_vec, p1_vec, p2_vec, base_vec, out_vec;        // whole rows on 16-byte boundaries
     int in_copy, p1_copy, p2_copy;           // Copy
     int most;                                // rows of a plan's tile
-    int scale_vec;                           // scale and shift on 16-byte boundaries
     int fine;                                // products of parts down to 2^-25
     int split;                               // blocks of a cluster
     Plan plan;
@@ -706,16 +705,6 @@ __global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constan
     }
 }
 
-// Bytes of a warp of the second half: its ring (blocks of 64 columns, 16 KS of r), h in parts.
-template <typename TP, int KS>
-struct WidenRing {
-    static constexpr int BLOCK = KS * 4 * (int)sizeof(TP) / 2 * 512;
-    static constexpr int BYTES = 2 * BLOCK > 16384 ? 2 * BLOCK : 16384;
-    static constexpr int DEPTH = BYTES / BLOCK;
-};
-// Halves (of 32 rows) x tiles of 16 x steps x parts.
-__host__ __device__ inline int h_bytes(int most, int rp, int fine) { return rp > 64 ? 0 : most / 16 * (rp / 16) * (fine ? 3 : 2) * 512; }
-
 // A lane's four rows of 16 columns.
 template <typename V>
 __device__ __forceinline__ void put16(const Args &a, const int (*rows)[2], int c, int left, const float (*acc)[8][4]) {
@@ -730,220 +719,187 @@ __device__ __forceinline__ void put16(const Args &a, const int (*rows)[2], int c
         }
 }
 
-// ... second half: a warp takes `per` blocks of 64 columns of a tile, and works by itself.
-template <typename TP, int KS, bool FINE>
-__global__ void __launch_bounds__(THREADS, 1) widen_kernel(const __grid_constant__ Args a, int tiles_most, int groups, int per) {
-    constexpr int PP = parts_of<TP>(), CP = sizeof(TP) / 2;
-    using Ring = WidenRing<TP, KS>;
+template <typename TP>
+struct WidenRing {
+    static constexpr int UNIT = 4 * (int)sizeof(TP) / 2 * 512, DEPTH = sizeof(TP) == 2 ? 4 : 3;      // 16 of r x 64 columns
+};
+
+// ... second half: a block takes `per` blocks of 64 columns of a tile, a warp at a time one of them for 32 rows.  h lies in shared
+// memory for all warps, p2 comes by a warp's ring.
+template <typename TP, bool FINE>
+__global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant__ Args a, int groups, int per) {
+    constexpr int PP = parts_of<TP>(), CP = sizeof(TP) / 2, PARTS = FINE ? 3 : 2;
+    using Ring = WidenRing<TP>;
     extern __shared__ __align__(16) uint8_t smem[];
+    __shared__ int rows[64];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    constexpr int PARTS = FINE ? 3 : 2;
-    const int steps = a.rp / 16;
-    const uint32_t ring = shared_at(smem) + warp * (Ring::BYTES + h_bytes(a.most, a.rp, FINE)) + lane * 16;
-    const uint32_t hs = ring - lane * 8 + Ring::BYTES;
-    const int64_t task = (int64_t)blockIdx.x * (blockDim.x >> 5) + warp;
-    const int tile = (int)(task / groups), first = (int)(task - (int64_t)tile * groups) * per, last = min((a.E + 63) / 64, first + per);
+    const int steps = a.rp / 16, hpitch = a.rp + 8;
+    const uint32_t ring = shared_at(smem) + warp * (Ring::DEPTH * Ring::UNIT) + lane * 16;
+    const uint16_t *hs = reinterpret_cast<uint16_t *>(smem + WARPS * Ring::DEPTH * Ring::UNIT);      // [PARTS][most][hpitch]
+    const int tile = blockIdx.x / groups, first = (blockIdx.x - tile * groups) * per, last = min((a.E + 63) / 64, first + per);
     pdl_trigger();
     pdl_wait();
-    if (tile >= tiles_most || first >= last) return;
     const int tiles = *a.plan.tiles_n;
     const Tile x = a.plan.tiles[tile];
     if (tile >= tiles) return;
-    const bool big = a.rp > 64;                                          // h stays in global memory, r in chunks of 64
-    const int chunks = big ? (a.rp + 63) / 64 : 1, units = x.id >= 0 ? (last - first) * chunks : 0;
-    const int halves = x.count > 32 ? 2 : 1;
-    int rows[2][2][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int e = 32 * h + 16 * m + 8 * i + g;
-                rows[h][m][i] = e < x.count ? a.plan.order[x.start + e] : -1;
-            }
+    const int halves = x.count > 32 ? 2 : 1, blocks = max(0, (last - first - warp + WARPS - 1) / WARPS);
+    // this warp's units: blocks first + warp, first + warp + WARPS, ..., their halves, steps along r
+    const int units = x.id >= 0 ? blocks * halves * steps : 0;
     const TP *p2 = static_cast<const TP *>(a.p2) + (int64_t)max(x.id, 0) * a.r * a.E;
-    int put = 0, next = 0;
+    int put = 0, next = 0, next_b = first + warp, next_h = 0, next_s = 0;
     auto fetch = [&]() {
         if (next < units) {
-            const int b = next / chunks, c = 64 * (first + b) + 8 * g, k0 = (next - b * chunks) * 64, left = a.E - c;
-            const uint32_t d = ring + put * Ring::BLOCK;
+            const int c = 64 * next_b + 8 * g, left = a.E - c;
+            const uint32_t d = ring + put * Ring::UNIT;
             if (a.p2_copy == BY_SIXTEEN) {
 #pragma unroll
-                for (int e = 0; e < 4 * KS; ++e) {
-                    const int j = k0 + 16 * (e >> 2) + 2 * t + (e & 1) + 8 * ((e >> 1) & 1);
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 16 * next_s + 2 * t + (e & 1) + 8 * (e >> 1);
                     const bool some = j < a.r && left > 0;
                     fetch8_wide(d + e * CP * 512, some ? p2 + (int64_t)j * a.E + c : p2, some ? left : 0);
                 }
             } else {
 #pragma unroll 1
-                for (int e = 0; e < 4 * KS; ++e) {
-                    const int j = k0 + 16 * (e >> 2) + 2 * t + (e & 1) + 8 * ((e >> 1) & 1);
+                for (int e = 0; e < 4; ++e) {
+                    const int j = 16 * next_s + 2 * t + (e & 1) + 8 * (e >> 1);
                     const bool some = j < a.r && left > 0;
                     fetch8(d + e * CP * 512, some ? p2 + (int64_t)j * a.E + c : p2, some ? left : 0, a.p2_copy);
                 }
             }
+            ++next;
+            if (++next_s == steps) {
+                next_s = 0;
+                if (++next_h == halves) {
+                    next_h = 0;
+                    next_b += WARPS;
+                }
+            }
         }
         commit();
-        ++next;
-        if (++put == Ring::DEPTH) put = 0;
+        put = (put + 1) % Ring::DEPTH;
     };
-    // Lane's parts of h of row e (of 16 + 8 i + g) at step s: 8 bytes.
-    auto h_at = [&](int q, int e, int s) { return a.hp + ((int64_t)q * a.T + x.start + min(e, x.count - 1)) * a.rp + 16 * s + 4 * t; };
-    if (x.id >= 0 && !big)
-        for (int m = 0; m < 2 * halves; ++m)
-            for (int s = 0; s < steps; ++s)
+    if (threadIdx.x < x.count) rows[threadIdx.x] = a.plan.order[x.start + threadIdx.x];
+    if (x.id >= 0) {
+        const int eights = a.rp / 8;
 #pragma unroll
-                for (int q = 0; q < PARTS; ++q)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int e = 16 * m + 8 * i + g;
-                        copy_fill<8>(hs + ((m * steps + s) * PARTS + q) * 512 + i * 256, h_at(q, e, s), e < x.count ? 8 : 0);
-                    }
-    if (x.id >= 0)
+        for (int q = 0; q < PARTS; ++q)
+            for (int e = threadIdx.x; e < a.most * eights; e += THREADS) {
+                const int m = e / eights, j = 8 * (e - m * eights);
+                copy_fill<16>(shared_at(hs + (q * a.most + m) * hpitch + j),
+                              a.hp + ((int64_t)q * a.T + x.start + min(m, x.count - 1)) * a.rp + j, m < x.count ? 16 : 0);
+            }
+        commit();
 #pragma unroll
         for (int d = 0; d < Ring::DEPTH - 1; ++d) fetch();
+        arrived<Ring::DEPTH - 1>();
+    }
+    __syncthreads();
     int get = 0;
-    for (int b = first; b < last; ++b) {
+    for (int u = 0; u < blocks * halves; ++u) {
+        const int h = halves == 2 ? u & 1 : 0, b = first + warp + (u / halves) * WARPS;
         const int c = 64 * b + 16 * t, left = a.E - c;
-        const bool whole = 64 * b + 64 <= a.E, early = a.base && a.base_bf16 && a.base_vec && whole;
+        int row[2][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (h >= halves) break;
-            uint4 base[2][2][2];                                         // on its way during the products
-            if (early) {
+        for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const uint16_t *p = static_cast<const uint16_t *>(a.base) + (int64_t)max(rows[h][m][i], 0) * a.ld_base + c;
-                        base[m][i][0] = reinterpret_cast<const uint4 *>(p)[0];
-                        base[m][i][1] = reinterpret_cast<const uint4 *>(p)[1];
-                    }
-            } else if (a.base && left > 0) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int64_t at = (int64_t)max(rows[h][m][i], 0) * a.ld_base + c;
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(a.base) + at * (a.base_bf16 ? 2 : 4)));
-                    }
+            for (int i = 0; i < 2; ++i) {
+                const int e = 32 * h + 16 * m + 8 * i + g;
+                row[m][i] = e < x.count ? rows[e] : -1;
+                if (a.base && left > 0 && row[m][i] >= 0)                // on its way to L2 during the products
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(a.base) +
+                                                                   ((int64_t)row[m][i] * a.ld_base + c) * (a.base_bf16 ? 2 : 4)));
             }
-            float acc[2][8][4];
+        float acc[2][8][4];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
+        if (x.id >= 0)
+#pragma unroll 1
+            for (int step = 0; step < steps; ++step) {
+                fetch();                                                 // where the last one read was
+                arrived<Ring::DEPTH - 1>();
+                const uint32_t d = ring + get * Ring::UNIT;
+                get = (get + 1) % Ring::DEPTH;
+                Eight<TP> p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fetched8(d + i * CP * 512, p[i]);
+                uint32_t f[2][3][4];
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint2 w = *reinterpret_cast<const uint2 *>(
+                                hs + (q * a.most + 32 * h + 16 * m + 8 * i + g) * hpitch + 16 * step + 4 * t);
+                            f[m][q][i] = w.x;
+                            f[m][q][2 + i] = w.y;
+                        }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t q0[PP], q1[PP];
+                    across(p[0], p[1], i, q0);
+                    across(p[2], p[3], i, q1);
+#pragma unroll
+                    for (int l = 2; l >= 0; --l)
+#pragma unroll
+                        for (int q = 0; q <= l; ++q) {
+                            const int v = l - q;
+                            if (v >= PP || (l == 2 && !FINE)) continue;
+#pragma unroll
+                            for (int m = 0; m < 2; ++m) mma16816(acc[m][i], f[m][q], q0[v], q1[v]);
+                        }
+                }
+            }
+        // value k of the lane's 16 of row (m, i)
+        auto z = [&](int m, int i, int k) -> float & { return acc[m][k & 7][2 * i + (k >> 3)]; };
+        if (a.base) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
+                for (int i = 0; i < 2; ++i) {
+                    float f[16];
+                    const int64_t at = (int64_t)max(row[m][i], 0) * a.ld_base + c;
+                    const int n = row[m][i] >= 0 ? left : 0;
+                    if (a.base_bf16) load16<uint16_t>(a.base, at, n, a.base_vec, f);
+                    else load16<float>(a.base, at, n, a.base_vec, f);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-            if (x.id >= 0)
-                for (int ch = 0; ch < chunks; ++ch) {
-                    if (h == 0) {
-                        fetch();                                         // where the last one read was
-                        arrived<Ring::DEPTH - 1>();
-                    }
-                    const uint32_t d = ring + get * Ring::BLOCK;
-                    if (h + 1 == halves && ++get == Ring::DEPTH) get = 0;
-#pragma unroll
-                    for (int s = 0; s < KS; ++s) {
-                        const int step = 4 * ch + s;
-                        if (step >= steps) break;
-                        Eight<TP> p[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) fetched8(d + (4 * s + i) * CP * 512, p[i]);
-                        uint32_t f[2][3][4];
-#pragma unroll
-                        for (int m = 0; m < 2; ++m)
-#pragma unroll
-                            for (int q = 0; q < PARTS; ++q) {
-#pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    uint32_t lo, hi;
-                                    if (big) {
-                                        const uint2 w = *reinterpret_cast<const uint2 *>(h_at(q, 16 * m + 8 * i + g, step));
-                                        lo = w.x;
-                                        hi = w.y;
-                                    } else {
-                                        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];"
-                                                     : "=r"(lo), "=r"(hi)
-                                                     : "r"(hs + (((2 * h + m) * steps + step) * PARTS + q) * 512 + i * 256)
-                                                     : "memory");
-                                    }
-                                    f[m][q][i] = lo;
-                                    f[m][q][2 + i] = hi;
-                                }
-                            }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            uint32_t q0[PP], q1[PP];
-                            across(p[0], p[1], i, q0);
-                            across(p[2], p[3], i, q1);
-#pragma unroll
-                            for (int l = 2; l >= 0; --l)
-#pragma unroll
-                                for (int q = 0; q <= l; ++q) {
-                                    const int v = l - q;
-                                    if (v >= PP || (l == 2 && !FINE)) continue;
-#pragma unroll
-                                    for (int m = 0; m < 2; ++m) mma16816(acc[m][i], f[m][q], q0[v], q1[v]);
-                                }
-                        }
-                    }
+                    for (int k = 0; k < 16; ++k) z(m, i, k) += f[k];
                 }
-            // value k of the lane's 16 of row (m, i)
-            auto z = [&](int m, int i, int k) -> float & { return acc[m][k & 7][2 * i + (k >> 3)]; };
-            if (early) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const uint4 q = base[m][i][k >> 3];
-                            const int e = (k & 7) >> 1;
-                            const uint32_t w = e == 0 ? q.x : e == 1 ? q.y : e == 2 ? q.z : q.w;
-                            z(m, i, k) += __uint_as_float((k & 1) ? w & 0xffff0000u : w << 16);
-                        }
-            } else if (a.base) {
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float f[16];
-                        const int64_t at = (int64_t)max(rows[h][m][i], 0) * a.ld_base + c;
-                        const int n = rows[h][m][i] >= 0 ? left : 0;
-                        if (a.base_bf16) load16<uint16_t>(a.base, at, n, a.base_vec, f);
-                        else load16<float>(a.base, at, n, a.base_vec, f);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) z(m, i, k) += f[k];
-                    }
-            }
-            if (a.scale || a.shift) {
-                float sc[16], sh[16];
-#pragma unroll
-                for (int k = 0; k < 16; ++k) { sc[k] = 1.0f; sh[k] = 0.0f; }
-                if (a.scale) load16<float>(a.scale, c, left, a.scale_vec, sc);
-                if (a.shift) load16<float>(a.shift, c, left, a.scale_vec, sh);
-#pragma unroll
-                for (int m = 0; m < 2; ++m)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int k = 0; k < 16; ++k) z(m, i, k) = fmaf(z(m, i, k), sc[k], sh[k]);
-            }
-            if (a.act != MINW_ACT_NONE)
-                with_act(a.act, [&](auto act) {
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-#pragma unroll
-                            for (int k = 0; k < 16; ++k) z(m, i, k) = act_value<act.value>(z(m, i, k));
-                });
-            if (a.out_bf16) put16<uint16_t>(a, rows[h], c, whole ? 64 : left, acc);
-            else put16<float>(a, rows[h], c, whole ? 64 : left, acc);
-            __syncwarp();
         }
+        if (a.scale || a.shift) {
+#pragma unroll
+            for (int k0 = 0; k0 < 16; k0 += 4) {
+                float sc[4], sh[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool some = k0 + k < left;
+                    sc[k] = a.scale && some ? a.scale[c + k0 + k] : 1.0f;
+                    sh[k] = a.shift && some ? a.shift[c + k0 + k] : 0.0f;
+                }
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) z(m, i, k0 + k) = fmaf(z(m, i, k0 + k), sc[k], sh[k]);
+            }
+        }
+        if (a.act != MINW_ACT_NONE)
+            with_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) z(m, i, k) = act_value<act.value>(z(m, i, k));
+            });
+        if (a.out_bf16) put16<uint16_t>(a, row, c, left, acc);
+        else put16<float>(a, row, c, left, acc);
+        __syncwarp();
     }
 }
 
@@ -971,7 +927,7 @@ constexpr int ORDER = 1024;                  // rows whose places are
 
 template <typename TZ, int RT>
 struct GradRing {
-    static constexpr int UNIT = 4 * (int)sizeof(TZ) / 2 * 512, DEPTH = 16384 / UNIT, BYTES = WARPS * DEPTH * UNIT;
+    static constexpr int UNIT = 4 * (int)sizeof(TZ) / 2 * 512, DEPTH = 8192 / UNIT, BYTES = WARPS * DEPTH * UNIT;
     static constexpr int PITCH = 16 * RT + 8, PARTS = 3 * CHUNK * PITCH * 2;       // bytes of a chunk's parts, twice
     static constexpr int ALL = BYTES + 2 * PARTS;
 };
@@ -979,7 +935,7 @@ struct GradRing {
 // RT: tiles of 16 of r in one go.  A warp takes 64 columns: its rows' values come by a ring of its own (as above), the parts of the
 // rows, which all warps need, by chunks for the block.
 template <typename TZ, int RT>
-__global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant__ GradArgs a) {
+__global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __grid_constant__ GradArgs a) {
     constexpr int PZ = parts_of<TZ>(), CZ = sizeof(TZ) / 2;
     using Ring = GradRing<TZ, RT>;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -1056,8 +1012,8 @@ __global__ void __launch_bounds__(THREADS, 1) grads_kernel(const __grid_constant
             }
             for (int chunk = 0; chunk * CHUNK < seg; ++chunk) {
                 // the chunk's parts went out before the units of the chunk before (the first one's: of the whole ring)
-                if (a.along == 1) arrived<(Ring::DEPTH > 4 ? 4 : 3)>();
-                else if (a.along == 2) arrived<2>();
+                if (a.along == 1) arrived<Ring::DEPTH - 1>();            // (at most four)
+                else if (a.along == 2) arrived<(Ring::DEPTH > 2 ? 2 : 1)>();
                 else arrived<1>();
                 __syncthreads();
                 fetch_parts(chunk + 1);
@@ -1222,17 +1178,16 @@ static cudaError_t launch_types(const Args &a, bool few, int64_t tiles, cudaStre
                      : a.most == 32 ? launch_narrow<TI, TP, 2, 8>(a, tiles, s) : launch_narrow<uint16_t, uint16_t, 4, 8>(a, tiles, s);
 }
 
-template <typename TP, int KS>
+template <typename TP>
 static cudaError_t launch_widen(const Args &a, int64_t tiles, cudaStream_t s) {
-    constexpr int LIMIT = 225 * 1024;
-    auto kern = a.fine ? widen_kernel<TP, KS, true> : widen_kernel<TP, KS, false>;
-    if (!allow_shared(reinterpret_cast<const void *>(kern), LIMIT)) return cudaErrorInvalidValue;
-    const int bytes = WidenRing<TP, KS>::BYTES + h_bytes(a.most, a.rp, a.fine), warps = std::min(WARPS, LIMIT / bytes);
-    // blocks of columns of a warp: all warps of the SMs busy once, if the tiles are few
+    constexpr int ring = WARPS * WidenRing<TP>::DEPTH * WidenRing<TP>::UNIT;
+    auto kern = a.fine ? widen_kernel<TP, true> : widen_kernel<TP, false>;
+    if (!allow_shared(reinterpret_cast<const void *>(kern), ring + 3 * 32 * (MAX_RANK + 8) * 2)) return cudaErrorInvalidValue;
+    // two blocks an SM, each of eight blocks of columns or more
     const int blocks = (a.E + 63) / 64, sms = num_sms() > 0 ? num_sms() : 152;
-    const int groups = (int)std::min<int64_t>(blocks, std::max<int64_t>(1, (int64_t)sms * warps / tiles));
-    const int per = (blocks + groups - 1) / groups, g = (blocks + per - 1) / per;
-    return launch_pdl(kern, dim3((unsigned)((tiles * g + warps - 1) / warps)), dim3(32 * warps), (size_t)warps * bytes, s, a, (int)tiles, g, per);
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((blocks + WARPS - 1) / WARPS, 4 * sms / tiles));
+    const int per = (int)((blocks + groups - 1) / groups + WARPS - 1) / WARPS * WARPS, g = (blocks + per - 1) / per;
+    return launch_pdl(kern, dim3((unsigned)(tiles * g)), dim3(THREADS), (size_t)ring + (a.fine ? 3 : 2) * a.most * (a.rp + 8) * 2, s, a, g, per);
 }
 
 static bool vec_rows(const void *p, int64_t ld, int bf16) {
@@ -1255,7 +1210,6 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     a.in_copy = copy_rows(a.in, a.ld_in, in_bf16);
     a.p1_copy = copy_rows(a.p1, a.D, p_bf16);
     a.p2_copy = copy_rows(a.p2, a.E, p_bf16);
-    a.scale_vec = vec_rows(a.scale, 4, 0) && vec_rows(a.shift, 4, 0);
     if (plan) a.plan = *plan;
     const int64_t tiles = plan ? tiles_of(a.T, a.n, a.most) : a.T;
     // a block an SM: as many blocks to a tile as there are SMs for
@@ -1267,10 +1221,7 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
                             : (p_bf16 ? launch_types<float, uint16_t>(a, !plan, tiles, s)
                                       : launch_types<float, float>(a, !plan, tiles, s));
     if (e == cudaSuccess && plan && a.E > 0)
-        e = p_bf16 ? (a.rp <= 16 ? launch_widen<uint16_t, 1>(a, tiles, s) : a.rp <= 32 ? launch_widen<uint16_t, 2>(a, tiles, s)
-                                                                                       : launch_widen<uint16_t, 4>(a, tiles, s))
-                   : (a.rp <= 16 ? launch_widen<float, 1>(a, tiles, s) : a.rp <= 32 ? launch_widen<float, 2>(a, tiles, s)
-                                                                                    : launch_widen<float, 4>(a, tiles, s));
+        e = p_bf16 ? launch_widen<uint16_t>(a, tiles, s) : launch_widen<float>(a, tiles, s);
     return e == cudaSuccess ? launch_status() : launch_failed();
 }
 
