@@ -474,6 +474,8 @@ __device__ __forceinline__ void widen(const Args &a, const int *rows, int count,
     __syncwarp();
 }
 
+__device__ __forceinline__ void prefetch(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 constexpr int SMALL = 64;                     // rows that need no plan
 
 // All of a few rows, one launch: cluster `tile` takes the rows of row `tile`'s user, if it is the first of them, 16 at a time.
@@ -484,30 +486,37 @@ __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__
     float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][R]
     float *part = red + WARPS * 16 * R;                                  // [SMALL][rp]
     uint16_t *hs = reinterpret_cast<uint16_t *>(part + SMALL * a.rp);    // [3][SMALL][rp + 8]
-    __shared__ int rows[SMALL];
-    __shared__ int tile_id, tile_rows;
+    __shared__ int all_rows[WARPS][SMALL];                               // each warp finds the rows by itself
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
+    int *rows = all_rows[warp];
     pdl_wait();
     pdl_trigger();                            // a dependent may rely on what came before this kernel
-    if (warp == 0) {
-        const int mine = user_of(a.ids[tile], a.n);
-        const int lo = lane < a.T ? user_of(a.ids[lane], a.n) : -1, hi = lane + 32 < a.T ? user_of(a.ids[lane + 32], a.n) : -1;
-        const uint32_t ml = __ballot_sync(0xffffffffu, lo == mine), mh = __ballot_sync(0xffffffffu, hi == mine);
-        const uint32_t below = (1u << lane) - 1;
-        if ((ml >> lane) & 1) rows[__popc(ml & below)] = lane;
-        if ((mh >> lane) & 1) rows[__popc(ml) + __popc(mh & below)] = lane + 32;
-        if (lane == 0) {
-            tile_id = mine < a.n ? mine : -1;
-            tile_rows = tile == (ml ? __ffs(ml) - 1 : 31 + __ffs(mh)) ? __popc(ml) + __popc(mh) : 0;
+    const int ids[3] = {a.ids[tile], lane < a.T ? a.ids[lane] : -1, lane + 32 < a.T ? a.ids[lane + 32] : -1};
+    const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
+    if (b0 + warp * DEPTH + lane < b1 && lane < DEPTH)
+        prefetch(static_cast<const TI *>(a.in) + tile * a.ld_in + 32 * (b0 + warp * DEPTH + lane));
+    const int mine = user_of(ids[0], a.n), lo = lane < a.T ? user_of(ids[1], a.n) : -1, hi = lane + 32 < a.T ? user_of(ids[2], a.n) : -1;
+    const uint32_t ml = __ballot_sync(0xffffffffu, lo == mine), mh = __ballot_sync(0xffffffffu, hi == mine);
+    if (tile != (ml ? __ffs(ml) - 1 : 31 + __ffs(mh))) return;           // an earlier row's tile; the whole cluster leaves
+    const uint32_t below = (1u << lane) - 1;
+    if ((ml >> lane) & 1) rows[__popc(ml & below)] = lane;
+    if ((mh >> lane) & 1) rows[__popc(ml) + __popc(mh & below)] = lane + 32;
+    __syncwarp();
+    const int count = __popc(ml) + __popc(mh), id = mine < a.n ? mine : -1, eblocks = (a.E + 63) / 64;
+    // what comes after h, on its way to L2: this warp's columns of p2 and base
+    if (id >= 0)
+        for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS) {
+            constexpr int LINES = 64 * (int)sizeof(TP) / 128, EACH = 128 / (int)sizeof(TP);
+            for (int e = lane; e < a.r * LINES; e += 32) {
+                const int j = e / LINES, c = 64 * b + e % LINES * EACH;
+                if (c < a.E) prefetch(static_cast<const TP *>(a.p2) + ((int64_t)id * a.r + j) * a.E + c);
+            }
         }
-    }
-    __syncthreads();
-    const int count = tile_rows, id = tile_id;
-    if (count == 0) return;                   // the whole cluster leaves
+    if (a.base && 64 * (rank * WARPS + warp) < a.E && lane < count)
+        prefetch(static_cast<const uint8_t *>(a.base) + ((int64_t)rows[lane] * a.ld_base + 64 * (rank * WARPS + warp)) * (a.base_bf16 ? 2 : 4));
     cg::cluster_group cluster = cg::this_cluster();
     if (id >= 0) {
-        const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
         for (int m0 = 0; m0 < count; m0 += 16)
             for (int j0 = 0; j0 < a.r; j0 += R) {
                 float acc[1][NT][4];
@@ -532,9 +541,9 @@ __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__
     } else if (rank == 0 && a.h) {
         for (int e = threadIdx.x; e < count * a.r; e += THREADS) a.h[(int64_t)rows[e / a.r] * a.r + e % a.r] = 0.0f;
     }
-    const int eblocks = (a.E + 63) / 64;
+    constexpr int KS = NT / 2 < 8 / (int)sizeof(TP) ? NT / 2 : 8 / (int)sizeof(TP);
     for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS)
-        for (int m0 = 0; m0 < count; m0 += 16) widen<TP, 1, 1>(a, rows, count, m0, id, b, hs, SMALL, a.rp + 8);
+        for (int m0 = 0; m0 < count; m0 += 16) widen<TP, 1, KS>(a, rows, count, m0, id, b, hs, SMALL, a.rp + 8);
     __syncwarp();
     if (a.split > 1 && id >= 0) cluster_leave();
 }
