@@ -536,6 +536,7 @@ __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__
 #pragma unroll
             for (int q = 0; q < 3; ++q) hs[(q * SMALL + m) * (a.rp + 8) + j] = (uint16_t)s[q];
         }
+        __syncwarp();
         if (a.split > 1) cluster_done_reading();
         __syncthreads();
     } else if (rank == 0 && a.h) {
