@@ -70,6 +70,9 @@ struct Stat {
     int finite;
 };
 
+// Levels on m x m results: Gram matrices, one product, two at a time.
+enum Kind { OF_X, ONE, TWO };
+
 struct Mat {
     const void *g;
     float *mom;
@@ -77,7 +80,8 @@ struct Mat {
     uint8_t *x0, *x1, *small;                // hi blocks, then lo blocks; `small`: SLOTS of them
     int64_t ldg, ldm, ldo;
     int rows, cols;
-    int tri0, full0;                         // tiles of the matrices before: lower triangles of m x m, of X
+    int full0;                               // tiles of X of the matrices before
+    int first[3], split[3];                  // of each Kind: clusters of the matrices before; shares of K of a tile
     float limit, rate;
     uint8_t g_bf16, o_bf16, tall, gvec, mvec, ovec;
 
@@ -88,8 +92,8 @@ struct Mat {
 };
 
 struct Sizes {
-    int count, tri, full;                    // matrices; tiles of their lower triangles, of X
-    int small_k, long_k;                     // the largest smaller and longer side, in blocks of 64
+    int count, full;                         // matrices; tiles of X
+    int clusters[3], blocks[3];              // of each Kind, for one product: clusters, their blocks
     const Mat *table;                        // in the workspace
     Stat *stat;
     double *part;                            // a sum of squares for each tile of X
@@ -100,13 +104,13 @@ struct Table {
     Mat m[N];
 };
 
-// The matrix of tile t: the last one that begins at or before it.
-template <bool TRI>
-__device__ __forceinline__ int find(const Mat *m, int count, int t) {
+// The matrix of tile or cluster t: the last one that begins at or before it.
+template <typename F>
+__device__ __forceinline__ int find(int count, int t, F first) {
     int lo = 0, hi = count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if ((TRI ? m[mid].tri0 : m[mid].full0) <= t) lo = mid;
+        if (first(mid) <= t) lo = mid;
         else hi = mid;
     }
     return lo;
@@ -224,7 +228,7 @@ __global__ void __launch_bounds__(THREADS) squares_kernel(const __grid_constant_
         uint64_t *to = reinterpret_cast<uint64_t *>(const_cast<Mat *>(l.table));
         for (int k = threadIdx.x; k < l.count * (int)(sizeof(Mat) / 8); k += THREADS) to[k] = from[k];
     }
-    const Mat &m = table.m[find<false>(table.m, l.count, blockIdx.x)];
+    const Mat &m = table.m[find(l.count, blockIdx.x, [&](int k) { return table.m[k].full0; })];
     const int t = blockIdx.x - m.full0, r0 = t / m.cb() * T + (threadIdx.x >> 4), c = t % m.cb() * T + (threadIdx.x & 15) * 8;
     float sum = 0.0f;
     double d = 0.0;
@@ -258,7 +262,7 @@ __global__ void __launch_bounds__(THREADS) enter_kernel(Sizes l, Step s, int lo_
     pdl_trigger();
     __shared__ double red[THREADS / 32];
     __shared__ Stat st;
-    const int which = find<false>(l.table, l.count, blockIdx.x);
+    const int which = find(l.count, blockIdx.x, [&](int k) { return l.table[k].full0; });
     const Mat m = l.table[which];
     const int t = blockIdx.x - m.full0, tiles = m.rb() * m.cb();
     double d = 0.0;
@@ -303,6 +307,11 @@ __global__ void __launch_bounds__(THREADS) enter_kernel(Sizes l, Step s, int lo_
 // Products
 // ---------------------------------------------------------------------------
 
+__device__ __forceinline__ float clipped(float w, float rate, float z, float limit) {
+    const float n = fmaf(rate, z, w);
+    return n > limit ? limit : n < -limit ? -limit : n;
+}
+
 enum Mode { GRAM, POLY, MUL, APPLY, LEAVE };
 
 struct Product {
@@ -311,7 +320,7 @@ struct Product {
 };
 
 struct Level {
-    int mode, products, split;
+    int mode, products, split;               // split: blocks of a cluster
     Product pr[2];
     int x1;                                  // GRAM, APPLY, LEAVE: X is the one of a later stage
     int x_lo;                                // ... and has a lo part
@@ -419,7 +428,7 @@ __device__ __forceinline__ void load32(uint32_t addr, float *v) {
     for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(w[k]);
 }
 
-__global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const __grid_constant__ Level v) {
+__global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_constant__ Sizes l, const __grid_constant__ Level v) {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *ring = smem_raw + ((1024u - (su32(smem_raw) & 1023u)) & 1023u);
     float *acc = reinterpret_cast<float *>(ring);               // the tile, once the ring is done with
@@ -445,30 +454,34 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
     fence_after();
     const uint32_t tmem = sm.tmem;
 
-    // what this block computes: matrix, product, tile (i, j), share of K
-    const int split = v.split, rank = blockIdx.x % split, tri = v.mode <= MUL;
+    // What this block computes: matrix, product, tile (i, j), share of K.  A cluster takes `split` blocks' work of one
+    // matrix: a tile in so many shares, or two tiles in half as many, or ...
+    const int split = v.split, in_cluster = blockIdx.x % split, tri = v.mode <= MUL;
     int t = blockIdx.x / split, which = 0;
+    const int kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO, all = tri ? l.clusters[kind] : l.full;
     if (tri) {
-        which = t / l.tri;
-        t -= which * l.tri;
+        which = t / all;
+        t -= which * all;
     }
     // the table is the first kernel's work, and that one was done before this one's predecessor let it start
-    const int index = tri ? find<true>(l.table, l.count, t) : find<false>(l.table, l.count, t);
+    const int index = tri ? find(l.count, t, [&](int k) { return l.table[k].first[kind]; })
+                          : find(l.count, t, [&](int k) { return l.table[k].full0; });
     const Mat m = l.table[index];
     const Product pr = v.pr[which];
+    const int shares = tri ? l.table[index].split[kind] : 1, rank = in_cluster % shares;
+    t = (t - (tri ? l.table[index].first[kind] : m.full0)) * (split / shares) + in_cluster / shares;
+    const bool idle = t >= (tri ? m.mb() * (m.mb() + 1) / 2 : m.rb() * m.cb());        // of a matrix's last cluster
     const int mb = m.mb();
     const int64_t small_blocks = (int64_t)mb * mb * 2 * BLOCK, slot = 2 * small_blocks;
     const int64_t x_blocks = (int64_t)m.rb() * m.cb() * 2 * BLOCK;
     uint8_t *x = v.x1 ? m.x1 : m.x0;
     int i, j;
     if (tri) {
-        t -= m.tri0;
         i = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
         while ((i + 1) * (i + 2) / 2 <= t) ++i;
         while (i * (i + 1) / 2 > t) --i;
         j = t - i * (i + 1) / 2;
     } else {
-        t -= m.full0;
         i = t / m.cb();
         j = t % m.cb();
     }
@@ -500,11 +513,19 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
             }
         }
     }
-    const int kb0 = rank * kbs / split, kb1 = (rank + 1) * kbs / split;
+    const int kb0 = idle ? 0 : rank * kbs / shares, kb1 = idle ? 0 : (rank + 1) * kbs / shares;
     const bool same = a.p == b.p && a.tile == b.tile && a.mn == b.mn && a.sym == b.sym;
     const uint32_t bytes = a.bytes() + (same ? 0 : b.bytes());
     pdl_wait();
     pdl_trigger();
+    if (v.mode == LEAVE && v.update && warp < THREADS / 32) {   // weights on their way to L2 during the products: a line a thread
+        const int each = m.o_bf16 ? 64 : 32, lines = T / each;
+        for (int e = threadIdx.x; e < T * lines; e += THREADS) {
+            const int r = i * T + e / lines, c = j * T + e % lines * each;
+            if (r < m.rows && c < m.cols)
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(m.out) + (r * m.ldo + c) * (m.o_bf16 ? 2 : 4)));
+        }
+    }
     bool ok = true;
     if (warp == LOADER) {
         if (lane == 0) {
@@ -597,12 +618,12 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
     // Rows of the tile that this block finishes.  The other blocks' sums for them arrive in its shared memory, a share after the
     // other, once all are done with their rings (reading them from here instead takes 2 us more: their way is there twice).
     cg::cluster_group cluster = cg::this_cluster();
-    const int rows = T / split, r0 = rank * rows;
+    const int rows = T / shares, r0 = rank * rows;
     if (split > 1) cluster.sync();
-    if (warp < THREADS / 32) {
+    if (warp < THREADS / 32 && !idle) {
         const int r = (warp & 3) * 32 + lane, owner = r / rows;
         float *d = acc + (rank * rows + r - owner * rows) * PITCH + (warp >> 2) * 64;
-        if (split > 1) d = cluster.map_shared_rank(d, owner);
+        if (shares > 1) d = cluster.map_shared_rank(d, in_cluster - rank + owner);
 #pragma unroll
         for (int k = 0; k < 64; k += 4) *reinterpret_cast<float4 *>(d + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
     }
@@ -618,13 +639,13 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
     const int wide = v.mode == APPLY ? 2 * m.cb() : 2 * mb;
     const int64_t lo = v.mode == APPLY ? x_blocks : small_blocks;
     const int c = (threadIdx.x & 15) * 8;
-    for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32; r += 16) {
+    for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32 && !idle; r += 16) {
         float z[8];
 #pragma unroll
         for (int k = 0; k < 8; k += 4) {
             const float *share = acc + (r - r0) * PITCH + c + k;
             float4 f = *reinterpret_cast<const float4 *>(share);
-            for (int p = 1; p < split; ++p) {
+            for (int p = 1; p < shares; ++p) {
                 const float4 o = *reinterpret_cast<const float4 *>(share + p * rows * PITCH);
                 f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
             }
@@ -661,10 +682,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(Sizes l, const
                 else load8(static_cast<const float *>(m.out), e, left, m.ovec, w);
                 const float rate = -v.lr * m.rate;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const float n = fmaf(rate, z[k], w[k]);
-                    z[k] = n > m.limit ? m.limit : n < -m.limit ? -m.limit : n;
-                }
+                for (int k = 0; k < 8; ++k) z[k] = clipped(w[k], rate, z[k], m.limit);
             } else if (!st.finite) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) z[k] = __int_as_float(0x7fc00000);
@@ -983,18 +1001,19 @@ __global__ void __launch_bounds__(THREADS, 1) small_kernel(const __grid_constant
     // this block's share [M][share], from rows of the matrix or from its columns; zeros around it
     uint32_t mx = 0u;
     const int n = M * z.share;
+    // place of the eight values at e0: row and column of X, of the matrix
+    auto place = [&](int e0, int &i, int &l, int &r, int &c) {
+        const int q = e0 / (m.tall ? M : z.share), rest = e0 - q * (m.tall ? M : z.share);
+        i = m.tall ? rest : q;
+        l = m.tall ? q : rest;
+        r = m.tall ? l0 + l : i;
+        c = m.tall ? i : l0 + l;
+    };
     for (int e0 = threadIdx.x * 8; e0 < n; e0 += THREADS * 8) {
         float u[8], mom[8];
-        int i, l;
-        if (!m.tall) {
-            i = e0 / z.share;
-            l = e0 - i * z.share;
-            value8(m, s, l0 + l < m.cols ? i : m.rows, l0 + l, u, mom);
-        } else {
-            l = e0 / M;
-            i = e0 - l * M;
-            value8(m, s, i < m.cols ? l0 + l : m.rows, i, u, mom);
-        }
+        int i, l, r, c;
+        place(e0, i, l, r, c);
+        value8(m, s, c < m.cols ? r : m.rows, c, u, mom);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             mx = max(mx, __float_as_uint(u[k]) & 0x7fffffffu);
@@ -1015,39 +1034,41 @@ __global__ void __launch_bounds__(THREADS, 1) small_kernel(const __grid_constant
         else small_steps<4>(cluster, X, z, steps, scale);
     }
     const float rate = -lr * m.rate;
-    for (int e0 = threadIdx.x * 8; e0 < n; e0 += THREADS * 8) {
-        int i, l;
-        if (!m.tall) {
-            i = e0 / z.share;
-            l = e0 - i * z.share;
-        } else {
-            l = e0 / M;
-            i = e0 - l * M;
-        }
-        const int r = m.tall ? l0 + l : i, c = m.tall ? i : l0 + l, left = m.cols - c;
-        if (r >= m.rows || left <= 0 || (update && !finite)) continue;
-        if (update && s.use) {
-            float u[8], mom[8];
-            value8(m, s, r, c, u, mom);
-            store8(m.mom, r * m.ldm + c, left, m.mvec, mom);
-        }
-        float v[8], w[8];
+    constexpr int LEAVES = 2;                                   // on their way at a time (one: 1.5 us more of 23)
+    for (int e0 = threadIdx.x * 8; e0 < n && (finite || !update); e0 += LEAVES * THREADS * 8) {
+        float w[LEAVES][8], u[LEAVES][8], mom[LEAVES][8];
+        int row[LEAVES], left[LEAVES];
+        int64_t at_[LEAVES];
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            v[k] = finite ? X[m.tall ? (i + k) * z.pitch + l : i * z.pitch + l + k] : __int_as_float(0x7fc00000);
-        const int64_t at_ = r * m.ldo + c;
-        if (update) {
-            if (m.o_bf16) load8(static_cast<const uint16_t *>(m.out), at_, left, m.ovec, w);
-            else load8(static_cast<const float *>(m.out), at_, left, m.ovec, w);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float x = fmaf(rate, v[k], w[k]);
-                v[k] = x > m.limit ? m.limit : x < -m.limit ? -m.limit : x;
+        for (int q = 0; q < LEAVES; ++q) {
+            int i, l, r, c;
+            place(e0 + q * THREADS * 8, i, l, r, c);
+            row[q] = r;
+            left[q] = e0 + q * THREADS * 8 < n && r < m.rows ? m.cols - c : 0;
+            at_[q] = r * m.ldo + c;
+            if (update) {
+                if (s.use) value8(m, s, left[q] > 0 ? r : m.rows, c, u[q], mom[q]);
+                if (m.o_bf16) load8(static_cast<const uint16_t *>(m.out), at_[q], left[q], m.ovec, w[q]);
+                else load8(static_cast<const float *>(m.out), at_[q], left[q], m.ovec, w[q]);
             }
         }
-        if (m.o_bf16) store8(static_cast<uint16_t *>(m.out), at_, left, m.ovec, v);
-        else store8(static_cast<float *>(m.out), at_, left, m.ovec, v);
+#pragma unroll
+        for (int q = 0; q < LEAVES; ++q) {
+            if (left[q] <= 0) continue;
+            int i, l, r, c;
+            place(e0 + q * THREADS * 8, i, l, r, c);
+            if (update && s.use) store8(m.mom, row[q] * m.ldm + c, left[q], m.mvec, mom[q]);
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = finite ? X[m.tall ? (i + k) * z.pitch + l : i * z.pitch + l + k] : __int_as_float(0x7fc00000);
+                if (update) v[k] = clipped(w[q][k], rate, v[k], m.limit);
+            }
+            if (m.o_bf16) store8(static_cast<uint16_t *>(m.out), at_[q], left[q], m.ovec, v);
+            else store8(static_cast<float *>(m.out), at_[q], left[q], m.ovec, v);
+        }
     }
+    __syncwarp();
     cluster.sync();                                             // others read this block's magnitude
 }
 
@@ -1100,35 +1121,82 @@ static bool is_small(const minw_matrix &g) {
     return std::min(g.rows, g.cols) <= SIDE && (int64_t)g.rows * g.cols <= (1 << 24) &&
            Small::of(g.rows, g.cols).bytes() <= SMALL_BYTES;
 }
-static bool is_large(const minw_matrix &g) { return g.rows > 0 && g.cols > 0 && !is_small(g); }
+
+// Whether those go with the large matrices of their list instead: where the launches for these have blocks to spare, that takes
+// no time of its own.
+static bool join(const minw_matrix *g, int count) {
+    const int sms = num_sms() > 0 ? num_sms() : 152;
+    int64_t tiles = 0, small = 0;
+    for (int k = 0; k < count; ++k) {
+        if (g[k].rows == 0 || g[k].cols == 0) continue;
+        const int64_t mb = (std::min(g[k].rows, g[k].cols) + T - 1) / T;
+        if (is_small(g[k])) ++small;
+        else tiles += mb * (mb + 1) / 2;
+    }
+    return tiles > 0 && (tiles + small <= sms || small <= tiles / 16);
+}
+static bool is_large(const minw_matrix &g, bool joined) { return g.rows > 0 && g.cols > 0 && (joined || !is_small(g)); }
+
+// Clusters of a level on m x m matrices (gram: of the Gram products): sums along K are split into shares where that ends the
+// level earlier.  A block of 64 of K takes 0.55 us, a tile's start and end 4.5, a sum over a cluster 3.5 more.
+static void shares(Mat *table, Sizes &l, Kind kind) {
+    const bool gram = kind == OF_X;
+    const int products = kind == TWO ? 2 : 1, sms = num_sms() > 0 ? num_sms() : 152;
+    float best = 1e30f;
+    for (int cluster = 1; cluster <= 8; cluster *= 2)
+        for (int most = 1 << 20; most >= 4; most = most > 256 ? 256 : most * 3 / 4) {  // blocks of 64 of a share
+            int64_t clusters = 0;
+            int longest = 0;
+            for (int k = 0; k < l.count; ++k) {
+                const int mb = table[k].mb(), kbs = gram ? 2 * std::max(table[k].rb(), table[k].cb()) : 2 * mb, tiles = mb * (mb + 1) / 2;
+                int split = 1;
+                while (split < cluster && (kbs + split - 1) / split > most) split *= 2;
+                clusters += (tiles * split + cluster - 1) / cluster;
+                longest = std::max(longest, (kbs + split - 1) / split);
+            }
+            // (the share of the SMs that clusters of 4 and 8 can take)
+            const int64_t places = (int)(sms * (cluster == 8 ? 0.948f : cluster == 4 ? 0.974f : 1.0f)) / cluster, waves = (clusters * products + places - 1) / places;
+            const float time = waves * (0.55f * longest + 4.5f + (cluster > 1 ? 3.5f : 0.0f));
+            if (time < best * 0.999f) {
+                best = time;
+                int at_ = 0;
+                for (int k = 0; k < l.count; ++k) {
+                    const int mb = table[k].mb(), kbs = gram ? 2 * std::max(table[k].rb(), table[k].cb()) : 2 * mb, tiles = mb * (mb + 1) / 2;
+                    int split = 1;
+                    while (split < cluster && (kbs + split - 1) / split > most) split *= 2;
+                    table[k].split[kind] = split;
+                    table[k].first[kind] = at_;
+                    at_ += (tiles * split + cluster - 1) / cluster;
+                }
+                l.clusters[kind] = at_;
+                l.blocks[kind] = cluster;
+            }
+        }
+}
 
 // Fills a launch's list from matrix k on; returns the next launch's first, and the workspace that it takes.  base null: the
 // sizes alone.
 static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int k, int count,
-                uint8_t *base, int64_t *need) {
-    l.count = l.tri = l.full = l.small_k = l.long_k = 0;
+                uint8_t *base, int64_t *need, bool joined) {
+    l.count = l.full = 0;
     l.table = reinterpret_cast<const Mat *>(base);
     int64_t used = up(CAP * sizeof(Mat), 256);
     l.stat = reinterpret_cast<Stat *>(base + used);
     used = up(used + CAP * sizeof(Stat), 256);
     int64_t tiles = 0;
     for (int e = k, n = 0; e < count && n < CAP; ++e) {         // the sums of squares lie before the matrices
-        if (!is_large(g[e])) continue;
+        if (!is_large(g[e], joined)) continue;
         ++n;
         tiles += tiles_of(g[e].rows, g[e].cols);
     }
     l.part = reinterpret_cast<double *>(base + used);
     used = up(used + tiles * (int64_t)sizeof(double), 1024);
     for (; k < count && l.count < CAP; ++k) {
-        if (!is_large(g[k])) continue;
+        if (!is_large(g[k], joined)) continue;
         Mat &m = table[l.count++];
         m = describe(g, mom, out, k);
-        m.tri0 = l.tri;
         m.full0 = l.full;
         const int mb = m.mb();
-        l.small_k = std::max(l.small_k, 2 * mb);
-        l.long_k = std::max(l.long_k, 2 * std::max(m.rb(), m.cb()));
-        l.tri += mb * (mb + 1) / 2;
         l.full += m.rb() * m.cb();
         const int64_t x = (int64_t)m.rb() * m.cb() * 4 * BLOCK;
         m.x0 = base + used;
@@ -1136,6 +1204,7 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
         m.small = m.x1 + x;
         used += matrix_bytes(m.rows, m.cols);
     }
+    for (const Kind kind : {OF_X, ONE, TWO}) shares(table, l, kind);
     *need = used;
     return k;
 }
@@ -1161,17 +1230,15 @@ static bool sizes_fit(const minw_matrix *g, int count) {
     return tiles < (1 << 26);
 }
 
-static cudaError_t launch(const Sizes &l, Level v, int64_t tiles, cudaStream_t s) {
-    const int sms = num_sms() > 0 ? num_sms() : 152;
-    // clusters split K where the tiles leave SMs idle, into shares of 256 at least
-    const int k = v.mode == GRAM ? l.long_k : l.small_k;
-    v.split = 8;
-    while (v.split > 1 && (tiles * v.split > sms || k < 4 * v.split)) v.split /= 2;
+static cudaError_t launch(const Sizes &l, Level v, cudaStream_t s) {
+    const Kind kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO;
+    v.split = v.mode <= MUL ? l.blocks[kind] : 1;
+    const int64_t clusters = v.mode <= MUL ? (int64_t)l.clusters[kind] * v.products : l.full;
     v.wait_cycles = (long long)plan_options().wait_cycles;
     const int smem = STAGES * (int)STAGE + 1024;
     if (!allow_shared(reinterpret_cast<const void *>(product_kernel), smem)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * v.split));
+    cfg.gridDim = dim3((unsigned)(clusters * v.split));
     cfg.blockDim = dim3(THREADS + 64);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
@@ -1219,7 +1286,7 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
         v.mode = GRAM;
         v.products = 1;
         v.pr[0] = {0, 0, A, two(SA - 30)};
-        if (launch(l, v, l.tri, s) != cudaSuccess) return launch_failed();
+        if (launch(l, v, s) != cudaSuccess) return launch_failed();
         for (int k = 1; k <= n; ++k) {
             const int Z = k == 1 ? 4 : 2;                                             // the first Z is Q
             Level p{};
@@ -1228,17 +1295,17 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
             p.pr[0] = {A, A, Z, CC * two(SZ - 2 * SA)};
             p.a = CA * two(SZ);
             p.b = CB * two(SZ - SA);
-            if (launch(l, p, l.tri, s) != cudaSuccess) return launch_failed();
+            if (launch(l, p, s) != cudaSuccess) return launch_failed();
             Level w{};
             w.mode = MUL;
             if (k < n) w.pr[w.products++] = {Z, A, 3, two(-SZ)};                      // Z A
             if (k > 1) w.pr[w.products++] = {Z, Q, Q ^ 1, two(SQ[k] - SZ - SQ[k - 1])};
             Q = k == 1 ? 4 : Q ^ 1;
-            if (w.products > 0 && launch(l, w, (int64_t)l.tri * w.products, s) != cudaSuccess) return launch_failed();
+            if (w.products > 0 && launch(l, w, s) != cudaSuccess) return launch_failed();
             if (k < n) {
                 w.products = 1;
                 w.pr[0] = {3, Z, A ^ 1, two(-SZ)};
-                if (launch(l, w, l.tri, s) != cudaSuccess) return launch_failed();
+                if (launch(l, w, s) != cudaSuccess) return launch_failed();
                 A ^= 1;
             }
         }
@@ -1250,7 +1317,7 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
         e.update = update;
         e.lr = lr;
         e.pr[0] = {Q, Q, 0, two((last ? 0 : 15) - SQ[n] - 15)};
-        if (launch(l, e, l.full, s) != cudaSuccess) return launch_failed();
+        if (launch(l, e, s) != cudaSuccess) return launch_failed();
     }
     return launch_status();
 }
@@ -1280,12 +1347,13 @@ static minw_status run(const minw_matrix *g, const minw_matrix *mom, const minw_
                        const Step &step, bool update, float lr, uint8_t *ws, cudaStream_t s) {
     bool x_lo = step.use != 0;                                  // bf16 gradients are fp16 numbers but for the smallest
     for (int k = 0; k < count; ++k) x_lo = x_lo || g[k].type == MINW_F32;
+    const bool joined = join(g, count);
     Table<CAP> table;
     for (int k = 0; k < count;) {
         int n = 0;
         int64_t bytes = 0;
         for (; k < count && n < CAP; ++k) {
-            if (g[k].rows == 0 || g[k].cols == 0 || !is_small(g[k])) continue;
+            if (g[k].rows == 0 || g[k].cols == 0 || is_large(g[k], joined)) continue;
             table.m[n++] = describe(g, mom, out, k);
             bytes = std::max(bytes, Small::of(g[k].rows, g[k].cols).bytes());
         }
@@ -1303,7 +1371,7 @@ static minw_status run(const minw_matrix *g, const minw_matrix *mom, const minw_
     Sizes l;
     for (int k = 0; k < count;) {
         int64_t need;
-        k = fill(table.m, l, g, mom, out, k, count, ws, &need);
+        k = fill(table.m, l, g, mom, out, k, count, ws, &need, joined);
         if (l.count == 0) break;
         const minw_status st = chain(table, l, step, steps, x_lo, update, lr, s);
         if (st != MINW_OK) return st;
@@ -1339,7 +1407,7 @@ size_t minw_orthogonal_workspace_bytes(const minw_matrix *grads, int32_t count) 
     int64_t most = 16;
     for (int k = 0; k < count;) {
         int64_t need;
-        k = orth::fill(table.m, l, grads, nullptr, nullptr, k, count, nullptr, &need);
+        k = orth::fill(table.m, l, grads, nullptr, nullptr, k, count, nullptr, &need, orth::join(grads, count));
         most = std::max(most, need);
     }
     return (size_t)most;
