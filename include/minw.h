@@ -757,7 +757,8 @@ MINW_API minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, 
  * once, to nearest even.  y may be base (same type and row length) and may
  * not overlap x.  An infinity or a NaN in a row, or in its adapter, makes that row's
  * outputs infinite or NaN, no other user's.  Elements past K and O of a row are
- * neither read nor written.  The same bits on every call.
+ * not written, and not read but where they share 16 aligned bytes with the
+ * row's own (no result depends on them).  The same bits on every call.
  * workspace: device scratch of minw_adapters_workspace_bytes (16-byte
  * aligned, contents meaningless before and after); calls that share one must
  * not run concurrently.  T = 0 does nothing.  Errors: MINW_EINVAL (null
@@ -765,7 +766,7 @@ MINW_API minw_status minw_w4_matvec(const void *x, int32_t x_type, int64_t ldx, 
  * tensor off its elements' boundary, y = x, y = base with another type or row
  * length, missing, misaligned or short workspace), MINW_EUNSUPPORTED (r >
  * 256, n >= 2^24, T >= 2^27, K or O past 2^28, more blocks than a grid holds).
- * Rows on 16-byte boundaries run wider loads. */
+ * Rows on 16-byte boundaries need fewer instructions. */
 MINW_API size_t minw_adapters_workspace_bytes(int64_t T, int32_t K, int32_t O, int32_t n, int32_t r, int32_t backward);
 MINW_API minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K, const int32_t *ids,
                                    const void *down, const void *up, int32_t p_type, int32_t n, int32_t r,

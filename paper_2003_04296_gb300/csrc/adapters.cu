@@ -136,60 +136,88 @@ __global__ void __launch_bounds__(PLAN_THREADS) plan_kernel(const int *__restric
 // Through an adapter
 // ---------------------------------------------------------------------------
 
-// How rows may be copied: by 16 bytes, by 4, or value by value.
-enum Copy { BY_VALUE, BY_WORD, BY_SIXTEEN };
-
-// `bytes` (16, 8 or 4) to shared memory, asynchronously, the first `n` of them from src and zeros behind.
-template <int BYTES>
+// `bytes` (16) to shared memory, asynchronously, the first `n` of them from src and zeros behind.
 __device__ __forceinline__ void copy_fill(uint32_t dst, const void *src, int n) {
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(n), "n"(BYTES) : "memory");
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 
-// Eight values to where this lane alone will read them back: 16 bytes at dst, the next 16 (fp32) 512 on.  Zeros from `left` on.
-template <typename V>
-__device__ __forceinline__ void fetch8_wide(uint32_t dst, const V *p, int left) {
-    constexpr int N = 16 / (int)sizeof(V);                               // values in 16 bytes
-#pragma unroll
-    for (int h = 0; h < 8 / N; ++h) {
-        const int n = min(max(left - h * N, 0), N);
-        copy_fill<16>(dst + 512 * h, n > 0 ? p + h * N : p, n * (int)sizeof(V));
-    }
-}
+// A warp's eights on their way through shared memory: 16 bytes a lane (fp32: twice).  ODD: rows lie off 16-byte boundaries.  Then
+// the aligned sixteens are copied that hold values of the row, and a lane's eight is shifted out of its own and the first
+// of the lane `next` behind; the last of these copies one more, to the end.
+template <typename V, bool ODD>
+struct Way {
+    static constexpr int C = (int)sizeof(V) / 2, BYTES = C * 512 + (ODD ? 128 : 0);
 
-// The same however the row lies.  For loops that are not unrolled: all ways inlined at a dozen places, the instructions do not
-// stay in their caches (half of the time lost).
-template <typename V>
-__device__ __forceinline__ void fetch8(uint32_t dst, const V *p, int left, int how) {
-    constexpr int N = 16 / (int)sizeof(V), W = 4 / (int)sizeof(V);      // ... in a word
-    if (how == BY_SIXTEEN) {
-        fetch8_wide(dst, p, left);
-    } else if (how == BY_WORD) {
+    // p: the lane's eight, left: values of the row from there on (few or none: zeros).  spare: the last lane's place at the end, else -1.
+    static __device__ __forceinline__ void fetch(uint32_t item, const V *p, int left, const void *safe, int spare) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (!ODD) {
+            constexpr int N = 8 / C;                                     // values in 16 bytes
 #pragma unroll
-        for (int k = 0; k < 8 / W; ++k) {
-            const int n = min(max(left - k * W, 0), W);
-            copy_fill<4>(dst + (k * W / N) * 512 + (k * 4) % 16, n > 0 ? p + k * W : p, n * (int)sizeof(V));
+            for (int h = 0; h < C; ++h) {
+                const int n = min(max(left - h * N, 0), N);
+                copy_fill(item + lane * 16 + 512 * h, n > 0 ? p + h * N : safe, n * (int)sizeof(V));
+            }
+        } else {
+            const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(p), first = at & ~(int64_t)15, end = at + (int64_t)left * (int)sizeof(V);
+#pragma unroll
+            for (int h = 0; h < C; ++h)
+                copy_fill(item + lane * 16 + 512 * h, first + 16 * h < end ? reinterpret_cast<const void *>(first + 16 * h) : safe,
+                          first + 16 * h < end ? 16 : 0);
+            if (spare >= 0)
+                copy_fill(item + C * 512 + spare * 16, first + 16 * C < end ? reinterpret_cast<const void *>(first + 16 * C) : safe,
+                          first + 16 * C < end ? 16 : 0);
         }
-    } else {
-        Eight<V> e;
-        e.load(p, left, false);
-#pragma unroll
-        for (int h = 0; h < 8 / N; ++h)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + 512 * h), "r"(e.w[4 * h]), "r"(e.w[4 * h + 1]),
-                         "r"(e.w[4 * h + 2]), "r"(e.w[4 * h + 3])
-                         : "memory");
     }
-}
-
-template <typename V>
-__device__ __forceinline__ void fetched8(uint32_t src, Eight<V> &e) {
+    // off: the row's distance from a 16-byte boundary
+    static __device__ __forceinline__ void read(uint32_t item, Eight<V> &e, int left, int off, int next, int spare) {
+        const int lane = threadIdx.x & 31;
+        uint32_t u[4 * C + 4];
 #pragma unroll
-    for (int h = 0; h < (int)sizeof(V) / 2; ++h)
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(e.w[4 * h]), "=r"(e.w[4 * h + 1]), "=r"(e.w[4 * h + 2]), "=r"(e.w[4 * h + 3])
-                     : "r"(src + 512 * h)
-                     : "memory");
+        for (int h = 0; h < C + (ODD ? 1 : 0); ++h) {
+            const uint32_t at = h < C ? item + lane * 16 + 512 * h : spare >= 0 ? item + C * 512 + spare * 16 : item + (lane + next) * 16;
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(u[4 * h]), "=r"(u[4 * h + 1]), "=r"(u[4 * h + 2]), "=r"(u[4 * h + 3])
+                         : "r"(at)
+                         : "memory");
+        }
+        if constexpr (ODD) shifted<4 * C>(u, off);
+#pragma unroll
+        for (int k = 0; k < 4 * C; ++k) e.w[k] = u[k];
+        if constexpr (ODD) e.cut(left);
+    }
+};
+
+// 8 rows of 64 columns, 16 a lane (row lane / 4, columns 16 (lane % 4) on), to rows anywhere: through shared memory, laid out as
+// the row lies to 16-byte boundaries, and from there by sixteens (a value at a time from here: 32 sectors an instruction).
+// row: this lane's row at the first of the columns, null for none.  n: columns of the row.
+template <typename V>
+__device__ __forceinline__ void put8(V *stage, const float *v, V *row, int n) {
+    constexpr int PITCH = 72, E = 16 / (int)sizeof(V), CHUNKS = PITCH / E;
+    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const int off = (int)(reinterpret_cast<uintptr_t>(row) & 15) / (int)sizeof(V);
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        Vec<V, 1> w;
+        w.set(v + k);
+        w.store(stage + g * PITCH + off + 16 * t + k);
+    }
+    __syncwarp();
+#pragma unroll 1
+    for (int e0 = 0; e0 < 8 * CHUNKS; e0 += 32) {
+        const int e = e0 + lane, r = min(e / CHUNKS, 7), c = (e - r * CHUNKS) * E;
+        V *to = reinterpret_cast<V *>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(row), 4 * r));
+        const int o = (int)(reinterpret_cast<uintptr_t>(to) & 15) / (int)sizeof(V), first = max(c, o), last = min(c + E, o + n);
+        if (e >= 8 * CHUNKS || !to || first >= last) continue;
+        const V *from = stage + r * PITCH;
+        if (last - first == E) *reinterpret_cast<uint4 *>(to - o + c) = *reinterpret_cast<const uint4 *>(from + c);
+        else
+            for (int k = first; k < last; ++k) to[k - o] = from[k];
+    }
+    __syncwarp();
 }
+constexpr int STAGE_BYTES = 8 * 72 * 4;
 
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -216,8 +244,8 @@ struct Args {
     int T, D, E, n, r, rp;                   // rp: r rounded up to 16
     int act, base_bf16, out_bf16;
     int in_vec, p1_vec, p2_vec, base_vec, out_vec;        // whole rows on 16-byte boundaries
-    int in_copy, p1_copy, p2_copy;           // Copy
     int most;                                // rows of a plan's tile
+    int scale_vec;                           // scale and shift on 16-byte boundaries
     int fine;                                // products of parts down to 2^-25
     int split;                               // blocks of a cluster
     Plan plan;
@@ -226,24 +254,13 @@ struct Args {
 template <typename V>
 __device__ __forceinline__ void load16(const void *p, int64_t at, int left, bool vec, float *v) {
     const V *q = static_cast<const V *>(p) + at;
-    if (vec && left >= 16) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            Vec<V, 8> w;
-            w.load(q + 8 * k);
+    for (int k = 0; k < 16; k += 8) {
+        Eight<V> e;
+        e.load(q + k, left - k, vec);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[8 * k + i] = w.get(i);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            v[i] = 0.0f;
-            if (i < left) {
-                Vec<V, 1> w;
-                w.load(q + i);
-                v[i] = w.get(0);
-            }
-        }
+        for (int i = 0; i < 8; ++i)
+            v[k + i] = __uint_as_float(sizeof(V) == 4 ? e.w[i % (2 * sizeof(V))] : (i & 1) ? e.w[i >> 1] & 0xffff0000u : e.w[i >> 1] << 16);
     }
 }
 
@@ -352,15 +369,15 @@ __device__ __forceinline__ void add_warps(float (*acc)[NT][4], float *red, float
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-            float *d = red + (warp * M + 16 * m + g) * R + 8 * j + 2 * t;
+            float *d = red + (warp * M + 16 * m + g) * (R + 8) + 8 * j + 2 * t;
             *reinterpret_cast<float2 *>(d) = make_float2(acc[m][j][0], acc[m][j][1]);
-            *reinterpret_cast<float2 *>(d + 8 * R) = make_float2(acc[m][j][2], acc[m][j][3]);
+            *reinterpret_cast<float2 *>(d + 8 * (R + 8)) = make_float2(acc[m][j][2], acc[m][j][3]);
         }
     __syncthreads();
     for (int e = threadIdx.x; e < M * R; e += THREADS) {
         float v[WARPS];
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) v[w] = red[w * M * R + e];
+        for (int w = 0; w < WARPS; ++w) v[w] = red[(w * M + e / R) * (R + 8) + e % R];
 #pragma unroll
         for (int w = 1; w < WARPS; ++w) v[0] += v[w];
         if (e % R < ranks) part[e / R * pitch + e % R] = v[0];
@@ -483,8 +500,8 @@ template <typename TI, typename TP, int NT>
 __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__ Args a) {
     constexpr int R = 8 * NT, BYTES = sizeof(TI) + sizeof(TP), DEPTH = NT == 2 ? 16 / BYTES : NT == 4 ? 8 / BYTES : 1;
     extern __shared__ __align__(16) uint8_t smem[];
-    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][R]
-    float *part = red + WARPS * 16 * R;                                  // [SMALL][rp]
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][R + 8]
+    float *part = red + WARPS * 16 * (R + 8);                                  // [SMALL][rp]
     uint16_t *hs = reinterpret_cast<uint16_t *>(part + SMALL * a.rp);    // [3][SMALL][rp + 8]
     __shared__ int all_rows[WARPS][SMALL];                               // each warp finds the rows by itself
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -553,26 +570,29 @@ __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__
 // memory, and a lane reads back what it has copied itself, without a barrier.  (The same loads into registers, two
 // blocks of 8 warps an SM: 35 and 67 us for the two halves of 4096 rows, 4096 -> 4096 at rank 64.)
 
-template <typename TI, typename TP, int MT, int NT>
+template <typename TI, typename TP, int MT, int NT, bool ODD>
 struct NarrowRing {
-    static constexpr int UNIT = (MT * 2 * (int)sizeof(TI) + NT * (int)sizeof(TP)) / 2 * 512;       // 32 values along D
-    static constexpr int DEPTH = 200 * 1024 / (WARPS * UNIT) < 4 ? 200 * 1024 / (WARPS * UNIT) : 4;
+    static constexpr int UNIT = MT * 2 * Way<TI, ODD>::BYTES + NT * Way<TP, ODD>::BYTES;           // 32 values along D
+    static constexpr int DEPTH = 220 * 1024 / (WARPS * UNIT) < 4 ? 220 * 1024 / (WARPS * UNIT) : 4;
     static constexpr int BYTES = WARPS * DEPTH * UNIT;
-    static_assert(DEPTH >= 2 && BYTES >= (WARPS + 1) * 16 * MT * 8 * NT * 4, "the sums lie where the ring was");
+    static_assert(DEPTH >= 2 && BYTES >= 16 * MT * (WARPS * (8 * NT + 8) + 8 * NT) * 4, "the sums lie where the ring was");
 };
 
 // The plan's tiles, first half: h, and alpha h in parts for the second half and the gradients.
-template <typename TI, typename TP, int MT, int NT>
+template <typename TI, typename TP, int MT, int NT, bool ODD>
 __global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constant__ Args a) {
-    constexpr int M = 16 * MT, R = 8 * NT, PI = parts_of<TI>(), PP = parts_of<TP>(), CI = sizeof(TI) / 2, CP = sizeof(TP) / 2;
-    using Ring = NarrowRing<TI, TP, MT, NT>;
+    constexpr int M = 16 * MT, R = 8 * NT, PI = parts_of<TI>(), PP = parts_of<TP>();
+    using Ring = NarrowRing<TI, TP, MT, NT, ODD>;
+    using In = Way<TI, ODD>;
+    using Pool = Way<TP, ODD>;
     extern __shared__ __align__(16) uint8_t smem[];
-    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R], when the ring is done with
-    float *part = red + WARPS * M * R;                                   // [M][R]
+    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][M][R + 8], when the ring is done with
+    float *part = red + WARPS * M * (R + 8);                             // [M][R]
     __shared__ int rows[M];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
-    const uint32_t ring = shared_at(smem) + warp * Ring::DEPTH * Ring::UNIT + lane * 16;
+    const uint32_t ring = shared_at(smem) + warp * Ring::DEPTH * Ring::UNIT;
+    const int spare = t == 3 ? g : -1;
     pdl_wait();
     pdl_trigger();
     const int tiles = *a.plan.tiles_n;
@@ -605,30 +625,15 @@ __global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constan
             if (next < b1) {
                 const uint32_t d = ring + put * Ring::UNIT;
                 const int k = 32 * next, left = a.D - k - 8 * t;
-                if (a.in_copy == BY_SIXTEEN && a.p1_copy == BY_SIXTEEN) {
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
+                for (int m = 0; m < MT; ++m)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            fetch8_wide(d + (2 * m + i) * CI * 512, left > 0 ? row[m][i] + k : row[m][i], live[m][i] ? left : 0);
+                    for (int i = 0; i < 2; ++i)
+                        In::fetch(d + (2 * m + i) * In::BYTES, row[m][i] + k, live[m][i] ? left : -8, a.in, spare);
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        const bool some = j0 + 8 * j + g < a.r && left > 0;
-                        fetch8_wide(d + (2 * MT * CI + j * CP) * 512, some ? p1 + (int64_t)(8 * j + g) * a.D + k : p1, some ? left : 0);
-                    }
-                } else {
-#pragma unroll 1
-                    for (int e = 0; e < 2 * MT; ++e) {
-                        const bool some = 8 * e + g < x.count && left > 0;
-                        const TI *in = static_cast<const TI *>(a.in);
-                        fetch8(d + e * CI * 512, some ? in + rows[8 * e + g] * a.ld_in + k + 8 * t : in, some ? left : 0, a.in_copy);
-                    }
-#pragma unroll 1
-                    for (int j = 0; j < NT; ++j) {
-                        const bool some = j0 + 8 * j + g < a.r && left > 0;
-                        fetch8(d + (2 * MT * CI + j * CP) * 512, some ? p1 + (int64_t)(8 * j + g) * a.D + k : p1, some ? left : 0, a.p1_copy);
-                    }
-                }
+                for (int j = 0; j < NT; ++j)
+                    Pool::fetch(d + 2 * MT * In::BYTES + j * Pool::BYTES, p1 + (int64_t)(8 * j + g) * a.D + k,
+                                j0 + 8 * j + g < a.r ? left : -8, a.p1, spare);
             }
             commit();
             next += WARPS;
@@ -645,23 +650,26 @@ __global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constan
                 for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
         for (int b = b0 + warp; b < b1; b += WARPS) {
             arrived<Ring::DEPTH - 2>();
+            if (ODD) __syncwarp();                                       // the neighbours' too; and they have read the slot that comes next
             fetch();
             const uint32_t d = ring + get * Ring::UNIT;
             if (++get == Ring::DEPTH) get = 0;
+            const int left = a.D - 32 * b - 8 * t;
             uint32_t xp[MT][2][PI][4];
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     Eight<TI> e;
-                    fetched8(d + (2 * m + i) * CI * 512, e);
+                    In::read(d + (2 * m + i) * In::BYTES, e, left, (int)(reinterpret_cast<uintptr_t>(row[m][i]) & 15), 1, spare);
                     along(e, xp[m][i]);
                 }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 Eight<TP> e;
                 uint32_t pp[PP][4];
-                fetched8(d + (2 * MT * CI + j * CP) * 512, e);
+                Pool::read(d + 2 * MT * In::BYTES + j * Pool::BYTES, e, left,
+                           (int)(reinterpret_cast<uintptr_t>(p1 + (int64_t)(8 * j + g) * a.D) & 15), 1, spare);
                 along(e, pp);
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
@@ -715,37 +723,81 @@ __global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constan
     }
 }
 
-// A lane's four rows of 16 columns.
+// A lane's four rows of 16 columns, c the first: base added, for whole blocks on 16-byte boundaries.
 template <typename V>
-__device__ __forceinline__ void put16(const Args &a, const int (*rows)[2], int c, int left, const float (*acc)[8][4]) {
+__device__ __forceinline__ void add16(const Args &a, const int (*rows)[2], int c, float (*acc)[8][4]) {
+    Vec<V, 8> w[2][2][2];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            float v[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) v[k] = acc[m][k & 7][2 * i + (k >> 3)];
-            if (rows[m][i] >= 0) store16<V>(a.out, (int64_t)rows[m][i] * a.ld_out + c, left, a.out_vec, v);
+            const V *p = static_cast<const V *>(a.base) + (int64_t)max(rows[m][i], 0) * a.ld_base + c;
+            w[m][i][0].load(p);
+            w[m][i][1].load(p + 8);
         }
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int k = 0; k < 16; ++k) acc[m][k & 7][2 * i + (k >> 3)] += w[m][i][k >> 3].get(k & 7);
 }
 
-template <typename TP>
+// ... and the result, n columns of a block of 64.
+template <typename V>
+__device__ __forceinline__ void put16(const Args &a, const int (*rows)[2], int c, int n, const float (*acc)[8][4], uint8_t *stage) {
+    const bool whole = a.out_vec && n == 64;
+    if (whole) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float v[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] = acc[m][k & 7][2 * i + (k >> 3)];
+                V *row = static_cast<V *>(a.out) + (int64_t)max(rows[m][i], 0) * a.ld_out + c;
+                if (rows[m][i] >= 0) {
+                    Vec<V, 8> w;
+                    w.set(v);
+                    w.store(row);
+                    w.set(v + 8);
+                    w.store(row + 8);
+                }
+            }
+    } else {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float v[16];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) v[k] = acc[m][k & 7][2 * i + (k >> 3)];
+                put8(reinterpret_cast<V *>(stage), v,
+                     rows[m][i] >= 0 ? static_cast<V *>(a.out) + (int64_t)rows[m][i] * a.ld_out + c - 16 * (threadIdx.x & 3) : nullptr, n);
+            }
+    }
+}
+
+template <typename TP, bool ODD>
 struct WidenRing {
-    static constexpr int UNIT = 4 * (int)sizeof(TP) / 2 * 512, DEPTH = sizeof(TP) == 2 ? 4 : 3;      // 16 of r x 64 columns
+    static constexpr int UNIT = 4 * Way<TP, ODD>::BYTES, DEPTH = sizeof(TP) == 2 ? 4 : 2;      // 16 of r x 64 columns
 };
 
 // ... second half: a block takes `per` blocks of 64 columns of a tile, a warp at a time one of them for 32 rows.  h lies in shared
 // memory for all warps, p2 comes by a warp's ring.
-template <typename TP, bool FINE>
+template <typename TP, bool FINE, bool ODD>
 __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant__ Args a, int groups, int per) {
-    constexpr int PP = parts_of<TP>(), CP = sizeof(TP) / 2, PARTS = FINE ? 3 : 2;
-    using Ring = WidenRing<TP>;
+    constexpr int PP = parts_of<TP>(), PARTS = FINE ? 3 : 2;
+    using Ring = WidenRing<TP, ODD>;
+    using Pool = Way<TP, ODD>;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ int rows[64];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const int steps = a.rp / 16, hpitch = a.rp + 8;
-    const uint32_t ring = shared_at(smem) + warp * (Ring::DEPTH * Ring::UNIT) + lane * 16;
-    const uint16_t *hs = reinterpret_cast<uint16_t *>(smem + WARPS * Ring::DEPTH * Ring::UNIT);      // [PARTS][most][hpitch]
+    const uint32_t ring = shared_at(smem) + warp * (Ring::DEPTH * Ring::UNIT);
+    const int spare = g == 7 ? t : -1;
+    uint8_t *stage = smem + WARPS * Ring::DEPTH * Ring::UNIT + warp * STAGE_BYTES;
+    const uint16_t *hs = reinterpret_cast<uint16_t *>(smem + WARPS * (Ring::DEPTH * Ring::UNIT + STAGE_BYTES));      // [PARTS][most][hpitch]
     const int tile = blockIdx.x / groups, first = (blockIdx.x - tile * groups) * per, last = min((a.E + 63) / 64, first + per);
     pdl_trigger();
     pdl_wait();
@@ -761,20 +813,10 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
         if (next < units) {
             const int c = 64 * next_b + 8 * g, left = a.E - c;
             const uint32_t d = ring + put * Ring::UNIT;
-            if (a.p2_copy == BY_SIXTEEN) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = 16 * next_s + 2 * t + (e & 1) + 8 * (e >> 1);
-                    const bool some = j < a.r && left > 0;
-                    fetch8_wide(d + e * CP * 512, some ? p2 + (int64_t)j * a.E + c : p2, some ? left : 0);
-                }
-            } else {
-#pragma unroll 1
-                for (int e = 0; e < 4; ++e) {
-                    const int j = 16 * next_s + 2 * t + (e & 1) + 8 * (e >> 1);
-                    const bool some = j < a.r && left > 0;
-                    fetch8(d + e * CP * 512, some ? p2 + (int64_t)j * a.E + c : p2, some ? left : 0, a.p2_copy);
-                }
+            for (int e = 0; e < 4; ++e) {
+                const int j = 16 * next_s + 2 * t + (e & 1) + 8 * (e >> 1);
+                Pool::fetch(d + e * Pool::BYTES, p2 + (int64_t)min(j, a.r - 1) * a.E + c, j < a.r ? left : -1000, a.p2, spare);
             }
             ++next;
             if (++next_s == steps) {
@@ -795,7 +837,7 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
         for (int q = 0; q < PARTS; ++q)
             for (int e = threadIdx.x; e < a.most * eights; e += THREADS) {
                 const int m = e / eights, j = 8 * (e - m * eights);
-                copy_fill<16>(shared_at(hs + (q * a.most + m) * hpitch + j),
+                copy_fill(shared_at(hs + (q * a.most + m) * hpitch + j),
                               a.hp + ((int64_t)q * a.T + x.start + min(m, x.count - 1)) * a.rp + j, m < x.count ? 16 : 0);
             }
         commit();
@@ -829,13 +871,19 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
         if (x.id >= 0)
 #pragma unroll 1
             for (int step = 0; step < steps; ++step) {
+                if (ODD) __syncwarp();
                 fetch();                                                 // where the last one read was
                 arrived<Ring::DEPTH - 1>();
+                if (ODD) __syncwarp();
                 const uint32_t d = ring + get * Ring::UNIT;
                 get = (get + 1) % Ring::DEPTH;
                 Eight<TP> p[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) fetched8(d + i * CP * 512, p[i]);
+                for (int i = 0; i < 4; ++i) {
+                    const int j = 16 * step + 2 * t + (i & 1) + 8 * (i >> 1);
+                    Pool::read(d + i * Pool::BYTES, p[i], a.E - 64 * b - 8 * g,
+                               (int)(reinterpret_cast<uintptr_t>(p2 + (int64_t)min(j, a.r - 1) * a.E) & 15), 4, spare);
+                }
                 uint32_t f[2][3][4];
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
@@ -866,7 +914,12 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
             }
         // value k of the lane's 16 of row (m, i)
         auto z = [&](int m, int i, int k) -> float & { return acc[m][k & 7][2 * i + (k >> 3)]; };
-        if (a.base) {
+        // Whole blocks on 16-byte boundaries by themselves: with the other way inlined beside each load, the instructions come late.
+        const bool whole = 64 * b + 64 <= a.E;
+        if (a.base && a.base_vec && whole) {
+            if (a.base_bf16) add16<uint16_t>(a, row, c, acc);
+            else add16<float>(a, row, c, acc);
+        } else if (a.base) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -874,8 +927,8 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
                     float f[16];
                     const int64_t at = (int64_t)max(row[m][i], 0) * a.ld_base + c;
                     const int n = row[m][i] >= 0 ? left : 0;
-                    if (a.base_bf16) load16<uint16_t>(a.base, at, n, a.base_vec, f);
-                    else load16<float>(a.base, at, n, a.base_vec, f);
+                    if (a.base_bf16) load16<uint16_t>(a.base, at, n, false, f);
+                    else load16<float>(a.base, at, n, false, f);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) z(m, i, k) += f[k];
                 }
@@ -883,12 +936,17 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
         if (a.scale || a.shift) {
 #pragma unroll
             for (int k0 = 0; k0 < 16; k0 += 4) {
-                float sc[4], sh[4];
+                float sc[4] = {1.0f, 1.0f, 1.0f, 1.0f}, sh[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                if (a.scale_vec && whole) {
+                    if (a.scale) *reinterpret_cast<float4 *>(sc) = *reinterpret_cast<const float4 *>(a.scale + c + k0);
+                    if (a.shift) *reinterpret_cast<float4 *>(sh) = *reinterpret_cast<const float4 *>(a.shift + c + k0);
+                } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bool some = k0 + k < left;
-                    sc[k] = a.scale && some ? a.scale[c + k0 + k] : 1.0f;
-                    sh[k] = a.shift && some ? a.shift[c + k0 + k] : 0.0f;
+                    for (int k = 0; k < 4; ++k)
+                        if (k0 + k < left) {
+                            if (a.scale) sc[k] = a.scale[c + k0 + k];
+                            if (a.shift) sh[k] = a.shift[c + k0 + k];
+                        }
                 }
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
@@ -907,8 +965,8 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
 #pragma unroll
                         for (int k = 0; k < 16; ++k) z(m, i, k) = act_value<act.value>(z(m, i, k));
             });
-        if (a.out_bf16) put16<uint16_t>(a, row, c, left, acc);
-        else put16<float>(a, row, c, left, acc);
+        if (a.out_bf16) put16<uint16_t>(a, row, c, min(64, a.E - 64 * b), acc, stage);
+        else put16<float>(a, row, c, min(64, a.E - 64 * b), acc, stage);
         __syncwarp();
     }
 }
@@ -923,7 +981,7 @@ struct Job {
     float *out;                              // [n][r][C]
     int64_t ld;
     int C, blocks;                           // blocks: of this job for a user
-    int copy, out_vec;
+    int odd, out_vec;                        // z, out: rows off 16-byte boundaries, on them
 };
 
 struct GradArgs {
@@ -935,19 +993,20 @@ struct GradArgs {
 constexpr int CHUNK = 64;                    // rows whose parts are in shared memory at a time
 constexpr int ORDER = 1024;                  // rows whose places are
 
-template <typename TZ, int RT>
+template <typename TZ, int RT, bool ODD>
 struct GradRing {
-    static constexpr int UNIT = 4 * (int)sizeof(TZ) / 2 * 512, DEPTH = 8192 / UNIT, BYTES = WARPS * DEPTH * UNIT;
+    static constexpr int UNIT = 4 * Way<TZ, ODD>::BYTES, DEPTH = sizeof(TZ) == 2 ? 4 : 2, BYTES = WARPS * DEPTH * UNIT;
     static constexpr int PITCH = 16 * RT + 8, PARTS = 3 * CHUNK * PITCH * 2;       // bytes of a chunk's parts, twice
-    static constexpr int ALL = BYTES + 2 * PARTS;
+    static constexpr int ALL = BYTES + (2 * PARTS > WARPS * STAGE_BYTES ? 2 * PARTS : WARPS * STAGE_BYTES);
 };
 
 // RT: tiles of 16 of r in one go.  A warp takes 64 columns: its rows' values come by a ring of its own (as above), the parts of the
 // rows, which all warps need, by chunks for the block.
-template <typename TZ, int RT>
+template <typename TZ, int RT, bool ODD>
 __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __grid_constant__ GradArgs a) {
-    constexpr int PZ = parts_of<TZ>(), CZ = sizeof(TZ) / 2;
-    using Ring = GradRing<TZ, RT>;
+    constexpr int PZ = parts_of<TZ>();
+    using Ring = GradRing<TZ, RT, ODD>;
+    using Row = Way<TZ, ODD>;
     extern __shared__ __align__(16) uint8_t smem[];
     float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][64] where warps share rows
     uint8_t *parts = smem + Ring::BYTES;                                 // [2][3][CHUNK][PITCH]
@@ -960,7 +1019,8 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
     if (b >= a.job[0].blocks) b -= a.job[0].blocks;
     const int wa = warp % a.along, wc = warp / a.along;
     const int c0 = 64 * (b * (WARPS / a.along) + wc), c = c0 + 8 * g, left = job.C - c;
-    const uint32_t ring = shared_at(smem) + warp * Ring::DEPTH * Ring::UNIT + lane * 16;
+    const uint32_t ring = shared_at(smem) + warp * Ring::DEPTH * Ring::UNIT;
+    const int spare = g == 7 ? t : -1;
     const TZ *z = static_cast<const TZ *>(job.z);
     pdl_trigger();
     pdl_wait();
@@ -984,20 +1044,10 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
             auto fetch = [&]() {
                 if (16 * next < seg) {
                     const uint32_t d = ring + put * Ring::UNIT;
-                    if (job.copy == BY_SIXTEEN) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = 16 * next + 2 * t + (i & 1) + 8 * (i >> 1);
-                            const bool some = e < seg && left > 0;
-                            fetch8_wide(d + i * CZ * 512, some ? z + order[e] * job.ld + c : z, some ? left : 0);
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int i = 0; i < 4; ++i) {
-                            const int e = 16 * next + 2 * t + (i & 1) + 8 * (i >> 1);
-                            const bool some = e < seg && left > 0;
-                            fetch8(d + i * CZ * 512, some ? z + order[e] * job.ld + c : z, some ? left : 0, job.copy);
-                        }
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = 16 * next + 2 * t + (i & 1) + 8 * (i >> 1);
+                        Row::fetch(d + i * Row::BYTES, z + order[min(e, seg - 1)] * job.ld + c, e < seg ? left : -1000, z, spare);
                     }
                 }
                 next += a.along;
@@ -1009,7 +1059,7 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
                     for (int e = threadIdx.x; e < 3 * CHUNK * eights; e += THREADS) {
                         const int q = e / (CHUNK * eights), m = e / eights - q * CHUNK, j = 8 * (e % eights);
                         const bool some = rows0 + m < seg;
-                        copy_fill<16>(shared_at(parts + (chunk & 1) * Ring::PARTS + ((q * CHUNK + m) * Ring::PITCH + j) * 2),
+                        copy_fill(shared_at(parts + (chunk & 1) * Ring::PARTS + ((q * CHUNK + m) * Ring::PITCH + j) * 2),
                                       job.a + ((int64_t)q * a.T + first + s0 + (some ? rows0 + m : 0)) * a.rp + j0 + j, some ? 16 : 0);
                     }
             };
@@ -1031,14 +1081,20 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
                 for (int s = 0; s < CHUNK / 16; ++s) {
                     const int step = chunk * (CHUNK / 16) + s;
                     if (step % a.along != wa || 16 * step >= seg) continue;
+                    if (ODD) __syncwarp();
                     fetch();
                     commit();
                     arrived<Ring::DEPTH - 1>();
+                    if (ODD) __syncwarp();
                     const uint32_t d = ring + get * Ring::UNIT;
                     if (++get == Ring::DEPTH) get = 0;
                     Eight<TZ> v[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) fetched8(d + i * CZ * 512, v[i]);
+                    for (int i = 0; i < 4; ++i) {
+                        const int e = 16 * step + 2 * t + (i & 1) + 8 * (i >> 1);
+                        const int off = ODD ? (int)(reinterpret_cast<uintptr_t>(z + order[min(e, seg - 1)] * job.ld) & 15) : 0;
+                        Row::read(d + i * Row::BYTES, v[i], left, off, 4, spare);
+                    }
                     uint32_t f[RT][3][4];
 #pragma unroll
                     for (int m = 0; m < RT; ++m)
@@ -1072,6 +1128,7 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
             }
             arrived<0>();
         }
+        __syncthreads();                      // results are staged where the parts were
 #pragma unroll
         for (int m = 0; m < RT; ++m) {
             if (a.along > 1) {                // the warps of a column block in their order, into the first
@@ -1092,14 +1149,16 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int j = j0 + 16 * m + value_at(8 * i + g), cc = c0 + 16 * t;
-                if (j >= a.r || cc >= job.C) continue;
                 float y[16];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     y[k] = acc[m][k][2 * i];
                     y[8 + k] = acc[m][k][2 * i + 1];
                 }
-                store16<float>(job.out, ((int64_t)u * a.r + j) * job.C + cc, job.C - cc, job.out_vec, y);
+                float *row = j < a.r ? job.out + ((int64_t)u * a.r + j) * job.C + c0 : nullptr;
+                if (c0 >= job.C) continue;
+                if (!job.out_vec || job.C - c0 < 64) put8(reinterpret_cast<float *>(parts + warp * STAGE_BYTES), y, row, min(64, job.C - c0));
+                else if (row) store16<float>(row, 16 * t, 16, true, y);
             }
         }
         __syncthreads();
@@ -1170,14 +1229,15 @@ static cudaError_t launch_clusters(void (*kern)(Args), const Args &a, int64_t ti
 template <typename TI, typename TP, int NT>
 static cudaError_t launch_few(const Args &a, cudaStream_t s) {
     constexpr int ranks = NT == 8 ? MAX_RANK : 8 * NT;
-    auto bytes = [](int rp) { return WARPS * 16 * 8 * NT * 4 + SMALL * rp * 4 + 3 * SMALL * (rp + 8) * 2; };
+    auto bytes = [](int rp) { return WARPS * 16 * (8 * NT + 8) * 4 + SMALL * rp * 4 + 3 * SMALL * (rp + 8) * 2; };
     return launch_clusters(few_kernel<TI, TP, NT>, a, a.T, bytes(a.rp), bytes(ranks), s);
 }
 
 template <typename TI, typename TP, int MT, int NT>
 static cudaError_t launch_narrow(const Args &a, int64_t tiles, cudaStream_t s) {
-    constexpr int bytes = NarrowRing<TI, TP, MT, NT>::BYTES;
-    return launch_clusters(narrow_kernel<TI, TP, MT, NT>, a, tiles, bytes, bytes, s);
+    constexpr int bytes = NarrowRing<TI, TP, MT, NT, false>::BYTES, odd = NarrowRing<TI, TP, MT, NT, true>::BYTES;
+    return a.in_vec && a.p1_vec ? launch_clusters(narrow_kernel<TI, TP, MT, NT, false>, a, tiles, bytes, bytes, s)
+                                : launch_clusters(narrow_kernel<TI, TP, MT, NT, true>, a, tiles, odd, odd, s);
 }
 
 template <typename TI, typename TP>
@@ -1188,10 +1248,10 @@ static cudaError_t launch_types(const Args &a, bool few, int64_t tiles, cudaStre
                      : a.most == 32 ? launch_narrow<TI, TP, 2, 8>(a, tiles, s) : launch_narrow<uint16_t, uint16_t, 4, 8>(a, tiles, s);
 }
 
-template <typename TP>
-static cudaError_t launch_widen(const Args &a, int64_t tiles, cudaStream_t s) {
-    constexpr int ring = WARPS * WidenRing<TP>::DEPTH * WidenRing<TP>::UNIT;
-    auto kern = a.fine ? widen_kernel<TP, true> : widen_kernel<TP, false>;
+template <typename TP, bool ODD>
+static cudaError_t launch_widen_of(const Args &a, int64_t tiles, cudaStream_t s) {
+    constexpr int ring = WARPS * (WidenRing<TP, ODD>::DEPTH * WidenRing<TP, ODD>::UNIT + STAGE_BYTES);
+    auto kern = a.fine ? widen_kernel<TP, true, ODD> : widen_kernel<TP, false, ODD>;
     if (!allow_shared(reinterpret_cast<const void *>(kern), ring + 3 * 32 * (MAX_RANK + 8) * 2)) return cudaErrorInvalidValue;
     // two blocks an SM, each of eight blocks of columns or more
     const int blocks = (a.E + 63) / 64, sms = num_sms() > 0 ? num_sms() : 152;
@@ -1200,13 +1260,13 @@ static cudaError_t launch_widen(const Args &a, int64_t tiles, cudaStream_t s) {
     return launch_pdl(kern, dim3((unsigned)(tiles * g)), dim3(THREADS), (size_t)ring + (a.fine ? 3 : 2) * a.most * (a.rp + 8) * 2, s, a, g, per);
 }
 
-static bool vec_rows(const void *p, int64_t ld, int bf16) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
+template <typename TP>
+static cudaError_t launch_widen(const Args &a, int64_t tiles, cudaStream_t s) {
+    return a.p2_vec ? launch_widen_of<TP, false>(a, tiles, s) : launch_widen_of<TP, true>(a, tiles, s);
 }
 
-static int copy_rows(const void *p, int64_t ld, int bf16) {
-    const int size = bf16 ? 2 : 4;
-    return vec_rows(p, ld, bf16) ? BY_SIXTEEN : reinterpret_cast<uintptr_t>(p) % 4 == 0 && ld * size % 4 == 0 ? BY_WORD : BY_VALUE;
+static bool vec_rows(const void *p, int64_t ld, int bf16) {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % (bf16 ? 8 : 4) == 0;
 }
 
 // One pass through the adapters; types as in the public calls.  plan null: T <= SMALL.
@@ -1217,9 +1277,7 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     a.p2_vec = vec_rows(a.p2, a.E, p_bf16);
     a.base_vec = vec_rows(a.base, a.ld_base, a.base_bf16);
     a.out_vec = vec_rows(a.out, a.ld_out, a.out_bf16);
-    a.in_copy = copy_rows(a.in, a.ld_in, in_bf16);
-    a.p1_copy = copy_rows(a.p1, a.D, p_bf16);
-    a.p2_copy = copy_rows(a.p2, a.E, p_bf16);
+    a.scale_vec = vec_rows(a.scale, 4, 0) && vec_rows(a.shift, 4, 0);
     if (plan) a.plan = *plan;
     const int64_t tiles = plan ? tiles_of(a.T, a.n, a.most) : a.T;
     // a block an SM: as many blocks to a tile as there are SMs for
@@ -1235,11 +1293,15 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     return e == cudaSuccess ? launch_status() : launch_failed();
 }
 
+template <typename TZ, int RT, bool ODD>
+static cudaError_t launch_grads_as(const GradArgs &a, int64_t grid, cudaStream_t s) {
+    constexpr int bytes = GradRing<TZ, RT, ODD>::ALL;
+    if (!allow_shared(reinterpret_cast<const void *>(grads_kernel<TZ, RT, ODD>), bytes)) return cudaErrorInvalidValue;
+    return launch_pdl(grads_kernel<TZ, RT, ODD>, dim3((unsigned)grid), dim3(THREADS), bytes, s, a);
+}
 template <typename TZ, int RT>
 static cudaError_t launch_grads_of(const GradArgs &a, int64_t grid, cudaStream_t s) {
-    constexpr int bytes = GradRing<TZ, RT>::ALL;
-    if (!allow_shared(reinterpret_cast<const void *>(grads_kernel<TZ, RT>), bytes)) return cudaErrorInvalidValue;
-    return launch_pdl(grads_kernel<TZ, RT>, dim3((unsigned)grid), dim3(THREADS), bytes, s, a);
+    return a.job[0].odd || (a.jobs > 1 && a.job[1].odd) ? launch_grads_as<TZ, RT, true>(a, grid, s) : launch_grads_as<TZ, RT, false>(a, grid, s);
 }
 
 template <typename TZ>
@@ -1390,8 +1452,8 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
     ga.along = 1;
     while (ga.along < WARPS / 2 && columns * ga.along / WARPS < 2 * sms && T / n >= 16 * ga.along) ga.along *= 2;
     const int wide = 64 * (WARPS / ga.along);
-    const Job jobs[2] = {{hp, x, ddown, ldx, K, (K + wide - 1) / wide, copy_rows(x, ldx, x_type == MINW_BF16), vec_rows(ddown, K, 0)},
-                         {hh, dy, dup, lddy, O, (O + wide - 1) / wide, copy_rows(dy, lddy, dy_type == MINW_BF16), vec_rows(dup, O, 0)}};
+    const Job jobs[2] = {{hp, x, ddown, ldx, K, (K + wide - 1) / wide, !vec_rows(x, ldx, x_type == MINW_BF16), vec_rows(ddown, K, 0)},
+                         {hh, dy, dup, lddy, O, (O + wide - 1) / wide, !vec_rows(dy, lddy, dy_type == MINW_BF16), vec_rows(dup, O, 0)}};
     const int types[2] = {x_type, dy_type};
     for (int k = 0; k < 2; ++k) {
         if (!jobs[k].out) continue;

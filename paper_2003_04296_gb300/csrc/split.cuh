@@ -12,32 +12,59 @@ namespace minw {
 template <typename V>
 constexpr int parts_of() { return sizeof(V) == 2 ? 1 : 3; }
 
+// Words on from byte `by` (a multiple of the values' size, below 16) of N + 4 words.
+template <int N>
+__device__ __forceinline__ void shifted(uint32_t *w, int by) {
+#pragma unroll
+    for (int k = 0; k < N + 2; ++k) w[k] = by & 8 ? w[k + 2] : w[k];
+#pragma unroll
+    for (int k = 0; k < N + 1; ++k) w[k] = by & 4 ? w[k + 1] : w[k];
+#pragma unroll
+    for (int k = 0; k < N; ++k) w[k] = by & 2 ? __funnelshift_r(w[k], w[k + 1], 16) : w[k];
+}
+
 // Eight consecutive values as they lie in memory; zeros from `left` on.
 template <typename V>
 struct Eight {
-    uint32_t w[2 * sizeof(V)];
+    static constexpr int WORDS = 2 * (int)sizeof(V);
+    uint32_t w[WORDS];
 
     __device__ __forceinline__ void zero() {
 #pragma unroll
-        for (int k = 0; k < 2 * (int)sizeof(V); ++k) w[k] = 0u;
+        for (int k = 0; k < WORDS; ++k) w[k] = 0u;
     }
+    __device__ __forceinline__ void cut(int left) {
+        if (left >= 8) return;
+        if constexpr (sizeof(V) == 4) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (k >= left) w[k] = 0u;
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = 2 * k >= left ? 0u : 2 * k + 1 >= left ? w[k] & 0xffffu : w[k];
+        }
+    }
+    // Off 16-byte boundaries, the aligned sixteens that hold values of these are read and shifted (value by value: twice the
+    // time and more).
     __device__ __forceinline__ void load(const V *p, int left, bool vec) {
         if (vec && left >= 8) {
             Vec<V, 8> v;
             v.load(p);
 #pragma unroll
-            for (int k = 0; k < 2 * (int)sizeof(V); ++k) w[k] = v.w[k];
+            for (int k = 0; k < WORDS; ++k) w[k] = v.w[k];
         } else {
-            zero();
-            if constexpr (sizeof(V) == 4) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~(uintptr_t)15, end = at + (left < 8 ? left : 8) * (int)sizeof(V);
+            uint32_t u[WORDS + 4];
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < left) w[k] = __float_as_uint(p[k]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (k < left) w[k >> 1] |= (uint32_t)p[k] << (16 * (k & 1));
+            for (int k = 0; k < WORDS + 4; k += 4) {
+                uint4 q = make_uint4(0u, 0u, 0u, 0u);
+                if (left > 0 && first + 4 * k < end) q = *reinterpret_cast<const uint4 *>(first + 4 * k);
+                u[k] = q.x; u[k + 1] = q.y; u[k + 2] = q.z; u[k + 3] = q.w;
             }
+            shifted<WORDS>(u, (int)(at & 15));
+#pragma unroll
+            for (int k = 0; k < WORDS; ++k) w[k] = u[k];
+            cut(left);
         }
     }
 };
