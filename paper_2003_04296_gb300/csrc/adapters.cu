@@ -20,47 +20,22 @@
 //   results are 16 consecutive columns a lane.
 // fp32 values enter as three bf16 parts (8 + 8 + 8 bits); products of parts below 2^-25 of the
 // whole are left out, and where only a bf16 result leaves, those below 2^-16.
-#include <cooperative_groups.h>
-#include <cuda_bf16.h>
-#include <cuda_runtime.h>
 #include <math.h>
-#include <stdint.h>
 
 #include <algorithm>
 
-#include "kernels.cuh"
-#include "split.cuh"
-#include "values.cuh"
+#include "adapters.cuh"
 #include "w4.cuh"
-
-namespace cg = cooperative_groups;
 
 namespace minw {
 namespace adapters {
 
-constexpr int WARPS = 8, THREADS = 32 * WARPS;
-constexpr int MAX_RANK = 256;
-
 // ---------------------------------------------------------------------------
-// The plan: rows sorted by user, in their order; tiles of at most `most` rows
+// The plan
 // ---------------------------------------------------------------------------
-
-struct Tile {
-    int id, start, count, pad;               // user (-1: none), place of its first row in the sorted order
-};
-
-struct Plan {
-    int *order;                              // [T] the rows, sorted
-    int *first;                              // [n + 2] place of each user's first row; n: rows of no user
-    int *tiles_n;
-    Tile *tiles;
-    int *counts;                             // [n + 1][COUNTS] where they exceed shared memory
-};
 
 constexpr int PLAN_THREADS = 1024, PLAN_WARPS = 32;
 constexpr int COUNTS = PLAN_WARPS + 1;       // of a user; odd, so that a warp's users lie in different banks
-
-__device__ __forceinline__ int user_of(int id, int n) { return id >= 0 && id < n ? id : n; }
 
 // A warp counts a run of rows, then places them; between the two, the counts [user][warp] become places.  One block:
 // 4096 rows are 4 rounds of a warp.
@@ -228,343 +203,6 @@ __device__ __forceinline__ uint32_t shared_at(const void *p) { return (uint32_t)
 // side by side.
 __device__ __forceinline__ int place(int j) { return ((j & 7) >> 1) * 4 + (j >> 3) * 2 + (j & 1); }
 __device__ __forceinline__ int value_at(int p) { return 2 * (p >> 2) + (p & 1) + 8 * ((p >> 1) & 1); }
-
-struct Args {
-    const void *in;                          // [T][D], rows ld_in apart
-    const int *ids;
-    const void *p1, *p2;                     // [n][r][D], [n][r][E]
-    const float *alpha;                      // [n], or null: 1
-    const void *base;                        // [T][E], or null: 0
-    const float *scale, *shift;              // [E], or null: 1 and 0
-    void *out;                               // [T][E]
-    float *h;                                // [T][r] by row, or null: in p1^T
-    const float *h_in;                       // backward: [T][r] by row ...
-    uint16_t *hp, *hh;                       // [3][T][rp] by sorted row, in parts: alpha times the values here, alpha times h_in
-    int64_t ld_in, ld_base, ld_out;
-    int T, D, E, n, r, rp;                   // rp: r rounded up to 16
-    int act, base_bf16, out_bf16;
-    int in_vec, p1_vec, p2_vec, base_vec, out_vec;        // whole rows on 16-byte boundaries
-    int most;                                // rows of a plan's tile
-    int scale_vec;                           // scale and shift on 16-byte boundaries
-    int fine;                                // products of parts down to 2^-25
-    int split;                               // blocks of a cluster
-    Plan plan;
-};
-
-template <typename V>
-__device__ __forceinline__ void load16(const void *p, int64_t at, int left, bool vec, float *v) {
-    const V *q = static_cast<const V *>(p) + at;
-#pragma unroll
-    for (int k = 0; k < 16; k += 8) {
-        Eight<V> e;
-        e.load(q + k, left - k, vec);
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[k + i] = __uint_as_float(sizeof(V) == 4 ? e.w[i % (2 * sizeof(V))] : (i & 1) ? e.w[i >> 1] & 0xffff0000u : e.w[i >> 1] << 16);
-    }
-}
-
-template <typename V>
-__device__ __forceinline__ void store16(void *p, int64_t at, int left, bool vec, const float *v) {
-    V *q = static_cast<V *>(p) + at;
-    if (vec && left >= 16) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            Vec<V, 8> w;
-            w.set(v + 8 * k);
-            w.store(q + 8 * k);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            if (i < left) {
-                Vec<V, 1> w;
-                w.set(v + i);
-                w.store(q + i);
-            }
-    }
-}
-
-// acc[m][j] += in[rows][k] p1[j][k] over this warp's share of the blocks b0 .. b1 of 32 values: lane t's eight values of a row are
-// the operands of two products.  DEPTH blocks are on their way at a time.
-template <typename TI, typename TP, int MT, int NT, int DEPTH>
-__device__ __forceinline__ void narrow(const Args &a, const int *rows, int count, const TP *p1, int ranks, int b0, int b1,
-                                       float (*acc)[NT][4]) {
-    constexpr int PI = parts_of<TI>(), PP = parts_of<TP>();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const TI *in = static_cast<const TI *>(a.in);
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-    const TI *row[MT][2];
-    bool live[MT][2];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int e = 16 * m + 8 * i + g;
-            live[m][i] = e < count;
-            row[m][i] = in + (live[m][i] ? rows[e] : 0) * a.ld_in + 8 * t;
-        }
-    for (int b = b0 + warp * DEPTH; b < b1; b += WARPS * DEPTH) {
-        Eight<TI> x[DEPTH][MT][2];
-        Eight<TP> p[DEPTH][NT];
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            const int k = 32 * (b + d), left = b + d < b1 ? a.D - k - 8 * t : 0;
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (live[m][i] && left > 0) x[d][m][i].load(row[m][i] + k, left, a.in_vec);
-                    else x[d][m][i].zero();
-                }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (8 * j + g < ranks && left > 0) p[d][j].load(p1 + (int64_t)(8 * j + g) * a.D + k + 8 * t, left, a.p1_vec);
-                else p[d][j].zero();
-            }
-        }
-#pragma unroll
-        for (int d = 0; d < DEPTH; ++d) {
-            uint32_t xp[MT][2][PI][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) along(x[d][m][i], xp[m][i]);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                uint32_t pp[PP][4];
-                along(p[d][j], pp);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int l = 2; l >= 0; --l)                                 // the smallest products first
-#pragma unroll
-                        for (int q = 0; q <= l; ++q) {
-                            const int v = l - q;
-                            if (q >= PI || v >= PP) continue;
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) {
-                                const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
-                                                       xp[m][1][q][2 * s + 1]};
-                                mma16816(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
-                            }
-                        }
-            }
-        }
-    }
-}
-
-// The warps' sums, in their order: part[m][j], rows `pitch` apart.
-template <int MT, int NT>
-__device__ __forceinline__ void add_warps(float (*acc)[NT][4], float *red, float *part, int pitch, int ranks) {
-    constexpr int M = 16 * MT, R = 8 * NT;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    __syncthreads();                          // an earlier round's sums have been read
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            float *d = red + (warp * M + 16 * m + g) * (R + 8) + 8 * j + 2 * t;
-            *reinterpret_cast<float2 *>(d) = make_float2(acc[m][j][0], acc[m][j][1]);
-            *reinterpret_cast<float2 *>(d + 8 * (R + 8)) = make_float2(acc[m][j][2], acc[m][j][3]);
-        }
-    __syncthreads();
-    for (int e = threadIdx.x; e < M * R; e += THREADS) {
-        float v[WARPS];
-#pragma unroll
-        for (int w = 0; w < WARPS; ++w) v[w] = red[(w * M + e / R) * (R + 8) + e % R];
-#pragma unroll
-        for (int w = 1; w < WARPS; ++w) v[0] += v[w];
-        if (e % R < ranks) part[e / R * pitch + e % R] = v[0];
-    }
-}
-
-// The blocks' parts at p, in their order.
-__device__ __forceinline__ float add_blocks(const cg::cluster_group &cluster, float *p, int split) {
-    float v[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) v[c] = split == 1 ? (c == 0 ? *p : 0.0f) : c < split ? *cluster.map_shared_rank(p, c) : 0.0f;
-#pragma unroll
-    for (int c = 1; c < 8; ++c) v[0] += v[c];
-    return v[0];
-}
-
-// Columns 64 b .. + 63 of ME tiles of 16 rows from row m0 of the tile on: h (parts in shared memory, [3][hrows][hpitch]) times the
-// user's p2, and the epilogue.  KS steps of 16 of r are loaded at a time.
-template <typename TP, int ME, int KS>
-__device__ __forceinline__ void widen(const Args &a, const int *rows, int count, int m0, int id, int b, const uint16_t *hs,
-                                      int hrows, int hpitch) {
-    constexpr int PP = parts_of<TP>();
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    float acc[ME][8][4];
-#pragma unroll
-    for (int m = 0; m < ME; ++m)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[m][j][i] = 0.0f;
-    if (id >= 0) {
-        const int c = 64 * b + 8 * g, left = a.E - c;
-        const TP *p2 = static_cast<const TP *>(a.p2) + (int64_t)id * a.r * a.E + c;
-        for (int k0 = 0; k0 < a.rp; k0 += 16 * KS) {
-            Eight<TP> p[KS][4];
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int j = k0 + 16 * s + 2 * t + (i & 1) + 8 * (i >> 1);
-                    if (j < a.r && left > 0) p[s][i].load(p2 + (int64_t)j * a.E, left, a.p2_vec);
-                    else p[s][i].zero();
-                }
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int k = k0 + 16 * s;
-                if (k >= a.rp) break;
-                uint32_t f[ME][3][4];
-#pragma unroll
-                for (int m = 0; m < ME; ++m)
-#pragma unroll
-                    for (int q = 0; q < 3; ++q) {
-                        const uint16_t *h = hs + (q * hrows + m0 + 16 * m + g) * hpitch + k + 2 * t;
-                        f[m][q][0] = *reinterpret_cast<const uint32_t *>(h);
-                        f[m][q][1] = *reinterpret_cast<const uint32_t *>(h + 8 * hpitch);
-                        f[m][q][2] = *reinterpret_cast<const uint32_t *>(h + 8);
-                        f[m][q][3] = *reinterpret_cast<const uint32_t *>(h + 8 * hpitch + 8);
-                    }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t q0[PP], q1[PP];
-                    across(p[s][0], p[s][1], i, q0);
-                    across(p[s][2], p[s][3], i, q1);
-#pragma unroll
-                    for (int l = 2; l >= 0; --l)
-#pragma unroll
-                        for (int q = 0; q <= l; ++q) {
-                            const int v = l - q;
-                            if (v >= PP) continue;
-#pragma unroll
-                            for (int m = 0; m < ME; ++m) mma16816(acc[m][i], f[m][q], q0[v], q1[v]);
-                        }
-                }
-            }
-        }
-    }
-    const int c = 64 * b + 16 * t, left = a.E - c;
-    if (left > 0) {
-#pragma unroll
-        for (int m = 0; m < ME; ++m)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int e = m0 + 16 * m + 8 * i + g;
-                if (e >= count) continue;
-                const int64_t row = rows[e];
-                float z[16], f[16];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    z[k] = acc[m][k][2 * i];
-                    z[8 + k] = acc[m][k][2 * i + 1];
-                }
-                if (a.base) {
-                    if (a.base_bf16) load16<uint16_t>(a.base, row * a.ld_base + c, left, a.base_vec, f);
-                    else load16<float>(a.base, row * a.ld_base + c, left, a.base_vec, f);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) z[k] += f[k];
-                }
-                if (a.scale || a.shift) {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        if (k < left) z[k] = fmaf(z[k], a.scale ? a.scale[c + k] : 1.0f, a.shift ? a.shift[c + k] : 0.0f);
-                }
-                with_act(a.act, [&](auto act) {
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) z[k] = act_value<act.value>(z[k]);
-                });
-                if (a.out_bf16) store16<uint16_t>(a.out, row * a.ld_out + c, left, a.out_vec, z);
-                else store16<float>(a.out, row * a.ld_out + c, left, a.out_vec, z);
-            }
-    }
-    __syncwarp();
-}
-
-__device__ __forceinline__ void prefetch(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
-constexpr int SMALL = 64;                     // rows that need no plan
-
-// All of a few rows, one launch: cluster `tile` takes the rows of row `tile`'s user, if it is the first of them, 16 at a time.
-template <typename TI, typename TP, int NT>
-__global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__ Args a) {
-    constexpr int R = 8 * NT, BYTES = sizeof(TI) + sizeof(TP), DEPTH = NT == 2 ? 16 / BYTES : NT == 4 ? 8 / BYTES : 1;
-    extern __shared__ __align__(16) uint8_t smem[];
-    float *red = reinterpret_cast<float *>(smem);                        // [WARPS][16][R + 8]
-    float *part = red + WARPS * 16 * (R + 8);                                  // [SMALL][rp]
-    uint16_t *hs = reinterpret_cast<uint16_t *>(part + SMALL * a.rp);    // [3][SMALL][rp + 8]
-    __shared__ int all_rows[WARPS][SMALL];                               // each warp finds the rows by itself
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = blockIdx.x % a.split, tile = blockIdx.x / a.split;
-    int *rows = all_rows[warp];
-    pdl_wait();
-    pdl_trigger();                            // a dependent may rely on what came before this kernel
-    const int ids[3] = {a.ids[tile], lane < a.T ? a.ids[lane] : -1, lane + 32 < a.T ? a.ids[lane + 32] : -1};
-    const int blocks = (a.D + 31) / 32, b0 = (int)((int64_t)rank * blocks / a.split), b1 = (int)((int64_t)(rank + 1) * blocks / a.split);
-    if (b0 + warp * DEPTH + lane < b1 && lane < DEPTH)
-        prefetch(static_cast<const TI *>(a.in) + tile * a.ld_in + 32 * (b0 + warp * DEPTH + lane));
-    const int mine = user_of(ids[0], a.n), lo = lane < a.T ? user_of(ids[1], a.n) : -1, hi = lane + 32 < a.T ? user_of(ids[2], a.n) : -1;
-    const uint32_t ml = __ballot_sync(0xffffffffu, lo == mine), mh = __ballot_sync(0xffffffffu, hi == mine);
-    if (tile != (ml ? __ffs(ml) - 1 : 31 + __ffs(mh))) return;           // an earlier row's tile; the whole cluster leaves
-    const uint32_t below = (1u << lane) - 1;
-    if ((ml >> lane) & 1) rows[__popc(ml & below)] = lane;
-    if ((mh >> lane) & 1) rows[__popc(ml) + __popc(mh & below)] = lane + 32;
-    __syncwarp();
-    const int count = __popc(ml) + __popc(mh), id = mine < a.n ? mine : -1, eblocks = (a.E + 63) / 64;
-    // what comes after h, on its way to L2: this warp's columns of p2 and base
-    if (id >= 0)
-        for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS) {
-            constexpr int LINES = 64 * (int)sizeof(TP) / 128, EACH = 128 / (int)sizeof(TP);
-            for (int e = lane; e < a.r * LINES; e += 32) {
-                const int j = e / LINES, c = 64 * b + e % LINES * EACH;
-                if (c < a.E) prefetch(static_cast<const TP *>(a.p2) + ((int64_t)id * a.r + j) * a.E + c);
-            }
-        }
-    if (a.base && 64 * (rank * WARPS + warp) < a.E && lane < count)
-        prefetch(static_cast<const uint8_t *>(a.base) + ((int64_t)rows[lane] * a.ld_base + 64 * (rank * WARPS + warp)) * (a.base_bf16 ? 2 : 4));
-    cg::cluster_group cluster = cg::this_cluster();
-    if (id >= 0) {
-        for (int m0 = 0; m0 < count; m0 += 16)
-            for (int j0 = 0; j0 < a.r; j0 += R) {
-                float acc[1][NT][4];
-                narrow<TI, TP, 1, NT, DEPTH>(a, rows + m0, count - m0, static_cast<const TP *>(a.p1) + ((int64_t)id * a.r + j0) * a.D,
-                                             a.r - j0, b0, b1, acc);
-                add_warps<1, NT>(acc, red, part + m0 * a.rp + j0, a.rp, a.rp - j0);
-            }
-        if (a.split > 1) cluster.sync();
-        else __syncthreads();
-        const float alpha = a.alpha ? a.alpha[id] : 1.0f;
-        for (int e = threadIdx.x; e < (count + 15) / 16 * 16 * a.rp; e += THREADS) {
-            const float v = add_blocks(cluster, part + e, a.split);
-            const int m = e / a.rp, j = e - m * a.rp;
-            if (a.h && rank == 0 && m < count && j < a.r) a.h[(int64_t)rows[m] * a.r + j] = v;
-            uint32_t s[3];
-            split2(__float_as_uint(alpha * v), 0u, s);
-#pragma unroll
-            for (int q = 0; q < 3; ++q) hs[(q * SMALL + m) * (a.rp + 8) + j] = (uint16_t)s[q];
-        }
-        __syncwarp();
-        if (a.split > 1) cluster_done_reading();
-        __syncthreads();
-    } else if (rank == 0 && a.h) {
-        for (int e = threadIdx.x; e < count * a.r; e += THREADS) a.h[(int64_t)rows[e / a.r] * a.r + e % a.r] = 0.0f;
-    }
-    constexpr int KS = NT / 2 < 8 / (int)sizeof(TP) ? NT / 2 : 8 / (int)sizeof(TP);
-    for (int b = rank * WARPS + warp; b < eblocks; b += a.split * WARPS)
-        for (int m0 = 0; m0 < count; m0 += 16) widen<TP, 1, KS>(a, rows, count, m0, id, b, hs, SMALL, a.rp + 8);
-    __syncwarp();
-    if (a.split > 1 && id >= 0) cluster_leave();
-}
 
 // What the kernels below have on its way: a warp copies units of what it will work on next into a ring of its own in shared
 // memory, and a lane reads back what it has copied itself, without a barrier.  (The same loads into registers, two
@@ -927,8 +565,8 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
                     float f[16];
                     const int64_t at = (int64_t)max(row[m][i], 0) * a.ld_base + c;
                     const int n = row[m][i] >= 0 ? left : 0;
-                    if (a.base_bf16) load16<uint16_t>(a.base, at, n, false, f);
-                    else load16<float>(a.base, at, n, false, f);
+                    if (a.base_bf16) load16<uint16_t, true>(a.base, at, n, f);
+                    else load16<float, true>(a.base, at, n, f);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) z(m, i, k) += f[k];
                 }
@@ -1208,7 +846,7 @@ static minw_status make_plan(const Plan &p, const int *ids, int T, int n, int mo
                ? MINW_OK : launch_failed();
 }
 
-static cudaError_t launch_clusters(void (*kern)(Args), const Args &a, int64_t tiles, int smem, int most, cudaStream_t s) {
+cudaError_t launch_clusters(void (*kern)(Args), const Args &a, int64_t tiles, int smem, int most, cudaStream_t s) {
     if (!allow_shared(reinterpret_cast<const void *>(kern), most)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * a.split));
@@ -1226,13 +864,6 @@ static cudaError_t launch_clusters(void (*kern)(Args), const Args &a, int64_t ti
     return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
-template <typename TI, typename TP, int NT>
-static cudaError_t launch_few(const Args &a, cudaStream_t s) {
-    constexpr int ranks = NT == 8 ? MAX_RANK : 8 * NT;
-    auto bytes = [](int rp) { return WARPS * 16 * (8 * NT + 8) * 4 + SMALL * rp * 4 + 3 * SMALL * (rp + 8) * 2; };
-    return launch_clusters(few_kernel<TI, TP, NT>, a, a.T, bytes(a.rp), bytes(ranks), s);
-}
-
 template <typename TI, typename TP, int MT, int NT>
 static cudaError_t launch_narrow(const Args &a, int64_t tiles, cudaStream_t s) {
     constexpr int bytes = NarrowRing<TI, TP, MT, NT, false>::BYTES, odd = NarrowRing<TI, TP, MT, NT, true>::BYTES;
@@ -1241,9 +872,7 @@ static cudaError_t launch_narrow(const Args &a, int64_t tiles, cudaStream_t s) {
 }
 
 template <typename TI, typename TP>
-static cudaError_t launch_types(const Args &a, bool few, int64_t tiles, cudaStream_t s) {
-    if (few)
-        return a.r <= 16 ? launch_few<TI, TP, 2>(a, s) : a.r <= 32 ? launch_few<TI, TP, 4>(a, s) : launch_few<TI, TP, 8>(a, s);
+static cudaError_t launch_types(const Args &a, int64_t tiles, cudaStream_t s) {
     return a.r <= 16 ? launch_narrow<TI, TP, 4, 2>(a, tiles, s) : a.r <= 32 ? launch_narrow<TI, TP, 4, 4>(a, tiles, s)
                      : a.most == 32 ? launch_narrow<TI, TP, 2, 8>(a, tiles, s) : launch_narrow<uint16_t, uint16_t, 4, 8>(a, tiles, s);
 }
@@ -1284,11 +913,12 @@ static minw_status through(Args a, int in_bf16, int p_bf16, const Plan *plan, cu
     const int sms = num_sms() > 0 ? num_sms() : 152;
     a.split = 8;
     while (plan && a.split > 1 && tiles * a.split > sms + sms / 8) a.split /= 2;         // (tiles: a bound, mostly above)
-    cudaError_t e = in_bf16 ? (p_bf16 ? launch_types<uint16_t, uint16_t>(a, !plan, tiles, s)
-                                      : launch_types<uint16_t, float>(a, !plan, tiles, s))
-                            : (p_bf16 ? launch_types<float, uint16_t>(a, !plan, tiles, s)
-                                      : launch_types<float, float>(a, !plan, tiles, s));
-    if (e == cudaSuccess && plan && a.E > 0)
+    if (!plan) return launch_few(a, in_bf16, p_bf16, s) == cudaSuccess ? launch_status() : launch_failed();
+    cudaError_t e = in_bf16 ? (p_bf16 ? launch_types<uint16_t, uint16_t>(a, tiles, s)
+                                      : launch_types<uint16_t, float>(a, tiles, s))
+                            : (p_bf16 ? launch_types<float, uint16_t>(a, tiles, s)
+                                      : launch_types<float, float>(a, tiles, s));
+    if (e == cudaSuccess && a.E > 0)
         e = p_bf16 ? launch_widen<uint16_t>(a, tiles, s) : launch_widen<float>(a, tiles, s);
     return e == cudaSuccess ? launch_status() : launch_failed();
 }

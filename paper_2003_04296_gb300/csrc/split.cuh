@@ -44,28 +44,24 @@ struct Eight {
             for (int k = 0; k < 4; ++k) w[k] = 2 * k >= left ? 0u : 2 * k + 1 >= left ? w[k] & 0xffffu : w[k];
         }
     }
-    // Off 16-byte boundaries, the aligned sixteens that hold values of these are read and shifted (value by value: twice the
-    // time and more).
-    __device__ __forceinline__ void load(const V *p, int left, bool vec) {
-        if (vec && left >= 8) {
-            Vec<V, 8> v;
-            v.load(p);
+    // ODD: off 16-byte boundaries, the aligned sixteens that hold values of these are read and shifted (value by value: twice
+    // the time and more).  On them, a sixteen is read that holds some.
+    template <bool ODD>
+    __device__ __forceinline__ void load(const V *p, int left) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = ODD ? at & ~(uintptr_t)15 : at,
+                        end = at + (left < 8 ? left : 8) * (int)sizeof(V);
+        constexpr int N = WORDS + (ODD ? 4 : 0);
+        uint32_t u[WORDS + 4];
 #pragma unroll
-            for (int k = 0; k < WORDS; ++k) w[k] = v.w[k];
-        } else {
-            const uintptr_t at = reinterpret_cast<uintptr_t>(p), first = at & ~(uintptr_t)15, end = at + (left < 8 ? left : 8) * (int)sizeof(V);
-            uint32_t u[WORDS + 4];
-#pragma unroll
-            for (int k = 0; k < WORDS + 4; k += 4) {
-                uint4 q = make_uint4(0u, 0u, 0u, 0u);
-                if (left > 0 && first + 4 * k < end) q = *reinterpret_cast<const uint4 *>(first + 4 * k);
-                u[k] = q.x; u[k + 1] = q.y; u[k + 2] = q.z; u[k + 3] = q.w;
-            }
-            shifted<WORDS>(u, (int)(at & 15));
-#pragma unroll
-            for (int k = 0; k < WORDS; ++k) w[k] = u[k];
-            cut(left);
+        for (int k = 0; k < N; k += 4) {
+            uint4 q = make_uint4(0u, 0u, 0u, 0u);
+            if (left > 0 && first + 4 * k < end) q = *reinterpret_cast<const uint4 *>(first + 4 * k);
+            u[k] = q.x; u[k + 1] = q.y; u[k + 2] = q.z; u[k + 3] = q.w;
         }
+        if constexpr (ODD) shifted<WORDS>(u, (int)(at & 15));
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) w[k] = u[k];
+        cut(left);
     }
 };
 
