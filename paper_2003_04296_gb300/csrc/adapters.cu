@@ -437,8 +437,8 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
     uint8_t *stage = smem + WARPS * Ring::DEPTH * Ring::UNIT + warp * STAGE_BYTES;
     const uint16_t *hs = reinterpret_cast<uint16_t *>(smem + WARPS * (Ring::DEPTH * Ring::UNIT + STAGE_BYTES));      // [PARTS][most][hpitch]
     const int tile = blockIdx.x / groups, first = (blockIdx.x - tile * groups) * per, last = min((a.E + 63) / 64, first + per);
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();                            // the gradients rely on what came before this kernel
     const int tiles = *a.plan.tiles_n;
     const Tile x = a.plan.tiles[tile];
     if (tile >= tiles) return;
@@ -625,6 +625,7 @@ struct Job {
 struct GradArgs {
     Job job[2];
     int jobs, T, n, r, rp, along;            // along: warps that share a user's rows (the others: columns)
+    int beside;                              // the kernel before this one makes dx
     Plan plan;
 };
 
@@ -661,7 +662,9 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
     const int spare = g == 7 ? t : -1;
     const TZ *z = static_cast<const TZ *>(job.z);
     pdl_trigger();
-    pdl_wait();
+    // Beside the kernel that makes dx, whose results are not needed here: it lets this one start once the parts are there, and is
+    // waited for at the end, for those who wait for this one.
+    if (!a.beside) pdl_wait();
     const int first = a.plan.first[u], count = a.plan.first[u + 1] - first;
     for (int j0 = 0; j0 < a.r; j0 += 16 * RT) {
         float acc[RT][8][4];
@@ -692,10 +695,12 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
                 if (++put == Ring::DEPTH) put = 0;
             };
             auto fetch_parts = [&](int chunk) {                          // rows past the last: zeros
-                const int rows0 = chunk * CHUNK, eights = ranks / 8;
+                constexpr int EIGHTS = 2 * RT;
+                const int rows0 = chunk * CHUNK;
                 if (rows0 < seg)
-                    for (int e = threadIdx.x; e < 3 * CHUNK * eights; e += THREADS) {
-                        const int q = e / (CHUNK * eights), m = e / eights - q * CHUNK, j = 8 * (e % eights);
+                    for (int e = threadIdx.x; e < 3 * CHUNK * EIGHTS; e += THREADS) {
+                        const int q = e / (CHUNK * EIGHTS), m = e / EIGHTS % CHUNK, j = 8 * (e % EIGHTS);
+                        if (j >= ranks) continue;
                         const bool some = rows0 + m < seg;
                         copy_fill(shared_at(parts + (chunk & 1) * Ring::PARTS + ((q * CHUNK + m) * Ring::PITCH + j) * 2),
                                       job.a + ((int64_t)q * a.T + first + s0 + (some ? rows0 + m : 0)) * a.rp + j0 + j, some ? 16 : 0);
@@ -716,9 +721,10 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
                 __syncthreads();
                 fetch_parts(chunk + 1);
                 commit();
-                for (int s = 0; s < CHUNK / 16; ++s) {
+#pragma unroll 1
+                for (int s = wa; s < CHUNK / 16; s += a.along) {         // (along divides a chunk's steps)
                     const int step = chunk * (CHUNK / 16) + s;
-                    if (step % a.along != wa || 16 * step >= seg) continue;
+                    if (16 * step >= seg) break;
                     if (ODD) __syncwarp();
                     fetch();
                     commit();
@@ -786,7 +792,7 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
             if (wa != 0) continue;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int j = j0 + 16 * m + value_at(8 * i + g), cc = c0 + 16 * t;
+                const int j = j0 + 16 * m + value_at(8 * i + g);
                 float y[16];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
@@ -801,6 +807,7 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
         }
         __syncthreads();
     }
+    if (a.beside) pdl_wait();
 }
 
 // ---------------------------------------------------------------------------
@@ -1075,7 +1082,7 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
     }
     // jobs of one type in one launch
     GradArgs ga{};
-    ga.T = (int)T; ga.n = n; ga.r = r; ga.rp = rank_pitch(r); ga.plan = p;
+    ga.T = (int)T; ga.n = n; ga.r = r; ga.rp = rank_pitch(r); ga.plan = p; ga.beside = dx && T > 0;
     // warps share a user's rows where its columns leave SMs without a block, if there are steps of 16 rows for them
     const int sms = num_sms() > 0 ? num_sms() : 152;
     const int64_t columns = ((ddown ? (K + 63) / 64 : 0) + (dup ? (O + 63) / 64 : 0)) * (int64_t)n;

@@ -41,6 +41,8 @@ __device__ __forceinline__ int user_of(int id, int n) { return id >= 0 && id < n
 // Through an adapter
 // ---------------------------------------------------------------------------
 
+__device__ __forceinline__ void prefetch(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
 struct Args {
     const void *in;                          // [T][D], rows ld_in apart
     const int *ids;

@@ -175,8 +175,6 @@ __device__ __forceinline__ void widen(const Args &a, const int *rows, int count,
     __syncwarp();
 }
 
-__device__ __forceinline__ void prefetch(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
-
 // All of a few rows, one launch: cluster `tile` takes the rows of row `tile`'s user, if it is the first of them, 16 at a time.
 template <typename TI, typename TP, int NT, bool ODD>
 __global__ void __launch_bounds__(THREADS, 2) few_kernel(const __grid_constant__ Args a) {

@@ -414,3 +414,66 @@ def test_without_dependent_launches(M):
     finally:
         M.set_plan_options(old)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [60, 2200])
+def test_rows_past_32_bits(M, T):
+    """Rows so far apart that they pass 2^31 values and 2^32 bytes."""
+    gen = torch.Generator(device="cuda").manual_seed(10)
+    K, O, n, r, ld = 72, 90, 3, 5, (1 << 32) // T // 8 * 8
+    ids = _users(gen, T, n, "mixed")
+    xbuf, ybuf = (torch.empty(T * ld, dtype=torch.bfloat16, device="cuda").view(T, ld) for _ in range(2))
+    x, y = xbuf[:, 16:16 + K], ybuf[:, 3:3 + O]
+    x.copy_(_rand(gen, T, K))
+    down, up = _rand(gen, n, r, K) / K ** 0.5, _rand(gen, n, r, O)
+    h = torch.empty(T, r, device="cuda")
+    ws = torch.empty(M.minw_adapters_workspace_bytes(T, K, O, n, r, True), dtype=torch.uint8, device="cuda")
+    M.minw_adapters(x, ids, down, up, y, h=h, workspace=ws)
+    want, wh, ey, eh = _forward(x.contiguous(), ids, down, up, None, None, None, None, 0, True, "b")
+    _check(y.contiguous(), want, ey, "y")
+    _check(h, wh, eh + U * wh.abs(), "h")
+    # backward: dy where y was, dx in the other buffer
+    dx, dd, du = xbuf[:, 1000:1000 + K], torch.empty_like(down), torch.empty_like(up)
+    M.minw_adapters_backward(x, ids, down, up, h, y, ddown=dd, dup=du, dx=dx, workspace=ws)
+    wx, edx, grads = _backward(x.contiguous(), ids, down, up, None, h, y.contiguous())
+    _check(dx.contiguous(), wx, edx[True] + (U + ROUND["b"]) * wx.abs(), "dx")
+    for name, got in (("ddown", dd), ("dup", du)):
+        _check(got, *grads[name], name)
+
+
+def test_pools_past_32_bits(M):
+    """The last adapter of a pool of more than 2^31 values."""
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    K, O, r = 1 << 16, 40, 16
+    n = (1 << 31) // (r * K) + 3
+    down = torch.empty((n, r, K), dtype=torch.bfloat16, device="cuda")
+    up = _rand(gen, n, r, O).bfloat16()
+    for T in (3, 100):
+        ids = torch.full((T,), n - 1, dtype=torch.int32, device="cuda")
+        down[n - 1].copy_(_rand(gen, r, K) / K ** 0.5)
+        x, y = _rand(gen, T, K).bfloat16(), torch.empty(T, O, device="cuda")
+        ws = torch.empty(M.minw_adapters_workspace_bytes(T, K, O, n, r), dtype=torch.uint8, device="cuda")
+        M.minw_adapters(x, ids, down, up, y, workspace=ws)
+        want, _, ey, _ = _forward(x, ids - (n - 1), down[n - 1:], up[n - 1:], None, None, None, None, 0, True, "f")
+        _check(y, want, ey, "y")
+
+
+def test_y_with_its_neighbours_written_at_the_same_time(M):
+    """Two batches whose rows share sixteens of bytes, on two streams: neither disturbs the other's values."""
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    T, K, O, n, r = 200, 64, 77, 3, 8
+    buf = torch.zeros(T, 2 * O + 1, dtype=torch.bfloat16, device="cuda")
+    ys = [buf[:, 1:1 + O], buf[:, 1 + O:1 + 2 * O]]
+    down, up = _rand(gen, n, r, K) / 8, _rand(gen, n, r, O)
+    args = [(_rand(gen, T, K), _users(gen, T, n, "mixed"), torch.empty(M.minw_adapters_workspace_bytes(T, K, O, n, r), dtype=torch.uint8,
+                                                                       device="cuda"), torch.cuda.Stream()) for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for (x, ids, ws, s), y in zip(args, ys):
+            M.minw_adapters(x, ids, down, up, y, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    for (x, ids, ws, s), y in zip(args, ys):
+        alone = torch.empty(T, O, dtype=torch.bfloat16, device="cuda")
+        M.minw_adapters(x, ids, down, up, alone, workspace=ws)
+        assert torch.equal(alone, y)
+    assert (buf[:, 0] == 0).all()

@@ -294,3 +294,35 @@ def test_without_dependent_launches(M):
 
 def test_no_wait_ran_out(M):
     assert M.minw_get_last_device_error() == M.MINW_OK
+
+
+@pytest.mark.parametrize("count,extra", [(300, 2), (3, 5), (0, 230)])
+def test_small_sides_beside_large_matrices(M, count, extra):
+    """Small sides in a launch of their own, with the large ones, and more large ones than a launch takes."""
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    shapes = [(1 + k % 30, 5 + (11 * k) % 90) for k in range(count)] + [(70 + k % 60, 66 + (3 * k) % 80) for k in range(extra)]
+    g = [_matrix(gen, m, n, "batch" if k % 3 else "noise") for k, (m, n) in enumerate(shapes)]
+    w, m = [torch.rand_like(x) for x in g], [torch.randn_like(x) for x in g]
+    w0, m0 = [x.clone() for x in w], [x.clone() for x in m]
+    M.minw_sgd_orthogonal(w, m, g, 0.1, _ws(M, g), momentum=0.5, nesterov=False)
+    for k, (a, b) in enumerate(shapes):
+        u = 0.5 * m0[k].double() + g[k].double()
+        assert ((m[k].double() - u).abs() <= U * u.abs()).all()
+        ns = _ns(u)
+        want = w0[k].double() - 0.1 * math.sqrt(max(1.0, a / b)) * ns
+        # fp32's u of the kernel and the weight's rounding
+        tol = (_bound() + 4 * U) * 0.1 * math.sqrt(max(1.0, a / b)) * float(ns.norm()) + 2 * U * float(want.norm())
+        assert float((w[k].double() - want).norm()) <= tol, (k, a, b)
+
+
+def test_rows_past_32_bits(M):
+    """Rows 2^20 values apart, past 2^31 values."""
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    rows = 2200
+    gbuf = torch.empty(rows << 20, dtype=torch.bfloat16, device="cuda").view(rows, 1 << 20)
+    obuf = torch.empty(rows << 20, dtype=torch.bfloat16, device="cuda").view(rows, 1 << 20)
+    for n in (40, 130):
+        g, o = gbuf[:, 8:8 + n], obuf[:, 8:8 + n]
+        g.copy_(torch.randn(rows, n, generator=gen, device="cuda"))
+        M.minw_orthogonalize([g], [o], _ws(M, [g]))
+        _close(o.contiguous(), _ns(g.contiguous()), "b")
