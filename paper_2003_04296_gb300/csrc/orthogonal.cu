@@ -81,6 +81,7 @@ struct Mat {
     int64_t ldg, ldm, ldo;
     int rows, cols;
     int full0;                               // tiles of X of the matrices before
+    int pair_tri0, pair_full0;               // ... clusters for pairs
     int first[3], split[3];                  // of each Kind: clusters of the matrices before; shares of K of a tile
     float limit, rate;
     uint8_t g_bf16, o_bf16, tall, gvec, mvec, ovec;
@@ -93,6 +94,8 @@ struct Mat {
 
 struct Sizes {
     int count, full;                         // matrices; tiles of X
+    int pair_tri, pair_full;                 // clusters for pairs, four tiles each: of lower triangles, of X
+    bool pairs[4];                           // of each Kind, and of X: blocks work in pairs
     int clusters[3], blocks[3];              // of each Kind, for one product: clusters, their blocks
     const Mat *table;                        // in the workspace
     Stat *stat;
@@ -321,6 +324,7 @@ struct Product {
 
 struct Level {
     int mode, products, split;               // split: blocks of a cluster
+    int pair;                                // blocks work in pairs
     Product pr[2];
     int x1;                                  // GRAM, APPLY, LEAVE: X is the one of a later stage
     int x_lo;                                // ... and has a lo part
@@ -386,8 +390,9 @@ struct Side {
     int64_t lo;
     int wide, tile;
     bool mn, sym;
+    int pair = 0;                            // 1: tiles 2 p and 2 p + 1 are read the same way (a block on the diagonal either way)
 
-    __device__ __forceinline__ bool turned(int kb) const { return sym ? (kb >> 1) > tile : mn; }
+    __device__ __forceinline__ bool turned(int kb) const { return sym ? (kb >> 1) > (tile & ~pair) : mn; }
     __device__ __forceinline__ void load(uint32_t dst, int kb, uint64_t *bar) const {
         if (!turned(kb)) {
             const uint8_t *s = p + ((int64_t)tile * wide + kb) * BLOCK;
@@ -407,9 +412,28 @@ struct Side {
 };
 
 struct Smem {
-    uint64_t full[STAGES], empty[STAGES], sums[2], taken[2];
+    uint64_t full[STAGES], empty[STAGES], peer[STAGES], sums[2], taken[2];
     uint32_t tmem;
 };
+
+// Pairs: the even block of a cluster of two issues products of 256 rows for both, each block's rows from its own shared memory, half
+// of the second operand from each.
+__device__ __forceinline__ void mma_f16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile("{\n .reg .pred p, e;\n .reg .b32 r;\n setp.ne.b32 p, %4, 0;\n elect.sync r|e, 0xffffffff;\n"
+                 " @e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+                 "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
+}
+__device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
+    asm volatile("{\n .reg .pred e;\n .reg .b32 r;\n elect.sync r|e, 0xffffffff;\n"
+                 " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}\n" ::"r"(su32(bar)),
+                 "h"((uint16_t)3)
+                 : "memory");
+}
+__device__ __forceinline__ void arrive_even(uint64_t *bar) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;\n" : "=r"(at) : "r"(su32(bar)));
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at) : "memory");
+}
 
 __device__ __forceinline__ void load32(uint32_t addr, float *v) {
     uint32_t w[32];
@@ -428,7 +452,15 @@ __device__ __forceinline__ void load32(uint32_t addr, float *v) {
     for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(w[k]);
 }
 
+// PAIR: four tiles by a cluster of two blocks, 256 x 256 sums, whose products read 64 KB a block for 64 of K where four blocks
+// by themselves read as much each: it is the way from L2 that products wait for.  Both parts' products go into one sum (two of
+// 256 columns fill the tensor memory), which registers take over after 128 of K.  4096 x 4096: 2.72 ms, 3.18 without pairs;
+// sums taken over after 64 of K 3.63, after 256 2.67 at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
+// in each block: 4.26, products of 128 columns take as long as of 256.)
+template <bool PAIR>
 __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_constant__ Sizes l, const __grid_constant__ Level v) {
+    constexpr int WIDTH = PAIR ? 2 * T : T;          // columns of a block's tile
+    constexpr int MINE = PAIR ? 128 : 64;                       // ... of a thread
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *ring = smem_raw + ((1024u - (su32(smem_raw) & 1023u)) & 1023u);
     float *acc = reinterpret_cast<float *>(ring);               // the tile, once the ring is done with
@@ -438,19 +470,27 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         for (int s = 0; s < STAGES; ++s) {
             bar_init(&sm.full[s], 1);
             bar_init(&sm.empty[s], 1);
+            bar_init(&sm.peer[s], 1);
         }
         for (int k = 0; k < 2; ++k) {
             bar_init(&sm.sums[k], 1);
-            bar_init(&sm.taken[k], THREADS / 32);
+            bar_init(&sm.taken[k], (PAIR ? 2 : 1) * THREADS / 32);
         }
         asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     }
+    cg::cluster_group cluster = cg::this_cluster();
     if (warp == ISSUER) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(su32(&sm.tmem)));
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n");
+        if constexpr (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(su32(&sm.tmem)));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;\n");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;\n" ::"r"(su32(&sm.tmem)));
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;\n");
+        }
     }
     fence_before();
-    __syncthreads();
+    if (PAIR) cluster.sync();                                   // the other block's barriers and columns are there
+    else __syncthreads();
     fence_after();
     const uint32_t tmem = sm.tmem;
 
@@ -458,25 +498,40 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     // matrix: a tile in so many shares, or two tiles in half as many, or ...
     const int split = v.split, in_cluster = blockIdx.x % split, tri = v.mode <= MUL;
     int t = blockIdx.x / split, which = 0;
-    const int kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO, all = tri ? l.clusters[kind] : l.full;
+    const int kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO, all = PAIR ? (tri ? l.pair_tri : l.pair_full) : tri ? l.clusters[kind] : l.full;
     if (tri) {
         which = t / all;
         t -= which * all;
     }
     // the table is the first kernel's work, and that one was done before this one's predecessor let it start
-    const int index = tri ? find(l.count, t, [&](int k) { return l.table[k].first[kind]; })
-                          : find(l.count, t, [&](int k) { return l.table[k].full0; });
+    const int index = PAIR  ? find(l.count, t, [&](int k) { return tri ? l.table[k].pair_tri0 : l.table[k].pair_full0; })
+                      : tri ? find(l.count, t, [&](int k) { return l.table[k].first[kind]; })
+                            : find(l.count, t, [&](int k) { return l.table[k].full0; });
     const Mat m = l.table[index];
     const Product pr = v.pr[which];
-    const int shares = tri ? l.table[index].split[kind] : 1, rank = in_cluster % shares;
-    t = (t - (tri ? l.table[index].first[kind] : m.full0)) * (split / shares) + in_cluster / shares;
-    const bool idle = t >= (tri ? m.mb() * (m.mb() + 1) / 2 : m.rb() * m.cb());        // of a matrix's last cluster
+    const int shares = tri && !PAIR ? l.table[index].split[kind] : 1, rank = PAIR ? 0 : in_cluster % shares;
+    if (PAIR) t -= tri ? m.pair_tri0 : m.pair_full0;
+    else t = (t - (tri ? l.table[index].first[kind] : m.full0)) * (split / shares) + in_cluster / shares;
+    bool idle = !PAIR && t >= (tri ? m.mb() * (m.mb() + 1) / 2 : m.rb() * m.cb());     // of a matrix's last cluster
     const int mb = m.mb();
     const int64_t small_blocks = (int64_t)mb * mb * 2 * BLOCK, slot = 2 * small_blocks;
     const int64_t x_blocks = (int64_t)m.rb() * m.cb() * 2 * BLOCK;
     uint8_t *x = v.x1 ? m.x1 : m.x0;
     int i, j;
-    if (tri) {
+    bool mute = false;                                          // computed for the other block's sake
+    const int columns = tri ? mb : m.cb();                      // of tiles
+    if (PAIR) {                                                 // rows 2 p and 2 p + 1, columns 2 q and 2 q + 1
+        int p = t / ((m.cb() + 1) / 2), q = t % ((m.cb() + 1) / 2);
+        if (tri) {
+            p = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
+            while ((p + 1) * (p + 2) / 2 <= t) ++p;
+            while (p * (p + 1) / 2 > t) --p;
+            q = t - p * (p + 1) / 2;
+        }
+        i = 2 * p + in_cluster;
+        j = 2 * q;
+        mute = i >= (tri ? mb : m.rb());
+    } else if (tri) {
         i = (int)((sqrtf(8.0f * t + 1.0f) - 1.0f) * 0.5f);
         while ((i + 1) * (i + 2) / 2 <= t) ++i;
         while (i * (i + 1) / 2 > t) --i;
@@ -485,6 +540,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         i = t / m.cb();
         j = t % m.cb();
     }
+    if (mute) i = min(i, (tri ? mb : m.rb()) - 1);
     const Side sx{x, v.x_lo ? x_blocks : 0, 2 * m.cb(), 0, false, false};
     Side a, b;
     int kbs;                                                    // blocks of 64 along K
@@ -513,13 +569,17 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
             }
         }
     }
+    if (PAIR) {
+        a.pair = b.pair = 1;
+        b.tile = min(j + in_cluster, columns - 1);
+    }
     const int kb0 = idle ? 0 : rank * kbs / shares, kb1 = idle ? 0 : (rank + 1) * kbs / shares;
-    const bool same = a.p == b.p && a.tile == b.tile && a.mn == b.mn && a.sym == b.sym;
+    const bool same = !PAIR && a.p == b.p && a.tile == b.tile && a.mn == b.mn && a.sym == b.sym;
     const uint32_t bytes = a.bytes() + (same ? 0 : b.bytes());
     pdl_wait();
     pdl_trigger();
     if (v.mode == LEAVE && v.update && warp < THREADS / 32) {   // weights on their way to L2 during the products: a line a thread
-        const int each = m.o_bf16 ? 64 : 32, lines = T / each;
+        const int each = m.o_bf16 ? 64 : 32, lines = WIDTH / each;
         for (int e = threadIdx.x; e < T * lines; e += THREADS) {
             const int r = i * T + e / lines, c = j * T + e % lines * each;
             if (r < m.rows && c < m.cols)
@@ -545,6 +605,14 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
                 if (!bar_wait(&sm.full[k % STAGES], (k / STAGES) & 1, v.wait_cycles)) break;
         }
         __syncwarp();
+    } else if (PAIR && warp == ISSUER && in_cluster == 1) {     // tells the even block what has landed here
+        int s = 0;
+        uint32_t phase = 0u;
+        for (int kb = kb0; kb < kb1 && ok; ++kb) {
+            ok = __all_sync(0xffffffffu, bar_wait(&sm.full[s], phase, v.wait_cycles));
+            if (ok && lane == 0) arrive_even(&sm.peer[s]);
+            if (++s == STAGES) { s = 0; phase ^= 1u; }
+        }
     } else if (warp == ISSUER) {
         // D fp32, A and B fp16; bits 15 and 16: MN-major
         int s = 0, chunk = 0;
@@ -554,59 +622,73 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
             if (chunk >= 2 && !__all_sync(0xffffffffu, bar_wait(&sm.taken[chunk & 1], (chunk / 2 - 1) & 1, v.wait_cycles)))
                 ok = false;
             fence_after();
-            const uint32_t d = tmem + T * (chunk & 1), small = tmem + 2 * T;
+            const uint32_t d = tmem + WIDTH * (chunk & 1), small = PAIR ? d : tmem + 2 * T;
+            if (PAIR) rest = 1u;
             uint32_t on = 0u;
             for (int kb = at_; kb < end && ok; ++kb) {
                 if (!__all_sync(0xffffffffu, bar_wait(&sm.full[s], phase, v.wait_cycles))) { ok = false; break; }
+                if (PAIR && !__all_sync(0xffffffffu, bar_wait(&sm.peer[s], phase, v.wait_cycles))) { ok = false; break; }
                 fence_after();
                 const uint32_t base = su32(ring) + s * STAGE;
                 const bool at = a.turned(kb), bt = b.turned(kb);
-                const uint32_t idesc = (1u << 4) | ((at ? 1u : 0u) << 15) | ((bt ? 1u : 0u) << 16) | ((uint32_t)(T >> 3) << 17) | (8u << 24);
+                const uint32_t idesc = (1u << 4) | ((at ? 1u : 0u) << 15) | ((bt ? 1u : 0u) << 16) | ((uint32_t)(WIDTH >> 3) << 17) | ((PAIR ? 16u : 8u) << 24);
                 const uint32_t ka = at ? 2048 >> 4 : 32 >> 4, kbk = bt ? 2048 >> 4 : 32 >> 4;  // 16 of K
                 const uint64_t ad = desc(base, at), bd = desc(same ? base : base + 2 * BLOCK, bt);
+                auto four = [&](uint32_t to, uint64_t x_, uint64_t y_, uint32_t first) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma_f16(d, ad + k * ka, bd + k * kbk, idesc, k > 0 ? 1u : on);
+                    for (int k = 0; k < 4; ++k) {
+                        if constexpr (PAIR) mma_f16_pair(to, x_ + k * ka, y_ + k * kbk, idesc, k > 0 ? 1u : first);
+                        else mma_f16(to, x_ + k * ka, y_ + k * kbk, idesc, k > 0 ? 1u : first);
+                    }
+                };
+                four(d, ad, bd, on);
                 on = 1u;
                 if (b.lo) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_f16(small, ad + k * ka, bd + (BLOCK >> 4) + k * kbk, idesc, k > 0 ? 1u : rest);
+                    four(small, ad, bd + (BLOCK >> 4), rest);
                     rest = 1u;
                 }
                 if (a.lo) {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_f16(small, ad + (BLOCK >> 4) + k * ka, bd + k * kbk, idesc, k > 0 ? 1u : rest);
+                    four(small, ad + (BLOCK >> 4), bd, rest);
                     rest = 1u;
                 }
-                mma_commit(&sm.empty[s]);
+                if constexpr (PAIR) mma_commit_pair(&sm.empty[s]);
+                else mma_commit(&sm.empty[s]);
                 if (++s == STAGES) { s = 0; phase ^= 1u; }
             }
-            if (ok) mma_commit(&sm.sums[chunk & 1]);
+            if (ok) {
+                if constexpr (PAIR) mma_commit_pair(&sm.sums[chunk & 1]);
+                else mma_commit(&sm.sums[chunk & 1]);
+            }
         }
     }
     __syncwarp();
     // The sums from tensor memory into registers, a chunk at a time; zero where this share of K is empty.
-    float sum[64];
-    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * 64);
+    float sum[MINE];
+    const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * MINE);
     if (warp < THREADS / 32) {
 #pragma unroll
-        for (int k = 0; k < 64; ++k) sum[k] = 0.0f;
+        for (int k = 0; k < MINE; ++k) sum[k] = 0.0f;
         int chunk = 0;
         for (int at_ = kb0; at_ < kb1 && ok; at_ += CHUNK, ++chunk) {
             ok = __all_sync(0xffffffffu, bar_wait(&sm.sums[chunk & 1], (chunk >> 1) & 1, v.wait_cycles));
             fence_after();
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
+            for (int c = 0; c < MINE; c += 32) {
                 float w[32];
-                load32(mine + T * (chunk & 1) + c, w);
+                load32(mine + WIDTH * (chunk & 1) + c, w);
 #pragma unroll
                 for (int k = 0; k < 32; ++k) sum[c + k] += w[k];
             }
             fence_before();
-            if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(su32(&sm.taken[chunk & 1])) : "memory");
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) arrive_even(&sm.taken[chunk & 1]);
+                else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(su32(&sm.taken[chunk & 1])) : "memory");
+            }
         }
-        if (kb1 > kb0 && (a.lo || b.lo)) {
+        if (!PAIR && kb1 > kb0 && (a.lo || b.lo)) {
 #pragma unroll
-            for (int c = 0; c < 64; c += 32) {
+            for (int c = 0; c < MINE; c += 32) {
                 float w[32];
                 load32(mine + 2 * T + c, w);
 #pragma unroll
@@ -617,18 +699,18 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     ok = __syncthreads_and(ok);                                 // and the last loads have landed
     // Rows of the tile that this block finishes.  The other blocks' sums for them arrive in its shared memory, a share after the
     // other, once all are done with their rings (reading them from here instead takes 2 us more: their way is there twice).
-    cg::cluster_group cluster = cg::this_cluster();
     const int rows = T / shares, r0 = rank * rows;
-    if (split > 1) cluster.sync();
+    if (split > 1 && !PAIR) cluster.sync();
     if (warp < THREADS / 32 && !idle) {
         const int r = (warp & 3) * 32 + lane, owner = r / rows;
-        float *d = acc + (rank * rows + r - owner * rows) * PITCH + (warp >> 2) * 64;
+        float *d = PAIR ? acc + ((warp >> 2) * T + r) * PITCH : acc + (rank * rows + r - owner * rows) * PITCH + (warp >> 2) * 64;
         if (shares > 1) d = cluster.map_shared_rank(d, in_cluster - rank + owner);
 #pragma unroll
-        for (int k = 0; k < 64; k += 4) *reinterpret_cast<float4 *>(d + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+        for (int k = 0; k < MINE; k += 4) *reinterpret_cast<float4 *>(d + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
     }
-    if (split > 1) cluster.sync();
+    if (split > 1 && !PAIR) cluster.sync();
     else __syncthreads();
+    if (mute) idle = true;
 
     // eight columns a thread at a time
     const Stat st = v.mode == GRAM || v.mode == LEAVE || v.mode == APPLY ? l.stat[index] : Stat{};
@@ -639,7 +721,8 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     const int wide = v.mode == APPLY ? 2 * m.cb() : 2 * mb;
     const int64_t lo = v.mode == APPLY ? x_blocks : small_blocks;
     const int c = (threadIdx.x & 15) * 8;
-    for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32 && !idle; r += 16) {
+    for (int tile = 0; tile < (PAIR ? 2 : 1); ++tile, ++j, acc += T * PITCH)
+    for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32 && !idle && (!PAIR || (j < columns && (!tri || j <= i))); r += 16) {
         float z[8];
 #pragma unroll
         for (int k = 0; k < 8; k += 4) {
@@ -692,10 +775,13 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         }
     }
     fence_before();
-    __syncthreads();
+    __syncwarp();
+    if (PAIR) cluster.sync();                                   // no block leaves while the other's arrivals are on their way to it
+    else __syncthreads();
     if (warp == ISSUER) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));
+        if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));
+        else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;\n" ::"r"(tmem));
     }
 }
 
@@ -1138,8 +1224,9 @@ static bool join(const minw_matrix *g, int count) {
 static bool is_large(const minw_matrix &g, bool joined) { return g.rows > 0 && g.cols > 0 && (joined || !is_small(g)); }
 
 // Clusters of a level on m x m matrices (gram: of the Gram products): sums along K are split into shares where that ends the
-// level earlier.  A block of 64 of K takes 0.55 us, a tile's start and end 4.5, a sum over a cluster 3.5 more.
-static void shares(Mat *table, Sizes &l, Kind kind) {
+// level earlier.  A block of 64 of K takes 0.55 us, a tile's start and end 4.5, a sum over a cluster 3.5 more.  Returns the
+// level's time by that.
+static float shares(Mat *table, Sizes &l, Kind kind) {
     const bool gram = kind == OF_X;
     const int products = kind == TWO ? 2 : 1, sms = num_sms() > 0 ? num_sms() : 152;
     float best = 1e30f;
@@ -1172,13 +1259,14 @@ static void shares(Mat *table, Sizes &l, Kind kind) {
                 l.blocks[kind] = cluster;
             }
         }
+    return best;
 }
 
 // Fills a launch's list from matrix k on; returns the next launch's first, and the workspace that it takes.  base null: the
 // sizes alone.
 static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int k, int count,
                 uint8_t *base, int64_t *need, bool joined) {
-    l.count = l.full = 0;
+    l.count = l.full = l.pair_tri = l.pair_full = 0;
     l.table = reinterpret_cast<const Mat *>(base);
     int64_t used = up(CAP * sizeof(Mat), 256);
     l.stat = reinterpret_cast<Stat *>(base + used);
@@ -1196,15 +1284,29 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
         Mat &m = table[l.count++];
         m = describe(g, mom, out, k);
         m.full0 = l.full;
+        m.pair_tri0 = l.pair_tri;
+        m.pair_full0 = l.pair_full;
         const int mb = m.mb();
         l.full += m.rb() * m.cb();
+        l.pair_tri += (mb + 1) / 2 * ((mb + 1) / 2 + 1) / 2;
+        l.pair_full += (m.rb() + 1) / 2 * ((m.cb() + 1) / 2);
         const int64_t x = (int64_t)m.rb() * m.cb() * 4 * BLOCK;
         m.x0 = base + used;
         m.x1 = m.x0 + x;
         m.small = m.x1 + x;
         used += matrix_bytes(m.rows, m.cols);
     }
-    for (const Kind kind : {OF_X, ONE, TWO}) shares(table, l, kind);
+    int small_k = 0, long_k = 0;
+    for (int e = 0; e < l.count; ++e) {
+        small_k = std::max(small_k, 2 * table[e].mb());
+        long_k = std::max(long_k, 2 * std::max(table[e].rb(), table[e].cb()));
+    }
+    // a pair's block of 64 of K takes 0.85 us, its tiles' start and end 7; those of a tile where there are several a block, 0.62 and 5
+    const int sms = num_sms() > 0 ? num_sms() : 152;
+    auto pairs = [&](int64_t clusters, int k) { return (2 * clusters + sms - 1) / sms * (0.85f * k + 7.0f); };
+    for (const Kind kind : {OF_X, ONE, TWO})
+        l.pairs[kind] = pairs((kind == TWO ? 2 : 1) * (int64_t)l.pair_tri, kind == OF_X ? long_k : small_k) < shares(table, l, kind);
+    l.pairs[3] = pairs(l.pair_full, small_k) < (l.full + sms - 1) / sms * (0.62f * small_k + 5.0f);
     *need = used;
     return k;
 }
@@ -1232,11 +1334,15 @@ static bool sizes_fit(const minw_matrix *g, int count) {
 
 static cudaError_t launch(const Sizes &l, Level v, cudaStream_t s) {
     const Kind kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO;
-    v.split = v.mode <= MUL ? l.blocks[kind] : 1;
-    const int64_t clusters = v.mode <= MUL ? (int64_t)l.clusters[kind] * v.products : l.full;
+    const bool tri = v.mode <= MUL;
+    const int64_t pairs = tri ? (int64_t)l.pair_tri * v.products : l.pair_full;
+    v.pair = l.pairs[tri ? kind : 3];
+    v.split = v.pair ? 2 : tri ? l.blocks[kind] : 1;
+    const int64_t clusters = v.pair ? pairs : tri ? (int64_t)l.clusters[kind] * v.products : l.full;
     v.wait_cycles = (long long)plan_options().wait_cycles;
-    const int smem = STAGES * (int)STAGE + 1024;
-    if (!allow_shared(reinterpret_cast<const void *>(product_kernel), smem)) return cudaErrorInvalidValue;
+    auto kern = v.pair ? product_kernel<true> : product_kernel<false>;
+    const int smem = STAGES * (int)STAGE + 1024;                // (as much for pairs)
+    if (!allow_shared(reinterpret_cast<const void *>(kern), smem)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * v.split));
     cfg.blockDim = dim3(THREADS + 64);
@@ -1250,8 +1356,8 @@ static cudaError_t launch(const Sizes &l, Level v, cudaStream_t s) {
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
-    max_shared_carveout(reinterpret_cast<const void *>(product_kernel));
-    return cudaLaunchKernelEx(&cfg, product_kernel, l, v);
+    max_shared_carveout(reinterpret_cast<const void *>(kern));
+    return cudaLaunchKernelEx(&cfg, kern, l, v);
 }
 
 // All steps of one list.

@@ -132,6 +132,24 @@ def test_orthogonalised(M, shapes, types, pad, off):
         assert all(torch.equal(a, b) for a, b in zip(first, gv))
 
 
+@pytest.mark.parametrize("shape", [(2200, 2310), (2310, 2190), (1100, 5000), (5000, 1100), (1500, 1200)])
+@pytest.mark.parametrize("types", ["fb", "bf"])
+def test_large(M, shape, types):
+    """Enough tiles for blocks in pairs, odd numbers of them."""
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(shape, types))
+    g = [_matrix(gen, *shape, "batch").to(DT[types[0]]), _matrix(gen, 300, 200).to(DT[types[0]])]
+    o = [torch.empty_like(x, dtype=DT[types[1]]) for x in g]
+    ws = _ws(M, g)
+    M.minw_orthogonalize(g, o, ws)
+    first = [x.clone() for x in o]
+    for x, y in zip(g, o):
+        _close(y, _ns(x), types[1])
+    ws.fill_(1)
+    M.minw_orthogonalize(g, o, ws)
+    assert all(torch.equal(a, b) for a, b in zip(first, o))
+    assert M.minw_get_last_device_error() == M.MINW_OK
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6, 7, 10])
 @pytest.mark.parametrize("t", ["f", "b"])
 def test_steps(M, steps, t):
