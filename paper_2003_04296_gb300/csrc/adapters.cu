@@ -7,12 +7,14 @@
 // tile holds all rows, every tile finds its own (tile t belongs to the first row of its
 // user, the others leave) and a cluster takes it: its blocks share the columns of x (K), add
 // up their parts of h through each other's shared memory, and share the columns of y (O), one
-// launch.  Else a plan sorts the rows by user, and the two products are a launch each.  The backward's v_t = alpha_u up_u dy_t, dx_t = down_u^T v_t is the
-// same kernel with the matrices exchanged; the matrices' gradients are sums over a user's rows,
+// launch (adapters_few.cu).  Else a plan sorts the rows by user, and the two products are a launch
+// each.  The backward's v_t = alpha_u up_u dy_t, dx_t = down_u^T v_t is the same kernel with the
+// matrices exchanged; the matrices' gradients are sums over a user's rows,
 //   ddown_u = sum v_t x_t^T,   dup_u = alpha_u sum h_t dy_t^T,   a kernel of their own.
 //
-// All of it is bound by memory (r <= 64 as a rule: 2 r operations a value), so the products run
-// on mma.sync (bf16, fp32 sums) from registers, without a trip through shared memory:
+// Few operations a value (2 r, r <= 64 as a rule) and short kernels: latency bounds them, and the way of
+// instructions that run once.  4096 bf16 rows of 8 users, 4096 -> 4096 at rank 64, 64 us (108 MB: 16 us at the copy rate);
+// the backward of 2048 at rank 32, 56.  The products run on mma.sync (bf16, fp32 sums) from registers:
 // - along K, the order of the values is free, as long as both operands have the same: a lane
 //   takes eight consecutive values of a row for two products of 16;
 // - along O (and along K in the gradients), lane g of a group of eight takes eight consecutive columns of
@@ -565,8 +567,8 @@ __global__ void __launch_bounds__(THREADS, 2) widen_kernel(const __grid_constant
                     float f[16];
                     const int64_t at = (int64_t)max(row[m][i], 0) * a.ld_base + c;
                     const int n = row[m][i] >= 0 ? left : 0;
-                    if (a.base_bf16) load16<uint16_t, true>(a.base, at, n, f);
-                    else load16<float, true>(a.base, at, n, f);
+                    if (a.base_bf16) load16<uint16_t>(a.base, at, n, f);
+                    else load16<float>(a.base, at, n, f);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) z(m, i, k) += f[k];
                 }
@@ -891,7 +893,7 @@ static cudaError_t launch_widen_of(const Args &a, int64_t tiles, cudaStream_t s)
     if (!allow_shared(reinterpret_cast<const void *>(kern), ring + 3 * 32 * (MAX_RANK + 8) * 2)) return cudaErrorInvalidValue;
     // two blocks an SM, each of eight blocks of columns or more
     const int blocks = (a.E + 63) / 64, sms = num_sms() > 0 ? num_sms() : 152;
-    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((blocks + WARPS - 1) / WARPS, 4 * sms / tiles));
+    const int64_t groups = std::max<int64_t>(1, std::min<int64_t>((blocks + WARPS - 1) / WARPS, 3 * sms / tiles));
     const int per = (int)((blocks + groups - 1) / groups + WARPS - 1) / WARPS * WARPS, g = (blocks + per - 1) / per;
     return launch_pdl(kern, dim3((unsigned)(tiles * g)), dim3(THREADS), (size_t)ring + (a.fine ? 3 : 2) * a.most * (a.rp + 8) * 2, s, a, g, per);
 }

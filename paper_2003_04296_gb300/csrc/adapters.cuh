@@ -65,13 +65,13 @@ struct Args {
     Plan plan;
 };
 
-template <typename V, bool ODD>
+template <typename V>
 __device__ __forceinline__ void load16(const void *p, int64_t at, int left, float *v) {
     const V *q = static_cast<const V *>(p) + at;
 #pragma unroll
     for (int k = 0; k < 16; k += 8) {
         Eight<V> e;
-        e.template load<ODD>(q + k, left - k);
+        e.template load<true>(q + k, left - k);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             v[k + i] = __uint_as_float(sizeof(V) == 4 ? e.w[i % (2 * sizeof(V))] : (i & 1) ? e.w[i >> 1] & 0xffff0000u : e.w[i >> 1] << 16);

@@ -154,8 +154,8 @@ __device__ __forceinline__ void widen(const Args &a, const int *rows, int count,
                     z[8 + k] = acc[m][k][2 * i + 1];
                 }
                 if (a.base) {
-                    if (a.base_bf16) load16<uint16_t, true>(a.base, row * a.ld_base + c, left, f);
-                    else load16<float, true>(a.base, row * a.ld_base + c, left, f);
+                    if (a.base_bf16) load16<uint16_t>(a.base, row * a.ld_base + c, left, f);
+                    else load16<float>(a.base, row * a.ld_base + c, left, f);
 #pragma unroll
                     for (int k = 0; k < 16; ++k) z[k] += f[k];
                 }

@@ -28,8 +28,12 @@
 // X Q without a transposed copy, a symmetric matrix is its lower triangle alone, blocks travel
 // as plain bulk copies, and no matrix of a list needs a tensor map.
 //
-// A list goes through the kernels together: level k of all its matrices is one
-// launch.  Clusters split the sums of a tile where there are fewer tiles than SMs.
+// A list goes through the kernels together: level k of all its matrices is one launch.
+// What bounds a level: where tiles are many, the way from L2 into the SMs (64 bytes a clock: 64 KB
+// for 64 of K, 0.55 to 0.67 us a tile of 128 x 128, of which the tensor cores need 0.4), so
+// pairs of blocks take 256 x 256; where they are few, latency (2.5 us between two launches, 4.5 for a
+// tile's start and end), so clusters split K.  4096 x 4096 2.64 ms (1.56 of the 1.88 PFLOP/s that
+// a library's bf16 product reaches), 1024 x 8192 290 us, 128 x 1152 111, 10 x 1024 10.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -429,10 +433,14 @@ __device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
                  "h"((uint16_t)3)
                  : "memory");
 }
+// An arrival at the even block's barrier.  RELAXED: of sums read from tensor memory, which the fence before orders; a release waits for
+// this thread's other memory operations as well.
+template <bool RELAXED>
 __device__ __forceinline__ void arrive_even(uint64_t *bar) {
     uint32_t at;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;\n" : "=r"(at) : "r"(su32(bar)));
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at) : "memory");
+    if constexpr (RELAXED) asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at) : "memory");
+    else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at) : "memory");
 }
 
 __device__ __forceinline__ void load32(uint32_t addr, float *v) {
@@ -454,8 +462,8 @@ __device__ __forceinline__ void load32(uint32_t addr, float *v) {
 
 // PAIR: four tiles by a cluster of two blocks, 256 x 256 sums, whose products read 64 KB a block for 64 of K where four blocks
 // by themselves read as much each: it is the way from L2 that products wait for.  Both parts' products go into one sum (two of
-// 256 columns fill the tensor memory), which registers take over after 128 of K.  4096 x 4096: 2.72 ms, 3.18 without pairs;
-// sums taken over after 64 of K 3.63, after 256 2.67 at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
+// 256 columns fill the tensor memory), which registers take over after 128 of K.  4096 x 4096: 2.64 ms, 3.18 without pairs;
+// sums taken over after 64 of K 3.63, after 256 2.60 at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
 // in each block: 4.26, products of 128 columns take as long as of 256.)
 template <bool PAIR>
 __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_constant__ Sizes l, const __grid_constant__ Level v) {
@@ -610,7 +618,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         uint32_t phase = 0u;
         for (int kb = kb0; kb < kb1 && ok; ++kb) {
             ok = __all_sync(0xffffffffu, bar_wait(&sm.full[s], phase, v.wait_cycles));
-            if (ok && lane == 0) arrive_even(&sm.peer[s]);
+            if (ok && lane == 0) arrive_even<false>(&sm.peer[s]);
             if (++s == STAGES) { s = 0; phase ^= 1u; }
         }
     } else if (warp == ISSUER) {
@@ -682,7 +690,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
             fence_before();
             __syncwarp();
             if (lane == 0) {
-                if constexpr (PAIR) arrive_even(&sm.taken[chunk & 1]);
+                if constexpr (PAIR) arrive_even<true>(&sm.taken[chunk & 1]);
                 else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(su32(&sm.taken[chunk & 1])) : "memory");
             }
         }
