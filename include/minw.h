@@ -794,9 +794,10 @@ MINW_API minw_status minw_w4_adapters(const void *x, int32_t x_type, int64_t ldx
  * dx [T][K] has x's type and rows of lddx.  dx, ddown and dup are nullable
  * (x is read for ddown alone, h for dup alone).  Users without rows get zeros,
  * rows without an adapter dx = 0 (accumulate: unchanged).  All sums are fp32
- * in a fixed order (the same bits on every call).  dx may overlap neither x
- * nor dy.  workspace with backward = 1; T = 0 writes zeros to ddown and dup.
- * Errors as minw_adapters. */
+ * in an order that the sizes, the types and the set of outputs asked for fix
+ * (the same bits on every call with these).  dx may overlap neither x nor dy.
+ * workspace with backward = 1; T = 0 writes zeros to ddown and dup.  Errors as
+ * minw_adapters. */
 MINW_API minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K,
                                             const int32_t *ids, const void *down, const void *up, int32_t p_type,
                                             int32_t n, int32_t r, const float *alpha, const float *h, const void *dy,

@@ -1085,11 +1085,16 @@ minw_status minw_adapters_backward(const void *x, int32_t x_type, int64_t ldx, i
     // jobs of one type in one launch
     GradArgs ga{};
     ga.T = (int)T; ga.n = n; ga.r = r; ga.rp = rank_pitch(r); ga.plan = p; ga.beside = dx && T > 0;
-    // warps share a user's rows where its columns leave SMs without a block, if there are steps of 16 rows for them
+    // Warps share a user's rows while the blocks that this makes are four for an SM, if each keeps a step of 16 rows.  Beside dx,
+    // whose blocks hold half of the SMs' places, a third and a fourth block only if each warp keeps 64 rows: users of 341 rows at
+    // 4096 + 4096 columns take 57 us, left at two blocks 68; users of 50 rows at 3001 + 2777 columns take 61 us (fp32) and 41
+    // (bf16), shared 70 and 47; without dx shared 44 and 31, left at two blocks 56 and 36.
     const int sms = num_sms() > 0 ? num_sms() : 152;
     const int64_t columns = ((ddown ? (K + 63) / 64 : 0) + (dup ? (O + 63) / 64 : 0)) * (int64_t)n;
     ga.along = 1;
-    while (ga.along < WARPS / 2 && columns * ga.along / WARPS < 2 * sms && T / n >= 16 * ga.along) ga.along *= 2;
+    while (ga.along < WARPS / 2 && columns * ga.along / WARPS <= 2 * sms &&
+           T / n >= (ga.beside && columns * 2 * ga.along / WARPS > 2 * sms ? 64 : 16) * ga.along)
+        ga.along *= 2;
     const int wide = 64 * (WARPS / ga.along);
     const Job jobs[2] = {{hp, x, ddown, ldx, K, (K + wide - 1) / wide, !vec_rows(x, ldx, x_type == MINW_BF16), vec_rows(ddown, K, 0)},
                          {hh, dy, dup, lddy, O, (O + wide - 1) / wide, !vec_rows(dy, lddy, dy_type == MINW_BF16), vec_rows(dup, O, 0)}};

@@ -463,7 +463,7 @@ __device__ __forceinline__ void load32(uint32_t addr, float *v) {
 // PAIR: four tiles by a cluster of two blocks, 256 x 256 sums, whose products read 64 KB a block for 64 of K where four blocks
 // by themselves read as much each: it is the way from L2 that products wait for.  Both parts' products go into one sum (two of
 // 256 columns fill the tensor memory), which registers take over after 128 of K.  4096 x 4096: 2.64 ms, 3.18 without pairs;
-// sums taken over after 64 of K 3.63, after 256 2.60 at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
+// sums taken over after 64 of K 1.33 times that, after 256 0.98 times at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
 // in each block: 4.26, products of 128 columns take as long as of 256.)
 template <bool PAIR>
 __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_constant__ Sizes l, const __grid_constant__ Level v) {
