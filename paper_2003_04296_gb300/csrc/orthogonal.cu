@@ -330,7 +330,8 @@ struct Level {
     int mode, products, split;               // split: blocks of a cluster
     int pair;                                // blocks work in pairs
     Product pr[2];
-    int x1;                                  // GRAM, APPLY, LEAVE: X is the one of a later stage
+    int later;                               // GRAM, APPLY, LEAVE: of a later stage than the first
+    int x1;                                  // ... X is in x1 (every other stage; APPLY writes the other one)
     int x_lo;                                // ... and has a lo part
     float a, b;                              // POLY: a I + b (slot p) + factor sum, in the result's scale
     int update;                              // LEAVE: weights are updated
@@ -723,9 +724,10 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     // eight columns a thread at a time
     const Stat st = v.mode == GRAM || v.mode == LEAVE || v.mode == APPLY ? l.stat[index] : Stat{};
     float factor = pr.factor;
-    if (v.mode == GRAM && !v.x1) factor *= st.gram;
-    if (v.mode >= APPLY && !v.x1) factor *= st.apply;
-    uint8_t *out = v.mode == APPLY ? m.x1 : m.small + pr.out * slot;
+    if (v.mode == GRAM && !v.later) factor *= st.gram;
+    if (v.mode >= APPLY && !v.later) factor *= st.apply;
+    // (tiles of Q X still read X where others are done: never into the X that this launch reads)
+    uint8_t *out = v.mode == APPLY ? (v.x1 ? m.x0 : m.x1) : m.small + pr.out * slot;
     const int wide = v.mode == APPLY ? 2 * m.cb() : 2 * mb;
     const int64_t lo = v.mode == APPLY ? x_blocks : small_blocks;
     const int c = (threadIdx.x & 15) * 8;
@@ -1395,7 +1397,8 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
         const bool last = st + 1 == stages;
         int A = 0, Q = -1;
         Level v{};
-        v.x1 = st > 0;
+        v.later = st > 0;
+        v.x1 = st & 1;
         v.x_lo = st > 0 || x_lo;
         v.mode = GRAM;
         v.products = 1;
@@ -1426,7 +1429,8 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
         Level e{};
         e.mode = last ? LEAVE : APPLY;
         e.products = 1;
-        e.x1 = st > 0;
+        e.later = st > 0;
+        e.x1 = st & 1;
         e.x_lo = st > 0 || x_lo;
         e.update = update;
         e.lr = lr;
