@@ -110,6 +110,10 @@ template <int N>
 struct Table {
     Mat m[N];
 };
+template <>
+struct Table<0> {
+    Mat *m = nullptr;
+};
 
 // The matrix of tile or cluster t: the last one that begins at or before it.
 template <typename F>
@@ -466,8 +470,11 @@ __device__ __forceinline__ void load32(uint32_t addr, float *v) {
 // 256 columns fill the tensor memory), which registers take over after 128 of K.  4096 x 4096: 2.64 ms, 3.18 without pairs;
 // sums taken over after 64 of K 1.33 times that, after 256 0.98 times at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
 // in each block: 4.26, products of 128 columns take as long as of 256.)
-template <bool PAIR>
-__global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_constant__ Sizes l, const __grid_constant__ Level v) {
+// N: matrices whose descriptions come with the launch, so that a block knows its work before it waits for the kernel before; 0:
+// they are read from the workspace, after that wait (what an earlier kernel wrote is there for certain only then).
+template <bool PAIR, int N>
+__global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_constant__ Sizes l, const __grid_constant__ Level v,
+                                                                  const __grid_constant__ Table<N> own) {
     constexpr int WIDTH = PAIR ? 2 * T : T;          // columns of a block's tile
     constexpr int MINE = PAIR ? 128 : 64;                       // ... of a thread
     extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -502,6 +509,8 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     else __syncthreads();
     fence_after();
     const uint32_t tmem = sm.tmem;
+    if (N == 0) pdl_wait();
+    const Mat *table = N == 0 ? l.table : own.m;
 
     // What this block computes: matrix, product, tile (i, j), share of K.  A cluster takes `split` blocks' work of one
     // matrix: a tile in so many shares, or two tiles in half as many, or ...
@@ -512,15 +521,14 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         which = t / all;
         t -= which * all;
     }
-    // the table is the first kernel's work, and that one was done before this one's predecessor let it start
-    const int index = PAIR  ? find(l.count, t, [&](int k) { return tri ? l.table[k].pair_tri0 : l.table[k].pair_full0; })
-                      : tri ? find(l.count, t, [&](int k) { return l.table[k].first[kind]; })
-                            : find(l.count, t, [&](int k) { return l.table[k].full0; });
-    const Mat m = l.table[index];
+    const int index = PAIR  ? find(l.count, t, [&](int k) { return tri ? table[k].pair_tri0 : table[k].pair_full0; })
+                      : tri ? find(l.count, t, [&](int k) { return table[k].first[kind]; })
+                            : find(l.count, t, [&](int k) { return table[k].full0; });
+    const Mat m = table[index];
     const Product pr = v.pr[which];
-    const int shares = tri && !PAIR ? l.table[index].split[kind] : 1, rank = PAIR ? 0 : in_cluster % shares;
+    const int shares = tri && !PAIR ? table[index].split[kind] : 1, rank = PAIR ? 0 : in_cluster % shares;
     if (PAIR) t -= tri ? m.pair_tri0 : m.pair_full0;
-    else t = (t - (tri ? l.table[index].first[kind] : m.full0)) * (split / shares) + in_cluster / shares;
+    else t = (t - (tri ? table[index].first[kind] : m.full0)) * (split / shares) + in_cluster / shares;
     bool idle = !PAIR && t >= (tri ? m.mb() * (m.mb() + 1) / 2 : m.rb() * m.cb());     // of a matrix's last cluster
     const int mb = m.mb();
     const int64_t small_blocks = (int64_t)mb * mb * 2 * BLOCK, slot = 2 * small_blocks;
@@ -585,7 +593,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     const int kb0 = idle ? 0 : rank * kbs / shares, kb1 = idle ? 0 : (rank + 1) * kbs / shares;
     const bool same = !PAIR && a.p == b.p && a.tile == b.tile && a.mn == b.mn && a.sym == b.sym;
     const uint32_t bytes = a.bytes() + (same ? 0 : b.bytes());
-    pdl_wait();
+    if (N > 0) pdl_wait();
     pdl_trigger();
     if (v.mode == LEAVE && v.update && warp < THREADS / 32) {   // weights on their way to L2 during the products: a line a thread
         const int each = m.o_bf16 ? 64 : 32, lines = WIDTH / each;
@@ -1342,7 +1350,8 @@ static bool sizes_fit(const minw_matrix *g, int count) {
     return tiles < (1 << 26);
 }
 
-static cudaError_t launch(const Sizes &l, Level v, cudaStream_t s) {
+template <int N>
+static cudaError_t launch(const Sizes &l, Level v, const Table<N> &own, cudaStream_t s) {
     const Kind kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO;
     const bool tri = v.mode <= MUL;
     const int64_t pairs = tri ? (int64_t)l.pair_tri * v.products : l.pair_full;
@@ -1350,7 +1359,7 @@ static cudaError_t launch(const Sizes &l, Level v, cudaStream_t s) {
     v.split = v.pair ? 2 : tri ? l.blocks[kind] : 1;
     const int64_t clusters = v.pair ? pairs : tri ? (int64_t)l.clusters[kind] * v.products : l.full;
     v.wait_cycles = (long long)plan_options().wait_cycles;
-    auto kern = v.pair ? product_kernel<true> : product_kernel<false>;
+    auto kern = v.pair ? product_kernel<true, N> : product_kernel<false, N>;
     const int smem = STAGES * (int)STAGE + 1024;                // (as much for pairs)
     if (!allow_shared(reinterpret_cast<const void *>(kern), smem)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
@@ -1367,22 +1376,15 @@ static cudaError_t launch(const Sizes &l, Level v, cudaStream_t s) {
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled() ? 2 : 1;
     max_shared_carveout(reinterpret_cast<const void *>(kern));
-    return cudaLaunchKernelEx(&cfg, kern, l, v);
+    return cudaLaunchKernelEx(&cfg, kern, l, v, own);
 }
 
-// All steps of one list.
-static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &step, int steps, bool x_lo, bool update, float lr,
-                         cudaStream_t s) {
+// All steps of one list; own: its descriptions for the launches of products (none: read from the workspace).
+template <int M, int N>
+static minw_status chain(const Table<M> &table, const Table<N> &own, const Sizes &l, const Step &step, int steps, bool x_lo, bool update,
+                         float lr, cudaStream_t s) {
     const dim3 tiles((unsigned)l.full);
-    cudaError_t e0;
-    if (l.count <= FEW) {
-        Table<FEW> few;
-        std::copy(table.m, table.m + l.count, few.m);
-        e0 = launch_pdl_stream(false, squares_kernel<FEW>, tiles, dim3(THREADS), 0, s, few, l, step);
-    } else {
-        e0 = launch_pdl_stream(false, squares_kernel<CAP>, tiles, dim3(THREADS), 0, s, table, l, step);
-    }
-    if (e0 != cudaSuccess) return launch_failed();
+    if (launch_pdl_stream(false, squares_kernel<M>, tiles, dim3(THREADS), 0, s, table, l, step) != cudaSuccess) return launch_failed();
     if (launch_pdl_stream(false, enter_kernel, tiles, dim3(THREADS), 0, s, l, step, x_lo ? 1 : 0) !=
         cudaSuccess)
         return launch_failed();
@@ -1403,7 +1405,7 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
         v.mode = GRAM;
         v.products = 1;
         v.pr[0] = {0, 0, A, two(SA - 30)};
-        if (launch(l, v, s) != cudaSuccess) return launch_failed();
+        if (launch(l, v, own, s) != cudaSuccess) return launch_failed();
         for (int k = 1; k <= n; ++k) {
             const int Z = k == 1 ? 4 : 2;                                             // the first Z is Q
             Level p{};
@@ -1412,17 +1414,17 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
             p.pr[0] = {A, A, Z, CC * two(SZ - 2 * SA)};
             p.a = CA * two(SZ);
             p.b = CB * two(SZ - SA);
-            if (launch(l, p, s) != cudaSuccess) return launch_failed();
+            if (launch(l, p, own, s) != cudaSuccess) return launch_failed();
             Level w{};
             w.mode = MUL;
             if (k < n) w.pr[w.products++] = {Z, A, 3, two(-SZ)};                      // Z A
             if (k > 1) w.pr[w.products++] = {Z, Q, Q ^ 1, two(SQ[k] - SZ - SQ[k - 1])};
             Q = k == 1 ? 4 : Q ^ 1;
-            if (w.products > 0 && launch(l, w, s) != cudaSuccess) return launch_failed();
+            if (w.products > 0 && launch(l, w, own, s) != cudaSuccess) return launch_failed();
             if (k < n) {
                 w.products = 1;
                 w.pr[0] = {3, Z, A ^ 1, two(-SZ)};
-                if (launch(l, w, s) != cudaSuccess) return launch_failed();
+                if (launch(l, w, own, s) != cudaSuccess) return launch_failed();
                 A ^= 1;
             }
         }
@@ -1435,7 +1437,7 @@ static minw_status chain(const Table<CAP> &table, const Sizes &l, const Step &st
         e.update = update;
         e.lr = lr;
         e.pr[0] = {Q, Q, 0, two((last ? 0 : 15) - SQ[n] - 15)};
-        if (launch(l, e, s) != cudaSuccess) return launch_failed();
+        if (launch(l, e, own, s) != cudaSuccess) return launch_failed();
     }
     return launch_status();
 }
@@ -1491,7 +1493,14 @@ static minw_status run(const minw_matrix *g, const minw_matrix *mom, const minw_
         int64_t need;
         k = fill(table.m, l, g, mom, out, k, count, ws, &need, joined);
         if (l.count == 0) break;
-        const minw_status st = chain(table, l, step, steps, x_lo, update, lr, s);
+        minw_status st;
+        if (l.count <= FEW) {
+            Table<FEW> few;
+            std::copy(table.m, table.m + l.count, few.m);
+            st = chain(few, few, l, step, steps, x_lo, update, lr, s);
+        } else {
+            st = chain(table, Table<0>{}, l, step, steps, x_lo, update, lr, s);
+        }
         if (st != MINW_OK) return st;
     }
     return launch_status();
