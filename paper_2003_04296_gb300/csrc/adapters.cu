@@ -665,9 +665,10 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
     const TZ *z = static_cast<const TZ *>(job.z);
     pdl_trigger();
     // Beside the kernel that makes dx, whose results are not needed here: it lets this one start once the parts are there, and is
-    // waited for at the end, for those who wait for this one.
+    // waited for at the end, for those who wait for this one.  Until then all that earlier kernels wrote is read through L2, where it
+    // lay before that one let this one start: what an SM's own cache holds is certain to be new only after a wait.
     if (!a.beside) pdl_wait();
-    const int first = a.plan.first[u], count = a.plan.first[u + 1] - first;
+    const int first = __ldcg(a.plan.first + u), count = __ldcg(a.plan.first + u + 1) - first;
     for (int j0 = 0; j0 < a.r; j0 += 16 * RT) {
         float acc[RT][8][4];
 #pragma unroll
@@ -680,7 +681,7 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
         for (int s0 = 0; s0 < count; s0 += ORDER) {
             const int seg = min(ORDER, count - s0);
             __syncthreads();
-            for (int e = threadIdx.x; e < seg; e += THREADS) order[e] = a.plan.order[first + s0 + e];
+            for (int e = threadIdx.x; e < seg; e += THREADS) order[e] = __ldcg(a.plan.order + first + s0 + e);
             __syncthreads();
             // the warp's steps of 16 rows: wa, wa + along, ...
             int next = wa, put = 0, get = 0;
