@@ -157,6 +157,10 @@ __device__ __forceinline__ void copy16(uint16_t *dst, const void *src, int bytes
     copy16((uint32_t)__cvta_generic_to_shared(dst), src, bytes);
 }
 
+// A value that is read before the wait (a.add), else after it.
+template <typename V>
+__device__ __forceinline__ V early(const Args &a, const V *p) { return a.add ? __ldcg(p) : *p; }
+
 // The pass's vectors from value k0 on into shared memory, xunits units of them: columns of xpitch values (the 64
 // bytes over put the eight columns of a tile into different banks), zero past K.
 __device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int tokens, int k0) {
@@ -173,7 +177,7 @@ __device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int
             } else {
                 uint16_t v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = i < left ? src[i] : (uint16_t)0;
+                for (int i = 0; i < 8; ++i) v[i] = i < left ? early(a, src + i) : (uint16_t)0;
                 *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16,
                                                              v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
             }
@@ -193,12 +197,12 @@ __device__ __forceinline__ void stage_x(const Args &a, uint16_t *xs, int t0, int
                 if (e >= all) continue;
                 const float *src = x + t * a.ldx + k;
                 if (wide && left >= 4) {
-                    v[u] = *reinterpret_cast<const float4 *>(src);
+                    v[u] = early(a, reinterpret_cast<const float4 *>(src));
                 } else {
-                    if (left > 0) v[u].x = src[0];
-                    if (left > 1) v[u].y = src[1];
-                    if (left > 2) v[u].z = src[2];
-                    if (left > 3) v[u].w = src[3];
+                    if (left > 0) v[u].x = early(a, src + 0);
+                    if (left > 1) v[u].y = early(a, src + 1);
+                    if (left > 2) v[u].z = early(a, src + 2);
+                    if (left > 3) v[u].w = early(a, src + 3);
                 }
             }
 #pragma unroll
@@ -232,7 +236,7 @@ __device__ __forceinline__ void stage_scales(const Args &a, uint16_t *ss, int ro
         } else {
             uint16_t v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = i < left ? src[i] : (uint16_t)0;
+            for (int i = 0; i < 8; ++i) v[i] = i < left ? early(a, src + i) : (uint16_t)0;
             *reinterpret_cast<uint4 *>(dst) = make_uint4(v[0] | (uint32_t)v[1] << 16, v[2] | (uint32_t)v[3] << 16,
                                                          v[4] | (uint32_t)v[5] << 16, v[6] | (uint32_t)v[7] << 16);
         }
@@ -249,7 +253,9 @@ constexpr int UNIT_BYTES = 2048;      // 16 rows x two blocks (128 bytes of a ro
 template <int NT, int FL>
 __global__ void __launch_bounds__(32 * WARPS, 2) matvec_kernel(Args a) {
     pdl_trigger();
-    if (!a.add) pdl_wait();            // what the kernel before this one wrote is needed at the end alone
+    // What the kernel before this one wrote (add) is needed at the end alone.  Until then x, codes and scales are read through
+    // L2, where they lay before that kernel let this one start: what an SM's own cache holds is certain to be new only after a wait.
+    if (!a.add) pdl_wait();
     constexpr int RING = ring_of(NT);
     extern __shared__ __align__(16) uint8_t smem[];
     uint16_t *xs = reinterpret_cast<uint16_t *>(smem), *ss = reinterpret_cast<uint16_t *>(smem + a.scale_at);
