@@ -311,21 +311,7 @@ __global__ void __launch_bounds__(THREADS, 1) narrow_kernel(const __grid_constan
                 Pool::read(d + 2 * MT * In::BYTES + j * Pool::BYTES, e, left,
                            (int)(reinterpret_cast<uintptr_t>(p1 + (int64_t)(8 * j + g) * a.D) & 15), 1, spare);
                 along(e, pp);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int l = 2; l >= 0; --l)                                 // the smallest products first
-#pragma unroll
-                        for (int q = 0; q <= l; ++q) {
-                            const int v = l - q;
-                            if (q >= PI || v >= PP) continue;
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) {
-                                const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
-                                                       xp[m][1][q][2 * s + 1]};
-                                mma16816(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
-                            }
-                        }
+                add_products<PI, PP>(xp, pp, [&](int m) { return acc[m][j]; });
             }
         }
         arrived<0>();
@@ -760,6 +746,11 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
                         uint32_t q0[PZ], q1[PZ];
                         across(v[0], v[1], i, q0);
                         across(v[2], v[3], i, q1);
+                        float sum[RT][4];                                // 16 rows, then to nearest into all rows' sums
+#pragma unroll
+                        for (int m = 0; m < RT; ++m)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) sum[m][k] = 0.0f;
 #pragma unroll
                         for (int l = 2; l >= 0; --l)
 #pragma unroll
@@ -767,8 +758,12 @@ __global__ void __launch_bounds__(THREADS, RT < 4 ? 2 : 1) grads_kernel(const __
                                 const int k = l - q;
                                 if (k >= PZ) continue;
 #pragma unroll
-                                for (int m = 0; m < RT; ++m) mma16816(acc[m][i], f[m][q], q0[k], q1[k]);
+                                for (int m = 0; m < RT; ++m) mma16816(sum[m], f[m][q], q0[k], q1[k]);
                             }
+#pragma unroll
+                        for (int m = 0; m < RT; ++m)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) acc[m][i][k] += sum[m][k];
                     }
                 }
                 __syncthreads();                                         // the parts have been read

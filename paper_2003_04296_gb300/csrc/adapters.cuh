@@ -99,6 +99,36 @@ __device__ __forceinline__ void store16(void *p, int64_t at, int left, bool vec,
     }
 }
 
+// acc(m) += 32 values along K of MT tiles of 16 rows times those of eight ranks, in parts, the smallest products first.  The tensor
+// cores truncate what they add to, so they start these from zero and the sums over K are added here, to nearest: a sum of one
+// sign loses no more the longer it gets.
+template <int PI, int PP, int MT, typename F>
+__device__ __forceinline__ void add_products(const uint32_t (&xp)[MT][2][PI][4], const uint32_t (&pp)[PP][4], F acc) {
+    float sum[MT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[m][i] = 0.0f;
+#pragma unroll
+    for (int l = 2; l >= 0; --l)
+#pragma unroll
+        for (int q = 0; q <= l; ++q) {
+            const int v = l - q;
+            if (q >= PI || v >= PP) continue;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1], xp[m][1][q][2 * s + 1]};
+                    mma16816(sum[m], f, pp[v][2 * s], pp[v][2 * s + 1]);
+                }
+        }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc(m)[i] += sum[m][i];
+}
+
 // The warps' sums, in their order: part[m][j], rows `pitch` apart.
 template <int MT, int NT>
 __device__ __forceinline__ void add_warps(float (*acc)[NT][4], float *red, float *part, int pitch, int ranks) {

@@ -59,21 +59,7 @@ __device__ __forceinline__ void narrow(const Args &a, const int *rows, int count
             for (int j = 0; j < NT; ++j) {
                 uint32_t pp[PP][4];
                 along(p[d][j], pp);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int l = 2; l >= 0; --l)                                 // the smallest products first
-#pragma unroll
-                        for (int q = 0; q <= l; ++q) {
-                            const int v = l - q;
-                            if (q >= PI || v >= PP) continue;
-#pragma unroll
-                            for (int m = 0; m < MT; ++m) {
-                                const uint32_t f[4] = {xp[m][0][q][2 * s], xp[m][1][q][2 * s], xp[m][0][q][2 * s + 1],
-                                                       xp[m][1][q][2 * s + 1]};
-                                mma16816(acc[m][j], f, pp[v][2 * s], pp[v][2 * s + 1]);
-                            }
-                        }
+                add_products<PI, PP>(xp, pp, [&](int m) { return acc[m][j]; });
             }
         }
     }
