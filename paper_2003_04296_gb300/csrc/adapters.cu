@@ -137,6 +137,7 @@ struct Way {
             }
         } else {
             const int64_t at = (int64_t)reinterpret_cast<uintptr_t>(p), first = at & ~(int64_t)15, end = at + (int64_t)left * (int)sizeof(V);
+            safe = reinterpret_cast<const void *>(reinterpret_cast<uintptr_t>(safe) & ~(uintptr_t)15);      // a copy of no bytes has to be aligned, too
 #pragma unroll
             for (int h = 0; h < C; ++h)
                 copy_fill(item + lane * 16 + 512 * h, first + 16 * h < end ? reinterpret_cast<const void *>(first + 16 * h) : safe,
