@@ -232,7 +232,7 @@ __device__ __forceinline__ void stage_scales(const Args &a, uint16_t *ss, int ro
         const uint16_t *src = a.scales + (int64_t)min(row0 + r, a.O - 1) * a.groups + g0 + k;
         uint16_t *dst = ss + 8 * e;
         if (wide) {
-            copy16(dst, left > 0 ? src : a.scales, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
+            copy16(dst, left > 0 ? src : a.scales + g0, left >= 8 ? 16 : left > 0 ? 2 * left : 0);
         } else {
             uint16_t v[8];
 #pragma unroll
