@@ -8,19 +8,28 @@
 //   Z = a I + b A + c A^2,   Q <- Z Q,   A <- (Z A) Z
 // and Q X comes once at the stage's end: for n >= m a third of the direct form's
 // operations, half of them on symmetric results whose other half is a mirror image.
-// What that costs is precision: an error e of A counts 11.9^steps e where the
-// singular values are small.  So every matrix is held as the sum of two fp16 numbers
-// (22 bits), a product takes three fp16 products, hi hi + hi lo + lo hi, and a stage has
-// three steps at most.  The tensor cores truncate their fp32 sums, so they add up hi hi over
-// 128 of K alone and fp32 registers the rest, to nearest.  Against the formula in 64 bits,
-// 1024 x 8192, a gradient of few strong directions (Frobenius): 1.3e-5, as near as plain fp32
-// products (1.5e-5); chunks of 256, 512 and all of K 2.4e-5, 3.2e-5 and 3.0e-5, of 64 7.5e-6
-// at 1.05 times the time; five steps in one stage 3e-3 to 9e-3.
+// What that costs is precision: an error e of A counts 11.9^steps e where the singular
+// values are small, and Q is up to 41 times what it leaves of strong directions.  So
+// - every matrix is held as the sum of two fp16 numbers (22 bits), and a product takes
+//   three fp16 products, lo hi + hi lo + hi hi;
+// - the tensor cores cut each addend at 2^-25 of the largest and what they add to, so they
+//   sum up 32 of K (pairs of blocks 64), and fp32 registers the rest, to nearest;
+// - Z and Q are held without their identity parts, Z = a I + W and Q = q I + R with q = a^steps:
+//     W = b A + c A^2,   Z A = a A + W A,   R <- q W + a R + W R,   Q X = q X + R X,
+//   and what the identity contributes is added in fp32, outside the truncated sums;
+// - all tiles of a matrix read a block of the diagonal the same way, else its roundings, which are
+//   not symmetric, do not cancel (600 x 700 of noise 7e-6 off instead of 2.5e-6);
+// - a stage has three steps at most (five: 3e-3 to 9e-3).
+// Against the formula in 64 bits (Frobenius; plain fp32 products in parentheses), noise / a gradient of few strong
+// directions: 128 x 1152 1.8e-6 / 1.8e-6 (1.2e-6 / 1.2e-6), 1024 x 8192 2.6e-6 / 1.2e-6 (3.9e-6 / 3.5e-6),
+// 4096 x 4096 2.2e-6 / 1.4e-6 (4.8e-6 / 6.6e-6).  Without all this but the stages, sums of 128 of K:
+// 8.7e-6 / 1.0e-5, 7.1e-6 / 5.4e-6 and 6.0e-6 / 5.0e-6, at 116 us instead of 130, 318 instead of 346,
+// 2.77 ms instead of 2.93.
 //
 // The scales are powers of two that the mathematics gives: a matrix of Frobenius norm
 // f in [1/2, 1) 2^e enters as X 2^(15 - e), so that nothing overflows and the smallest
 // part lost is 2^-40 of the norm; singular values stay below 1.2025 from then on,
-// A below 1.447, Z below 3.4446.
+// A below 1.447, W below 2.81, R below 3.4446^steps.
 //
 // Operands lie in the workspace as the tensor cores read them: blocks of 128 rows x 64
 // columns, 16 KB, swizzled in rows of 128 bytes.  Such a block is a K-major operand of
@@ -32,8 +41,8 @@
 // What bounds a level: where tiles are many, the way from L2 into the SMs (64 bytes a clock: 64 KB
 // for 64 of K, 0.55 to 0.67 us a tile of 128 x 128, of which the tensor cores need 0.4), so
 // pairs of blocks take 256 x 256; where they are few, latency (2.5 us between two launches, 4.5 for a
-// tile's start and end), so clusters split K.  4096 x 4096 2.64 ms (1.56 of the 1.88 PFLOP/s that
-// a library's bf16 product reaches), 1024 x 8192 290 us, 128 x 1152 111, 10 x 1024 10.
+// tile's start and end), so clusters split K.  4096 x 4096 of bf16 2.8 to 2.9 ms (1.4 of the 1.88
+// PFLOP/s that a library's bf16 product reaches), 1024 x 8192 of fp32 346 us, 128 x 1152 130, 10 x 1024 11.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -58,9 +67,9 @@ constexpr int T = 128;                       // rows and columns of a tile
 constexpr uint32_t BLOCK = 16384;            // bytes of 128 rows x 64 columns of fp16
 constexpr int THREADS = 256;
 constexpr int LOADER = 8, ISSUER = 9;        // a product's warps beside the eight that take its sums
-constexpr int CHUNK = 2;                     // blocks of 64 of K that the tensor cores sum by themselves
 constexpr int STAGES = 3;
 constexpr uint32_t STAGE = 4 * BLOCK;        // hi and lo of both operands, 64 of K
+constexpr int EARLY = 4;                     // steps of a tile's end, 16 rows each, whose added values are ready before the sums are
 constexpr int PITCH = 132;                   // floats between rows of a tile in shared memory
 constexpr int CAP = 224;                     // matrices of a launch
 constexpr int FEW = 16;                      // ... of a launch with short arguments
@@ -99,7 +108,7 @@ struct Mat {
 struct Sizes {
     int count, full;                         // matrices; tiles of X
     int pair_tri, pair_full;                 // clusters for pairs, four tiles each: of lower triangles, of X
-    bool pairs[4];                           // of each Kind, and of X: blocks work in pairs
+    bool pairs, pairs_x;                     // blocks work in pairs: in the levels on m x m results, in those on X
     int clusters[3], blocks[3];              // of each Kind, for one product: clusters, their blocks
     const Mat *table;                        // in the workspace
     Stat *stat;
@@ -110,6 +119,7 @@ template <int N>
 struct Table {
     Mat m[N];
 };
+static_assert(sizeof(Table<CAP>) + sizeof(Sizes) + 16 <= 32764, "a launch's arguments");
 template <>
 struct Table<0> {
     Mat *m = nullptr;
@@ -231,8 +241,8 @@ __global__ void __launch_bounds__(THREADS) squares_kernel(const __grid_constant_
     pdl_wait();
     pdl_trigger();
     __shared__ double red[THREADS / 32];
-    // the list's matrices into the workspace, where the kernels after this one find them (a launch with 23 KB of
-    // arguments takes the host three times as long)
+    // the list's matrices into the workspace, where the kernels after this one find them (a launch with all of
+    // a long list in its arguments takes the host three times as long)
     if (blockIdx.x == 0) {
         static_assert(sizeof(Mat) % 8 == 0, "whole words");
         const uint64_t *from = reinterpret_cast<const uint64_t *>(&table);
@@ -323,21 +333,22 @@ __device__ __forceinline__ float clipped(float w, float rate, float z, float lim
     return n > limit ? limit : n < -limit ? -limit : n;
 }
 
-enum Mode { GRAM, POLY, MUL, APPLY, LEAVE };
+enum Mode { GRAM, MUL, APPLY, LEAVE };
 
 struct Product {
-    int p, q, out;                           // slots of the factors and the result (LEAVE, APPLY: p = Q)
+    int p, q, out;                           // slots of the factors and the result (LEAVE, APPLY: p = R)
     float factor;                            // of the sum, on its way to the result's scale
+    int add[2];                              // slots of what is added to it, -1: none (LEAVE, APPLY: X) ...
+    float times[2];                          // ... so many times
 };
 
 struct Level {
     int mode, products, split;               // split: blocks of a cluster
-    int pair;                                // blocks work in pairs
+    int upper;                               // the m x m matrices were made by pairs
     Product pr[2];
     int later;                               // GRAM, APPLY, LEAVE: of a later stage than the first
     int x1;                                  // ... X is in x1 (every other stage; APPLY writes the other one)
     int x_lo;                                // ... and has a lo part
-    float a, b;                              // POLY: a I + b (slot p) + factor sum, in the result's scale
     int update;                              // LEAVE: weights are updated
     float lr;
     long long wait_cycles;
@@ -350,7 +361,7 @@ __device__ __forceinline__ void bar_init(uint64_t *b, uint32_t n) {
 __device__ __forceinline__ bool bar_try(uint64_t *b, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 100000;\n selp.u32 %0, 1, 0, p;\n}\n"
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
         : "=r"(ok)
         : "r"(su32(b)), "r"(parity)
         : "memory");
@@ -376,15 +387,19 @@ __device__ __forceinline__ uint64_t desc(uint32_t addr, bool mn) {
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(mn ? 8192u >> 4 : 1u) << 16) | ((uint64_t)(1024 >> 4) << 32) |
            ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
+// (By one thread, as are the commits.)
+__device__ __forceinline__ bool elected() {
+    uint32_t e;
+    asm volatile("{\n .reg .pred p;\n .reg .b32 r;\n elect.sync r|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(e));
+    return e != 0;
+}
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p, e;\n .reg .b32 r;\n setp.ne.b32 p, %4, 0;\n elect.sync r|e, 0xffffffff;\n"
-                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
                  "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
 }
 __device__ __forceinline__ void mma_commit(uint64_t *bar) {
-    asm volatile("{\n .reg .pred e;\n .reg .b32 r;\n elect.sync r|e, 0xffffffff;\n"
-                 " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(su32(bar))
-                 : "memory");
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n" ::"r"(su32(bar)) : "memory");
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const uint8_t *src, uint32_t bytes, uint64_t *bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst),
@@ -399,9 +414,12 @@ struct Side {
     int64_t lo;
     int wide, tile;
     bool mn, sym;
-    int pair = 0;                            // 1: tiles 2 p and 2 p + 1 are read the same way (a block on the diagonal either way)
+    // PAIR: tiles 2 p and 2 p + 1 are read the same way, from 2 p + 2 on as mirror images; levels of pairs leave tile (2 p, 2 p + 1) for
+    // that.  Without it (APPLY and LEAVE after levels without pairs) from 2 p + 1 on: a block on the diagonal is its mirror image then.
+    // (So in all levels, its own roundings count: 600 x 700 of noise 7e-6 off instead of 2.4e-6.)
+    int last = -1;                           // the last tile that is read as it lies, -1: `tile`
 
-    __device__ __forceinline__ bool turned(int kb) const { return sym ? (kb >> 1) > (tile & ~pair) : mn; }
+    __device__ __forceinline__ bool turned(int kb) const { return sym ? (kb >> 1) > (last < 0 ? tile : last) : mn; }
     __device__ __forceinline__ void load(uint32_t dst, int kb, uint64_t *bar) const {
         if (!turned(kb)) {
             const uint8_t *s = p + ((int64_t)tile * wide + kb) * BLOCK;
@@ -421,20 +439,19 @@ struct Side {
 };
 
 struct Smem {
-    uint64_t full[STAGES], empty[STAGES], peer[STAGES], sums[2], taken[2];
+    uint64_t full[STAGES], empty[STAGES], peer[STAGES], sums[4], taken[4];
     uint32_t tmem;
 };
 
 // Pairs: the even block of a cluster of two issues products of 256 rows for both, each block's rows from its own shared memory, half
 // of the second operand from each.
 __device__ __forceinline__ void mma_f16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n .reg .pred p, e;\n .reg .b32 r;\n setp.ne.b32 p, %4, 0;\n elect.sync r|e, 0xffffffff;\n"
-                 " @e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+                 " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
                  "l"(a), "l"(b), "r"(idesc), "r"(accumulate));
 }
 __device__ __forceinline__ void mma_commit_pair(uint64_t *bar) {
-    asm volatile("{\n .reg .pred e;\n .reg .b32 r;\n elect.sync r|e, 0xffffffff;\n"
-                 " @e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}\n" ::"r"(su32(bar)),
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n" ::"r"(su32(bar)),
                  "h"((uint16_t)3)
                  : "memory");
 }
@@ -448,8 +465,7 @@ __device__ __forceinline__ void arrive_even(uint64_t *bar) {
     else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(at) : "memory");
 }
 
-__device__ __forceinline__ void load32(uint32_t addr, float *v) {
-    uint32_t w[32];
+__device__ __forceinline__ void load32(uint32_t addr, uint32_t *w) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, "
         "%13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, "
@@ -460,16 +476,25 @@ __device__ __forceinline__ void load32(uint32_t addr, float *v) {
           "=r"(w[22]), "=r"(w[23]), "=r"(w[24]), "=r"(w[25]), "=r"(w[26]), "=r"(w[27]), "=r"(w[28]),
           "=r"(w[29]), "=r"(w[30]), "=r"(w[31])
         : "r"(addr));
+}
+// sum += 64 columns.
+__device__ __forceinline__ void add64(uint32_t addr, float *sum) {
+    uint32_t w[64];
+    load32(addr, w);
+    load32(addr + 32, w + 32);
     asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
+    // (what was loaded is there from here on alone)
 #pragma unroll
-    for (int k = 0; k < 32; ++k) v[k] = __uint_as_float(w[k]);
+    for (int k = 0; k < 64; ++k) asm volatile("" : "+r"(w[k]));
+#pragma unroll
+    for (int k = 0; k < 64; ++k) sum[k] += __uint_as_float(w[k]);
 }
 
 // PAIR: four tiles by a cluster of two blocks, 256 x 256 sums, whose products read 64 KB a block for 64 of K where four blocks
-// by themselves read as much each: it is the way from L2 that products wait for.  Both parts' products go into one sum (two of
-// 256 columns fill the tensor memory), which registers take over after 128 of K.  4096 x 4096: 2.64 ms, 3.18 without pairs;
-// sums taken over after 64 of K 1.33 times that, after 256 0.98 times at 1.7 times the error.  (Pairs on 256 x 128, half of the second operand
-// in each block: 4.26, products of 128 columns take as long as of 256.)
+// by themselves read as much each: it is the way from L2 that products wait for.  Two sums of 256 columns fill the tensor memory;
+// registers take them over after 64 of K: 4096 x 4096 in 2.92 ms, after 32 in 3.02, after 128 in 2.88 at 1.4 times the error (noise).
+// A tile for itself has four sums of 128 columns, each of 32 of K: 512 x 512 in 192 us, of 64 in 176 at 1.15 times the error, and wide
+// matrices of noise at 1.5 to 1.7 times it.
 // N: matrices whose descriptions come with the launch, so that a block knows its work before it waits for the kernel before; 0:
 // they are read from the workspace, after that wait (what an earlier kernel wrote is there for certain only then).
 template <bool PAIR, int N>
@@ -477,6 +502,11 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
                                                                   const __grid_constant__ Table<N> own) {
     constexpr int WIDTH = PAIR ? 2 * T : T;          // columns of a block's tile
     constexpr int MINE = PAIR ? 128 : 64;                       // ... of a thread
+    constexpr int SUMS = 512 / WIDTH;                           // sums in tensor memory
+    constexpr int SPAN = PAIR ? 64 : 32;                        // of K that the tensor cores sum by themselves
+    constexpr int ADDED = PAIR ? 3 : 4;                         // steps of the end whose values are on their way at a time
+    static_assert((PAIR ? 2 * T * PITCH * 4 : (STAGES - 1) * STAGE) + ADDED * 4 * THREADS * 16 <= STAGES * STAGE, "in the ring");
+    static_assert(STAGES == 3 && T * PITCH * 4 <= (STAGES - 1) * STAGE, "behind the sums");
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *ring = smem_raw + ((1024u - (su32(smem_raw) & 1023u)) & 1023u);
     float *acc = reinterpret_cast<float *>(ring);               // the tile, once the ring is done with
@@ -488,7 +518,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
             bar_init(&sm.empty[s], 1);
             bar_init(&sm.peer[s], 1);
         }
-        for (int k = 0; k < 2; ++k) {
+        for (int k = 0; k < SUMS; ++k) {
             bar_init(&sm.sums[k], 1);
             bar_init(&sm.taken[k], (PAIR ? 2 : 1) * THREADS / 32);
         }
@@ -587,8 +617,9 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         }
     }
     if (PAIR) {
-        a.pair = b.pair = 1;
         b.tile = min(j + in_cluster, columns - 1);
+        a.last = v.upper ? a.tile | 1 : a.tile & ~1;
+        b.last = v.upper ? b.tile | 1 : b.tile & ~1;
     }
     const int kb0 = idle ? 0 : rank * kbs / shares, kb1 = idle ? 0 : (rank + 1) * kbs / shares;
     const bool same = !PAIR && a.p == b.p && a.tile == b.tile && a.mn == b.mn && a.sym == b.sym;
@@ -603,13 +634,89 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
                 asm volatile("prefetch.global.L2 [%0];" ::"l"(static_cast<const uint8_t *>(m.out) + (r * m.ldo + c) * (m.o_bf16 ? 2 : 4)));
         }
     }
+    // what is added to the sums: values of two slots, or of X
+    const Stat st = v.mode != MUL ? l.stat[index] : Stat{};
+    const int wide = tri ? 2 * mb : 2 * m.cb(), rows = T / shares, r0 = rank * rows, c = (threadIdx.x & 15) * 8;
+    const int64_t lo = tri ? small_blocks : x_blocks;
+    // ... 16 rows of this block's share of a tile at a time, eight columns a thread
+    const int steps = mute || idle || warp >= THREADS / 32 ? 0 : PAIR && j + 1 < columns ? T / 8 : rows / 16;
+    auto row_of = [&](int step) { return r0 + (PAIR ? step % (T / 16) : step) * 16 + (int)(threadIdx.x >> 4); };
+    auto tile_of = [&](int step) { return PAIR ? j + step / (T / 16) : j; };
+    auto place = [&](int step) {
+        return ((int64_t)i * wide + 2 * tile_of(step) + (c >> 6)) * BLOCK + at(row_of(step), c & 63);
+    };
+    const uint8_t *from[2] = {nullptr, nullptr};
+    int64_t from_lo = small_blocks;
+    float times[2] = {pr.times[0], pr.times[1]};
+    if (v.mode == MUL) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (pr.add[e] >= 0) from[e] = m.small + pr.add[e] * slot;
+    } else if (!tri) {
+        from[0] = x;
+        from_lo = v.x_lo ? x_blocks : 0;
+        if (!v.later) times[0] *= st.apply;
+    }
+    // eight values of them, as their parts lie at w
+    auto sum_of = [&](const uint4 (*w)[2], float *f) {
+        join8(w[0][0], w[0][1], f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] *= times[0];
+        if (from[1]) {
+            float g[8];
+            join8(w[1][0], w[1][1], g);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) f[k] = fmaf(times[1], g[k], f[k]);
+        }
+    };
+    // The first steps' while the tensor cores are busy, into shared memory behind the ring (all of them at the end, as they were loaded: 2 us
+    // of a level's 10); a thread reads back its own.
+    float4 *early = reinterpret_cast<float4 *>(ring + STAGES * STAGE) + threadIdx.x;
+    if (from[0]) {
+#pragma unroll 2
+        for (int step = 0; step < min(steps, EARLY); ++step) {
+            uint4 w[2][2] = {};
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (from[e]) {
+                    w[e][0] = *reinterpret_cast<const uint4 *>(from[e] + place(step));
+                    if (from_lo) w[e][1] = *reinterpret_cast<const uint4 *>(from[e] + place(step) + from_lo);
+                }
+            float f[8];
+            sum_of(w, f);
+            early[2 * step * THREADS] = make_float4(f[0], f[1], f[2], f[3]);
+            early[(2 * step + 1) * THREADS] = make_float4(f[4], f[5], f[6], f[7]);
+        }
+    }
+    // The later steps' as they lie, on their way to shared memory behind the sums.  That is the ring's last stage (of pairs: part of
+    // it), which the third last block of K leaves for good, for the stages are taken so.
+    const int off = PAIR ? 0 : 2 - (kb1 - kb0) % 3;
+    auto stage = [&](int s) { return (uint32_t)((s + off) % STAGES) * STAGE; };
+    uint8_t *added = ring + (PAIR ? 2 * T * PITCH * 4 : (STAGES - 1) * (int)STAGE) + threadIdx.x * 16;
+    auto fetch = [&](int step) {
+        if (step < steps) {
+            uint8_t *d = added + step % ADDED * (4 * THREADS * 16);
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (from[e]) {
+                    copy_async<16>(d + 2 * e * THREADS * 16, from[e] + place(step));
+                    if (from_lo) copy_async<16>(d + (2 * e + 1) * THREADS * 16, from[e] + place(step) + from_lo);
+                }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto fetch_later = [&]() {
+        if (steps > EARLY && from[0])
+#pragma unroll 1
+            for (int step = EARLY; step < EARLY + ADDED; ++step) fetch(step);
+    };
     bool ok = true;
     if (warp == LOADER) {
         if (lane == 0) {
             int s = 0, lap = 0, g = 0;
             for (int kb = kb0; kb < kb1; ++kb, ++g) {
                 if (lap > 0 && !bar_wait(&sm.empty[s], (lap - 1) & 1, v.wait_cycles)) break;
-                const uint32_t dst = su32(ring) + s * STAGE;
+                const uint32_t dst = su32(ring) + stage(s);
                 asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n" ::"r"(su32(&sm.full[s])),
                              "r"(bytes)
                              : "memory");
@@ -632,50 +739,50 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         }
     } else if (warp == ISSUER) {
         // D fp32, A and B fp16; bits 15 and 16: MN-major
-        int s = 0, chunk = 0;
-        uint32_t phase = 0u, rest = 0u;
-        for (int at_ = kb0; at_ < kb1 && ok; at_ += CHUNK, ++chunk) {
-            const int end = min(at_ + CHUNK, kb1);
-            if (chunk >= 2 && !__all_sync(0xffffffffu, bar_wait(&sm.taken[chunk & 1], (chunk / 2 - 1) & 1, v.wait_cycles)))
-                ok = false;
-            fence_after();
-            const uint32_t d = tmem + WIDTH * (chunk & 1), small = PAIR ? d : tmem + 2 * T;
-            if (PAIR) rest = 1u;
-            uint32_t on = 0u;
-            for (int kb = at_; kb < end && ok; ++kb) {
-                if (!__all_sync(0xffffffffu, bar_wait(&sm.full[s], phase, v.wait_cycles))) { ok = false; break; }
-                if (PAIR && !__all_sync(0xffffffffu, bar_wait(&sm.peer[s], phase, v.wait_cycles))) { ok = false; break; }
-                fence_after();
-                const uint32_t base = su32(ring) + s * STAGE;
-                const bool at = a.turned(kb), bt = b.turned(kb);
-                const uint32_t idesc = (1u << 4) | ((at ? 1u : 0u) << 15) | ((bt ? 1u : 0u) << 16) | ((uint32_t)(WIDTH >> 3) << 17) | ((PAIR ? 16u : 8u) << 24);
-                const uint32_t ka = at ? 2048 >> 4 : 32 >> 4, kbk = bt ? 2048 >> 4 : 32 >> 4;  // 16 of K
-                const uint64_t ad = desc(base, at), bd = desc(same ? base : base + 2 * BLOCK, bt);
-                auto four = [&](uint32_t to, uint64_t x_, uint64_t y_, uint32_t first) {
+        int s = 0, sum = 0;
+        uint32_t phase = 0u;
+        const bool leader = elected();
+        for (int kb = kb0; kb < kb1; ++kb) {
+            ok = bar_wait(&sm.full[s], phase, v.wait_cycles);
+            if (PAIR) ok = ok && bar_wait(&sm.peer[s], phase, v.wait_cycles);
+            const uint32_t base = su32(ring) + stage(s);
+            const bool at = a.turned(kb), bt = b.turned(kb);
+            const uint32_t idesc = (1u << 4) | ((at ? 1u : 0u) << 15) | ((bt ? 1u : 0u) << 16) | ((uint32_t)(WIDTH >> 3) << 17) | ((PAIR ? 16u : 8u) << 24);
+            const uint32_t ka = at ? 2048 >> 4 : 32 >> 4, kbk = bt ? 2048 >> 4 : 32 >> 4;      // 16 of K
+            const uint64_t ad = desc(base, at), bd = desc(same ? base : base + 2 * BLOCK, bt);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if constexpr (PAIR) mma_f16_pair(to, x_ + k * ka, y_ + k * kbk, idesc, k > 0 ? 1u : first);
-                        else mma_f16(to, x_ + k * ka, y_ + k * kbk, idesc, k > 0 ? 1u : first);
-                    }
-                };
-                four(d, ad, bd, on);
-                on = 1u;
-                if (b.lo) {
-                    four(small, ad, bd + (BLOCK >> 4), rest);
-                    rest = 1u;
+            for (int half = 0; half < 64 / SPAN; ++half, ++sum) {
+                if (sum >= SUMS) ok = ok && bar_wait(&sm.taken[sum % SUMS], (sum / SUMS - 1) & 1, v.wait_cycles);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                fence_after();
+                if (leader) {
+                    const uint32_t d = WIDTH * (sum % SUMS);    // (all columns are this block's: they begin at 0)
+                    uint32_t on = 0u;
+                    auto add = [&](uint64_t x_, uint64_t y_) {
+#pragma unroll
+                        for (int k = half * SPAN / 16; k < (half + 1) * SPAN / 16; ++k) {
+                            if constexpr (PAIR) mma_f16_pair(d, x_ + k * ka, y_ + k * kbk, idesc, on);
+                            else mma_f16(d, x_ + k * ka, y_ + k * kbk, idesc, on);
+                            on = 1u;
+                        }
+                    };
+                    // the small products first: less is cut off them, and off the others by theirs
+                    if (b.lo) add(ad, bd + (BLOCK >> 4));
+                    if (a.lo) add(ad + (BLOCK >> 4), bd);
+                    add(ad, bd);
+                    if constexpr (PAIR) mma_commit_pair(&sm.sums[sum % SUMS]);
+                    else mma_commit(&sm.sums[sum % SUMS]);
                 }
-                if (a.lo) {
-                    four(small, ad + (BLOCK >> 4), bd, rest);
-                    rest = 1u;
-                }
+                __syncwarp();
+            }
+            if (!ok) break;
+            if (leader) {
                 if constexpr (PAIR) mma_commit_pair(&sm.empty[s]);
                 else mma_commit(&sm.empty[s]);
-                if (++s == STAGES) { s = 0; phase ^= 1u; }
             }
-            if (ok) {
-                if constexpr (PAIR) mma_commit_pair(&sm.sums[chunk & 1]);
-                else mma_commit(&sm.sums[chunk & 1]);
-            }
+            __syncwarp();
+            if (++s == STAGES) { s = 0; phase ^= 1u; }
         }
     }
     __syncwarp();
@@ -685,38 +792,27 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     if (warp < THREADS / 32) {
 #pragma unroll
         for (int k = 0; k < MINE; ++k) sum[k] = 0.0f;
-        int chunk = 0;
-        for (int at_ = kb0; at_ < kb1 && ok; at_ += CHUNK, ++chunk) {
-            ok = __all_sync(0xffffffffu, bar_wait(&sm.sums[chunk & 1], (chunk >> 1) & 1, v.wait_cycles));
+        const int sums = (kb1 - kb0) * (64 / SPAN);
+        const int left = PAIR ? -2 : max((kb1 - kb0 - 2) * (64 / SPAN) - 1, -1);         // the sum after which the last stage is free (-1: at once)
+        if (left == -1) fetch_later();
+        for (int e = 0; e < sums && ok; ++e) {
+            ok = __all_sync(0xffffffffu, bar_wait(&sm.sums[e % SUMS], (e / SUMS) & 1, v.wait_cycles));
             fence_after();
+            if (e == left) fetch_later();
 #pragma unroll
-            for (int c = 0; c < MINE; c += 32) {
-                float w[32];
-                load32(mine + WIDTH * (chunk & 1) + c, w);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) sum[c + k] += w[k];
-            }
+            for (int c = 0; c < MINE; c += 64) add64(mine + WIDTH * (e % SUMS) + c, sum + c);
             fence_before();
             __syncwarp();
             if (lane == 0) {
-                if constexpr (PAIR) arrive_even<true>(&sm.taken[chunk & 1]);
-                else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(su32(&sm.taken[chunk & 1])) : "memory");
-            }
-        }
-        if (!PAIR && kb1 > kb0 && (a.lo || b.lo)) {
-#pragma unroll
-            for (int c = 0; c < MINE; c += 32) {
-                float w[32];
-                load32(mine + 2 * T + c, w);
-#pragma unroll
-                for (int k = 0; k < 32; ++k) sum[c + k] += w[k];
+                if constexpr (PAIR) arrive_even<true>(&sm.taken[e % SUMS]);
+                else asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];\n" ::"r"(su32(&sm.taken[e % SUMS])) : "memory");
             }
         }
     }
     ok = __syncthreads_and(ok);                                 // and the last loads have landed
     // Rows of the tile that this block finishes.  The other blocks' sums for them arrive in its shared memory, a share after the
     // other, once all are done with their rings (reading them from here instead takes 2 us more: their way is there twice).
-    const int rows = T / shares, r0 = rank * rows;
+    if constexpr (PAIR) fetch_later();
     if (split > 1 && !PAIR) cluster.sync();
     if (warp < THREADS / 32 && !idle) {
         const int r = (warp & 3) * 32 + lane, owner = r / rows;
@@ -727,55 +823,60 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     }
     if (split > 1 && !PAIR) cluster.sync();
     else __syncthreads();
-    if (mute) idle = true;
 
-    // eight columns a thread at a time
-    const Stat st = v.mode == GRAM || v.mode == LEAVE || v.mode == APPLY ? l.stat[index] : Stat{};
     float factor = pr.factor;
     if (v.mode == GRAM && !v.later) factor *= st.gram;
     if (v.mode >= APPLY && !v.later) factor *= st.apply;
     // (tiles of Q X still read X where others are done: never into the X that this launch reads)
     uint8_t *out = v.mode == APPLY ? (v.x1 ? m.x0 : m.x1) : m.small + pr.out * slot;
-    const int wide = v.mode == APPLY ? 2 * m.cb() : 2 * mb;
-    const int64_t lo = v.mode == APPLY ? x_blocks : small_blocks;
-    const int c = (threadIdx.x & 15) * 8;
-    for (int tile = 0; tile < (PAIR ? 2 : 1); ++tile, ++j, acc += T * PITCH)
-    for (int r = r0 + (threadIdx.x >> 4); r < r0 + rows && warp < THREADS / 32 && !idle && (!PAIR || (j < columns && (!tri || j <= i))); r += 16) {
+#pragma unroll 1
+    for (int step = 0; step < steps; ++step) {
+        const int r = row_of(step), jt = tile_of(step);
+        const float *mine_ = acc + ((jt - j) * T + r - r0) * PITCH + c;
         float z[8];
 #pragma unroll
         for (int k = 0; k < 8; k += 4) {
-            const float *share = acc + (r - r0) * PITCH + c + k;
-            float4 f = *reinterpret_cast<const float4 *>(share);
+            float4 y = *reinterpret_cast<const float4 *>(mine_ + k);
             for (int p = 1; p < shares; ++p) {
-                const float4 o = *reinterpret_cast<const float4 *>(share + p * rows * PITCH);
-                f.x += o.x; f.y += o.y; f.z += o.z; f.w += o.w;
+                const float4 o = *reinterpret_cast<const float4 *>(mine_ + k + p * rows * PITCH);
+                y.x += o.x; y.y += o.y; y.z += o.z; y.w += o.w;
             }
-            z[k] = f.x; z[k + 1] = f.y; z[k + 2] = f.z; z[k + 3] = f.w;
+            z[k] = y.x; z[k + 1] = y.y; z[k + 2] = y.z; z[k + 3] = y.w;
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k) z[k] *= factor;
-        const uint32_t in_block = at(r, c & 63);
-        if (v.mode == POLY) {
-            const uint8_t *s = m.small + pr.p * slot + ((int64_t)i * wide + 2 * j + (c >> 6)) * BLOCK + in_block;
+        if (from[0]) {
             float f[8];
-            join8(*reinterpret_cast<const uint4 *>(s), *reinterpret_cast<const uint4 *>(s + small_blocks), f);
+            if (step < EARLY) {
+                *reinterpret_cast<float4 *>(f) = early[2 * step * THREADS];
+                *reinterpret_cast<float4 *>(f + 4) = early[(2 * step + 1) * THREADS];
+            } else {
+                asm volatile("cp.async.wait_group %0;" ::"n"(PAIR ? ADDED - 1 : 0) : "memory");
+                const uint4 *d = reinterpret_cast<const uint4 *>(added + step % ADDED * (4 * THREADS * 16));
+                uint4 w[2][2] = {};
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                z[k] = fmaf(v.b, f[k], z[k]);
-                if (i * T + r == j * T + c + k) z[k] += v.a;
+                for (int e = 0; e < 2; ++e)
+                    if (from[e]) {
+                        w[e][0] = d[2 * e * THREADS];
+                        if (from_lo) w[e][1] = d[(2 * e + 1) * THREADS];
+                    }
+                sum_of(w, f);
+                if (PAIR) fetch(step + ADDED);
             }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) z[k] += f[k];
         }
         if (v.mode != LEAVE) {
             if (ok) {
                 uint4 h, w;
                 split8(z, h, w);
-                uint8_t *d = out + ((int64_t)i * wide + 2 * j + (c >> 6)) * BLOCK + in_block;
+                uint8_t *d = out + place(step);
                 *reinterpret_cast<uint4 *>(d) = h;
                 *reinterpret_cast<uint4 *>(d + lo) = w;
             }
         } else if (ok && i * T + r < m.rows) {
-            const int64_t e = (int64_t)(i * T + r) * m.ldo + j * T + c;
-            const int left = m.cols - j * T - c;
+            const int64_t e = (int64_t)(i * T + r) * m.ldo + jt * T + c;
+            const int left = m.cols - jt * T - c;
             if (v.update) {
                 if (!st.finite) continue;
                 float w[8];
@@ -852,6 +953,14 @@ __device__ __forceinline__ void mma_parts(float *c, const uint32_t (*a)[4], cons
         for (int q = 0; q <= l; ++q) mma16816(c, a[q], b0[l - q], b1[l - q]);
 }
 
+// c += them, to nearest: the tensor cores cut what they add to, so they start from zero.
+__device__ __forceinline__ void add_parts(float *c, const uint32_t (*a)[4], const uint32_t *b0, const uint32_t *b1) {
+    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    mma_parts(sum, a, b0, b1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) c[k] += sum[k];
+}
+
 // out = factor P Q + b P + a I for m x m matrices in shared memory, Q symmetric.
 template <int MT>
 __device__ __forceinline__ void small_product(const float *P, const float *Q, float *out, int pitch, float factor, float b, float a) {
@@ -880,7 +989,7 @@ __device__ __forceinline__ void small_product(const float *P, const float *Q, fl
                 uint32_t b0[3], b1[3];
                 parts_at(Q + (j0 + 8 * e + g) * pitch + k + 2 * t, b0);
                 parts_at(Q + (j0 + 8 * e + g) * pitch + k + 2 * t + 8, b1);
-                mma_parts(c[e], f, b0, b1);
+                add_parts(c[e], f, b0, b1);
             }
         }
 #pragma unroll
@@ -936,7 +1045,7 @@ __device__ __forceinline__ void small_gram(const cg::cluster_group &cluster, con
                     uint32_t b0[3], b1[3];
 #pragma unroll
                     for (int q = 0; q < 3; ++q) { b0[q] = p[j][q][2 * s]; b1[q] = p[j][q][2 * s + 1]; }
-                    mma_parts(c[i][j], f, b0, b1);
+                    add_parts(c[i][j], f, b0, b1);
                 }
             }
     }
@@ -1025,7 +1134,7 @@ __device__ __forceinline__ void small_apply(float *X, const Small &z, const floa
                     split2(at_(0), at_(1), b0);
                     split2(at_(2), at_(3), b1);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) mma_parts(c[i][j0 + j], f[i], b0, b1);
+                    for (int i = 0; i < MT; ++i) add_parts(c[i][j0 + j], f[i], b0, b1);
                 }
             }
         }
@@ -1322,9 +1431,10 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
     // a pair's block of 64 of K takes 0.85 us, its tiles' start and end 7; those of a tile where there are several a block, 0.62 and 5
     const int sms = num_sms() > 0 ? num_sms() : 152;
     auto pairs = [&](int64_t clusters, int k) { return (2 * clusters + sms - 1) / sms * (0.85f * k + 7.0f); };
-    for (const Kind kind : {OF_X, ONE, TWO})
-        l.pairs[kind] = pairs((kind == TWO ? 2 : 1) * (int64_t)l.pair_tri, kind == OF_X ? long_k : small_k) < shares(table, l, kind);
-    l.pairs[3] = pairs(l.pair_full, small_k) < (l.full + sms - 1) / sms * (0.62f * small_k + 5.0f);
+    // (five steps: 2 Gram levels, 12 of one product, one of two)
+    const float of_x = shares(table, l, OF_X), one = shares(table, l, ONE), two = shares(table, l, TWO);
+    l.pairs = 2 * pairs(l.pair_tri, long_k) + 12 * pairs(l.pair_tri, small_k) + pairs(2 * (int64_t)l.pair_tri, small_k) < 2 * of_x + 12 * one + two;
+    l.pairs_x = pairs(l.pair_full, small_k) < (l.full + sms - 1) / sms * (0.62f * small_k + 5.0f);
     *need = used;
     return k;
 }
@@ -1355,12 +1465,13 @@ static cudaError_t launch(const Sizes &l, Level v, const Table<N> &own, cudaStre
     const Kind kind = v.mode == GRAM ? OF_X : v.products == 1 ? ONE : TWO;
     const bool tri = v.mode <= MUL;
     const int64_t pairs = tri ? (int64_t)l.pair_tri * v.products : l.pair_full;
-    v.pair = l.pairs[tri ? kind : 3];
-    v.split = v.pair ? 2 : tri ? l.blocks[kind] : 1;
-    const int64_t clusters = v.pair ? pairs : tri ? (int64_t)l.clusters[kind] * v.products : l.full;
+    const bool pair = tri ? l.pairs : l.pairs_x;
+    v.upper = l.pairs;
+    v.split = pair ? 2 : tri ? l.blocks[kind] : 1;
+    const int64_t clusters = pair ? pairs : tri ? (int64_t)l.clusters[kind] * v.products : l.full;
     v.wait_cycles = (long long)plan_options().wait_cycles;
-    auto kern = v.pair ? product_kernel<true, N> : product_kernel<false, N>;
-    const int smem = STAGES * (int)STAGE + 1024;                // (as much for pairs)
+    auto kern = pair ? product_kernel<true, N> : product_kernel<false, N>;
+    const int smem = STAGES * (int)STAGE + EARLY * 2 * THREADS * 16 + 1024;                               // (as much for pairs)
     if (!allow_shared(reinterpret_cast<const void *>(kern), smem)) return cudaErrorInvalidValue;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * v.split));
@@ -1388,42 +1499,44 @@ static minw_status chain(const Table<M> &table, const Table<N> &own, const Sizes
     if (launch_pdl_stream(false, enter_kernel, tiles, dim3(THREADS), 0, s, l, step, x_lo ? 1 : 0) !=
         cudaSuccess)
         return launch_failed();
-    // powers of two at which the m x m matrices are held: A, Z A below 1.447, Z below 3.4446, Q after k steps below 3.4446^k
-    const int SA = 15, SZ = 14;
-    static const int SQ[4] = {0, 14, 12, 10};
+    // powers of two at which the m x m matrices are held: A, Z A below 1.447, W below 2.81, R after k steps below 3.4446^k
+    const int SA = 15, SW = 14;
+    static const int SR[4] = {0, 14, 12, 10};
     auto two = [](int e) { return ldexpf(1.0f, e); };
     const int stages = (steps + 2) / 3;
     for (int st = 0, left = steps; st < stages; ++st) {
         const int n = (left + stages - st - 1) / (stages - st);                       // 3 + 2 of five
         left -= n;
         const bool last = st + 1 == stages;
-        int A = 0, Q = -1;
+        int A = 0, R = -1;
+        float q = CA;                                                                 // Q = q I + R
         Level v{};
         v.later = st > 0;
         v.x1 = st & 1;
         v.x_lo = st > 0 || x_lo;
         v.mode = GRAM;
         v.products = 1;
-        v.pr[0] = {0, 0, A, two(SA - 30)};
+        v.pr[0] = {0, 0, A, two(SA - 30), {-1, -1}, {}};
         if (launch(l, v, own, s) != cudaSuccess) return launch_failed();
         for (int k = 1; k <= n; ++k) {
-            const int Z = k == 1 ? 4 : 2;                                             // the first Z is Q
+            const int W = k == 1 ? 4 : 2;                                             // the first W is R
             Level p{};
-            p.mode = POLY;
+            p.mode = MUL;
             p.products = 1;
-            p.pr[0] = {A, A, Z, CC * two(SZ - 2 * SA)};
-            p.a = CA * two(SZ);
-            p.b = CB * two(SZ - SA);
+            p.pr[0] = {A, A, W, CC * two(SW - 2 * SA), {A, -1}, {CB * two(SW - SA), 0.0f}};
             if (launch(l, p, own, s) != cudaSuccess) return launch_failed();
             Level w{};
             w.mode = MUL;
-            if (k < n) w.pr[w.products++] = {Z, A, 3, two(-SZ)};                      // Z A
-            if (k > 1) w.pr[w.products++] = {Z, Q, Q ^ 1, two(SQ[k] - SZ - SQ[k - 1])};
-            Q = k == 1 ? 4 : Q ^ 1;
+            if (k < n) w.pr[w.products++] = {W, A, 3, two(-SW), {A, -1}, {CA, 0.0f}};                     // Z A = W A + a A
+            if (k > 1) {                                                              // Z Q = W R + a R + q W, and a q I
+                w.pr[w.products++] = {W, R, R ^ 1, two(SR[k] - SW - SR[k - 1]), {R, W}, {CA * two(SR[k] - SR[k - 1]), q * two(SR[k] - SW)}};
+                q *= CA;
+            }
+            R = k == 1 ? 4 : R ^ 1;
             if (w.products > 0 && launch(l, w, own, s) != cudaSuccess) return launch_failed();
             if (k < n) {
                 w.products = 1;
-                w.pr[0] = {3, Z, A ^ 1, two(-SZ)};
+                w.pr[0] = {3, W, A ^ 1, two(-SW), {3, -1}, {CA, 0.0f}};               // (Z A) Z
                 if (launch(l, w, own, s) != cudaSuccess) return launch_failed();
                 A ^= 1;
             }
@@ -1436,7 +1549,7 @@ static minw_status chain(const Table<M> &table, const Table<N> &own, const Sizes
         e.x_lo = st > 0 || x_lo;
         e.update = update;
         e.lr = lr;
-        e.pr[0] = {Q, Q, 0, two((last ? 0 : 15) - SQ[n] - 15)};
+        e.pr[0] = {R, R, 0, two((last ? 0 : 15) - SR[n] - 15), {-1, -1}, {q * two(last ? -15 : 0), 0.0f}};
         if (launch(l, e, own, s) != cudaSuccess) return launch_failed();
     }
     return launch_status();
