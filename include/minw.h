@@ -681,7 +681,8 @@ typedef struct {
  * grads, out: host arrays of count, read during the call; out has the
  * gradients' rows and cols, any type and ld, and may be its gradient (same
  * type and ld), but may overlap no other tensor.  workspace: device scratch of
- * minw_orthogonal_workspace_bytes(grads, count) (rows and cols count; about 28
+ * minw_orthogonal_workspace_bytes(grads, count) (rows and cols count; 0 for
+ * lists that a call refuses, so data has to be set, but is not read; about 28
  * bytes a value of a square matrix, 8 to 16 of a long one, its sides
  * rounded up to 128), 16-byte aligned, contents meaningless before and after;
  * calls that share one must not run concurrently.  count = 0 does nothing.

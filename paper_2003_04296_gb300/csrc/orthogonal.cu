@@ -1358,7 +1358,8 @@ static float shares(Mat *table, Sizes &l, Kind kind) {
     const int products = kind == TWO ? 2 : 1, sms = num_sms() > 0 ? num_sms() : 152;
     float best = 1e30f;
     for (int cluster = 1; cluster <= 8; cluster *= 2)
-        for (int most = 1 << 20; most >= 4; most = most > 256 ? 256 : most * 3 / 4) {  // blocks of 64 of a share
+        // blocks of 64 of a share (where none is split: one round)
+        for (int most = 1 << 20; most >= 4 && (cluster > 1 || most > 256); most = most > 256 ? 256 : most * 3 / 4) {
             int64_t clusters = 0;
             int longest = 0;
             for (int k = 0; k < l.count; ++k) {
@@ -1369,7 +1370,7 @@ static float shares(Mat *table, Sizes &l, Kind kind) {
                 longest = std::max(longest, (kbs + split - 1) / split);
             }
             // (the share of the SMs that clusters of 4 and 8 can take)
-            const int64_t places = (int)(sms * (cluster == 8 ? 0.948f : cluster == 4 ? 0.974f : 1.0f)) / cluster, waves = (clusters * products + places - 1) / places;
+            const int64_t places = std::max(1, (int)(sms * (cluster == 8 ? 0.948f : cluster == 4 ? 0.974f : 1.0f)) / cluster), waves = (clusters * products + places - 1) / places;
             const float time = waves * (0.55f * longest + 4.5f + (cluster > 1 ? 3.5f : 0.0f));
             if (time < best * 0.999f) {
                 best = time;
@@ -1389,8 +1390,8 @@ static float shares(Mat *table, Sizes &l, Kind kind) {
     return best;
 }
 
-// Fills a launch's list from matrix k on; returns the next launch's first, and the workspace that it takes.  base null: the
-// sizes alone.
+// Fills a launch's list from matrix k on; returns the next launch's first, and the workspace that it takes.  base null: that
+// alone, without a plan of the levels.
 static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *mom, const minw_matrix *out, int k, int count,
                 uint8_t *base, int64_t *need, bool joined) {
     l.count = l.full = l.pair_tri = l.pair_full = 0;
@@ -1423,6 +1424,8 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
         m.small = m.x1 + x;
         used += matrix_bytes(m.rows, m.cols);
     }
+    *need = used;
+    if (!base) return k;
     int small_k = 0, long_k = 0;
     for (int e = 0; e < l.count; ++e) {
         small_k = std::max(small_k, 2 * table[e].mb());
@@ -1435,7 +1438,6 @@ static int fill(Mat *table, Sizes &l, const minw_matrix *g, const minw_matrix *m
     const float of_x = shares(table, l, OF_X), one = shares(table, l, ONE), two = shares(table, l, TWO);
     l.pairs = 2 * pairs(l.pair_tri, long_k) + 12 * pairs(l.pair_tri, small_k) + pairs(2 * (int64_t)l.pair_tri, small_k) < 2 * of_x + 12 * one + two;
     l.pairs_x = pairs(l.pair_full, small_k) < (l.full + sms - 1) / sms * (0.62f * small_k + 5.0f);
-    *need = used;
     return k;
 }
 
@@ -1644,10 +1646,11 @@ size_t minw_orthogonal_workspace_bytes(const minw_matrix *grads, int32_t count) 
         return 0;
     orth::Table<orth::CAP> table;
     orth::Sizes l;
+    const bool joined = orth::join(grads, count);
     int64_t most = 16;
     for (int k = 0; k < count;) {
         int64_t need;
-        k = orth::fill(table.m, l, grads, nullptr, nullptr, k, count, nullptr, &need, orth::join(grads, count));
+        k = orth::fill(table.m, l, grads, nullptr, nullptr, k, count, nullptr, &need, joined);
         most = std::max(most, need);
     }
     return (size_t)most;
