@@ -779,8 +779,11 @@ MINW_API minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, i
 /* minw_w4_matvec with adapters: the base is the product with the w4 weights,
  *   y[t] = act(fmaf(acc[t] + alpha[u] up[u]^T (down[u] x[t]), scale, shift))
  * The weights are read once for up to 32 bf16 or 10 fp32 vectors.  Workspace
- * (backward = 0), ids and adapters as minw_adapters, the rest as
- * minw_w4_matvec. */
+ * as minw_adapters (backward = 0; 4 O bytes for each row up to the 32nd are enough),
+ * ids and adapters as there, the rest as minw_w4_matvec.  Long prompts
+ * read the weights again for every 32 rows; from about 128 rows on, a product
+ * with bf16 weights as minw_adapters' base costs less (4096 -> 4096, 512 rows:
+ * 58 us for 267). */
 MINW_API minw_status minw_w4_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, const uint8_t *codes,
                                       const uint16_t *scales, int32_t O, int32_t K, int32_t group, const int32_t *ids,
                                       const void *down, const void *up, int32_t p_type, int32_t n, int32_t r,

@@ -822,6 +822,7 @@ static int rows_of(int r, bool bf16) { return r <= 32 || (r <= 64 && bf16) ? 64 
 static int rank_pitch(int r) { return (r + 15) / 16 * 16; }
 
 constexpr int W4_ROWS = 32;                  // rows of w4 products at a time
+static int64_t w4_bytes(int64_t T, int O) { return std::min<int64_t>(T, W4_ROWS) * O * 4; }       // their adapters' terms
 
 static int64_t tiles_of(int64_t T, int n, int most) { return std::min<int64_t>(T, T / most + std::min<int64_t>(T, (int64_t)n + 1)); }
 
@@ -971,11 +972,13 @@ size_t minw_adapters_workspace_bytes(int64_t T, int32_t K, int32_t O, int32_t n,
     using namespace adapters;
     const Shape z{T, K, O, n, r};
     if (T < 0 || K < 1 || O < 1 || n < 1 || r < 1 || !sizes_fit(z)) return 0;
+    const int64_t terms = w4_bytes(T, O);
+    if (!backward && T <= SMALL) return (size_t)std::max<int64_t>(16, terms);        // no plan (which grows with n)
     int64_t used;
     plan_at(nullptr, T, n, r, &used);
     used += 3 * T * rank_pitch(r) * 2;
     if (backward) return (size_t)(used + 3 * T * rank_pitch(r) * 2);
-    return (size_t)std::max<int64_t>(used, std::min<int64_t>(T, W4_ROWS) * O * 4);
+    return (size_t)std::max<int64_t>(used, terms);
 }
 
 minw_status minw_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t T, int32_t K, const int32_t *ids,
@@ -1023,7 +1026,7 @@ minw_status minw_w4_adapters(const void *x, int32_t x_type, int64_t ldx, int64_t
     if (ok != MINW_OK) return ok;
     if (!sizes_fit(Shape{T, K, O, n, r})) return MINW_EUNSUPPORTED;
     if (T == 0) return MINW_OK;
-    if (!workspace || !aligned16(workspace) || workspace_bytes < minw_adapters_workspace_bytes(T, K, O, n, r, 0)) return MINW_EINVAL;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < (size_t)w4_bytes(T, O)) return MINW_EINVAL;
     const int xs = x_type == MINW_BF16 ? 2 : 4, ys = y_type == MINW_BF16 ? 2 : 4;
     // the products of so many rows read the weights once (bf16 x); their adapters' terms go through the workspace
     for (int64_t t0 = 0; t0 < T; t0 += W4_ROWS) {
