@@ -672,9 +672,10 @@ typedef struct {
  * from about 1e-3 |g|_F up lie between 0.68 and 1.21.
  * Products run on two-part fp16 operands (22 bits) with fp32 sums.  Against
  * the formula in 64 bits, relative to the result's Frobenius norm: within
- * 1e-4 for each three steps begun (five, as measured: 1e-5 at most, and no more than
- * 3 times what plain fp32 products are off plus 1e-6), and one
- * rounding to nearest even for bf16 outputs.  The norm
+ * 1e-4 for each three steps begun; five, as measured, are 1e-6 to 9e-6 off
+ * where plain fp32 products are 5e-7 to 7e-6 off (about as much, but 2e-6 to 4e-6
+ * where the shorter side is 128 at most, beside larger matrices also 64 at most,
+ * for 1e-6); and one rounding to nearest even for bf16 outputs.  The norm
  * is right wherever its square is an fp64 number.  A matrix of zeros gives
  * zeros; one with an infinity or a NaN gives NaN everywhere and changes no
  * other's result.  The same bits on every call.
