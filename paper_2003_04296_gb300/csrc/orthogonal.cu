@@ -23,8 +23,8 @@
 // Against the formula in 64 bits (Frobenius; plain fp32 products in parentheses), noise / a gradient of few strong
 // directions: 128 x 1152 1.8e-6 / 1.8e-6 (1.2e-6 / 1.2e-6), 1024 x 8192 2.6e-6 / 1.2e-6 (3.9e-6 / 3.5e-6),
 // 4096 x 4096 2.2e-6 / 1.4e-6 (4.8e-6 / 6.6e-6).  Without all this but the stages, sums of 128 of K:
-// 8.7e-6 / 1.0e-5, 7.1e-6 / 5.4e-6 and 6.0e-6 / 5.0e-6, at 116 us instead of 130, 318 instead of 346,
-// 2.77 ms instead of 2.93.
+// 8.7e-6 / 1.0e-5, 7.1e-6 / 5.4e-6 and 6.0e-6 / 5.0e-6, at 116 us instead of 126, 318 instead of 336,
+// 2.77 ms instead of 2.89.
 //
 // The scales are powers of two that the mathematics gives: a matrix of Frobenius norm
 // f in [1/2, 1) 2^e enters as X 2^(15 - e), so that nothing overflows and the smallest
@@ -42,7 +42,7 @@
 // for 64 of K, 0.55 to 0.67 us a tile of 128 x 128, of which the tensor cores need 0.4), so
 // pairs of blocks take 256 x 256; where they are few, latency (2.5 us between two launches, 4.5 for a
 // tile's start and end), so clusters split K.  4096 x 4096 of bf16 2.8 to 2.9 ms (1.4 of the 1.88
-// PFLOP/s that a library's bf16 product reaches), 1024 x 8192 of fp32 346 us, 128 x 1152 130, 10 x 1024 11.
+// PFLOP/s that a library's bf16 product reaches), 1024 x 8192 of fp32 336 us, 128 x 1152 126, 10 x 1024 11.
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -477,8 +477,8 @@ __device__ __forceinline__ void load32(uint32_t addr, uint32_t *w) {
           "=r"(w[29]), "=r"(w[30]), "=r"(w[31])
         : "r"(addr));
 }
-// sum += 64 columns.
-__device__ __forceinline__ void add64(uint32_t addr, float *sum) {
+// sum += 64 columns, two an instruction.
+__device__ __forceinline__ void add64(uint32_t addr, Pair *sum) {
     uint32_t w[64];
     load32(addr, w);
     load32(addr + 32, w + 32);
@@ -487,14 +487,14 @@ __device__ __forceinline__ void add64(uint32_t addr, float *sum) {
 #pragma unroll
     for (int k = 0; k < 64; ++k) asm volatile("" : "+r"(w[k]));
 #pragma unroll
-    for (int k = 0; k < 64; ++k) sum[k] += __uint_as_float(w[k]);
+    for (int k = 0; k < 32; ++k) sum[k] = add2(sum[k], pair(__uint_as_float(w[2 * k]), __uint_as_float(w[2 * k + 1])));
 }
 
 // PAIR: four tiles by a cluster of two blocks, 256 x 256 sums, whose products read 64 KB a block for 64 of K where four blocks
 // by themselves read as much each: it is the way from L2 that products wait for.  Two sums of 256 columns fill the tensor memory;
-// registers take them over after 64 of K: 4096 x 4096 in 2.92 ms, after 32 in 3.02, after 128 in 2.88 at 1.4 times the error (noise).
-// A tile for itself has four sums of 128 columns, each of 32 of K: 512 x 512 in 192 us, of 64 in 176 at 1.15 times the error, and wide
-// matrices of noise at 1.5 to 1.7 times it.
+// registers take them over after 64 of K: 4096 x 4096 in 2.89 ms, after 32 1.03 times that, after 128 0.99 times at 1.4 times the error (noise).
+// A tile for itself has four sums of 128 columns, each of 32 of K: 512 x 512 in 186 us (a value at a time instead of two 192); of
+// 64 in 0.92 times that at 1.15 times the error, wide matrices of noise at 1.5 to 1.7 times it.
 // N: matrices whose descriptions come with the launch, so that a block knows its work before it waits for the kernel before; 0:
 // they are read from the workspace, after that wait (what an earlier kernel wrote is there for certain only then).
 template <bool PAIR, int N>
@@ -787,11 +787,11 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
     }
     __syncwarp();
     // The sums from tensor memory into registers, a chunk at a time; zero where this share of K is empty.
-    float sum[MINE];
+    Pair sum[MINE / 2];
     const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)((warp >> 2) * MINE);
     if (warp < THREADS / 32) {
 #pragma unroll
-        for (int k = 0; k < MINE; ++k) sum[k] = 0.0f;
+        for (int k = 0; k < MINE / 2; ++k) sum[k] = pair(0.0f, 0.0f);
         const int sums = (kb1 - kb0) * (64 / SPAN);
         const int left = PAIR ? -2 : max((kb1 - kb0 - 2) * (64 / SPAN) - 1, -1);         // the sum after which the last stage is free (-1: at once)
         if (left == -1) fetch_later();
@@ -800,7 +800,7 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
             fence_after();
             if (e == left) fetch_later();
 #pragma unroll
-            for (int c = 0; c < MINE; c += 64) add64(mine + WIDTH * (e % SUMS) + c, sum + c);
+            for (int c = 0; c < MINE; c += 64) add64(mine + WIDTH * (e % SUMS) + c, sum + c / 2);
             fence_before();
             __syncwarp();
             if (lane == 0) {
@@ -819,7 +819,10 @@ __global__ void __launch_bounds__(THREADS + 64, 1) product_kernel(const __grid_c
         float *d = PAIR ? acc + ((warp >> 2) * T + r) * PITCH : acc + (rank * rows + r - owner * rows) * PITCH + (warp >> 2) * 64;
         if (shares > 1) d = cluster.map_shared_rank(d, in_cluster - rank + owner);
 #pragma unroll
-        for (int k = 0; k < MINE; k += 4) *reinterpret_cast<float4 *>(d + k) = make_float4(sum[k], sum[k + 1], sum[k + 2], sum[k + 3]);
+        for (int k = 0; k < MINE; k += 4) {
+            const float2 lower = halves(sum[k / 2]), upper = halves(sum[k / 2 + 1]);
+            *reinterpret_cast<float4 *>(d + k) = make_float4(lower.x, lower.y, upper.x, upper.y);
+        }
     }
     if (split > 1 && !PAIR) cluster.sync();
     else __syncthreads();
@@ -1336,7 +1339,7 @@ static bool is_small(const minw_matrix &g) {
 }
 
 // Whether those go with the large matrices of their list instead: where the launches for these have blocks to spare, that takes
-// no time of its own (the ConvNet's list with its classifier and first layer 619 us, 656 in a launch of their own), at 2e-6 to 4e-6 off
+// no time of its own (the ConvNet's list with its classifier and first layer 591 us, 37 more in a launch of their own), at 2e-6 to 4e-6 off
 // the formula instead of 1e-6.
 static bool join(const minw_matrix *g, int count) {
     const int sms = num_sms() > 0 ? num_sms() : 152;
