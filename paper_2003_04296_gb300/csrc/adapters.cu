@@ -14,7 +14,8 @@
 //
 // Few operations a value (2 r, r <= 64 as a rule) and short kernels: latency bounds them, and the way of
 // instructions that run once.  4096 bf16 rows of 8 users, 4096 -> 4096 at rank 64, 64 us (108 MB: 16 us at the copy rate);
-// the backward of 2048 at rank 32, 56.  The products run on mma.sync (bf16, fp32 sums) from registers:
+// the backward of 2048 at rank 32, 59.  The products run on mma.sync (bf16; sums over K and over rows in fp32, to nearest, of 32 and 16
+// terms each by the tensor cores, which truncate) from registers:
 // - along K, the order of the values is free, as long as both operands have the same: a lane
 //   takes eight consecutive values of a row for two products of 16;
 // - along O (and along K in the gradients), lane g of a group of eight takes eight consecutive columns of

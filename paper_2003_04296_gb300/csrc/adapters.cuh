@@ -24,7 +24,7 @@ constexpr int SMALL = 64;                     // rows that need no plan
 // ---------------------------------------------------------------------------
 
 struct Tile {
-    int id, start, count, pad;               // user (-1: none), place of its first row in the sorted order
+    int id, start, count, pad;               // user (-1: none), place of its first row in the sorted order; pad: one load of 16 bytes
 };
 
 struct Plan {
