@@ -48,7 +48,7 @@ def _matrix(gen, m, n, kind):
 LISTS = [[(10, 1024)], [(16, 8192)], [(64, 300)], [(33, 3000)], [(100, 130)], [(130, 100)], [(128, 1152)], [(300, 200)], [(256, 2304)],
          [(512, 512)], [(512, 4608)], [(1001, 333)], [(1024, 1024)], [(1024, 8192)], [(2200, 2310)], [(600, 700)] * 12,
          [(2300, 2400), (300, 200), (100, 130), (512, 4608), (700, 1000), (1500, 1600)],
-         [(100 + 3 * k, 130 + 5 * k) for k in range(20)]]
+         [(100 + 3 * k, 130 + 5 * k) for k in range(20)], [(600, 700)] * 20]
 
 
 @pytest.mark.parametrize("shapes", LISTS, ids=lambda s: f"{len(s)}x{s[0][0]}x{s[0][1]}")
@@ -71,3 +71,20 @@ def test_as_near_as_fp32_products(M, shapes, kind, bf16):
             assert own <= 3 * plain + 1e-6, (tuple(x.shape), own, plain)
     finally:
         torch.backends.cuda.matmul.allow_tf32 = allowed
+
+
+@pytest.mark.parametrize("kind", ["batch", "noise"])
+@pytest.mark.parametrize("shapes", [[(10, 1024), (5, 49), (23, 5), (60, 3000), (1100, 1200), (127, 40)],
+                                    [(1200, 1300), (16, 300), (2, 7), (64, 64), (33, 500), (100, 90)]])
+def test_small_sides_beside_large_matrices(M, shapes, kind):
+    """They join the large ones: q X + R X then takes up to 41 times the result from values held in 22 bits and sums rounded to 24,
+    2.4 u together, 41 2.4 u = 6e-6 off where plain products have small matrices' few roundings."""
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(shapes, kind))
+    g = [_matrix(gen, m, n, kind) for m, n in shapes]
+    o = [torch.empty_like(x) for x in g]
+    M.minw_orthogonalize(g, o, torch.empty(M.minw_orthogonal_workspace_bytes(g), dtype=torch.uint8, device="cuda"))
+    for x, y in zip(g, o):
+        want = _ns(x.double())
+        scale = float(want.norm())
+        plain = float((_ns(x).double() - want).norm()) / scale
+        assert float((y.double() - want).norm()) / scale <= 3 * plain + 7e-6, tuple(x.shape)

@@ -111,3 +111,41 @@ def test_lists_of_other_matrices(M, count):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for g, o in zip(want, got) for a, b in zip(g, o))
     assert M.minw_get_last_device_error() == M.MINW_OK
+
+
+@pytest.mark.parametrize("shapes", [[(1100, 1300), (40, 90)], [(2300, 2400)], [(300, 400)] * 20])
+def test_two_lists_at_once(M, shapes):
+    """Two streams, a list and a workspace each, call after call: the same bits as alone."""
+    gen = torch.Generator(device="cuda").manual_seed(len(shapes))
+    lists = [[_rand(gen, m, n) for m, n in shapes] for _ in range(2)]
+    want, got = ([[torch.zeros_like(x) for x in g] for g in lists] for _ in range(2))
+    ws = [_scratch(M.minw_orthogonal_workspace_bytes(g), 255) for g in lists]
+    for g, o, w in zip(lists, want, ws):
+        M.minw_orthogonalize(g, o, w)
+        torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in lists]
+    held = [(M.MatrixList(g), M.MatrixList(o)) for g, o in zip(lists, got)]
+    for _ in range(4):
+        for (g, o), w, s in zip(held, ws, streams):
+            M.minw_orthogonalize(g, o, w, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, y in zip(want, got) for a, b in zip(x, y))
+    assert M.minw_get_last_device_error() == M.MINW_OK
+
+
+@pytest.mark.parametrize("T", [1, 64, 65, 100])
+def test_beside_4_bit_weights_the_least_workspace(M, T):
+    """4 O bytes for each row up to the 32nd; nothing behind them is written."""
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    K, O, n, r, group = 256, 130, 3, 8, 64
+    cs, ss = M.w4_shapes(O, K, group)
+    codes, scales = torch.empty(cs, dtype=torch.uint8, device="cuda"), torch.empty(ss, dtype=torch.bfloat16, device="cuda")
+    M.minw_pack_w4(_rand(gen, O, K) / 16, group, codes, scales)
+    down, up, x = _rand(gen, n, r, K) / 16, _rand(gen, n, r, O), _rand(gen, T, K)
+    ids = torch.randint(-1, n, (T,), generator=gen, device="cuda").to(torch.int32)
+    need = 4 * O * min(T, 32)
+    buf = _scratch(need + 4096, 77)
+    want, got = torch.empty(T, O, device="cuda"), torch.empty(T, O, device="cuda")
+    M.minw_w4_adapters(x, codes, scales, group, ids, down, up, want, workspace=_scratch(1 << 20, 0))
+    M.minw_w4_adapters(x, codes, scales, group, ids, down, up, got, workspace=buf[:need])
+    assert torch.equal(want, got) and (buf[need:] == 77).all()
